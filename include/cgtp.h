@@ -72,6 +72,7 @@ extern "C" {
 /* dtypes */
 #define CGTP_F32 0
 #define CGTP_F64 1
+#define CGTP_BF16 2 /* row operators and AdamW gradients only */
 
 /* plan flags */
 #define CGTP_VALIDATE_CSR 1u   /* copy the CSR to the host and check it before launching */
@@ -375,6 +376,129 @@ int cgtp_gather_probe(cgtp_plan plan, int64_t n_nodes, int64_t n_edges, const in
 int cgtp_receiver_order(int64_t n_nodes, int64_t n_edges, const int32_t *row_ptr,
                         const int32_t *col, const float *edge_vec, int32_t *order);
 int cgtp_plan_set_receiver_order(cgtp_plan plan, int64_t n_nodes, const int32_t *order);
+
+/* Row operators: the learned linear maps beside the products above. A radial network turns the
+ * basis values of an edge into the edge_radial [E][C][L] of cgtp_message_pass, and a node's
+ * scalars are mixed, with weights that depend on the row's group: the chemical element of the
+ * node, the pair of elements of the edge, or the request whose fine-tune the structure is
+ * evaluated with. They need no plan. Conventions beyond those at the top of this file:
+ *  - dtype is CGTP_F32 or CGTP_BF16 for every tensor of values, unless noted. Sums are held in fp32
+ *    and rounded once, to the output's type.
+ *  - x, y, dx, dy are rows: element (i, c) at [i * stride + c], stride >= width. Other tensors are
+ *    contiguous. Any width, stride and alignment of the element works; widths and strides that
+ *    are multiples of 16 bytes with pointers on 16-byte boundaries are the fastest.
+ *  - 0 <= n_rows < 2^31, 1 <= n_groups <= CGTP_MAX_GROUPS, widths 1 .. CGTP_MAX_WIDTH.
+ *  - Outputs must not overlap inputs or each other. They are fully overwritten. Results do not
+ *    depend on how the work is spread over the GPU: the same inputs give the same bits.
+ *  - The caller passes the workspace, of the bytes that the query beside the call gives, on a
+ *    256-byte boundary; it may be NULL where the query gives 0.
+ *  - offsets and order are device arrays as cgtp_group_rows makes them. Group g owns the rows
+ *    order[offsets[g]] .. order[offsets[g + 1] - 1]; the rows order[offsets[n_groups]] .. belong
+ *    to none. order NULL: the rows are sorted already (order[p] = p). They are not validated
+ *    beyond bounds: offsets are clamped to [0, n_rows], and entries of order outside
+ *    [0, n_rows) are skipped. */
+#define CGTP_MAX_GROUPS 4096
+#define CGTP_MAX_WIDTH 65536
+#define CGTP_MAX_ADAPTER_RANK 64
+
+/* Order rows by group: a stable counting sort of the group ids.
+ *   ids     [n_rows] int32; a row whose id is outside [0, n_groups) belongs to no group.
+ *   offsets [n_groups + 1] int32, order [n_rows] int32: outputs. Rows of one group, and the rows
+ *           of none after them, keep their order.
+ * Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
+int cgtp_group_rows_bytes(int64_t n_rows, int n_groups, size_t *bytes);
+int cgtp_group_rows(int64_t n_rows, int n_groups, const int32_t *ids, int32_t *offsets,
+                    int32_t *order, void *workspace, size_t ws_bytes, void *stream);
+
+/* Products grouped by row: y_i = w[g(i)]^T x_i, y_i = 0 for a row of no group.
+ *   x [n_rows][n_in], w [n_groups][n_in][n_out], y [n_rows][n_out].
+ * Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
+int cgtp_grouped_linear(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                        const int32_t *offsets, const int32_t *order, const void *x,
+                        int64_t x_stride, const void *w, void *y, int64_t y_stride, void *stream);
+
+/* Its gradients, from dy [n_rows][n_out]:
+ *   dx_i  = w[g(i)] dy_i                 [n_rows][n_in], 0 for a row of no group;
+ *   dw[g] = sum over its rows x_i dy_i^T [n_groups][n_in][n_out], 0 for a group without rows.
+ * Either may be NULL (not both); x is needed for dw alone, w for dx alone. The sums over rows run
+ * in a fixed order. Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
+int cgtp_grouped_linear_grad_bytes(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                                   size_t *bytes);
+int cgtp_grouped_linear_grad(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                             const int32_t *offsets, const int32_t *order, const void *x,
+                             int64_t x_stride, const void *w, const void *dy, int64_t dy_stride,
+                             void *dx, int64_t dx_stride, void *dw, void *workspace,
+                             size_t ws_bytes, void *stream);
+
+/* A projection shared by all rows with a low-rank adapter of each row's group:
+ *   y_i = w^T x_i + scale[g] b[g]^T (a[g]^T x_i), g = g(i); y_i = w^T x_i for a row of no group.
+ *   w [n_in][n_out], a [n_groups][n_in][rank], b [n_groups][rank][n_out],
+ *   scale [n_groups] fp32 or NULL (all 1); 1 <= rank <= CGTP_MAX_ADAPTER_RANK.
+ * a[g]^T x_i is kept between the two products in fp32 or, for CGTP_BF16, in two bf16 parts (16
+ * bits of significand). Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
+int cgtp_adapter_linear_bytes(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                              int rank, size_t *bytes);
+int cgtp_adapter_linear(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out, int rank,
+                        const int32_t *offsets, const int32_t *order, const void *x,
+                        int64_t x_stride, const void *w, const void *a, const void *b,
+                        const float *scale, void *y, int64_t y_stride, void *workspace,
+                        size_t ws_bytes, void *stream);
+
+/* Its gradients with respect to the rows and the adapters (the shared projection is frozen):
+ *   u_i   = scale[g] b[g] dy_i,  dx_i = w dy_i + a[g] u_i  (w dy_i for a row of no group);
+ *   da[g] = sum over its rows x_i u_i^T;
+ *   db[g] = scale[g] sum over its rows (a[g]^T x_i) dy_i^T.
+ * dx [n_rows][n_in], da and db as a and b, 0 for a group without rows; any of the three may be NULL
+ * (not all). All inputs are required. Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
+int cgtp_adapter_linear_grad_bytes(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                                   int rank, size_t *bytes);
+int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                             int rank, const int32_t *offsets, const int32_t *order,
+                             const void *x, int64_t x_stride, const void *w, const void *a,
+                             const void *b, const float *scale, const void *dy,
+                             int64_t dy_stride, void *dx, int64_t dx_stride, void *da, void *db,
+                             void *workspace, size_t ws_bytes, void *stream);
+
+/* AdamW over many tensors in one launch. For every element, in fp32 with each operation rounded
+ * (no fused multiply-add), g = grad * grad_scale[0]:
+ *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2,
+ *   p' = p (1 - lr weight_decay) - (lr / c1) m' / (sqrt(v' / c2) + eps),
+ *   c1 = 1 - beta1^step, c2 = 1 - beta2^step, step counting from 1.
+ * state_bits 32: m, v fp32. state_bits 8: blocks of CGTP_ADAMW_BLOCK consecutive elements of a
+ * tensor (the last one may be short) share the scales m_scale = max |m'|, v_scale = max v';
+ *   m is int8,  standing for m_scale (m/127) |m/127|,  m = +-round(127 sqrt(|m'| / m_scale));
+ *   v is uint8, standing for v_scale (v/255)^4, v = round(255 (v' / v_scale)^(1/4)), at least 1
+ *     where v' > 0, so that no element that has seen a gradient is divided by eps alone.
+ * The step itself uses the unrounded m' and v'. States start at zero (codes and scales). A
+ * gradient that is not finite spoils its element (state_bits 32) or the states of its block (8).
+ *
+ * cgtp_adamw_create takes the addresses once (HOST array, copied to a table on the current
+ * device, which the handle owns); the tensors stay the caller's and must outlive the handle's use.
+ * A handle serves one host thread and one stream at a time. */
+#define CGTP_ADAMW_BLOCK 256
+typedef struct cgtp_adamw_s *cgtp_adamw;
+typedef struct {
+    float *param;       /* updated in place */
+    const void *grad;   /* CGTP_F32 or CGTP_BF16, as given to cgtp_adamw_create */
+    void *m, *v;        /* first and second moments, updated in place */
+    float *m_scale, *v_scale; /* state_bits 8: one per block of elements; else ignored */
+    void *copy;         /* bf16 copy of the updated parameters, or NULL */
+    int64_t n;          /* elements, >= 0 */
+} cgtp_adamw_tensor;
+
+/* Errors: CGTP_ERR_ARG, CGTP_ERR_UNSUPPORTED (2^31 blocks or more), CGTP_ERR_HIP. */
+int cgtp_adamw_create(int n_tensors, const cgtp_adamw_tensor *tensors, int grad_dtype,
+                      int state_bits, cgtp_adamw *handle);
+/* One step. grad_scale: device float, or NULL (1). 0 <= beta < 1, eps >= 0, step >= 1.
+ * Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
+int cgtp_adamw_step(cgtp_adamw handle, double lr, double beta1, double beta2, double eps,
+                    double weight_decay, int64_t step, const float *grad_scale, void *stream);
+/* The values that 8-bit states stand for (to save them, or to go on in 32 bits): m_out and v_out
+ * are HOST arrays of one device pointer per tensor, [n] fp32 each.
+ * Errors: CGTP_ERR_ARG (also for 32-bit states), CGTP_ERR_HIP. */
+int cgtp_adamw_states(cgtp_adamw handle, float *const *m_out, float *const *v_out, void *stream);
+/* Synchronises the device; NULL is a no-op. */
+int cgtp_adamw_destroy(cgtp_adamw handle);
 
 /* Release the plan and everything it owns. Synchronises the device first.
  * cgtp_destroy(NULL) is a no-op. */

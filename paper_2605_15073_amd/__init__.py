@@ -24,6 +24,7 @@ CGTP_ERR_HIP = -4
 CGTP_ERR_UNSUPPORTED = -5
 CGTP_F32 = 0
 CGTP_F64 = 1
+CGTP_BF16 = 2
 CGTP_VALIDATE_CSR = 1
 CGTP_EDGE_SEPARATED = 2
 CGTP_TIME_STAGES = 4
@@ -36,6 +37,10 @@ CGTP_OP_MESSAGE_PASS_FIELDS = 5
 CGTP_OP_ONSITE_NBODY = 6
 CGTP_MAX_NU = 8
 CGTP_MAX_LMAX = 24
+CGTP_MAX_GROUPS = 4096
+CGTP_MAX_WIDTH = 65536
+CGTP_MAX_ADAPTER_RANK = 64
+CGTP_ADAMW_BLOCK = 256
 
 EXPORTED = ("cgtp_plan_create", "cgtp_plan_grid", "cgtp_workspace_bytes", "cgtp_onsite",
             "cgtp_message_pass", "cgtp_message_pass_two_slot", "cgtp_workspace_bytes_general",
@@ -43,7 +48,11 @@ EXPORTED = ("cgtp_plan_create", "cgtp_plan_grid", "cgtp_workspace_bytes", "cgtp_
             "cgtp_workspace_bytes_nbody", "cgtp_onsite_nbody", "cgtp_stage_times",
             "cgtp_destroy", "cgtp_status_string", "cgtp_last_error", "cgtp_host_tables",
             "cgtp_onsite_noalloc", "cgtp_gather_probe", "cgtp_receiver_order",
-            "cgtp_plan_set_receiver_order")
+            "cgtp_plan_set_receiver_order", "cgtp_group_rows_bytes", "cgtp_group_rows",
+            "cgtp_grouped_linear", "cgtp_grouped_linear_grad_bytes", "cgtp_grouped_linear_grad",
+            "cgtp_adapter_linear_bytes", "cgtp_adapter_linear", "cgtp_adapter_linear_grad_bytes",
+            "cgtp_adapter_linear_grad", "cgtp_adamw_create", "cgtp_adamw_step",
+            "cgtp_adamw_states", "cgtp_adamw_destroy")
 CGTP_NOALLOC_SCRATCH_BYTES = 64 << 20
 ONSITE_STAGES = ("contract_operands", "grid_product_curl_analysis", "project")
 ONSITE_GENERAL_STAGES = ("contract_a", "contract_b", "grid_product_curl_analysis",
@@ -63,6 +72,11 @@ class _Desc(ctypes.Structure):
     _fields_ = [("lmax", ctypes.c_int), ("channels", ctypes.c_int), ("rank", ctypes.c_int),
                 ("n_theta", ctypes.c_int), ("n_phi", ctypes.c_int), ("dtype", ctypes.c_int),
                 ("flags", ctypes.c_uint)]
+
+
+class _AdamWTensor(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("param", "grad", "m", "v", "m_scale", "v_scale",
+                                                "copy")] + [("n", ctypes.c_int64)])
 
 
 _lib = None
@@ -105,11 +119,31 @@ def load_library(path: str = LIB_PATH):
     lib.cgtp_host_tables.argtypes = [i32, i32, i32] + [vp] * 5
     lib.cgtp_receiver_order.argtypes = [i64, i64, vp, vp, vp, vp]
     lib.cgtp_plan_set_receiver_order.argtypes = [vp, i64, vp]
+    f64, szp = ctypes.c_double, ctypes.POINTER(sz)
+    lib.cgtp_group_rows_bytes.argtypes = [i64, i32, szp]
+    lib.cgtp_group_rows.argtypes = [i64, i32] + [vp] * 4 + [sz, vp]
+    rows = [i32, i64, i32, i32, i32]              # dtype, n_rows, n_groups, n_in, n_out
+    lib.cgtp_grouped_linear.argtypes = rows + [vp] * 3 + [i64, vp, vp, i64, vp]
+    lib.cgtp_grouped_linear_grad_bytes.argtypes = rows + [szp]
+    lib.cgtp_grouped_linear_grad.argtypes = (rows + [vp] * 3 + [i64, vp, vp, i64, vp, i64, vp, vp]
+                                             + [sz, vp])
+    lib.cgtp_adapter_linear_bytes.argtypes = rows + [i32, szp]
+    lib.cgtp_adapter_linear.argtypes = (rows + [i32] + [vp] * 3 + [i64] + [vp] * 5 + [i64, vp]
+                                        + [sz, vp])
+    lib.cgtp_adapter_linear_grad_bytes.argtypes = rows + [i32, szp]
+    lib.cgtp_adapter_linear_grad.argtypes = (rows + [i32] + [vp] * 3 + [i64] + [vp] * 5
+                                             + [i64, vp, i64] + [vp] * 3 + [sz, vp])
+    lib.cgtp_adamw_create.argtypes = [i32, ctypes.POINTER(_AdamWTensor), i32, i32,
+                                      ctypes.POINTER(vp)]
+    lib.cgtp_adamw_step.argtypes = [vp] + [f64] * 5 + [i64, vp, vp]
+    lib.cgtp_adamw_states.argtypes = [vp] * 4
+    lib.cgtp_adamw_destroy.argtypes = [vp]
     for name in ("cgtp_plan_create", "cgtp_plan_grid", "cgtp_workspace_bytes", "cgtp_onsite",
                  "cgtp_onsite_noalloc", "cgtp_gather_probe",
                  "cgtp_message_pass", "cgtp_message_pass_two_slot", "cgtp_stage_times",
                  "cgtp_destroy", "cgtp_host_tables", "cgtp_receiver_order",
-                 "cgtp_plan_set_receiver_order"):
+                 "cgtp_plan_set_receiver_order", *(n for n in EXPORTED if n.startswith(
+                     ("cgtp_group", "cgtp_adapter", "cgtp_adamw")))):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -549,3 +583,303 @@ def host_tables(lmax: int, n_theta: int = 0, n_phi: int = 0):
     args = [ctypes.c_void_p(a.ctypes.data) for a in (x, w, p, dp, q)]
     _check(lib.cgtp_host_tables(lmax, n_theta, n_phi, *args), "cgtp_host_tables")
     return x, w, p, dp, q
+
+
+# ---------------------------------------------------------------- row operators
+
+def _row_dtype(name, t):
+    torch = _torch()
+    if t.dtype == torch.float32:
+        return CGTP_F32
+    if t.dtype == torch.bfloat16:
+        return CGTP_BF16
+    raise ValueError(f"{name}: expected float32 or bfloat16, got {t.dtype}")
+
+
+def _want_rows(name, t, n, width, like):
+    """[n, width] rows on like's device, of like's type, contiguous along the width; returns the
+    row stride."""
+    if (t.dim() != 2 or tuple(t.shape) != (n, width) or t.dtype != like.dtype
+            or t.device != like.device or not t.is_cuda
+            or (width > 1 and n > 0 and t.stride(1) != 1)
+            or (n > 1 and t.stride(0) < width)):
+        raise ValueError(f"{name}: expected {like.dtype} rows ({n}, {width}) on {like.device}, "
+                         f"contiguous along the width, got {t.dtype} {tuple(t.shape)} with strides "
+                         f"{t.stride()} on {t.device}")
+    return max(t.stride(0), width) if n > 1 else width
+
+
+def _want_dev(name, t, shape, dtype, like):
+    if (not t.is_cuda or t.device != like.device or t.dtype != dtype or not t.is_contiguous()
+            or tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected contiguous {dtype} tensor of shape {tuple(shape)} on "
+                         f"{like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _row_call(like, stream):
+    """(device guard, stream to run on, its handle) of a call on like's device."""
+    torch = _torch()
+    s = stream if stream is not None else torch.cuda.current_stream(like.device)
+    return torch.cuda.device(like.device), s, ctypes.c_void_p(s.cuda_stream)
+
+
+def _new(shape, dtype, like, s):
+    """A tensor for work on stream s, whose memory is not reused before that work is done."""
+    torch = _torch()
+    t = torch.empty(shape, dtype=dtype, device=like.device)
+    if t.numel() and s != torch.cuda.current_stream(like.device):
+        # the memory may have been freed by the current stream's pending work
+        s.wait_stream(torch.cuda.current_stream(like.device))
+        t.record_stream(s)
+    return t
+
+
+def _row_workspace(workspace, need, like, s):
+    torch = _torch()
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = _new((need,), torch.uint8, like, s)
+    elif not workspace.is_cuda or workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {like.device}")
+    return _ptr(workspace), workspace.numel() * workspace.element_size(), workspace
+
+
+def _bytes(name, *args):
+    out = ctypes.c_size_t()
+    _check(getattr(load_library(), name)(*args, ctypes.byref(out)), name)
+    return out.value
+
+
+def _want_order(offsets, order, n, G, like):
+    torch = _torch()
+    _want_dev("offsets", offsets, (G + 1,), torch.int32, like)
+    if order is not None:
+        _want_dev("order", order, (n,), torch.int32, like)
+
+
+def group_rows(ids, n_groups: int, offsets=None, order=None, workspace=None, stream=None):
+    """cgtp_group_rows: (offsets [n_groups + 1], order [n]) of the rows with group ids [n] (int32;
+    a row whose id is outside [0, n_groups) belongs to no group and comes last)."""
+    torch = _torch()
+    if ids.dim() != 1:
+        raise ValueError(f"ids: expected one dimension, got {tuple(ids.shape)}")
+    n = ids.shape[0]
+    _want_dev("ids", ids, (n,), torch.int32, ids)
+    need = _bytes("cgtp_group_rows_bytes", n, n_groups)
+    guard, s, handle = _row_call(ids, stream)
+    if offsets is None:
+        offsets = _new((n_groups + 1,), torch.int32, ids, s)
+    if order is None:
+        order = _new((n,), torch.int32, ids, s)
+    _want_order(offsets, order, n, n_groups, ids)
+    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, ids, s)
+    with guard:
+        _check(load_library().cgtp_group_rows(n, n_groups, _ptr(ids), _ptr(offsets), _ptr(order),
+                                              ws_ptr, ws_len, handle), "cgtp_group_rows")
+    return offsets, order
+
+
+def _linear_head(x, w, offsets, order, shared):
+    if x.dim() != 2 or w.dim() != (2 if shared else 3):
+        raise ValueError(f"x, w: expected 2 and {2 if shared else 3} dimensions, got "
+                         f"{tuple(x.shape)} and {tuple(w.shape)}")
+    n, (n_in, n_out) = x.shape[0], w.shape[-2:]
+    G = offsets.shape[0] - 1
+    _want_order(offsets, order, n, G, x)
+    _want_dev("w", w, (n_in, n_out) if shared else (G, n_in, n_out), x.dtype, x)
+    return _row_dtype("x", x), n, G, n_in, n_out, _want_rows("x", x, n, n_in, x)
+
+
+def grouped_linear(x, w, offsets, order=None, y=None, stream=None):
+    """cgtp_grouped_linear: y_i = w[g(i)]^T x_i (0 for a row of no group). x [n, n_in] and
+    y [n, n_out] rows (any row stride), w [G, n_in, n_out]; offsets, order from group_rows (order
+    None: the rows are sorted by group)."""
+    dt, n, G, n_in, n_out, xs = _linear_head(x, w, offsets, order, False)
+    guard, s, handle = _row_call(x, stream)
+    if y is None:
+        y = _new((n, n_out), x.dtype, x, s)
+    ys = _want_rows("y", y, n, n_out, x)
+    with guard:
+        _check(load_library().cgtp_grouped_linear(dt, n, G, n_in, n_out, _ptr(offsets), _ptr(order),
+                                                  _ptr(x), xs, _ptr(w), _ptr(y), ys, handle),
+               "cgtp_grouped_linear")
+    return y
+
+
+def _grad_out(name, out, shape, like, s, rows):
+    """An output of a gradient call: allocated if None, skipped if False; (tensor, row stride)."""
+    if out is False:
+        return None, 0
+    if out is None:
+        out = _new(shape, like.dtype, like, s)
+    if rows:
+        return out, _want_rows(name, out, *shape, like)
+    _want_dev(name, out, shape, like.dtype, like)
+    return out, 0
+
+
+def grouped_linear_grad(x, w, dy, offsets, order=None, dx=None, dw=None, workspace=None,
+                        stream=None):
+    """cgtp_grouped_linear_grad: (dx [n, n_in], dw [G, n_in, n_out]) from dy [n, n_out]; an output
+    given as False is skipped (None in its place)."""
+    dt, n, G, n_in, n_out, xs = _linear_head(x, w, offsets, order, False)
+    dys = _want_rows("dy", dy, n, n_out, x)
+    guard, s, handle = _row_call(x, stream)
+    dx, dxs = _grad_out("dx", dx, (n, n_in), x, s, True)
+    dw, _ = _grad_out("dw", dw, (G, n_in, n_out), x, s, False)
+    ws_ptr, ws_len, _keep = None, 0, None
+    if dw is not None:
+        need = _bytes("cgtp_grouped_linear_grad_bytes", dt, n, G, n_in, n_out)
+        ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, s)
+    with guard:
+        _check(load_library().cgtp_grouped_linear_grad(
+            dt, n, G, n_in, n_out, _ptr(offsets), _ptr(order), _ptr(x), xs, _ptr(w), _ptr(dy), dys,
+            _ptr(dx), dxs, _ptr(dw), ws_ptr, ws_len, handle), "cgtp_grouped_linear_grad")
+    return dx, dw
+
+
+def _adapter_head(x, w, a, b, offsets, order, scale):
+    head = _linear_head(x, w, offsets, order, True)
+    dt, n, G, n_in, n_out, xs = head
+    if a.dim() != 3:
+        raise ValueError(f"a: expected three dimensions, got {tuple(a.shape)}")
+    r = a.shape[2]
+    _want_dev("a", a, (G, n_in, r), x.dtype, x)
+    _want_dev("b", b, (G, r, n_out), x.dtype, x)
+    if scale is not None:
+        _want_dev("scale", scale, (G,), _torch().float32, x)
+    return head, r
+
+
+def adapter_linear(x, w, a, b, offsets, order=None, scale=None, y=None, workspace=None,
+                   stream=None):
+    """cgtp_adapter_linear: y_i = w^T x_i + scale[g] b[g]^T (a[g]^T x_i), g = g(i). x [n, n_in] and
+    y [n, n_out] rows, w [n_in, n_out] shared, a [G, n_in, r], b [G, r, n_out], scale [G] float32
+    or None (1)."""
+    (dt, n, G, n_in, n_out, xs), r = _adapter_head(x, w, a, b, offsets, order, scale)
+    guard, s, handle = _row_call(x, stream)
+    if y is None:
+        y = _new((n, n_out), x.dtype, x, s)
+    ys = _want_rows("y", y, n, n_out, x)
+    need = _bytes("cgtp_adapter_linear_bytes", dt, n, G, n_in, n_out, r)
+    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, s)
+    with guard:
+        _check(load_library().cgtp_adapter_linear(
+            dt, n, G, n_in, n_out, r, _ptr(offsets), _ptr(order), _ptr(x), xs, _ptr(w), _ptr(a),
+            _ptr(b), _ptr(scale), _ptr(y), ys, ws_ptr, ws_len, handle), "cgtp_adapter_linear")
+    return y
+
+
+def adapter_linear_grad(x, w, a, b, dy, offsets, order=None, scale=None, dx=None, da=None, db=None,
+                        workspace=None, stream=None):
+    """cgtp_adapter_linear_grad: (dx, da, db) from dy [n, n_out], the shared projection frozen; an
+    output given as False is skipped (None in its place)."""
+    (dt, n, G, n_in, n_out, xs), r = _adapter_head(x, w, a, b, offsets, order, scale)
+    dys = _want_rows("dy", dy, n, n_out, x)
+    guard, s, handle = _row_call(x, stream)
+    dx, dxs = _grad_out("dx", dx, (n, n_in), x, s, True)
+    da, _ = _grad_out("da", da, (G, n_in, r), x, s, False)
+    db, _ = _grad_out("db", db, (G, r, n_out), x, s, False)
+    need = _bytes("cgtp_adapter_linear_grad_bytes", dt, n, G, n_in, n_out, r)
+    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, s)
+    with guard:
+        _check(load_library().cgtp_adapter_linear_grad(
+            dt, n, G, n_in, n_out, r, _ptr(offsets), _ptr(order), _ptr(x), xs, _ptr(w), _ptr(a),
+            _ptr(b), _ptr(scale), _ptr(dy), dys, _ptr(dx), dxs, _ptr(da), _ptr(db), ws_ptr, ws_len,
+            handle), "cgtp_adapter_linear_grad")
+    return dx, da, db
+
+
+class AdamWTensors:
+    """Owns a cgtp_adamw handle over lists of device tensors, which it keeps alive: params (float32),
+    grads (all float32 or all bfloat16), the moments m and v (float32; or int8 and uint8 with the
+    float32 scales m_scale and v_scale, one per CGTP_ADAMW_BLOCK elements) and, if given, bfloat16
+    copies of the parameters that each step writes. All contiguous, on one device; grads are read
+    where they lie when a step runs."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
+        torch = _torch()
+        lists = [params, grads, m, v, m_scale, v_scale, copies]
+        n = len(params)
+        if n == 0 or any(x is not None and len(x) != n for x in lists):
+            raise ValueError("params, grads, m, v (, scales, copies): lists of one length >= 1")
+        if (m_scale is None) != (v_scale is None):
+            raise ValueError("m_scale and v_scale: both or neither")
+        bits = 32 if m_scale is None else 8
+        gdt = grads[0].dtype
+        self.state_bits, self.device = bits, params[0].device
+        code = _row_dtype("grads", grads[0])
+        table = (_AdamWTensor * n)()
+        for i in range(n):
+            k = params[i].numel()
+            shape, nb = params[i].shape, ((k + CGTP_ADAMW_BLOCK - 1) // CGTP_ADAMW_BLOCK,)
+            _want_dev(f"params[{i}]", params[i], shape, torch.float32, params[0])
+            _want_dev(f"grads[{i}]", grads[i], shape, gdt, params[0])
+            _want_dev(f"m[{i}]", m[i], shape, torch.float32 if bits == 32 else torch.int8, params[0])
+            _want_dev(f"v[{i}]", v[i], shape, torch.float32 if bits == 32 else torch.uint8,
+                      params[0])
+            row = dict(param=params[i], grad=grads[i], m=m[i], v=v[i])
+            if bits == 8:
+                _want_dev(f"m_scale[{i}]", m_scale[i], nb, torch.float32, params[0])
+                _want_dev(f"v_scale[{i}]", v_scale[i], nb, torch.float32, params[0])
+                row.update(m_scale=m_scale[i], v_scale=v_scale[i])
+            if copies is not None:
+                _want_dev(f"copies[{i}]", copies[i], shape, torch.bfloat16, params[0])
+                row.update(copy=copies[i])
+            for name, t in row.items():
+                setattr(table[i], name, t.data_ptr())
+            table[i].n = k
+        self._keep = [list(x) for x in lists if x is not None]
+        self.shapes = [p.shape for p in params]
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(load_library().cgtp_adamw_create(n, table, code, bits, ctypes.byref(h)),
+                   "cgtp_adamw_create")
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            with _torch().cuda.device(self.device):
+                _check(load_library().cgtp_adamw_destroy(self.handle), "cgtp_adamw_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def adamw(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+          eps: float = 1e-8, weight_decay: float = 0.01, grad_scale=None, stream=None) -> None:
+    """cgtp_adamw_step: update the tensors of the handle in place. step counts from 1; grad_scale: a
+    device float32 tensor of one element that multiplies every gradient (clipping), or None."""
+    first = tensors._keep[0][0]
+    if grad_scale is not None:
+        _want_dev("grad_scale", grad_scale, (1,), _torch().float32, first)
+    guard, _, handle = _row_call(first, stream)
+    with guard:
+        _check(load_library().cgtp_adamw_step(tensors.handle, lr, beta1, beta2, eps, weight_decay,
+                                              step, _ptr(grad_scale), handle), "cgtp_adamw_step")
+
+
+def adamw_states(tensors: AdamWTensors, m_out=None, v_out=None, stream=None):
+    """cgtp_adamw_states: the float32 values that 8-bit states stand for, as lists (m, v)."""
+    torch = _torch()
+    first = tensors._keep[0][0]
+    guard, s, handle = _row_call(first, stream)
+    outs = []
+    for name, given in (("m_out", m_out), ("v_out", v_out)):
+        if given is None:
+            given = [_new(shape, torch.float32, first, s) for shape in tensors.shapes]
+        if len(given) != len(tensors.shapes):
+            raise ValueError(f"{name}: expected {len(tensors.shapes)} tensors, got {len(given)}")
+        for i, (t, shape) in enumerate(zip(given, tensors.shapes)):
+            _want_dev(f"{name}[{i}]", t, shape, torch.float32, first)
+        outs.append(given)
+    arrays = [(ctypes.c_void_p * len(o))(*[t.data_ptr() for t in o]) for o in outs]
+    with guard:
+        _check(load_library().cgtp_adamw_states(tensors.handle, arrays[0], arrays[1], handle),
+               "cgtp_adamw_states")
+    return outs[0], outs[1]

@@ -11,9 +11,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libcgtp.so")
-SOURCES = ["plan.cpp", "tables.cpp", "order.cpp", "contract.hip", "contract_rows.hip", "kernels.hip", "onsite.hip", "receiver_mfma.hip",
+SOURCES = ["plan.cpp", "tables.cpp", "order.cpp", "rows.cpp", "contract.hip", "contract_rows.hip", "kernels.hip", "onsite.hip", "receiver_mfma.hip",
            "receiver_values.hip", "folded.hip",
-           "fourier_mfma.hip", "noalloc.hip"]
+           "fourier_mfma.hip", "noalloc.hip", "group_rows.hip", "rows_product.hip", "adamw.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Per-source flags. The receivers' matrix-core results feed vector ALU products at once:
 # accumulating them in VGPRs (not AccVGPRs) saves a copy per result element and registers.
