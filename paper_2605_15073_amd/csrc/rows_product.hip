@@ -1,130 +1,290 @@
-// Products of grouped rows (cgtp_grouped_linear, cgtp_adapter_linear and their gradients).
+// Products of grouped rows, out_i = in_i W_g, on the matrix cores (cgtp_grouped_linear, the row
+// gradients, the narrow products of adapters and the shared projection with them).
+//
+// A workgroup owns up to BM rows of one group (of any groups where W is shared) and runs over tiles
+// of BN columns of its share of the output, so that its input rows come from HBM once and from the
+// L2 for every further column tile; the weights of a group stay in the L2s. The loads of a step
+// (rows and weights, kStep deep) are in flight while the step before is multiplied.
+//
+// Adapters: after the steps over the shared W, a tile's sums go on over the adapters of its rows, one
+// segment of rows at a time, with the narrow product's result as input rows (zero outside the
+// segment) and the adapter's second matrix as weights: the epilogue is fused, and rows of many
+// adapters share the tile.
 #include "internal.h"
-#include "rows.h"
+#include "rows_tile.h"
 
 namespace cgtp {
 
 namespace {
 
-typedef __bf16 bf16_t;
+using namespace rows;
 
-template <typename T> __device__ __forceinline__ float to_f32(T v) { return (float)v; }
+constexpr int kMaxSegments = 128;  // at most one per row of a tile
 
-__device__ __forceinline__ int clamp_offset(int v, int64_t n)
+template <typename T, bool WNK, int BM, int BN, int WR, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits, bool v_vec)
 {
-    return v < 0 ? 0 : (int64_t)v > n ? (int)n : v;
-}
+    constexpr int U = kU<T>, BK = kStep<T>, P = kParts<T>;
+    constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
+    constexpr int kShift = BM == 128 ? 7 : BM == 64 ? 6 : 5;
+    static_assert(BM == 1 << kShift && TR >= 1 && TC >= 1, "tile");
+    constexpr int NR = BM * kGroups / kThreads;        // units of the rows a thread stages
+    constexpr int NC = BN * kGroups / kThreads;        // units of [N][K] weights
+    typedef typename Four<T>::t F;
+    __shared__ uint4_t s_cols[kGroups * (BN + 1)], s_rows[kGroups * (BM + 1)];
+    __shared__ int s_row[BM], s_seg_g[kMaxSegments], s_seg_at[kMaxSegments + 1], s_nseg;
 
-// Groups share the sequence of rows; a tile of R positions of one group has the index
-// offsets[g] / R + g + j: since floor((o + m) / R) + 1 >= floor(o / R) + ceil(m / R), the tiles of
-// different groups never meet, and no prefix sum of tile counts is needed. Group G holds the
-// rows of no group.
-struct Tile {
-    int g;          // G: no group; -1: none at this index
-    int64_t p0, p1; // positions
-};
-
-__device__ Tile find_tile(const RowOrder &o, int R, int64_t index)
-{
-    int lo = 0, hi = o.G;  // the last group whose first tile index is <= index
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if ((int64_t)clamp_offset(o.offsets[mid], o.n) / R + mid <= index) lo = mid;
-        else hi = mid - 1;
+    const bool shared_w = p.w_group == 0;
+    Tile t;
+    if (shared_w) {
+        t.p0 = (int64_t)blockIdx.x * BM;
+        t.p1 = t.p0 + BM < o.n ? t.p0 + BM : o.n;
+        t.g = 0;
+    } else {
+        t = find_tile(o, kShift, blockIdx.x);
+        if (t.g < 0 || t.p0 >= t.p1) return;
     }
-    const int64_t start = clamp_offset(o.offsets[lo], o.n);
-    const int64_t end = lo < o.G ? clamp_offset(o.offsets[lo + 1], o.n) : o.n;
-    const int64_t p0 = start + (index - (start / R + lo)) * R;
-    if (p0 >= end) return {-1, 0, 0};
-    return {lo, p0, p0 + R < end ? p0 + R : end};
-}
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rows = (int)(t.p1 - t.p0);
+    // this workgroup's column tiles
+    const int ctiles = (p.N + BN - 1) / BN;
+    const int ct0 = (int)((int64_t)ctiles * blockIdx.y / splits);
+    const int ct1 = (int)((int64_t)ctiles * (blockIdx.y + 1) / splits);
+    if (ct0 >= ct1) return;
 
-__device__ __forceinline__ int64_t row_at(const RowOrder &o, int64_t p)
-{
-    return o.order ? o.order[p] : p;
-}
-
-__device__ __forceinline__ bool row_ok(const RowOrder &o, int64_t row)
-{
-    return row >= 0 && row < o.n;
-}
-
-constexpr int kTileRows = 16;
-
-template <typename T>
-__global__ __launch_bounds__(256) void k_row_product(RowOrder o, RowProduct p)
-{
-    const Tile t = find_tile(o, kTileRows, blockIdx.x);
-    if (t.g < 0) return;
-    const int c = blockIdx.y * 64 + (threadIdx.x & 63);
-    if (c >= p.N) return;
-    const T *w = (const T *)p.w + (p.w_group ? (int64_t)(t.g < o.G ? t.g : 0) * p.w_group : 0);
-    const bool bare = t.g == o.G;
-    const float scale = p.narrow_scale && !bare ? p.narrow_scale[t.g] : 1.f;
-    for (int64_t pos = t.p0 + (threadIdx.x >> 6); pos < t.p1; pos += 4) {
-        const int64_t row = row_at(o, pos);
-        if (!row_ok(o, row)) continue;
-        float acc = 0.f;
-        if (!bare || !p.w_group) {
-            const T *in = (const T *)p.in + row * p.in_stride;
-            for (int k = 0; k < p.K; ++k)
-                acc += to_f32(in[k]) * to_f32(w[p.w_nk ? (int64_t)c * p.K + k : (int64_t)k * p.N + c]);
+    if (tid < BM) s_row[tid] = tid < rows ? row_at(o, t.p0 + tid) : -1;
+    if (!shared_w && t.g == o.G) {  // rows of no group
+        if (p.narrow) return;
+        __syncthreads();
+        T *const out = static_cast<T *>(p.out);
+        const int c0 = ct0 * BN, c1 = ct1 * BN < p.N ? ct1 * BN : p.N;
+        for (int r = wave; r < rows; r += 4) {
+            const int row = s_row[r];
+            if (row >= 0)
+                for (int c = c0 + lane; c < c1; c += 64) out[row * p.out_stride + c] = (T)0.f;
         }
-        if (p.h && !bare) {
-            const T *v = (const T *)p.v + (int64_t)t.g * p.r * p.N;
-            const float *h = (const float *)p.h + pos * p.r;
-            for (int k = 0; k < p.r; ++k)
-                acc += h[k] * to_f32(v[p.w_nk ? (int64_t)c * p.r + k : (int64_t)k * p.N + c]);
+        return;
+    }
+    if (shared_w && p.h) {  // the segments of rows that share an adapter
+        __shared__ int s_g[BM];
+        if (tid < BM) {
+            int lo = 0, hi = o.G;  // the last group that starts at or before this position
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (clamp_offset(o.offsets[mid], o.n) <= t.p0 + tid) lo = mid;
+                else hi = mid - 1;
+            }
+            s_g[tid] = tid < rows ? lo : o.G;
         }
-        if (p.narrow) ((float *)p.out)[pos * p.N + c] = acc * scale;
-        else ((T *)p.out)[row * p.out_stride + c] = (T)acc;
+        __syncthreads();
+        if (wave == 0) {
+            int n = 0;
+#pragma unroll
+            for (int b = 0; b < BM; b += 64) {
+                const int r = b + lane;
+                const bool in = r < BM;
+                const int g = in ? s_g[r] : o.G;
+                const bool first = in && g < o.G && (r == 0 || s_g[r - 1] != g);
+                const unsigned long long m = __ballot(first);
+                const int at = n + __popcll(m & ((1ull << lane) - 1));
+                if (first) {
+                    s_seg_g[at] = g;
+                    s_seg_at[at] = r;
+                }
+                n += __popcll(m);
+            }
+            if (lane == 0) s_nseg = n;
+        }
+        __syncthreads();
+        // where a segment ends: at the first row of another group
+        const int n = s_nseg;
+        if (tid < BM && s_g[tid] == o.G && (tid == 0 || s_g[tid - 1] != o.G)) s_seg_at[n] = tid;
+        if (tid == 0 && s_g[BM - 1] != o.G) s_seg_at[n] = BM;
+    }
+    __syncthreads();
+    const int nseg = shared_w && p.h ? __builtin_amdgcn_readfirstlane(s_nseg) : 0;
+
+    // the row units this thread stages: k-group tid % 8 of rows tid / 8 + 32 i
+    const int kg = tid & 7, rr = tid >> 3;
+    const T *in[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const int row = s_row[rr + 32 * i];
+        in[i] = row >= 0 ? static_cast<const T *>(p.in) + row * p.in_stride + kg * U : nullptr;
+    }
+    const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
+    const int W = narrow_width<T>(p.r);  // of a part of the narrow input
+
+    // transposed weights: columns 4 tc .. 4 tc + 3, k-group tg
+    const int tc = tid % (BN / 4), tg = tid / (BN / 4);
+
+    uint4_t xr[NR], wn[WNK ? NC : 1];
+    F wt[WNK ? 1 : U];
+    // the loads of step k of column tile ct; seg < 0: the shared weights, else an adapter
+    auto fetch = [&](int ct, int seg, int k) {
+        const int c0 = ct * BN;
+        int K = p.K;
+        const T *wb = w;
+        int wk = p.K;  // k of the weights from which on there are none
+        int kw = k;    // k in the weights
+        if (seg >= 0) {
+            K = P * W;
+            wb = static_cast<const T *>(p.v) + (int64_t)s_seg_g[seg] * p.r * p.N;
+            wk = p.r;
+            const int at = s_seg_at[seg], end = s_seg_at[seg + 1];
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const int r = rr + 32 * i;
+                const int left = r >= at && r < end && s_row[r] >= 0 ? K - k - kg * U : 0;
+                xr[i] = load_unit<T, true>(static_cast<const T *>(p.h) + (t.p0 + r) * K + k + kg * U, left);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) xr[i] = load_unit<T, VEC>(in[i] + k, in[i] ? K - k - kg * U : 0);
+        }
+        if constexpr (WNK) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const int c = c0 + rr + 32 * i;
+                int kk = kw + kg * U;
+                if (seg >= 0 && P == 2 && kk >= W) kk -= W;  // the second part meets the same weights
+                const T *const q = wb + (int64_t)c * wk + kk;
+                const int left = c < p.N && k + kg * U < K ? wk - kk : 0;
+                if (seg >= 0 && !v_vec) wn[i] = load_unit<T, false>(q, left);
+                else wn[i] = load_unit<T, VEC>(q, left);
+            }
+        } else if (tg < kGroups) {
+            const int c = c0 + 4 * tc;
+            int kk = kw + tg * U;
+            const bool in_k = k + tg * U < K;
+            if (seg >= 0 && P == 2 && kk >= W) kk -= W;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                wt[u] = load_four<T, VEC>(wb + (int64_t)(kk + u) * p.N + c, in_k && kk + u < wk ? p.N - c : 0);
+        }
+    };
+    auto stage = [&]() {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) s_rows[kg * (BM + 1) + rr + 32 * i] = xr[i];
+        if constexpr (WNK) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) s_cols[kg * (BN + 1) + rr + 32 * i] = wn[i];
+        } else if (tg < kGroups) {
+            uint4_t u[4];
+            transpose4(wt, u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s_cols[tg * (BN + 1) + place(4 * tc + j)] = u[j];
+        }
+    };
+
+    const int wr = wave % WR, wc = wave / WR;
+    const int r0 = wr * (BM / WR), c0w = wc * (BN / WC);
+    float16_t acc[TC][TR];
+    int ct = ct0, seg = -1, k = 0;
+    fetch(ct, seg, k);
+    while (ct < ct1) {
+#pragma unroll
+        for (int c = 0; c < TC; ++c)
+#pragma unroll
+            for (int r = 0; r < TR; ++r)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c][r][i] = 0.f;
+        const int now = ct;
+        while (ct == now) {
+            const int left = (seg < 0 ? p.K : P * W) - k;
+            const int pairs = left >= BK ? kGroups / 2 : (left + 2 * U - 1) / (2 * U);
+            __syncthreads();
+            stage();
+            __syncthreads();
+            k += BK;
+            if (k >= (seg < 0 ? p.K : P * W)) {
+                k = 0;
+                if (++seg >= nseg) {
+                    seg = -1;
+                    ++ct;
+                }
+            }
+            if (ct < ct1) fetch(ct, seg, k);
+            step_products<T, BN, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0, pairs);
+        }
+        const int c0 = now * BN + c0w;
+        if (p.narrow) {
+            const float scale = p.narrow_scale ? p.narrow_scale[t.g] : 1.f;
+            const int No = narrow_width<T>(p.N);
+#pragma unroll
+            for (int r = 0; r < TR; ++r) {
+                const int pl = r0 + 32 * r + (lane & 31);
+                if (pl >= rows) continue;
+                T *const q = static_cast<T *>(p.out) + (t.p0 + pl) * (P * No);
+#pragma unroll
+                for (int c = 0; c < TC; ++c)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const int col = c0 + 32 * c + vec_col<!WNK>(v, half);
+                        float4_t x = vec_val<!WNK>(acc[c][r], v);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = col + e < p.N ? x[e] * scale : 0.f;
+                        if (col < No) store_narrow(q + col, No, x);
+                    }
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < TR; ++r) {
+                const int row = s_row[r0 + 32 * r + (lane & 31)];
+                if (row < 0) continue;
+                T *const q = static_cast<T *>(p.out) + row * p.out_stride;
+#pragma unroll
+                for (int c = 0; c < TC; ++c)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const int col = c0 + 32 * c + vec_col<!WNK>(v, half);
+                        store_four<VEC>(q + col, vec_val<!WNK>(acc[c][r], v), p.N - col);
+                    }
+            }
+        }
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_row_outer(RowOrder o, RowOuter q)
+template <typename T, bool WNK, int BM, int BN, int WR>
+hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    const int g = blockIdx.x;
-    const int64_t start = clamp_offset(o.offsets[g], o.n);
-    const int64_t end = clamp_offset(o.offsets[g + 1], o.n);
-    const int cols = q.r > 0 ? q.r : q.B;
-    for (int64_t e = blockIdx.y * 256 + threadIdx.x; e < (int64_t)q.A * cols; e += 256 * gridDim.y) {
-        const int i = (int)(e / cols), c = (int)(e % cols);
-        float acc = 0.f;
-        for (int64_t pos = start; pos < end; ++pos) {
-            const int64_t row = row_at(o, pos);
-            if (!row_ok(o, row)) continue;
-            const float b = q.r > 0 ? ((const float *)q.h)[pos * q.r + c]
-                                : to_f32(((const T *)q.b)[row * q.b_stride + c]);
-            acc += to_f32(((const T *)q.a)[row * q.a_stride + i]) * b;
-        }
-        const int64_t at = q.transposed ? (int64_t)c * q.A + i : e;
-        ((T *)q.out)[(int64_t)g * q.A * cols + at] = (T)acc;
-    }
+    const bool vec = unit_aligned<T>(p.in, p.in_stride) && p.K % kU<T> == 0 && p.N % kU<T> == 0 &&
+                     unit_aligned<T>(p.w, 0) && (p.narrow || unit_aligned<T>(p.out, p.out_stride)) &&
+                     (!p.h || unit_aligned<T>(p.v, 0));
+    const bool v_vec = vec && p.r % kU<T> == 0;  // rows of r adapter weights
+    const int64_t tiles = p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
+    const int ctiles = (p.N + BN - 1) / BN;
+    // few rows: column tiles go to workgroups of their own
+    int splits = (int)(2048 / tiles);
+    splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
+    auto *kernel = vec ? k_row_product<T, WNK, BM, BN, WR, true> : k_row_product<T, WNK, BM, BN, WR, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits, v_vec);
+    return hipGetLastError();
+}
+
+template <typename T, bool WNK>
+hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    const bool few = o.n < 64 * (p.w_group ? (int64_t)o.G : 1);  // rows per group
+    if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);
+    if (few && p.N > 64) return launch<T, WNK, 32, 128, 1>(o, p, s);
+    if (few || p.N <= 64) return launch<T, WNK, 64, 64, 2>(o, p, s);
+    return launch<T, WNK, 128, 128, 2>(o, p, s);
 }
 
 }  // namespace
 
-size_t narrow_bytes(int dtype, int64_t n_rows, int N) { return (size_t)n_rows * N * 4; }
-
-size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B) { return 0; }
+size_t narrow_bytes(int dtype, int64_t n_rows, int N)
+{
+    return dtype == CGTP_BF16 ? (size_t)n_rows * narrow_width<bf16_t>(N) * 4
+                              : (size_t)n_rows * narrow_width<float>(N) * 4;
+}
 
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)(o.n / kTileRows + o.G + 1), (unsigned)((p.N + 63) / 64));
-    if (dtype == CGTP_BF16) hipLaunchKernelGGL(k_row_product<bf16_t>, grid, dim3(256), 0, s, o, p);
-    else hipLaunchKernelGGL(k_row_product<float>, grid, dim3(256), 0, s, o, p);
-    return hipGetLastError();
-}
-
-hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &q, void *ws, hipStream_t s)
-{
-    const int64_t cells = (int64_t)q.A * (q.r > 0 ? q.r : q.B);
-    const int64_t by = (cells + 255) / 256;
-    const dim3 grid((unsigned)o.G, (unsigned)(by < 1024 ? by : 1024));
-    if (dtype == CGTP_BF16) hipLaunchKernelGGL(k_row_outer<bf16_t>, grid, dim3(256), 0, s, o, q);
-    else hipLaunchKernelGGL(k_row_outer<float>, grid, dim3(256), 0, s, o, q);
-    return hipGetLastError();
+    if (dtype == CGTP_BF16) return p.w_nk ? pick<bf16_t, true>(o, p, s) : pick<bf16_t, false>(o, p, s);
+    return p.w_nk ? pick<float, true>(o, p, s) : pick<float, false>(o, p, s);
 }
 
 }  // namespace cgtp
