@@ -44,6 +44,9 @@ struct RowProduct {
     const float *narrow_scale;  // its factor per group, or NULL
 };
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
+// The form for short inputs and wide outputs (rows_wide.hip), and whether it covers a product.
+bool row_wide_takes(int dtype, const RowProduct &p);
+hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
 
 // out_g = sum over the rows of group g of a_i b_i^T, [A][B]; with h, the result of a narrow product,
 // in place of b: [A][r], or [r][A] where transposed.

@@ -19,8 +19,6 @@ namespace {
 
 using namespace rows;
 
-constexpr int kMaxSegments = 128;  // at most one per row of a tile
-
 template <typename T, bool WNK, int BM, int BN, int WR, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits, bool v_vec)
 {
@@ -32,7 +30,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     constexpr int NC = BN * kGroups / kThreads;        // units of [N][K] weights
     typedef typename Four<T>::t F;
     __shared__ uint4_t s_cols[kGroups * (BN + 1)], s_rows[kGroups * (BM + 1)];
-    __shared__ int s_row[BM], s_seg_g[kMaxSegments], s_seg_at[kMaxSegments + 1], s_nseg;
+    __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg;
 
     const bool shared_w = p.w_group == 0;
     Tile t;
@@ -57,53 +55,12 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     if (!shared_w && t.g == o.G) {  // rows of no group
         if (p.narrow) return;
         __syncthreads();
-        T *const out = static_cast<T *>(p.out);
-        const int c0 = ct0 * BN, c1 = ct1 * BN < p.N ? ct1 * BN : p.N;
-        for (int r = wave; r < rows; r += 4) {
-            const int row = s_row[r];
-            if (row >= 0)
-                for (int c = c0 + lane; c < c1; c += 64) out[row * p.out_stride + c] = (T)0.f;
-        }
+        store_zeros<T>(p, s_row, rows, ct0 * BN, ct1 * BN < p.N ? ct1 * BN : p.N);
         return;
     }
-    if (shared_w && p.h) {  // the segments of rows that share an adapter
-        __shared__ int s_g[BM];
-        if (tid < BM) {
-            int lo = 0, hi = o.G;  // the last group that starts at or before this position
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) / 2;
-                if (clamp_offset(o.offsets[mid], o.n) <= t.p0 + tid) lo = mid;
-                else hi = mid - 1;
-            }
-            s_g[tid] = tid < rows ? lo : o.G;
-        }
-        __syncthreads();
-        if (wave == 0) {
-            int n = 0;
-#pragma unroll
-            for (int b = 0; b < BM; b += 64) {
-                const int r = b + lane;
-                const bool in = r < BM;
-                const int g = in ? s_g[r] : o.G;
-                const bool first = in && g < o.G && (r == 0 || s_g[r - 1] != g);
-                const unsigned long long m = __ballot(first);
-                const int at = n + __popcll(m & ((1ull << lane) - 1));
-                if (first) {
-                    s_seg_g[at] = g;
-                    s_seg_at[at] = r;
-                }
-                n += __popcll(m);
-            }
-            if (lane == 0) s_nseg = n;
-        }
-        __syncthreads();
-        // where a segment ends: at the first row of another group
-        const int n = s_nseg;
-        if (tid < BM && s_g[tid] == o.G && (tid == 0 || s_g[tid - 1] != o.G)) s_seg_at[n] = tid;
-        if (tid == 0 && s_g[BM - 1] != o.G) s_seg_at[n] = BM;
-    }
+    int nseg = 0;
+    if (shared_w && p.h) nseg = find_segments<BM>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
     __syncthreads();
-    const int nseg = shared_w && p.h ? __builtin_amdgcn_readfirstlane(s_nseg) : 0;
 
     // the row units this thread stages: k-group tid % 8 of rows tid / 8 + 32 i
     const int kg = tid & 7, rr = tid >> 3;
@@ -267,6 +224,8 @@ template <typename T, bool WNK>
 hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const bool few = o.n < 64 * (p.w_group ? (int64_t)o.G : 1);  // rows per group
+    const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
+    if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1>(o, p, s);
     if (few || p.N <= 64) return launch<T, WNK, 64, 64, 2>(o, p, s);

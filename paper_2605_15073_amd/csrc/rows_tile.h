@@ -84,6 +84,49 @@ __device__ __forceinline__ int row_at(const RowOrder &o, int64_t p)
     return (unsigned)r < (unsigned)o.n ? r : -1;
 }
 
+// The segments of a tile's positions that share a group, for R = 32 .. 128 positions from p0 on: their
+// groups seg_g[0 .. count), where they start seg_at[0 .. count), and seg_at[count], the end of the last.
+// Positions of no group, and those from `rows` on, come after it. Returns the count. Called by the whole
+// workgroup; g: R ints of LDS.
+template <int R>
+__device__ __forceinline__ int find_segments(const RowOrder &o, int64_t p0, int rows, int *g, int *seg_g,
+                                             int *seg_at, int *count)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (tid < R) {
+        int lo = 0, hi = o.G;  // the last group that starts at or before this position
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (clamp_offset(o.offsets[mid], o.n) <= p0 + tid) lo = mid;
+            else hi = mid - 1;
+        }
+        g[tid] = tid < rows ? lo : o.G;
+    }
+    __syncthreads();
+    if (tid < 64) {
+        int n = 0;
+        for (int b = 0; b < R; b += 64) {
+            const int r = b + lane;
+            const int gr = r < R ? g[r] : o.G;
+            const bool first = gr < o.G && (r == 0 || g[r - 1] != gr);
+            const unsigned long long m = __ballot(first);
+            const int at = n + __popcll(m & ((1ull << lane) - 1));
+            if (first) {
+                seg_g[at] = gr;
+                seg_at[at] = r;
+            }
+            n += __popcll(m);
+        }
+        if (lane == 0) *count = n;
+    }
+    __syncthreads();
+    const int n = __builtin_amdgcn_readfirstlane(*count);
+    if (tid < R && g[tid] == o.G && (tid == 0 || g[tid - 1] != o.G)) seg_at[n] = tid;
+    if (tid == 0 && g[R - 1] != o.G) seg_at[n] = R;
+    __syncthreads();
+    return n;
+}
+
 // One unit: kU values from p on, zero past the `left` that exist.
 template <typename T, bool VEC>
 __device__ __forceinline__ uint4_t load_unit(const T *p, int64_t left)
@@ -232,6 +275,16 @@ template <bool VEC> __device__ __forceinline__ void store_four(bf16_t *p, float4
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (left > e) p[e] = h[e];
+}
+
+// Zeros in the columns [c0, c1) of the tile's rows: those of no group.
+template <typename T>
+__device__ __forceinline__ void store_zeros(const RowProduct &p, const int *row, int rows, int c0, int c1)
+{
+    for (int r = threadIdx.x >> 6; r < rows; r += kThreads / 64)
+        if (row[r] >= 0)
+            for (int c = c0 + (threadIdx.x & 63); c < c1; c += 64)
+                static_cast<T *>(p.out)[row[r] * p.out_stride + c] = (T)0.f;
 }
 
 // Results of narrow products (width N <= 64, between the two products of an adapter), in sequence

@@ -1,0 +1,315 @@
+// Products of grouped rows with short inputs and wide outputs: a radial network's last layer.
+//
+// Such a product writes far more than it reads, so what counts is that stores leave in whole lines and
+// that many waves have some under way. A wave keeps its 32 input rows in registers, one matrix operand
+// per lane as the instruction wants it, straight from memory, and runs over tiles of kCols output columns;
+// only the weights of a tile pass through LDS, loaded a tile ahead. The results are turned in a piece of LDS
+// that the wave has for itself, and leave as rows of kCols values, four rows a store.
+//
+// Nothing in the loop over column tiles branches, where vectors are whole (VEC): the wait for the next
+// tile's weights can then leave this tile's stores in flight, and the sums stay where they are (a branch
+// around a matrix instruction costs a copy of its 32 registers). So the number of k is a template
+// argument, rounded up with zeros; places without a row of their own take another place's of the tile
+// (and store the same values to the same place), columns past the end the last ones.
+//
+// Adapters: the narrow product's rows are further k of the same tile, held in registers like the
+// inputs, with the adapter's second matrix behind the shared weights in LDS; a tile whose rows have several
+// adapters takes them one after the other, with the rows of the others zero.
+#include "internal.h"
+#include "rows_tile.h"
+
+namespace cgtp {
+
+namespace {
+
+using namespace rows;
+
+constexpr int kRows = 128;    // positions of a workgroup, 32 a wave
+constexpr int kCols = 64;     // columns of a tile
+constexpr int kPairs = 8;     // pairs of k-groups at most: inputs of up to 128 bf16 or 64 fp32
+constexpr int kExtPairs = 4;  // of a narrow product's rows
+
+// Row stride of the turned results, in values: a multiple of their vectors, clear of bank conflicts
+// between the rows that the 8 (fp32, 16 bytes) or 16 (bf16, 8 bytes) lanes of a cycle write.
+template <typename T> constexpr int kTurn = kCols + 4;
+
+template <typename T> struct Out4;
+template <> struct Out4<float> { typedef float4_t t; };
+template <> struct Out4<bf16_t> { typedef bf4_t t; };
+
+__device__ __forceinline__ void convert(float4_t v, float4_t &o) { o = v; }
+__device__ __forceinline__ void convert(float4_t v, bf4_t &o)
+{
+    o = bf4_t{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+}
+
+// Orders a wave's LDS writes before its other lanes' reads.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters).
+template <typename T, bool WNK, int NP, int XP, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p, int splits)
+{
+    constexpr int U = kU<T>, P = kParts<T>, KG = 2 * (NP + XP), LD = kCols + 1;
+    constexpr bool EXT = XP > 0;
+    static_assert(!(EXT && (WNK || !VEC)), "adapters: [K][N] weights, whole vectors");
+    typedef typename Four<T>::t F;
+    typedef typename Out4<T>::t O;
+    __shared__ uint4_t s_w[KG * LD];
+    __shared__ O s_turn[4 * 32 * kTurn<T> / 4];
+    __shared__ int s_row[kRows], s_place[kRows], s_any;
+    __shared__ int s_g[EXT ? kRows : 1], s_seg_g[EXT ? kRows : 1], s_seg_at[EXT ? kRows + 1 : 1], s_nseg;
+
+    Tile t;
+    if (EXT) {
+        t.p0 = (int64_t)blockIdx.x * kRows;
+        t.p1 = t.p0 + kRows < o.n ? t.p0 + kRows : o.n;
+        t.g = 0;
+    } else {
+        t = find_tile(o, 7, blockIdx.x);
+        if (t.g < 0 || t.p0 >= t.p1) return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rows = (int)(t.p1 - t.p0);
+    const int ctiles = (p.N + kCols - 1) / kCols;
+    const int ct0 = (int)((int64_t)ctiles * blockIdx.y / splits);
+    const int ct1 = (int)((int64_t)ctiles * (blockIdx.y + 1) / splits);
+    if (ct0 >= ct1) return;
+    const int my_row = tid < rows ? row_at(o, t.p0 + tid) : -1;
+    if (tid < kRows) s_row[tid] = my_row;
+    if (tid == 0) s_any = -1;
+    __syncthreads();
+    if (my_row >= 0) s_any = tid;  // any place that has a row
+    if (!EXT && t.g == o.G) {
+        store_zeros<T>(p, s_row, rows, ct0 * kCols, ct1 * kCols < p.N ? ct1 * kCols : p.N);
+        return;
+    }
+    int nseg = 0;
+    if (EXT) nseg = find_segments<kRows>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
+    else __syncthreads();
+    if (s_any < 0) return;
+    if (tid < kRows) s_place[tid] = my_row >= 0 ? tid : s_any;
+    __syncthreads();
+
+    // inputs: row 32 wave + lane % 32, k-groups 2 s + half
+    const int pl = s_place[32 * wave + (lane & 31)];
+    const T *const in = static_cast<const T *>(p.in) + s_row[pl] * p.in_stride;
+    const int W = EXT ? narrow_width<T>(p.r) : 0;
+    uint4_t x[NP], h[EXT ? XP : 1];
+#pragma unroll
+    for (int s = 0; s < NP; ++s) {
+        const int k = (2 * s + half) * U;
+        x[s] = load_unit<T, VEC>(in + k, p.K - k);
+    }
+    if (EXT) {
+        const bool grouped = s_g[pl] < o.G;
+#pragma unroll
+        for (int s = 0; s < XP; ++s) {
+            const int k = (2 * s + half) * U;
+            h[s] = load_unit<T, true>(static_cast<const T *>(p.h) + (grouped ? (t.p0 + pl) * (P * W) : 0) + k,
+                                      grouped ? P * W - k : 0);
+        }
+    }
+    // outputs: this lane stores vector lane % 16 of rows 4 i + lane / 16
+    T *out[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        out[i] = static_cast<T *>(p.out) + s_row[s_place[32 * wave + 4 * i + (lane >> 4)]] * p.out_stride;
+
+    // Weights. Round 0 of a column tile: the shared ones, with the first adapter's behind them; then the
+    // other adapters' of the tile.
+    constexpr int kTasks = (WNK ? kCols : kCols / 4) * KG;  // units, or units of four columns
+    constexpr int NT = (kTasks + kThreads - 1) / kThreads;
+    const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
+    uint4_t wn[WNK ? NT : 1];
+    F wt[WNK ? 1 : NT][WNK ? 1 : U];
+    unsigned we[VEC ? 1 : NT][VEC ? 1 : U * 4];  // single values, packed when they are staged
+    int have[NT];  // k of the k-groups in flight that the weights have
+    auto fetch = [&](int ct, int seg) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int task = tid + kThreads * i;
+            const int g = WNK ? task % KG : task / (kCols / 4);
+            int k = g * U, K = p.K;
+            const T *wb = w;
+            if (EXT && g >= 2 * NP) {
+                k = (g - 2 * NP) * U;
+                K = k < P * W && nseg > 0 ? p.r : 0;
+                if (P == 2 && k >= W) k -= W;  // the second part meets the same weights
+                wb = static_cast<const T *>(p.v) + (int64_t)(nseg > 0 ? s_seg_g[seg] : 0) * p.r * p.N;
+            }
+            have[i] = K - k;
+            if (have[i] <= 0) k = 0;
+            if constexpr (WNK) {
+                const int c = ct * kCols + task / KG;
+                const T *const q = wb + (int64_t)(c < p.N ? c : p.N - 1) * p.K + k;
+                if (VEC) wn[i] = *reinterpret_cast<const uint4_t *>(q);
+                else wn[i] = load_unit<T, false>(q, have[i]);
+            } else {
+                const int c = ct * kCols + 4 * (task % (kCols / 4));
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const T *const q = wb + (int64_t)(u < have[i] ? k + u : 0) * p.N;
+                    if constexpr (VEC) {
+                        wt[i][u] = *reinterpret_cast<const F *>(q + (c < p.N ? c : p.N - 4));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const T *const z = q + (c + e < p.N ? c + e : p.N - 1);
+                            we[i][4 * u + e] = sizeof(T) == 2 ? *reinterpret_cast<const unsigned short *>(z)
+                                                              : *reinterpret_cast<const unsigned *>(z);
+                        }
+                    }
+                }
+            }
+        }
+    };
+    auto stage = [&]() {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int task = tid + kThreads * i;
+            if (kTasks % kThreads != 0 && task >= kTasks) continue;
+            if constexpr (WNK) {
+                s_w[task % KG * LD + task / KG] = have[i] > 0 ? wn[i] : uint4_t{0, 0, 0, 0};
+            } else {
+                if constexpr (!VEC) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int e = 0; e < (int)(sizeof(F) / 4); ++e)
+                            wt[i][u][e] = sizeof(T) == 2 ? we[i][4 * u + 2 * e] | we[i][4 * u + 2 * e + 1] << 16
+                                                         : we[i][4 * u + e];
+                }
+                uint4_t unit[4];
+#pragma unroll
+                for (int u = 0; u < U; ++u) wt[i][u] = u < have[i] ? wt[i][u] : F{};
+                transpose4(wt[i], unit);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    s_w[task / (kCols / 4) * LD + place(4 * (task % (kCols / 4)) + j)] = unit[j];
+            }
+        }
+    };
+
+    O *const turn = s_turn + wave * (32 * kTurn<T> / 4);
+    const uint4_t *const a = s_w + half * LD + (lane & 31);
+    fetch(ct0, 0);
+    for (int ct = ct0; ct < ct1; ++ct) {
+        float16_t acc[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
+        __syncthreads();
+        stage();
+        __syncthreads();
+        fetch(nseg > 1 || ct + 1 == ct1 ? ct : ct + 1, nseg > 1 ? 1 : 0);
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+            mma(acc[0], a[2 * s * LD], x[s], T{});
+            mma(acc[1], a[2 * s * LD + 32], x[s], T{});
+        }
+        if (EXT) {
+            for (int seg = 0;;) {
+                const bool in_seg = nseg > 0 && pl >= s_seg_at[seg] && pl < s_seg_at[seg + 1];
+#pragma unroll
+                for (int s = 0; s < XP; ++s) {
+                    uint4_t b;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) b[e] = in_seg ? h[s][e] : 0u;
+                    mma(acc[0], a[2 * (NP + s) * LD], b, T{});
+                    mma(acc[1], a[2 * (NP + s) * LD + 32], b, T{});
+                }
+                if (++seg >= nseg) break;
+                __syncthreads();
+                stage();
+                __syncthreads();
+                if (seg + 1 < nseg) fetch(ct, seg + 1);
+                else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
+            }
+        }
+        // rows of kCols values, four at a time
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                convert(vec_val<!WNK>(acc[c], v), turn[((lane & 31) * kTurn<T> + 32 * c + vec_col<!WNK>(v, half)) / 4]);
+        wave_sync();
+        int in_tile = 4 * (lane & 15);
+        if (VEC && ct * kCols + in_tile >= p.N) in_tile = p.N - 4 - ct * kCols;
+        const int col = ct * kCols + in_tile;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const O val = turn[((4 * i + (lane >> 4)) * kTurn<T> + in_tile) / 4];
+            if (VEC) {
+                *reinterpret_cast<O *>(out[i] + col) = val;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < p.N) out[i][col + e] = val[e];
+            }
+        }
+        wave_sync();
+    }
+}
+
+template <typename T> bool whole_vectors(const RowProduct &p)
+{
+    return unit_aligned<T>(p.in, p.in_stride) && p.K % kU<T> == 0 && p.N % kU<T> == 0 &&
+           unit_aligned<T>(p.w, 0) && unit_aligned<T>(p.out, p.out_stride) && (!p.h || unit_aligned<T>(p.v, 0));
+}
+
+template <typename T, bool WNK, int NP, int XP, bool VEC>
+hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    const int64_t tiles = XP > 0 ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
+    const int ctiles = (p.N + kCols - 1) / kCols;
+    int splits = (int)(2048 / tiles);  // few rows: column tiles go to workgroups of their own
+    splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
+    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, VEC>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
+                       0, s, o, p, splits);
+    return hipGetLastError();
+}
+
+template <typename T, int NP> hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    if (!p.h) return p.w_nk ? launch<T, true, NP, 0, true>(o, p, s) : launch<T, false, NP, 0, true>(o, p, s);
+    const bool two = kParts<T> * narrow_width<T>(p.r) <= 4 * kU<T>;
+    return two ? launch<T, false, NP, 2, true>(o, p, s) : launch<T, false, NP, kExtPairs, true>(o, p, s);
+}
+
+template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    if (!whole_vectors<T>(p))
+        return p.w_nk ? launch<T, true, kPairs, 0, false>(o, p, s) : launch<T, false, kPairs, 0, false>(o, p, s);
+    if (p.K <= 4 * kU<T>) return with_pairs<T, 2>(o, p, s);
+    if (p.K <= 8 * kU<T>) return with_pairs<T, 4>(o, p, s);
+    return with_pairs<T, kPairs>(o, p, s);
+}
+
+template <typename T> bool takes(const RowProduct &p)
+{
+    if (p.narrow || p.N <= kCols || p.K > 2 * kPairs * kU<T>) return false;
+    if (!p.h) return p.w_group != 0;
+    return !p.w_nk && whole_vectors<T>(p) && kParts<T> * narrow_width<T>(p.r) <= 2 * kExtPairs * kU<T>;
+}
+
+}  // namespace
+
+bool row_wide_takes(int dtype, const RowProduct &p)
+{
+    return dtype == CGTP_BF16 ? takes<bf16_t>(p) : takes<float>(p);
+}
+
+hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    return dtype == CGTP_BF16 ? pick<bf16_t>(o, p, s) : pick<float>(o, p, s);
+}
+
+}  // namespace cgtp
