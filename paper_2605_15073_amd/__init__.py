@@ -9,6 +9,7 @@ fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -599,56 +600,80 @@ def _row_dtype(name, t):
 def _want_rows(name, t, n, width, like):
     """[n, width] rows on like's device, of like's type, contiguous along the width; returns the
     row stride."""
-    if (t.dim() != 2 or tuple(t.shape) != (n, width) or t.dtype != like.dtype
-            or t.device != like.device or not t.is_cuda
-            or (width > 1 and n > 0 and t.stride(1) != 1)
-            or (n > 1 and t.stride(0) < width)):
-        raise ValueError(f"{name}: expected {like.dtype} rows ({n}, {width}) on {like.device}, "
-                         f"contiguous along the width, got {t.dtype} {tuple(t.shape)} with strides "
-                         f"{t.stride()} on {t.device}")
-    return max(t.stride(0), width) if n > 1 else width
+    if t.shape == (n, width) and t.dtype == like.dtype and t.device == like.device:
+        row, step = t.stride()
+        if n <= 1:
+            if step == 1 or width == 1 or n == 0:
+                return width
+        elif (step == 1 or width == 1) and row >= width:
+            return row
+    raise ValueError(f"{name}: expected {like.dtype} rows ({n}, {width}) on {like.device}, contiguous "
+                     f"along the width, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on "
+                     f"{t.device}")
 
 
 def _want_dev(name, t, shape, dtype, like):
-    if (not t.is_cuda or t.device != like.device or t.dtype != dtype or not t.is_contiguous()
-            or tuple(t.shape) != tuple(shape)):
+    """A contiguous tensor on like's device, which is a GPU (checked by _row_call)."""
+    if t.device != like.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous {dtype} tensor of shape {tuple(shape)} on "
                          f"{like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _row_call(like, stream):
-    """(device guard, stream to run on, its handle) of a call on like's device."""
+    """(handle of the stream that a call on like's device runs on, the stream if it is not the
+    current one)."""
     torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream(like.device)
-    return torch.cuda.device(like.device), s, ctypes.c_void_p(s.cuda_stream)
+    if not like.is_cuda:
+        raise ValueError(f"expected device tensors, got one on {like.device}")
+    current = torch.cuda.current_stream(like.device.index)
+    if stream is None or stream == current:
+        return current.cuda_stream, None
+    return stream.cuda_stream, stream
 
 
-def _new(shape, dtype, like, s):
-    """A tensor for work on stream s, whose memory is not reused before that work is done."""
+def _new(shape, dtype, like, side):
+    """A tensor for work on the current stream, or on the stream side: then its memory is neither
+    taken before the current stream's pending work on it is done nor reused before side's."""
     torch = _torch()
     t = torch.empty(shape, dtype=dtype, device=like.device)
-    if t.numel() and s != torch.cuda.current_stream(like.device):
-        # the memory may have been freed by the current stream's pending work
-        s.wait_stream(torch.cuda.current_stream(like.device))
-        t.record_stream(s)
+    if side is not None and t.numel():
+        side.wait_stream(torch.cuda.current_stream(like.device))
+        t.record_stream(side)
     return t
 
 
-def _row_workspace(workspace, need, like, s):
-    torch = _torch()
+def _row_workspace(workspace, need, like, side):
+    """(pointer, bytes, the tensor) of the caller's workspace or of a new one."""
     if workspace is None:
         if need == 0:
             return None, 0, None
-        workspace = _new((need,), torch.uint8, like, s)
-    elif not workspace.is_cuda or workspace.device != like.device or not workspace.is_contiguous():
+        workspace = _new((need,), _torch().uint8, like, side)
+    elif workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError(f"workspace: expected a contiguous tensor on {like.device}")
-    return _ptr(workspace), workspace.numel() * workspace.element_size(), workspace
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
+@functools.lru_cache(maxsize=1024)
 def _bytes(name, *args):
     out = ctypes.c_size_t()
     _check(getattr(load_library(), name)(*args, ctypes.byref(out)), name)
     return out.value
+
+
+def _run(name, like, *args):
+    """The call on like's device. Pointers are integers or None."""
+    torch = _torch()
+    if torch.cuda.current_device() == like.device.index:
+        status = getattr(_lib, name)(*args)
+    else:
+        with torch.cuda.device(like.device):
+            status = getattr(_lib, name)(*args)
+    if status != CGTP_OK:
+        _check(status, name)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _want_order(offsets, order, n, G, like):
@@ -665,18 +690,17 @@ def group_rows(ids, n_groups: int, offsets=None, order=None, workspace=None, str
     if ids.dim() != 1:
         raise ValueError(f"ids: expected one dimension, got {tuple(ids.shape)}")
     n = ids.shape[0]
+    handle, side = _row_call(ids, stream)
     _want_dev("ids", ids, (n,), torch.int32, ids)
     need = _bytes("cgtp_group_rows_bytes", n, n_groups)
-    guard, s, handle = _row_call(ids, stream)
     if offsets is None:
-        offsets = _new((n_groups + 1,), torch.int32, ids, s)
+        offsets = _new((n_groups + 1,), torch.int32, ids, side)
     if order is None:
-        order = _new((n,), torch.int32, ids, s)
+        order = _new((n,), torch.int32, ids, side)
     _want_order(offsets, order, n, n_groups, ids)
-    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, ids, s)
-    with guard:
-        _check(load_library().cgtp_group_rows(n, n_groups, _ptr(ids), _ptr(offsets), _ptr(order),
-                                              ws_ptr, ws_len, handle), "cgtp_group_rows")
+    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, ids, side)
+    _run("cgtp_group_rows", ids, n, n_groups, ids.data_ptr(), offsets.data_ptr(), order.data_ptr(),
+         ws_ptr, ws_len, handle)
     return offsets, order
 
 
@@ -684,6 +708,7 @@ def _linear_head(x, w, offsets, order, shared):
     if x.dim() != 2 or w.dim() != (2 if shared else 3):
         raise ValueError(f"x, w: expected 2 and {2 if shared else 3} dimensions, got "
                          f"{tuple(x.shape)} and {tuple(w.shape)}")
+    load_library()
     n, (n_in, n_out) = x.shape[0], w.shape[-2:]
     G = offsets.shape[0] - 1
     _want_order(offsets, order, n, G, x)
@@ -696,23 +721,21 @@ def grouped_linear(x, w, offsets, order=None, y=None, stream=None):
     y [n, n_out] rows (any row stride), w [G, n_in, n_out]; offsets, order from group_rows (order
     None: the rows are sorted by group)."""
     dt, n, G, n_in, n_out, xs = _linear_head(x, w, offsets, order, False)
-    guard, s, handle = _row_call(x, stream)
+    handle, side = _row_call(x, stream)
     if y is None:
-        y = _new((n, n_out), x.dtype, x, s)
+        y = _new((n, n_out), x.dtype, x, side)
     ys = _want_rows("y", y, n, n_out, x)
-    with guard:
-        _check(load_library().cgtp_grouped_linear(dt, n, G, n_in, n_out, _ptr(offsets), _ptr(order),
-                                                  _ptr(x), xs, _ptr(w), _ptr(y), ys, handle),
-               "cgtp_grouped_linear")
+    _run("cgtp_grouped_linear", x, dt, n, G, n_in, n_out, _addr(offsets), _addr(order), _addr(x),
+         xs, _addr(w), _addr(y), ys, handle)
     return y
 
 
-def _grad_out(name, out, shape, like, s, rows):
+def _grad_out(name, out, shape, like, side, rows):
     """An output of a gradient call: allocated if None, skipped if False; (tensor, row stride)."""
     if out is False:
         return None, 0
     if out is None:
-        out = _new(shape, like.dtype, like, s)
+        out = _new(shape, like.dtype, like, side)
     if rows:
         return out, _want_rows(name, out, *shape, like)
     _want_dev(name, out, shape, like.dtype, like)
@@ -725,17 +748,15 @@ def grouped_linear_grad(x, w, dy, offsets, order=None, dx=None, dw=None, workspa
     given as False is skipped (None in its place)."""
     dt, n, G, n_in, n_out, xs = _linear_head(x, w, offsets, order, False)
     dys = _want_rows("dy", dy, n, n_out, x)
-    guard, s, handle = _row_call(x, stream)
-    dx, dxs = _grad_out("dx", dx, (n, n_in), x, s, True)
-    dw, _ = _grad_out("dw", dw, (G, n_in, n_out), x, s, False)
+    handle, side = _row_call(x, stream)
+    dx, dxs = _grad_out("dx", dx, (n, n_in), x, side, True)
+    dw, _ = _grad_out("dw", dw, (G, n_in, n_out), x, side, False)
     ws_ptr, ws_len, _keep = None, 0, None
     if dw is not None:
         need = _bytes("cgtp_grouped_linear_grad_bytes", dt, n, G, n_in, n_out)
-        ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, s)
-    with guard:
-        _check(load_library().cgtp_grouped_linear_grad(
-            dt, n, G, n_in, n_out, _ptr(offsets), _ptr(order), _ptr(x), xs, _ptr(w), _ptr(dy), dys,
-            _ptr(dx), dxs, _ptr(dw), ws_ptr, ws_len, handle), "cgtp_grouped_linear_grad")
+        ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, side)
+    _run("cgtp_grouped_linear_grad", x, dt, n, G, n_in, n_out, _addr(offsets), _addr(order),
+         _addr(x), xs, _addr(w), _addr(dy), dys, _addr(dx), dxs, _addr(dw), ws_ptr, ws_len, handle)
     return dx, dw
 
 
@@ -758,16 +779,14 @@ def adapter_linear(x, w, a, b, offsets, order=None, scale=None, y=None, workspac
     y [n, n_out] rows, w [n_in, n_out] shared, a [G, n_in, r], b [G, r, n_out], scale [G] float32
     or None (1)."""
     (dt, n, G, n_in, n_out, xs), r = _adapter_head(x, w, a, b, offsets, order, scale)
-    guard, s, handle = _row_call(x, stream)
+    handle, side = _row_call(x, stream)
     if y is None:
-        y = _new((n, n_out), x.dtype, x, s)
+        y = _new((n, n_out), x.dtype, x, side)
     ys = _want_rows("y", y, n, n_out, x)
     need = _bytes("cgtp_adapter_linear_bytes", dt, n, G, n_in, n_out, r)
-    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, s)
-    with guard:
-        _check(load_library().cgtp_adapter_linear(
-            dt, n, G, n_in, n_out, r, _ptr(offsets), _ptr(order), _ptr(x), xs, _ptr(w), _ptr(a),
-            _ptr(b), _ptr(scale), _ptr(y), ys, ws_ptr, ws_len, handle), "cgtp_adapter_linear")
+    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, side)
+    _run("cgtp_adapter_linear", x, dt, n, G, n_in, n_out, r, _addr(offsets), _addr(order), _addr(x),
+         xs, _addr(w), _addr(a), _addr(b), _addr(scale), _addr(y), ys, ws_ptr, ws_len, handle)
     return y
 
 
@@ -777,17 +796,15 @@ def adapter_linear_grad(x, w, a, b, dy, offsets, order=None, scale=None, dx=None
     output given as False is skipped (None in its place)."""
     (dt, n, G, n_in, n_out, xs), r = _adapter_head(x, w, a, b, offsets, order, scale)
     dys = _want_rows("dy", dy, n, n_out, x)
-    guard, s, handle = _row_call(x, stream)
-    dx, dxs = _grad_out("dx", dx, (n, n_in), x, s, True)
-    da, _ = _grad_out("da", da, (G, n_in, r), x, s, False)
-    db, _ = _grad_out("db", db, (G, r, n_out), x, s, False)
+    handle, side = _row_call(x, stream)
+    dx, dxs = _grad_out("dx", dx, (n, n_in), x, side, True)
+    da, _ = _grad_out("da", da, (G, n_in, r), x, side, False)
+    db, _ = _grad_out("db", db, (G, r, n_out), x, side, False)
     need = _bytes("cgtp_adapter_linear_grad_bytes", dt, n, G, n_in, n_out, r)
-    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, s)
-    with guard:
-        _check(load_library().cgtp_adapter_linear_grad(
-            dt, n, G, n_in, n_out, r, _ptr(offsets), _ptr(order), _ptr(x), xs, _ptr(w), _ptr(a),
-            _ptr(b), _ptr(scale), _ptr(dy), dys, _ptr(dx), dxs, _ptr(da), _ptr(db), ws_ptr, ws_len,
-            handle), "cgtp_adapter_linear_grad")
+    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, side)
+    _run("cgtp_adapter_linear_grad", x, dt, n, G, n_in, n_out, r, _addr(offsets), _addr(order),
+         _addr(x), xs, _addr(w), _addr(a), _addr(b), _addr(scale), _addr(dy), dys, _addr(dx), dxs,
+         _addr(da), _addr(db), ws_ptr, ws_len, handle)
     return dx, da, db
 
 
@@ -806,6 +823,8 @@ class AdamWTensors:
             raise ValueError("params, grads, m, v (, scales, copies): lists of one length >= 1")
         if (m_scale is None) != (v_scale is None):
             raise ValueError("m_scale and v_scale: both or neither")
+        if not params[0].is_cuda:
+            raise ValueError(f"params[0]: expected a device tensor, got one on {params[0].device}")
         bits = 32 if m_scale is None else 8
         gdt = grads[0].dtype
         self.state_bits, self.device = bits, params[0].device
@@ -858,28 +877,25 @@ def adamw(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9, beta2
     first = tensors._keep[0][0]
     if grad_scale is not None:
         _want_dev("grad_scale", grad_scale, (1,), _torch().float32, first)
-    guard, _, handle = _row_call(first, stream)
-    with guard:
-        _check(load_library().cgtp_adamw_step(tensors.handle, lr, beta1, beta2, eps, weight_decay,
-                                              step, _ptr(grad_scale), handle), "cgtp_adamw_step")
+    handle, _ = _row_call(first, stream)
+    _run("cgtp_adamw_step", first, tensors.handle, lr, beta1, beta2, eps, weight_decay, step,
+         _addr(grad_scale), handle)
 
 
 def adamw_states(tensors: AdamWTensors, m_out=None, v_out=None, stream=None):
     """cgtp_adamw_states: the float32 values that 8-bit states stand for, as lists (m, v)."""
     torch = _torch()
     first = tensors._keep[0][0]
-    guard, s, handle = _row_call(first, stream)
+    handle, side = _row_call(first, stream)
     outs = []
     for name, given in (("m_out", m_out), ("v_out", v_out)):
         if given is None:
-            given = [_new(shape, torch.float32, first, s) for shape in tensors.shapes]
+            given = [_new(shape, torch.float32, first, side) for shape in tensors.shapes]
         if len(given) != len(tensors.shapes):
             raise ValueError(f"{name}: expected {len(tensors.shapes)} tensors, got {len(given)}")
         for i, (t, shape) in enumerate(zip(given, tensors.shapes)):
             _want_dev(f"{name}[{i}]", t, shape, torch.float32, first)
         outs.append(given)
     arrays = [(ctypes.c_void_p * len(o))(*[t.data_ptr() for t in o]) for o in outs]
-    with guard:
-        _check(load_library().cgtp_adamw_states(tensors.handle, arrays[0], arrays[1], handle),
-               "cgtp_adamw_states")
+    _run("cgtp_adamw_states", first, tensors.handle, arrays[0], arrays[1], handle)
     return outs[0], outs[1]
