@@ -112,8 +112,6 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         __syncthreads();
         fetch(0);
         for (int s = 0; s < steps; ++s) {
-            const int64_t left = t.p1 - t.p0 - (int64_t)s * BK;
-            const int pairs = left >= BK ? kGroups / 2 : (int)((left + 2 * U - 1) / (2 * U));
             __syncthreads();
             stage();
             if (tid < BK) s_id[(s + 1) & 1][tid] = id;
@@ -124,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             }
 #pragma unroll
             for (int e = 0; e < P; ++e)
-                step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0, pairs);
+                step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0);
         }
     }
     const bool whole = t.end - t.start <= ((int64_t)1 << shift);
@@ -157,29 +155,52 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     }
 }
 
-// out_g = its slots' sum, for the groups of more than one chunk. Such a group holds the first multiple
-// of the chunk size beyond its start, by which it is found: block x is for multiple x + 1.
+constexpr int kJoinCells = 32, kJoinLanes = kThreads / kJoinCells;
+
+// out_g = its slots' sum, for the groups of more than one chunk: a workgroup takes 32 cells, 8 threads
+// each with every eighth slot, whose sums are then added in order. Where there are fewer groups than
+// chunk sizes in the sequence, block x is for group x; else for the group whose first multiple of the
+// chunk size beyond its start is x + 1 (each such group has one).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, int shift, int64_t cells,
+__global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, int shift, bool by_group, int64_t cells,
                                                        const float *__restrict__ slots, T *__restrict__ out)
 {
+    __shared__ float s_sum[kJoinLanes][kJoinCells];
     const int64_t pos = ((int64_t)blockIdx.x + 1) << shift;
-    int lo = 0, hi = o.G;  // the group that holds pos
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (clamp_offset(o.offsets[mid], o.n) <= pos) lo = mid;
-        else hi = mid - 1;
-    }
+    int lo = 0, hi = o.G;
+    if (by_group) lo = blockIdx.x;
+    else
+        while (lo < hi) {  // the group that holds pos
+            const int mid = (lo + hi + 1) / 2;
+            if (clamp_offset(o.offsets[mid], o.n) <= pos) lo = mid;
+            else hi = mid - 1;
+        }
     if (lo >= o.G) return;
     const int64_t start = clamp_offset(o.offsets[lo], o.n), end = clamp_offset(o.offsets[lo + 1], o.n);
     const int64_t chunks = (end - start + ((int64_t)1 << shift) - 1) >> shift;
-    if ((start >> shift) + 1 != pos >> shift || chunks < 2) return;
+    if (chunks < 2 || (!by_group && (start >> shift) + 1 != pos >> shift)) return;
     const float *const src = slots + 2 * (start >> shift) * cells;
-    for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < cells;
-         i += (int64_t)gridDim.y * kThreads) {
+    const int cell = threadIdx.x % kJoinCells, lane = threadIdx.x / kJoinCells;
+    for (int64_t c0 = (int64_t)blockIdx.y * kJoinCells; c0 < cells; c0 += (int64_t)gridDim.y * kJoinCells) {
+        const int64_t i = c0 + cell;
         float sum = 0.f;
-        for (int64_t c = 0; c < chunks; ++c) sum += src[c * cells + i];
-        out[lo * cells + i] = (T)sum;
+        if (i < cells) {
+            int64_t c = lane;
+            for (; c + 3 * kJoinLanes < chunks; c += 4 * kJoinLanes) {
+                const float v0 = src[c * cells + i], v1 = src[(c + kJoinLanes) * cells + i];
+                const float v2 = src[(c + 2 * kJoinLanes) * cells + i], v3 = src[(c + 3 * kJoinLanes) * cells + i];
+                sum += (v0 + v1) + (v2 + v3);
+            }
+            for (; c < chunks; c += kJoinLanes) sum += src[c * cells + i];
+        }
+        __syncthreads();
+        s_sum[lane][cell] = sum;
+        __syncthreads();
+        if (lane == 0 && i < cells) {
+#pragma unroll
+            for (int j = 1; j < kJoinLanes; ++j) sum += s_sum[j][cell];
+            out[lo * cells + i] = (T)sum;
+        }
     }
 }
 
@@ -237,9 +258,11 @@ template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float
     else if (sh.bn == 64) e = launch<T, 128, 64, 4>(o, q, sh, slots, s);
     else e = launch<T, 128, 128, 2>(o, q, sh, slots, s);
     if (e != hipSuccess || o.n >> sh.shift == 0) return e;
-    const int64_t cells = (int64_t)q.A * B, by = (cells + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL(k_row_join<T>, dim3((unsigned)(o.n >> sh.shift), (unsigned)(by < 1024 ? by : 1024)),
-                       dim3(kThreads), 0, s, o, sh.shift, cells, slots, static_cast<T *>(q.out));
+    const int64_t cells = (int64_t)q.A * B, by = (cells + kJoinCells - 1) / kJoinCells;
+    const int64_t spans = o.n >> sh.shift, bx = o.G < spans ? o.G : spans;
+    const int64_t y = 8192 / bx < 1 ? 1 : 8192 / bx;
+    hipLaunchKernelGGL(k_row_join<T>, dim3((unsigned)bx, (unsigned)(by < y ? by : y)), dim3(kThreads), 0, s, o,
+                       sh.shift, o.G < spans, cells, slots, static_cast<T *>(q.out));
     return hipGetLastError();
 }
 

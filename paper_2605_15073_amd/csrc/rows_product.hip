@@ -149,8 +149,6 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
                 for (int i = 0; i < 16; ++i) acc[c][r][i] = 0.f;
         const int now = ct;
         while (ct == now) {
-            const int left = (seg < 0 ? p.K : P * W) - k;
-            const int pairs = left >= BK ? kGroups / 2 : (left + 2 * U - 1) / (2 * U);
             __syncthreads();
             stage();
             __syncthreads();
@@ -163,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
                 }
             }
             if (ct < ct1) fetch(ct, seg, k);
-            step_products<T, BN, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0, pairs);
+            step_products<T, BN, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0);
         }
         const int c0 = now * BN + c0w;
         if (p.narrow) {

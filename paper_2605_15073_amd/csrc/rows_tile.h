@@ -218,26 +218,25 @@ __device__ __forceinline__ void mma(float16_t &acc, uint4_t a, uint4_t b, float)
 }
 
 // The products of a step: TC blocks of 32 columns (from unit column c0 of cols) by TR blocks of 32
-// rows, over the first `pairs` pairs of k-groups. acc[c][r][i]: column place 8 (i / 4) + 4 (lane / 32)
-// + i % 4 of block c, row place lane % 32 of block r.
+// rows. acc[c][r][i]: column place 8 (i / 4) + 4 (lane / 32) + i % 4 of block c, row place lane % 32 of
+// block r. All k-groups always, zeros past the end: a branch around a matrix instruction costs a copy of
+// its sums.
 template <typename T, int BN, int BM, int TC, int TR>
 __device__ __forceinline__ void step_products(float16_t (&acc)[TC][TR], const uint4_t *cols,
-                                              const uint4_t *rws, int c0, int r0, int pairs)
+                                              const uint4_t *rws, int c0, int r0)
 {
     const int lane = threadIdx.x & 63, half = lane >> 5, n = lane & 31;
 #pragma unroll
     for (int s = 0; s < kGroups / 2; ++s) {
-        if (s < pairs) {
-            uint4_t a[TC], b[TR];
+        uint4_t a[TC], b[TR];
 #pragma unroll
-            for (int c = 0; c < TC; ++c) a[c] = cols[(2 * s + half) * (BN + 1) + c0 + 32 * c + n];
+        for (int c = 0; c < TC; ++c) a[c] = cols[(2 * s + half) * (BN + 1) + c0 + 32 * c + n];
 #pragma unroll
-            for (int r = 0; r < TR; ++r) b[r] = rws[(2 * s + half) * (BM + 1) + r0 + 32 * r + n];
+        for (int r = 0; r < TR; ++r) b[r] = rws[(2 * s + half) * (BM + 1) + r0 + 32 * r + n];
 #pragma unroll
-            for (int c = 0; c < TC; ++c)
+        for (int c = 0; c < TC; ++c)
 #pragma unroll
-                for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r], T{});
-        }
+            for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r], T{});
     }
 }
 
