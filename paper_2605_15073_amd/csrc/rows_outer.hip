@@ -21,30 +21,30 @@ using namespace rows;
 template <typename T, int BM, int BN, int WR, bool VEC, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, int shift, float *slots)
 {
-    constexpr int U = kU<T>, BK = kStep<T>, P = NARROW ? kParts<T> : 1;
+    constexpr int KG = kGroups<T>, BK = kStep<T>, P = NARROW ? kNarrow<T> : 1, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
-    typedef typename Four<T>::t F;
-    __shared__ uint4_t s_cols[P][kGroups * (BN + 1)], s_rows[kGroups * (BM + 1)];
+    __shared__ uint4_t s_cols[P][kTile<T, BN>], s_rows[kTile<T, BM>];
     __shared__ int s_id[2][BK];
 
     // Block b runs on XCD b % 8: the tiles of a chunk, which share its rows, follow each other on one.
-    const int btiles = ((NARROW ? q.r : q.B) + BN - 1) / BN, tiles = btiles * ((q.A + BM - 1) / BM);
+    const int B = NARROW ? q.r : q.B;
+    const int btiles = (B + BN - 1) / BN, tiles = btiles * ((q.A + BM - 1) / BM);
     const int on_xcd = blockIdx.x / 8, tile = on_xcd % tiles;
     const int64_t chunk = (int64_t)(on_xcd / tiles) * 8 + blockIdx.x % 8;
     const Tile t = find_tile(o, shift, chunk);
     if (t.g < 0 || t.g >= o.G) return;
-    const int B = NARROW ? q.r : q.B;
-    const int W = narrow_width<T>(B);
+    const int W = narrow_width(B);
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int a0 = tile / btiles * BM, b0 = tile % btiles * BN;
     const int wr = wave % WR, wc = wave / WR;
     const int r0 = wr * (BM / WR), c0w = wc * (BN / WC);
 
-    // lanes 4 l .. 4 l + 3 of an operand, k-group g
-    const int al = tid % (BM / 4), ag = tid / (BM / 4);
-    const int bl = tid % (BN / 4), bg = tid / (BN / 4);
-    F ar[U], br[P][U];
+    // lanes CW l .. CW l + CW - 1 of an operand, k-group g
+    const int al = tid % (BM / CW), ag = tid / (BM / CW);
+    const int bl = tid % (BN / CW), bg = tid / (BN / CW);
+    uint2_t ar[8], br[P][8];
+    bool lose = false;
     int id = -1;
     const int steps = (int)((t.p1 - t.p0 + BK - 1) / BK);
     auto fetch_ids = [&](int s) {
@@ -53,46 +53,46 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     };
     auto fetch = [&](int s) {
         const int *const ids = s_id[s & 1];
-        if (ag < kGroups) {
+        if (ag < KG) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int row = ids[ag * U + u];
-                const int c = a0 + 4 * al;
-                ar[u] = load_four<T, VEC>(static_cast<const T *>(q.a) + (row < 0 ? 0 : row * q.a_stride) + c,
-                                          row < 0 ? 0 : q.A - c);
+            for (int u = 0; u < 8; ++u) {
+                const int row = ids[ag * kU + u];
+                const int c = a0 + CW * al;
+                ar[u] = load_8<T, VEC>(static_cast<const T *>(q.a) + (row < 0 ? 0 : row * q.a_stride) + c,
+                                       row < 0 ? 0 : q.A - c);
             }
         }
-        if (bg < kGroups) {
+        if (bg < KG) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int row = ids[bg * U + u];
-                const int c = b0 + 4 * bl;
+            for (int u = 0; u < 8; ++u) {
+                const int row = ids[bg * kU + u];
+                const int c = b0 + CW * bl;
                 if (NARROW) {
-                    const int64_t pos = t.p0 + (int64_t)s * BK + bg * U + u;
+                    const int64_t pos = t.p0 + (int64_t)s * BK + bg * kU + u;
 #pragma unroll
                     for (int e = 0; e < P; ++e)
-                        br[e][u] = load_four<T, true>(static_cast<const T *>(q.h) + (pos * P + e) * W + c,
-                                                      row < 0 ? 0 : W - c);
+                        br[e][u] = load_8<T, true>(static_cast<const T *>(q.h) + (pos * P + e) * W + c,
+                                                   row < 0 ? 0 : W - c);
                 } else {
-                    br[0][u] = load_four<T, VEC>(static_cast<const T *>(q.b) + (row < 0 ? 0 : row * q.b_stride) + c,
-                                                 row < 0 ? 0 : B - c);
+                    br[0][u] = load_8<T, VEC>(static_cast<const T *>(q.b) + (row < 0 ? 0 : row * q.b_stride) + c,
+                                              row < 0 ? 0 : B - c);
                 }
             }
         }
     };
     auto stage = [&]() {
-        uint4_t u[4];
-        if (ag < kGroups) {
-            transpose4(ar, u);
+        uint4_t u[CW][Q];
+        if (ag < KG) {
+            to_units(ar, u, lose);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s_rows[ag * (BM + 1) + place(4 * al + j)] = u[j];
+            for (int j = 0; j < CW; ++j) put<T, BM>(s_rows, KG, ag, place<T>(CW * al + j), u[j]);
         }
-        if (bg < kGroups) {
+        if (bg < KG) {
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                transpose4(br[e], u);
+                to_units(br[e], u, lose);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s_cols[e][bg * (BN + 1) + place(4 * bl + j)] = u[j];
+                for (int j = 0; j < CW; ++j) put<T, BN>(s_cols[e], KG, bg, place<T>(CW * bl + j), u[j]);
             }
         }
     };
@@ -121,35 +121,56 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                 fetch_ids(s + 2);
             }
 #pragma unroll
-            for (int e = 0; e < P; ++e)
-                step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0);
+            for (int e = 0; e < P; ++e) step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0);
         }
     }
     const bool whole = t.end - t.start <= ((int64_t)1 << shift);
     const int64_t cells = (int64_t)q.A * B;
     const int64_t slot = 2 * (t.start >> shift) + ((t.p0 - t.start) >> shift);
+    T *const out = static_cast<T *>(q.out) + t.g * cells;
+    float *const part = slots + (whole ? 0 : slot * cells);
+    if constexpr (Q > 1) {
+        if (__syncthreads_or(lose)) {  // values outside the range of parts: plain fp32 sums
+            const int na = q.A - a0 < BM ? q.A - a0 : BM, nb = B - b0 < BN ? B - b0 : BN;
+            for (int e = tid; e < na * nb; e += kThreads) {
+                const int i = a0 + e / nb, c = b0 + e % nb;
+                float sum = 0.f;
+                for (int64_t pos = t.p0; pos < t.p1; ++pos) {
+                    const int row = row_at(o, pos);
+                    if (row < 0) continue;
+                    const float y = NARROW ? narrow_at<float>(q.h, pos, W, c)
+                                           : static_cast<const float *>(q.b)[row * q.b_stride + c];
+                    sum += static_cast<const float *>(q.a)[row * q.a_stride + i] * y;
+                }
+                const int64_t at = q.transposed ? (int64_t)c * q.A + i : (int64_t)i * B + c;
+                if (whole) out[at] = (T)sum;
+                else part[at] = sum;
+            }
+            return;
+        }
+    }
 #pragma unroll
     for (int r = 0; r < TR; ++r) {
-        const int i = a0 + lane_of(r0 + 32 * r + (lane & 31));
+        const int i = a0 + lane_of<T>(r0 + 32 * r + (lane & 31));
         if (i >= q.A) continue;
 #pragma unroll
         for (int c = 0; c < TC; ++c)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const int col = b0 + c0w + 32 * c + vec_col<true>(v, half);
-                const float4_t x = vec_val<true>(acc[c][r], v);
+                const int col = b0 + c0w + 32 * c + vec_col<T, true>(v, half);
+                const float4_t x = vec_val<T, true>(acc[c][r], v);
                 if (q.transposed) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (col + e < B) {
                             const int64_t at = (int64_t)(col + e) * q.A + i;
-                            if (whole) static_cast<T *>(q.out)[t.g * cells + at] = (T)x[e];
-                            else slots[slot * cells + at] = x[e];
+                            if (whole) out[at] = (T)x[e];
+                            else part[at] = x[e];
                         }
                 } else {
                     const int64_t at = (int64_t)i * B + col;
-                    if (whole) store_four<VEC>(static_cast<T *>(q.out) + t.g * cells + at, x, B - col);
-                    else store_four<VEC>(slots + slot * cells + at, x, B - col);
+                    if (whole) store_four<VEC>(out + at, x, B - col);
+                    else store_four<VEC>(part + at, x, B - col);
                 }
             }
     }
@@ -238,8 +259,9 @@ template <typename T, int BM, int BN, int WR>
 hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, float *slots, hipStream_t s)
 {
     const int B = q.r > 0 ? q.r : q.B;
-    const bool vec = unit_aligned<T>(q.a, q.a_stride) && q.A % kU<T> == 0 && B % kU<T> == 0 &&
-                     unit_aligned<T>(q.out, 0) && (q.r > 0 || unit_aligned<T>(q.b, q.b_stride));
+    constexpr int V = 16 / (int)sizeof(T);
+    const bool vec = aligned_rows<T>(q.a, q.a_stride) && q.A % V == 0 && B % V == 0 &&
+                     aligned_rows<T>(q.out, 0) && (q.r > 0 || aligned_rows<T>(q.b, q.b_stride));
     const int64_t chunks = ((o.n >> sh.shift) + o.G + 7) / 8 * 8;
     if (chunks * sh.tiles > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     auto *kernel = q.r > 0 ? (vec ? k_row_outer<T, BM, BN, WR, true, true> : k_row_outer<T, BM, BN, WR, false, true>)

@@ -22,14 +22,14 @@ using namespace rows;
 template <typename T, bool WNK, int BM, int BN, int WR, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits, bool v_vec)
 {
-    constexpr int U = kU<T>, BK = kStep<T>, P = kParts<T>;
+    constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
     constexpr int kShift = BM == 128 ? 7 : BM == 64 ? 6 : 5;
     static_assert(BM == 1 << kShift && TR >= 1 && TC >= 1, "tile");
-    constexpr int NR = BM * kGroups / kThreads;        // units of the rows a thread stages
-    constexpr int NC = BN * kGroups / kThreads;        // units of [N][K] weights
-    typedef typename Four<T>::t F;
-    __shared__ uint4_t s_cols[kGroups * (BN + 1)], s_rows[kGroups * (BM + 1)];
+    constexpr int kLanes = kThreads / KG;              // rows staged at once
+    constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
+    constexpr int NC = BN / kLanes > 0 ? BN / kLanes : 1;
+    __shared__ uint4_t s_cols[kTile<T, BN>], s_rows[kTile<T, BM>];
     __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg;
 
     const bool shared_w = p.w_group == 0;
@@ -50,41 +50,41 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     const int ct0 = (int)((int64_t)ctiles * blockIdx.y / splits);
     const int ct1 = (int)((int64_t)ctiles * (blockIdx.y + 1) / splits);
     if (ct0 >= ct1) return;
+    const int col_end = ct1 * BN < p.N ? ct1 * BN : p.N;
 
     if (tid < BM) s_row[tid] = tid < rows ? row_at(o, t.p0 + tid) : -1;
     if (!shared_w && t.g == o.G) {  // rows of no group
         if (p.narrow) return;
         __syncthreads();
-        store_zeros<T>(p, s_row, rows, ct0 * BN, ct1 * BN < p.N ? ct1 * BN : p.N);
+        store_zeros<T>(p, s_row, rows, ct0 * BN, col_end);
         return;
     }
     int nseg = 0;
     if (shared_w && p.h) nseg = find_segments<BM>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
     __syncthreads();
 
-    // the row units this thread stages: k-group tid % 8 of rows tid / 8 + 32 i
-    const int kg = tid & 7, rr = tid >> 3;
+    // rows of the input, and of [N][K] weights: k-group tid % KG of lanes tid / KG + kLanes i
+    const int kg = tid % KG, rr = tid / KG;
     const T *in[NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-        const int row = s_row[rr + 32 * i];
-        in[i] = row >= 0 ? static_cast<const T *>(p.in) + row * p.in_stride + kg * U : nullptr;
+        const int r = rr + kLanes * i, row = r < BM ? s_row[r] : -1;
+        in[i] = row >= 0 ? static_cast<const T *>(p.in) + row * p.in_stride + kg * kU : nullptr;
     }
     const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
-    const int W = narrow_width<T>(p.r);  // of a part of the narrow input
+    const int W = narrow_width(p.r);  // of a part of the narrow input
+    // transposed weights: columns CW tc .. CW tc + CW - 1, k-group tg
+    const int tc = tid % (BN / CW), tg = tid / (BN / CW);
 
-    // transposed weights: columns 4 tc .. 4 tc + 3, k-group tg
-    const int tc = tid % (BN / 4), tg = tid / (BN / 4);
-
-    uint4_t xr[NR], wn[WNK ? NC : 1];
-    F wt[WNK ? 1 : U];
+    Raw8<T> xr[NR], wn[WNK ? NC : 1];
+    uint2_t wt[8];
+    bool lose = false;
     // the loads of step k of column tile ct; seg < 0: the shared weights, else an adapter
     auto fetch = [&](int ct, int seg, int k) {
         const int c0 = ct * BN;
         int K = p.K;
         const T *wb = w;
         int wk = p.K;  // k of the weights from which on there are none
-        int kw = k;    // k in the weights
         if (seg >= 0) {
             K = P * W;
             wb = static_cast<const T *>(p.v) + (int64_t)s_seg_g[seg] * p.r * p.N;
@@ -92,46 +92,56 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
             const int at = s_seg_at[seg], end = s_seg_at[seg + 1];
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
-                const int r = rr + 32 * i;
-                const int left = r >= at && r < end && s_row[r] >= 0 ? K - k - kg * U : 0;
-                xr[i] = load_unit<T, true>(static_cast<const T *>(p.h) + (t.p0 + r) * K + k + kg * U, left);
+                const int r = rr + kLanes * i;
+                const int left = r >= at && r < end && in[i] ? K - k - kg * kU : 0;
+                xr[i] = load_row8<T, true>(static_cast<const T *>(p.h) + (t.p0 + r) * K + k + kg * kU, left);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < NR; ++i) xr[i] = load_unit<T, VEC>(in[i] + k, in[i] ? K - k - kg * U : 0);
+            for (int i = 0; i < NR; ++i) xr[i] = load_row8<T, VEC>(in[i] + k, in[i] ? K - k - kg * kU : 0);
         }
         if constexpr (WNK) {
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                const int c = c0 + rr + 32 * i;
-                int kk = kw + kg * U;
+                const int c = c0 + rr + kLanes * i;
+                int kk = k + kg * kU;
+                const bool in_k = kk < K && rr + kLanes * i < BN;
                 if (seg >= 0 && P == 2 && kk >= W) kk -= W;  // the second part meets the same weights
                 const T *const q = wb + (int64_t)c * wk + kk;
-                const int left = c < p.N && k + kg * U < K ? wk - kk : 0;
-                if (seg >= 0 && !v_vec) wn[i] = load_unit<T, false>(q, left);
-                else wn[i] = load_unit<T, VEC>(q, left);
+                const int left = c < p.N && in_k ? wk - kk : 0;
+                if (seg >= 0 && !v_vec) wn[i] = load_row8<T, false>(q, left);
+                else wn[i] = load_row8<T, VEC>(q, left);
             }
-        } else if (tg < kGroups) {
-            const int c = c0 + 4 * tc;
-            int kk = kw + tg * U;
-            const bool in_k = k + tg * U < K;
+        } else if (tg < KG) {
+            const int c = c0 + CW * tc;
+            int kk = k + tg * kU;
+            const bool in_k = kk < K;
             if (seg >= 0 && P == 2 && kk >= W) kk -= W;
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                wt[u] = load_four<T, VEC>(wb + (int64_t)(kk + u) * p.N + c, in_k && kk + u < wk ? p.N - c : 0);
+            for (int u = 0; u < 8; ++u)
+                wt[u] = load_8<T, VEC>(wb + (int64_t)(kk + u) * p.N + c, in_k && kk + u < wk ? p.N - c : 0);
         }
     };
     auto stage = [&]() {
+        uint4_t u[Q];
 #pragma unroll
-        for (int i = 0; i < NR; ++i) s_rows[kg * (BM + 1) + rr + 32 * i] = xr[i];
+        for (int i = 0; i < NR; ++i) {
+            if (BM < kLanes && rr >= BM) break;
+            to_units(xr[i], u, lose);
+            put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
+        }
         if constexpr (WNK) {
 #pragma unroll
-            for (int i = 0; i < NC; ++i) s_cols[kg * (BN + 1) + rr + 32 * i] = wn[i];
-        } else if (tg < kGroups) {
-            uint4_t u[4];
-            transpose4(wt, u);
+            for (int i = 0; i < NC; ++i) {
+                if (BN < kLanes && rr >= BN) break;
+                to_units(wn[i], u, lose);
+                put<T, BN>(s_cols, KG, kg, rr + kLanes * i, u);
+            }
+        } else if (tg < KG) {
+            uint4_t c[CW][Q];
+            to_units(wt, c, lose);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s_cols[tg * (BN + 1) + place(4 * tc + j)] = u[j];
+            for (int j = 0; j < CW; ++j) put<T, BN>(s_cols, KG, tg, place<T>(CW * tc + j), c[j]);
         }
     };
 
@@ -166,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         const int c0 = now * BN + c0w;
         if (p.narrow) {
             const float scale = p.narrow_scale ? p.narrow_scale[t.g] : 1.f;
-            const int No = narrow_width<T>(p.N);
+            const int No = narrow_width(p.N);
 #pragma unroll
             for (int r = 0; r < TR; ++r) {
                 const int pl = r0 + 32 * r + (lane & 31);
@@ -176,8 +186,8 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
                 for (int c = 0; c < TC; ++c)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const int col = c0 + 32 * c + vec_col<!WNK>(v, half);
-                        float4_t x = vec_val<!WNK>(acc[c][r], v);
+                        const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
+                        float4_t x = vec_val<T, !WNK>(acc[c][r], v);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = col + e < p.N ? x[e] * scale : 0.f;
                         if (col < No) store_narrow(q + col, No, x);
@@ -193,21 +203,26 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
                 for (int c = 0; c < TC; ++c)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const int col = c0 + 32 * c + vec_col<!WNK>(v, half);
-                        store_four<VEC>(q + col, vec_val<!WNK>(acc[c][r], v), p.N - col);
+                        const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
+                        store_four<VEC>(q + col, vec_val<T, !WNK>(acc[c][r], v), p.N - col);
                     }
             }
         }
+    }
+    if constexpr (Q > 1) {
+        __threadfence_block();
+        if (__syncthreads_or(lose)) row_plain_sums<WNK>(o, p, t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end);
     }
 }
 
 template <typename T, bool WNK, int BM, int BN, int WR>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    const bool vec = unit_aligned<T>(p.in, p.in_stride) && p.K % kU<T> == 0 && p.N % kU<T> == 0 &&
-                     unit_aligned<T>(p.w, 0) && (p.narrow || unit_aligned<T>(p.out, p.out_stride)) &&
-                     (!p.h || unit_aligned<T>(p.v, 0));
-    const bool v_vec = vec && p.r % kU<T> == 0;  // rows of r adapter weights
+    constexpr int V = 16 / (int)sizeof(T);
+    const bool vec = aligned_rows<T>(p.in, p.in_stride) && p.K % V == 0 && p.N % V == 0 &&
+                     aligned_rows<T>(p.w, 0) && (p.narrow || aligned_rows<T>(p.out, p.out_stride)) &&
+                     (!p.h || aligned_rows<T>(p.v, 0));
+    const bool v_vec = vec && p.r % V == 0;  // rows of r adapter weights
     const int64_t tiles = p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
     const int ctiles = (p.N + BN - 1) / BN;
     // few rows: column tiles go to workgroups of their own
@@ -234,8 +249,7 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 
 size_t narrow_bytes(int dtype, int64_t n_rows, int N)
 {
-    return dtype == CGTP_BF16 ? (size_t)n_rows * narrow_width<bf16_t>(N) * 4
-                              : (size_t)n_rows * narrow_width<float>(N) * 4;
+    return (size_t)n_rows * narrow_width(N) * 4;  // one fp32 or two bf16
 }
 
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)

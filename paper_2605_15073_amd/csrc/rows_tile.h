@@ -1,16 +1,23 @@
-// Tiles of the row products in LDS and registers, shared by the kernels of rows_product.hip and
-// rows_outer.hip.
+// Tiles of the row products in LDS and registers, shared by rows_product.hip, rows_outer.hip and
+// rows_wide.hip.
 //
 // An operand tile of R lanes (rows of the input, columns of the weights, ...) by kGroups k-groups is
-// held in 16-byte units of consecutive k: kU = 8 bf16 or 4 fp32 values. Unit (kg, r) lies at
-// kg (R + 1) + r, so that the 32 lanes of a matrix instruction's half read consecutive units and the
-// eight lanes that stage one row's eight units hit different banks.
+// held in 16-byte units of 8 consecutive k in bf16. Unit (kg, r) lies at kg (R + 1) + r, so that the 32
+// lanes of a matrix instruction's half read consecutive units and the eight lanes that stage one row's
+// units hit different banks.
 //
-// Operands whose k is contiguous in memory are staged a unit a load. The others (weights of the
-// forward product, both operands of a weight gradient) are loaded four lanes wide, kU rows deep and
-// transposed in registers; the four units of a thread then go to places 8 apart within a block of 32
-// (place()), so that neighbouring threads write neighbouring units. The matrix instruction does not
-// care which lane carries which column: lane_of() gives the column that a place holds.
+// fp32 operands are three bf16 parts each, x = h + m + l (24 bits of significand), and a product is hh,
+// hm, mh, mm, hl, lh, summed in fp32: six matrix instructions for 16 k, where the fp32 ones take eight
+// of twice the time; what is left out is below 2^-24 of the term. The parts are exact where the third is
+// no smaller than bf16's smallest step, 2^-133, so from 2^-109 on, and up to bf16's largest value; an
+// infinity has none. A workgroup that meets eight values that all lose bits, or one above the range
+// (parts_lose), forms its sums again in plain fp32.
+//
+// Operands whose k is contiguous in memory are staged eight k a load. The others (weights of the
+// forward product, both operands of a weight gradient) are loaded 8 bytes wide (kWide lanes), 8 rows
+// deep, and transposed in registers; the units of a thread then go to places 32 / kWide apart within a
+// block of 32 (place()), so that neighbouring threads write neighbouring units. The matrix instruction
+// does not care which lane carries which column: lane_of() gives the column that a place holds.
 #ifndef CGTP_ROWS_TILE_H
 #define CGTP_ROWS_TILE_H
 
@@ -29,10 +36,13 @@ typedef bf16_t bf4_t __attribute__((ext_vector_type(4)));
 typedef bf16_t bf8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
-constexpr int kGroups = 8;  // k-groups of a step
+constexpr int kU = 8;  // k of a unit
 
-template <typename T> constexpr int kU = 16 / (int)sizeof(T);
-template <typename T> constexpr int kStep = kGroups * kU<T>;  // k of a step: 64 bf16, 32 fp32
+template <typename T> constexpr int kSplit = sizeof(T) == 2 ? 1 : 3;   // parts of an operand
+template <typename T> constexpr int kGroups = sizeof(T) == 2 ? 8 : 4;  // k-groups of a step
+template <typename T> constexpr int kStep = kGroups<T> * kU;           // k of a step: 64 bf16, 32 fp32
+template <typename T> constexpr int kWide = 8 / (int)sizeof(T);        // lanes of a transposed load
+template <typename T, int R> constexpr int kTile = kSplit<T> * kGroups<T> * (R + 1);  // units of a tile
 
 __device__ __forceinline__ int clamp_offset(int v, int64_t n)
 {
@@ -127,9 +137,9 @@ __device__ __forceinline__ int find_segments(const RowOrder &o, int64_t p0, int 
     return n;
 }
 
-// One unit: kU values from p on, zero past the `left` that exist.
+// 16 bytes of values from p on, zero past the `left` that exist.
 template <typename T, bool VEC>
-__device__ __forceinline__ uint4_t load_unit(const T *p, int64_t left)
+__device__ __forceinline__ uint4_t load_16(const T *p, int64_t left)
 {
     uint4_t v = {0, 0, 0, 0};
     if (VEC) {
@@ -151,21 +161,16 @@ __device__ __forceinline__ uint4_t load_unit(const T *p, int64_t left)
     return v;
 }
 
-// Four consecutive values, as loaded: 16 or 8 bytes.
-template <typename T> struct Four;
-template <> struct Four<float> { typedef uint4_t t; };
-template <> struct Four<bf16_t> { typedef uint2_t t; };
-
+// The same for 8 bytes: kWide values.
 template <typename T, bool VEC>
-__device__ __forceinline__ typename Four<T>::t load_four(const T *p, int64_t left)
+__device__ __forceinline__ uint2_t load_8(const T *p, int64_t left)
 {
-    typedef typename Four<T>::t F;
-    F v = {};
+    uint2_t v = {0, 0};
     if (VEC) {
-        if (left > 0) v = *reinterpret_cast<const F *>(p);
+        if (left > 0) v = *reinterpret_cast<const uint2_t *>(p);
     } else if (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 2; ++e)
             if (left > e) v[e] = reinterpret_cast<const unsigned *>(p)[e];
     } else {
         const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
@@ -180,41 +185,119 @@ __device__ __forceinline__ typename Four<T>::t load_four(const T *p, int64_t lef
     return v;
 }
 
-// The units of four lanes from kU loads of four values each.
-__device__ __forceinline__ void transpose4(const uint4_t (&in)[4], uint4_t (&out)[4])
+// Eight consecutive k of a lane as loaded: one unit of bf16, or 32 bytes of fp32.
+template <typename T> struct Raw8 { uint4_t v[sizeof(T) / 2]; };
+
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw8<T> load_row8(const T *p, int64_t left)
 {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = uint4_t{in[0][j], in[1][j], in[2][j], in[3][j]};
+    Raw8<T> r;
+    r.v[0] = load_16<T, VEC>(p, left);
+    if constexpr (sizeof(T) == 4) r.v[1] = load_16<T, VEC>(p + 4, left - 4);
+    return r;
 }
 
-__device__ __forceinline__ void transpose4(const uint2_t (&in)[8], uint4_t (&out)[4])
+// The largest of m, |a| and |b| (fmaxf would first quieten each operand, an instruction of its own).
+__device__ __forceinline__ void max_abs(float &m, float a, float b)
+{
+    asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(m) : "v"(a), "v"(b));
+}
+
+// Whether parts lose bits of values whose largest magnitude is m (a maximum that skips NaN, which parts
+// propagate): all of them below the range (one inside dwarfs what the others lose, 2^-134 each), or one
+// above it.
+__device__ __forceinline__ bool parts_lose(float m) { return (m < 0x1p-104f && m != 0.f) || m > 0x1.fep127f; }
+
+// The three parts of eight values.
+__device__ __forceinline__ void split8(const float (&x)[8], uint4_t (&part)[3], bool &lose)
+{
+    float m = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        max_abs(m, x[2 * k], x[2 * k + 1]);
+        float r0 = x[2 * k], r1 = x[2 * k + 1];
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+            const bf2_t b = {(bf16_t)r0, (bf16_t)r1};
+            const unsigned bits = __builtin_bit_cast(unsigned, b);
+            part[c][k] = bits;
+            r0 -= __builtin_bit_cast(float, bits << 16);
+            r1 -= __builtin_bit_cast(float, bits & 0xffff0000u);
+        }
+    }
+    lose |= parts_lose(m);
+}
+
+// The units of a lane's eight k.
+__device__ __forceinline__ void to_units(const Raw8<bf16_t> &raw, uint4_t (&u)[1], bool &) { u[0] = raw.v[0]; }
+__device__ __forceinline__ void to_units(const Raw8<float> &raw, uint4_t (&u)[3], bool &lose)
+{
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, (unsigned)raw.v[e / 4][e % 4]);
+    split8(x, u, lose);
+}
+
+// The units of kWide lanes from 8 loads of 8 bytes.
+__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[4][1], bool &)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned a = in[2 * e][j >> 1], b = in[2 * e + 1][j >> 1];
-            out[j][e] = __builtin_amdgcn_perm(b, a, (j & 1) ? 0x07060302u : 0x05040100u);
-        }
+        for (int e = 0; e < 4; ++e)
+            u[j][0][e] = __builtin_amdgcn_perm(in[2 * e + 1][j >> 1], in[2 * e][j >> 1],
+                                               (j & 1) ? 0x07060302u : 0x05040100u);
+}
+
+__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[2][3], bool &lose)
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, (unsigned)in[e][j]);
+        split8(x, u[j], lose);
+    }
+}
+
+// Writes a lane's units, all parts of k-group kg, to place r of a tile of R.
+template <typename T, int R>
+__device__ __forceinline__ void put(uint4_t *tile, int groups, int kg, int r, const uint4_t (&u)[kSplit<T>])
+{
+#pragma unroll
+    for (int c = 0; c < kSplit<T>; ++c) tile[(c * groups + kg) * (R + 1) + r] = u[c];
 }
 
 // Where a transposed operand's lane r lies in its block of 32, and which lane a place holds.
-__device__ __forceinline__ int place(int r) { return (r & ~31) | (r & 3) << 3 | (r >> 2 & 7); }
-__device__ __forceinline__ int lane_of(int p) { return (p & ~31) | (p & 7) << 2 | (p >> 3 & 3); }
+template <typename T> __device__ __forceinline__ int place(int r)
+{
+    return sizeof(T) == 2 ? (r & ~31) | (r & 3) << 3 | (r >> 2 & 7) : (r & ~31) | (r & 1) << 4 | (r >> 1 & 15);
+}
+template <typename T> __device__ __forceinline__ int lane_of(int p)
+{
+    return sizeof(T) == 2 ? (p & ~31) | (p & 7) << 2 | (p >> 3 & 3) : (p & ~31) | (p & 15) << 1 | (p >> 4 & 1);
+}
 
-// acc += A B for one unit of each lane: lanes 0..31 carry k-group 2 s, lanes 32..63 2 s + 1.
-__device__ __forceinline__ void mma(float16_t &acc, uint4_t a, uint4_t b, bf16_t)
+__device__ __forceinline__ void mfma(float16_t &acc, uint4_t a, uint4_t b)
 {
     acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8_t, a),
                                                   __builtin_bit_cast(bf8_t, b), acc, 0, 0, 0);
 }
 
-__device__ __forceinline__ void mma(float16_t &acc, uint4_t a, uint4_t b, float)
+// acc += A B for one unit of each lane (lanes 0..31 carry k-group 2 s, lanes 32..63 2 s + 1), the smallest
+// terms first.
+__device__ __forceinline__ void mma(float16_t &acc, const uint4_t (&a)[1], const uint4_t (&b)[1])
 {
-    const float4_t x = __builtin_bit_cast(float4_t, a), y = __builtin_bit_cast(float4_t, b);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
+    mfma(acc, a[0], b[0]);
+}
+__device__ __forceinline__ void mma(float16_t &acc, const uint4_t (&a)[3], const uint4_t (&b)[3])
+{
+    mfma(acc, a[0], b[2]);
+    mfma(acc, a[2], b[0]);
+    mfma(acc, a[1], b[1]);
+    mfma(acc, a[0], b[1]);
+    mfma(acc, a[1], b[0]);
+    mfma(acc, a[0], b[0]);
 }
 
 // The products of a step: TC blocks of 32 columns (from unit column c0 of cols) by TR blocks of 32
@@ -225,31 +308,39 @@ template <typename T, int BN, int BM, int TC, int TR>
 __device__ __forceinline__ void step_products(float16_t (&acc)[TC][TR], const uint4_t *cols,
                                               const uint4_t *rws, int c0, int r0)
 {
+    constexpr int Q = kSplit<T>, KG = kGroups<T>;
     const int lane = threadIdx.x & 63, half = lane >> 5, n = lane & 31;
 #pragma unroll
-    for (int s = 0; s < kGroups / 2; ++s) {
-        uint4_t a[TC], b[TR];
+    for (int s = 0; s < KG / 2; ++s) {
+        uint4_t a[TC][Q], b[TR][Q];
 #pragma unroll
-        for (int c = 0; c < TC; ++c) a[c] = cols[(2 * s + half) * (BN + 1) + c0 + 32 * c + n];
+        for (int q = 0; q < Q; ++q) {
 #pragma unroll
-        for (int r = 0; r < TR; ++r) b[r] = rws[(2 * s + half) * (BM + 1) + r0 + 32 * r + n];
+            for (int c = 0; c < TC; ++c) a[c][q] = cols[(q * KG + 2 * s + half) * (BN + 1) + c0 + 32 * c + n];
+#pragma unroll
+            for (int r = 0; r < TR; ++r) b[r][q] = rws[(q * KG + 2 * s + half) * (BM + 1) + r0 + 32 * r + n];
+        }
 #pragma unroll
         for (int c = 0; c < TC; ++c)
 #pragma unroll
-            for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r], T{});
+            for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r]);
     }
 }
 
-// Four consecutive columns of a lane's row: the first of vector v, and the values. With a
-// transposed column operand they are the accumulators 4 apart.
-template <bool TRANS>
-__device__ __forceinline__ int vec_col(int v, int half) { return TRANS ? 4 * (4 * half + v) : 8 * v + 4 * half; }
-
-template <bool TRANS>
-__device__ __forceinline__ float4_t vec_val(const float16_t &acc, int v)
+// Four consecutive columns of a lane's row, v = 0..3: the first of them, and the values. With a
+// transposed column operand they come from the places that place() gives them.
+template <typename T, bool TRANS> __device__ __forceinline__ int vec_col(int v, int half)
 {
-    return TRANS ? float4_t{acc[v], acc[4 + v], acc[8 + v], acc[12 + v]}
-                 : float4_t{acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]};
+    if (!TRANS) return 8 * v + 4 * half;
+    return sizeof(T) == 2 ? 4 * (4 * half + v) : 4 * (2 * half + (v & 1) + 4 * (v >> 1));
+}
+
+template <typename T, bool TRANS> __device__ __forceinline__ float4_t vec_val(const float16_t &acc, int v)
+{
+    if (!TRANS) return float4_t{acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]};
+    if (sizeof(T) == 2) return float4_t{acc[v], acc[4 + v], acc[8 + v], acc[12 + v]};
+    const int i = 4 * (v >> 1) + 2 * (v & 1);
+    return float4_t{acc[i], acc[i + 8], acc[i + 1], acc[i + 9]};
 }
 
 // Stores four consecutive values, of which `left` exist.
@@ -289,8 +380,41 @@ __device__ __forceinline__ void store_zeros(const RowProduct &p, const int *row,
 // Results of narrow products (width N <= 64, between the two products of an adapter), in sequence
 // order: fp32 [n][W], or for bf16 two parts hi + lo [n][2][W], 16 bits of significand; W is N
 // rounded up to a unit, the rest zero.
-template <typename T> __host__ __device__ constexpr int narrow_width(int N) { return (N + kU<T> - 1) / kU<T> * kU<T>; }
-template <typename T> constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
+__host__ __device__ constexpr int narrow_width(int N) { return (N + kU - 1) / kU * kU; }
+template <typename T> constexpr int kNarrow = sizeof(T) == 2 ? 2 : 1;
+
+template <typename T> __device__ __forceinline__ float narrow_at(const void *h, int64_t pos, int W, int k)
+{
+    const T *const p = static_cast<const T *>(h) + pos * (kNarrow<T> * W) + k;
+    return sizeof(T) == 2 ? (float)p[0] + (float)p[W] : (float)p[0];
+}
+
+// The sums of a workgroup that met values outside the range of parts, in plain fp32: columns [c0, c1) of its
+// rows, one result a thread at a time.
+template <bool WNK>
+__device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group, int64_t p0, int rows, const int *s_row,
+                               const int *s_g, int c0, int c1)
+{
+    const int W = narrow_width(p.r), width = c1 - c0;
+    const float *const w = static_cast<const float *>(p.w) + (int64_t)group * p.w_group;
+    for (int e = threadIdx.x; e < rows * width; e += kThreads) {
+        const int r = e / width, c = c0 + e % width;
+        if (s_row[r] < 0) continue;
+        const float *const in = static_cast<const float *>(p.in) + s_row[r] * p.in_stride;
+        float sum = 0.f;
+        for (int k = 0; k < p.K; ++k) sum += in[k] * w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c];
+        if (p.h && s_g[r] < o.G) {
+            const float *const v = static_cast<const float *>(p.v) + (int64_t)s_g[r] * p.r * p.N;
+            for (int k = 0; k < p.r; ++k)
+                sum += narrow_at<float>(p.h, p0 + r, W, k) * v[WNK ? (int64_t)c * p.r + k : (int64_t)k * p.N + c];
+        }
+        if (p.narrow)
+            static_cast<float *>(p.out)[(p0 + r) * narrow_width(p.N) + c] =
+                p.narrow_scale ? sum * p.narrow_scale[group] : sum;
+        else
+            static_cast<float *>(p.out)[s_row[r] * p.out_stride + c] = sum;
+    }
+}
 
 __device__ __forceinline__ void store_narrow(float *p, int W, float4_t v)
 {
@@ -310,9 +434,10 @@ __device__ __forceinline__ void store_narrow(bf16_t *p, int W, float4_t v)
     *reinterpret_cast<bf4_t *>(p + W) = lo;
 }
 
-template <typename T> bool unit_aligned(const void *p, int64_t stride)
+// Whether rows at this stride start on 16-byte boundaries.
+template <typename T> bool aligned_rows(const void *p, int64_t stride)
 {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % kU<T> == 0;
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (int64_t)sizeof(T) % 16 == 0;
 }
 
 }  // namespace rows

@@ -26,12 +26,14 @@ using namespace rows;
 
 constexpr int kRows = 128;    // positions of a workgroup, 32 a wave
 constexpr int kCols = 64;     // columns of a tile
-constexpr int kPairs = 8;     // pairs of k-groups at most: inputs of up to 128 bf16 or 64 fp32
-constexpr int kExtPairs = 4;  // of a narrow product's rows
+template <typename T> constexpr int kPairs = sizeof(T) == 2 ? 8 : 4;  // pairs of k-groups: up to 128 bf16, 64 fp32
+template <typename T> constexpr int kExtPairs = sizeof(T) == 2 ? 4 : 2;  // of a narrow product's rows, up to 32 wide
 
-// Row stride of the turned results, in values: a multiple of their vectors, clear of bank conflicts
-// between the rows that the 8 (fp32, 16 bytes) or 16 (bf16, 8 bytes) lanes of a cycle write.
-template <typename T> constexpr int kTurn = kCols + 4;
+// The results are turned 64 (bf16) or 32 (fp32) columns at a time, 128 bytes a row. Row stride of the turned
+// results, in values: a multiple of their vectors, clear of bank conflicts between the rows that the 8
+// (fp32, 16 bytes) or 16 (bf16, 8 bytes) lanes of a cycle write.
+template <typename T> constexpr int kPiece = 128 / (int)sizeof(T);
+template <typename T> constexpr int kTurn = kPiece<T> + 4;
 
 template <typename T> struct Out4;
 template <> struct Out4<float> { typedef float4_t t; };
@@ -55,12 +57,11 @@ __device__ __forceinline__ void wave_sync()
 template <typename T, bool WNK, int NP, int XP, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p, int splits)
 {
-    constexpr int U = kU<T>, P = kParts<T>, KG = 2 * (NP + XP), LD = kCols + 1;
+    constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, KG = 2 * (NP + XP), LD = kCols + 1, CW = kWide<T>;
     constexpr bool EXT = XP > 0;
-    static_assert(!(EXT && (WNK || !VEC)), "adapters: [K][N] weights, whole vectors");
-    typedef typename Four<T>::t F;
+    static_assert(NP <= kPairs<T> && !(EXT && (WNK || !VEC)), "adapters: [K][N] weights, whole vectors");
     typedef typename Out4<T>::t O;
-    __shared__ uint4_t s_w[KG * LD];
+    __shared__ uint4_t s_w[Q * KG * LD];
     __shared__ O s_turn[4 * 32 * kTurn<T> / 4];
     __shared__ int s_row[kRows], s_place[kRows], s_any;
     __shared__ int s_g[EXT ? kRows : 1], s_seg_g[EXT ? kRows : 1], s_seg_at[EXT ? kRows + 1 : 1], s_nseg;
@@ -100,42 +101,44 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     // inputs: row 32 wave + lane % 32, k-groups 2 s + half
     const int pl = s_place[32 * wave + (lane & 31)];
     const T *const in = static_cast<const T *>(p.in) + s_row[pl] * p.in_stride;
-    const int W = EXT ? narrow_width<T>(p.r) : 0;
-    uint4_t x[NP], h[EXT ? XP : 1];
+    const int W = EXT ? narrow_width(p.r) : 0;
+    uint4_t x[NP][Q], h[EXT ? XP : 1][Q];
+    bool lose = false;
 #pragma unroll
     for (int s = 0; s < NP; ++s) {
         const int k = (2 * s + half) * U;
-        x[s] = load_unit<T, VEC>(in + k, p.K - k);
+        to_units(load_row8<T, VEC>(in + k, p.K - k), x[s], lose);
     }
     if (EXT) {
         const bool grouped = s_g[pl] < o.G;
 #pragma unroll
         for (int s = 0; s < XP; ++s) {
             const int k = (2 * s + half) * U;
-            h[s] = load_unit<T, true>(static_cast<const T *>(p.h) + (grouped ? (t.p0 + pl) * (P * W) : 0) + k,
-                                      grouped ? P * W - k : 0);
+            const T *const q = static_cast<const T *>(p.h) + (grouped ? (t.p0 + pl) * (P * W) : 0) + k;
+            to_units(load_row8<T, true>(q, grouped ? P * W - k : 0), h[s], lose);
         }
     }
-    // outputs: this lane stores vector lane % 16 of rows 4 i + lane / 16
-    T *out[8];
+    // outputs: of a piece of 128 bytes this lane stores vector lane % kVecs of rows 64 / kVecs i + lane / kVecs
+    constexpr int kVecs = kPiece<T> / 4, kStores = 32 * kVecs / 64;
+    T *out[kStores];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        out[i] = static_cast<T *>(p.out) + s_row[s_place[32 * wave + 4 * i + (lane >> 4)]] * p.out_stride;
+    for (int i = 0; i < kStores; ++i)
+        out[i] = static_cast<T *>(p.out) + s_row[s_place[32 * wave + (64 / kVecs) * i + lane / kVecs]] * p.out_stride;
 
     // Weights. Round 0 of a column tile: the shared ones, with the first adapter's behind them; then the
     // other adapters' of the tile.
-    constexpr int kTasks = (WNK ? kCols : kCols / 4) * KG;  // units, or units of four columns
+    constexpr int kTasks = (WNK ? kCols : kCols / CW) * KG;  // units, or units of CW columns
     constexpr int NT = (kTasks + kThreads - 1) / kThreads;
     const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
-    uint4_t wn[WNK ? NT : 1];
-    F wt[WNK ? 1 : NT][WNK ? 1 : U];
-    unsigned we[VEC ? 1 : NT][VEC ? 1 : U * 4];  // single values, packed when they are staged
+    Raw8<T> wn[WNK ? NT : 1];
+    uint2_t wt[WNK ? 1 : NT][8];
+    unsigned we[VEC || WNK ? 1 : NT][VEC || WNK ? 1 : 8 * CW];  // single values, packed when they are staged
     int have[NT];  // k of the k-groups in flight that the weights have
     auto fetch = [&](int ct, int seg) {
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const int task = tid + kThreads * i;
-            const int g = WNK ? task % KG : task / (kCols / 4);
+            const int g = WNK ? task % KG : task / (kCols / CW);
             int k = g * U, K = p.K;
             const T *wb = w;
             if (EXT && g >= 2 * NP) {
@@ -149,21 +152,25 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             if constexpr (WNK) {
                 const int c = ct * kCols + task / KG;
                 const T *const q = wb + (int64_t)(c < p.N ? c : p.N - 1) * p.K + k;
-                if (VEC) wn[i] = *reinterpret_cast<const uint4_t *>(q);
-                else wn[i] = load_unit<T, false>(q, have[i]);
+                if (VEC) {  // of fp32 the second half of a k-group may be past the end: the first again
+                    wn[i].v[0] = *reinterpret_cast<const uint4_t *>(q);
+                    if constexpr (Q > 1) wn[i].v[1] = *reinterpret_cast<const uint4_t *>(q + (have[i] > 4 ? 4 : 0));
+                } else {
+                    wn[i] = load_row8<T, false>(q, have[i]);
+                }
             } else {
-                const int c = ct * kCols + 4 * (task % (kCols / 4));
+                const int c = ct * kCols + CW * (task % (kCols / CW));
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const T *const q = wb + (int64_t)(u < have[i] ? k + u : 0) * p.N;
                     if constexpr (VEC) {
-                        wt[i][u] = *reinterpret_cast<const F *>(q + (c < p.N ? c : p.N - 4));
+                        wt[i][u] = *reinterpret_cast<const uint2_t *>(q + (c < p.N ? c : p.N - CW));
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
+                        for (int e = 0; e < CW; ++e) {
                             const T *const z = q + (c + e < p.N ? c + e : p.N - 1);
-                            we[i][4 * u + e] = sizeof(T) == 2 ? *reinterpret_cast<const unsigned short *>(z)
-                                                              : *reinterpret_cast<const unsigned *>(z);
+                            we[i][CW * u + e] = sizeof(T) == 2 ? *reinterpret_cast<const unsigned short *>(z)
+                                                               : *reinterpret_cast<const unsigned *>(z);
                         }
                     }
                 }
@@ -176,23 +183,31 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             const int task = tid + kThreads * i;
             if (kTasks % kThreads != 0 && task >= kTasks) continue;
             if constexpr (WNK) {
-                s_w[task % KG * LD + task / KG] = have[i] > 0 ? wn[i] : uint4_t{0, 0, 0, 0};
+                uint4_t unit[Q];
+                Raw8<T> raw = wn[i];
+                if (have[i] <= 0) raw.v[0] = uint4_t{0, 0, 0, 0};
+                if constexpr (Q > 1)
+                    if (have[i] <= 4) raw.v[1] = uint4_t{0, 0, 0, 0};
+                to_units(raw, unit, lose);
+                put<T, kCols>(s_w, KG, task % KG, task / KG, unit);
             } else {
-                if constexpr (!VEC) {
+                uint2_t in[8];
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u) {
+                    in[u] = wt[i][u];
+                    if constexpr (!VEC) {
 #pragma unroll
-                        for (int e = 0; e < (int)(sizeof(F) / 4); ++e)
-                            wt[i][u][e] = sizeof(T) == 2 ? we[i][4 * u + 2 * e] | we[i][4 * u + 2 * e + 1] << 16
-                                                         : we[i][4 * u + e];
+                        for (int e = 0; e < 2; ++e)
+                            in[u][e] = sizeof(T) == 2 ? we[i][CW * u + 2 * e] | we[i][CW * u + 2 * e + 1] << 16
+                                                      : we[i][CW * u + e];
+                    }
+                    if (u >= have[i]) in[u] = uint2_t{0, 0};
                 }
-                uint4_t unit[4];
+                uint4_t unit[CW][Q];
+                to_units(in, unit, lose);
 #pragma unroll
-                for (int u = 0; u < U; ++u) wt[i][u] = u < have[i] ? wt[i][u] : F{};
-                transpose4(wt[i], unit);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    s_w[task / (kCols / 4) * LD + place(4 * (task % (kCols / 4)) + j)] = unit[j];
+                for (int j = 0; j < CW; ++j)
+                    put<T, kCols>(s_w, KG, task / (kCols / CW), place<T>(CW * (task % (kCols / CW)) + j), unit[j]);
             }
         }
     };
@@ -210,21 +225,29 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         stage();
         __syncthreads();
         fetch(nseg > 1 || ct + 1 == ct1 ? ct : ct + 1, nseg > 1 ? 1 : 0);
+        auto product = [&](int pair, const uint4_t (&b)[Q]) {
+            uint4_t c0[Q], c1[Q];
 #pragma unroll
-        for (int s = 0; s < NP; ++s) {
-            mma(acc[0], a[2 * s * LD], x[s], T{});
-            mma(acc[1], a[2 * s * LD + 32], x[s], T{});
-        }
+            for (int q = 0; q < Q; ++q) {
+                c0[q] = a[(q * KG + 2 * pair) * LD];
+                c1[q] = a[(q * KG + 2 * pair) * LD + 32];
+            }
+            mma(acc[0], c0, b);
+            mma(acc[1], c1, b);
+        };
+#pragma unroll
+        for (int s = 0; s < NP; ++s) product(s, x[s]);
         if (EXT) {
             for (int seg = 0;;) {
                 const bool in_seg = nseg > 0 && pl >= s_seg_at[seg] && pl < s_seg_at[seg + 1];
 #pragma unroll
                 for (int s = 0; s < XP; ++s) {
-                    uint4_t b;
+                    uint4_t b[Q];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) b[e] = in_seg ? h[s][e] : 0u;
-                    mma(acc[0], a[2 * (NP + s) * LD], b, T{});
-                    mma(acc[1], a[2 * (NP + s) * LD + 32], b, T{});
+                    for (int q = 0; q < Q; ++q)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) b[q][e] = in_seg ? h[s][q][e] : 0u;
+                    product(NP + s, b);
                 }
                 if (++seg >= nseg) break;
                 __syncthreads();
@@ -234,35 +257,47 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
             }
         }
-        // rows of kCols values, four at a time
+        // rows of 128 bytes, several a store
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int piece = 0; piece < kCols; piece += kPiece<T>) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-                convert(vec_val<!WNK>(acc[c], v), turn[((lane & 31) * kTurn<T> + 32 * c + vec_col<!WNK>(v, half)) / 4]);
-        wave_sync();
-        int in_tile = 4 * (lane & 15);
-        if (VEC && ct * kCols + in_tile >= p.N) in_tile = p.N - 4 - ct * kCols;
-        const int col = ct * kCols + in_tile;
+            for (int c = 0; c < kPiece<T> / 32; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const O val = turn[((4 * i + (lane >> 4)) * kTurn<T> + in_tile) / 4];
-            if (VEC) {
-                *reinterpret_cast<O *>(out[i] + col) = val;
-            } else {
+                for (int v = 0; v < 4; ++v)
+                    convert(vec_val<T, !WNK>(acc[piece / 32 + c], v),
+                            turn[((lane & 31) * kTurn<T> + 32 * c + vec_col<T, !WNK>(v, half)) / 4]);
+            wave_sync();
+            const int first = ct * kCols + piece;
+            if (piece > 0 && first >= p.N) break;
+            int in_piece = 4 * (lane % kVecs);  // past the last column, the last columns again
+            if (VEC && first + in_piece >= p.N) in_piece = p.N - 4 - first;
+            const int col = first + in_piece;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col + e < p.N) out[i][col + e] = val[e];
+            for (int i = 0; i < kStores; ++i) {
+                const O val = turn[(((64 / kVecs) * i + lane / kVecs) * kTurn<T> + in_piece) / 4];
+                if (VEC) {
+                    *reinterpret_cast<O *>(out[i] + col) = val;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < p.N) out[i][col + e] = val[e];
+                }
             }
+            wave_sync();
         }
-        wave_sync();
+    }
+    if constexpr (Q > 1) {
+        __threadfence_block();
+        if (__syncthreads_or(lose))
+            row_plain_sums<WNK>(o, p, t.g, t.p0, rows, s_row, s_g, ct0 * kCols, ct1 * kCols < p.N ? ct1 * kCols : p.N);
     }
 }
 
 template <typename T> bool whole_vectors(const RowProduct &p)
 {
-    return unit_aligned<T>(p.in, p.in_stride) && p.K % kU<T> == 0 && p.N % kU<T> == 0 &&
-           unit_aligned<T>(p.w, 0) && unit_aligned<T>(p.out, p.out_stride) && (!p.h || unit_aligned<T>(p.v, 0));
+    constexpr int V = 16 / (int)sizeof(T);
+    return aligned_rows<T>(p.in, p.in_stride) && p.K % V == 0 && p.N % V == 0 && aligned_rows<T>(p.w, 0) &&
+           aligned_rows<T>(p.out, p.out_stride) && (!p.h || aligned_rows<T>(p.v, 0));
 }
 
 template <typename T, bool WNK, int NP, int XP, bool VEC>
@@ -280,24 +315,26 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 template <typename T, int NP> hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     if (!p.h) return p.w_nk ? launch<T, true, NP, 0, true>(o, p, s) : launch<T, false, NP, 0, true>(o, p, s);
-    const bool two = kParts<T> * narrow_width<T>(p.r) <= 4 * kU<T>;
-    return two ? launch<T, false, NP, 2, true>(o, p, s) : launch<T, false, NP, kExtPairs, true>(o, p, s);
+    constexpr int X = kExtPairs<T>;
+    const bool half = kNarrow<T> * narrow_width(p.r) <= X * kU;
+    return half ? launch<T, false, NP, X / 2, true>(o, p, s) : launch<T, false, NP, X, true>(o, p, s);
 }
 
 template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
+    constexpr int M = kPairs<T>;
     if (!whole_vectors<T>(p))
-        return p.w_nk ? launch<T, true, kPairs, 0, false>(o, p, s) : launch<T, false, kPairs, 0, false>(o, p, s);
-    if (p.K <= 4 * kU<T>) return with_pairs<T, 2>(o, p, s);
-    if (p.K <= 8 * kU<T>) return with_pairs<T, 4>(o, p, s);
-    return with_pairs<T, kPairs>(o, p, s);
+        return p.w_nk ? launch<T, true, M, 0, false>(o, p, s) : launch<T, false, M, 0, false>(o, p, s);
+    if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4>(o, p, s);
+    if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2>(o, p, s);
+    return with_pairs<T, M>(o, p, s);
 }
 
 template <typename T> bool takes(const RowProduct &p)
 {
-    if (p.narrow || p.N <= kCols || p.K > 2 * kPairs * kU<T>) return false;
+    if (p.narrow || p.N <= kCols || p.K > 2 * kPairs<T> * kU) return false;
     if (!p.h) return p.w_group != 0;
-    return !p.w_nk && whole_vectors<T>(p) && kParts<T> * narrow_width<T>(p.r) <= 2 * kExtPairs * kU<T>;
+    return !p.w_nk && whole_vectors<T>(p) && kNarrow<T> * narrow_width(p.r) <= 2 * kExtPairs<T> * kU;
 }
 
 }  // namespace
