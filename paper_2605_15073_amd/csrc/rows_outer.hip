@@ -23,8 +23,11 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = NARROW ? kNarrow<T> : 1, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
+    // steps of operands in flight: two, but one where vectors are not whole or a narrow operand's further
+    // registers leave fewer waves (bf16, 525,308 x 64 by rank 16, 90 us against 99)
+    constexpr int kAhead = VEC && !NARROW ? 2 : 1;
     __shared__ uint4_t s_cols[P][kTile<T, BN>], s_rows[kTile<T, BM>];
-    __shared__ int s_id[2][BK];
+    __shared__ int s_id[4][BK];
 
     // Block b runs on XCD b % 8: the tiles of a chunk, which share its rows, follow each other on one.
     const int B = NARROW ? q.r : q.B;
@@ -41,56 +44,76 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     const int r0 = wr * (BM / WR), c0w = wc * (BN / WC);
 
     // lanes CW l .. CW l + CW - 1 of an operand, k-group g
-    const int al = tid % (BM / CW), ag = tid / (BM / CW);
-    const int bl = tid % (BN / CW), bg = tid / (BN / CW);
-    uint2_t ar[8], br[P][8];
+    constexpr bool kIdleA = BM / CW * KG < kThreads, kIdleB = BN / CW * KG < kThreads;
+    const int al = tid % (BM / CW), ag = tid / (BM / CW) % KG;
+    const int bl = tid % (BN / CW), bg = tid / (BN / CW) % KG;
+    const bool has_a = !kIdleA || tid < BM / CW * KG, has_b = !kIdleB || tid < BN / CW * KG;
+    struct Loads {
+        uint2_t a[8], b[P][8];
+        unsigned arows, brows;  // bit u: row u of the k-group exists
+    } even, odd;
     bool lose = false;
-    int id = -1;
     const int steps = (int)((t.p1 - t.p0 + BK - 1) / BK);
+    // ids of the rows of step s, -1 past the chunk; loads without a condition, as the operands'
+    const int32_t *const ids_at = o.order ? o.order : o.offsets;
+    int id = -1;
     auto fetch_ids = [&](int s) {
+        const int64_t pos = t.p0 + (int64_t)s * BK + tid % BK;
+        id = ids_at[o.order && pos < t.p1 ? pos : 0];
+    };
+    auto put_ids = [&](int s) {
         const int64_t pos = t.p0 + (int64_t)s * BK + tid;
-        id = tid < BK && pos < t.p1 ? row_at(o, pos) : -1;
+        const int row = o.order ? id : (int)pos;
+        if (tid < BK) s_id[s & 3][tid] = pos < t.p1 && (unsigned)row < (unsigned)o.n ? row : -1;
     };
-    auto fetch = [&](int s) {
-        const int *const ids = s_id[s & 1];
-        if (ag < KG) {
+    auto fetch = [&](Loads &l, int s) {
+        const int *const ids = s_id[s & 3];
+        l.arows = l.brows = 0;
+        const int ca = a0 + CW * al, cb = b0 + CW * bl;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int row = ids[ag * kU + u];
-                const int c = a0 + CW * al;
-                ar[u] = load_8<T, VEC>(static_cast<const T *>(q.a) + (row < 0 ? 0 : row * q.a_stride) + c,
-                                       row < 0 ? 0 : q.A - c);
+        for (int u = 0; u < 8; ++u) {
+            const int row = ids[ag * kU + u];
+            l.arows |= (row >= 0 ? 1u : 0u) << u;
+            const T *const p = static_cast<const T *>(q.a) + (row < 0 ? 0 : row) * q.a_stride;
+            if (VEC) l.a[u] = *reinterpret_cast<const uint2_t *>(p + (ca < q.A ? ca : q.A - CW));
+            else l.a[u] = load_8<T, false>(p + ca, row < 0 ? 0 : q.A - ca);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int row = ids[bg * kU + u];
+            l.brows |= (row >= 0 ? 1u : 0u) << u;
+            if (NARROW) {
+                const int64_t pos = row < 0 ? t.p0 : t.p0 + (int64_t)s * BK + bg * kU + u;
+#pragma unroll
+                for (int e = 0; e < P; ++e)
+                    l.b[e][u] = *reinterpret_cast<const uint2_t *>(static_cast<const T *>(q.h) + (pos * P + e) * W +
+                                                                   (cb < W ? cb : W - CW));
+            } else {
+                const T *const p = static_cast<const T *>(q.b) + (row < 0 ? 0 : row) * q.b_stride;
+                if (VEC) l.b[0][u] = *reinterpret_cast<const uint2_t *>(p + (cb < B ? cb : B - CW));
+                else l.b[0][u] = load_8<T, false>(p + cb, row < 0 ? 0 : B - cb);
             }
         }
-        if (bg < KG) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int row = ids[bg * kU + u];
-                const int c = b0 + CW * bl;
-                if (NARROW) {
-                    const int64_t pos = t.p0 + (int64_t)s * BK + bg * kU + u;
-#pragma unroll
-                    for (int e = 0; e < P; ++e)
-                        br[e][u] = load_8<T, true>(static_cast<const T *>(q.h) + (pos * P + e) * W + c,
-                                                   row < 0 ? 0 : W - c);
-                } else {
-                    br[0][u] = load_8<T, VEC>(static_cast<const T *>(q.b) + (row < 0 ? 0 : row * q.b_stride) + c,
-                                              row < 0 ? 0 : B - c);
-                }
-            }
-        }
     };
-    auto stage = [&]() {
+    auto stage = [&](Loads &l) {
         uint4_t u[CW][Q];
-        if (ag < KG) {
-            to_units(ar, u, lose);
+        if (has_a) {
+            if (l.arows != 0xffu) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) l.a[e] = l.arows >> e & 1 ? l.a[e] : uint2_t{0, 0};
+            }
+            to_units(l.a, u, lose);
 #pragma unroll
             for (int j = 0; j < CW; ++j) put<T, BM>(s_rows, KG, ag, place<T>(CW * al + j), u[j]);
         }
-        if (bg < KG) {
+        if (has_b) {
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                to_units(br[e], u, lose);
+                if (l.brows != 0xffu) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) l.b[e][r] = l.brows >> r & 1 ? l.b[e][r] : uint2_t{0, 0};
+                }
+                to_units(l.b[e], u, lose);
 #pragma unroll
                 for (int j = 0; j < CW; ++j) put<T, BN>(s_cols[e], KG, bg, place<T>(CW * bl + j), u[j]);
             }
@@ -105,23 +128,28 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[c][r][i] = 0.f;
     if (steps > 0) {
-        // row ids two steps ahead of the products, operands one
+        // operands kAhead steps ahead of the products, row ids one more
         fetch_ids(0);
-        if (tid < BK) s_id[0][tid] = id;
+        put_ids(0);
         fetch_ids(1);
+        put_ids(1);
+        fetch_ids(2);
         __syncthreads();
-        fetch(0);
-        for (int s = 0; s < steps; ++s) {
+        fetch(even, 0);
+        if (kAhead == 2) fetch(odd, 1);
+        auto step = [&](Loads &l, int s) {
             __syncthreads();
-            stage();
-            if (tid < BK) s_id[(s + 1) & 1][tid] = id;
+            stage(l);
+            put_ids(s + 2);
             __syncthreads();
-            if (s + 1 < steps) {
-                fetch(s + 1);
-                fetch_ids(s + 2);
-            }
+            fetch_ids(s + 3);  // before the operands, whose loads then stay in flight when it is written
+            fetch(l, s + kAhead);
 #pragma unroll
             for (int e = 0; e < P; ++e) step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0);
+        };
+        for (int s = 0; s < steps; s += 2) {
+            step(even, s);
+            if (s + 1 < steps) step(kAhead == 2 ? odd : even, s + 1);
         }
     }
     const bool whole = t.end - t.start <= ((int64_t)1 << shift);
@@ -176,17 +204,17 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     }
 }
 
-constexpr int kJoinCells = 32, kJoinLanes = kThreads / kJoinCells;
+constexpr int kJoinCells = 128, kJoinLanes = 8;
 
-// out_g = its slots' sum, for the groups of more than one chunk: a workgroup takes 32 cells, 8 threads
-// each with every eighth slot, whose sums are then added in order. Where there are fewer groups than
-// chunk sizes in the sequence, block x is for group x; else for the group whose first multiple of the
-// chunk size beyond its start is x + 1 (each such group has one).
-template <typename T>
+// out_g = its slots' sum, for the groups of more than one chunk: a workgroup takes 128 cells, each thread
+// four of them of every eighth slot, and the eight sums are then added in order. Where there are fewer
+// groups than chunk sizes in the sequence, block x is for group x; else for the group whose first multiple
+// of the chunk size beyond its start is x + 1 (each such group has one).
+template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, int shift, bool by_group, int64_t cells,
                                                        const float *__restrict__ slots, T *__restrict__ out)
 {
-    __shared__ float s_sum[kJoinLanes][kJoinCells];
+    __shared__ float4_t s_sum[kJoinLanes][kJoinCells / 4];
     const int64_t pos = ((int64_t)blockIdx.x + 1) << shift;
     int lo = 0, hi = o.G;
     if (by_group) lo = blockIdx.x;
@@ -201,26 +229,34 @@ __global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, int shift, bo
     const int64_t chunks = (end - start + ((int64_t)1 << shift) - 1) >> shift;
     if (chunks < 2 || (!by_group && (start >> shift) + 1 != pos >> shift)) return;
     const float *const src = slots + 2 * (start >> shift) * cells;
-    const int cell = threadIdx.x % kJoinCells, lane = threadIdx.x / kJoinCells;
+    const int quad = threadIdx.x % (kJoinCells / 4), lane = threadIdx.x / (kJoinCells / 4);
     for (int64_t c0 = (int64_t)blockIdx.y * kJoinCells; c0 < cells; c0 += (int64_t)gridDim.y * kJoinCells) {
-        const int64_t i = c0 + cell;
-        float sum = 0.f;
-        if (i < cells) {
-            int64_t c = lane;
-            for (; c + 3 * kJoinLanes < chunks; c += 4 * kJoinLanes) {
-                const float v0 = src[c * cells + i], v1 = src[(c + kJoinLanes) * cells + i];
-                const float v2 = src[(c + 2 * kJoinLanes) * cells + i], v3 = src[(c + 3 * kJoinLanes) * cells + i];
-                sum += (v0 + v1) + (v2 + v3);
-            }
-            for (; c < chunks; c += kJoinLanes) sum += src[c * cells + i];
+        const int64_t i = c0 + 4 * quad, left = cells - i;
+        auto slot = [&](int64_t c) {
+            return __builtin_bit_cast(float4_t, load_16<float, VEC>(src + c * cells + i, left));
+        };
+        float4_t sum = {0.f, 0.f, 0.f, 0.f};
+        int64_t c = lane;
+        for (; c + 3 * kJoinLanes < chunks; c += 4 * kJoinLanes) {
+            const float4_t v0 = slot(c), v1 = slot(c + kJoinLanes);
+            const float4_t v2 = slot(c + 2 * kJoinLanes), v3 = slot(c + 3 * kJoinLanes);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += (v0[e] + v1[e]) + (v2[e] + v3[e]);
+        }
+        for (; c < chunks; c += kJoinLanes) {
+            const float4_t v = slot(c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += v[e];
         }
         __syncthreads();
-        s_sum[lane][cell] = sum;
+        s_sum[lane][quad] = sum;
         __syncthreads();
-        if (lane == 0 && i < cells) {
+        if (lane == 0) {
 #pragma unroll
-            for (int j = 1; j < kJoinLanes; ++j) sum += s_sum[j][cell];
-            out[lo * cells + i] = (T)sum;
+            for (int j = 1; j < kJoinLanes; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += s_sum[j][quad][e];
+            store_four<VEC>(out + lo * cells + i, sum, left);
         }
     }
 }
@@ -228,14 +264,16 @@ __global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, int shift, bo
 constexpr int64_t kBlocks = 1536;  // workgroups that fill the GPU
 constexpr int kMinShift = 8, kMaxShift = 14;
 
-// Rows of a chunk: as many as leave kBlocks workgroups, but no fewer than keep the traffic of the
-// slots (8 bytes a cell and chunk) at a quarter of the operands'.
+// Rows of a chunk: as many as leave kBlocks workgroups, and then more while the traffic of the slots (8
+// bytes a cell and chunk) is over a quarter of the operands' and a third of the workgroups remain.
 int chunk_shift(size_t es, int64_t n, int A, int B, int64_t tiles)
 {
     const int64_t fill = n * tiles / kBlocks;
     const int64_t least = (int64_t)(32.0 * A * B / ((double)(A + B) * es));
     int shift = kMinShift;
-    while (shift < kMaxShift && (((int64_t)2 << shift) <= fill || ((int64_t)1 << shift) < least)) ++shift;
+    while (shift < kMaxShift && (((int64_t)2 << shift) <= fill ||
+                                 (((int64_t)1 << shift) < least && ((int64_t)2 << shift) <= 3 * fill)))
+        ++shift;
     return shift;
 }
 
@@ -283,8 +321,10 @@ template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float
     const int64_t cells = (int64_t)q.A * B, by = (cells + kJoinCells - 1) / kJoinCells;
     const int64_t spans = o.n >> sh.shift, bx = o.G < spans ? o.G : spans;
     const int64_t y = 8192 / bx < 1 ? 1 : 8192 / bx;
-    hipLaunchKernelGGL(k_row_join<T>, dim3((unsigned)bx, (unsigned)(by < y ? by : y)), dim3(kThreads), 0, s, o,
-                       sh.shift, o.G < spans, cells, slots, static_cast<T *>(q.out));
+    const bool vec = cells % 4 == 0 && aligned_rows<T>(q.out, 0);
+    auto *kernel = vec ? k_row_join<T, true> : k_row_join<T, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)bx, (unsigned)(by < y ? by : y)), dim3(kThreads), 0, s, o, sh.shift,
+                       o.G < spans, cells, slots, static_cast<T *>(q.out));
     return hipGetLastError();
 }
 

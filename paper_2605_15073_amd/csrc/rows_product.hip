@@ -3,8 +3,10 @@
 //
 // A workgroup owns up to BM rows of one group (of any groups where W is shared) and runs over tiles
 // of BN columns of its share of the output, so that its input rows come from HBM once and from the
-// L2 for every further column tile; the weights of a group stay in the L2s. The loads of a step
-// (rows and weights, kStep deep) are in flight while the step before is multiplied.
+// L2 for every further column tile; the weights of a group stay in the L2s. The loads of the next
+// step or two (rows and weights, kStep deep) are in flight while a step is multiplied. Where vectors are whole
+// (VEC) none of them is under a condition, or the wait for one step would be for all: addresses without a
+// value point to one that exists, and the value is zeroed when it is staged.
 //
 // Adapters: after the steps over the shared W, a tile's sums go on over the adapters of its rows, one
 // segment of rows at a time, with the narrow product's result as input rows (zero outside the
@@ -20,12 +22,15 @@ namespace {
 using namespace rows;
 
 template <typename T, bool WNK, int BM, int BN, int WR, bool VEC>
-__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits, bool v_vec)
+__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
     constexpr int kShift = BM == 128 ? 7 : BM == 64 ? 6 : 5;
     static_assert(BM == 1 << kShift && TR >= 1 && TC >= 1, "tile");
+    // steps of loads in flight: two of fp32, whose parts take longer to form and multiply, one where that
+    // costs waves (bf16, 261,766 x 1344 -> 128, 194 us against 218; fp32, 131,327 x 896 -> 128, 323 and 275)
+    constexpr int kAhead = VEC && Q > 1 ? 2 : 1;
     constexpr int kLanes = kThreads / KG;              // rows staged at once
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
     constexpr int NC = BN / kLanes > 0 ? BN / kLanes : 1;
@@ -69,77 +74,115 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const int r = rr + kLanes * i, row = r < BM ? s_row[r] : -1;
-        in[i] = row >= 0 ? static_cast<const T *>(p.in) + row * p.in_stride + kg * kU : nullptr;
+        in[i] = static_cast<const T *>(p.in) + (row < 0 ? 0 : row) * p.in_stride;  // row 0: never stored
     }
     const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
     const int W = narrow_width(p.r);  // of a part of the narrow input
     // transposed weights: columns CW tc .. CW tc + CW - 1, k-group tg
-    const int tc = tid % (BN / CW), tg = tid / (BN / CW);
+    constexpr bool kIdle = BN / CW * KG < kThreads;  // some threads have none to stage
+    const int tc = tid % (BN / CW), tg = kIdle ? tid / (BN / CW) % KG : tid / (BN / CW);
+    const bool has_w = !kIdle || tid < BN / CW * KG;
 
-    Raw8<T> xr[NR], wn[WNK ? NC : 1];
-    uint2_t wt[8];
-    bool lose = false;
-    // the loads of step k of column tile ct; seg < 0: the shared weights, else an adapter
-    auto fetch = [&](int ct, int seg, int k) {
-        const int c0 = ct * BN;
-        int K = p.K;
-        const T *wb = w;
-        int wk = p.K;  // k of the weights from which on there are none
-        if (seg >= 0) {
-            K = P * W;
-            wb = static_cast<const T *>(p.v) + (int64_t)s_seg_g[seg] * p.r * p.N;
-            wk = p.r;
-            const int at = s_seg_at[seg], end = s_seg_at[seg + 1];
-#pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                const int r = rr + kLanes * i;
-                const int left = r >= at && r < end && in[i] ? K - k - kg * kU : 0;
-                xr[i] = load_row8<T, true>(static_cast<const T *>(p.h) + (t.p0 + r) * K + k + kg * kU, left);
+    // The steps: of the shared or the group's weights (seg < 0), then of each adapter.
+    struct Cursor { int ct, seg, k; } next = {ct0, -1, 0}, now = next;  // the step to load, to multiply
+    auto advance = [&](Cursor &c) {
+        c.k += BK;
+        if (c.k >= (c.seg < 0 ? p.K : P * W)) {
+            c.k = 0;
+            if (++c.seg >= nseg) {
+                c.seg = -1;
+                ++c.ct;
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NR; ++i) xr[i] = load_row8<T, VEC>(in[i] + k, in[i] ? K - k - kg * kU : 0);
         }
+    };
+    struct Loads {
+        Raw8<T> x[NR], wn[WNK ? NC : 1];
+        uint2_t wt[WNK ? 1 : 8];
+        int xk, wk;  // values that exist of this thread's k-group of rows and weights
+        unsigned rows;  // bit i: x[i] is of a row that takes part
+    } even, odd;
+    bool lose = false;
+    auto fetch = [&](Loads &l) {
+        if (!VEC && next.ct >= ct1) return;
+        const bool ext = next.seg >= 0;
+        const int seg = ext ? next.seg : 0, c0 = (next.ct < ct1 ? next.ct : ct1 - 1) * BN, k = next.k;
+        const int K = ext ? P * W : p.K;   // of the rows
+        const int ld = ext ? p.r : p.K;    // of the weights
+        const T *wb = w;
+        int at = 0, end = BM;
+        if (nseg > 0) {
+            wb = ext ? static_cast<const T *>(p.v) + (int64_t)s_seg_g[seg] * p.r * p.N : w;
+            at = ext ? s_seg_at[seg] : 0;
+            end = ext ? s_seg_at[seg + 1] : BM;
+        }
+        const int kx = k + kg * kU;
+        l.xk = K - kx;
+        l.rows = 0;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = rr + kLanes * i;
+            if (r >= at && r < end) l.rows |= 1u << i;
+            const T *q = ext ? static_cast<const T *>(p.h) + (t.p0 + (r < rows ? r : 0)) * K : in[i];
+            if constexpr (VEC) {
+                q += l.xk > 0 ? kx : 0;
+                l.x[i].v[0] = *reinterpret_cast<const uint4_t *>(q);
+                if constexpr (Q > 1) l.x[i].v[1] = *reinterpret_cast<const uint4_t *>(q + (l.xk > 4 ? 4 : 0));
+            } else {
+                l.x[i] = load_row8<T, false>(q + kx, l.xk);
+            }
+        }
+        int kw = WNK ? kx : k + tg * kU;
+        const bool in_k = kw < K;
+        if (P == 2 && ext && kw >= W) kw -= W;  // the second part meets the same weights
+        l.wk = in_k ? ld - kw : 0;
         if constexpr (WNK) {
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
                 const int c = c0 + rr + kLanes * i;
-                int kk = k + kg * kU;
-                const bool in_k = kk < K && rr + kLanes * i < BN;
-                if (seg >= 0 && P == 2 && kk >= W) kk -= W;  // the second part meets the same weights
-                const T *const q = wb + (int64_t)c * wk + kk;
-                const int left = c < p.N && in_k ? wk - kk : 0;
-                if (seg >= 0 && !v_vec) wn[i] = load_row8<T, false>(q, left);
-                else wn[i] = load_row8<T, VEC>(q, left);
+                const T *q = wb + (int64_t)(c < p.N ? c : p.N - 1) * ld;
+                if constexpr (VEC) {
+                    q += l.wk > 0 ? kw : 0;
+                    l.wn[i].v[0] = *reinterpret_cast<const uint4_any *>(q);
+                    if constexpr (Q > 1) l.wn[i].v[1] = *reinterpret_cast<const uint4_any *>(q + (l.wk > 4 ? 4 : 0));
+                } else {
+                    l.wn[i] = load_row8<T, false>(q + kw, l.wk);
+                }
             }
-        } else if (tg < KG) {
+        } else {
             const int c = c0 + CW * tc;
-            int kk = k + tg * kU;
-            const bool in_k = kk < K;
-            if (seg >= 0 && P == 2 && kk >= W) kk -= W;
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                wt[u] = load_8<T, VEC>(wb + (int64_t)(kk + u) * p.N + c, in_k && kk + u < wk ? p.N - c : 0);
+            for (int u = 0; u < 8; ++u) {
+                const T *q = wb + (int64_t)(u < l.wk ? kw + u : 0) * p.N;
+                if constexpr (VEC) l.wt[u] = *reinterpret_cast<const uint2_t *>(q + (c < p.N ? c : p.N - CW));
+                else l.wt[u] = load_8<T, false>(q + c, u < l.wk ? p.N - c : 0);
+            }
         }
+        if (next.ct < ct1) advance(next);
     };
-    auto stage = [&]() {
+    auto stage = [&](Loads &l) {
         uint4_t u[Q];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             if (BM < kLanes && rr >= BM) break;
-            to_units(xr[i], u, lose);
+            if (l.xk < kU || !(l.rows >> i & 1)) keep(l.x[i], l.rows >> i & 1 ? l.xk : 0);
+            to_units(l.x[i], u, lose);
             put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
         }
         if constexpr (WNK) {
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
                 if (BN < kLanes && rr >= BN) break;
-                to_units(wn[i], u, lose);
+                if (l.wk < kU) keep(l.wn[i], l.wk);
+                to_units(l.wn[i], u, lose);
                 put<T, BN>(s_cols, KG, kg, rr + kLanes * i, u);
             }
-        } else if (tg < KG) {
+        } else if (has_w) {
+            if (l.wk < kU) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) l.wt[e] = e < l.wk ? l.wt[e] : uint2_t{0, 0};
+            }
             uint4_t c[CW][Q];
-            to_units(wt, c, lose);
+            to_units(l.wt, c, lose);
 #pragma unroll
             for (int j = 0; j < CW; ++j) put<T, BN>(s_cols, KG, tg, place<T>(CW * tc + j), c[j]);
         }
@@ -148,32 +191,16 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     const int wr = wave % WR, wc = wave / WR;
     const int r0 = wr * (BM / WR), c0w = wc * (BN / WC);
     float16_t acc[TC][TR];
-    int ct = ct0, seg = -1, k = 0;
-    fetch(ct, seg, k);
-    while (ct < ct1) {
+    auto clear = [&]() {
 #pragma unroll
         for (int c = 0; c < TC; ++c)
 #pragma unroll
             for (int r = 0; r < TR; ++r)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[c][r][i] = 0.f;
-        const int now = ct;
-        while (ct == now) {
-            __syncthreads();
-            stage();
-            __syncthreads();
-            k += BK;
-            if (k >= (seg < 0 ? p.K : P * W)) {
-                k = 0;
-                if (++seg >= nseg) {
-                    seg = -1;
-                    ++ct;
-                }
-            }
-            if (ct < ct1) fetch(ct, seg, k);
-            step_products<T, BN, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0);
-        }
-        const int c0 = now * BN + c0w;
+    };
+    auto store = [&](int ct) {
+        const int c0 = ct * BN + c0w;
         if (p.narrow) {
             const float scale = p.narrow_scale ? p.narrow_scale[t.g] : 1.f;
             const int No = narrow_width(p.N);
@@ -208,6 +235,26 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
                     }
             }
         }
+    };
+    auto step = [&](Loads &l) {
+        __syncthreads();
+        stage(l);
+        __syncthreads();
+        fetch(l);
+        step_products<T, BN, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0);
+        const int ct = now.ct;
+        advance(now);
+        if (now.ct != ct) {
+            store(ct);
+            clear();
+        }
+    };
+    clear();
+    fetch(even);
+    if (kAhead == 2) fetch(odd);
+    while (now.ct < ct1) {
+        step(even);
+        if (now.ct < ct1) step(kAhead == 2 ? odd : even);
     }
     if constexpr (Q > 1) {
         __threadfence_block();
@@ -222,14 +269,13 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     const bool vec = aligned_rows<T>(p.in, p.in_stride) && p.K % V == 0 && p.N % V == 0 &&
                      aligned_rows<T>(p.w, 0) && (p.narrow || aligned_rows<T>(p.out, p.out_stride)) &&
                      (!p.h || aligned_rows<T>(p.v, 0));
-    const bool v_vec = vec && p.r % V == 0;  // rows of r adapter weights
     const int64_t tiles = p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
     const int ctiles = (p.N + BN - 1) / BN;
     // few rows: column tiles go to workgroups of their own
     int splits = (int)(2048 / tiles);
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
     auto *kernel = vec ? k_row_product<T, WNK, BM, BN, WR, true> : k_row_product<T, WNK, BM, BN, WR, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits, v_vec);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits);
     return hipGetLastError();
 }
 

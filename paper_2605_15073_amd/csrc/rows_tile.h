@@ -137,26 +137,28 @@ __device__ __forceinline__ int find_segments(const RowOrder &o, int64_t p0, int 
     return n;
 }
 
+// 16 and 8 bytes of values at the alignment of one (global memory accesses need no more).
+typedef uint4_t uint4_any __attribute__((aligned(2)));
+typedef uint2_t uint2_any __attribute__((aligned(2)));
+typedef float4_t float4_any __attribute__((aligned(4)));
+typedef bf4_t bf4_any __attribute__((aligned(2)));
+
 // 16 bytes of values from p on, zero past the `left` that exist.
 template <typename T, bool VEC>
 __device__ __forceinline__ uint4_t load_16(const T *p, int64_t left)
 {
+    constexpr int V = 16 / (int)sizeof(T);
     uint4_t v = {0, 0, 0, 0};
-    if (VEC) {
-        if (left > 0) v = *reinterpret_cast<const uint4_t *>(p);
-    } else if (sizeof(T) == 4) {
+    if (left >= V) {
+        if (VEC) v = *reinterpret_cast<const uint4_t *>(p);
+        else v = *reinterpret_cast<const uint4_any *>(p);
+    } else if (!VEC && left > 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (left > e) v[e] = reinterpret_cast<const unsigned *>(p)[e];
-    } else {
-        const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            unsigned lo = 0, hi = 0;
-            if (left > 2 * e) lo = h[2 * e];
-            if (left > 2 * e + 1) hi = h[2 * e + 1];
-            v[e] = lo | hi << 16;
-        }
+        for (int e = 0; e < V; ++e)
+            if (left > e) {
+                if (sizeof(T) == 4) v[e % 4] = reinterpret_cast<const unsigned *>(p)[e];
+                else v[e / 2] |= (unsigned)reinterpret_cast<const unsigned short *>(p)[e] << (e % 2 * 16);
+            }
     }
     return v;
 }
@@ -165,22 +167,18 @@ __device__ __forceinline__ uint4_t load_16(const T *p, int64_t left)
 template <typename T, bool VEC>
 __device__ __forceinline__ uint2_t load_8(const T *p, int64_t left)
 {
+    constexpr int V = 8 / (int)sizeof(T);
     uint2_t v = {0, 0};
-    if (VEC) {
-        if (left > 0) v = *reinterpret_cast<const uint2_t *>(p);
-    } else if (sizeof(T) == 4) {
+    if (left >= V) {
+        if (VEC) v = *reinterpret_cast<const uint2_t *>(p);
+        else v = *reinterpret_cast<const uint2_any *>(p);
+    } else if (!VEC && left > 0) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (left > e) v[e] = reinterpret_cast<const unsigned *>(p)[e];
-    } else {
-        const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            unsigned lo = 0, hi = 0;
-            if (left > 2 * e) lo = h[2 * e];
-            if (left > 2 * e + 1) hi = h[2 * e + 1];
-            v[e] = lo | hi << 16;
-        }
+        for (int e = 0; e < V; ++e)
+            if (left > e) {
+                if (sizeof(T) == 4) v[e % 2] = reinterpret_cast<const unsigned *>(p)[e];
+                else v[e / 2] |= (unsigned)reinterpret_cast<const unsigned short *>(p)[e] << (e % 2 * 16);
+            }
     }
     return v;
 }
@@ -195,6 +193,17 @@ __device__ __forceinline__ Raw8<T> load_row8(const T *p, int64_t left)
     r.v[0] = load_16<T, VEC>(p, left);
     if constexpr (sizeof(T) == 4) r.v[1] = load_16<T, VEC>(p + 4, left - 4);
     return r;
+}
+
+// Zeros from value `left` on.
+template <typename T> __device__ __forceinline__ void keep(Raw8<T> &r, int left)
+{
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(T) * 2); ++e) {
+        const int first = e * 4 / (int)sizeof(T);  // of the values in this register
+        const unsigned v = r.v[e / 4][e % 4];
+        r.v[e / 4][e % 4] = first + (sizeof(T) == 2) < left ? v : first < left ? v & 0xffffu : 0u;
+    }
 }
 
 // The largest of m, |a| and |b| (fmaxf would first quieten each operand, an instruction of its own).
@@ -350,6 +359,10 @@ template <bool VEC> __device__ __forceinline__ void store_four(float *p, float4_
         if (left > 0) *reinterpret_cast<float4_t *>(p) = v;
         return;
     }
+    if (left >= 4) {
+        *reinterpret_cast<float4_any *>(p) = v;
+        return;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (left > e) p[e] = v[e];
@@ -360,6 +373,10 @@ template <bool VEC> __device__ __forceinline__ void store_four(bf16_t *p, float4
     const bf4_t h = {(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
     if (VEC) {
         if (left > 0) *reinterpret_cast<bf4_t *>(p) = h;
+        return;
+    }
+    if (left >= 4) {
+        *reinterpret_cast<bf4_any *>(p) = h;
         return;
     }
 #pragma unroll
