@@ -13,7 +13,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libcgtp.so")
 SOURCES = ["plan.cpp", "tables.cpp", "order.cpp", "rows.cpp", "contract.hip", "contract_rows.hip", "kernels.hip", "onsite.hip", "receiver_mfma.hip",
            "receiver_values.hip", "folded.hip",
-           "fourier_mfma.hip", "noalloc.hip", "group_rows.hip", "rows_product.hip", "rows_outer.hip", "rows_wide.hip", "adamw.hip"]
+           "fourier_mfma.hip", "noalloc.hip", "group_rows.hip", "rows_product.hip", "rows_outer.hip", "rows_wide.hip", "rows_few.hip", "adamw.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Per-source flags. The receivers' matrix-core results feed vector ALU products at once, those of
 # the row products the conversion of a store: accumulating them in VGPRs (not AccVGPRs) saves a

@@ -18,8 +18,11 @@ namespace {
 
 using namespace rows;
 
+constexpr int kFewMean = 16;
+
 template <typename T, int BM, int BN, int WR, bool VEC, bool NARROW>
-__global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, int shift, float *slots)
+__global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, int shift, bool big,
+                                                        float *slots)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = NARROW ? kNarrow<T> : 1, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
@@ -34,7 +37,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     const int btiles = (B + BN - 1) / BN, tiles = btiles * ((q.A + BM - 1) / BM);
     const int on_xcd = blockIdx.x / 8, tile = on_xcd % tiles;
     const int64_t chunk = (int64_t)(on_xcd / tiles) * 8 + blockIdx.x % 8;
-    const Tile t = find_tile(o, shift, chunk);
+    const Tile t = big ? find_big(o, shift, chunk) : find_tile(o, shift, chunk);
     if (t.g < 0 || t.g >= o.G) return;
     const int W = narrow_width(B);
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -294,17 +297,18 @@ Shape shape(size_t es, int64_t n, int A, int B)
 }
 
 template <typename T, int BM, int BN, int WR>
-hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, float *slots, hipStream_t s)
+hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, bool big, float *slots, hipStream_t s)
 {
     const int B = q.r > 0 ? q.r : q.B;
     constexpr int V = 16 / (int)sizeof(T);
     const bool vec = aligned_rows<T>(q.a, q.a_stride) && q.A % V == 0 && B % V == 0 &&
                      aligned_rows<T>(q.out, 0) && (q.r > 0 || aligned_rows<T>(q.b, q.b_stride));
-    const int64_t chunks = ((o.n >> sh.shift) + o.G + 7) / 8 * 8;
+    const int64_t chunks = ((big ? o.n / kFewRows : (o.n >> sh.shift) + o.G) + 7) / 8 * 8;
     if (chunks * sh.tiles > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     auto *kernel = q.r > 0 ? (vec ? k_row_outer<T, BM, BN, WR, true, true> : k_row_outer<T, BM, BN, WR, false, true>)
                            : (vec ? k_row_outer<T, BM, BN, WR, true, false> : k_row_outer<T, BM, BN, WR, false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks * sh.tiles)), dim3(kThreads), 0, s, o, q, sh.shift, slots);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks * sh.tiles)), dim3(kThreads), 0, s, o, q, sh.shift, big,
+                       slots);
     return hipGetLastError();
 }
 
@@ -312,11 +316,16 @@ template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float
 {
     const int B = q.r > 0 ? q.r : q.B;
     const Shape sh = shape(sizeof(T), o.n, q.A, B);
+    const bool big = o.n <= kFewMean * (int64_t)o.G;  // the groups of few rows go their own way
     hipError_t e;
-    if (sh.bm == 64) e = launch<T, 64, 64, 2>(o, q, sh, slots, s);
-    else if (sh.bn == 32) e = launch<T, 128, 32, 4>(o, q, sh, slots, s);
-    else if (sh.bn == 64) e = launch<T, 128, 64, 4>(o, q, sh, slots, s);
-    else e = launch<T, 128, 128, 2>(o, q, sh, slots, s);
+    if (big) {
+        e = launch_row_outer_few(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, q, s);
+        if (e != hipSuccess || o.n <= kFewRows) return e;
+    }
+    if (sh.bm == 64) e = launch<T, 64, 64, 2>(o, q, sh, big, slots, s);
+    else if (sh.bn == 32) e = launch<T, 128, 32, 4>(o, q, sh, big, slots, s);
+    else if (sh.bn == 64) e = launch<T, 128, 64, 4>(o, q, sh, big, slots, s);
+    else e = launch<T, 128, 128, 2>(o, q, sh, big, slots, s);
     if (e != hipSuccess || o.n >> sh.shift == 0) return e;
     const int64_t cells = (int64_t)q.A * B, by = (cells + kJoinCells - 1) / kJoinCells;
     const int64_t spans = o.n >> sh.shift, bx = o.G < spans ? o.G : spans;

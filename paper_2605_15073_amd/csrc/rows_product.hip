@@ -21,8 +21,10 @@ namespace {
 
 using namespace rows;
 
+constexpr int kFewMean = 8;
+
 template <typename T, bool WNK, int BM, int BN, int WR, bool VEC>
-__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits)
+__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits, bool big)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
@@ -44,7 +46,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         t.p1 = t.p0 + BM < o.n ? t.p0 + BM : o.n;
         t.g = 0;
     } else {
-        t = find_tile(o, kShift, blockIdx.x);
+        t = big ? find_big(o, kShift, blockIdx.x) : find_tile(o, kShift, blockIdx.x);
         if (t.g < 0 || t.p0 >= t.p1) return;
     }
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -263,27 +265,33 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
 }
 
 template <typename T, bool WNK, int BM, int BN, int WR>
-hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
+hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s, bool big = false)
 {
     constexpr int V = 16 / (int)sizeof(T);
     const bool vec = aligned_rows<T>(p.in, p.in_stride) && p.K % V == 0 && p.N % V == 0 &&
                      aligned_rows<T>(p.w, 0) && (p.narrow || aligned_rows<T>(p.out, p.out_stride)) &&
                      (!p.h || aligned_rows<T>(p.v, 0));
-    const int64_t tiles = p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
+    const int64_t tiles = big ? o.n / kFewRows : p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
     const int ctiles = (p.N + BN - 1) / BN;
     // few rows: column tiles go to workgroups of their own
     int splits = (int)(2048 / tiles);
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
     auto *kernel = vec ? k_row_product<T, WNK, BM, BN, WR, true> : k_row_product<T, WNK, BM, BN, WR, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits, big);
     return hipGetLastError();
 }
 
 template <typename T, bool WNK>
 hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    const bool few = o.n < 64 * (p.w_group ? (int64_t)o.G : 1);  // rows per group
     const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
+    const int64_t groups = p.w_group ? o.G : 1;
+    if (p.w_group && o.n <= kFewMean * groups) {
+        const hipError_t e = launch_row_few(dtype, o, p, s);
+        if (e != hipSuccess || o.n <= kFewRows) return e;
+        return p.N <= 32 ? launch<T, WNK, 128, 32, 4>(o, p, s, true) : launch<T, WNK, 128, 128, 2>(o, p, s, true);
+    }
+    const bool few = o.n < 64 * groups;  // rows per group
     if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1>(o, p, s);

@@ -86,6 +86,36 @@ __device__ __forceinline__ Tile find_tile(const RowOrder &o, int shift, int64_t 
     return t;
 }
 
+// Tile j of a group of more than kFewRows rows, where the others are looked after elsewhere: index m is for
+// the group that holds position (m + 1) kFewRows, and the i-th such index of a group for its tile i. A group of
+// n rows, n > kFewRows, holds at least floor((n - 1) / kFewRows) such positions beyond its start, no fewer than
+// tiles of 2 kFewRows.
+__device__ __forceinline__ Tile find_big(const RowOrder &o, int shift, int64_t m)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t pos = (m + 1) * kFewRows;
+    int lo = 0, len = o.G + 1;  // the last g with offsets[g] <= pos lies in [lo, lo + len)
+    while (len > 1) {
+        const int s = (len + 63) / 64;
+        const bool in = lane * s < len;
+        const int cnt = __popcll(__ballot(in && clamp_offset(o.offsets[in ? lo + lane * s : lo], o.n) <= pos));
+        const int skip = (cnt > 0 ? cnt - 1 : 0) * s;
+        lo += skip;
+        len = len - skip < s ? len - skip : s;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    Tile t;
+    t.g = -1;
+    if (lo >= o.G) return t;
+    t.start = clamp_offset(o.offsets[lo], o.n);
+    t.end = clamp_offset(o.offsets[lo + 1], o.n);
+    const int64_t i = m - t.start / kFewRows;
+    t.p0 = t.start + (i << shift);
+    t.p1 = t.p0 + ((int64_t)1 << shift) < t.end ? t.p0 + ((int64_t)1 << shift) : t.end;
+    if (t.end - t.start > kFewRows && i >= 0 && t.p0 < t.end) t.g = lo;
+    return t;
+}
+
 // Row of a position, -1 where the order holds none.
 __device__ __forceinline__ int row_at(const RowOrder &o, int64_t p)
 {

@@ -129,6 +129,64 @@ def test_grouped(cg, dtype, n, G, n_in, n_out, kind):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,G,n_in,n_out", [(1, 9, 1344, 448), (8, 8, 520, 70), (65, 40, 64, 64),
+                                            (900, 400, 70, 90), (900, 400, 96, 32),
+                                            (3000, 4096, 37, 129), (2500, 600, 129, 257)])
+@pytest.mark.parametrize("kind", ["even", "one", "holes", "none", "spikes"])
+def test_grouped_few_rows_a_group(cg, dtype, n, G, n_in, n_out, kind):
+    """Many groups, few rows on the mean: all even, or some groups of many rows among empty ones."""
+    rng = np.random.default_rng([n, G, n_in, n_out])
+    x, w, dy = _linear(rng, n, G, n_in, n_out, dtype)
+    if kind == "spikes":
+        ids = draw_ids(rng, n, G, "even")
+        ids[: n // 2] = rng.integers(0, min(G, 3), n // 2)
+    else:
+        ids = draw_ids(rng, n, G, kind)
+    offsets, order = cg.group_rows(dev(ids), G)
+    X, W, DY = (dev(t, dtype) for t in (x, w, dy))
+    check(cg.grouped_linear(X, W, offsets, order), ref.grouped(x, w, ids, dtype), "y")
+    want = ref.grouped_grad(x, w, dy, ids, dtype)
+    dx, dw = cg.grouped_linear_grad(X, W, DY, offsets, order)
+    check(dx, want[0], "dx")
+    check(dw, want[1], "dw")
+
+
+@pytest.mark.parametrize("where", ["x", "w", "dy"])
+@pytest.mark.parametrize("value", [1e-38, 3e-40, 3.3e38, float("inf")])
+@pytest.mark.parametrize("n,n_in,n_out", [(300, 64, 130), (300, 130, 72), (700, 96, 40)])
+def test_grouped_fp32_extremes(cg, where, value, n, n_in, n_out):
+    """Values that bf16 parts cannot hold, beside ordinary ones: the results of fp32 sums."""
+    rng = np.random.default_rng([n, n_in])
+    x, w, dy = _linear(rng, n, 2, n_in, n_out, "f32")
+    ids = draw_ids(rng, n, 2, "even")
+    t = dict(x=x, w=w, dy=dy)[where]
+    if value < 1:                            # a whole operand of tiny values
+        t *= value / 4
+        other = dict(x=w, w=x, dy=w)[where]
+        other *= 1e30
+        t[...] = rounded(t, "f32")
+        other[...] = rounded(other, "f32")
+    else:                                    # single large ones, times others below 1/8
+        t[..., 3, :] = np.where(rng.random(t[..., 3, :].shape) < 0.2, value, 0)
+        for u in (x, w, dy):
+            if u is not t:
+                u[...] = rounded(u / 64, "f32")
+        t[...] = rounded(t, "f32")
+    offsets, order = cg.group_rows(dev(ids), 2)
+    X, W, DY = (dev(v) for v in (x, w, dy))
+    with np.errstate(all="ignore"):
+        want = [ref.grouped(x, w, ids, "f32"), *ref.grouped_grad(x, w, dy, ids, "f32")]
+    got = [cg.grouped_linear(X, W, offsets, order), *cg.grouped_linear_grad(X, W, DY, offsets, order)]
+    for g, (v, bound), name in zip(got, want, ("y", "dx", "dw")):
+        g = host(g)
+        fine = np.isfinite(v) & (np.abs(v) < 3e38)
+        assert np.array_equal(np.isfinite(g) & (np.abs(g) < 3e38), fine), name
+        assert np.all(np.abs(g - v)[fine] <= bound[fine]), name
+        inf = np.isinf(v)
+        assert np.array_equal(g[inf], v[inf]), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,G,n_in,n_out", [(300, 5, 40, 56), (131, 3, 37, 29), (5000, 2, 64, 64)])
 @pytest.mark.parametrize("kind", ["none", "one", "holes"])
 @pytest.mark.parametrize("pad", [1, 8])
