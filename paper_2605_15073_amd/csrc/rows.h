@@ -48,11 +48,6 @@ hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p,
 bool row_wide_takes(int dtype, const RowProduct &p);
 hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
 
-// The forms for groups of few rows (rows_few.hip): they take groups of up to kFewRows rows and leave the
-// others to the tiled kernels.
-constexpr int kFewRows = 64;
-hipError_t launch_row_few(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
-
 // out_g = sum over the rows of group g of a_i b_i^T, [A][B]; with h, the result of a narrow product,
 // in place of b: [A][r], or [r][A] where transposed.
 struct RowOuter {
@@ -70,6 +65,9 @@ struct RowOuter {
 size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B);
 hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &p, void *ws,
                             hipStream_t s);
+// The form for groups of few rows (rows_few.hip): it takes groups of up to kFewRows rows and leaves the
+// others to the tiled kernel.
+constexpr int kFewRows = 64;
 hipError_t launch_row_outer_few(int dtype, const RowOrder &o, const RowOuter &q, hipStream_t s);
 size_t narrow_bytes(int dtype, int64_t n_rows, int N);
 

@@ -18,17 +18,17 @@ namespace {
 
 using namespace rows;
 
-constexpr int kFewMean = 16;
+constexpr int kFewMean = 4;
 
-template <typename T, int BM, int BN, int WR, bool VEC, bool NARROW>
+template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, int shift, bool big,
                                                         float *slots)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = NARROW ? kNarrow<T> : 1, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
-    // steps of operands in flight: two, but one where vectors are not whole or a narrow operand's further
+    // steps of operands in flight: two, but one where rows are below a vector or a narrow operand's further
     // registers leave fewer waves (bf16, 525,308 x 64 by rank 16, 90 us against 99)
-    constexpr int kAhead = VEC && !NARROW ? 2 : 1;
+    constexpr int kAhead = WIDE && !NARROW ? 2 : 1;
     __shared__ uint4_t s_cols[P][kTile<T, BN>], s_rows[kTile<T, BM>];
     __shared__ int s_id[4][BK];
 
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             const int row = ids[ag * kU + u];
             l.arows |= (row >= 0 ? 1u : 0u) << u;
             const T *const p = static_cast<const T *>(q.a) + (row < 0 ? 0 : row) * q.a_stride;
-            if (VEC) l.a[u] = *reinterpret_cast<const uint2_t *>(p + (ca < q.A ? ca : q.A - CW));
+            if (WIDE) l.a[u] = *reinterpret_cast<const uint2_any *>(p + (ca + CW <= q.A ? ca : q.A - CW));
             else l.a[u] = load_8<T, false>(p + ca, row < 0 ? 0 : q.A - ca);
         }
 #pragma unroll
@@ -93,14 +93,21 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                                                                    (cb < W ? cb : W - CW));
             } else {
                 const T *const p = static_cast<const T *>(q.b) + (row < 0 ? 0 : row) * q.b_stride;
-                if (VEC) l.b[0][u] = *reinterpret_cast<const uint2_t *>(p + (cb < B ? cb : B - CW));
+                if (WIDE) l.b[0][u] = *reinterpret_cast<const uint2_any *>(p + (cb + CW <= B ? cb : B - CW));
                 else l.b[0][u] = load_8<T, false>(p + cb, row < 0 ? 0 : B - cb);
             }
         }
     };
+    // what the loads of the last columns started early
+    const int early_a = WIDE && a0 + CW * al < q.A && a0 + CW * al + CW > q.A ? a0 + CW * al + CW - q.A : 0;
+    const int early_b = WIDE && !NARROW && b0 + CW * bl < B && b0 + CW * bl + CW > B ? b0 + CW * bl + CW - B : 0;
     auto stage = [&](Loads &l) {
         uint4_t u[CW][Q];
         if (has_a) {
+            if (early_a > 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) settle<T>(l.a[e], early_a);
+            }
             if (l.arows != 0xffu) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) l.a[e] = l.arows >> e & 1 ? l.a[e] : uint2_t{0, 0};
@@ -112,6 +119,10 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         if (has_b) {
 #pragma unroll
             for (int e = 0; e < P; ++e) {
+                if (early_b > 0) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) settle<T>(l.b[e][r], early_b);
+                }
                 if (l.brows != 0xffu) {
 #pragma unroll
                     for (int r = 0; r < 8; ++r) l.b[e][r] = l.brows >> r & 1 ? l.b[e][r] : uint2_t{0, 0};
@@ -200,8 +211,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                         }
                 } else {
                     const int64_t at = (int64_t)i * B + col;
-                    if (whole) store_four<VEC>(out + at, x, B - col);
-                    else store_four<VEC>(part + at, x, B - col);
+                    if (whole) store_four<false>(out + at, x, B - col);
+                    else store_four<false>(part + at, x, B - col);
                 }
             }
     }
@@ -300,13 +311,11 @@ template <typename T, int BM, int BN, int WR>
 hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, bool big, float *slots, hipStream_t s)
 {
     const int B = q.r > 0 ? q.r : q.B;
-    constexpr int V = 16 / (int)sizeof(T);
-    const bool vec = aligned_rows<T>(q.a, q.a_stride) && q.A % V == 0 && B % V == 0 &&
-                     aligned_rows<T>(q.out, 0) && (q.r > 0 || aligned_rows<T>(q.b, q.b_stride));
+    const bool wide = q.A >= kWide<T> && B >= kWide<T>;
     const int64_t chunks = ((big ? o.n / kFewRows : (o.n >> sh.shift) + o.G) + 7) / 8 * 8;
     if (chunks * sh.tiles > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    auto *kernel = q.r > 0 ? (vec ? k_row_outer<T, BM, BN, WR, true, true> : k_row_outer<T, BM, BN, WR, false, true>)
-                           : (vec ? k_row_outer<T, BM, BN, WR, true, false> : k_row_outer<T, BM, BN, WR, false, false>);
+    auto *kernel = q.r > 0 ? (wide ? k_row_outer<T, BM, BN, WR, true, true> : k_row_outer<T, BM, BN, WR, false, true>)
+                           : (wide ? k_row_outer<T, BM, BN, WR, true, false> : k_row_outer<T, BM, BN, WR, false, false>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks * sh.tiles)), dim3(kThreads), 0, s, o, q, sh.shift, big,
                        slots);
     return hipGetLastError();

@@ -4,9 +4,10 @@
 // A workgroup owns up to BM rows of one group (of any groups where W is shared) and runs over tiles
 // of BN columns of its share of the output, so that its input rows come from HBM once and from the
 // L2 for every further column tile; the weights of a group stay in the L2s. The loads of the next
-// step or two (rows and weights, kStep deep) are in flight while a step is multiplied. Where vectors are whole
-// (VEC) none of them is under a condition, or the wait for one step would be for all: addresses without a
-// value point to one that exists, and the value is zeroed when it is staged.
+// step or two (rows and weights, kStep deep) are in flight while a step is multiplied. None of them is under
+// a condition, or the wait for one step would be for all: a vector that would pass the end of its row starts
+// early, one without values points to some that exist, and both are put right when they are staged. Only
+// widths below a vector (WIDE false) load value by value.
 //
 // Adapters: after the steps over the shared W, a tile's sums go on over the adapters of its rows, one
 // segment of rows at a time, with the narrow product's result as input rows (zero outside the
@@ -21,10 +22,8 @@ namespace {
 
 using namespace rows;
 
-constexpr int kFewMean = 8;
-
-template <typename T, bool WNK, int BM, int BN, int WR, bool VEC>
-__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits, bool big)
+template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE>
+__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
@@ -32,7 +31,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     static_assert(BM == 1 << kShift && TR >= 1 && TC >= 1, "tile");
     // steps of loads in flight: two of fp32, whose parts take longer to form and multiply, one where that
     // costs waves (bf16, 261,766 x 1344 -> 128, 194 us against 218; fp32, 131,327 x 896 -> 128, 323 and 275)
-    constexpr int kAhead = VEC && Q > 1 ? 2 : 1;
+    constexpr int kAhead = WIDE && Q > 1 ? 2 : 1;
     constexpr int kLanes = kThreads / KG;              // rows staged at once
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
     constexpr int NC = BN / kLanes > 0 ? BN / kLanes : 1;
@@ -46,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         t.p1 = t.p0 + BM < o.n ? t.p0 + BM : o.n;
         t.g = 0;
     } else {
-        t = big ? find_big(o, kShift, blockIdx.x) : find_tile(o, kShift, blockIdx.x);
+        t = find_tile(o, kShift, blockIdx.x);
         if (t.g < 0 || t.p0 >= t.p1) return;
     }
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -101,11 +100,12 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         Raw8<T> x[NR], wn[WNK ? NC : 1];
         uint2_t wt[WNK ? 1 : 8];
         int xk, wk;  // values that exist of this thread's k-group of rows and weights
+        int xe, we;  // what their loads started early
         unsigned rows;  // bit i: x[i] is of a row that takes part
     } even, odd;
     bool lose = false;
     auto fetch = [&](Loads &l) {
-        if (!VEC && next.ct >= ct1) return;
+        if (!WIDE && next.ct >= ct1) return;
         const bool ext = next.seg >= 0;
         const int seg = ext ? next.seg : 0, c0 = (next.ct < ct1 ? next.ct : ct1 - 1) * BN, k = next.k;
         const int K = ext ? P * W : p.K;   // of the rows
@@ -119,43 +119,38 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         }
         const int kx = k + kg * kU;
         l.xk = K - kx;
+        const int xs = l.xk > 0 ? start8(kx, K) : 0;
+        l.xe = l.xk > 0 ? kx - xs : 0;
         l.rows = 0;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int r = rr + kLanes * i;
             if (r >= at && r < end) l.rows |= 1u << i;
             const T *q = ext ? static_cast<const T *>(p.h) + (t.p0 + (r < rows ? r : 0)) * K : in[i];
-            if constexpr (VEC) {
-                q += l.xk > 0 ? kx : 0;
-                l.x[i].v[0] = *reinterpret_cast<const uint4_t *>(q);
-                if constexpr (Q > 1) l.x[i].v[1] = *reinterpret_cast<const uint4_t *>(q + (l.xk > 4 ? 4 : 0));
-            } else {
-                l.x[i] = load_row8<T, false>(q + kx, l.xk);
-            }
+            if constexpr (WIDE) l.x[i] = load_any8(q + xs);
+            else l.x[i] = load_row8<T, false>(q + kx, l.xk);
         }
         int kw = WNK ? kx : k + tg * kU;
         const bool in_k = kw < K;
         if (P == 2 && ext && kw >= W) kw -= W;  // the second part meets the same weights
         l.wk = in_k ? ld - kw : 0;
         if constexpr (WNK) {
+            const int ws = l.wk > 0 ? start8(kw, ld) : 0;
+            l.we = l.wk > 0 ? kw - ws : 0;
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
                 const int c = c0 + rr + kLanes * i;
                 const T *q = wb + (int64_t)(c < p.N ? c : p.N - 1) * ld;
-                if constexpr (VEC) {
-                    q += l.wk > 0 ? kw : 0;
-                    l.wn[i].v[0] = *reinterpret_cast<const uint4_any *>(q);
-                    if constexpr (Q > 1) l.wn[i].v[1] = *reinterpret_cast<const uint4_any *>(q + (l.wk > 4 ? 4 : 0));
-                } else {
-                    l.wn[i] = load_row8<T, false>(q + kw, l.wk);
-                }
+                if constexpr (WIDE) l.wn[i] = load_any8(q + ws);
+                else l.wn[i] = load_row8<T, false>(q + kw, l.wk);
             }
         } else {
             const int c = c0 + CW * tc;
+            l.we = c + CW <= p.N || c >= p.N ? 0 : c + CW - p.N;
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const T *q = wb + (int64_t)(u < l.wk ? kw + u : 0) * p.N;
-                if constexpr (VEC) l.wt[u] = *reinterpret_cast<const uint2_t *>(q + (c < p.N ? c : p.N - CW));
+                if constexpr (WIDE) l.wt[u] = *reinterpret_cast<const uint2_any *>(q + (c + CW <= p.N ? c : p.N - CW));
                 else l.wt[u] = load_8<T, false>(q + c, u < l.wk ? p.N - c : 0);
             }
         }
@@ -166,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             if (BM < kLanes && rr >= BM) break;
-            if (l.xk < kU || !(l.rows >> i & 1)) keep(l.x[i], l.rows >> i & 1 ? l.xk : 0);
+            if (l.xk < kU || !(l.rows >> i & 1)) settle(l.x[i], WIDE ? l.xe : 0, l.rows >> i & 1 ? l.xk : 0);
             to_units(l.x[i], u, lose);
             put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
         }
@@ -174,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
                 if (BN < kLanes && rr >= BN) break;
-                if (l.wk < kU) keep(l.wn[i], l.wk);
+                if (l.wk < kU) settle(l.wn[i], WIDE ? l.we : 0, l.wk);
                 to_units(l.wn[i], u, lose);
                 put<T, BN>(s_cols, KG, kg, rr + kLanes * i, u);
             }
@@ -182,6 +177,10 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
             if (l.wk < kU) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) l.wt[e] = e < l.wk ? l.wt[e] : uint2_t{0, 0};
+            }
+            if (WIDE && l.we > 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) settle<T>(l.wt[e], l.we);
             }
             uint4_t c[CW][Q];
             to_units(l.wt, c, lose);
@@ -233,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
-                        store_four<VEC>(q + col, vec_val<T, !WNK>(acc[c][r], v), p.N - col);
+                        store_four<false>(q + col, vec_val<T, !WNK>(acc[c][r], v), p.N - col);
                     }
             }
         }
@@ -259,25 +258,22 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         if (now.ct < ct1) step(kAhead == 2 ? odd : even);
     }
     if constexpr (Q > 1) {
-        __threadfence_block();
         if (__syncthreads_or(lose)) row_plain_sums<WNK>(o, p, t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end);
     }
 }
 
 template <typename T, bool WNK, int BM, int BN, int WR>
-hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s, bool big = false)
+hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    constexpr int V = 16 / (int)sizeof(T);
-    const bool vec = aligned_rows<T>(p.in, p.in_stride) && p.K % V == 0 && p.N % V == 0 &&
-                     aligned_rows<T>(p.w, 0) && (p.narrow || aligned_rows<T>(p.out, p.out_stride)) &&
-                     (!p.h || aligned_rows<T>(p.v, 0));
-    const int64_t tiles = big ? o.n / kFewRows : p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
+    // rows of eight values or more, of columns or k as they are loaded
+    const bool wide = p.K >= kU && (WNK ? !p.h || p.r >= kU : p.N >= kWide<T>);
+    const int64_t tiles = p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
     const int ctiles = (p.N + BN - 1) / BN;
     // few rows: column tiles go to workgroups of their own
     int splits = (int)(2048 / tiles);
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
-    auto *kernel = vec ? k_row_product<T, WNK, BM, BN, WR, true> : k_row_product<T, WNK, BM, BN, WR, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits, big);
+    auto *kernel = wide ? k_row_product<T, WNK, BM, BN, WR, true> : k_row_product<T, WNK, BM, BN, WR, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits);
     return hipGetLastError();
 }
 
@@ -286,11 +282,6 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
     const int64_t groups = p.w_group ? o.G : 1;
-    if (p.w_group && o.n <= kFewMean * groups) {
-        const hipError_t e = launch_row_few(dtype, o, p, s);
-        if (e != hipSuccess || o.n <= kFewRows) return e;
-        return p.N <= 32 ? launch<T, WNK, 128, 32, 4>(o, p, s, true) : launch<T, WNK, 128, 128, 2>(o, p, s, true);
-    }
     const bool few = o.n < 64 * groups;  // rows per group
     if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);

@@ -225,14 +225,46 @@ __device__ __forceinline__ Raw8<T> load_row8(const T *p, int64_t left)
     return r;
 }
 
-// Zeros from value `left` on.
-template <typename T> __device__ __forceinline__ void keep(Raw8<T> &r, int left)
+// Loads that must not pass the end of a row, and must not be under a condition, start early enough to end
+// with it; the values are moved down by what they started early when they are staged.
+
+// Where the load of eight values from k on starts in a row of K >= 8.
+__device__ __forceinline__ int start8(int k, int K) { return k + 8 <= K ? k : K - 8; }
+
+// Eight values at the alignment of one.
+template <typename T> __device__ __forceinline__ Raw8<T> load_any8(const T *q)
 {
+    Raw8<T> r;
+    r.v[0] = *reinterpret_cast<const uint4_any *>(q);
+    if constexpr (sizeof(T) == 4) r.v[1] = *reinterpret_cast<const uint4_any *>(q + 4);
+    return r;
+}
+
+// Moves the values down by `early`, and leaves zeros from value `left` on.
+template <typename T> __device__ __forceinline__ void settle(Raw8<T> &r, int early, int left)
+{
+    constexpr int D = (int)sizeof(T) * 2;  // registers
+    for (int i = 0; i < early; ++i) {
 #pragma unroll
-    for (int e = 0; e < (int)(sizeof(T) * 2); ++e) {
+        for (int e = 0; e < D; ++e) {
+            const unsigned v = r.v[e / 4][e % 4], up = e + 1 < D ? r.v[(e + 1) / 4 % (D / 4)][(e + 1) % 4] : 0u;
+            r.v[e / 4][e % 4] = sizeof(T) == 4 ? up : v >> 16 | up << 16;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < D; ++e) {
         const int first = e * 4 / (int)sizeof(T);  // of the values in this register
         const unsigned v = r.v[e / 4][e % 4];
         r.v[e / 4][e % 4] = first + (sizeof(T) == 2) < left ? v : first < left ? v & 0xffffu : 0u;
+    }
+}
+
+// The same for transposed loads of kWide columns, whose values past the last column are never used.
+template <typename T> __device__ __forceinline__ void settle(uint2_t &v, int early)
+{
+    for (int i = 0; i < early; ++i) {
+        v[0] = sizeof(T) == 4 ? v[1] : v[0] >> 16 | v[1] << 16;
+        v[1] = sizeof(T) == 4 ? 0u : v[1] >> 16;
     }
 }
 
@@ -442,6 +474,9 @@ template <bool WNK>
 __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group, int64_t p0, int rows, const int *s_row,
                                const int *s_g, int c0, int c1)
 {
+    // every wave's stores of these columns are done before they are stored again
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
     const int W = narrow_width(p.r), width = c1 - c0;
     const float *const w = static_cast<const float *>(p.w) + (int64_t)group * p.w_group;
     for (int e = threadIdx.x; e < rows * width; e += kThreads) {

@@ -6,11 +6,12 @@
 // only the weights of a tile pass through LDS, loaded a tile ahead. The results are turned in a piece of LDS
 // that the wave has for itself, and leave as rows of kCols values, four rows a store.
 //
-// Nothing in the loop over column tiles branches, where vectors are whole (VEC): the wait for the next
-// tile's weights can then leave this tile's stores in flight, and the sums stay where they are (a branch
-// around a matrix instruction costs a copy of its 32 registers). So the number of k is a template
-// argument, rounded up with zeros; places without a row of their own take another place's of the tile
-// (and store the same values to the same place), columns past the end the last ones.
+// Nothing in the loop over column tiles branches: the wait for the next tile's weights can then leave this
+// tile's stores in flight, and the sums stay where they are (a branch around a matrix instruction costs a
+// copy of its 32 registers). So the number of k is a template argument, rounded up with zeros; places
+// without a row of their own take another place's of the tile (and store the same values to the same
+// place), and the last column tile starts early enough to end with the rows. WHOLE: columns come in aligned
+// fours.
 //
 // Adapters: the narrow product's rows are further k of the same tile, held in registers like the
 // inputs, with the adapter's second matrix behind the shared weights in LDS; a tile whose rows have several
@@ -36,8 +37,8 @@ template <typename T> constexpr int kPiece = 128 / (int)sizeof(T);
 template <typename T> constexpr int kTurn = kPiece<T> + 4;
 
 template <typename T> struct Out4;
-template <> struct Out4<float> { typedef float4_t t; };
-template <> struct Out4<bf16_t> { typedef bf4_t t; };
+template <> struct Out4<float> { typedef float4_t t; typedef float4_any any; };
+template <> struct Out4<bf16_t> { typedef bf4_t t; typedef bf4_any any; };
 
 __device__ __forceinline__ void convert(float4_t v, float4_t &o) { o = v; }
 __device__ __forceinline__ void convert(float4_t v, bf4_t &o)
@@ -54,13 +55,14 @@ __device__ __forceinline__ void wave_sync()
 }
 
 // NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters).
-template <typename T, bool WNK, int NP, int XP, bool VEC>
+template <typename T, bool WNK, int NP, int XP, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p, int splits)
 {
     constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, KG = 2 * (NP + XP), LD = kCols + 1, CW = kWide<T>;
     constexpr bool EXT = XP > 0;
-    static_assert(NP <= kPairs<T> && !(EXT && (WNK || !VEC)), "adapters: [K][N] weights, whole vectors");
+    static_assert(NP <= kPairs<T> && !(EXT && WNK), "adapters: [K][N] weights");
     typedef typename Out4<T>::t O;
+    typedef typename Out4<T>::any O_any;
     __shared__ uint4_t s_w[Q * KG * LD];
     __shared__ O s_turn[4 * 32 * kTurn<T> / 4];
     __shared__ int s_row[kRows], s_place[kRows], s_any;
@@ -79,8 +81,10 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rows = (int)(t.p1 - t.p0);
     const int ctiles = (p.N + kCols - 1) / kCols;
-    const int ct0 = (int)((int64_t)ctiles * blockIdx.y / splits);
-    const int ct1 = (int)((int64_t)ctiles * (blockIdx.y + 1) / splits);
+    // this workgroup's column tiles: the last two, which overlap, go together
+    const int whole = p.N / kCols;
+    const int ct0 = (int)((int64_t)whole * blockIdx.y / splits);
+    const int ct1 = blockIdx.y + 1 == gridDim.y ? ctiles : (int)((int64_t)whole * (blockIdx.y + 1) / splits);
     if (ct0 >= ct1) return;
     const int my_row = tid < rows ? row_at(o, t.p0 + tid) : -1;
     if (tid < kRows) s_row[tid] = my_row;
@@ -107,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
 #pragma unroll
     for (int s = 0; s < NP; ++s) {
         const int k = (2 * s + half) * U;
-        to_units(load_row8<T, VEC>(in + k, p.K - k), x[s], lose);
+        to_units(load_row8<T, false>(in + k, p.K - k), x[s], lose);
     }
     if (EXT) {
         const bool grouped = s_g[pl] < o.G;
@@ -132,9 +136,11 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
     Raw8<T> wn[WNK ? NT : 1];
     uint2_t wt[WNK ? 1 : NT][8];
-    unsigned we[VEC || WNK ? 1 : NT][VEC || WNK ? 1 : 8 * CW];  // single values, packed when they are staged
+    int early[WNK ? NT : 1];  // what the loads started early
     int have[NT];  // k of the k-groups in flight that the weights have
+    auto first_col = [&](int ct) { return ct * kCols + kCols <= p.N ? ct * kCols : p.N - kCols; };
     auto fetch = [&](int ct, int seg) {
+        const int c0 = first_col(ct);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const int task = tid + kThreads * i;
@@ -150,30 +156,15 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             have[i] = K - k;
             if (have[i] <= 0) k = 0;
             if constexpr (WNK) {
-                const int c = ct * kCols + task / KG;
-                const T *const q = wb + (int64_t)(c < p.N ? c : p.N - 1) * p.K + k;
-                if (VEC) {  // of fp32 the second half of a k-group may be past the end: the first again
-                    wn[i].v[0] = *reinterpret_cast<const uint4_t *>(q);
-                    if constexpr (Q > 1) wn[i].v[1] = *reinterpret_cast<const uint4_t *>(q + (have[i] > 4 ? 4 : 0));
-                } else {
-                    wn[i] = load_row8<T, false>(q, have[i]);
-                }
+                const T *const q = wb + (int64_t)(c0 + task / KG) * p.K;
+                const int at = start8(k, p.K);
+                early[i] = k - at;
+                wn[i] = load_any8(q + at);
             } else {
-                const int c = ct * kCols + CW * (task % (kCols / CW));
+                const int c = c0 + CW * (task % (kCols / CW));
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const T *const q = wb + (int64_t)(u < have[i] ? k + u : 0) * p.N;
-                    if constexpr (VEC) {
-                        wt[i][u] = *reinterpret_cast<const uint2_t *>(q + (c < p.N ? c : p.N - CW));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < CW; ++e) {
-                            const T *const z = q + (c + e < p.N ? c + e : p.N - 1);
-                            we[i][CW * u + e] = sizeof(T) == 2 ? *reinterpret_cast<const unsigned short *>(z)
-                                                               : *reinterpret_cast<const unsigned *>(z);
-                        }
-                    }
-                }
+                for (int u = 0; u < U; ++u)
+                    wt[i][u] = *reinterpret_cast<const uint2_any *>(wb + (int64_t)(u < have[i] ? k + u : 0) * p.N + c);
             }
         }
     };
@@ -185,24 +176,13 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             if constexpr (WNK) {
                 uint4_t unit[Q];
                 Raw8<T> raw = wn[i];
-                if (have[i] <= 0) raw.v[0] = uint4_t{0, 0, 0, 0};
-                if constexpr (Q > 1)
-                    if (have[i] <= 4) raw.v[1] = uint4_t{0, 0, 0, 0};
+                if (have[i] < kU) settle(raw, early[i], have[i]);
                 to_units(raw, unit, lose);
                 put<T, kCols>(s_w, KG, task % KG, task / KG, unit);
             } else {
                 uint2_t in[8];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    in[u] = wt[i][u];
-                    if constexpr (!VEC) {
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            in[u][e] = sizeof(T) == 2 ? we[i][CW * u + 2 * e] | we[i][CW * u + 2 * e + 1] << 16
-                                                      : we[i][CW * u + e];
-                    }
-                    if (u >= have[i]) in[u] = uint2_t{0, 0};
-                }
+                for (int u = 0; u < U; ++u) in[u] = u < have[i] ? wt[i][u] : uint2_t{0, 0};
                 uint4_t unit[CW][Q];
                 to_units(in, unit, lose);
 #pragma unroll
@@ -267,47 +247,31 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                     convert(vec_val<T, !WNK>(acc[piece / 32 + c], v),
                             turn[((lane & 31) * kTurn<T> + 32 * c + vec_col<T, !WNK>(v, half)) / 4]);
             wave_sync();
-            const int first = ct * kCols + piece;
-            if (piece > 0 && first >= p.N) break;
-            int in_piece = 4 * (lane % kVecs);  // past the last column, the last columns again
-            if (VEC && first + in_piece >= p.N) in_piece = p.N - 4 - first;
-            const int col = first + in_piece;
+            const int in_piece = 4 * (lane % kVecs), col = first_col(ct) + piece + in_piece;
 #pragma unroll
             for (int i = 0; i < kStores; ++i) {
-                const O val = turn[(((64 / kVecs) * i + lane / kVecs) * kTurn<T> + in_piece) / 4];
-                if (VEC) {
-                    *reinterpret_cast<O *>(out[i] + col) = val;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + e < p.N) out[i][col + e] = val[e];
-                }
+                const T *const from = reinterpret_cast<const T *>(turn) +
+                                      ((64 / kVecs) * i + lane / kVecs) * kTurn<T> + in_piece;
+                if (WHOLE) *reinterpret_cast<O *>(out[i] + col) = *reinterpret_cast<const O *>(from);
+                else *reinterpret_cast<O_any *>(out[i] + col) = *reinterpret_cast<const O_any *>(from);
             }
             wave_sync();
         }
     }
     if constexpr (Q > 1) {
-        __threadfence_block();
-        if (__syncthreads_or(lose))
-            row_plain_sums<WNK>(o, p, t.g, t.p0, rows, s_row, s_g, ct0 * kCols, ct1 * kCols < p.N ? ct1 * kCols : p.N);
+        const int end = ct1 * kCols < p.N ? ct1 * kCols : p.N;
+        if (__syncthreads_or(lose)) row_plain_sums<WNK>(o, p, t.g, t.p0, rows, s_row, s_g, ct0 * kCols, end);
     }
 }
 
-template <typename T> bool whole_vectors(const RowProduct &p)
-{
-    constexpr int V = 16 / (int)sizeof(T);
-    return aligned_rows<T>(p.in, p.in_stride) && p.K % V == 0 && p.N % V == 0 && aligned_rows<T>(p.w, 0) &&
-           aligned_rows<T>(p.out, p.out_stride) && (!p.h || aligned_rows<T>(p.v, 0));
-}
-
-template <typename T, bool WNK, int NP, int XP, bool VEC>
+template <typename T, bool WNK, int NP, int XP, bool WHOLE>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int64_t tiles = XP > 0 ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
-    const int ctiles = (p.N + kCols - 1) / kCols;
+    const int whole = p.N / kCols;
     int splits = (int)(2048 / tiles);  // few rows: column tiles go to workgroups of their own
-    splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
-    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, VEC>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
+    splits = splits < 1 ? 1 : splits > whole ? whole : splits;
+    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, WHOLE>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
                        0, s, o, p, splits);
     return hipGetLastError();
 }
@@ -323,8 +287,11 @@ template <typename T, int NP> hipError_t with_pairs(const RowOrder &o, const Row
 template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     constexpr int M = kPairs<T>;
-    if (!whole_vectors<T>(p))
+    const bool whole = p.N % 4 == 0 && p.out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * sizeof(T)) == 0;
+    if (!whole) {
+        if (p.h) return launch<T, false, M, kExtPairs<T>, false>(o, p, s);
         return p.w_nk ? launch<T, true, M, 0, false>(o, p, s) : launch<T, false, M, 0, false>(o, p, s);
+    }
     if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4>(o, p, s);
     if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2>(o, p, s);
     return with_pairs<T, M>(o, p, s);
@@ -333,8 +300,8 @@ template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hi
 template <typename T> bool takes(const RowProduct &p)
 {
     if (p.narrow || p.N <= kCols || p.K > 2 * kPairs<T> * kU) return false;
-    if (!p.h) return p.w_group != 0;
-    return !p.w_nk && whole_vectors<T>(p) && kNarrow<T> * narrow_width(p.r) <= 2 * kExtPairs<T> * kU;
+    if (!p.h) return p.w_group != 0 && (!p.w_nk || p.K >= kU);
+    return !p.w_nk && kNarrow<T> * narrow_width(p.r) <= 2 * kExtPairs<T> * kU;
 }
 
 }  // namespace
