@@ -246,19 +246,7 @@ extern "C" int cgtp_adapter_linear(int dtype, int64_t n_rows, int n_groups, int 
     CGTP_TRY(check_ws(workspace, ws_bytes, adapter_bytes(dtype, n_rows, rank)));
     const cgtp::RowOrder o{n_rows, n_groups, offsets, order};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    cgtp::RowProduct p{};  // h = scale a^T x
-    p.in = x;
-    p.in_stride = x_stride;
-    p.K = n_in;
-    p.w = a;
-    p.w_group = (int64_t)n_in * rank;
-    p.N = rank;
-    p.out = workspace;
-    p.narrow = true;
-    p.narrow_scale = scale;
-    hipError_t e = cgtp::launch_row_product(dtype, o, p, s);
-    if (e != hipSuccess) return hip_fail(e, "adapter's first product");
-    p = cgtp::RowProduct{};
+    cgtp::RowProduct p{};
     p.in = x;
     p.in_stride = x_stride;
     p.K = n_in;
@@ -266,9 +254,30 @@ extern "C" int cgtp_adapter_linear(int dtype, int64_t n_rows, int n_groups, int 
     p.N = n_out;
     p.out = y;
     p.out_stride = y_stride;
-    p.h = workspace;
+    p.a = a;
     p.v = b;
     p.r = rank;
+    p.narrow_scale = scale;
+    hipError_t e;
+    if (cgtp::adapter_wide_takes(dtype, o, p)) {
+        e = cgtp::launch_adapter_wide(dtype, o, p, s);
+        return e == hipSuccess ? CGTP_OK : hip_fail(e, "adapter product");
+    }
+    cgtp::RowProduct q{};  // h = scale a^T x
+    q.in = x;
+    q.in_stride = x_stride;
+    q.K = n_in;
+    q.w = a;
+    q.w_group = (int64_t)n_in * rank;
+    q.N = rank;
+    q.out = workspace;
+    q.narrow = true;
+    q.narrow_scale = scale;
+    e = cgtp::launch_row_product(dtype, o, q, s);
+    if (e != hipSuccess) return hip_fail(e, "adapter's first product");
+    p.a = nullptr;
+    p.narrow_scale = nullptr;
+    p.h = workspace;
     e = cgtp::launch_row_product(dtype, o, p, s);
     return e == hipSuccess ? CGTP_OK : hip_fail(e, "shared product");
 }

@@ -469,10 +469,10 @@ template <typename T> __device__ __forceinline__ float narrow_at(const void *h, 
 }
 
 // The sums of a workgroup that met values outside the range of parts, in plain fp32: columns [c0, c1) of its
-// rows, one result a thread at a time.
+// rows, one result a thread at a time. h: the narrow product's rows in LDS, 32 apart, in place of p.h.
 template <bool WNK>
 __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group, int64_t p0, int rows, const int *s_row,
-                               const int *s_g, int c0, int c1)
+                               const int *s_g, int c0, int c1, const float *h = nullptr)
 {
     // every wave's stores of these columns are done before they are stored again
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -485,10 +485,10 @@ __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group
         const float *const in = static_cast<const float *>(p.in) + s_row[r] * p.in_stride;
         float sum = 0.f;
         for (int k = 0; k < p.K; ++k) sum += in[k] * w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c];
-        if (p.h && s_g[r] < o.G) {
+        if ((p.h || h) && s_g[r] < o.G) {
             const float *const v = static_cast<const float *>(p.v) + (int64_t)s_g[r] * p.r * p.N;
             for (int k = 0; k < p.r; ++k)
-                sum += narrow_at<float>(p.h, p0 + r, W, k) * v[WNK ? (int64_t)c * p.r + k : (int64_t)k * p.N + c];
+                sum += (h ? h[32 * r + k] : narrow_at<float>(p.h, p0 + r, W, k)) * v[WNK ? (int64_t)c * p.r + k : (int64_t)k * p.N + c];
         }
         if (p.narrow)
             static_cast<float *>(p.out)[(p0 + r) * narrow_width(p.N) + c] =

@@ -15,7 +15,9 @@
 //
 // Adapters: the narrow product's rows are further k of the same tile, held in registers like the
 // inputs, with the adapter's second matrix behind the shared weights in LDS; a tile whose rows have several
-// adapters takes them one after the other, with the rows of the others zero.
+// adapters takes them one after the other, with the rows of the others zero. Where adapters have rows enough
+// for tiles of their own (FUSED) the narrow product is formed here too: from the inputs in registers and the
+// adapter's first matrix through LDS, turned in the wave's piece, and held from then on.
 #include "internal.h"
 #include "rows_tile.h"
 
@@ -27,6 +29,7 @@ using namespace rows;
 
 constexpr int kRows = 128;    // positions of a workgroup, 32 a wave
 constexpr int kCols = 64;     // columns of a tile
+constexpr int kTilesAtOnce = 256;
 template <typename T> constexpr int kPairs = sizeof(T) == 2 ? 8 : 4;  // pairs of k-groups: up to 128 bf16, 64 fp32
 template <typename T> constexpr int kExtPairs = sizeof(T) == 2 ? 4 : 2;  // of a narrow product's rows, up to 32 wide
 
@@ -55,7 +58,7 @@ __device__ __forceinline__ void wave_sync()
 }
 
 // NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters).
-template <typename T, bool WNK, int NP, int XP, bool WHOLE>
+template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p, int splits)
 {
     constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, KG = 2 * (NP + XP), LD = kCols + 1, CW = kWide<T>;
@@ -69,7 +72,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     __shared__ int s_g[EXT ? kRows : 1], s_seg_g[EXT ? kRows : 1], s_seg_at[EXT ? kRows + 1 : 1], s_nseg;
 
     Tile t;
-    if (EXT) {
+    if (EXT && !FUSED) {
         t.p0 = (int64_t)blockIdx.x * kRows;
         t.p1 = t.p0 + kRows < o.n ? t.p0 + kRows : o.n;
         t.g = 0;
@@ -96,7 +99,15 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         return;
     }
     int nseg = 0;
-    if (EXT) nseg = find_segments<kRows>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
+    if (FUSED) {
+        nseg = t.g < o.G;
+        if (tid == 0) {
+            s_seg_g[0] = nseg ? t.g : 0;
+            s_seg_at[0] = 0;
+            s_seg_at[1] = kRows;
+        }
+        __syncthreads();
+    } else if (EXT) nseg = find_segments<kRows>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
     else __syncthreads();
     if (s_any < 0) return;
     if (tid < kRows) s_place[tid] = my_row >= 0 ? tid : s_any;
@@ -113,7 +124,51 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         const int k = (2 * s + half) * U;
         to_units(load_row8<T, false>(in + k, p.K - k), x[s], lose);
     }
-    if (EXT) {
+    O *const turn = s_turn + wave * (32 * kTurn<T> / 4);
+    if constexpr (FUSED) {
+        // the adapter's first matrix, [K][r], as a tile of 32 columns
+        constexpr int kQuads = 32 / CW;
+        for (int task = tid; task < kQuads * 2 * NP; task += kThreads) {
+            const int g = task / kQuads, c = CW * (task % kQuads);
+            const T *const q = static_cast<const T *>(p.a) + ((int64_t)(nseg ? t.g : 0) * p.K + g * U) * p.r + c;
+            uint2_t in[8];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                in[u] = load_8<T, false>(q + (int64_t)u * p.r, nseg && g * U + u < p.K ? p.r - c : 0);
+            uint4_t unit[CW][Q];
+            to_units(in, unit, lose);
+#pragma unroll
+            for (int j = 0; j < CW; ++j) put<T, kCols>(s_w, KG, g, place<T>(c + j), unit[j]);
+        }
+        __syncthreads();
+        float16_t sum;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+            uint4_t c[Q];
+#pragma unroll
+            for (int q = 0; q < Q; ++q) c[q] = s_w[(q * KG + 2 * s + half) * LD + (lane & 31)];
+            mma(sum, c, x[s]);
+        }
+        const float scale = p.narrow_scale && nseg ? p.narrow_scale[t.g] : 1.f;
+        T *const mine = reinterpret_cast<T *>(turn) + (lane & 31) * kTurn<T>;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int col = vec_col<T, true>(v, half);
+            float4_t f = vec_val<T, true>(sum, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] *= scale;
+            if (col < W) store_narrow(mine + col, W, f);
+        }
+        wave_sync();
+#pragma unroll
+        for (int s = 0; s < XP; ++s) {
+            const int k = (2 * s + half) * U;
+            to_units(load_row8<T, false>(mine + k, P * W - k), h[s], lose);
+        }
+        wave_sync();
+    } else if (EXT) {
         const bool grouped = s_g[pl] < o.G;
 #pragma unroll
         for (int s = 0; s < XP; ++s) {
@@ -133,7 +188,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     // other adapters' of the tile.
     constexpr int kTasks = (WNK ? kCols : kCols / CW) * KG;  // units, or units of CW columns
     constexpr int NT = (kTasks + kThreads - 1) / kThreads;
-    const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
+    const T *const w = static_cast<const T *>(p.w) + (FUSED ? 0 : (int64_t)t.g * p.w_group);
     Raw8<T> wn[WNK ? NT : 1];
     uint2_t wt[WNK ? 1 : NT][8];
     int early[WNK ? NT : 1];  // what the loads started early
@@ -192,7 +247,6 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         }
     };
 
-    O *const turn = s_turn + wave * (32 * kTurn<T> / 4);
     const uint4_t *const a = s_w + half * LD + (lane & 31);
     fetch(ct0, 0);
     for (int ct = ct0; ct < ct1; ++ct) {
@@ -260,47 +314,63 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     }
     if constexpr (Q > 1) {
         const int end = ct1 * kCols < p.N ? ct1 * kCols : p.N;
-        if (__syncthreads_or(lose)) row_plain_sums<WNK>(o, p, t.g, t.p0, rows, s_row, s_g, ct0 * kCols, end);
+        if (__syncthreads_or(lose)) {
+            float *const plain_h = FUSED ? reinterpret_cast<float *>(s_turn) : nullptr;
+            if constexpr (FUSED) {
+                static_assert(sizeof(s_turn) >= sizeof(float) * kRows * 32, "rows of up to 32 values");
+                for (int e = tid; e < rows * p.r; e += kThreads) {
+                    const int r = e / p.r, c = e % p.r;
+                    const float *const ac = reinterpret_cast<const float *>(p.a) + (int64_t)(nseg ? t.g : 0) * p.K * p.r + c;
+                    float sum = 0.f;
+                    if (nseg && s_row[r] >= 0)
+                        for (int k = 0; k < p.K; ++k)
+                            sum += reinterpret_cast<const float *>(p.in)[s_row[r] * p.in_stride + k] * ac[(int64_t)k * p.r];
+                    plain_h[32 * r + c] = p.narrow_scale && nseg ? sum * p.narrow_scale[t.g] : sum;
+                }
+                if (tid < rows) s_g[tid] = t.g;
+            }
+            row_plain_sums<WNK>(o, p, p.w_group ? t.g : 0, t.p0, rows, s_row, s_g, ct0 * kCols, end, plain_h);
+        }
     }
 }
 
-template <typename T, bool WNK, int NP, int XP, bool WHOLE>
+template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    const int64_t tiles = XP > 0 ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
+    const int64_t tiles = XP > 0 && !FUSED ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
     const int whole = p.N / kCols;
     int splits = (int)(2048 / tiles);  // few rows: column tiles go to workgroups of their own
     splits = splits < 1 ? 1 : splits > whole ? whole : splits;
-    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, WHOLE>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
+    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
                        0, s, o, p, splits);
     return hipGetLastError();
 }
 
-template <typename T, int NP> hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
+template <typename T, int NP, bool WHOLE> hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    if (!p.h) return p.w_nk ? launch<T, true, NP, 0, true>(o, p, s) : launch<T, false, NP, 0, true>(o, p, s);
+    if (!p.h && !p.a)
+        return p.w_nk ? launch<T, true, NP, 0, false, WHOLE>(o, p, s) : launch<T, false, NP, 0, false, WHOLE>(o, p, s);
     constexpr int X = kExtPairs<T>;
-    const bool half = kNarrow<T> * narrow_width(p.r) <= X * kU;
-    return half ? launch<T, false, NP, X / 2, true>(o, p, s) : launch<T, false, NP, X, true>(o, p, s);
+    const bool half = WHOLE && kNarrow<T> * narrow_width(p.r) <= X * kU;
+    constexpr int H = WHOLE ? X / 2 : X;
+    if (p.a) return half ? launch<T, false, NP, H, true, WHOLE>(o, p, s) : launch<T, false, NP, X, true, WHOLE>(o, p, s);
+    return half ? launch<T, false, NP, H, false, WHOLE>(o, p, s) : launch<T, false, NP, X, false, WHOLE>(o, p, s);
 }
 
 template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     constexpr int M = kPairs<T>;
     const bool whole = p.N % 4 == 0 && p.out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * sizeof(T)) == 0;
-    if (!whole) {
-        if (p.h) return launch<T, false, M, kExtPairs<T>, false>(o, p, s);
-        return p.w_nk ? launch<T, true, M, 0, false>(o, p, s) : launch<T, false, M, 0, false>(o, p, s);
-    }
-    if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4>(o, p, s);
-    if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2>(o, p, s);
-    return with_pairs<T, M>(o, p, s);
+    if (!whole) return with_pairs<T, M, false>(o, p, s);
+    if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4, true>(o, p, s);
+    if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2, true>(o, p, s);
+    return with_pairs<T, M, true>(o, p, s);
 }
 
 template <typename T> bool takes(const RowProduct &p)
 {
     if (p.narrow || p.N <= kCols || p.K > 2 * kPairs<T> * kU) return false;
-    if (!p.h) return p.w_group != 0 && (!p.w_nk || p.K >= kU);
+    if (!p.h && !p.a) return p.w_group != 0 && (!p.w_nk || p.K >= kU);
     return !p.w_nk && kNarrow<T> * narrow_width(p.r) <= 2 * kExtPairs<T> * kU;
 }
 
@@ -309,6 +379,17 @@ template <typename T> bool takes(const RowProduct &p)
 bool row_wide_takes(int dtype, const RowProduct &p)
 {
     return dtype == CGTP_BF16 ? takes<bf16_t>(p) : takes<float>(p);
+}
+
+// Tiles of one adapter each: where adapters have 64 rows on the mean, or all tiles run at once anyway.
+bool adapter_wide_takes(int dtype, const RowOrder &o, const RowProduct &p)
+{
+    return (o.n >= 64 * (int64_t)o.G || o.n / kRows + o.G < kTilesAtOnce) && row_wide_takes(dtype, p);
+}
+
+hipError_t launch_adapter_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    return launch_row_wide(dtype, o, p, s);
 }
 
 hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)
