@@ -260,7 +260,7 @@ extern "C" int cgtp_adapter_linear(int dtype, int64_t n_rows, int n_groups, int 
     p.narrow_scale = scale;
     hipError_t e;
     if (cgtp::adapter_wide_takes(dtype, o, p)) {
-        e = cgtp::launch_adapter_wide(dtype, o, p, s);
+        e = cgtp::launch_row_product(dtype, o, p, s);
         return e == hipSuccess ? CGTP_OK : hip_fail(e, "adapter product");
     }
     cgtp::RowProduct q{};  // h = scale a^T x
@@ -325,7 +325,22 @@ extern "C" int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups,
     char *const u = h + adapter_bytes(dtype, n_rows, rank);
     char *const sums = u + adapter_bytes(dtype, n_rows, rank);
     hipError_t e;
-    if ((dx || da) && n_rows > 0) {  // u = scale b dy
+    cgtp::RowProduct px{};  // dx = w dy + a u
+    px.in = dy;
+    px.in_stride = dy_stride;
+    px.K = n_out;
+    px.w = w;
+    px.w_nk = true;
+    px.N = n_in;
+    px.out = dx;
+    px.out_stride = dx_stride;
+    px.a = b;
+    px.h_out = u;
+    px.v = a;
+    px.r = rank;
+    px.narrow_scale = scale;
+    const bool together = dx && n_rows > 0 && cgtp::adapter_product_takes(dtype, o, px);
+    if ((dx || da) && n_rows > 0 && !together) {  // u = scale b dy
         cgtp::RowProduct p{};
         p.in = dy;
         p.in_stride = dy_stride;
@@ -355,19 +370,13 @@ extern "C" int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups,
         if (e != hipSuccess) return hip_fail(e, "adapter's first product");
     }
     if (dx && n_rows > 0) {
-        cgtp::RowProduct p{};
-        p.in = dy;
-        p.in_stride = dy_stride;
-        p.K = n_out;
-        p.w = w;
-        p.w_nk = true;
-        p.N = n_in;
-        p.out = dx;
-        p.out_stride = dx_stride;
-        p.h = u;
-        p.v = a;
-        p.r = rank;
-        e = cgtp::launch_row_product(dtype, o, p, s);
+        if (!together) {
+            px.a = nullptr;
+            px.h_out = nullptr;
+            px.narrow_scale = nullptr;
+            px.h = u;
+        }
+        e = cgtp::launch_row_product(dtype, o, px, s);
         if (e != hipSuccess) return hip_fail(e, "row gradient");
     }
     if (da) {

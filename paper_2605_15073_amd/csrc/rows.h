@@ -37,7 +37,9 @@ struct RowProduct {
     // adapters: out_i += scale_g H_i V_g with H from a narrow product before, V per group [r][N] or
     // [N][r] (as W). NULL: none.
     const void *h;
-    const void *a;     // instead of h: the adapters' first matrices (launch_adapter_wide)
+    const void *a;     // instead of h: the adapters' first matrices, [K][r] or [r][K] as W, from which the
+                       // kernel forms H itself (where *_takes says so); narrow_scale is its factor
+    void *h_out;       // then, if not NULL: H, as a narrow product leaves it
     const void *v;
     int r;
     bool narrow;       // out is a narrow product: in sequence order, fp32 [n][N]
@@ -47,10 +49,9 @@ hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p,
 // The form for short inputs and wide outputs (rows_wide.hip), and whether it covers a product.
 bool row_wide_takes(int dtype, const RowProduct &p);
 hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
-// The same with the adapters' first product inside: p.a is their [K][r] matrices, p.h NULL, p.narrow_scale the
-// factor of that product.
+// Products with p.a: whether some form covers one (the launch is that of launch_row_product).
 bool adapter_wide_takes(int dtype, const RowOrder &o, const RowProduct &p);
-hipError_t launch_adapter_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
+bool adapter_product_takes(int dtype, const RowOrder &o, const RowProduct &p);
 
 // out_g = sum over the rows of group g of a_i b_i^T, [A][B]; with h, the result of a narrow product,
 // in place of b: [A][r], or [r][A] where transposed.

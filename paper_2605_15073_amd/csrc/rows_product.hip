@@ -13,6 +13,10 @@
 // segment of rows at a time, with the narrow product's result as input rows (zero outside the
 // segment) and the adapter's second matrix as weights: the epilogue is fused, and rows of many
 // adapters share the tile.
+//
+// FUSED: tiles of one adapter each, whose narrow product is formed here too. Its matrix, [r][K] like the
+// shared weights, gives 32 more columns of the tile (so the input is read once for both); the result goes
+// through LDS as the input rows of one more step, over the adapter's second matrix.
 #include "internal.h"
 #include "rows_tile.h"
 
@@ -22,11 +26,13 @@ namespace {
 
 using namespace rows;
 
-template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE>
+template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED>
 __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
+    constexpr int BX = BN + (FUSED ? 32 : 0), TX = TC + (FUSED ? 1 : 0);  // with the narrow product's columns
+    static_assert(!FUSED || (WNK && WR == 4 && WIDE), "fused: a wave has whole rows, weights are [N][K]");
     constexpr int kShift = BM == 128 ? 7 : BM == 64 ? 6 : 5;
     static_assert(BM == 1 << kShift && TR >= 1 && TC >= 1, "tile");
     // steps of loads in flight: two of fp32, whose parts take longer to form and multiply, one where that
@@ -34,11 +40,11 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     constexpr int kAhead = WIDE && Q > 1 ? 2 : 1;
     constexpr int kLanes = kThreads / KG;              // rows staged at once
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
-    constexpr int NC = BN / kLanes > 0 ? BN / kLanes : 1;
-    __shared__ uint4_t s_cols[kTile<T, BN>], s_rows[kTile<T, BM>];
+    constexpr int NC = (BX + kLanes - 1) / kLanes;
+    __shared__ uint4_t s_cols[kTile<T, BX>], s_rows[kTile<T, BM>];
     __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg;
 
-    const bool shared_w = p.w_group == 0;
+    const bool shared_w = !FUSED && p.w_group == 0;
     Tile t;
     if (shared_w) {
         t.p0 = (int64_t)blockIdx.x * BM;
@@ -59,12 +65,13 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     const int col_end = ct1 * BN < p.N ? ct1 * BN : p.N;
 
     if (tid < BM) s_row[tid] = tid < rows ? row_at(o, t.p0 + tid) : -1;
-    if (!shared_w && t.g == o.G) {  // rows of no group
+    if (!FUSED && !shared_w && t.g == o.G) {  // rows of no group
         if (p.narrow) return;
         __syncthreads();
         store_zeros<T>(p, s_row, rows, ct0 * BN, col_end);
         return;
     }
+    const bool grouped = t.g < o.G;
     int nseg = 0;
     if (shared_w && p.h) nseg = find_segments<BM>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
     __syncthreads();
@@ -77,7 +84,8 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         const int r = rr + kLanes * i, row = r < BM ? s_row[r] : -1;
         in[i] = static_cast<const T *>(p.in) + (row < 0 ? 0 : row) * p.in_stride;  // row 0: never stored
     }
-    const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
+    const T *const w = static_cast<const T *>(p.w) + (FUSED ? 0 : (int64_t)t.g * p.w_group);
+    const T *const narrow_w = FUSED && grouped ? static_cast<const T *>(p.a) + (int64_t)t.g * p.r * p.K : w;
     const int W = narrow_width(p.r);  // of a part of the narrow input
     // transposed weights: columns CW tc .. CW tc + CW - 1, k-group tg
     constexpr bool kIdle = BN / CW * KG < kThreads;  // some threads have none to stage
@@ -139,8 +147,9 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
             l.we = l.wk > 0 ? kw - ws : 0;
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                const int c = c0 + rr + kLanes * i;
+                const int cl = rr + kLanes * i, c = c0 + cl;
                 const T *q = wb + (int64_t)(c < p.N ? c : p.N - 1) * ld;
+                if (FUSED && cl >= BN) q = narrow_w + (int64_t)(grouped && cl - BN < p.r ? cl - BN : 0) * ld;
                 if constexpr (WIDE) l.wn[i] = load_any8(q + ws);
                 else l.wn[i] = load_row8<T, false>(q + kw, l.wk);
             }
@@ -168,10 +177,10 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         if constexpr (WNK) {
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                if (BN < kLanes && rr >= BN) break;
+                if (BX % kLanes != 0 && rr + kLanes * i >= BX) break;
                 if (l.wk < kU) settle(l.wn[i], WIDE ? l.we : 0, l.wk);
                 to_units(l.wn[i], u, lose);
-                put<T, BN>(s_cols, KG, kg, rr + kLanes * i, u);
+                put<T, BX>(s_cols, KG, kg, rr + kLanes * i, u);
             }
         } else if (has_w) {
             if (l.wk < kU) {
@@ -185,16 +194,16 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
             uint4_t c[CW][Q];
             to_units(l.wt, c, lose);
 #pragma unroll
-            for (int j = 0; j < CW; ++j) put<T, BN>(s_cols, KG, tg, place<T>(CW * tc + j), c[j]);
+            for (int j = 0; j < CW; ++j) put<T, BX>(s_cols, KG, tg, place<T>(CW * tc + j), c[j]);
         }
     };
 
     const int wr = wave % WR, wc = wave / WR;
     const int r0 = wr * (BM / WR), c0w = wc * (BN / WC);
-    float16_t acc[TC][TR];
+    float16_t acc[TX][TR];
     auto clear = [&]() {
 #pragma unroll
-        for (int c = 0; c < TC; ++c)
+        for (int c = 0; c < TX; ++c)
 #pragma unroll
             for (int r = 0; r < TR; ++r)
 #pragma unroll
@@ -237,15 +246,49 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
             }
         }
     };
+    // FUSED: the narrow sums, scaled, are written out and become the rows of a step over v
+    auto narrow_step = [&]() {
+        const float scale = p.narrow_scale && grouped ? p.narrow_scale[t.g] : grouped ? 1.f : 0.f;
+        const int place = r0 + (lane & 31);
+        T *const out = static_cast<T *>(p.h_out) + (t.p0 + place) * (P * W);
+        __syncthreads();  // the last step's tiles are consumed
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int col = vec_col<T, false>(v, half);
+            float4_t x = vec_val<T, false>(acc[TX - 1][0], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = grouped && col + e < p.r ? x[e] * scale : 0.f;
+            if (p.h_out && grouped && place < rows && col < W) store_narrow(out + col, W, x);
+            put_narrow<T, BM>(s_rows, v, place, half, W / kU, x, lose);
+        }
+        uint4_t u[Q];
+        for (int task = tid; task < BN * KG; task += kThreads) {
+            const int g = task % KG, c = task / KG;
+            int k = g * kU;
+            const bool in_k = k < P * W && c < p.N && grouped;
+            if (P == 2 && k >= W) k -= W;  // the second part meets the same weights
+            const T *const q = static_cast<const T *>(p.v) + ((int64_t)(grouped ? t.g : 0) * p.N + c) * p.r + k;
+            to_units(load_row8<T, false>(q, in_k ? p.r - k : 0), u, lose);
+            put<T, BX>(s_cols, KG, g, c, u);
+        }
+        __syncthreads();
+        float16_t sums[TC][TR];
+#pragma unroll
+        for (int c = 0; c < TC; ++c) sums[c][0] = acc[c][0];
+        step_products<T, BX, BM, TC, TR>(sums, s_cols, s_rows, c0w, r0);
+#pragma unroll
+        for (int c = 0; c < TC; ++c) acc[c][0] = sums[c][0];
+    };
     auto step = [&](Loads &l) {
         __syncthreads();
         stage(l);
         __syncthreads();
         fetch(l);
-        step_products<T, BN, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0);
+        step_products<T, BX, BM, TX, TR>(acc, s_cols, s_rows, c0w, r0);
         const int ct = now.ct;
         advance(now);
         if (now.ct != ct) {
+            if constexpr (FUSED) narrow_step();
             store(ct);
             clear();
         }
@@ -258,21 +301,40 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         if (now.ct < ct1) step(kAhead == 2 ? odd : even);
     }
     if constexpr (Q > 1) {
-        if (__syncthreads_or(lose)) row_plain_sums<WNK>(o, p, t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end);
+        if (__syncthreads_or(lose)) {
+            float *const h = FUSED ? reinterpret_cast<float *>(s_cols) : nullptr;
+            if constexpr (FUSED) {
+                static_assert(sizeof(s_cols) >= sizeof(float) * BM * 32, "rows of up to 32 values");
+                for (int e = tid; e < rows * p.r; e += kThreads) {
+                    const int r = e / p.r, c = e % p.r;
+                    float sum = 0.f;
+                    if (grouped && s_row[r] >= 0)
+                        for (int k = 0; k < p.K; ++k)
+                            sum += reinterpret_cast<const float *>(p.in)[s_row[r] * p.in_stride + k] *
+                                   reinterpret_cast<const float *>(narrow_w)[(int64_t)c * p.K + k];
+                    if (p.narrow_scale && grouped) sum *= p.narrow_scale[t.g];
+                    h[32 * r + c] = sum;
+                    if (p.h_out && grouped) static_cast<float *>(p.h_out)[(t.p0 + r) * W + c] = sum;
+                }
+                if (tid < rows) s_g[tid] = t.g;
+            }
+            row_plain_sums<WNK>(o, p, FUSED ? 0 : t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end, h);
+        }
     }
 }
 
-template <typename T, bool WNK, int BM, int BN, int WR>
+template <typename T, bool WNK, int BM, int BN, int WR, bool FUSED = false>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     // rows of eight values or more, of columns or k as they are loaded
     const bool wide = p.K >= kU && (WNK ? !p.h || p.r >= kU : p.N >= kWide<T>);
-    const int64_t tiles = p.w_group ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
+    const int64_t tiles = p.w_group || FUSED ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
     const int ctiles = (p.N + BN - 1) / BN;
     // few rows: column tiles go to workgroups of their own
     int splits = (int)(2048 / tiles);
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
-    auto *kernel = wide ? k_row_product<T, WNK, BM, BN, WR, true> : k_row_product<T, WNK, BM, BN, WR, false>;
+    auto *kernel = FUSED || wide ? k_row_product<T, WNK, BM, BN, WR, true, FUSED>
+                                 : k_row_product<T, WNK, BM, BN, WR, FUSED, FUSED>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits);
     return hipGetLastError();
 }
@@ -281,6 +343,9 @@ template <typename T, bool WNK>
 hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
+    if constexpr (WNK)
+        if (p.a) return p.N <= 64 ? launch<T, true, 128, 64, 4, true>(o, p, s) : launch<T, true, 128, 128, 4, true>(o, p, s);
+    if (p.a) return launch_row_wide(dtype, o, p, s);
     const int64_t groups = p.w_group ? o.G : 1;
     const bool few = o.n < 64 * groups;  // rows per group
     if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);
@@ -295,6 +360,12 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 size_t narrow_bytes(int dtype, int64_t n_rows, int N)
 {
     return (size_t)n_rows * narrow_width(N) * 4;  // one fp32 or two bf16
+}
+
+// Adapters of 64 rows on the mean, one column tile of [N][K] weights.
+bool adapter_product_takes(int dtype, const RowOrder &o, const RowProduct &p)
+{
+    return p.a && p.w_nk && p.N <= 128 && p.r <= 32 && p.K >= kU && o.n >= 64 * (int64_t)o.G;
 }
 
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)

@@ -462,6 +462,39 @@ __device__ __forceinline__ void store_zeros(const RowProduct &p, const int *row,
 __host__ __device__ constexpr int narrow_width(int N) { return (N + kU - 1) / kU * kU; }
 template <typename T> constexpr int kNarrow = sizeof(T) == 2 ? 2 : 1;
 
+// Values 4 half .. 4 half + 3 of k-group g of a narrow result's row, as operands in a tile of R rows at
+// place r; second: the k-group where bf16's second part begins. k-groups that the result does not reach
+// come as zeros.
+template <typename T, int R>
+__device__ __forceinline__ void put_narrow(uint4_t *tile, int g, int r, int half, int second, float4_t x, bool &lose)
+{
+    auto at = [&](int group) { return reinterpret_cast<uint2_t *>(tile + group * (R + 1) + r) + half; };
+    if constexpr (sizeof(T) == 2) {
+        bf4_t hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            hi[e] = (bf16_t)x[e];
+            lo[e] = (bf16_t)(__builtin_isfinite((float)hi[e]) ? x[e] - (float)hi[e] : 0.f);
+        }
+        // k-groups 0 .. 7: the first parts, the second ones behind them, zeros
+        const uint2_t h = __builtin_bit_cast(uint2_t, hi), l = __builtin_bit_cast(uint2_t, lo), zero = {0, 0};
+        *at(g < second ? g : 2 * second + 2 * (g - second)) = g < second ? h : zero;
+        *at(g < second ? second + g : 2 * second + 2 * (g - second) + 1) = g < second ? l : zero;
+    } else {
+        float m = 0.f;
+        max_abs(m, x[0], x[1]);
+        max_abs(m, x[2], x[3]);
+        lose |= parts_lose(m);
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+            const bf4_t b = {(bf16_t)x[0], (bf16_t)x[1], (bf16_t)x[2], (bf16_t)x[3]};
+            *at(c * kGroups<T> + g) = __builtin_bit_cast(uint2_t, b);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] -= (float)b[e];
+        }
+    }
+}
+
 template <typename T> __device__ __forceinline__ float narrow_at(const void *h, int64_t pos, int W, int k)
 {
     const T *const p = static_cast<const T *>(h) + pos * (kNarrow<T> * W) + k;

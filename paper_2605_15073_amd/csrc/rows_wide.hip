@@ -384,12 +384,7 @@ bool row_wide_takes(int dtype, const RowProduct &p)
 // Tiles of one adapter each: where adapters have 64 rows on the mean, or all tiles run at once anyway.
 bool adapter_wide_takes(int dtype, const RowOrder &o, const RowProduct &p)
 {
-    return (o.n >= 64 * (int64_t)o.G || o.n / kRows + o.G < kTilesAtOnce) && row_wide_takes(dtype, p);
-}
-
-hipError_t launch_adapter_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)
-{
-    return launch_row_wide(dtype, o, p, s);
+    return p.a && !p.h_out && (o.n >= 64 * (int64_t)o.G || o.n / kRows + o.G < kTilesAtOnce) && row_wide_takes(dtype, p);
 }
 
 hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)

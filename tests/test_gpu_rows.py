@@ -361,6 +361,66 @@ def test_adapter(cg, dtype, n, G, n_in, n_out, r, kind):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,G,n_in,n_out,r", [
+    (1500, 3, 64, 200, 16), (1500, 3, 128, 72, 8), (900, 9, 40, 131, 4), (1300, 2, 121, 90, 32),
+    (700, 1, 16, 96, 1), (2100, 4, 64, 129, 24), (3000, 300, 64, 200, 8), (3000, 300, 33, 131, 20)])
+@pytest.mark.parametrize("kind", ["even", "holes", "one", "none"])
+def test_adapter_forms(cg, dtype, n, G, n_in, n_out, r, kind):
+    """Adapters with tiles of their own, whose narrow products are formed inside the shared one, and
+    tiles that many adapters share."""
+    rng = np.random.default_rng([n, G, n_in, n_out, r, 7])
+    x, w, a, b, dy, scale = _adapters(rng, n, G, n_in, n_out, r, dtype)
+    ids = draw_ids(rng, n, G, kind)
+    offsets, order = cg.group_rows(dev(ids), G)
+    X, W, A, B, DY = (dev(t, dtype) for t in (x, w, a, b, dy))
+    S = dev(scale)
+    check(cg.adapter_linear(X, W, A, B, offsets, order, scale=S),
+          ref.adapter(x, w, a, b, scale, ids, dtype), "y")
+    want = ref.adapter_grad(x, w, a, b, dy, scale, ids, dtype)
+    grads = cg.adapter_linear_grad(X, W, A, B, DY, offsets, order, scale=S)
+    for got, exp, what in zip(grads, want, ("dx", "da", "db")):
+        check(got, exp, what)
+    alone = [cg.adapter_linear_grad(X, W, A, B, DY, offsets, order, scale=S,
+                                    **{k: False for k in ("dx", "da", "db") if k != keep})
+             for keep in ("dx", "da", "db")]
+    check(alone[0][0], want[0], "dx alone")
+    check(alone[1][1], want[1], "da alone")
+    check(alone[2][2], want[2], "db alone")
+
+
+@pytest.mark.parametrize("where", ["x", "w", "a", "b", "dy"])
+@pytest.mark.parametrize("value", [1e-38, float("inf")])
+@pytest.mark.parametrize("n,G,n_in,n_out,r", [(400, 2, 64, 130, 8), (400, 2, 100, 72, 16),
+                                              (600, 40, 64, 72, 8)])
+def test_adapter_fp32_extremes(cg, where, value, n, G, n_in, n_out, r):
+    """Values that bf16 parts cannot hold: the results of fp32 sums, infinities where those have them."""
+    rng = np.random.default_rng([n, n_in])
+    t = dict(zip(("x", "w", "a", "b", "dy"), _adapters(rng, n, G, n_in, n_out, r, "f32")[:5]))
+    ids = draw_ids(rng, n, G, "even")
+    if value < 1:
+        t[where] = rounded(t[where] * value, "f32")
+    else:
+        flat = t[where].reshape(-1)
+        flat[5] = value                      # the first row of x or dy, of w, of the first adapter
+    one = np.ones(G)
+    offsets, order = cg.group_rows(dev(ids), G)
+    X, W, A, B, DY = (dev(t[k]) for k in ("x", "w", "a", "b", "dy"))
+    with np.errstate(all="ignore"):
+        want = [ref.adapter(t["x"], t["w"], t["a"], t["b"], one, ids, "f32"),
+                *ref.adapter_grad(t["x"], t["w"], t["a"], t["b"], t["dy"], one, ids, "f32")]
+    got = [cg.adapter_linear(X, W, A, B, offsets, order),
+           *cg.adapter_linear_grad(X, W, A, B, DY, offsets, order)]
+    for g, (v, bound), name in zip(got, want, ("y", "dx", "da", "db")):
+        g = host(g)
+        fine = np.isfinite(v) & np.isfinite(bound)
+        # a product between that underflows loses its own smallest step, 2^-149, times what follows
+        slack = 2.0 ** -149 * 4096 * 16
+        assert np.isfinite(g[fine]).all(), name
+        assert np.all(np.abs(g - v)[fine] <= bound[fine] + slack), name
+        assert not np.isfinite(g[~fine]).any(), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [0, 3, 8])
 def test_adapter_strided_bare_rows_and_no_scale(cg, dtype, pad):
     """Rows of no adapter get the shared projection alone; their NaN reaches no adapter's gradient."""
