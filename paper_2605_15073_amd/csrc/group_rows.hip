@@ -1,12 +1,14 @@
 // Row order by group (cgtp_group_rows): a stable counting sort of the group ids.
 //
 // Chunks of consecutive rows count their ids, a scan over the chunks turns the counts into the
-// position of each chunk's first row of each group, and the chunks then place their rows. Within
-// a workgroup every wave owns consecutive rows; a row's rank among the 64 that the wave handles
-// together comes from ballots over the bits of the id, so no atomic decides an order. Rows whose
-// id is outside [0, G) form a group G of their own, placed last.
+// position of each chunk's first row of each group, and the chunks then place their rows. A workgroup
+// takes its chunk in rounds of kRound rows, whose ids it holds in registers, eight to a thread, so that
+// counting and placing wait for memory once; every wave owns consecutive rows of a round. A row's rank among
+// the 64 that a wave handles together comes from ballots over the bits of the id: no atomic decides an
+// order. Rows whose id is outside [0, G) form a group G of their own, placed last.
 //
-// Up to kSmall rows one workgroup does all of it in one launch.
+// Up to kRound rows one workgroup does all of it in one launch. Bound by latency: the chains of three
+// launches, and in each of memory, LDS and barriers.
 #include "internal.h"
 #include "rows.h"
 
@@ -16,133 +18,186 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
-constexpr int kSmall = 4096;   // rows of the one-launch form
-constexpr int kChunks = 64;    // chunks at most: a wave scans one lane per chunk
-constexpr int kMinChunk = 2048;
+constexpr int kPer = 8;                       // ids of a thread
+constexpr int kRound = kThreads * kPer;       // rows of a round
+constexpr int kChunks = 256;                  // chunks at most
+constexpr int kScanKeys = 64, kScanSlices = 4;
 
 struct Shape {
-    int chunks, rows;  // rows per chunk, a multiple of 64 * kWaves
+    int chunks, rounds;  // rounds of a chunk
 };
 
 Shape shape(int64_t n)
 {
-    int64_t rows = (n + kChunks - 1) / kChunks;
-    if (rows < kMinChunk) rows = kMinChunk;
-    rows = (rows + kThreads - 1) / kThreads * kThreads;
-    return {(int)((n + rows - 1) / rows), (int)rows};
+    const int64_t all = (n + kRound - 1) / kRound, rounds = (all + kChunks - 1) / kChunks;
+    return {(int)((all + rounds - 1) / rounds), (int)rounds};
 }
 
 __device__ __forceinline__ int key_of(int id, int G) { return (unsigned)id < (unsigned)G ? id : G; }
 
-// counts[key][chunk]
-__global__ __launch_bounds__(kThreads) void k_group_count(int64_t n, int G, int rows, int chunks,
+// The keys of this thread's rows of the round that starts at r0: rows r0 + wave kPer 64 + 64 i + lane; -1 past n.
+__device__ __forceinline__ void load_keys(int (&key)[kPer], int64_t r0, int64_t n, int G, const int32_t *ids)
+{
+    const int64_t r = r0 + (threadIdx.x >> 6) * (kPer * 64) + (threadIdx.x & 63);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i] = ids[r + 64 * i < n ? r + 64 * i : 0];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i] = r + 64 * i < n ? key_of(key[i], G) : -1;
+}
+
+// counts[chunk][key]
+__global__ __launch_bounds__(kThreads) void k_group_count(int64_t n, int G, int rounds,
                                                           const int32_t *__restrict__ ids,
                                                           int32_t *__restrict__ counts)
 {
     extern __shared__ int sh[];
+    int key[kPer];
+    const int64_t r0 = (int64_t)blockIdx.x * rounds * kRound;
+    load_keys(key, r0, n, G, ids);
     for (int g = threadIdx.x; g <= G; g += kThreads) sh[g] = 0;
     __syncthreads();
-    const int64_t r0 = (int64_t)blockIdx.x * rows, r1 = r0 + rows < n ? r0 + rows : n;
-    for (int64_t r = r0 + threadIdx.x; r < r1; r += kThreads) atomicAdd(&sh[key_of(ids[r], G)], 1);
-    __syncthreads();
-    for (int g = threadIdx.x; g <= G; g += kThreads)
-        counts[(int64_t)g * chunks + blockIdx.x] = sh[g];
-}
-
-// In place: the rows of the key in the chunks before; totals[key].
-__global__ __launch_bounds__(256) void k_group_scan(int G, int chunks, int32_t *__restrict__ counts,
-                                                    int32_t *__restrict__ totals)
-{
-    const int g = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (g > G) return;
-    const int c = lane < chunks ? counts[(int64_t)g * chunks + lane] : 0;
-    int sum = c;
+    for (int round = 0;;) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int up = __shfl_up(sum, d);
-        if (lane >= d) sum += up;
+        for (int i = 0; i < kPer; ++i)
+            if (key[i] >= 0) atomicAdd(&sh[key[i]], 1);
+        if (++round == rounds) break;
+        load_keys(key, r0 + (int64_t)round * kRound, n, G, ids);
     }
-    if (lane < chunks) counts[(int64_t)g * chunks + lane] = sum - c;
-    if (lane == 63) totals[g] = sum;
+    __syncthreads();
+    for (int g = threadIdx.x; g <= G; g += kThreads) counts[(int64_t)blockIdx.x * (G + 1) + g] = sh[g];
 }
 
-// LDS: base[G + 1] (int), the position of the chunk's first row of each key, then
-// run[kWaves][G + 1], the rows of each key that the waves before, then this one, have placed.
+// In place: the rows of the key in the chunks before; totals[key]. A workgroup takes 64 keys, four threads a
+// key with a quarter of the chunks each.
+__global__ __launch_bounds__(kScanKeys *kScanSlices) void k_group_scan(int G, int chunks,
+                                                                       int32_t *__restrict__ counts,
+                                                                       int32_t *__restrict__ totals)
+{
+    __shared__ int s_sum[kScanSlices][kScanKeys];
+    const int k = threadIdx.x % kScanKeys, slice = threadIdx.x / kScanKeys;
+    const int g = blockIdx.x * kScanKeys + k;
+    const int per = (chunks + kScanSlices - 1) / kScanSlices;
+    const int c0 = slice * per, c1 = c0 + per < chunks ? c0 + per : chunks;
+    int sum = 0;
+    if (g <= G) {
+#pragma unroll 8
+        for (int c = c0; c < c1; ++c) sum += counts[(int64_t)c * (G + 1) + g];
+    }
+    s_sum[slice][k] = sum;
+    __syncthreads();
+    if (g > G) return;
+    int before = 0;
+    for (int s = 0; s < slice; ++s) before += s_sum[s][k];
+    if (slice == kScanSlices - 1) totals[g] = before + sum;
+    for (int c = c0; c < c1; c += 8) {
+        int v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = counts[(int64_t)(c + i < c1 ? c + i : c0) * (G + 1) + g];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < c1) {
+                counts[(int64_t)(c + i) * (G + 1) + g] = before;
+                before += v[i];
+            }
+    }
+}
+
+// LDS: base[G + 1], the position of the round's first row of each key, then run[kWaves][G + 1], the rows of
+// each key that the waves before, then this one, have placed in the round.
 __global__ __launch_bounds__(kThreads) void k_group_place(
-    int64_t n, int G, int rows, int chunks, const int32_t *__restrict__ ids,
-    const int32_t *__restrict__ counts, const int32_t *__restrict__ totals,
-    int32_t *__restrict__ offsets, int32_t *__restrict__ order)
+    int64_t n, int G, int rounds, const int32_t *__restrict__ ids, const int32_t *__restrict__ counts,
+    const int32_t *__restrict__ totals, int32_t *__restrict__ offsets, int32_t *__restrict__ order)
 {
     extern __shared__ int sh[];
     __shared__ int wave_sum[kWaves];
     int *const base = sh;
-    int *const run = sh + G + 1;  // [kWaves][G + 1]
+    int *const run = sh + G + 1;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t r0 = (int64_t)blockIdx.x * rows, r1 = r0 + rows < n ? r0 + rows : n;
-    const int per = rows / kWaves;  // rows of a wave, consecutive, a multiple of 64
-    const int64_t w0 = r0 + (int64_t)wave * per;
-    const int64_t w1 = w0 + per < r1 ? w0 + per : r1;
-    for (int i = tid; i < kWaves * (G + 1); i += kThreads) run[i] = 0;
-    __syncthreads();
+    const int64_t r0 = (int64_t)blockIdx.x * rounds * kRound;
     int *const mine = run + wave * (G + 1);
-    for (int64_t r = w0 + lane; r < w1; r += 64) atomicAdd(&mine[key_of(ids[r], G)], 1);
-    __syncthreads();
-    // totals of the keys (of this workgroup where there is one chunk), then their exclusive scan
-    for (int g = tid; g <= G; g += kThreads) {
-        int t = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            const int c = run[w * (G + 1) + g];
-            run[w * (G + 1) + g] = t;
-            t += c;
-        }
-        base[g] = totals ? totals[g] : t;
-    }
-    __syncthreads();
-    const int span = (G + 1 + kThreads - 1) / kThreads;
-    int first = tid * span, last = first + span;
-    if (first > G + 1) first = G + 1;
-    if (last > G + 1) last = G + 1;
-    int sum = 0;
-    for (int g = first; g < last; ++g) sum += base[g];
-    int scan = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int up = __shfl_up(scan, d);
-        if (lane >= d) scan += up;
-    }
-    if (lane == 63) wave_sum[wave] = scan;
-    __syncthreads();
-    int at = scan - sum;
-    for (int w = 0; w < wave; ++w) at += wave_sum[w];
-    for (int g = first; g < last; ++g) {
-        const int t = base[g];
-        base[g] = at + (counts ? counts[(int64_t)g * chunks + blockIdx.x] : 0);
-        if (blockIdx.x == 0) offsets[g] = at;
-        at += t;
-    }
-    __syncthreads();
-    if (n == 0) return;
+    int key[kPer];
+    if (n > 0) load_keys(key, r0, n, G, ids);
     int bits = 1;
     while ((G >> bits) != 0) ++bits;
-    for (int64_t b = w0; b < w1; b += 64) {
-        const int64_t r = b + lane;
-        const bool in = r < w1;
-        const int key = in ? key_of(ids[r], G) : 0;
-        unsigned long long same = __ballot(in);
-        for (int k = 0; k < bits; ++k) {
-            const unsigned long long set = __ballot((key >> k) & 1);
-            same &= ((key >> k) & 1) ? set : ~set;
+    for (int round = 0; round < rounds; ++round) {
+        for (int i = tid; i < kWaves * (G + 1); i += kThreads) run[i] = 0;
+        __syncthreads();
+        if (n > 0) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (key[i] >= 0) atomicAdd(&mine[key[i]], 1);
         }
-        if (in) {
+        __syncthreads();
+        // each wave's first place among the round's rows of a key; in the first round the keys' first
+        // positions: the exclusive scan of their totals (the round's own where there is one chunk)
+        for (int g = tid; g <= G; g += kThreads) {
+            int t = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const int c = run[w * (G + 1) + g];
+                run[w * (G + 1) + g] = t;
+                t += c;
+            }
+            if (round == 0) base[g] = totals ? totals[g] : t;
+        }
+        __syncthreads();
+        if (round == 0) {
+            const int span = (G + 1 + kThreads - 1) / kThreads;
+            int first = tid * span, last = first + span;
+            if (first > G + 1) first = G + 1;
+            if (last > G + 1) last = G + 1;
+            int sum = 0;
+            for (int g = first; g < last; ++g) sum += base[g];
+            int scan = sum;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int up = __shfl_up(scan, d);
+                if (lane >= d) scan += up;
+            }
+            if (lane == 63) wave_sum[wave] = scan;
+            __syncthreads();
+            int at = scan - sum;
+            for (int w = 0; w < wave; ++w) at += wave_sum[w];
+            for (int g = first; g < last; ++g) {
+                const int t = base[g];
+                base[g] = at;
+                at += t;
+            }
+            __syncthreads();
+            if (blockIdx.x == 0)
+                for (int g = tid; g <= G; g += kThreads) offsets[g] = base[g];
+            if (counts)
+                for (int g = tid; g <= G; g += kThreads) base[g] += counts[(int64_t)blockIdx.x * (G + 1) + g];
+            __syncthreads();
+        }
+        if (n == 0) return;
+        const int64_t r = r0 + (int64_t)round * kRound + wave * (kPer * 64) + lane;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const bool in = key[i] >= 0;
+            const int k = in ? key[i] : 0;
+            unsigned long long same = __ballot(in);
+            for (int b = 0; b < bits; ++b) {
+                const unsigned long long set = __ballot((k >> b) & 1);
+                same &= ((k >> b) & 1) ? set : ~set;
+            }
             const unsigned long long below = same & ((1ull << lane) - 1);
-            const int rank = __popcll(below);
-            const int before = mine[key];
-            order[base[key] + before + rank] = (int)r;
+            int before = 0;
+            if (in) {
+                before = mine[k];
+                order[base[k] + before + __popcll(below)] = (int)(r + 64 * i);
+            }
             // the first of the rows that share a key moves its count on, once all have read it
             __builtin_amdgcn_wave_barrier();
-            if (below == 0) mine[key] = before + __popcll(same);
+            if (in && below == 0) mine[k] = before + __popcll(same);
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_wave_barrier();
+        if (round + 1 == rounds) break;
+        load_keys(key, r0 + (int64_t)(round + 1) * kRound, n, G, ids);
+        __syncthreads();
+        // the last wave's counts are the round's
+        for (int g = tid; g <= G; g += kThreads) base[g] += run[(kWaves - 1) * (G + 1) + g];
+        __syncthreads();
     }
 }
 
@@ -150,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void k_group_place(
 
 size_t group_rows_bytes(int64_t n, int G)
 {
-    if (n <= kSmall) return 0;
+    if (n <= kRound) return 0;
     return 4 * ((size_t)(G + 1) * shape(n).chunks + (size_t)(G + 1));
 }
 
@@ -159,24 +214,24 @@ hipError_t launch_group_rows(int64_t n, int G, const int32_t *ids, int32_t *offs
 {
     const size_t place_lds = 4 * (size_t)(kWaves + 1) * (G + 1);
     static_assert(4 * (kWaves + 1) * (CGTP_MAX_GROUPS + 1) + 1024 <= 160 * 1024, "LDS");
-    if (n <= kSmall) {
-        hipLaunchKernelGGL(k_group_place, dim3(1), dim3(kThreads), place_lds, s, n, G, kSmall, 1,
-                           ids, nullptr, nullptr, offsets, order);
+    if (n <= kRound) {
+        hipLaunchKernelGGL(k_group_place, dim3(1), dim3(kThreads), place_lds, s, n, G, 1, ids, nullptr,
+                           nullptr, offsets, order);
         return hipGetLastError();
     }
     const Shape sh = shape(n);
     int32_t *const counts = static_cast<int32_t *>(ws);
     int32_t *const totals = counts + (size_t)(G + 1) * sh.chunks;
     hipLaunchKernelGGL(k_group_count, dim3(sh.chunks), dim3(kThreads), 4 * (size_t)(G + 1), s, n, G,
-                       sh.rows, sh.chunks, ids, counts);
+                       sh.rounds, ids, counts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_group_scan, dim3((G + 1 + 3) / 4), dim3(256), 0, s, G, sh.chunks, counts,
-                       totals);
+    hipLaunchKernelGGL(k_group_scan, dim3((G + kScanKeys) / kScanKeys), dim3(kScanKeys * kScanSlices), 0, s,
+                       G, sh.chunks, counts, totals);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_group_place, dim3(sh.chunks), dim3(kThreads), place_lds, s, n, G, sh.rows,
-                       sh.chunks, ids, counts, totals, offsets, order);
+    hipLaunchKernelGGL(k_group_place, dim3(sh.chunks), dim3(kThreads), place_lds, s, n, G, sh.rounds, ids,
+                       counts, totals, offsets, order);
     return hipGetLastError();
 }
 

@@ -84,6 +84,17 @@ def test_group_rows(cg, n, G, kind):
     assert np.array_equal(order.cpu().numpy(), rord)
 
 
+@pytest.mark.parametrize("n", [1048576, 1048577, 3000000])
+def test_group_rows_in_rounds(cg, n):
+    """More rows than 256 chunks of one round hold."""
+    for G in (3, 1000):
+        ids = draw_ids(np.random.default_rng(n), n, G, "holes")
+        offsets, order = cg.group_rows(dev(ids), G)
+        roff, rord = ref.order(ids, G)
+        assert np.array_equal(offsets.cpu().numpy(), roff)
+        assert np.array_equal(order.cpu().numpy(), rord)
+
+
 @pytest.mark.parametrize("n", [100, 30000])
 @pytest.mark.parametrize("kind", ["none", "one"])
 def test_group_rows_degenerate(cg, n, kind):
