@@ -26,11 +26,9 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = NARROW ? kNarrow<T> : 1, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
-    // steps of operands in flight: two, but one where rows are below a vector or a narrow operand's further
-    // registers leave fewer waves (bf16, 525,308 x 64 by rank 16, 90 us against 99)
-    constexpr int kAhead = WIDE && !NARROW ? 2 : 1;
     __shared__ uint4_t s_cols[P][kTile<T, BN>], s_rows[kTile<T, BM>];
-    __shared__ int s_id[4][BK];
+    __shared__ int64_t s_at[2][2][BK];  // where the rows of a and b of a step start
+    __shared__ unsigned s_rows_in[2][BK / 32];  // bit per row of a step: it exists
 
     // Block b runs on XCD b % 8: the tiles of a chunk, which share its rows, follow each other on one.
     const int B = NARROW ? q.r : q.B;
@@ -51,10 +49,10 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     const int al = tid % (BM / CW), ag = tid / (BM / CW) % KG;
     const int bl = tid % (BN / CW), bg = tid / (BN / CW) % KG;
     const bool has_a = !kIdleA || tid < BM / CW * KG, has_b = !kIdleB || tid < BN / CW * KG;
-    struct Loads {
+    struct {
         uint2_t a[8], b[P][8];
         unsigned arows, brows;  // bit u: row u of the k-group exists
-    } even, odd;
+    } l;
     bool lose = false;
     const int steps = (int)((t.p1 - t.p0 + BK - 1) / BK);
     // ids of the rows of step s, -1 past the chunk; loads without a condition, as the operands'
@@ -67,41 +65,45 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     auto put_ids = [&](int s) {
         const int64_t pos = t.p0 + (int64_t)s * BK + tid;
         const int row = o.order ? id : (int)pos;
-        if (tid < BK) s_id[s & 3][tid] = pos < t.p1 && (unsigned)row < (unsigned)o.n ? row : -1;
-    };
-    auto fetch = [&](Loads &l, int s) {
-        const int *const ids = s_id[s & 3];
-        l.arows = l.brows = 0;
-        const int ca = a0 + CW * al, cb = b0 + CW * bl;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int row = ids[ag * kU + u];
-            l.arows |= (row >= 0 ? 1u : 0u) << u;
-            const T *const p = static_cast<const T *>(q.a) + (row < 0 ? 0 : row) * q.a_stride;
-            if (WIDE) l.a[u] = *reinterpret_cast<const uint2_any *>(p + (ca + CW <= q.A ? ca : q.A - CW));
-            else l.a[u] = load_8<T, false>(p + ca, row < 0 ? 0 : q.A - ca);
+        const bool in = pos < t.p1 && (unsigned)row < (unsigned)o.n;
+        if (tid < BK) {
+            s_at[0][s & 1][tid] = in ? row * q.a_stride : 0;  // row 0 in place of none: zeroed when staged
+            s_at[1][s & 1][tid] = !in ? 0 : NARROW ? pos * (P * W) : row * q.b_stride;
+            const unsigned long long m = __ballot(in);
+            if (tid % 32 == 0) s_rows_in[s & 1][tid / 32] = (unsigned)(m >> (tid & 32));
         }
+    };
+    auto fetch = [&](int s) {
+        const int64_t *const at_a = s_at[0][s & 1] + ag * kU, *const at_b = s_at[1][s & 1] + bg * kU;
+        l.arows = s_rows_in[s & 1][ag / 4] >> 8 * (ag % 4) & 0xffu;
+        l.brows = s_rows_in[s & 1][bg / 4] >> 8 * (bg % 4) & 0xffu;
+        const int ca = a0 + CW * al, cb = b0 + CW * bl;
+        const T *const pa = static_cast<const T *>(q.a) + (WIDE && ca + CW > q.A ? q.A - CW : ca);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int row = ids[bg * kU + u];
-            l.brows |= (row >= 0 ? 1u : 0u) << u;
-            if (NARROW) {
-                const int64_t pos = row < 0 ? t.p0 : t.p0 + (int64_t)s * BK + bg * kU + u;
+            if (WIDE) l.a[u] = *reinterpret_cast<const uint2_any *>(pa + at_a[u]);
+            else l.a[u] = load_8<T, false>(pa + at_a[u], q.A - ca);
+        }
+        if (NARROW) {
+            if (!has_b) return;
+            const T *const pb = static_cast<const T *>(q.h) + (cb < W ? cb : W - CW);
 #pragma unroll
-                for (int e = 0; e < P; ++e)
-                    l.b[e][u] = *reinterpret_cast<const uint2_t *>(static_cast<const T *>(q.h) + (pos * P + e) * W +
-                                                                   (cb < W ? cb : W - CW));
-            } else {
-                const T *const p = static_cast<const T *>(q.b) + (row < 0 ? 0 : row) * q.b_stride;
-                if (WIDE) l.b[0][u] = *reinterpret_cast<const uint2_any *>(p + (cb + CW <= B ? cb : B - CW));
-                else l.b[0][u] = load_8<T, false>(p + cb, row < 0 ? 0 : B - cb);
-            }
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int e = 0; e < P; ++e) l.b[e][u] = *reinterpret_cast<const uint2_t *>(pb + at_b[u] + e * W);
+            return;
+        }
+        const T *const pb = static_cast<const T *>(q.b) + (WIDE && cb + CW > B ? B - CW : cb);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (WIDE) l.b[0][u] = *reinterpret_cast<const uint2_any *>(pb + at_b[u]);
+            else l.b[0][u] = load_8<T, false>(pb + at_b[u], B - cb);
         }
     };
     // what the loads of the last columns started early
     const int early_a = WIDE && a0 + CW * al < q.A && a0 + CW * al + CW > q.A ? a0 + CW * al + CW - q.A : 0;
     const int early_b = WIDE && !NARROW && b0 + CW * bl < B && b0 + CW * bl + CW > B ? b0 + CW * bl + CW - B : 0;
-    auto stage = [&](Loads &l) {
+    auto stage = [&]() {
         uint4_t u[CW][Q];
         if (has_a) {
             if (early_a > 0) {
@@ -142,28 +144,21 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[c][r][i] = 0.f;
     if (steps > 0) {
-        // operands kAhead steps ahead of the products, row ids one more
+        // operands a step ahead of the products, row ids two
         fetch_ids(0);
         put_ids(0);
         fetch_ids(1);
-        put_ids(1);
-        fetch_ids(2);
         __syncthreads();
-        fetch(even, 0);
-        if (kAhead == 2) fetch(odd, 1);
-        auto step = [&](Loads &l, int s) {
+        fetch(0);
+        for (int s = 0; s < steps; ++s) {
             __syncthreads();
-            stage(l);
-            put_ids(s + 2);
+            stage();
+            put_ids(s + 1);
             __syncthreads();
-            fetch_ids(s + 3);  // before the operands, whose loads then stay in flight when it is written
-            fetch(l, s + kAhead);
+            fetch_ids(s + 2);  // before the operands, whose loads then stay in flight when it is written
+            fetch(s + 1);
 #pragma unroll
             for (int e = 0; e < P; ++e) step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0);
-        };
-        for (int s = 0; s < steps; s += 2) {
-            step(even, s);
-            if (s + 1 < steps) step(kAhead == 2 ? odd : even, s + 1);
         }
     }
     const bool whole = t.end - t.start <= ((int64_t)1 << shift);
