@@ -54,6 +54,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         unsigned arows, brows;  // bit u: row u of the k-group exists
     } l;
     bool lose = false;
+    float sign = 1.f;  // of the step's a
     const int steps = (int)((t.p1 - t.p0 + BK - 1) / BK);
     // ids of the rows of step s, -1 past the chunk; loads without a condition, as the operands'
     const int32_t *const ids_at = o.order ? o.order : o.offsets;
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 #pragma unroll
                 for (int e = 0; e < 8; ++e) l.a[e] = l.arows >> e & 1 ? l.a[e] : uint2_t{0, 0};
             }
-            to_units(l.a, u, lose);
+            to_units(l.a, u, lose, sign);
 #pragma unroll
             for (int j = 0; j < CW; ++j) put<T, BM>(s_rows, KG, ag, place<T>(CW * al + j), u[j]);
         }
@@ -158,7 +159,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             fetch_ids(s + 2);  // before the operands, whose loads then stay in flight when it is written
             fetch(s + 1);
 #pragma unroll
-            for (int e = 0; e < P; ++e) step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0);
+            for (int e = 0; e < P; ++e) step_products<T, BN, BM, TC, TR>(acc, s_cols[e], s_rows, c0w, r0, sign);
+            sign = -sign;
         }
     }
     const bool whole = t.end - t.start <= ((int64_t)1 << shift);
@@ -329,7 +331,7 @@ template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float
     if (sh.bm == 64) e = launch<T, 64, 64, 2>(o, q, sh, big, slots, s);
     else if (sh.bn == 32) e = launch<T, 128, 32, 4>(o, q, sh, big, slots, s);
     else if (sh.bn == 64) e = launch<T, 128, 64, 4>(o, q, sh, big, slots, s);
-    else e = launch<T, 128, 128, 2>(o, q, sh, big, slots, s);
+    else e = launch<T, 128, 128, kWaveRows<T>>(o, q, sh, big, slots, s);
     if (e != hipSuccess || o.n >> sh.shift == 0) return e;
     const int64_t cells = (int64_t)q.A * B, by = (cells + kJoinCells - 1) / kJoinCells;
     const int64_t spans = o.n >> sh.shift, bx = o.G < spans ? o.G : spans;

@@ -4,10 +4,10 @@
 // A workgroup owns up to BM rows of one group (of any groups where W is shared) and runs over tiles
 // of BN columns of its share of the output, so that its input rows come from HBM once and from the
 // L2 for every further column tile; the weights of a group stay in the L2s. The loads of the next
-// step or two (rows and weights, kStep deep) are in flight while a step is multiplied. None of them is under
-// a condition, or the wait for one step would be for all: a vector that would pass the end of its row starts
-// early, one without values points to some that exist, and both are put right when they are staged. Only
-// widths below a vector (WIDE false) load value by value.
+// step (rows and weights, kStep deep) are in flight while a step is multiplied. None of them is under a
+// condition: a vector that would pass the end of its row starts early, one without values points to some
+// that exist, and both are put right when they are staged. Only widths below a vector (WIDE false) load
+// value by value.
 //
 // Adapters: after the steps over the shared W, a tile's sums go on over the adapters of its rows, one
 // segment of rows at a time, with the narrow product's result as input rows (zero outside the
@@ -27,7 +27,7 @@ namespace {
 using namespace rows;
 
 template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED>
-__global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct p, int splits)
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_product(RowOrder o, RowProduct p, int splits)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
@@ -35,9 +35,6 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
     static_assert(!FUSED || (WNK && WR == 4 && WIDE), "fused: a wave has whole rows, weights are [N][K]");
     constexpr int kShift = BM == 128 ? 7 : BM == 64 ? 6 : 5;
     static_assert(BM == 1 << kShift && TR >= 1 && TC >= 1, "tile");
-    // steps of loads in flight: two of fp32, whose parts take longer to form and multiply, one where that
-    // costs waves (bf16, 261,766 x 1344 -> 128, 194 us against 218; fp32, 131,327 x 896 -> 128, 323 and 275)
-    constexpr int kAhead = WIDE && Q > 1 ? 2 : 1;
     constexpr int kLanes = kThreads / KG;              // rows staged at once
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
     constexpr int NC = (BX + kLanes - 1) / kLanes;
@@ -104,18 +101,19 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
             }
         }
     };
-    struct Loads {
+    struct {
         Raw8<T> x[NR], wn[WNK ? NC : 1];
         uint2_t wt[WNK ? 1 : 8];
         int xk, wk;  // values that exist of this thread's k-group of rows and weights
         int xe, we;  // what their loads started early
         unsigned rows;  // bit i: x[i] is of a row that takes part
-    } even, odd;
+    } l;
     bool lose = false;
-    auto fetch = [&](Loads &l) {
-        if (!WIDE && next.ct >= ct1) return;
+    float sign = 1.f;  // of the step's rows
+    auto fetch = [&]() {
+        if (next.ct >= ct1) return;
         const bool ext = next.seg >= 0;
-        const int seg = ext ? next.seg : 0, c0 = (next.ct < ct1 ? next.ct : ct1 - 1) * BN, k = next.k;
+        const int seg = ext ? next.seg : 0, c0 = next.ct * BN, k = next.k;
         const int K = ext ? P * W : p.K;   // of the rows
         const int ld = ext ? p.r : p.K;    // of the weights
         const T *wb = w;
@@ -163,15 +161,15 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
                 else l.wt[u] = load_8<T, false>(q + c, u < l.wk ? p.N - c : 0);
             }
         }
-        if (next.ct < ct1) advance(next);
+        advance(next);
     };
-    auto stage = [&](Loads &l) {
+    auto stage = [&]() {
         uint4_t u[Q];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             if (BM < kLanes && rr >= BM) break;
             if (l.xk < kU || !(l.rows >> i & 1)) settle(l.x[i], WIDE ? l.xe : 0, l.rows >> i & 1 ? l.xk : 0);
-            to_units(l.x[i], u, lose);
+            to_units(l.x[i], u, lose, sign);
             put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
         }
         if constexpr (WNK) {
@@ -272,19 +270,15 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
             put<T, BX>(s_cols, KG, g, c, u);
         }
         __syncthreads();
-        float16_t sums[TC][TR];
-#pragma unroll
-        for (int c = 0; c < TC; ++c) sums[c][0] = acc[c][0];
-        step_products<T, BX, BM, TC, TR>(sums, s_cols, s_rows, c0w, r0);
-#pragma unroll
-        for (int c = 0; c < TC; ++c) acc[c][0] = sums[c][0];
+        step_products<T, BX, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0, 1.f);
     };
-    auto step = [&](Loads &l) {
+    auto step = [&]() {
         __syncthreads();
-        stage(l);
+        stage();
         __syncthreads();
-        fetch(l);
-        step_products<T, BX, BM, TX, TR>(acc, s_cols, s_rows, c0w, r0);
+        fetch();
+        step_products<T, BX, BM, TX, TR>(acc, s_cols, s_rows, c0w, r0, sign);
+        sign = -sign;
         const int ct = now.ct;
         advance(now);
         if (now.ct != ct) {
@@ -294,12 +288,8 @@ __global__ __launch_bounds__(kThreads) void k_row_product(RowOrder o, RowProduct
         }
     };
     clear();
-    fetch(even);
-    if (kAhead == 2) fetch(odd);
-    while (now.ct < ct1) {
-        step(even);
-        if (now.ct < ct1) step(kAhead == 2 ? odd : even);
-    }
+    fetch();
+    while (now.ct < ct1) step();
     if constexpr (Q > 1) {
         if (__syncthreads_or(lose)) {
             float *const h = FUSED ? reinterpret_cast<float *>(s_cols) : nullptr;
@@ -352,7 +342,7 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1>(o, p, s);
     if (few || p.N <= 64) return launch<T, WNK, 64, 64, 2>(o, p, s);
-    return launch<T, WNK, 128, 128, 2>(o, p, s);
+    return launch<T, WNK, 128, 128, kWaveRows<T>>(o, p, s);
 }
 
 }  // namespace

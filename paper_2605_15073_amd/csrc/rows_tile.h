@@ -299,18 +299,21 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4_t (&part)[3], 
     lose |= parts_lose(m);
 }
 
-// The units of a lane's eight k.
-__device__ __forceinline__ void to_units(const Raw8<bf16_t> &raw, uint4_t (&u)[1], bool &) { u[0] = raw.v[0]; }
-__device__ __forceinline__ void to_units(const Raw8<float> &raw, uint4_t (&u)[3], bool &lose)
+// The units of a lane's eight k; of fp32 times sign, 1 or -1.
+__device__ __forceinline__ void to_units(const Raw8<bf16_t> &raw, uint4_t (&u)[1], bool &, float = 1.f)
+{
+    u[0] = raw.v[0];
+}
+__device__ __forceinline__ void to_units(const Raw8<float> &raw, uint4_t (&u)[3], bool &lose, float sign = 1.f)
 {
     float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, (unsigned)raw.v[e / 4][e % 4]);
+    for (int e = 0; e < 8; ++e) x[e] = sign * __builtin_bit_cast(float, (unsigned)raw.v[e / 4][e % 4]);
     split8(x, u, lose);
 }
 
 // The units of kWide lanes from 8 loads of 8 bytes.
-__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[4][1], bool &)
+__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[4][1], bool &, float = 1.f)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -320,13 +323,13 @@ __device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[4]
                                                (j & 1) ? 0x07060302u : 0x05040100u);
 }
 
-__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[2][3], bool &lose)
+__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[2][3], bool &lose, float sign = 1.f)
 {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, (unsigned)in[e][j]);
+        for (int e = 0; e < 8; ++e) x[e] = sign * __builtin_bit_cast(float, (unsigned)in[e][j]);
         split8(x, u[j], lose);
     }
 }
@@ -375,26 +378,53 @@ __device__ __forceinline__ void mma(float16_t &acc, const uint4_t (&a)[3], const
 // rows. acc[c][r][i]: column place 8 (i / 4) + 4 (lane / 32) + i % 4 of block c, row place lane % 32 of
 // block r. All k-groups always, zeros past the end: a branch around a matrix instruction costs a copy of
 // its sums.
-template <typename T, int BN, int BM, int TC, int TR>
-__device__ __forceinline__ void step_products(float16_t (&acc)[TC][TR], const uint4_t *cols,
-                                              const uint4_t *rws, int c0, int r0)
+//
+// The matrix instruction rounds its sums down, towards minus infinity (measured: results of 896 terms low by
+// 4e-8 of their spread on the mean, which a later sum over many rows picks up). fp32 products therefore sum
+// a step from zero and add it in fp32, and every other step has its rows negated and is subtracted (sign).
+template <typename T, int BN, int BM, int TC, int TR, int TX>
+__device__ __forceinline__ void step_products(float16_t (&acc)[TX][TR], const uint4_t *cols,
+                                              const uint4_t *rws, int c0, int r0, float sign)
 {
-    constexpr int Q = kSplit<T>, KG = kGroups<T>;
+    constexpr int Q = kSplit<T>, KG = kGroups<T>, S = KG / 2;
     const int lane = threadIdx.x & 63, half = lane >> 5, n = lane & 31;
+    if constexpr (Q == 1) {
 #pragma unroll
-    for (int s = 0; s < KG / 2; ++s) {
-        uint4_t a[TC][Q], b[TR][Q];
+        for (int s = 0; s < S; ++s) {
+            uint4_t a[TC][1], b[TR][1];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
+            for (int c = 0; c < TC; ++c) a[c][0] = cols[(2 * s + half) * (BN + 1) + c0 + 32 * c + n];
 #pragma unroll
-            for (int c = 0; c < TC; ++c) a[c][q] = cols[(q * KG + 2 * s + half) * (BN + 1) + c0 + 32 * c + n];
+            for (int r = 0; r < TR; ++r) b[r][0] = rws[(2 * s + half) * (BM + 1) + r0 + 32 * r + n];
 #pragma unroll
-            for (int r = 0; r < TR; ++r) b[r][q] = rws[(q * KG + 2 * s + half) * (BM + 1) + r0 + 32 * r + n];
+            for (int c = 0; c < TC; ++c)
+#pragma unroll
+                for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r]);
         }
+    } else {
 #pragma unroll
-        for (int c = 0; c < TC; ++c)
+        for (int r = 0; r < TR; ++r) {
+            uint4_t b[S][Q];
 #pragma unroll
-            for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r]);
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) b[s][q] = rws[(q * KG + 2 * s + half) * (BM + 1) + r0 + 32 * r + n];
+#pragma unroll
+            for (int c = 0; c < TC; ++c) {
+                float16_t sum;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    uint4_t a[Q];
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) a[q] = cols[(q * KG + 2 * s + half) * (BN + 1) + c0 + 32 * c + n];
+                    mma(sum, a, b[s]);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c][r][i] = fmaf(sign, sum[i], acc[c][r][i]);
+            }
+        }
     }
 }
 
@@ -500,6 +530,10 @@ template <typename T> __device__ __forceinline__ float narrow_at(const void *h, 
     const T *const p = static_cast<const T *>(h) + pos * (kNarrow<T> * W) + k;
     return sizeof(T) == 2 ? (float)p[0] + (float)p[W] : (float)p[0];
 }
+
+// Waves along the rows of a 128 x 128 tile: fp32 operands, three parts each, are read once a wave where it
+// has rows of its own.
+template <typename T> constexpr int kWaveRows = sizeof(T) == 2 ? 2 : 4;
 
 // The sums of a workgroup that met values outside the range of parts, in plain fp32: columns [c0, c1) of its
 // rows, one result a thread at a time. h: the narrow product's rows in LDS, 32 apart, in place of p.h.

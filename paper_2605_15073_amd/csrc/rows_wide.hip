@@ -63,6 +63,9 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
 {
     constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, KG = 2 * (NP + XP), LD = kCols + 1, CW = kWide<T>;
     constexpr bool EXT = XP > 0;
+    // fp32: the matrix instruction rounds down, so the second half of the k is summed negated (step_products)
+    constexpr int kPlus = Q > 1 && NP > 1 ? NP / 2 : NP;
+    constexpr float kSign = kPlus < NP ? -1.f : 1.f;  // of the adapters' products and of the result
     static_assert(NP <= kPairs<T> && !(EXT && WNK), "adapters: [K][N] weights");
     typedef typename Out4<T>::t O;
     typedef typename Out4<T>::any O_any;
@@ -122,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
 #pragma unroll
     for (int s = 0; s < NP; ++s) {
         const int k = (2 * s + half) * U;
-        to_units(load_row8<T, false>(in + k, p.K - k), x[s], lose);
+        to_units(load_row8<T, false>(in + k, p.K - k), x[s], lose, s < kPlus ? 1.f : -1.f);
     }
     O *const turn = s_turn + wave * (32 * kTurn<T> / 4);
     if constexpr (FUSED) {
@@ -149,9 +152,12 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             uint4_t c[Q];
 #pragma unroll
             for (int q = 0; q < Q; ++q) c[q] = s_w[(q * KG + 2 * s + half) * LD + (lane & 31)];
+            if (s == kPlus)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[i] = -sum[i];
             mma(sum, c, x[s]);
         }
-        const float scale = p.narrow_scale && nseg ? p.narrow_scale[t.g] : 1.f;
+        const float scale = kSign * (p.narrow_scale && nseg ? p.narrow_scale[t.g] : 1.f);
         T *const mine = reinterpret_cast<T *>(turn) + (lane & 31) * kTurn<T>;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
@@ -165,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
 #pragma unroll
         for (int s = 0; s < XP; ++s) {
             const int k = (2 * s + half) * U;
-            to_units(load_row8<T, false>(mine + k, P * W - k), h[s], lose);
+            to_units(load_row8<T, false>(mine + k, P * W - k), h[s], lose, kSign);
         }
         wave_sync();
     } else if (EXT) {
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         for (int s = 0; s < XP; ++s) {
             const int k = (2 * s + half) * U;
             const T *const q = static_cast<const T *>(p.h) + (grouped ? (t.p0 + pl) * (P * W) : 0) + k;
-            to_units(load_row8<T, true>(q, grouped ? P * W - k : 0), h[s], lose);
+            to_units(load_row8<T, true>(q, grouped ? P * W - k : 0), h[s], lose, kSign);
         }
     }
     // outputs: of a piece of 128 bytes this lane stores vector lane % kVecs of rows 64 / kVecs i + lane / kVecs
@@ -270,7 +276,14 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             mma(acc[1], c1, b);
         };
 #pragma unroll
-        for (int s = 0; s < NP; ++s) product(s, x[s]);
+        for (int s = 0; s < NP; ++s) {
+            if (s == kPlus)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c][i] = -acc[c][i];
+            product(s, x[s]);
+        }
         if (EXT) {
             for (int seg = 0;;) {
                 const bool in_seg = nseg > 0 && pl >= s_seg_at[seg] && pl < s_seg_at[seg + 1];
@@ -298,7 +311,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             for (int c = 0; c < kPiece<T> / 32; ++c)
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    convert(vec_val<T, !WNK>(acc[piece / 32 + c], v),
+                    convert(kSign * vec_val<T, !WNK>(acc[piece / 32 + c], v),
                             turn[((lane & 31) * kTurn<T> + 32 * c + vec_col<T, !WNK>(v, half)) / 4]);
             wave_sync();
             const int in_piece = 4 * (lane % kVecs), col = first_col(ct) + piece + in_piece;
