@@ -5,7 +5,7 @@
 // of BN columns of its share of the output, so that its input rows come from HBM once and from the
 // L2 for every further column tile; the weights of a group stay in the L2s. The loads of the next
 // step (rows and weights, kStep deep) are in flight while a step is multiplied. None of them is under a
-// condition: a vector that would pass the end of its row starts early, one without values points to some
+// condition (adapters' gradients 500 us, with one 530): a vector that would pass the end of its row starts early, one without values points to some
 // that exist, and both are put right when they are staged. Only widths below a vector (WIDE false) load
 // value by value.
 //
@@ -111,9 +111,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     bool lose = false;
     float sign = 1.f;  // of the step's rows
     auto fetch = [&]() {
-        if (next.ct >= ct1) return;
+        if (!WIDE && next.ct >= ct1) return;  // else past the last step the last tile's first loads again
         const bool ext = next.seg >= 0;
-        const int seg = ext ? next.seg : 0, c0 = next.ct * BN, k = next.k;
+        const int seg = ext ? next.seg : 0, c0 = (next.ct < ct1 ? next.ct : ct1 - 1) * BN, k = next.k;
         const int K = ext ? P * W : p.K;   // of the rows
         const int ld = ext ? p.r : p.K;    // of the weights
         const T *wb = w;
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
                 else l.wt[u] = load_8<T, false>(q + c, u < l.wk ? p.N - c : 0);
             }
         }
-        advance(next);
+        if (next.ct < ct1) advance(next);
     };
     auto stage = [&]() {
         uint4_t u[Q];

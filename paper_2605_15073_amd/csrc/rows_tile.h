@@ -14,10 +14,10 @@
 // (parts_lose), forms its sums again in plain fp32.
 //
 // Operands whose k is contiguous in memory are staged eight k a load. The others (weights of the
-// forward product, both operands of a weight gradient) are loaded 8 bytes wide (kWide lanes), 8 rows
-// deep, and transposed in registers; the units of a thread then go to places 32 / kWide apart within a
-// block of 32 (place()), so that neighbouring threads write neighbouring units. The matrix instruction
-// does not care which lane carries which column: lane_of() gives the column that a place holds.
+// forward product, both operands of a weight gradient) are loaded 8 or 16 bytes wide (kWide, kFull lanes), 8
+// rows deep, and transposed in registers; the units of a thread then go to places apart within a block of 32
+// (place(), place_full()), so that neighbouring threads write neighbouring units. The matrix instruction does
+// not care which lane carries which column; the stores find each column where its place is.
 #ifndef CGTP_ROWS_TILE_H
 #define CGTP_ROWS_TILE_H
 
@@ -342,14 +342,65 @@ __device__ __forceinline__ void put(uint4_t *tile, int groups, int kg, int r, co
     for (int c = 0; c < kSplit<T>; ++c) tile[(c * groups + kg) * (R + 1) + r] = u[c];
 }
 
-// Where a transposed operand's lane r lies in its block of 32, and which lane a place holds.
+// Where a transposed operand's lane r lies in its block of 32.
 template <typename T> __device__ __forceinline__ int place(int r)
 {
     return sizeof(T) == 2 ? (r & ~31) | (r & 3) << 3 | (r >> 2 & 7) : (r & ~31) | (r & 1) << 4 | (r >> 1 & 15);
 }
-template <typename T> __device__ __forceinline__ int lane_of(int p)
+
+// The forms for 16-byte loads (rows_outer.hip): the units of kFull lanes, their places, and the columns that a
+// lane's sums hold. bf16's eight units go four apart in a block of 32, in odd blocks with the halves of the
+// wave exchanged, so that neighbouring threads and blocks write to different banks.
+template <typename T> constexpr int kFull = 16 / (int)sizeof(T);
+
+__device__ __forceinline__ void to_units(const uint4_t (&in)[8], uint4_t (&u)[8][1], bool &, float = 1.f)
 {
-    return sizeof(T) == 2 ? (p & ~31) | (p & 7) << 2 | (p >> 3 & 3) : (p & ~31) | (p & 15) << 1 | (p >> 4 & 1);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            u[j][0][e] = __builtin_amdgcn_perm(in[2 * e + 1][j >> 1], in[2 * e][j >> 1],
+                                               (j & 1) ? 0x07060302u : 0x05040100u);
+}
+
+__device__ __forceinline__ void to_units(const uint4_t (&in)[8], uint4_t (&u)[4][3], bool &lose, float sign = 1.f)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = sign * __builtin_bit_cast(float, (unsigned)in[e][j]);
+        split8(x, u[j], lose);
+    }
+}
+
+template <typename T> __device__ __forceinline__ int place_full(int r)
+{
+    if (sizeof(T) == 4) return (r & ~31) | (r & 3) << 3 | (r >> 2 & 7);
+    return (r & ~31) | (r & 3) << 3 | ((r >> 2 ^ r >> 5) & 1) << 2 | (r >> 3 & 3);
+}
+template <typename T> __device__ __forceinline__ int lane_of_full(int p)
+{
+    if (sizeof(T) == 4) return (p & ~31) | (p & 7) << 2 | (p >> 3 & 3);
+    return (p & ~31) | (p & 3) << 3 | ((p >> 2 ^ p >> 5) & 1) << 2 | (p >> 3 & 3);
+}
+
+// Four consecutive columns, v = 0..3, of the block of 32 that starts at place p: the first, from p on; the
+// values are the sums v, 4 + v, 8 + v, 12 + v.
+template <typename T> __device__ __forceinline__ int vec_col_full(int p, int v, int half)
+{
+    return p + (sizeof(T) == 4 ? 4 * (4 * half + v) : 8 * v + 4 * (half ^ (p >> 5 & 1)));
+}
+
+template <typename T> __device__ __forceinline__ void settle(uint4_t &v, int early)
+{
+    for (int i = 0; i < early; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned up = e < 3 ? v[(e + 1) % 4] : 0u;
+            v[e] = sizeof(T) == 4 ? up : v[e] >> 16 | up << 16;
+        }
+    }
 }
 
 __device__ __forceinline__ void mfma(float16_t &acc, uint4_t a, uint4_t b)
