@@ -13,11 +13,15 @@
 // place), and the last column tile starts early enough to end with the rows. WHOLE: columns come in aligned
 // fours.
 //
+// Measured: 525,308 rows, 64 -> 896: 474 us in fp32 (4.3 TB/s) and 232 us in bf16 (4.4 TB/s), 93% of it
+// stores; bound by memory, a large copy reaches 4.8 TB/s.
+//
 // Adapters: the narrow product's rows are further k of the same tile, held in registers like the
 // inputs, with the adapter's second matrix behind the shared weights in LDS; a tile whose rows have several
 // adapters takes them one after the other, with the rows of the others zero. Where adapters have rows enough
 // for tiles of their own (FUSED) the narrow product is formed here too: from the inputs in registers and the
-// adapter's first matrix through LDS, turned in the wave's piece, and held from then on.
+// adapter's first matrix through LDS, turned in the wave's piece, and held from then on: 525,308 rows of 32
+// adapters, 64 -> 896, rank 16, bf16 240 us (4.2 TB/s), as a pass of its own 305.
 #include "internal.h"
 #include "rows_tile.h"
 
