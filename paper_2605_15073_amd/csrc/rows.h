@@ -70,9 +70,11 @@ struct RowOuter {
 size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B);
 hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &p, void *ws,
                             hipStream_t s);
-// The form for groups of few rows (rows_few.hip): it takes groups of up to kFewRows rows and leaves the
-// others to the tiled kernel.
-constexpr int kFewRows = 64;
+// The forms for groups of few rows (rows_few.hip), up to kFewMean on the mean, and whether that of products
+// covers one. Of weight gradients, groups of more than kFewRows rows are left to the tiled kernel.
+constexpr int kFewMean = 4, kFewRows = 64;
+bool row_few_takes(int dtype, const RowOrder &o, const RowProduct &p);
+hipError_t launch_row_few(const RowOrder &o, const RowProduct &p, hipStream_t s);
 hipError_t launch_row_outer_few(int dtype, const RowOrder &o, const RowOuter &q, hipStream_t s);
 size_t narrow_bytes(int dtype, int64_t n_rows, int N);
 

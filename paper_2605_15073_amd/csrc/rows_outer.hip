@@ -22,7 +22,6 @@ namespace {
 
 using namespace rows;
 
-constexpr int kFewMean = 4;
 
 template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, int shift, bool big,

@@ -341,6 +341,7 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
     if constexpr (WNK)
         if (p.a) return p.N <= 64 ? launch<T, true, 128, 64, 4, true>(o, p, s) : launch<T, true, 128, 128, 4, true>(o, p, s);
     if (p.a) return launch_row_wide(dtype, o, p, s);
+    if (row_few_takes(dtype, o, p)) return launch_row_few(o, p, s);
     const int64_t groups = p.w_group ? o.G : 1;
     const bool few = o.n < 64 * groups;  // rows per group
     if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);

@@ -86,15 +86,11 @@ __device__ __forceinline__ Tile find_tile(const RowOrder &o, int shift, int64_t 
     return t;
 }
 
-// Tile j of a group of more than kFewRows rows, where the others are looked after elsewhere: index m is for
-// the group that holds position (m + 1) kFewRows, and the i-th such index of a group for its tile i. A group of
-// n rows, n > kFewRows, holds at least floor((n - 1) / kFewRows) such positions beyond its start, no fewer than
-// tiles of 2 kFewRows.
-__device__ __forceinline__ Tile find_big(const RowOrder &o, int shift, int64_t m)
+// The last group, of G + 1, that starts at position pos or before it: the one that holds pos.
+__device__ __forceinline__ int group_at(const RowOrder &o, int64_t pos)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t pos = (m + 1) * kFewRows;
-    int lo = 0, len = o.G + 1;  // the last g with offsets[g] <= pos lies in [lo, lo + len)
+    int lo = 0, len = o.G + 1;  // it lies in [lo, lo + len)
     while (len > 1) {
         const int s = (len + 63) / 64;
         const bool in = lane * s < len;
@@ -103,7 +99,16 @@ __device__ __forceinline__ Tile find_big(const RowOrder &o, int shift, int64_t m
         lo += skip;
         len = len - skip < s ? len - skip : s;
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Tile j of a group of more than kFewRows rows, where the others are looked after elsewhere: index m is for
+// the group that holds position (m + 1) kFewRows, and the i-th such index of a group for its tile i. A group of
+// n rows, n > kFewRows, holds at least floor((n - 1) / kFewRows) such positions beyond its start, no fewer than
+// tiles of 2 kFewRows.
+__device__ __forceinline__ Tile find_big(const RowOrder &o, int shift, int64_t m)
+{
+    const int lo = group_at(o, (m + 1) * kFewRows);
     Tile t;
     t.g = -1;
     if (lo >= o.G) return t;

@@ -162,6 +162,42 @@ def test_grouped_few_rows_a_group(cg, dtype, n, G, n_in, n_out, kind):
     check(dw, want[1], "dw")
 
 
+@pytest.mark.parametrize("n_in,n_out", [(600, 5), (5, 600), (129, 70), (9, 8), (70, 4), (3, 40), (33, 65)])
+@pytest.mark.parametrize("kind", ["even", "holes"])
+@pytest.mark.parametrize("pad", [0, 1, 4])
+def test_grouped_few_rows_strided_and_masked(cg, n_in, n_out, kind, pad):
+    """Few rows a group in fp32, one group of many: strides, bare rows that hold NaN and infinities,
+    inputs with a place that order leaves out, and rows without values past their end."""
+    import torch
+
+    n, G = 230, 90
+    rng = np.random.default_rng([n_in, n_out, pad])
+    x, w, dy = _linear(rng, n, G, n_in, n_out, "f32")
+    ids = draw_ids(rng, n, G, kind)
+    ids[:77] = 4                              # more rows than a workgroup, or a weight gradient's form, takes
+    bare = np.flatnonzero((ids < 0) | (ids >= G))
+    xn, dyn = x.copy(), dy.copy()
+    xn[bare], dyn[bare] = np.nan, np.inf
+    x[bare], dy[bare] = 0, 0
+    offsets, order = cg.group_rows(dev(ids), G)
+    lost = int(order[3])
+    order[3] = -7
+    x[lost], dy[lost] = 0, 0
+    X, DY, W = strided(dev(xn), pad), strided(dev(dyn), pad), dev(w)
+    y = strided(torch.full((n, n_out), 7.0, device="cuda"), pad)
+    dx = strided(torch.full((n, n_in), 7.0, device="cuda"), pad)
+    cg.grouped_linear(X, W, offsets, order, y=y)
+    _, dw = cg.grouped_linear_grad(X, W, DY, offsets, order, dx=dx)
+    assert (y[lost] == 7).all() and (dx[lost] == 7).all()
+    y[lost], dx[lost] = 0, 0
+    check(y, ref.grouped(x, w, ids, "f32"), "y")
+    want = ref.grouped_grad(x, w, dy, ids, "f32")
+    check(dx, want[0], "dx")
+    check(dw, want[1], "dw")
+    for t in (y, dx):
+        assert pad == 0 or torch.isnan(t._base[:, t.shape[1]:]).all()
+
+
 @pytest.mark.parametrize("where", ["x", "w", "dy"])
 @pytest.mark.parametrize("value", [1e-38, 3e-40, 3.3e38, float("inf")])
 @pytest.mark.parametrize("n,n_in,n_out", [(300, 64, 130), (300, 130, 72), (700, 96, 40)])
