@@ -625,9 +625,10 @@ def _row_call(like, stream):
     torch = _torch()
     if not like.is_cuda:
         raise ValueError(f"expected device tensors, got one on {like.device}")
-    current = torch.cuda.current_stream(like.device.index)
-    if stream is None or stream == current:
-        return current.cuda_stream, None
+    # the handle itself: a Stream object costs a tenth of a small call
+    current = torch._C._cuda_getCurrentRawStream(like.device.index)
+    if stream is None or stream.cuda_stream == current:
+        return current, None
     return stream.cuda_stream, stream
 
 
@@ -663,7 +664,7 @@ def _bytes(name, *args):
 def _run(name, like, *args):
     """The call on like's device. Pointers are integers or None."""
     torch = _torch()
-    if torch.cuda.current_device() == like.device.index:
+    if torch._C._cuda_getDevice() == like.device.index:
         status = getattr(_lib, name)(*args)
     else:
         with torch.cuda.device(like.device):

@@ -81,6 +81,23 @@ size_t adapter_bytes(int dtype, int64_t n, int rank)
     return align256(cgtp::narrow_bytes(dtype, n, rank));
 }
 
+// The product y of adapters, but for the pointers: what forms cover it does not depend on them.
+cgtp::RowProduct adapter_product(int n_in, int n_out, int rank, const void *a)
+{
+    cgtp::RowProduct p{};
+    p.K = n_in;
+    p.N = n_out;
+    p.a = a;
+    p.r = rank;
+    return p;
+}
+
+// h, where the product does not form it itself
+size_t adapter_forward_bytes(int dtype, int64_t n, int G, const cgtp::RowProduct &p)
+{
+    return cgtp::adapter_wide_takes(dtype, {n, G, nullptr, nullptr}, p) ? 0 : adapter_bytes(dtype, n, p.r);
+}
+
 // h and u, then the sums of da and of db, which use the same space one after the other
 size_t adapter_grad_bytes(int dtype, int64_t n, int G, int n_in, int n_out, int rank)
 {
@@ -221,7 +238,8 @@ extern "C" int cgtp_adapter_linear_bytes(int dtype, int64_t n_rows, int n_groups
     CGTP_TRY(check_sizes(dtype, n_rows, n_groups, n_in, n_out));
     CGTP_TRY(check_rank(rank));
     if (!bytes) return report(CGTP_ERR_ARG, "bytes is NULL");
-    *bytes = adapter_bytes(dtype, n_rows, rank);
+    const cgtp::RowProduct p = adapter_product(n_in, n_out, rank, bytes);  // a: any pointer, for "adapters"
+    *bytes = adapter_forward_bytes(dtype, n_rows, n_groups, p);
     return CGTP_OK;
 }
 
@@ -243,20 +261,16 @@ extern "C" int cgtp_adapter_linear(int dtype, int64_t n_rows, int n_groups, int 
     CGTP_TRY(check_ptr(b, "b", es));
     if (scale) CGTP_TRY(check_ptr(scale, "scale", 4));
     CGTP_TRY(check_rows(y, "y", y_stride, n_out, n_rows, es));
-    CGTP_TRY(check_ws(workspace, ws_bytes, adapter_bytes(dtype, n_rows, rank)));
+    cgtp::RowProduct p = adapter_product(n_in, n_out, rank, a);
+    CGTP_TRY(check_ws(workspace, ws_bytes, adapter_forward_bytes(dtype, n_rows, n_groups, p)));
     const cgtp::RowOrder o{n_rows, n_groups, offsets, order};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    cgtp::RowProduct p{};
     p.in = x;
     p.in_stride = x_stride;
-    p.K = n_in;
     p.w = w;
-    p.N = n_out;
     p.out = y;
     p.out_stride = y_stride;
-    p.a = a;
     p.v = b;
-    p.r = rank;
     p.narrow_scale = scale;
     hipError_t e;
     if (cgtp::adapter_wide_takes(dtype, o, p)) {
