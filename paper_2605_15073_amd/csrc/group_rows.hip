@@ -2,14 +2,15 @@
 //
 // Chunks of consecutive rows count their ids, a scan over the chunks turns the counts into the
 // position of each chunk's first row of each group, and the chunks then place their rows. A workgroup
-// takes its chunk in rounds of kRound rows, whose ids it holds in registers, eight to a thread, so that
+// takes its chunk in rounds of kRound rows, whose ids it holds in registers, four to a thread, so that
 // counting and placing wait for memory once; every wave owns consecutive rows of a round. A row's rank among
 // the 64 that a wave handles together comes from ballots over the bits of the id: no atomic decides an
 // order. Rows whose id is outside [0, G) form a group G of their own, placed last.
 //
 // Up to kRound rows one workgroup does all of it in one launch. Bound by latency: the chains of three
-// launches, and in each of memory, LDS and barriers. Measured: 525,308 rows of 4,005 groups 33 us (counting
-// 6.5, scan 7.6, placing 20.3), 64 rows 9.8 us (the kernel 4.4).
+// launches, and in each of memory, LDS and barriers. Measured: 525,308 rows of 4,005 groups 26 us (counting
+// 6.3, scan 4.5, placing 15; 1.5 of it for stores to scattered places), of 5 groups 18, 64 rows 9 us (the kernel 5.5).
+// 512 threads of eight ids took 27 us; ranks from atomic adds, with ballots only where keys meet, 27.
 #include "internal.h"
 #include "rows.h"
 
@@ -17,12 +18,16 @@ namespace cgtp {
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
-constexpr int kPer = 8;                       // ids of a thread
+constexpr int kPer = 4;                       // ids of a thread
 constexpr int kRound = kThreads * kPer;       // rows of a round
 constexpr int kChunks = 256;                  // chunks at most
-constexpr int kScanKeys = 64, kScanSlices = 4;
+constexpr int kScanKeys = 64, kScanSlices = 16;
+constexpr int kWordsEach = ((CGTP_MAX_GROUPS + 2) / 2 + kThreads - 1) / kThreads;  // words of two keys of a thread
+
+// Words of two of the G + 1 keys, in whole 16 bytes.
+__host__ __device__ constexpr int word_stride(int G) { return ((G + 2) / 2 + 3) / 4 * 4; }
 
 struct Shape {
     int chunks, rounds;  // rounds of a chunk
@@ -68,109 +73,135 @@ __global__ __launch_bounds__(kThreads) void k_group_count(int64_t n, int G, int 
     for (int g = threadIdx.x; g <= G; g += kThreads) counts[(int64_t)blockIdx.x * (G + 1) + g] = sh[g];
 }
 
-// In place: the rows of the key in the chunks before; totals[key]. A workgroup takes 64 keys, four threads a
-// key with a quarter of the chunks each.
+// In place: the rows of the key in the chunks before; totals[key]. A workgroup takes 64 keys, a wave of it a slice
+// of the chunks, whose counts it holds in registers: one trip to memory.
 __global__ __launch_bounds__(kScanKeys *kScanSlices) void k_group_scan(int G, int chunks,
                                                                        int32_t *__restrict__ counts,
                                                                        int32_t *__restrict__ totals)
 {
+    constexpr int kMost = kChunks / kScanSlices;
     __shared__ int s_sum[kScanSlices][kScanKeys];
     const int k = threadIdx.x % kScanKeys, slice = threadIdx.x / kScanKeys;
     const int g = blockIdx.x * kScanKeys + k;
     const int per = (chunks + kScanSlices - 1) / kScanSlices;
-    const int c0 = slice * per, c1 = c0 + per < chunks ? c0 + per : chunks;
-    int sum = 0;
-    if (g <= G) {
-#pragma unroll 8
-        for (int c = c0; c < c1; ++c) sum += counts[(int64_t)c * (G + 1) + g];
-    }
+    const int c0 = slice * per, own = chunks - c0 < per ? chunks - c0 : per;
+    int v[kMost], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) v[i] = g <= G ? counts[(int64_t)(i < own ? c0 + i : 0) * (G + 1) + g] : 0;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) sum += i < own ? v[i] : 0;
     s_sum[slice][k] = sum;
     __syncthreads();
     if (g > G) return;
     int before = 0;
     for (int s = 0; s < slice; ++s) before += s_sum[s][k];
     if (slice == kScanSlices - 1) totals[g] = before + sum;
-    for (int c = c0; c < c1; c += 8) {
-        int v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = counts[(int64_t)(c + i < c1 ? c + i : c0) * (G + 1) + g];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < c1) {
-                counts[(int64_t)(c + i) * (G + 1) + g] = before;
-                before += v[i];
-            }
+    for (int i = 0; i < kMost; ++i) {
+        if (i >= own) break;
+        counts[(int64_t)(c0 + i) * (G + 1) + g] = before;
+        before += v[i];
     }
 }
 
-// LDS: base[G + 1], the position of the round's first row of each key, then run[kWaves][G + 1], the rows of
+// Counts of a wave fit 16 bits (a round's are kRound at most), so a word holds those of two keys: it is scanned
+// over the waves as one. Word w = tid + kThreads j, keys 2 w and 2 w + 1, is this thread's throughout; its loads
+// of totals and counts are on their way while the round is counted.
+//
+// LDS: base[2 words], the position of the round's first row of each key, then run[kWaves][words], the rows of
 // each key that the waves before, then this one, have placed in the round.
 __global__ __launch_bounds__(kThreads) void k_group_place(
     int64_t n, int G, int rounds, const int32_t *__restrict__ ids, const int32_t *__restrict__ counts,
     const int32_t *__restrict__ totals, int32_t *__restrict__ offsets, int32_t *__restrict__ order)
 {
-    extern __shared__ int sh[];
-    __shared__ int wave_sum[kWaves];
+    extern __shared__ __align__(16) int sh[];
+    __shared__ int wave_sum[64];
+    static_assert(kWordsEach * kWaves <= 64, "one wave scans the sums");
+    const int words = (G + 2) / 2, stride = word_stride(G);
     int *const base = sh;
-    int *const run = sh + G + 1;
+    unsigned *const run = reinterpret_cast<unsigned *>(sh + 2 * stride);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t r0 = (int64_t)blockIdx.x * rounds * kRound;
-    int *const mine = run + wave * (G + 1);
+    unsigned *const mine = run + wave * stride;
     int key[kPer];
     if (n > 0) load_keys(key, r0, n, G, ids);
+    int total[kWordsEach][2], count[kWordsEach][2];
+#pragma unroll
+    for (int j = 0; j < kWordsEach; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int g = 2 * (tid + kThreads * j) + h;
+            total[j][h] = totals && g <= G ? totals[g] : 0;
+            count[j][h] = counts && g <= G ? counts[(int64_t)blockIdx.x * (G + 1) + g] : 0;
+        }
     int bits = 1;
     while ((G >> bits) != 0) ++bits;
     for (int round = 0; round < rounds; ++round) {
-        for (int i = tid; i < kWaves * (G + 1); i += kThreads) run[i] = 0;
+        for (int i = tid; i < kWaves * stride / 4; i += kThreads) reinterpret_cast<uint4 *>(run)[i] = uint4{0, 0, 0, 0};
         __syncthreads();
         if (n > 0) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
-                if (key[i] >= 0) atomicAdd(&mine[key[i]], 1);
+                if (key[i] >= 0) atomicAdd(&mine[key[i] >> 1], 1u << (16 * (key[i] & 1)));
         }
         __syncthreads();
-        // each wave's first place among the round's rows of a key; in the first round the keys' first
-        // positions: the exclusive scan of their totals (the round's own where there is one chunk)
-        for (int g = tid; g <= G; g += kThreads) {
-            int t = 0;
+        // each wave's first place among the round's rows of a key
+        unsigned in_round[kWordsEach];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const int c = run[w * (G + 1) + g];
-                run[w * (G + 1) + g] = t;
-                t += c;
+        for (int j = 0; j < kWordsEach; ++j) {
+            const int w = tid + kThreads * j;
+            unsigned t = 0;
+            if (w < words) {
+#pragma unroll
+                for (int v = 0; v < kWaves; ++v) {
+                    const unsigned c = run[v * stride + w];
+                    run[v * stride + w] = t;
+                    t += c;
+                }
             }
-            if (round == 0) base[g] = totals ? totals[g] : t;
+            in_round[j] = t;
         }
-        __syncthreads();
         if (round == 0) {
-            const int span = (G + 1 + kThreads - 1) / kThreads;
-            int first = tid * span, last = first + span;
-            if (first > G + 1) first = G + 1;
-            if (last > G + 1) last = G + 1;
-            int sum = 0;
-            for (int g = first; g < last; ++g) sum += base[g];
-            int scan = sum;
+            // the keys' first positions: the exclusive scan of their totals (the round's own where there is
+            // one chunk), j by j, in each over the threads
+            int sum[kWordsEach], scan[kWordsEach];
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int up = __shfl_up(scan, d);
-                if (lane >= d) scan += up;
-            }
-            if (lane == 63) wave_sum[wave] = scan;
-            __syncthreads();
-            int at = scan - sum;
-            for (int w = 0; w < wave; ++w) at += wave_sum[w];
-            for (int g = first; g < last; ++g) {
-                const int t = base[g];
-                base[g] = at;
-                at += t;
+            for (int j = 0; j < kWordsEach; ++j) {
+                if (!totals) total[j][0] = in_round[j] & 0xffff, total[j][1] = in_round[j] >> 16;
+                scan[j] = sum[j] = total[j][0] + total[j][1];
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const int up = __shfl_up(scan[j], d);
+                    if (lane >= d) scan[j] += up;
+                }
+                if (lane == 63) wave_sum[j * kWaves + wave] = scan[j];
             }
             __syncthreads();
-            if (blockIdx.x == 0)
-                for (int g = tid; g <= G; g += kThreads) offsets[g] = base[g];
-            if (counts)
-                for (int g = tid; g <= G; g += kThreads) base[g] += counts[(int64_t)blockIdx.x * (G + 1) + g];
+            if (wave == 0) {
+                const int own = lane < kWordsEach * kWaves ? wave_sum[lane] : 0;
+                int at = own;
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const int up = __shfl_up(at, d);
+                    if (lane >= d) at += up;
+                }
+                wave_sum[lane] = at - own;
+            }
             __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kWordsEach; ++j) {
+                const int w = tid + kThreads * j;
+                if (w >= words) break;
+                int at = wave_sum[j * kWaves + wave] + scan[j] - sum[j];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (blockIdx.x == 0 && 2 * w + h <= G) offsets[2 * w + h] = at;
+                    base[2 * w + h] = at + count[j][h];
+                    at += total[j][h];
+                }
+            }
         }
+        __syncthreads();
         if (n == 0) return;
         const int64_t r = r0 + (int64_t)round * kRound + wave * (kPer * 64) + lane;
 #pragma unroll
@@ -183,22 +214,22 @@ __global__ __launch_bounds__(kThreads) void k_group_place(
                 same &= ((k >> b) & 1) ? set : ~set;
             }
             const unsigned long long below = same & ((1ull << lane) - 1);
-            int before = 0;
-            if (in) {
-                before = mine[k];
-                order[base[k] + before + __popcll(below)] = (int)(r + 64 * i);
-            }
+            if (in) order[base[k] + (int)(mine[k >> 1] >> (16 * (k & 1)) & 0xffff) + __popcll(below)] = (int)(r + 64 * i);
             // the first of the rows that share a key moves its count on, once all have read it
             __builtin_amdgcn_wave_barrier();
-            if (in && below == 0) mine[k] = before + __popcll(same);
+            if (in && below == 0) atomicAdd(&mine[k >> 1], (unsigned)__popcll(same) << (16 * (k & 1)));
             __builtin_amdgcn_wave_barrier();
         }
         if (round + 1 == rounds) break;
         load_keys(key, r0 + (int64_t)(round + 1) * kRound, n, G, ids);
         __syncthreads();
-        // the last wave's counts are the round's
-        for (int g = tid; g <= G; g += kThreads) base[g] += run[(kWaves - 1) * (G + 1) + g];
-        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kWordsEach; ++j) {
+            const int w = tid + kThreads * j;
+            if (w >= words) break;
+            base[2 * w] += in_round[j] & 0xffff;
+            base[2 * w + 1] += in_round[j] >> 16;
+        }
     }
 }
 
@@ -213,8 +244,8 @@ size_t group_rows_bytes(int64_t n, int G)
 hipError_t launch_group_rows(int64_t n, int G, const int32_t *ids, int32_t *offsets, int32_t *order,
                              void *ws, hipStream_t s)
 {
-    const size_t place_lds = 4 * (size_t)(kWaves + 1) * (G + 1);
-    static_assert(4 * (kWaves + 1) * (CGTP_MAX_GROUPS + 1) + 1024 <= 160 * 1024, "LDS");
+    const size_t place_lds = 4 * (size_t)(kWaves + 2) * word_stride(G);
+    static_assert(4 * (kWaves + 2) * word_stride(CGTP_MAX_GROUPS) + 1024 <= 160 * 1024, "LDS");
     if (n <= kRound) {
         hipLaunchKernelGGL(k_group_place, dim3(1), dim3(kThreads), place_lds, s, n, G, 1, ids, nullptr,
                            nullptr, offsets, order);
