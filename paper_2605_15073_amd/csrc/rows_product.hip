@@ -38,8 +38,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
     constexpr int BX = BN + (FUSED ? 32 : 0), TX = TC + (FUSED ? 1 : 0);  // with the narrow product's columns
     static_assert(!FUSED || (WNK && WR == 4 && WIDE), "fused: a wave has whole rows, weights are [N][K]");
-    constexpr int kShift = BM == 128 ? 7 : BM == 64 ? 6 : 5;
-    static_assert(BM == 1 << kShift && TR >= 1 && TC >= 1, "tile");
+    static_assert(TR >= 1 && TC >= 1, "tile");
     constexpr int kLanes = kThreads / KG;              // rows staged at once
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
     constexpr int NC = (BX + kLanes - 1) / kLanes;
@@ -53,7 +52,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         t.p1 = t.p0 + BM < o.n ? t.p0 + BM : o.n;
         t.g = 0;
     } else {
-        t = find_tile(o, kShift, blockIdx.x);
+        t = find_tile(o, TileRows<BM>{}, blockIdx.x);
         if (t.g < 0 || t.p0 >= t.p1) return;
     }
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;

@@ -49,7 +49,21 @@ __device__ __forceinline__ int clamp_offset(int v, int64_t n)
     return v < 0 ? 0 : (int64_t)v > n ? (int)n : v;
 }
 
-// Groups share the sequence of rows. Cut into tiles of R = 2^shift positions of one group, tile j of
+// Positions over the rows of a tile: R, a power of two known here, or the chunks of a weight gradient, a multiple
+// of 64 up to 2^14. Of those the quotient is that of 64ths, x < 2^25 over q <= 256, by m = ceil(2^33 / q): what m
+// exceeds 2^33 / q by adds x (m q - 2^33) / (2^33 q) < 1 / q.
+template <int R> struct TileRows {
+    static constexpr int rows = R;
+    __device__ int of(int pos) const { return pos / R; }
+};
+struct ChunkRows {
+    int rows;
+    unsigned m;
+    explicit ChunkRows(int r) : rows(r), m((unsigned)(((1ull << 33) + r / 64 - 1) / (r / 64))) {}
+    __device__ int of(int pos) const { return (int)(((unsigned long long)(pos >> 6) * m) >> 33); }
+};
+
+// Groups share the sequence of rows. Cut into tiles of R positions of one group, tile j of
 // group g has the index offsets[g] / R + g + j: since floor((o + m) / R) + 1 >= floor(o / R) +
 // ceil(m / R), tiles of different groups never meet, and no prefix sum of tile counts is needed.
 // Group G holds the rows of no group. An empty group has one empty tile.
@@ -60,7 +74,7 @@ struct Tile {
 };
 
 // The wave searches 64 candidates at a time: three loads deep for 4096 groups.
-__device__ __forceinline__ Tile find_tile(const RowOrder &o, int shift, int64_t index)
+template <typename Rows> __device__ __forceinline__ Tile find_tile(const RowOrder &o, Rows R, int64_t index)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, len = o.G + 1;  // the last g with offsets[g] / R + g <= index lies in [lo, lo + len)
@@ -68,7 +82,7 @@ __device__ __forceinline__ Tile find_tile(const RowOrder &o, int shift, int64_t 
         const int s = (len + 63) / 64;
         const int c = lo + lane * s;
         const bool ok = lane * s < len &&
-                        (clamp_offset(o.offsets[lane * s < len ? c : lo], o.n) >> shift) + (int64_t)c <= index;
+                        R.of(clamp_offset(o.offsets[lane * s < len ? c : lo], o.n)) + (int64_t)c <= index;
         const int cnt = __popcll(__ballot(ok));
         const int skip = (cnt > 0 ? cnt - 1 : 0) * s;
         lo += skip;
@@ -78,9 +92,9 @@ __device__ __forceinline__ Tile find_tile(const RowOrder &o, int shift, int64_t 
     Tile t;
     t.start = clamp_offset(o.offsets[lo], o.n);
     t.end = lo < o.G ? clamp_offset(o.offsets[lo + 1], o.n) : o.n;
-    const int64_t j = index - ((t.start >> shift) + lo);
-    t.p0 = t.start + (j << shift);
-    t.p1 = t.p0 + ((int64_t)1 << shift) < t.end ? t.p0 + ((int64_t)1 << shift) : t.end;
+    const int64_t j = index - (R.of((int)t.start) + lo);
+    t.p0 = t.start + j * R.rows;
+    t.p1 = t.p0 + R.rows < t.end ? t.p0 + R.rows : t.end;
     t.g = lo;
     if (j < 0 || (j > 0 && t.p0 >= t.end)) t.g = -1;
     return t;
@@ -106,7 +120,7 @@ __device__ __forceinline__ int group_at(const RowOrder &o, int64_t pos)
 // the group that holds position (m + 1) kFewRows, and the i-th such index of a group for its tile i. A group of
 // n rows, n > kFewRows, holds at least floor((n - 1) / kFewRows) such positions beyond its start, no fewer than
 // tiles of 2 kFewRows.
-__device__ __forceinline__ Tile find_big(const RowOrder &o, int shift, int64_t m)
+__device__ __forceinline__ Tile find_big(const RowOrder &o, int R, int64_t m)
 {
     const int lo = group_at(o, (m + 1) * kFewRows);
     Tile t;
@@ -115,8 +129,8 @@ __device__ __forceinline__ Tile find_big(const RowOrder &o, int shift, int64_t m
     t.start = clamp_offset(o.offsets[lo], o.n);
     t.end = clamp_offset(o.offsets[lo + 1], o.n);
     const int64_t i = m - t.start / kFewRows;
-    t.p0 = t.start + (i << shift);
-    t.p1 = t.p0 + ((int64_t)1 << shift) < t.end ? t.p0 + ((int64_t)1 << shift) : t.end;
+    t.p0 = t.start + i * R;
+    t.p1 = t.p0 + R < t.end ? t.p0 + R : t.end;
     if (t.end - t.start > kFewRows && i >= 0 && t.p0 < t.end) t.g = lo;
     return t;
 }

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         t.p1 = t.p0 + kRows < o.n ? t.p0 + kRows : o.n;
         t.g = 0;
     } else {
-        t = find_tile(o, 7, blockIdx.x);
+        t = find_tile(o, TileRows<kRows>{}, blockIdx.x);
         if (t.g < 0 || t.p0 >= t.p1) return;
     }
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
