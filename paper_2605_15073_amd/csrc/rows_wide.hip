@@ -11,7 +11,7 @@
 // copy of its 32 registers). So the number of k is a template argument, rounded up with zeros; places
 // without a row of their own take another place's of the tile (and store the same values to the same
 // place), and the last column tile starts early enough to end with the rows. WHOLE: columns come in aligned
-// fours.
+// fours; PAST: and pieces in whole lines, which are stored past the caches.
 //
 // Measured: 525,308 rows, 64 -> 896: 474 us in fp32 (4.3 TB/s) and 232 us in bf16 (4.4 TB/s), 93% of it
 // stores; bound by memory, a large copy reaches 4.8 TB/s.
@@ -62,7 +62,7 @@ __device__ __forceinline__ void wave_sync()
 }
 
 // NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters).
-template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE>
+template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p, int splits)
 {
     constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, KG = 2 * (NP + XP), LD = kCols + 1, CW = kWide<T>;
@@ -308,8 +308,8 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
             }
         }
-        // rows of 128 bytes, several a store; whole lines go past the caches (bf16 255 us without, 199 so), parts
-        // of lines do not: 451 columns 265 us, 509 so
+        // rows of 128 bytes, several a store; whole lines go past the caches (bf16 243 us without, 200 so; fp32
+        // 505 and 440), parts of lines do not: bf16, 452 columns 250 us, 473 so; fp32, 900 columns 817 and 1,540
 #pragma unroll
         for (int piece = 0; piece < kCols; piece += kPiece<T>) {
 #pragma unroll
@@ -324,7 +324,8 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             for (int i = 0; i < kStores; ++i) {
                 const T *const from = reinterpret_cast<const T *>(turn) +
                                       ((64 / kVecs) * i + lane / kVecs) * kTurn<T> + in_piece;
-                if (WHOLE) __builtin_nontemporal_store(*reinterpret_cast<const O *>(from), reinterpret_cast<O *>(out[i] + col));
+                if (PAST) __builtin_nontemporal_store(*reinterpret_cast<const O *>(from), reinterpret_cast<O *>(out[i] + col));
+                else if (WHOLE) *reinterpret_cast<O *>(out[i] + col) = *reinterpret_cast<const O *>(from);
                 else *reinterpret_cast<O_any *>(out[i] + col) = *reinterpret_cast<const O_any *>(from);
             }
             wave_sync();
@@ -352,37 +353,47 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     }
 }
 
-template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE>
+template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool PAST>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int64_t tiles = XP > 0 && !FUSED ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
     const int whole = p.N / kCols;
     int splits = (int)(2048 / tiles);  // few rows: column tiles go to workgroups of their own
     splits = splits < 1 ? 1 : splits > whole ? whole : splits;
-    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
+    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, PAST>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
                        0, s, o, p, splits);
     return hipGetLastError();
 }
 
-template <typename T, int NP, bool WHOLE> hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
+template <typename T, int NP, bool WHOLE, bool PAST>
+hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     if (!p.h && !p.a)
-        return p.w_nk ? launch<T, true, NP, 0, false, WHOLE>(o, p, s) : launch<T, false, NP, 0, false, WHOLE>(o, p, s);
+        return p.w_nk ? launch<T, true, NP, 0, false, WHOLE, PAST>(o, p, s)
+                      : launch<T, false, NP, 0, false, WHOLE, PAST>(o, p, s);
     constexpr int X = kExtPairs<T>;
     const bool half = WHOLE && kNarrow<T> * narrow_width(p.r) <= X * kU;
     constexpr int H = WHOLE ? X / 2 : X;
-    if (p.a) return half ? launch<T, false, NP, H, true, WHOLE>(o, p, s) : launch<T, false, NP, X, true, WHOLE>(o, p, s);
-    return half ? launch<T, false, NP, H, false, WHOLE>(o, p, s) : launch<T, false, NP, X, false, WHOLE>(o, p, s);
+    if (p.a)
+        return half ? launch<T, false, NP, H, true, WHOLE, PAST>(o, p, s) : launch<T, false, NP, X, true, WHOLE, PAST>(o, p, s);
+    return half ? launch<T, false, NP, H, false, WHOLE, PAST>(o, p, s) : launch<T, false, NP, X, false, WHOLE, PAST>(o, p, s);
+}
+
+template <typename T, bool PAST> hipError_t with_fours(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    constexpr int M = kPairs<T>;
+    if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4, true, PAST>(o, p, s);
+    if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2, true, PAST>(o, p, s);
+    return with_pairs<T, M, true, PAST>(o, p, s);
 }
 
 template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    constexpr int M = kPairs<T>;
-    const bool whole = p.N % 4 == 0 && p.out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * sizeof(T)) == 0;
-    if (!whole) return with_pairs<T, M, false>(o, p, s);
-    if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4, true>(o, p, s);
-    if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2, true>(o, p, s);
-    return with_pairs<T, M, true>(o, p, s);
+    const uintptr_t out = reinterpret_cast<uintptr_t>(p.out);
+    if (p.N % 4 != 0 || p.out_stride % 4 != 0 || out % (4 * sizeof(T)) != 0)
+        return with_pairs<T, kPairs<T>, false, false>(o, p, s);
+    const bool lines = p.N % kPiece<T> == 0 && p.out_stride % kPiece<T> == 0 && out % 128 == 0;
+    return lines ? with_fours<T, true>(o, p, s) : with_fours<T, false>(o, p, s);
 }
 
 template <typename T> bool takes(const RowProduct &p)

@@ -615,3 +615,27 @@ def test_bad_offsets_and_order_stay_in_bounds(cg):
     assert (y[keep] == 16).all() and (y[[7, 60]] == -1).all()
     dx, dw = cg.grouped_linear_grad(x, w, torch.ones_like(y), offsets, order)
     assert (dw[0] == 39).all() and (dw[1] == 59).all() and (dw[2] == 0).all()
+
+
+# ---------------------------------------------------------------- lines
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n_out,pad,start", [(96, 0, 0), (128, 0, 0), (128, 4, 0), (128, 64, 0), (128, 64, 32),
+                                             (160, 0, 0), (164, 28, 0), (192, 0, 64), (196, 0, 4), (70, 2, 2)])
+def test_wide_outputs_on_lines_and_apart(cg, dtype, n_out, pad, start):
+    """Output rows that begin on lines and apart from them, in a buffer whose other values stay."""
+    import torch
+
+    rng = np.random.default_rng([n_out, pad, start])
+    n, G, n_in = 700, 3, 40
+    x, w, dy = _linear(rng, n, G, n_in, n_out, dtype)
+    ids = draw_ids(rng, n, G, "holes")
+    offsets, order = cg.group_rows(dev(ids), G)
+    X, W = dev(x, dtype), dev(w, dtype)
+    stride = n_out + pad
+    buf = torch.full((start + n * stride + 64,), 7.0, dtype=X.dtype, device="cuda")
+    y = buf[start:start + n * stride].view(n, stride)[:, :n_out]
+    cg.grouped_linear(X, W, offsets, order, y=y)
+    check(y, ref.grouped(x, w, ids, dtype), "y")
+    assert (buf[:start] == 7).all() and (buf[start + n * stride:] == 7).all()
+    assert (buf[start:start + n * stride].view(n, stride)[:, n_out:] == 7).all()
