@@ -111,6 +111,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         int xk, wk;  // values that exist of this thread's k-group of rows and weights
         int xe, we;  // what their loads started early
         unsigned rows;  // bit i: x[i] is of a row that takes part
+        bool ext;  // the step is of an adapter
     } l;
     bool lose = false;
     float sign = 1.f;  // of the step's rows
@@ -132,6 +133,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         const int xs = l.xk > 0 ? start8(kx, K) : 0;
         l.xe = l.xk > 0 ? kx - xs : 0;
         l.rows = 0;
+        l.ext = ext;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int r = rr + kLanes * i;
@@ -181,6 +183,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
             for (int i = 0; i < NC; ++i) {
                 if (BX % kLanes != 0 && rr + kLanes * i >= BX) break;
                 if (l.wk < kU) settle(l.wn[i], WIDE ? l.we : 0, l.wk);
+                if (!FUSED && l.ext) lose |= non_finite<T>(l.wn[i]);
                 to_units(l.wn[i], u, lose);
                 put<T, BX>(s_cols, KG, kg, rr + kLanes * i, u);
             }
@@ -193,6 +196,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
 #pragma unroll
                 for (int e = 0; e < 8; ++e) settle<T>(l.wt[e], l.we);
             }
+            if (!FUSED && l.ext) lose |= non_finite<T>(l.wt);
             uint4_t c[CW][Q];
             to_units(l.wt, c, lose);
 #pragma unroll
@@ -294,8 +298,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     clear();
     fetch();
     while (now.ct < ct1) step();
-    if constexpr (Q > 1) {
-        if (__syncthreads_or(lose)) {
+    if constexpr (Q > 1 || !FUSED) {
+        if ((Q > 1 || nseg > 0) && __syncthreads_or(lose)) {
             float *const h = FUSED ? reinterpret_cast<float *>(s_cols) : nullptr;
             if constexpr (FUSED) {
                 static_assert(sizeof(s_cols) >= sizeof(float) * BM * 32, "rows of up to 32 values");
@@ -312,7 +316,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
                 }
                 if (tid < rows) s_g[tid] = t.g;
             }
-            row_plain_sums<WNK>(o, p, FUSED ? 0 : t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end, h);
+            row_plain_sums<T, WNK>(o, p, FUSED ? 0 : t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end, h);
         }
     }
 }

@@ -605,9 +605,35 @@ template <typename T> __device__ __forceinline__ float narrow_at(const void *h, 
 // has rows of its own.
 template <typename T> constexpr int kWaveRows = sizeof(T) == 2 ? 2 : 4;
 
-// The sums of a workgroup that met values outside the range of parts, in plain fp32: columns [c0, c1) of its
-// rows, one result a thread at a time. h: the narrow product's rows in LDS, 32 apart, in place of p.h.
-template <bool WNK>
+// Whether one of these weights is infinite or NaN. A tile's rows of other adapters meet those of one adapter as
+// zeros, and zero times such a weight is NaN: a workgroup that finds one forms its sums row by row.
+template <typename T> __device__ __forceinline__ unsigned raised(unsigned v)
+{
+    // the sign of each value's place is set where its exponent is full: it is clear after the mask
+    return sizeof(T) == 4 ? (v & 0x7fffffffu) + 0x00800000u : ((v & 0x7fff7fffu) + 0x00800080u);
+}
+template <typename T> constexpr unsigned kSigns = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+
+template <typename T> __device__ __forceinline__ bool non_finite(const Raw8<T> &r)
+{
+    unsigned m = 0;
+#pragma unroll
+    for (int e = 0; e < 2 * (int)sizeof(T); ++e) m |= raised<T>(r.v[e / 4][e % 4]);
+    return m & kSigns<T>;
+}
+
+template <typename T> __device__ __forceinline__ bool non_finite(const uint2_t (&in)[8])
+{
+    unsigned m = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m |= raised<T>(in[e / 2][e % 2]);
+    return m & kSigns<T>;
+}
+
+// The sums of a workgroup that met values outside the range of parts or an adapter's non-finite ones, in plain
+// fp32: columns [c0, c1) of its rows, one result a thread at a time. h: the narrow product's rows in LDS, 32
+// apart, in place of p.h.
+template <typename T, bool WNK>
 __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group, int64_t p0, int rows, const int *s_row,
                                const int *s_g, int c0, int c1, const float *h = nullptr)
 {
@@ -615,23 +641,24 @@ __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const int W = narrow_width(p.r), width = c1 - c0;
-    const float *const w = static_cast<const float *>(p.w) + (int64_t)group * p.w_group;
+    const T *const w = static_cast<const T *>(p.w) + (int64_t)group * p.w_group;
     for (int e = threadIdx.x; e < rows * width; e += kThreads) {
         const int r = e / width, c = c0 + e % width;
         if (s_row[r] < 0) continue;
-        const float *const in = static_cast<const float *>(p.in) + s_row[r] * p.in_stride;
+        const T *const in = static_cast<const T *>(p.in) + s_row[r] * p.in_stride;
         float sum = 0.f;
-        for (int k = 0; k < p.K; ++k) sum += in[k] * w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c];
+        for (int k = 0; k < p.K; ++k) sum += (float)in[k] * (float)w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c];
         if ((p.h || h) && s_g[r] < o.G) {
-            const float *const v = static_cast<const float *>(p.v) + (int64_t)s_g[r] * p.r * p.N;
+            const T *const v = static_cast<const T *>(p.v) + (int64_t)s_g[r] * p.r * p.N;
             for (int k = 0; k < p.r; ++k)
-                sum += (h ? h[32 * r + k] : narrow_at<float>(p.h, p0 + r, W, k)) * v[WNK ? (int64_t)c * p.r + k : (int64_t)k * p.N + c];
+                sum += (h ? h[32 * r + k] : narrow_at<T>(p.h, p0 + r, W, k)) *
+                       (float)v[WNK ? (int64_t)c * p.r + k : (int64_t)k * p.N + c];
         }
-        if (p.narrow)
+        if (sizeof(T) == 4 && p.narrow)  // bf16: not of narrow products, which have no adapters
             static_cast<float *>(p.out)[(p0 + r) * narrow_width(p.N) + c] =
                 p.narrow_scale ? sum * p.narrow_scale[group] : sum;
         else
-            static_cast<float *>(p.out)[s_row[r] * p.out_stride + c] = sum;
+            static_cast<T *>(p.out)[s_row[r] * p.out_stride + c] = (T)sum;
     }
 }
 

@@ -248,6 +248,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 uint2_t in[8];
 #pragma unroll
                 for (int u = 0; u < U; ++u) in[u] = u < have[i] ? wt[i][u] : uint2_t{0, 0};
+                if (EXT && !FUSED && task / (kCols / CW) >= 2 * NP) lose |= non_finite<T>(in);
                 uint4_t unit[CW][Q];
                 to_units(in, unit, lose);
 #pragma unroll
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             wave_sync();
         }
     }
-    if constexpr (Q > 1) {
+    if constexpr (Q > 1 || (EXT && !FUSED)) {
         const int end = ct1 * kCols < p.N ? ct1 * kCols : p.N;
         if (__syncthreads_or(lose)) {
             float *const plain_h = FUSED ? reinterpret_cast<float *>(s_turn) : nullptr;
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 }
                 if (tid < rows) s_g[tid] = t.g;
             }
-            row_plain_sums<WNK>(o, p, p.w_group ? t.g : 0, t.p0, rows, s_row, s_g, ct0 * kCols, end, plain_h);
+            row_plain_sums<T, WNK>(o, p, p.w_group ? t.g : 0, t.p0, rows, s_row, s_g, ct0 * kCols, end, plain_h);
         }
     }
 }

@@ -617,7 +617,7 @@ def test_bad_offsets_and_order_stay_in_bounds(cg):
     assert (dw[0] == 39).all() and (dw[1] == 59).all() and (dw[2] == 0).all()
 
 
-# ---------------------------------------------------------------- lines
+# ---------------------------------------------------------------- lines, and rows of other adapters
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n_out,pad,start", [(96, 0, 0), (128, 0, 0), (128, 4, 0), (128, 64, 0), (128, 64, 32),
@@ -639,3 +639,41 @@ def test_wide_outputs_on_lines_and_apart(cg, dtype, n_out, pad, start):
     check(y, ref.grouped(x, w, ids, dtype), "y")
     assert (buf[:start] == 7).all() and (buf[start + n * stride:] == 7).all()
     assert (buf[start:start + n * stride].view(n, stride)[:, n_out:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("n,G,n_in,n_out,r", [
+    (600, 40, 64, 72, 8), (3000, 300, 64, 200, 8), (3000, 300, 33, 131, 20),   # tiles of many adapters
+    (600, 40, 64, 48, 8), (500, 40, 200, 130, 8), (300, 40, 200, 130, 64), (300, 40, 200, 130, 3),
+    (50, 9, 896, 40, 16), (1500, 3, 64, 200, 16), (1500, 3, 64, 200, 40)])
+def test_adapter_not_finite_stays_with_its_rows(cg, dtype, value, n, G, n_in, n_out, r):
+    """One adapter's second (then first) matrix has such a value: y and dx of all other rows, of other
+    adapters and of none, are what they are without it."""
+    rng = np.random.default_rng([n, n_in, r])
+    x, w, a, b, dy, scale = _adapters(rng, n, G, n_in, n_out, r, dtype)
+    ids = draw_ids(rng, n, G, "even")
+    ids[rng.random(n) < 0.1] = -1
+    bad = G // 2
+    others = ids != bad
+    assert others.any() and not others.all()
+    offsets, order = cg.group_rows(dev(ids), G)
+    X, W, DY, S = dev(x, dtype), dev(w, dtype), dev(dy, dtype), dev(scale)
+    y, y_bound = ref.adapter(x, w, a, b, scale, ids, dtype)
+    (dx, dx_bound), _, _ = ref.adapter_grad(x, w, a, b, dy, scale, ids, dtype)
+    for spoiled in ("b", "a"):
+        A, B = dev(a, dtype), dev(b, dtype)
+        if spoiled == "b":
+            B[bad, r // 2, n_out // 3] = value
+        else:
+            A[bad, n_in // 3, r // 2] = value
+        got = host(cg.adapter_linear(X, W, A, B, offsets, order, scale=S))
+        assert np.isfinite(got[others]).all(), spoiled
+        assert np.all(np.abs(got - y)[others] <= y_bound[others]), spoiled
+        col = slice(n_out // 3, n_out // 3 + 1) if spoiled == "b" else slice(None)
+        assert not np.isfinite(got[~others][:, col]).any(), spoiled
+        got = host(cg.adapter_linear_grad(X, W, A, B, DY, offsets, order, scale=S, da=False, db=False)[0])
+        assert np.isfinite(got[others]).all(), spoiled
+        assert np.all(np.abs(got - dx)[others] <= dx_bound[others]), spoiled
+        col = slice(None) if spoiled == "b" else slice(n_in // 3, n_in // 3 + 1)
+        assert not np.isfinite(got[~others][:, col]).any(), spoiled
