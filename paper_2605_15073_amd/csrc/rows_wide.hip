@@ -10,18 +10,27 @@
 // tile's stores in flight, and the sums stay where they are (a branch around a matrix instruction costs a
 // copy of its 32 registers). So the number of k is a template argument, rounded up with zeros; places
 // without a row of their own take another place's of the tile (and store the same values to the same
-// place), and the last column tile starts early enough to end with the rows. WHOLE: columns come in aligned
-// fours; PAST: and pieces in whole lines, which are stored past the caches.
+// place), and the last column tile starts early enough to end with the rows.
 //
-// Measured: 525,308 rows, 64 -> 896: 474 us in fp32 (4.3 TB/s) and 232 us in bf16 (4.4 TB/s), 93% of it
-// stores; bound by memory, a large copy reaches 4.8 TB/s.
+// Stores. LINES: every row starts on half a line, so pieces of 128 bytes go out as they are, past the caches.
+// Else a row's results are turned into a ring of two pieces, each value where its address lies in a line, and
+// leave line by line: a line is stored once the columns that it takes are there, the ends of a row in vectors that
+// overlap. WHOLE: columns come in aligned fours. Pieces stored as they come, across lines, and for all of these
+// rows either way of the caches, were slower (525,308 rows from 64, us; now, through the caches, past them):
+// bf16 452 195, 252, 473; 480 148, 201, 148; 900 345, 485, 896; fp32 452 377, 433, 812; 900 667, 815, 1,540; 912
+// 541, 659, 544; 451, odd: bf16 227, before 265. Past the caches also pays for rows on lines: bf16 896 200 us,
+// through them 243; fp32 440 and 505; and a reader of a 17 to 900 MB result behind it is no slower for it.
+//
+// Measured: 525,308 rows, 64 -> 896: 440 to 470 us in fp32 (4.3 to 4.6 TB/s) and 199 us in bf16 (5.1 TB/s), 93% of
+// it stores; bound by memory, a large copy reaches 4.8 TB/s. Rows apart from lines: 2.3 to 3.4 TB/s, bound by the
+// two broken lines of each row, whose other parts other workgroups write.
 //
 // Adapters: the narrow product's rows are further k of the same tile, held in registers like the
 // inputs, with the adapter's second matrix behind the shared weights in LDS; a tile whose rows have several
 // adapters takes them one after the other, with the rows of the others zero. Where adapters have rows enough
 // for tiles of their own (FUSED) the narrow product is formed here too: from the inputs in registers and the
 // adapter's first matrix through LDS, turned in the wave's piece, and held from then on: 525,308 rows of 32
-// adapters, 64 -> 896, rank 16, bf16 240 us (4.2 TB/s), as a pass of its own 305.
+// adapters, 64 -> 896, rank 16, bf16 201 us (5.0 TB/s), as a pass of its own 305 where this took 240.
 #include "internal.h"
 #include "rows_tile.h"
 
@@ -41,7 +50,7 @@ template <typename T> constexpr int kExtPairs = sizeof(T) == 2 ? 4 : 2;  // of a
 // results, in values: a multiple of their vectors, clear of bank conflicts between the rows that the 8
 // (fp32, 16 bytes) or 16 (bf16, 8 bytes) lanes of a cycle write.
 template <typename T> constexpr int kPiece = 128 / (int)sizeof(T);
-template <typename T> constexpr int kTurn = kPiece<T> + 4;
+template <typename T, bool LINES> constexpr int kTurn = (LINES ? 1 : 2) * kPiece<T> + 4;
 
 template <typename T> struct Out4;
 template <> struct Out4<float> { typedef float4_t t; typedef float4_any any; };
@@ -62,7 +71,7 @@ __device__ __forceinline__ void wave_sync()
 }
 
 // NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters).
-template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool PAST>
+template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool LINES>
 __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p, int splits)
 {
     constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, KG = 2 * (NP + XP), LD = kCols + 1, CW = kWide<T>;
@@ -74,7 +83,8 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     typedef typename Out4<T>::t O;
     typedef typename Out4<T>::any O_any;
     __shared__ uint4_t s_w[Q * KG * LD];
-    __shared__ O s_turn[4 * 32 * kTurn<T> / 4];
+    constexpr int TURN = kTurn<T, LINES>, RING = 2 * kPiece<T>;
+    __shared__ O s_turn[4 * 32 * TURN / 4];
     __shared__ int s_row[kRows], s_place[kRows], s_any;
     __shared__ int s_g[EXT ? kRows : 1], s_seg_g[EXT ? kRows : 1], s_seg_at[EXT ? kRows + 1 : 1], s_nseg;
 
@@ -131,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         const int k = (2 * s + half) * U;
         to_units(load_row8<T, false>(in + k, p.K - k), x[s], lose, s < kPlus ? 1.f : -1.f);
     }
-    O *const turn = s_turn + wave * (32 * kTurn<T> / 4);
+    O *const turn = s_turn + wave * (32 * TURN / 4);
     if constexpr (FUSED) {
         // the adapter's first matrix, [K][r], as a tile of 32 columns
         constexpr int kQuads = 32 / CW;
@@ -162,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             mma(sum, c, x[s]);
         }
         const float scale = kSign * (p.narrow_scale && nseg ? p.narrow_scale[t.g] : 1.f);
-        T *const mine = reinterpret_cast<T *>(turn) + (lane & 31) * kTurn<T>;
+        T *const mine = reinterpret_cast<T *>(turn) + (lane & 31) * TURN;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int col = vec_col<T, true>(v, half);
@@ -193,6 +203,9 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
 #pragma unroll
     for (int i = 0; i < kStores; ++i)
         out[i] = static_cast<T *>(p.out) + s_row[s_place[32 * wave + (64 / kVecs) * i + lane / kVecs]] * p.out_stride;
+
+    // what this lane's row of results is off the start of a line by, in values
+    const int my_at = (int)(reinterpret_cast<uintptr_t>(static_cast<T *>(p.out) + s_row[pl] * p.out_stride) % 128 / sizeof(T));
 
     // Weights. Round 0 of a column tile: the shared ones, with the first adapter's behind them; then the
     // other adapters' of the tile.
@@ -309,25 +322,60 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
             }
         }
-        // rows of 128 bytes, several a store; whole lines go past the caches (bf16 243 us without, 200 so; fp32
-        // 505 and 440), parts of lines do not: bf16, 452 columns 250 us, 473 so; fp32, 900 columns 817 and 1,540
+        // rows of 128 bytes, several a store
 #pragma unroll
         for (int piece = 0; piece < kCols; piece += kPiece<T>) {
+            const int first = first_col(ct) + piece, end = first + kPiece<T>;
 #pragma unroll
             for (int c = 0; c < kPiece<T> / 32; ++c)
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    convert(kSign * vec_val<T, !WNK>(acc[piece / 32 + c], v),
-                            turn[((lane & 31) * kTurn<T> + 32 * c + vec_col<T, !WNK>(v, half)) / 4]);
-            wave_sync();
-            const int in_piece = 4 * (lane % kVecs), col = first_col(ct) + piece + in_piece;
+                for (int v = 0; v < 4; ++v) {
+                    const float4_t f = kSign * vec_val<T, !WNK>(acc[piece / 32 + c], v);
+                    const int col = 32 * c + vec_col<T, !WNK>(v, half);
+                    if (LINES) convert(f, turn[((lane & 31) * TURN + col) / 4]);
+                    else if (WHOLE) convert(f, turn[((lane & 31) * TURN + (my_at + first + col) % RING) / 4]);
+                    else {
 #pragma unroll
-            for (int i = 0; i < kStores; ++i) {
-                const T *const from = reinterpret_cast<const T *>(turn) +
-                                      ((64 / kVecs) * i + lane / kVecs) * kTurn<T> + in_piece;
-                if (PAST) __builtin_nontemporal_store(*reinterpret_cast<const O *>(from), reinterpret_cast<O *>(out[i] + col));
-                else if (WHOLE) *reinterpret_cast<O *>(out[i] + col) = *reinterpret_cast<const O *>(from);
-                else *reinterpret_cast<O_any *>(out[i] + col) = *reinterpret_cast<const O_any *>(from);
+                        for (int e = 0; e < 4; ++e)
+                            reinterpret_cast<T *>(turn)[(lane & 31) * TURN + (my_at + first + col + e) % RING] = (T)f[e];
+                    }
+                }
+            wave_sync();
+            const int in_piece = 4 * (lane % kVecs);
+            if (LINES) {
+#pragma unroll
+                for (int i = 0; i < kStores; ++i) {
+                    const T *const from = reinterpret_cast<const T *>(turn) +
+                                          ((64 / kVecs) * i + lane / kVecs) * TURN + in_piece;
+                    __builtin_nontemporal_store(*reinterpret_cast<const O *>(from), reinterpret_cast<O *>(out[i] + first + in_piece));
+                }
+            } else {
+                const int from_col = ct0 * kCols > end - RING ? ct0 * kCols : end - RING;
+                // line `line` of each row, as far as its columns are there: places past them take the last or the first
+                auto store_line = [&](int line) {
+#pragma unroll
+                    for (int i = 0; i < kStores; ++i) {
+                        const int at = (int)(reinterpret_cast<uintptr_t>(out[i]) % 128 / sizeof(T));
+                        int c = line * kPiece<T> - at + in_piece;
+                        c = c < from_col ? from_col : c > end - 4 ? end - 4 : c;
+                        const T *const from = reinterpret_cast<const T *>(turn) + ((64 / kVecs) * i + lane / kVecs) * TURN;
+                        O v;
+                        if (WHOLE) v = *reinterpret_cast<const O *>(from + (at + c) % RING);
+                        else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] = from[(at + c + e) % RING];
+                        }
+                        *reinterpret_cast<O_any *>(out[i] + c) = v;
+                    }
+                };
+                // a line more for each piece; at the end all that is left
+                const bool early_tile = first_col(ct) < ct * kCols;
+                int line = ct * kCols / kPiece<T> + (early_tile ? 0 : piece / kPiece<T>);
+                if (ct + 1 < ct1 || piece + kPiece<T> < kCols) {
+                    store_line(line);
+                } else {
+                    for (; (line - 1) * kPiece<T> + 1 < end; ++line) store_line(line);
+                }
             }
             wave_sync();
         }
@@ -354,47 +402,49 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     }
 }
 
-template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool PAST>
+template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool LINES>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int64_t tiles = XP > 0 && !FUSED ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
     const int whole = p.N / kCols;
     int splits = (int)(2048 / tiles);  // few rows: column tiles go to workgroups of their own
     splits = splits < 1 ? 1 : splits > whole ? whole : splits;
-    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, PAST>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
+    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, LINES>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
                        0, s, o, p, splits);
     return hipGetLastError();
 }
 
-template <typename T, int NP, bool WHOLE, bool PAST>
+template <typename T, int NP, bool WHOLE, bool LINES>
 hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     if (!p.h && !p.a)
-        return p.w_nk ? launch<T, true, NP, 0, false, WHOLE, PAST>(o, p, s)
-                      : launch<T, false, NP, 0, false, WHOLE, PAST>(o, p, s);
+        return p.w_nk ? launch<T, true, NP, 0, false, WHOLE, LINES>(o, p, s)
+                      : launch<T, false, NP, 0, false, WHOLE, LINES>(o, p, s);
     constexpr int X = kExtPairs<T>;
-    const bool half = WHOLE && kNarrow<T> * narrow_width(p.r) <= X * kU;
-    constexpr int H = WHOLE ? X / 2 : X;
+    const bool half = kNarrow<T> * narrow_width(p.r) <= X * kU;
     if (p.a)
-        return half ? launch<T, false, NP, H, true, WHOLE, PAST>(o, p, s) : launch<T, false, NP, X, true, WHOLE, PAST>(o, p, s);
-    return half ? launch<T, false, NP, H, false, WHOLE, PAST>(o, p, s) : launch<T, false, NP, X, false, WHOLE, PAST>(o, p, s);
+        return half ? launch<T, false, NP, X / 2, true, WHOLE, LINES>(o, p, s)
+                    : launch<T, false, NP, X, true, WHOLE, LINES>(o, p, s);
+    return half ? launch<T, false, NP, X / 2, false, WHOLE, LINES>(o, p, s)
+                : launch<T, false, NP, X, false, WHOLE, LINES>(o, p, s);
 }
 
-template <typename T, bool PAST> hipError_t with_fours(const RowOrder &o, const RowProduct &p, hipStream_t s)
+template <typename T, bool WHOLE, bool LINES>
+hipError_t with_rows(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     constexpr int M = kPairs<T>;
-    if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4, true, PAST>(o, p, s);
-    if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2, true, PAST>(o, p, s);
-    return with_pairs<T, M, true, PAST>(o, p, s);
+    if (p.K <= M / 4 * 2 * kU) return with_pairs<T, M / 4, WHOLE, LINES>(o, p, s);
+    if (p.K <= M / 2 * 2 * kU) return with_pairs<T, M / 2, WHOLE, LINES>(o, p, s);
+    return with_pairs<T, M, WHOLE, LINES>(o, p, s);
 }
 
 template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const uintptr_t out = reinterpret_cast<uintptr_t>(p.out);
-    if (p.N % 4 != 0 || p.out_stride % 4 != 0 || out % (4 * sizeof(T)) != 0)
-        return with_pairs<T, kPairs<T>, false, false>(o, p, s);
-    const bool lines = p.N % kPiece<T> == 0 && p.out_stride % kPiece<T> == 0 && out % 128 == 0;
-    return lines ? with_fours<T, true>(o, p, s) : with_fours<T, false>(o, p, s);
+    constexpr int kHalf = kPiece<T> / 2;
+    if (p.N % kHalf == 0 && p.out_stride % kHalf == 0 && out % 64 == 0) return with_rows<T, true, true>(o, p, s);
+    if (p.N % 4 == 0 && p.out_stride % 4 == 0 && out % (4 * sizeof(T)) == 0) return with_rows<T, true, false>(o, p, s);
+    return with_rows<T, false, false>(o, p, s);
 }
 
 template <typename T> bool takes(const RowProduct &p)
