@@ -8,8 +8,8 @@
 // gets the same ones.
 //
 // Measured: 5 million parameters in 200 tensors, 32-bit states, 24 us (5.9 TB/s, partly from the caches); 64
-// million, 8-bit states, bf16 gradients and copies, the step 240 us (4.2 TB/s; 320 with the codes from rounded
-// divisions and roots throughout, bound by the vector ALU) and the decoding 139 us (4.6 TB/s, a copy's rate).
+// million, 8-bit states, bf16 gradients and copies, the step 232 us (4.4 TB/s; 80 more with the codes from
+// rounded divisions and roots throughout, bound by the vector ALU) and the decoding 128 us (5.0 TB/s).
 #include <cmath>
 #include <new>
 #include <vector>

@@ -9,7 +9,7 @@
 // early, one without values points to some that exist, and both are put right when they are staged. Only
 // widths below a vector (WIDE false) load value by value.
 //
-// Measured: row gradients of 261,766 rows, 1344 -> 128 bf16, 209 us (3.7 TB/s; bound by the reads and the
+// Measured: row gradients of 261,766 rows, 1344 -> 128 bf16, 203 us (3.8 TB/s; bound by the reads and the
 // latency of a step's loads); 60,000 rows, 896 x 896: 184 us in bf16 (520 TFLOP/s), 708 us in fp32
 // (136 TFLOP/s, six instructions a product: bound by the matrix cores and the splitting of the operands).
 //
@@ -21,7 +21,7 @@
 // FUSED: tiles of one adapter each, whose narrow product is formed here too. Its matrix, [r][K] like the
 // shared weights, gives 32 more columns of the tile (so the input is read once for both); the result goes
 // through LDS as the input rows of one more step, over the adapter's second matrix: 131,327 rows of 8
-// adapters, 896 -> 128, rank 16, fp32 350 us where the two products apart took 323 and 138.
+// adapters, 896 -> 128, rank 16, fp32 344 us where the two products apart took 323 and 138.
 #include "internal.h"
 #include "rows_tile.h"
 

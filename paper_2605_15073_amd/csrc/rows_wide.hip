@@ -15,11 +15,11 @@
 // Stores. LINES: every row starts on half a line, so pieces of 128 bytes go out as they are, past the caches.
 // Else a row's results are turned into a ring of two pieces, each value where its address lies in a line, and
 // leave line by line: a line is stored once the columns that it takes are there, the ends of a row in vectors that
-// overlap. WHOLE: columns come in aligned fours. Pieces stored as they come, across lines, and for all of these
-// rows either way of the caches, were slower (525,308 rows from 64, us; now, through the caches, past them):
+// overlap. WHOLE: columns come in aligned fours.
+// 525,308 rows from 64, us now, and with pieces stored where their columns start, through and past the caches:
 // bf16 452 195, 252, 473; 480 148, 201, 148; 900 345, 485, 896; fp32 452 377, 433, 812; 900 667, 815, 1,540; 912
-// 541, 659, 544; 451, odd: bf16 227, before 265. Past the caches also pays for rows on lines: bf16 896 200 us,
-// through them 243; fp32 440 and 505; and a reader of a 17 to 900 MB result behind it is no slower for it.
+// 541, 659, 544. Rows on lines, past and through the caches: bf16 896 200, 243, fp32 440, 505; with a reader right
+// behind, results of 4 to 900 MB, between 9% more (4 MB) and 13% less.
 //
 // Measured: 525,308 rows, 64 -> 896: 440 to 470 us in fp32 (4.3 to 4.6 TB/s) and 199 us in bf16 (5.1 TB/s), 93% of
 // it stores; bound by memory, a large copy reaches 4.8 TB/s. Rows apart from lines: 2.3 to 3.4 TB/s, bound by the
@@ -30,7 +30,8 @@
 // adapters takes them one after the other, with the rows of the others zero. Where adapters have rows enough
 // for tiles of their own (FUSED) the narrow product is formed here too: from the inputs in registers and the
 // adapter's first matrix through LDS, turned in the wave's piece, and held from then on: 525,308 rows of 32
-// adapters, 64 -> 896, rank 16, bf16 201 us (5.0 TB/s), as a pass of its own 305 where this took 240.
+// adapters, 64 -> 896, rank 16, bf16 201 us (5.0 TB/s); before its stores went past the caches 240, and 305 with a
+// narrow product of its own.
 #include "internal.h"
 #include "rows_tile.h"
 
