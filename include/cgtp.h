@@ -437,8 +437,8 @@ int cgtp_grouped_linear_grad(int dtype, int64_t n_rows, int n_groups, int n_in, 
  *   y_i = w^T x_i + scale[g] b[g]^T (a[g]^T x_i), g = g(i); y_i = w^T x_i for a row of no group.
  *   w [n_in][n_out], a [n_groups][n_in][rank], b [n_groups][rank][n_out],
  *   scale [n_groups] fp32 or NULL (all 1); 1 <= rank <= CGTP_MAX_ADAPTER_RANK.
- * a[g]^T x_i is kept between the two products in fp32 or, for CGTP_BF16, in two bf16 parts (16
- * bits of significand). Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
+ * a[g]^T x_i is kept between the two products in fp32 or, for CGTP_BF16, in three bf16 parts:
+ * 24 bits of significand either way. Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
 int cgtp_adapter_linear_bytes(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
                               int rank, size_t *bytes);
 int cgtp_adapter_linear(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out, int rank,

@@ -8,7 +8,7 @@
 // one multiple of the chunk size beyond its start, and 2 floor((s + m) / R) - 2 floor(s / R) >=
 // ceil(m / R) for m > R, so slots of different groups never meet and 2 (n / R) + 2 suffice.
 //
-// With a narrow product's result as b, bf16 multiplies both of its parts into the same sums.
+// With a narrow product's result as b, bf16 multiplies all of its parts into the same sums.
 //
 // Half of the waves stage a, half b, 16 bytes of eight rows a thread: 242 us for 261,766 rows, 128 x 1344 bf16
 // (0.77 GB read, 0.09 GB of slots written), where every wave staging both in 8 bytes took 270. Bound by the
@@ -89,10 +89,11 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         for (int u = 0; u < 8; ++u) {
             if (WIDE) l[0][u] = *reinterpret_cast<const uint4_any *>(from + at[u]);
             else l[0][u] = load_16<T, false>(from + at[u], width - col);
-            if constexpr (P == 2)
-                if (of_b) {
-                    if (WIDE) l[1][u] = *reinterpret_cast<const uint4_any *>(from + at[u] + W);
-                    else l[1][u] = load_16<T, false>(from + at[u] + W, width - col);
+            if (of_b)
+#pragma unroll
+                for (int e = 1; e < P; ++e) {
+                    if (WIDE) l[e][u] = *reinterpret_cast<const uint4_any *>(from + at[u] + e * W);
+                    else l[e][u] = load_16<T, false>(from + at[u] + e * W, width - col);
                 }
         }
     };

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         }
         int kw = WNK ? kx : k + tg * kU;
         const bool in_k = kw < K;
-        if (P == 2 && ext && kw >= W) kw -= W;  // the second part meets the same weights
+        if (ext) kw = narrow_k<T>(kw, W);
         l.wk = in_k ? ld - kw : 0;
         if constexpr (WNK) {
             const int ws = l.wk > 0 ? start8(kw, ld) : 0;
@@ -257,28 +257,33 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         const float scale = p.narrow_scale && grouped ? p.narrow_scale[t.g] : grouped ? 1.f : 0.f;
         const int place = r0 + (lane & 31);
         T *const out = static_cast<T *>(p.h_out) + (t.p0 + place) * (P * W);
-        __syncthreads();  // the last step's tiles are consumed
+        float4_t x[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int col = vec_col<T, false>(v, half);
-            float4_t x = vec_val<T, false>(acc[TX - 1][0], v);
+            x[v] = vec_val<T, false>(acc[TX - 1][0], v);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = grouped && col + e < p.r ? x[e] * scale : 0.f;
-            if (p.h_out && grouped && place < rows && col < W) store_narrow(out + col, W, x);
-            put_narrow<T, BM>(s_rows, v, place, half, W / kU, x, lose);
+            for (int e = 0; e < 4; ++e) x[v][e] = grouped && col + e < p.r ? x[v][e] * scale : 0.f;
+            if (p.h_out && grouped && place < rows && col < W) store_narrow(out + col, W, x[v]);
         }
-        uint4_t u[Q];
-        for (int task = tid; task < BN * KG; task += kThreads) {
-            const int g = task % KG, c = task / KG;
-            int k = g * kU;
-            const bool in_k = k < P * W && c < p.N && grouped;
-            if (P == 2 && k >= W) k -= W;  // the second part meets the same weights
-            const T *const q = static_cast<const T *>(p.v) + ((int64_t)(grouped ? t.g : 0) * p.N + c) * p.r + k;
-            to_units(load_row8<T, false>(q, in_k ? p.r - k : 0), u, lose);
-            put<T, BX>(s_cols, KG, g, c, u);
+        const int most = KG * kU / W;  // parts that a step has room for: all, or two of bf16's three
+        for (int first = 0; first < P; first += most) {
+            const int count = P - first < most ? P - first : most;
+            __syncthreads();  // the last step's tiles are consumed
+#pragma unroll
+            for (int v = 0; v < 4; ++v) put_narrow<T, BM>(s_rows, v, place, half, W / kU, first, count, x[v], lose);
+            uint4_t u[Q];
+            for (int task = tid; task < BN * KG; task += kThreads) {
+                const int g = task % KG, c = task / KG;
+                const bool in_k = g * kU < count * W && c < p.N && grouped;
+                const int k = narrow_k<T>(g * kU, W);
+                const T *const q = static_cast<const T *>(p.v) + ((int64_t)(grouped ? t.g : 0) * p.N + c) * p.r + k;
+                to_units(load_row8<T, false>(q, in_k ? p.r - k : 0), u, lose);
+                put<T, BX>(s_cols, KG, g, c, u);
+            }
+            __syncthreads();
+            step_products<T, BX, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0, 1.f);
         }
-        __syncthreads();
-        step_products<T, BX, BM, TC, TR>(acc, s_cols, s_rows, c0w, r0, 1.f);
     };
     auto step = [&]() {
         __syncthreads();
@@ -358,7 +363,7 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 
 size_t narrow_bytes(int dtype, int64_t n_rows, int N)
 {
-    return (size_t)n_rows * narrow_width(N) * 4;  // one fp32 or two bf16
+    return (size_t)n_rows * narrow_width(N) * (dtype == CGTP_BF16 ? kNarrow<bf16_t> * 2 : 4);
 }
 
 // Adapters of 64 rows on the mean, one column tile of [N][K] weights.

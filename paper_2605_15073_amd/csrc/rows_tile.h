@@ -557,29 +557,40 @@ __device__ __forceinline__ void store_zeros(const RowProduct &p, const int *row,
 }
 
 // Results of narrow products (width N <= 64, between the two products of an adapter), in sequence
-// order: fp32 [n][W], or for bf16 two parts hi + lo [n][2][W], 16 bits of significand; W is N
+// order: fp32 [n][W], or for bf16 three parts [n][3][W], fp32's 24 bits of significand; W is N
 // rounded up to a unit, the rest zero.
 __host__ __device__ constexpr int narrow_width(int N) { return (N + kU - 1) / kU * kU; }
-template <typename T> constexpr int kNarrow = sizeof(T) == 2 ? 2 : 1;
+template <typename T> constexpr int kNarrow = sizeof(T) == 2 ? 3 : 1;
 
-// Values 4 half .. 4 half + 3 of k-group g of a narrow result's row, as operands in a tile of R rows at
-// place r; second: the k-group where bf16's second part begins. k-groups that the result does not reach
-// come as zeros.
+// The three bf16 parts of four values; an infinity or NaN has one.
+__device__ __forceinline__ void narrow_parts(float4_t x, bf4_t (&part)[3])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        part[0][e] = (bf16_t)x[e];
+        const float r = __builtin_isfinite((float)part[0][e]) ? x[e] - (float)part[0][e] : 0.f;
+        part[1][e] = (bf16_t)r;
+        part[2][e] = (bf16_t)(r - (float)part[1][e]);
+    }
+}
+
+// Values 4 half .. 4 half + 3 of k-group g of a narrow result's row of `groups`, as operands in a tile of R rows
+// at place r; of bf16 the parts first .. first + count - 1, each behind the one before. k-groups that they do
+// not reach come as zeros.
 template <typename T, int R>
-__device__ __forceinline__ void put_narrow(uint4_t *tile, int g, int r, int half, int second, float4_t x, bool &lose)
+__device__ __forceinline__ void put_narrow(uint4_t *tile, int g, int r, int half, int groups, int first, int count,
+                                           float4_t x, bool &lose)
 {
     auto at = [&](int group) { return reinterpret_cast<uint2_t *>(tile + group * (R + 1) + r) + half; };
     if constexpr (sizeof(T) == 2) {
-        bf4_t hi, lo;
+        bf4_t part[3];
+        narrow_parts(x, part);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            hi[e] = (bf16_t)x[e];
-            lo[e] = (bf16_t)(__builtin_isfinite((float)hi[e]) ? x[e] - (float)hi[e] : 0.f);
-        }
-        // k-groups 0 .. 7: the first parts, the second ones behind them, zeros
-        const uint2_t h = __builtin_bit_cast(uint2_t, hi), l = __builtin_bit_cast(uint2_t, lo), zero = {0, 0};
-        *at(g < second ? g : 2 * second + 2 * (g - second)) = g < second ? h : zero;
-        *at(g < second ? second + g : 2 * second + 2 * (g - second) + 1) = g < second ? l : zero;
+        for (int e = 0; e < 3; ++e)
+            if (g < groups && e >= first && e < first + count)
+                *at((e - first) * groups + g) = __builtin_bit_cast(uint2_t, part[e]);
+        for (int z = count * groups; z < kGroups<T>; ++z)
+            if (z % 4 == g) *at(z) = uint2_t{0, 0};
     } else {
         float m = 0.f;
         max_abs(m, x[0], x[1]);
@@ -595,10 +606,17 @@ __device__ __forceinline__ void put_narrow(uint4_t *tile, int g, int r, int half
     }
 }
 
+// Where the parts of a narrow result meet the same weights again: k of the parts' row as k of the weights.
+template <typename T> __device__ __forceinline__ int narrow_k(int k, int W)
+{
+    if (kNarrow<T> == 1) return k;
+    return k >= 2 * W ? k - 2 * W : k >= W ? k - W : k;
+}
+
 template <typename T> __device__ __forceinline__ float narrow_at(const void *h, int64_t pos, int W, int k)
 {
     const T *const p = static_cast<const T *>(h) + pos * (kNarrow<T> * W) + k;
-    return sizeof(T) == 2 ? (float)p[0] + (float)p[W] : (float)p[0];
+    return sizeof(T) == 2 ? (float)p[0] + (float)p[W] + (float)p[2 * W] : (float)p[0];
 }
 
 // Waves along the rows of a 128 x 128 tile: fp32 operands, three parts each, are read once a wave where it
@@ -669,15 +687,10 @@ __device__ __forceinline__ void store_narrow(float *p, int W, float4_t v)
 
 __device__ __forceinline__ void store_narrow(bf16_t *p, int W, float4_t v)
 {
-    bf4_t hi, lo;
+    bf4_t part[3];
+    narrow_parts(v, part);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        hi[e] = (bf16_t)v[e];
-        const float h = (float)hi[e];
-        lo[e] = (bf16_t)(__builtin_isfinite(h) ? v[e] - h : 0.f);  // an infinity has no second part
-    }
-    *reinterpret_cast<bf4_t *>(p) = hi;
-    *reinterpret_cast<bf4_t *>(p + W) = lo;
+    for (int e = 0; e < 3; ++e) *reinterpret_cast<bf4_t *>(p + e * W) = part[e];
 }
 
 // Whether rows at this stride start on 16-byte boundaries.

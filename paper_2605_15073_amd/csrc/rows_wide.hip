@@ -45,13 +45,14 @@ constexpr int kRows = 128;    // positions of a workgroup, 32 a wave
 constexpr int kCols = 64;     // columns of a tile
 constexpr int kTilesAtOnce = 256;
 template <typename T> constexpr int kPairs = sizeof(T) == 2 ? 8 : 4;  // pairs of k-groups: up to 128 bf16, 64 fp32
-template <typename T> constexpr int kExtPairs = sizeof(T) == 2 ? 4 : 2;  // of a narrow product's rows, up to 32 wide
+template <typename T> constexpr int kExtPairs = sizeof(T) == 2 ? 6 : 2;  // of a narrow product's rows, up to 32 wide
 
 // The results are turned 64 (bf16) or 32 (fp32) columns at a time, 128 bytes a row. Row stride of the turned
 // results, in values: a multiple of their vectors, clear of bank conflicts between the rows that the 8
-// (fp32, 16 bytes) or 16 (bf16, 8 bytes) lanes of a cycle write.
+// (fp32, 16 bytes) or 16 (bf16, 8 bytes) lanes of a cycle write. XP: of a narrow product that is turned here too.
 template <typename T> constexpr int kPiece = 128 / (int)sizeof(T);
-template <typename T, bool LINES> constexpr int kTurn = (LINES ? 1 : 2) * kPiece<T> + 4;
+template <typename T, bool LINES, int XP>
+constexpr int kTurn = ((LINES ? 1 : 2) * kPiece<T> > 2 * XP * kU ? (LINES ? 1 : 2) * kPiece<T> : 2 * XP * kU) + 4;
 
 template <typename T> struct Out4;
 template <> struct Out4<float> { typedef float4_t t; typedef float4_any any; };
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     typedef typename Out4<T>::t O;
     typedef typename Out4<T>::any O_any;
     __shared__ uint4_t s_w[Q * KG * LD];
-    constexpr int TURN = kTurn<T, LINES>, RING = 2 * kPiece<T>;
+    constexpr int TURN = kTurn<T, LINES, FUSED ? XP : 0>, RING = 2 * kPiece<T>;
     __shared__ O s_turn[4 * 32 * TURN / 4];
     __shared__ int s_row[kRows], s_place[kRows], s_any;
     __shared__ int s_g[EXT ? kRows : 1], s_seg_g[EXT ? kRows : 1], s_seg_at[EXT ? kRows + 1 : 1], s_nseg;
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             if (EXT && g >= 2 * NP) {
                 k = (g - 2 * NP) * U;
                 K = k < P * W && nseg > 0 ? p.r : 0;
-                if (P == 2 && k >= W) k -= W;  // the second part meets the same weights
+                k = narrow_k<T>(k, W);
                 wb = static_cast<const T *>(p.v) + (int64_t)(nseg > 0 ? s_seg_g[seg] : 0) * p.r * p.N;
             }
             have[i] = K - k;
