@@ -22,6 +22,7 @@
 #define CGTP_ROWS_TILE_H
 
 #include "rows.h"
+#include "rows_index.h"
 
 namespace cgtp {
 namespace rows {
@@ -246,9 +247,6 @@ __device__ __forceinline__ Raw8<T> load_row8(const T *p, int64_t left)
 
 // Loads that must not pass the end of a row, and must not be under a condition, start early enough to end
 // with it; the values are moved down by what they started early when they are staged.
-
-// Where the load of eight values from k on starts in a row of K >= 8.
-__device__ __forceinline__ int start8(int k, int K) { return k + 8 <= K ? k : K - 8; }
 
 // Eight values at the alignment of one.
 template <typename T> __device__ __forceinline__ Raw8<T> load_any8(const T *q)

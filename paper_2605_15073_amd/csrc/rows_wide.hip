@@ -42,7 +42,7 @@ namespace {
 using namespace rows;
 
 constexpr int kRows = 128;    // positions of a workgroup, 32 a wave
-constexpr int kCols = 64;     // columns of a tile
+constexpr int kCols = kWideCols;  // columns of a tile
 constexpr int kTilesAtOnce = 256;
 template <typename T> constexpr int kPairs = sizeof(T) == 2 ? 8 : 4;  // pairs of k-groups: up to 128 bf16, 64 fp32
 template <typename T> constexpr int kExtPairs = sizeof(T) == 2 ? 6 : 2;  // of a narrow product's rows, up to 32 wide
@@ -212,18 +212,19 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     // Weights. Round 0 of a column tile: the shared ones, with the first adapter's behind them; then the
     // other adapters' of the tile.
     constexpr int kTasks = (WNK ? kCols : kCols / CW) * KG;  // units, or units of CW columns
-    constexpr int NT = (kTasks + kThreads - 1) / kThreads;
+    constexpr int NT = wide_rounds(kTasks);
+    static_assert(kThreads == kWideThreads, "units of the threads");
     const T *const w = static_cast<const T *>(p.w) + (FUSED ? 0 : (int64_t)t.g * p.w_group);
     Raw8<T> wn[WNK ? NT : 1];
     uint2_t wt[WNK ? 1 : NT][8];
     int early[WNK ? NT : 1];  // what the loads started early
     int have[NT];  // k of the k-groups in flight that the weights have
-    auto first_col = [&](int ct) { return ct * kCols + kCols <= p.N ? ct * kCols : p.N - kCols; };
+    auto first_col = [&](int ct) { return wide_first_col(ct, p.N); };
     auto fetch = [&](int ct, int seg) {
         const int c0 = first_col(ct);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            const int task = tid + kThreads * i;
+            const int task = wide_unit(tid, i, kTasks);
             const int g = WNK ? task % KG : task / (kCols / CW);
             int k = g * U, K = p.K;
             const T *wb = w;
