@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             const int col = vec_col<T, true>(v, half);
             float4_t f = vec_val<T, true>(sum, v);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] *= scale;
+            for (int e = 0; e < 4; ++e) f[e] = col + e < p.r ? f[e] * scale : 0.f;  // an infinite input times nothing is NaN
             if (col < W) store_narrow(mine + col, W, f);
         }
         wave_sync();
