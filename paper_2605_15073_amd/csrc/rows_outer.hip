@@ -60,7 +60,6 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     const int early = WIDE && col < width && col + CW > width ? col + CW - width : 0;
     uint4_t l[P][8];
     unsigned in;  // bit u: row u of the k-group exists
-    bool lose = false;
     float sign = 1.f;  // of the step's a
     const int steps = (int)((t.p1 - t.p0 + BK - 1) / BK);
     // ids of the rows of step s, -1 past the chunk; loads without a condition, as the operands'
@@ -111,7 +110,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                 for (int r = 0; r < 8; ++r) l[e][r] = in >> r & 1 ? l[e][r] : uint4_t{0, 0, 0, 0};
             }
             uint4_t u[CW][Q];
-            to_units(l[e], u, lose, of_b ? 1.f : sign);
+            to_units(l[e], u, of_b ? 1.f : sign);
 #pragma unroll
             for (int j = 0; j < CW; ++j) {
                 if (of_b) put<T, BN>(s_cols[e], KG, kg, place_full<T>(first + j), u[j]);
@@ -151,26 +150,6 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     const int64_t slot = 2 * (int64_t)R.of((int)t.start) + R.of((int)(t.p0 - t.start));
     T *const out = static_cast<T *>(q.out) + t.g * cells;
     float *const part = slots + (whole ? 0 : slot * cells);
-    if constexpr (Q > 1) {
-        if (__syncthreads_or(lose)) {  // values outside the range of parts: plain fp32 sums
-            const int na = q.A - a0 < BM ? q.A - a0 : BM, nb = B - b0 < BN ? B - b0 : BN;
-            for (int e = tid; e < na * nb; e += kThreads) {
-                const int i = a0 + e / nb, c = b0 + e % nb;
-                float sum = 0.f;
-                for (int64_t pos = t.p0; pos < t.p1; ++pos) {
-                    const int row = row_at(o, pos);
-                    if (row < 0) continue;
-                    const float y = NARROW ? narrow_at<float>(q.h, pos, W, c)
-                                           : static_cast<const float *>(q.b)[row * q.b_stride + c];
-                    sum += static_cast<const float *>(q.a)[row * q.a_stride + i] * y;
-                }
-                const int64_t at = q.transposed ? (int64_t)c * q.A + i : (int64_t)i * B + c;
-                if (whole) out[at] = (T)sum;
-                else part[at] = sum;
-            }
-            return;
-        }
-    }
 #pragma unroll
     for (int r = 0; r < TR; ++r) {
         const int i = a0 + lane_of_full<T>(r0 + 32 * r + (lane & 31));
@@ -195,6 +174,32 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                     else store_four<false>(part + at, x, B - col);
                 }
             }
+    }
+    if constexpr (Q > 1) {
+        float odd = 0.f;
+#pragma unroll
+        for (int c = 0; c < TC; ++c)
+#pragma unroll
+            for (int r = 0; r < TR; ++r) probe(odd, acc[c][r]);
+        if (!__syncthreads_or(odd != odd)) return;
+        // the sums that are not finite, in plain fp32
+        stores_done();
+        const int na = q.A - a0 < BM ? q.A - a0 : BM, nb = B - b0 < BN ? B - b0 : BN;
+        for (int e = tid; e < na * nb; e += kThreads) {
+            const int i = a0 + e / nb, c = b0 + e % nb;
+            const int64_t at = q.transposed ? (int64_t)c * q.A + i : (int64_t)i * B + c;
+            if (__builtin_isfinite(whole ? stored(out + at) : stored(part + at))) continue;
+            float sum = 0.f;
+            for (int64_t pos = t.p0; pos < t.p1; ++pos) {
+                const int row = row_at(o, pos);
+                if (row < 0) continue;
+                const float y = NARROW ? narrow_at<float>(q.h, pos, W, c)
+                                       : static_cast<const float *>(q.b)[row * q.b_stride + c];
+                sum += static_cast<const float *>(q.a)[row * q.a_stride + i] * y;
+            }
+            if (whole) out[at] = (T)sum;
+            else part[at] = sum;
+        }
     }
 }
 

@@ -111,9 +111,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         int xk, wk;  // values that exist of this thread's k-group of rows and weights
         int xe, we;  // what their loads started early
         unsigned rows;  // bit i: x[i] is of a row that takes part
-        bool ext;  // the step is of an adapter
     } l;
-    bool lose = false;
+    float odd = 0.f;  // NaN once a result is not finite
     float sign = 1.f;  // of the step's rows
     auto fetch = [&]() {
         if (!WIDE && next.ct >= ct1) return;  // else past the last step the last tile's first loads again
@@ -133,7 +132,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         const int xs = l.xk > 0 ? start8(kx, K) : 0;
         l.xe = l.xk > 0 ? kx - xs : 0;
         l.rows = 0;
-        l.ext = ext;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int r = rr + kLanes * i;
@@ -175,7 +173,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         for (int i = 0; i < NR; ++i) {
             if (BM < kLanes && rr >= BM) break;
             if (l.xk < kU || !(l.rows >> i & 1)) settle(l.x[i], WIDE ? l.xe : 0, l.rows >> i & 1 ? l.xk : 0);
-            to_units(l.x[i], u, lose, sign);
+            to_units(l.x[i], u, sign);
             put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
         }
         if constexpr (WNK) {
@@ -183,8 +181,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
             for (int i = 0; i < NC; ++i) {
                 if (BX % kLanes != 0 && rr + kLanes * i >= BX) break;
                 if (l.wk < kU) settle(l.wn[i], WIDE ? l.we : 0, l.wk);
-                if (!FUSED && l.ext) lose |= non_finite<T>(l.wn[i]);
-                to_units(l.wn[i], u, lose);
+                to_units(l.wn[i], u);
                 put<T, BX>(s_cols, KG, kg, rr + kLanes * i, u);
             }
         } else if (has_w) {
@@ -196,9 +193,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
 #pragma unroll
                 for (int e = 0; e < 8; ++e) settle<T>(l.wt[e], l.we);
             }
-            if (!FUSED && l.ext) lose |= non_finite<T>(l.wt);
             uint4_t c[CW][Q];
-            to_units(l.wt, c, lose);
+            to_units(l.wt, c);
 #pragma unroll
             for (int j = 0; j < CW; ++j) put<T, BX>(s_cols, KG, tg, place<T>(CW * tc + j), c[j]);
         }
@@ -271,14 +267,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
             const int count = P - first < most ? P - first : most;
             __syncthreads();  // the last step's tiles are consumed
 #pragma unroll
-            for (int v = 0; v < 4; ++v) put_narrow<T, BM>(s_rows, v, place, half, W / kU, first, count, x[v], lose);
+            for (int v = 0; v < 4; ++v) put_narrow<T, BM>(s_rows, v, place, half, W / kU, first, count, x[v]);
             uint4_t u[Q];
             for (int task = tid; task < BN * KG; task += kThreads) {
                 const int g = task % KG, c = task / KG;
                 const bool in_k = g * kU < count * W && c < p.N && grouped;
                 const int k = narrow_k<T>(g * kU, W);
                 const T *const q = static_cast<const T *>(p.v) + ((int64_t)(grouped ? t.g : 0) * p.N + c) * p.r + k;
-                to_units(load_row8<T, false>(q, in_k ? p.r - k : 0), u, lose);
+                to_units(load_row8<T, false>(q, in_k ? p.r - k : 0), u);
                 put<T, BX>(s_cols, KG, g, c, u);
             }
             __syncthreads();
@@ -297,6 +293,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         if (now.ct != ct) {
             if constexpr (FUSED) narrow_step();
             store(ct);
+            if (Q > 1 || nseg > 0)
+#pragma unroll
+                for (int c = 0; c < TC; ++c)
+#pragma unroll
+                    for (int r = 0; r < TR; ++r) probe(odd, acc[c][r]);
             clear();
         }
     };
@@ -304,9 +305,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     fetch();
     while (now.ct < ct1) step();
     if constexpr (Q > 1 || !FUSED) {
-        if ((Q > 1 || nseg > 0) && __syncthreads_or(lose)) {
+        if ((Q > 1 || nseg > 0) && __syncthreads_or(odd != odd)) {
             float *const h = FUSED ? reinterpret_cast<float *>(s_cols) : nullptr;
             if constexpr (FUSED) {
+                stores_done();
                 static_assert(sizeof(s_cols) >= sizeof(float) * BM * 32, "rows of up to 32 values");
                 for (int e = tid; e < rows * p.r; e += kThreads) {
                     const int r = e / p.r, c = e % p.r;
@@ -317,7 +319,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
                                    reinterpret_cast<const float *>(narrow_w)[(int64_t)c * p.K + k];
                     if (p.narrow_scale && grouped) sum *= p.narrow_scale[t.g];
                     h[32 * r + c] = sum;
-                    if (p.h_out && grouped) static_cast<float *>(p.h_out)[(t.p0 + r) * W + c] = sum;
+                    float *const out = static_cast<float *>(p.h_out) + (t.p0 + r) * W + c;
+                    if (p.h_out && grouped && !__builtin_isfinite(stored(out))) *out = sum;
                 }
                 if (tid < rows) s_g[tid] = t.g;
             }

@@ -6,12 +6,14 @@
 // lanes of a matrix instruction's half read consecutive units and the eight lanes that stage one row's
 // units hit different banks.
 //
-// fp32 operands are three bf16 parts each, x = h + m + l (24 bits of significand), and a product is hh,
+// fp32 operands are three bf16 parts each, 2^16 x = h + m + l (24 bits of significand), and a product is hh,
 // hm, mh, mm, hl, lh, summed in fp32: six matrix instructions for 16 k, where the fp32 ones take eight
-// of twice the time; what is left out is below 2^-24 of the term. The parts are exact where the third is
-// no smaller than bf16's smallest step, 2^-133, so from 2^-109 on, and up to bf16's largest value; an
-// infinity has none. A workgroup that meets eight values that all lose bits, or one above the range
-// (parts_lose), forms its sums again in plain fp32.
+// of twice the time; what is left out is below 2^-24 of the term. 2^16 x is a multiple of 2^-133, bf16's smallest
+// step, so that the parts hold every x up to 2^112 whole, however small, beside whatever others. Sums beyond
+// 2^96, larger inputs, infinities and NaN leave results that are not finite, and so do an adapter's weights that
+// are not, which rows of other adapters in a tile meet as zeros. Those results, and no others, are formed again in
+// plain fp32, one result a thread at a time. 131,072 rows, 64 -> 896, 8 groups: y 121 us, with one infinite input
+// 370, with one in every 128 rows 778; all gradients 382, 2,990 and 5,580 us (a cell of dw runs over its chunk's rows).
 //
 // Operands whose k is contiguous in memory are staged eight k a load. The others (weights of the
 // forward product, both operands of a weight gradient) are loaded 8 or 16 bytes wide (kWide, kFull lanes), 8
@@ -285,24 +287,14 @@ template <typename T> __device__ __forceinline__ void settle(uint2_t &v, int ear
     }
 }
 
-// The largest of m, |a| and |b| (fmaxf would first quieten each operand, an instruction of its own).
-__device__ __forceinline__ void max_abs(float &m, float a, float b)
-{
-    asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(m) : "v"(a), "v"(b));
-}
-
-// Whether parts lose bits of values whose largest magnitude is m (a maximum that skips NaN, which parts
-// propagate): all of them below the range (one inside dwarfs what the others lose, 2^-134 each), or one
-// above it.
-__device__ __forceinline__ bool parts_lose(float m) { return (m < 0x1p-104f && m != 0.f) || m > 0x1.fep127f; }
+// Of fp32 operands as parts, and of the sums of their products.
+constexpr float kUp = 0x1p16f, kDown = 0x1p-32f;
 
 // The three parts of eight values.
-__device__ __forceinline__ void split8(const float (&x)[8], uint4_t (&part)[3], bool &lose)
+__device__ __forceinline__ void split8(const float (&x)[8], uint4_t (&part)[3])
 {
-    float m = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        max_abs(m, x[2 * k], x[2 * k + 1]);
         float r0 = x[2 * k], r1 = x[2 * k + 1];
 #pragma unroll
         for (int c = 0; c < 3; ++c) {
@@ -313,24 +305,30 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4_t (&part)[3], 
             r1 -= __builtin_bit_cast(float, bits & 0xffff0000u);
         }
     }
-    lose |= parts_lose(m);
+}
+
+// Adds NaN to `odd` if one of the sums is not finite, else zero.
+__device__ __forceinline__ void probe(float &odd, const float16_t &sum)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) odd = fmaf(sum[i], 0.f, odd);
 }
 
 // The units of a lane's eight k; of fp32 times sign, 1 or -1.
-__device__ __forceinline__ void to_units(const Raw8<bf16_t> &raw, uint4_t (&u)[1], bool &, float = 1.f)
+__device__ __forceinline__ void to_units(const Raw8<bf16_t> &raw, uint4_t (&u)[1], float = 1.f)
 {
     u[0] = raw.v[0];
 }
-__device__ __forceinline__ void to_units(const Raw8<float> &raw, uint4_t (&u)[3], bool &lose, float sign = 1.f)
+__device__ __forceinline__ void to_units(const Raw8<float> &raw, uint4_t (&u)[3], float sign = 1.f)
 {
     float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = sign * __builtin_bit_cast(float, (unsigned)raw.v[e / 4][e % 4]);
-    split8(x, u, lose);
+    for (int e = 0; e < 8; ++e) x[e] = sign * kUp * __builtin_bit_cast(float, (unsigned)raw.v[e / 4][e % 4]);
+    split8(x, u);
 }
 
 // The units of kWide lanes from 8 loads of 8 bytes.
-__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[4][1], bool &, float = 1.f)
+__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[4][1], float = 1.f)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -340,14 +338,14 @@ __device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[4]
                                                (j & 1) ? 0x07060302u : 0x05040100u);
 }
 
-__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[2][3], bool &lose, float sign = 1.f)
+__device__ __forceinline__ void to_units(const uint2_t (&in)[8], uint4_t (&u)[2][3], float sign = 1.f)
 {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = sign * __builtin_bit_cast(float, (unsigned)in[e][j]);
-        split8(x, u[j], lose);
+        for (int e = 0; e < 8; ++e) x[e] = sign * kUp * __builtin_bit_cast(float, (unsigned)in[e][j]);
+        split8(x, u[j]);
     }
 }
 
@@ -370,7 +368,7 @@ template <typename T> __device__ __forceinline__ int place(int r)
 // wave exchanged, so that neighbouring threads and blocks write to different banks.
 template <typename T> constexpr int kFull = 16 / (int)sizeof(T);
 
-__device__ __forceinline__ void to_units(const uint4_t (&in)[8], uint4_t (&u)[8][1], bool &, float = 1.f)
+__device__ __forceinline__ void to_units(const uint4_t (&in)[8], uint4_t (&u)[8][1], float = 1.f)
 {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -380,14 +378,14 @@ __device__ __forceinline__ void to_units(const uint4_t (&in)[8], uint4_t (&u)[8]
                                                (j & 1) ? 0x07060302u : 0x05040100u);
 }
 
-__device__ __forceinline__ void to_units(const uint4_t (&in)[8], uint4_t (&u)[4][3], bool &lose, float sign = 1.f)
+__device__ __forceinline__ void to_units(const uint4_t (&in)[8], uint4_t (&u)[4][3], float sign = 1.f)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = sign * __builtin_bit_cast(float, (unsigned)in[e][j]);
-        split8(x, u[j], lose);
+        for (int e = 0; e < 8; ++e) x[e] = sign * kUp * __builtin_bit_cast(float, (unsigned)in[e][j]);
+        split8(x, u[j]);
     }
 }
 
@@ -490,7 +488,7 @@ __device__ __forceinline__ void step_products(float16_t (&acc)[TX][TR], const ui
                     mma(sum, a, b[s]);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[c][r][i] = fmaf(sign, sum[i], acc[c][r][i]);
+                for (int i = 0; i < 16; ++i) acc[c][r][i] = fmaf(sign * kDown, sum[i], acc[c][r][i]);
             }
         }
     }
@@ -577,7 +575,7 @@ __device__ __forceinline__ void narrow_parts(float4_t x, bf4_t (&part)[3])
 // not reach come as zeros.
 template <typename T, int R>
 __device__ __forceinline__ void put_narrow(uint4_t *tile, int g, int r, int half, int groups, int first, int count,
-                                           float4_t x, bool &lose)
+                                           float4_t x)
 {
     auto at = [&](int group) { return reinterpret_cast<uint2_t *>(tile + group * (R + 1) + r) + half; };
     if constexpr (sizeof(T) == 2) {
@@ -590,10 +588,7 @@ __device__ __forceinline__ void put_narrow(uint4_t *tile, int g, int r, int half
         for (int z = count * groups; z < kGroups<T>; ++z)
             if (z % 4 == g) *at(z) = uint2_t{0, 0};
     } else {
-        float m = 0.f;
-        max_abs(m, x[0], x[1]);
-        max_abs(m, x[2], x[3]);
-        lose |= parts_lose(m);
+        x *= kUp;
 #pragma unroll
         for (int c = 0; c < 3; ++c) {
             const bf4_t b = {(bf16_t)x[0], (bf16_t)x[1], (bf16_t)x[2], (bf16_t)x[3]};
@@ -621,46 +616,41 @@ template <typename T> __device__ __forceinline__ float narrow_at(const void *h, 
 // has rows of its own.
 template <typename T> constexpr int kWaveRows = sizeof(T) == 2 ? 2 : 4;
 
-// Whether one of these weights is infinite or NaN. A tile's rows of other adapters meet those of one adapter as
-// zeros, and zero times such a weight is NaN: a workgroup that finds one forms its sums row by row.
-template <typename T> __device__ __forceinline__ unsigned raised(unsigned v)
+// A result that this workgroup has stored, past the caches that other workgroups' stores do not reach.
+__device__ __forceinline__ float stored(const float *p)
 {
-    // the sign of each value's place is set where its exponent is full: it is clear after the mask
-    return sizeof(T) == 4 ? (v & 0x7fffffffu) + 0x00800000u : ((v & 0x7fff7fffu) + 0x00800080u);
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-template <typename T> constexpr unsigned kSigns = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
-
-template <typename T> __device__ __forceinline__ bool non_finite(const Raw8<T> &r)
+__device__ __forceinline__ float stored(const bf16_t *p)
 {
-    unsigned m = 0;
-#pragma unroll
-    for (int e = 0; e < 2 * (int)sizeof(T); ++e) m |= raised<T>(r.v[e / 4][e % 4]);
-    return m & kSigns<T>;
+    const unsigned short bits = __hip_atomic_load(reinterpret_cast<const unsigned short *>(p), __ATOMIC_RELAXED,
+                                                  __HIP_MEMORY_SCOPE_AGENT);
+    return __builtin_bit_cast(float, (unsigned)bits << 16);
 }
 
-template <typename T> __device__ __forceinline__ bool non_finite(const uint2_t (&in)[8])
+// Every wave's stores are done: what follows reads and replaces some of them.
+__device__ __forceinline__ void stores_done()
 {
-    unsigned m = 0;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) m |= raised<T>(in[e / 2][e % 2]);
-    return m & kSigns<T>;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
 }
 
-// The sums of a workgroup that met values outside the range of parts or an adapter's non-finite ones, in plain
-// fp32: columns [c0, c1) of its rows, one result a thread at a time. h: the narrow product's rows in LDS, 32
-// apart, in place of p.h.
+// The results of a workgroup that are not finite, in the columns [c0, c1) of its rows, in plain fp32. h: the
+// narrow product's rows in LDS, 32 apart, in place of p.h.
 template <typename T, bool WNK>
 __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group, int64_t p0, int rows, const int *s_row,
                                const int *s_g, int c0, int c1, const float *h = nullptr)
 {
-    // every wave's stores of these columns are done before they are stored again
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    stores_done();
     const int W = narrow_width(p.r), width = c1 - c0;
     const T *const w = static_cast<const T *>(p.w) + (int64_t)group * p.w_group;
     for (int e = threadIdx.x; e < rows * width; e += kThreads) {
         const int r = e / width, c = c0 + e % width;
         if (s_row[r] < 0) continue;
+        float *const narrow_out = static_cast<float *>(p.out) + (p0 + r) * narrow_width(p.N) + c;  // fp32 alone
+        T *const out = static_cast<T *>(p.out) + s_row[r] * p.out_stride + c;
+        const bool narrow = sizeof(T) == 4 && p.narrow;
+        if (__builtin_isfinite(narrow ? stored(narrow_out) : stored(out))) continue;
         const T *const in = static_cast<const T *>(p.in) + s_row[r] * p.in_stride;
         float sum = 0.f;
         for (int k = 0; k < p.K; ++k) sum += (float)in[k] * (float)w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c];
@@ -670,11 +660,8 @@ __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group
                 sum += (h ? h[32 * r + k] : narrow_at<T>(p.h, p0 + r, W, k)) *
                        (float)v[WNK ? (int64_t)c * p.r + k : (int64_t)k * p.N + c];
         }
-        if (sizeof(T) == 4 && p.narrow)  // bf16: not of narrow products, which have no adapters
-            static_cast<float *>(p.out)[(p0 + r) * narrow_width(p.N) + c] =
-                p.narrow_scale ? sum * p.narrow_scale[group] : sum;
-        else
-            static_cast<T *>(p.out)[s_row[r] * p.out_stride + c] = (T)sum;
+        if (narrow) *narrow_out = p.narrow_scale ? sum * p.narrow_scale[group] : sum;
+        else *out = (T)sum;
     }
 }
 

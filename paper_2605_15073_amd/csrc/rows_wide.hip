@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     // fp32: the matrix instruction rounds down, so the second half of the k is summed negated (step_products)
     constexpr int kPlus = Q > 1 && NP > 1 ? NP / 2 : NP;
     constexpr float kSign = kPlus < NP ? -1.f : 1.f;  // of the adapters' products and of the result
+    constexpr float kOut = Q > 1 ? kSign * kDown : kSign;
     static_assert(NP <= kPairs<T> && !(EXT && WNK), "adapters: [K][N] weights");
     typedef typename Out4<T>::t O;
     typedef typename Out4<T>::any O_any;
@@ -137,11 +138,11 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     const T *const in = static_cast<const T *>(p.in) + s_row[pl] * p.in_stride;
     const int W = EXT ? narrow_width(p.r) : 0;
     uint4_t x[NP][Q], h[EXT ? XP : 1][Q];
-    bool lose = false;
+    float odd = 0.f;  // NaN once a result is not finite
 #pragma unroll
     for (int s = 0; s < NP; ++s) {
         const int k = (2 * s + half) * U;
-        to_units(load_row8<T, false>(in + k, p.K - k), x[s], lose, s < kPlus ? 1.f : -1.f);
+        to_units(load_row8<T, false>(in + k, p.K - k), x[s], s < kPlus ? 1.f : -1.f);
     }
     O *const turn = s_turn + wave * (32 * TURN / 4);
     if constexpr (FUSED) {
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             for (int u = 0; u < U; ++u)
                 in[u] = load_8<T, false>(q + (int64_t)u * p.r, nseg && g * U + u < p.K ? p.r - c : 0);
             uint4_t unit[CW][Q];
-            to_units(in, unit, lose);
+            to_units(in, unit);
 #pragma unroll
             for (int j = 0; j < CW; ++j) put<T, kCols>(s_w, KG, g, place<T>(c + j), unit[j]);
         }
@@ -173,21 +174,21 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 for (int i = 0; i < 16; ++i) sum[i] = -sum[i];
             mma(sum, c, x[s]);
         }
-        const float scale = kSign * (p.narrow_scale && nseg ? p.narrow_scale[t.g] : 1.f);
+        const float scale = p.narrow_scale && nseg ? p.narrow_scale[t.g] : 1.f;
         T *const mine = reinterpret_cast<T *>(turn) + (lane & 31) * TURN;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int col = vec_col<T, true>(v, half);
             float4_t f = vec_val<T, true>(sum, v);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = col + e < p.r ? f[e] * scale : 0.f;  // an infinite input times nothing is NaN
+            for (int e = 0; e < 4; ++e) f[e] = col + e < p.r ? f[e] * kOut * scale : 0.f;  // an infinite input times nothing is NaN
             if (col < W) store_narrow(mine + col, W, f);
         }
         wave_sync();
 #pragma unroll
         for (int s = 0; s < XP; ++s) {
             const int k = (2 * s + half) * U;
-            to_units(load_row8<T, false>(mine + k, P * W - k), h[s], lose, kSign);
+            to_units(load_row8<T, false>(mine + k, P * W - k), h[s], kSign);
         }
         wave_sync();
     } else if (EXT) {
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         for (int s = 0; s < XP; ++s) {
             const int k = (2 * s + half) * U;
             const T *const q = static_cast<const T *>(p.h) + (grouped ? (t.p0 + pl) * (P * W) : 0) + k;
-            to_units(load_row8<T, true>(q, grouped ? P * W - k : 0), h[s], lose, kSign);
+            to_units(load_row8<T, true>(q, grouped ? P * W - k : 0), h[s], kSign);
         }
     }
     // outputs: of a piece of 128 bytes this lane stores vector lane % kVecs of rows 64 / kVecs i + lane / kVecs
@@ -258,15 +259,14 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 uint4_t unit[Q];
                 Raw8<T> raw = wn[i];
                 if (have[i] < kU) settle(raw, early[i], have[i]);
-                to_units(raw, unit, lose);
+                to_units(raw, unit);
                 put<T, kCols>(s_w, KG, task % KG, task / KG, unit);
             } else {
                 uint2_t in[8];
 #pragma unroll
                 for (int u = 0; u < U; ++u) in[u] = u < have[i] ? wt[i][u] : uint2_t{0, 0};
-                if (EXT && !FUSED && task / (kCols / CW) >= 2 * NP) lose |= non_finite<T>(in);
                 uint4_t unit[CW][Q];
-                to_units(in, unit, lose);
+                to_units(in, unit);
 #pragma unroll
                 for (int j = 0; j < CW; ++j)
                     put<T, kCols>(s_w, KG, task / (kCols / CW), place<T>(CW * (task % (kCols / CW)) + j), unit[j]);
@@ -325,6 +325,9 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
             }
         }
+        if (Q > 1 || (EXT && !FUSED))
+#pragma unroll
+            for (int c = 0; c < 2; ++c) probe(odd, acc[c]);
         // rows of 128 bytes, several a store
 #pragma unroll
         for (int piece = 0; piece < kCols; piece += kPiece<T>) {
@@ -333,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             for (int c = 0; c < kPiece<T> / 32; ++c)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const float4_t f = kSign * vec_val<T, !WNK>(acc[piece / 32 + c], v);
+                    const float4_t f = kOut * vec_val<T, !WNK>(acc[piece / 32 + c], v);
                     const int col = 32 * c + vec_col<T, !WNK>(v, half);
                     if (LINES) convert(f, turn[((lane & 31) * TURN + col) / 4]);
                     else if (WHOLE) convert(f, turn[((lane & 31) * TURN + (my_at + first + col) % RING) / 4]);
@@ -385,7 +388,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     }
     if constexpr (Q > 1 || (EXT && !FUSED)) {
         const int end = ct1 * kCols < p.N ? ct1 * kCols : p.N;
-        if (__syncthreads_or(lose)) {
+        if (__syncthreads_or(odd != odd)) {
             float *const plain_h = FUSED ? reinterpret_cast<float *>(s_turn) : nullptr;
             if constexpr (FUSED) {
                 static_assert(sizeof(s_turn) >= sizeof(float) * kRows * 32, "rows of up to 32 values");
