@@ -384,10 +384,9 @@ int cgtp_plan_set_receiver_order(cgtp_plan plan, int64_t n_nodes, const int32_t 
  * evaluated with. They need no plan. Conventions beyond those at the top of this file:
  *  - dtype is CGTP_F32 or CGTP_BF16 for every tensor of values, unless noted. Sums are held in fp32
  *    and rounded once, to the output's type. Products of fp32 operands leave out less than 2^-24 of
- *    a term; infinities, NaN and values of any magnitude are treated as fp32 arithmetic does, but for
- *    an infinite adapter weight in bf16, which may give NaN for the rows of its own adapter where fp32
- *    sums would give infinity. What is not finite in one group reaches no row of another. fp32 results
- *    whose sums pass 2^96 or are not finite are formed a second time, one by one: correct, but slow.
+ *    a term; infinities, NaN and values of any magnitude are treated as fp32 arithmetic does. What is
+ *    not finite in one group reaches no row of another. Results that are not finite, and fp32 ones
+ *    whose sums pass 2^96, are formed a second time, one by one: correct, but slow.
  *  - x, y, dx, dy are rows: element (i, c) at [i * stride + c], stride >= width. Other tensors are
  *    contiguous. Any width, stride and alignment of the element works; widths and strides that
  *    are multiples of 64 bytes with pointers on 64-byte boundaries are the fastest, of 16 the next.

@@ -175,14 +175,14 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                 }
             }
     }
-    if constexpr (Q > 1) {
+    if constexpr (Q > 1 || NARROW) {
         float odd = 0.f;
 #pragma unroll
         for (int c = 0; c < TC; ++c)
 #pragma unroll
             for (int r = 0; r < TR; ++r) probe(odd, acc[c][r]);
         if (!__syncthreads_or(odd != odd)) return;
-        // the sums that are not finite, in plain fp32
+        // the sums that are not finite, in plain fp32 (bf16: an infinity times the parts of a narrow result may be NaN)
         stores_done();
         const int na = q.A - a0 < BM ? q.A - a0 : BM, nb = B - b0 < BN ? B - b0 : BN;
         for (int e = tid; e < na * nb; e += kThreads) {
@@ -193,9 +193,9 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             for (int64_t pos = t.p0; pos < t.p1; ++pos) {
                 const int row = row_at(o, pos);
                 if (row < 0) continue;
-                const float y = NARROW ? narrow_at<float>(q.h, pos, W, c)
-                                       : static_cast<const float *>(q.b)[row * q.b_stride + c];
-                sum += static_cast<const float *>(q.a)[row * q.a_stride + i] * y;
+                const float y = NARROW ? narrow_at<T>(q.h, pos, W, c)
+                                       : (float)static_cast<const T *>(q.b)[row * q.b_stride + c];
+                sum += (float)static_cast<const T *>(q.a)[row * q.a_stride + i] * y;
             }
             if (whole) out[at] = (T)sum;
             else part[at] = sum;

@@ -42,7 +42,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     constexpr int kLanes = kThreads / KG;              // rows staged at once
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
     constexpr int NC = (BX + kLanes - 1) / kLanes;
-    __shared__ uint4_t s_cols[kTile<T, BX>], s_rows[kTile<T, BM>];
+    __shared__ uint4_t s_tiles[kTile<T, BX> + kTile<T, BM>];
+    uint4_t *const s_cols = s_tiles, *const s_rows = s_tiles + kTile<T, BX>;
     __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg;
 
     const bool shared_w = !FUSED && p.w_group == 0;
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         if (now.ct != ct) {
             if constexpr (FUSED) narrow_step();
             store(ct);
-            if (Q > 1 || nseg > 0)
+            if (Q > 1 || FUSED || nseg > 0)
 #pragma unroll
                 for (int c = 0; c < TC; ++c)
 #pragma unroll
@@ -304,28 +305,28 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     clear();
     fetch();
     while (now.ct < ct1) step();
-    if constexpr (Q > 1 || !FUSED) {
-        if ((Q > 1 || nseg > 0) && __syncthreads_or(odd != odd)) {
-            float *const h = FUSED ? reinterpret_cast<float *>(s_cols) : nullptr;
-            if constexpr (FUSED) {
-                stores_done();
-                static_assert(sizeof(s_cols) >= sizeof(float) * BM * 32, "rows of up to 32 values");
-                for (int e = tid; e < rows * p.r; e += kThreads) {
-                    const int r = e / p.r, c = e % p.r;
-                    float sum = 0.f;
-                    if (grouped && s_row[r] >= 0)
-                        for (int k = 0; k < p.K; ++k)
-                            sum += reinterpret_cast<const float *>(p.in)[s_row[r] * p.in_stride + k] *
-                                   reinterpret_cast<const float *>(narrow_w)[(int64_t)c * p.K + k];
-                    if (p.narrow_scale && grouped) sum *= p.narrow_scale[t.g];
-                    h[32 * r + c] = sum;
+    if ((Q > 1 || FUSED || nseg > 0) && __syncthreads_or(odd != odd)) {
+        float *const h = FUSED ? reinterpret_cast<float *>(s_tiles) : nullptr;
+        if constexpr (FUSED) {
+            stores_done();
+            static_assert(sizeof(s_tiles) >= sizeof(float) * BM * 32, "rows of up to 32 values");
+            for (int e = tid; e < rows * p.r; e += kThreads) {
+                const int r = e / p.r, c = e % p.r;
+                float sum = 0.f;
+                if (grouped && s_row[r] >= 0)
+                    for (int k = 0; k < p.K; ++k)
+                        sum += (float)static_cast<const T *>(p.in)[s_row[r] * p.in_stride + k] *
+                               (float)narrow_w[(int64_t)c * p.K + k];
+                if (p.narrow_scale && grouped) sum *= p.narrow_scale[t.g];
+                h[32 * r + c] = sum;
+                if constexpr (Q > 1) {  // sums of bf16 products are right as they are
                     float *const out = static_cast<float *>(p.h_out) + (t.p0 + r) * W + c;
                     if (p.h_out && grouped && !__builtin_isfinite(stored(out))) *out = sum;
                 }
-                if (tid < rows) s_g[tid] = t.g;
             }
-            row_plain_sums<T, WNK>(o, p, FUSED ? 0 : t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end, h);
+            if (tid < rows) s_g[tid] = t.g;
         }
+        row_plain_sums<T, WNK>(o, p, FUSED ? 0 : t.g, t.p0, rows, s_row, s_g, ct0 * BN, col_end, h);
     }
 }
 

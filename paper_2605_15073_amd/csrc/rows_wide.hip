@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
             }
         }
-        if (Q > 1 || (EXT && !FUSED))
+        if (Q > 1 || EXT)
 #pragma unroll
             for (int c = 0; c < 2; ++c) probe(odd, acc[c]);
         // rows of 128 bytes, several a store
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             wave_sync();
         }
     }
-    if constexpr (Q > 1 || (EXT && !FUSED)) {
+    if constexpr (Q > 1 || EXT) {
         const int end = ct1 * kCols < p.N ? ct1 * kCols : p.N;
         if (__syncthreads_or(odd != odd)) {
             float *const plain_h = FUSED ? reinterpret_cast<float *>(s_turn) : nullptr;
@@ -394,11 +394,11 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 static_assert(sizeof(s_turn) >= sizeof(float) * kRows * 32, "rows of up to 32 values");
                 for (int e = tid; e < rows * p.r; e += kThreads) {
                     const int r = e / p.r, c = e % p.r;
-                    const float *const ac = reinterpret_cast<const float *>(p.a) + (int64_t)(nseg ? t.g : 0) * p.K * p.r + c;
+                    const T *const ac = static_cast<const T *>(p.a) + (int64_t)(nseg ? t.g : 0) * p.K * p.r + c;
                     float sum = 0.f;
                     if (nseg && s_row[r] >= 0)
                         for (int k = 0; k < p.K; ++k)
-                            sum += reinterpret_cast<const float *>(p.in)[s_row[r] * p.in_stride + k] * ac[(int64_t)k * p.r];
+                            sum += (float)static_cast<const T *>(p.in)[s_row[r] * p.in_stride + k] * (float)ac[(int64_t)k * p.r];
                     plain_h[32 * r + c] = p.narrow_scale && nseg ? sum * p.narrow_scale[t.g] : sum;
                 }
                 if (tid < rows) s_g[tid] = t.g;

@@ -180,3 +180,46 @@ def test_fp32_infinite_row_leaves_other_bits(cg, n, G, n_in, n_out):
     keep = np.arange(n_in) != 3, np.arange(n_out) != 5
     mine = int(ids[0])
     assert (dw[mine][keep[0]][:, keep[1]] == clean[2][mine][keep[0]][:, keep[1]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,G,n_in,n_out,r", [(300, 2, 64, 128, 4), (300, 2, 40, 131, 20), (300, 80, 64, 128, 8),
+                                              (300, 2, 140, 72, 16), (300, 2, 100, 200, 12), (300, 2, 72, 140, 40)])
+def test_adapter_infinite_weights_and_gradients(cg, dtype, n, G, n_in, n_out, r):
+    """An infinite weight of an adapter, or an infinite row, among values of one sign: infinities, as fp32 sums
+    give, and no NaN; other adapters' rows and gradients as without it."""
+    rng = np.random.default_rng([n, n_in, r])
+    x, w, a, b, dy, _ = (rounded(np.abs(t) + 2.0 ** -10, dtype) for t in _adapters(rng, n, G, n_in, n_out, r, dtype))
+    ids = draw_ids(rng, n, G, "even")
+    offsets, order = cg.group_rows(dev(ids), G)
+    one = np.ones(G)
+    mine, D = ids == ids[0], lambda *s: [dev(t, dtype) for t in s]
+    put = lambda t, *at: (lambda c: (c.__setitem__(at, np.inf), c)[1])(t.copy())
+
+    want, bound = ref.adapter(x, w, a, b, one, ids, dtype)
+    wants = ref.adapter_grad(x, w, a, b, dy, one, ids, dtype)
+
+    def near(got, exp, where):
+        got = host(got)
+        assert np.all(np.abs(got - exp[0])[where] <= exp[1][where])
+
+    inf = lambda t: bool((host(t) == np.inf).all())
+    y = cg.adapter_linear(*D(x, w, a, put(b, ids[0], 1, 5)), offsets, order)
+    assert inf(y[np.flatnonzero(mine)][:, 5])
+    near(y, (want, bound), ~mine)
+    near(y[:, :5], (want[:, :5], bound[:, :5]), slice(None))
+    dx, _, db = cg.adapter_linear_grad(*D(x, w, put(a, ids[0], 7, 2), b, dy), offsets, order)
+    assert inf(dx[np.flatnonzero(mine)][:, 7])
+    near(dx, wants[0], ~mine)
+    assert inf(db[int(ids[0]), 2])
+    xi, dyi = put(x, 0, 3), put(dy, 0, 6)
+    _, da, db = cg.adapter_linear_grad(*D(xi, w, a, b, dy), offsets, order)
+    assert inf(da[int(ids[0]), 3]) and inf(db[int(ids[0])])
+    others = np.arange(G) != ids[0]
+    near(da, wants[1], others)
+    keep = np.arange(n_in) != 3
+    near(da[int(ids[0])][keep], (wants[1][0][ids[0]][keep], wants[1][1][ids[0]][keep]), slice(None))
+    dx, da, db = cg.adapter_linear_grad(*D(x, w, a, b, dyi), offsets, order)
+    assert inf(dx[0]) and inf(da[int(ids[0])]) and inf(db[int(ids[0]), :, 6])
+    near(dx[1:], (wants[0][0][1:], wants[0][1][1:]), slice(None))
+    near(db, wants[2], others)
