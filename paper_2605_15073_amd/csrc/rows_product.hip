@@ -81,10 +81,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     // rows of the input, and of [N][K] weights: k-group tid % KG of lanes tid / KG + kLanes i
     const int kg = tid % KG, rr = tid / KG;
     const T *in[NR];
+    unsigned exist = 0;  // bit i: in[i] is a row of the tile
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const int r = rr + kLanes * i, row = r < BM ? s_row[r] : -1;
-        in[i] = static_cast<const T *>(p.in) + (row < 0 ? 0 : row) * p.in_stride;  // row 0: never stored
+        in[i] = static_cast<const T *>(p.in) + (row < 0 ? 0 : row) * p.in_stride;  // row 0: zeroed when staged
+        if (row >= 0) exist |= 1u << i;
     }
     const T *const w = static_cast<const T *>(p.w) + (FUSED ? 0 : (int64_t)t.g * p.w_group);
     const T *const narrow_w = FUSED && grouped ? static_cast<const T *>(p.a) + (int64_t)t.g * p.r * p.K : w;
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int r = rr + kLanes * i;
-            if (r >= at && r < end) l.rows |= 1u << i;
+            if (r >= at && r < end) l.rows |= exist & 1u << i;
             const T *q = ext ? static_cast<const T *>(p.h) + (t.p0 + (r < rows ? r : 0)) * K : in[i];
             if constexpr (WIDE) l.x[i] = load_any8(q + xs);
             else l.x[i] = load_row8<T, false>(q + kx, l.xk);

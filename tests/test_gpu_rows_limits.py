@@ -223,3 +223,21 @@ def test_adapter_infinite_weights_and_gradients(cg, dtype, n, G, n_in, n_out, r)
     assert inf(dx[0]) and inf(da[int(ids[0])]) and inf(db[int(ids[0]), :, 6])
     near(dx[1:], (wants[0][0][1:], wants[0][1][1:]), slice(None))
     near(db, wants[2], others)
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan"), 3e38])
+@pytest.mark.parametrize("n,G,n_in,n_out", [(900, 90, 130, 72), (900, 90, 64, 40), (900, 5, 200, 140)])
+def test_fp32_first_row_of_the_input_is_no_other_tiles(cg, value, n, G, n_in, n_out):
+    """Partly filled tiles, and places that order leaves out, take nothing from row 0."""
+    import torch
+
+    rng = np.random.default_rng([n, n_in])
+    x, w, _ = _linear(rng, n, G, n_in, n_out, "f32")
+    ids = draw_ids(rng, n, G, "even")
+    offsets, order = cg.group_rows(dev(ids), G)
+    order[17] = -1
+    X, W = dev(x), dev(w)
+    clean = cg.grouped_linear(X, W, offsets, order, y=torch.zeros(n, n_out, device="cuda"))
+    X[0] = value
+    y = cg.grouped_linear(X, W, offsets, order, y=torch.zeros(n, n_out, device="cuda"))
+    assert torch.equal(y[1:], clean[1:])
