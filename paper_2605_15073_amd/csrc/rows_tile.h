@@ -447,7 +447,10 @@ __device__ __forceinline__ void mma(float16_t &acc, const uint4_t (&a)[3], const
 //
 // The matrix instruction rounds its sums down, towards minus infinity (measured: results of 896 terms low by
 // 4e-8 of their spread on the mean, which a later sum over many rows picks up). fp32 products therefore sum
-// a step from zero and add it in fp32, and every other step has its rows negated and is subtracted (sign).
+// a step from zero and add it in fp32, and every other step has its rows negated and is subtracted (sign). bf16
+// products keep it: against sums in 64 bits rounded to bf16, results are low by 1e-8 of their magnitude on the mean
+// for up to 1,344 terms and for chunks of 16,384 rows, by 1.6e-7 for 20,000 terms of one sign, and 5e-6 to 6e-4 of
+// them are another bf16 number (of fp32 sums in another order 1e-3).
 template <typename T, int BN, int BM, int TC, int TR, int TX>
 __device__ __forceinline__ void step_products(float16_t (&acc)[TX][TR], const uint4_t *cols,
                                               const uint4_t *rws, int c0, int r0, float sign)
