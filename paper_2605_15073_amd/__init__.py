@@ -621,7 +621,8 @@ def _want_dev(name, t, shape, dtype, like):
 
 def _row_call(like, stream):
     """(handle of the stream that a call on like's device runs on, the stream if it is not the
-    current one)."""
+    current one). Work on another stream waits for what the current one has pending, whether the call
+    allocates or not; what reads its results is for the caller to order."""
     torch = _torch()
     if not like.is_cuda:
         raise ValueError(f"expected device tensors, got one on {like.device}")
@@ -629,26 +630,20 @@ def _row_call(like, stream):
     current = torch._C._cuda_getCurrentRawStream(like.device.index)
     if stream is None or stream.cuda_stream == current:
         return current, None
+    stream.wait_stream(torch.cuda.current_stream(like.device))
     return stream.cuda_stream, stream
 
 
-def _new(shape, dtype, like, side):
-    """A tensor for work on the current stream, or on the stream side: then its memory is neither
-    taken before the current stream's pending work on it is done nor reused before side's."""
-    torch = _torch()
-    t = torch.empty(shape, dtype=dtype, device=like.device)
-    if side is not None and t.numel():
-        side.wait_stream(torch.cuda.current_stream(like.device))
-        t.record_stream(side)
-    return t
+def _new(shape, dtype, like):
+    return _torch().empty(shape, dtype=dtype, device=like.device)
 
 
-def _row_workspace(workspace, need, like, side):
+def _row_workspace(workspace, need, like):
     """(pointer, bytes, the tensor) of the caller's workspace or of a new one."""
     if workspace is None:
         if need == 0:
             return None, 0, None
-        workspace = _new((need,), _torch().uint8, like, side)
+        workspace = _new((need,), _torch().uint8, like)
     elif workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError(f"workspace: expected a contiguous tensor on {like.device}")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
@@ -661,9 +656,14 @@ def _bytes(name, *args):
     return out.value
 
 
-def _run(name, like, *args):
-    """The call on like's device. Pointers are integers or None."""
+def _run(name, like, side, tensors, *args):
+    """The call on like's device. Pointers are integers or None. Where it runs on the stream side, the
+    memory of its tensors is not reused before that stream is done with them."""
     torch = _torch()
+    if side is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(side)
     if torch._C._cuda_getDevice() == like.device.index:
         status = getattr(_lib, name)(*args)
     else:
@@ -695,12 +695,12 @@ def group_rows(ids, n_groups: int, offsets=None, order=None, workspace=None, str
     _want_dev("ids", ids, (n,), torch.int32, ids)
     need = _bytes("cgtp_group_rows_bytes", n, n_groups)
     if offsets is None:
-        offsets = _new((n_groups + 1,), torch.int32, ids, side)
+        offsets = _new((n_groups + 1,), torch.int32, ids)
     if order is None:
-        order = _new((n,), torch.int32, ids, side)
+        order = _new((n,), torch.int32, ids)
     _want_order(offsets, order, n, n_groups, ids)
-    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, ids, side)
-    _run("cgtp_group_rows", ids, n, n_groups, ids.data_ptr(), offsets.data_ptr(), order.data_ptr(),
+    ws_ptr, ws_len, ws = _row_workspace(workspace, need, ids)
+    _run("cgtp_group_rows", ids, side, (ids, offsets, order, ws), n, n_groups, ids.data_ptr(), offsets.data_ptr(), order.data_ptr(),
          ws_ptr, ws_len, handle)
     return offsets, order
 
@@ -724,19 +724,19 @@ def grouped_linear(x, w, offsets, order=None, y=None, stream=None):
     dt, n, G, n_in, n_out, xs = _linear_head(x, w, offsets, order, False)
     handle, side = _row_call(x, stream)
     if y is None:
-        y = _new((n, n_out), x.dtype, x, side)
+        y = _new((n, n_out), x.dtype, x)
     ys = _want_rows("y", y, n, n_out, x)
-    _run("cgtp_grouped_linear", x, dt, n, G, n_in, n_out, _addr(offsets), _addr(order), _addr(x),
+    _run("cgtp_grouped_linear", x, side, (x, w, offsets, order, y), dt, n, G, n_in, n_out, _addr(offsets), _addr(order), _addr(x),
          xs, _addr(w), _addr(y), ys, handle)
     return y
 
 
-def _grad_out(name, out, shape, like, side, rows):
+def _grad_out(name, out, shape, like, rows):
     """An output of a gradient call: allocated if None, skipped if False; (tensor, row stride)."""
     if out is False:
         return None, 0
     if out is None:
-        out = _new(shape, like.dtype, like, side)
+        out = _new(shape, like.dtype, like)
     if rows:
         return out, _want_rows(name, out, *shape, like)
     _want_dev(name, out, shape, like.dtype, like)
@@ -750,13 +750,13 @@ def grouped_linear_grad(x, w, dy, offsets, order=None, dx=None, dw=None, workspa
     dt, n, G, n_in, n_out, xs = _linear_head(x, w, offsets, order, False)
     dys = _want_rows("dy", dy, n, n_out, x)
     handle, side = _row_call(x, stream)
-    dx, dxs = _grad_out("dx", dx, (n, n_in), x, side, True)
-    dw, _ = _grad_out("dw", dw, (G, n_in, n_out), x, side, False)
-    ws_ptr, ws_len, _keep = None, 0, None
+    dx, dxs = _grad_out("dx", dx, (n, n_in), x, True)
+    dw, _ = _grad_out("dw", dw, (G, n_in, n_out), x, False)
+    ws_ptr, ws_len, ws = None, 0, None
     if dw is not None:
         need = _bytes("cgtp_grouped_linear_grad_bytes", dt, n, G, n_in, n_out)
-        ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, side)
-    _run("cgtp_grouped_linear_grad", x, dt, n, G, n_in, n_out, _addr(offsets), _addr(order),
+        ws_ptr, ws_len, ws = _row_workspace(workspace, need, x)
+    _run("cgtp_grouped_linear_grad", x, side, (x, w, dy, offsets, order, dx, dw, ws), dt, n, G, n_in, n_out, _addr(offsets), _addr(order),
          _addr(x), xs, _addr(w), _addr(dy), dys, _addr(dx), dxs, _addr(dw), ws_ptr, ws_len, handle)
     return dx, dw
 
@@ -782,11 +782,11 @@ def adapter_linear(x, w, a, b, offsets, order=None, scale=None, y=None, workspac
     (dt, n, G, n_in, n_out, xs), r = _adapter_head(x, w, a, b, offsets, order, scale)
     handle, side = _row_call(x, stream)
     if y is None:
-        y = _new((n, n_out), x.dtype, x, side)
+        y = _new((n, n_out), x.dtype, x)
     ys = _want_rows("y", y, n, n_out, x)
     need = _bytes("cgtp_adapter_linear_bytes", dt, n, G, n_in, n_out, r)
-    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, side)
-    _run("cgtp_adapter_linear", x, dt, n, G, n_in, n_out, r, _addr(offsets), _addr(order), _addr(x),
+    ws_ptr, ws_len, ws = _row_workspace(workspace, need, x)
+    _run("cgtp_adapter_linear", x, side, (x, w, a, b, offsets, order, scale, y, ws), dt, n, G, n_in, n_out, r, _addr(offsets), _addr(order), _addr(x),
          xs, _addr(w), _addr(a), _addr(b), _addr(scale), _addr(y), ys, ws_ptr, ws_len, handle)
     return y
 
@@ -798,12 +798,12 @@ def adapter_linear_grad(x, w, a, b, dy, offsets, order=None, scale=None, dx=None
     (dt, n, G, n_in, n_out, xs), r = _adapter_head(x, w, a, b, offsets, order, scale)
     dys = _want_rows("dy", dy, n, n_out, x)
     handle, side = _row_call(x, stream)
-    dx, dxs = _grad_out("dx", dx, (n, n_in), x, side, True)
-    da, _ = _grad_out("da", da, (G, n_in, r), x, side, False)
-    db, _ = _grad_out("db", db, (G, r, n_out), x, side, False)
+    dx, dxs = _grad_out("dx", dx, (n, n_in), x, True)
+    da, _ = _grad_out("da", da, (G, n_in, r), x, False)
+    db, _ = _grad_out("db", db, (G, r, n_out), x, False)
     need = _bytes("cgtp_adapter_linear_grad_bytes", dt, n, G, n_in, n_out, r)
-    ws_ptr, ws_len, _keep = _row_workspace(workspace, need, x, side)
-    _run("cgtp_adapter_linear_grad", x, dt, n, G, n_in, n_out, r, _addr(offsets), _addr(order),
+    ws_ptr, ws_len, ws = _row_workspace(workspace, need, x)
+    _run("cgtp_adapter_linear_grad", x, side, (x, w, a, b, dy, offsets, order, scale, dx, da, db, ws), dt, n, G, n_in, n_out, r, _addr(offsets), _addr(order),
          _addr(x), xs, _addr(w), _addr(a), _addr(b), _addr(scale), _addr(dy), dys, _addr(dx), dxs,
          _addr(da), _addr(db), ws_ptr, ws_len, handle)
     return dx, da, db
@@ -874,12 +874,13 @@ class AdamWTensors:
 def adamw(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
           eps: float = 1e-8, weight_decay: float = 0.01, grad_scale=None, stream=None) -> None:
     """cgtp_adamw_step: update the tensors of the handle in place. step counts from 1; grad_scale: a
-    device float32 tensor of one element that multiplies every gradient (clipping), or None."""
+    device float32 tensor of one element that multiplies every gradient (clipping), or None. The
+    handle's tensors live as long as it does, and closing it waits for the device."""
     first = tensors._keep[0][0]
     if grad_scale is not None:
         _want_dev("grad_scale", grad_scale, (1,), _torch().float32, first)
-    handle, _ = _row_call(first, stream)
-    _run("cgtp_adamw_step", first, tensors.handle, lr, beta1, beta2, eps, weight_decay, step,
+    handle, side = _row_call(first, stream)
+    _run("cgtp_adamw_step", first, side, (grad_scale,), tensors.handle, lr, beta1, beta2, eps, weight_decay, step,
          _addr(grad_scale), handle)
 
 
@@ -891,12 +892,12 @@ def adamw_states(tensors: AdamWTensors, m_out=None, v_out=None, stream=None):
     outs = []
     for name, given in (("m_out", m_out), ("v_out", v_out)):
         if given is None:
-            given = [_new(shape, torch.float32, first, side) for shape in tensors.shapes]
+            given = [_new(shape, torch.float32, first) for shape in tensors.shapes]
         if len(given) != len(tensors.shapes):
             raise ValueError(f"{name}: expected {len(tensors.shapes)} tensors, got {len(given)}")
         for i, (t, shape) in enumerate(zip(given, tensors.shapes)):
             _want_dev(f"{name}[{i}]", t, shape, torch.float32, first)
         outs.append(given)
     arrays = [(ctypes.c_void_p * len(o))(*[t.data_ptr() for t in o]) for o in outs]
-    _run("cgtp_adamw_states", first, tensors.handle, arrays[0], arrays[1], handle)
+    _run("cgtp_adamw_states", first, side, (*outs[0], *outs[1]), tensors.handle, arrays[0], arrays[1], handle)
     return outs[0], outs[1]
