@@ -619,6 +619,16 @@ def _want_dev(name, t, shape, dtype, like):
                          f"{like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
+@functools.lru_cache(maxsize=1)
+def _current():
+    """(handle of the current stream of a device, number of the current device). A Stream object costs a
+    tenth of a small call, so torch's own handle of it is taken where this torch has such a call."""
+    torch = _torch()
+    return (getattr(torch._C, "_cuda_getCurrentRawStream",
+                    lambda index: torch.cuda.current_stream(index).cuda_stream),
+            getattr(torch._C, "_cuda_getDevice", lambda: torch.cuda.current_device()))
+
+
 def _row_call(like, stream):
     """(handle of the stream that a call on like's device runs on, the stream if it is not the
     current one). Work on another stream waits for what the current one has pending, whether the call
@@ -626,8 +636,7 @@ def _row_call(like, stream):
     torch = _torch()
     if not like.is_cuda:
         raise ValueError(f"expected device tensors, got one on {like.device}")
-    # the handle itself: a Stream object costs a tenth of a small call
-    current = torch._C._cuda_getCurrentRawStream(like.device.index)
+    current = _current()[0](like.device.index)
     if stream is None or stream.cuda_stream == current:
         return current, None
     stream.wait_stream(torch.cuda.current_stream(like.device))
@@ -664,7 +673,7 @@ def _run(name, like, side, tensors, *args):
         for t in tensors:
             if t is not None:
                 t.record_stream(side)
-    if torch._C._cuda_getDevice() == like.device.index:
+    if _current()[1]() == like.device.index:
         status = getattr(_lib, name)(*args)
     else:
         with torch.cuda.device(like.device):
