@@ -1,5 +1,5 @@
-// Which weights a thread of the wide row products (rows_wide.hip) loads. Plain integer arithmetic, shared by the
-// kernel and compiled by itself in a host test.
+// Index arithmetic of the row products: the grid of their tiles, and which weights a thread of the wide ones
+// (rows_wide.hip) loads. Plain integers, shared by the kernels and compiled by themselves in a host test.
 #pragma once
 
 #include <cstdint>
@@ -14,6 +14,19 @@
 
 namespace cgtp {
 namespace rows {
+
+// Workgroups of a launch for `tiles` tiles: one dimension holds fewer than 2^32 threads, so that they are cut over
+// x and z; tile x + z * (size in x), which may lie past the last one.
+struct TileGrid {
+    unsigned x, z;
+};
+CGTP_HD constexpr TileGrid tile_grid(int64_t tiles)
+{
+    constexpr int64_t most = 1 << 23;
+    const int64_t x = tiles < most ? tiles : most;
+    return {(unsigned)x, (unsigned)((tiles + x - 1) / x)};
+}
+CGTP_HD constexpr int64_t tile_at(unsigned x, unsigned z, unsigned size_x) { return x + (int64_t)z * size_x; }
 
 constexpr int kWideThreads = 256;
 constexpr int kWideCols = 64;  // columns of a tile

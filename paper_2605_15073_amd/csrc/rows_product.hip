@@ -47,13 +47,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg;
 
     const bool shared_w = !FUSED && p.w_group == 0;
+    const int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
     Tile t;
     if (shared_w) {
-        t.p0 = (int64_t)blockIdx.x * BM;
+        t.p0 = index * BM;
+        if (t.p0 >= o.n) return;
         t.p1 = t.p0 + BM < o.n ? t.p0 + BM : o.n;
         t.g = 0;
     } else {
-        t = find_tile(o, TileRows<BM>{}, blockIdx.x);
+        t = find_tile(o, TileRows<BM>{}, index);
         if (t.g < 0 || t.p0 >= t.p1) return;
     }
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -344,7 +346,8 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
     auto *kernel = FUSED || wide ? k_row_product<T, WNK, BM, BN, WR, true, FUSED>
                                  : k_row_product<T, WNK, BM, BN, WR, FUSED, FUSED>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), 0, s, o, p, splits);
+    const TileGrid grid = tile_grid(tiles);
+    hipLaunchKernelGGL(kernel, dim3(grid.x, (unsigned)splits, grid.z), dim3(kThreads), 0, s, o, p, splits);
     return hipGetLastError();
 }
 

@@ -91,13 +91,15 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     __shared__ int s_row[kRows], s_place[kRows], s_any;
     __shared__ int s_g[EXT ? kRows : 1], s_seg_g[EXT ? kRows : 1], s_seg_at[EXT ? kRows + 1 : 1], s_nseg;
 
+    const int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
     Tile t;
     if (EXT && !FUSED) {
-        t.p0 = (int64_t)blockIdx.x * kRows;
+        t.p0 = index * kRows;
+        if (t.p0 >= o.n) return;
         t.p1 = t.p0 + kRows < o.n ? t.p0 + kRows : o.n;
         t.g = 0;
     } else {
-        t = find_tile(o, TileRows<kRows>{}, blockIdx.x);
+        t = find_tile(o, TileRows<kRows>{}, index);
         if (t.g < 0 || t.p0 >= t.p1) return;
     }
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -415,7 +417,8 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     const int whole = p.N / kCols;
     int splits = (int)(2048 / tiles);  // few rows: column tiles go to workgroups of their own
     splits = splits < 1 ? 1 : splits > whole ? whole : splits;
-    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, LINES>), dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads),
+    const TileGrid grid = tile_grid(tiles);
+    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, LINES>), dim3(grid.x, (unsigned)splits, grid.z), dim3(kThreads),
                        0, s, o, p, splits);
     return hipGetLastError();
 }

@@ -241,3 +241,29 @@ def test_fp32_first_row_of_the_input_is_no_other_tiles(cg, value, n, G, n_in, n_
     X[0] = value
     y = cg.grouped_linear(X, W, offsets, order, y=torch.zeros(n, n_out, device="cuda"))
     assert torch.equal(y[1:], clean[1:])
+
+
+@pytest.mark.parametrize("n,n_in,n_out,adapter", [(2 ** 31 - 1, 1, 1, False), (2 ** 30 + 1000, 1, 33, False),
+                                                  (2 ** 30 + 1000, 1, 33, True)])
+def test_as_many_rows_as_there_may_be(cg, n, n_in, n_out, adapter):
+    """Launches of 2^32 threads and more."""
+    import torch
+
+    one = lambda *s: torch.ones(*s, dtype=torch.bfloat16, device="cuda")
+    offsets = torch.tensor([0, n - 7], dtype=torch.int32, device="cuda")
+    x, y = one(n, n_in), torch.empty(n, n_out, dtype=torch.bfloat16, device="cuda")
+    ends = torch.tensor([0, 1, n // 2, n - 9, n - 8, n - 7, n - 1], device="cuda")
+    x[ends] = torch.arange(2, 9, device="cuda", dtype=torch.bfloat16)[:, None]
+    if adapter:
+        cg.adapter_linear(x, one(n_in, n_out), one(1, n_in, 1), one(1, 1, n_out), offsets, y=y)
+        inside, outside = 2, 1
+    else:
+        cg.grouped_linear(x, one(1, n_in, n_out), offsets, y=y)
+        inside, outside = 1, 0
+    step = 1 << 26
+    for at in range(0, n, step):
+        end = min(at + step, n)
+        want = x[at:end].clone()
+        want[:max(0, n - 7 - at)] *= inside
+        want[max(0, n - 7 - at):] *= outside
+        assert torch.equal(y[at:end], want.expand(end - at, n_out)), at

@@ -1,5 +1,5 @@
-"""CPU test of the index arithmetic of the wide row products (csrc/rows_index.h): every weight that a thread can
-load lies inside its group's weights, and every unit of a tile is some thread's."""
+"""CPU test of the index arithmetic of the row products (csrc/rows_index.h): every weight that a thread can load lies
+inside its group's weights, every unit of a tile is some thread's, and every tile some workgroup's."""
 from __future__ import annotations
 
 import os
@@ -58,6 +58,14 @@ int main()
                             if (col < 0 || col + wide > N) fail("columns", groups, 0, N, ct, thread);
                         }
                 }
+    // grids: every tile is some workgroup's, and no dimension has 2^32 threads
+    for (long long tiles : {1ll, 2ll, 1000ll, (1ll << 23) - 1, 1ll << 23, (1ll << 23) + 1, 1ll << 24, (1ll << 24) + 4097, 67112961ll}) {
+        const TileGrid g = tile_grid(tiles);
+        if ((long long)g.x * kWideThreads >= 1ll << 32 || g.z > 65535) fail("grid", 0, 0, 0, 0, (int)g.z);
+        if (tile_at(0, 0, g.x) != 0 || tile_at(0, g.z - 1, g.x) >= tiles || tile_at(g.x - 1, g.z - 1, g.x) + 1 < tiles ||
+            (g.z > 1 && tile_at(0, 1, g.x) != tile_at(g.x - 1, 0, g.x) + 1))
+            fail("tiles", 0, 0, 0, 0, (int)g.z);
+    }
     std::printf("%lld loads, %lld faults\n", loads, bad);
     return bad != 0;
 }
