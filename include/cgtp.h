@@ -475,10 +475,13 @@ int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups, int n_in, 
  *   v is uint8, standing for v_scale (v/255)^4, v = round(255 (v' / v_scale)^(1/4)), at least 1
  *     where v' > 0, so that no element that has seen a gradient is divided by eps alone.
  * The step itself uses the unrounded m' and v'. States start at zero (codes and scales). A
- * gradient that is not finite spoils its element (state_bits 32) or the states of its block (8).
+ * gradient that is not finite, or whose square is not, spoils its element (state_bits 32) or the
+ * states of its block (8).
  *
  * cgtp_adamw_create takes the addresses once (HOST array, copied to a table on the current
  * device, which the handle owns); the tensors stay the caller's and must outlive the handle's use.
+ * The arrays that a step writes must not overlap, of one tensor or of several: weights that two
+ * parts of a model share are listed once, with the sum of their gradients.
  * A handle serves one host thread and one stream at a time. */
 #define CGTP_ADAMW_BLOCK 256
 typedef struct cgtp_adamw_s *cgtp_adamw;

@@ -10,6 +10,7 @@
 // Measured: 5 million parameters in 200 tensors, 32-bit states, 24 us (5.9 TB/s, partly from the caches); 64
 // million, 8-bit states, bf16 gradients and copies, the step 232 us (4.4 TB/s; 80 more with the codes from
 // rounded divisions and roots throughout, bound by the vector ALU) and the decoding 128 us (5.0 TB/s).
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -306,6 +307,41 @@ int check_tensor(const cgtp_adamw_tensor &t, int i, int grad_dtype, int state_bi
     return CGTP_OK;
 }
 
+// What a step writes, of all tensors, lies apart: a parameter that is listed twice would be updated by two
+// workgroups at once.
+int check_apart(int n_tensors, const cgtp_adamw_tensor *tensors, int state_bits)
+{
+    struct Written {
+        uintptr_t start, end;
+        int tensor;
+    };
+    std::vector<Written> all;
+    const size_t ss = state_bits == 8 ? 1 : 4;
+    for (int i = 0; i < n_tensors; ++i) {
+        const cgtp_adamw_tensor &t = tensors[i];
+        if (t.n == 0) continue;
+        const size_t n = (size_t)t.n, blocks = (n + CGTP_ADAMW_BLOCK - 1) / CGTP_ADAMW_BLOCK;
+        auto add = [&](const void *p, size_t bytes) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            if (p) all.push_back({at, at + bytes, i});
+        };
+        add(t.param, 4 * n);
+        add(t.m, ss * n);
+        add(t.v, ss * n);
+        add(t.copy, 2 * n);
+        if (state_bits == 8) {
+            add(t.m_scale, 4 * blocks);
+            add(t.v_scale, 4 * blocks);
+        }
+    }
+    std::sort(all.begin(), all.end(), [](const Written &a, const Written &b) { return a.start < b.start; });
+    for (size_t k = 1; k < all.size(); ++k)
+        if (all[k].start < all[k - 1].end)
+            return report(CGTP_ERR_ARG, "arrays that a step writes overlap, of tensors %d and %d", all[k - 1].tensor,
+                          all[k].tensor);
+    return CGTP_OK;
+}
+
 int create(int n_tensors, const cgtp_adamw_tensor *tensors, int grad_dtype, int state_bits,
            cgtp_adamw *handle)
 {
@@ -326,6 +362,8 @@ int create(int n_tensors, const cgtp_adamw_tensor *tensors, int grad_dtype, int 
         n_items += (t.n + kItem - 1) / kItem;
     }
     first.push_back(n_items);
+    const int apart = check_apart(n_tensors, tensors, state_bits);
+    if (apart != CGTP_OK) return apart;
     if (n_items > 0x7fffffffLL)
         return report(CGTP_ERR_UNSUPPORTED, "%lld work items", (long long)n_items);
     std::vector<Item> items;
