@@ -49,6 +49,14 @@ hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p,
 // The form for short inputs and wide outputs (rows_wide.hip), and whether it covers a product.
 bool row_wide_takes(int dtype, const RowProduct &p);
 hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
+// Whether adapters get tiles of 128 rows of their own, in which the product forms the narrow rows itself: where they
+// have 64 rows on the mean, or all tiles run at once anyway. Us in one launch, and with a narrow product of its own
+// and tiles that adapters share: 300 adapters of 1, 8 and 48 rows, bf16, y 64 -> 896, rank 16 23 and 94, 28 and 33,
+// 29 and 40, dx 896 -> 128 34 and 207, 35 and 86, 34 and 55; fp32 y 49 and 138, 66 and 58, 62 and 68, dx 101 and
+// 323, 102 and 168, 98 and 126. 4,000 adapters: bf16 y 120 and 116, 188 and 156, 202 and 222, dx 208 and 276, 269
+// and 175, 291 and 266; fp32 y 329 and 226, 485 and 353, 580 and 527, dx 601 and 492, 809 and 396, 899 and 691. 100
+// of 1,000 rows: bf16 dx 71 and 105, fp32 265 and 298; 800 of 125: y 41 and 66, 101 and 125.
+inline bool own_tiles(const RowOrder &o) { return o.n >= 64 * (int64_t)o.G || o.n / 128 + o.G < 512; }
 // Products with p.a: whether some form covers one (the launch is that of launch_row_product).
 bool adapter_wide_takes(int dtype, const RowOrder &o, const RowProduct &p);
 bool adapter_product_takes(int dtype, const RowOrder &o, const RowProduct &p);

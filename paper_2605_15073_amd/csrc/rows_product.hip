@@ -341,7 +341,8 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     const bool wide = p.K >= kU && (WNK ? !p.h || p.r >= kU : p.N >= kWide<T>);
     const int64_t tiles = p.w_group || FUSED ? o.n / BM + o.G + 1 : (o.n + BM - 1) / BM;
     const int ctiles = (p.N + BN - 1) / BN;
-    // few rows: column tiles go to workgroups of their own
+    // few rows: column tiles go to workgroups of their own (20,000 rows, 300 -> 896 fp32, with 512, 2,048 and 8,192
+    // workgroups 119, 113 and 113 us; 60,000 rows, 300 -> 1344 443, 439 and 455, bf16 160, 155 and 156)
     int splits = (int)(2048 / tiles);
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
     auto *kernel = FUSED || wide ? k_row_product<T, WNK, BM, BN, WR, true, FUSED>
@@ -356,11 +357,17 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
     if constexpr (WNK)
+        // 100,000 rows, 896 -> 64, us with tiles of 64 and 128 columns: bf16 51 and 62, fp32 169 and 234
         if (p.a) return p.N <= 64 ? launch<T, true, 128, 64, 4, true>(o, p, s) : launch<T, true, 128, 128, 4, true>(o, p, s);
     if (p.a) return launch_row_wide(dtype, o, p, s);
     if (row_few_takes(dtype, o, p)) return launch_row_few(o, p, s);
     const int64_t groups = p.w_group ? o.G : 1;
-    const bool few = o.n < 64 * groups;  // rows per group
+    // Rows of a tile, by those of a group. Us with tiles of 32 and of 128 rows (or the wide form), 500 groups of 24, 32,
+    // 40, 48 and 64 rows: 256 -> 256 bf16 22 27 33 34 41 and 27 27 28 29 31, fp32 41 51 66 70 79 and 74 74 74 76 78;
+    // 64 -> 448 bf16 15 19 24 24 28 and 18 18 18 17 18, fp32 29 34 43 44 49 and 37 37 38 38 40.
+    const bool few = o.n < 40 * groups;
+    // Columns of a tile: 200,000 rows, us with 32, 64 and 128: bf16 256 -> 32 29 33 38, -> 64 49 36 38, -> 72 70 60 42;
+    // fp32 1344 -> 32 283 433 542, -> 64 563 444 555, -> 72 865 842 557.
     if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1>(o, p, s);
@@ -375,10 +382,10 @@ size_t narrow_bytes(int dtype, int64_t n_rows, int N)
     return (size_t)n_rows * narrow_width(N) * (dtype == CGTP_BF16 ? kNarrow<bf16_t> * 2 : 4);
 }
 
-// Adapters of 64 rows on the mean, one column tile of [N][K] weights.
+// Adapters with tiles of their own, one column tile of [N][K] weights.
 bool adapter_product_takes(int dtype, const RowOrder &o, const RowProduct &p)
 {
-    return p.a && p.w_nk && p.N <= 128 && p.r <= 32 && p.K >= kU && o.n >= 64 * (int64_t)o.G;
+    return p.a && p.w_nk && p.N <= 128 && p.r <= 32 && p.K >= kU && own_tiles(o);
 }
 
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)

@@ -43,7 +43,6 @@ using namespace rows;
 
 constexpr int kRows = 128;    // positions of a workgroup, 32 a wave
 constexpr int kCols = kWideCols;  // columns of a tile
-constexpr int kTilesAtOnce = 256;
 template <typename T> constexpr int kPairs = sizeof(T) == 2 ? 8 : 4;  // pairs of k-groups: up to 128 bf16, 64 fp32
 template <typename T> constexpr int kExtPairs = sizeof(T) == 2 ? 6 : 2;  // of a narrow product's rows, up to 32 wide
 
@@ -415,7 +414,9 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int64_t tiles = XP > 0 && !FUSED ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
     const int whole = p.N / kCols;
-    int splits = (int)(2048 / tiles);  // few rows: column tiles go to workgroups of their own
+    // few rows: column tiles go to workgroups of their own (60,000 rows, 64 -> 1344, with 512, 2,048 and 8,192
+    // workgroups bf16 37, 39 and 54 us, fp32 95, 94 and 124; 20,000 rows, 64 -> 896 bf16 12, 16 and 16)
+    int splits = (int)(2048 / tiles);
     splits = splits < 1 ? 1 : splits > whole ? whole : splits;
     const TileGrid grid = tile_grid(tiles);
     hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, LINES>), dim3(grid.x, (unsigned)splits, grid.z), dim3(kThreads),
@@ -470,10 +471,10 @@ bool row_wide_takes(int dtype, const RowProduct &p)
     return dtype == CGTP_BF16 ? takes<bf16_t>(p) : takes<float>(p);
 }
 
-// Tiles of one adapter each: where adapters have 64 rows on the mean, or all tiles run at once anyway.
+// Tiles of one adapter each.
 bool adapter_wide_takes(int dtype, const RowOrder &o, const RowProduct &p)
 {
-    return p.a && !p.h_out && (o.n >= 64 * (int64_t)o.G || o.n / kRows + o.G < kTilesAtOnce) && row_wide_takes(dtype, p);
+    return p.a && !p.h_out && own_tiles(o) && row_wide_takes(dtype, p);
 }
 
 hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)

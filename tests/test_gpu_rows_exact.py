@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,G,n_in,n_out,r", [
     (700, 2, 64, 448, 8), (700, 2, 64, 200, 16), (900, 3, 40, 131, 32), (300, 90, 64, 200, 24), (300, 90, 33, 72, 4),
-    (500, 2, 100, 60, 6), (500, 2, 200, 300, 64), (500, 2, 131, 40, 17), (64, 64, 48, 40, 8)])
+    (500, 2, 100, 60, 6), (500, 2, 200, 300, 64), (500, 2, 131, 40, 17), (64, 64, 48, 40, 8), (2000, 700, 64, 200, 24), (2000, 700, 40, 72, 4)])
 def test_adapter_between_the_products(cg, dtype, n, G, n_in, n_out, r):
     """The narrow products between an adapter's two matrices are held in 24 bits. Operands are whole numbers;
     those products pass 2^18, and meet another of the same adapter that differs in one term, times -1."""

@@ -25,7 +25,8 @@ def test_row_gradient_of_few_columns(cg, dtype, n, G, n_in, n_out):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("r", [1, 4, 12, 24])
-@pytest.mark.parametrize("n,G,n_in,n_out", [(300, 2, 64, 128), (300, 2, 40, 131), (300, 80, 64, 128), (300, 2, 140, 72)])
+@pytest.mark.parametrize("n,G,n_in,n_out", [(300, 2, 64, 128), (300, 2, 40, 131), (300, 80, 64, 128), (300, 2, 140, 72),
+                                            (2000, 700, 64, 128), (2000, 700, 40, 131), (2000, 700, 140, 72)])
 def test_adapter_infinite_inputs(cg, dtype, r, n, G, n_in, n_out):
     """Infinite inputs meet weights of one sign: infinite rows, no NaN, and no other rows."""
     rng = np.random.default_rng([n, n_in, r])
@@ -94,7 +95,7 @@ def test_fp32_tiny_beside_ordinary(cg, tiny, n, G, n_in, n_out):
 
 @pytest.mark.parametrize("tiny", [1.2345678e-37, 2.0 ** -130, 3 * 2.0 ** -149])
 @pytest.mark.parametrize("n,G,n_in,n_out,r", [(300, 2, 64, 130, 8), (300, 60, 64, 72, 16), (300, 2, 200, 72, 20),
-                                              (400, 2, 70, 40, 40)])
+                                              (400, 2, 70, 40, 40), (2000, 700, 64, 130, 8)])
 def test_fp32_adapter_tiny_beside_ordinary(cg, tiny, n, G, n_in, n_out, r):
     """The same through an adapter: a^T x from tiny inputs, and tiny values of b beside ordinary ones."""
     rng = np.random.default_rng([n, n_in, r])
@@ -184,7 +185,8 @@ def test_fp32_infinite_row_leaves_other_bits(cg, n, G, n_in, n_out):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,G,n_in,n_out,r", [(300, 2, 64, 128, 4), (300, 2, 40, 131, 20), (300, 80, 64, 128, 8),
-                                              (300, 2, 140, 72, 16), (300, 2, 100, 200, 12), (300, 2, 72, 140, 40)])
+                                              (300, 2, 140, 72, 16), (300, 2, 100, 200, 12), (300, 2, 72, 140, 40),
+                                              (2000, 700, 64, 128, 8), (2000, 700, 40, 131, 20), (2000, 700, 140, 72, 16)])
 def test_adapter_infinite_weights_and_gradients(cg, dtype, n, G, n_in, n_out, r):
     """An infinite weight of an adapter, or an infinite row, among values of one sign: infinities, as fp32 sums
     give, and no NaN; other adapters' rows and gradients as without it."""
