@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     constexpr int NC = (BX + kLanes - 1) / kLanes;
     __shared__ uint4_t s_tiles[kTile<T, BX> + kTile<T, BM>];
     uint4_t *const s_cols = s_tiles, *const s_rows = s_tiles + kTile<T, BX>;
-    __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg;
+    __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg, s_any;
 
     const bool shared_w = !FUSED && p.w_group == 0;
     const int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
@@ -68,7 +68,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     if (ct0 >= ct1) return;
     const int col_end = ct1 * BN < p.N ? ct1 * BN : p.N;
 
-    if (tid < BM) s_row[tid] = tid < rows ? row_at(o, t.p0 + tid) : -1;
+    const int my_row = tid < rows ? row_at(o, t.p0 + tid) : -1;
+    if (tid < BM) s_row[tid] = my_row;
+    if (tid == 0) s_any = -1;
     if (!FUSED && !shared_w && t.g == o.G) {  // rows of no group
         if (p.narrow) return;
         __syncthreads();
@@ -77,18 +79,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     }
     const bool grouped = t.g < o.G;
     int nseg = 0;
-    if (shared_w && p.h) nseg = find_segments<BM>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
     __syncthreads();
+    if (my_row >= 0) s_any = my_row;  // any row of the tile
+    if (shared_w && p.h) nseg = find_segments<BM>(o, t.p0, rows, s_g, s_seg_g, s_seg_at, &s_nseg);
+    else __syncthreads();
+    if (s_any < 0) return;
 
     // rows of the input, and of [N][K] weights: k-group tid % KG of lanes tid / KG + kLanes i
     const int kg = tid % KG, rr = tid / KG;
     const T *in[NR];
-    unsigned exist = 0;  // bit i: in[i] is a row of the tile
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const int r = rr + kLanes * i, row = r < BM ? s_row[r] : -1;
-        in[i] = static_cast<const T *>(p.in) + (row < 0 ? 0 : row) * p.in_stride;  // row 0: zeroed when staged
-        if (row >= 0) exist |= 1u << i;
+        in[i] = static_cast<const T *>(p.in) + (row < 0 ? s_any : row) * p.in_stride;  // any: never stored
     }
     const T *const w = static_cast<const T *>(p.w) + (FUSED ? 0 : (int64_t)t.g * p.w_group);
     const T *const narrow_w = FUSED && grouped ? static_cast<const T *>(p.a) + (int64_t)t.g * p.r * p.K : w;
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int r = rr + kLanes * i;
-            if (r >= at && r < end) l.rows |= exist & 1u << i;
+            if (r >= at && r < end) l.rows |= 1u << i;
             const T *q = ext ? static_cast<const T *>(p.h) + (t.p0 + (r < rows ? r : 0)) * K : in[i];
             if constexpr (WIDE) l.x[i] = load_any8(q + xs);
             else l.x[i] = load_row8<T, false>(q + kx, l.xk);
