@@ -71,11 +71,12 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters).
+// NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters). All parts of those
+// rows, XP / P pairs each, meet the same weights, which lie in LDS once.
 template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool LINES>
 __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p, int splits)
 {
-    constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, KG = 2 * (NP + XP), LD = kCols + 1, CW = kWide<T>;
+    constexpr int U = kU, P = kNarrow<T>, Q = kSplit<T>, XE = XP > 0 ? XP / P : 1, KG = 2 * (NP + XP / P), LD = kCols + 1, CW = kWide<T>;
     constexpr bool EXT = XP > 0;
     // fp32: the matrix instruction rounds down, so the second half of the k is summed negated (step_products)
     constexpr int kPlus = Q > 1 && NP > 1 ? NP / 2 : NP;
@@ -188,17 +189,17 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
         wave_sync();
 #pragma unroll
         for (int s = 0; s < XP; ++s) {
-            const int k = (2 * s + half) * U;
-            to_units(load_row8<T, false>(mine + k, P * W - k), h[s], kSign);
+            const int k = (2 * (s % XE) + half) * U;
+            to_units(load_row8<T, false>(mine + s / XE * W + k, W - k), h[s], kSign);
         }
         wave_sync();
     } else if (EXT) {
         const bool grouped = s_g[pl] < o.G;
 #pragma unroll
         for (int s = 0; s < XP; ++s) {
-            const int k = (2 * s + half) * U;
-            const T *const q = static_cast<const T *>(p.h) + (grouped ? (t.p0 + pl) * (P * W) : 0) + k;
-            to_units(load_row8<T, true>(q, grouped ? P * W - k : 0), h[s], kSign);
+            const int k = (2 * (s % XE) + half) * U;
+            const T *const q = static_cast<const T *>(p.h) + (grouped ? (t.p0 + pl) * (P * W) + s / XE * W : 0) + k;
+            to_units(load_row8<T, true>(q, grouped ? W - k : 0), h[s], kSign);
         }
     }
     // outputs: of a piece of 128 bytes this lane stores vector lane % kVecs of rows 64 / kVecs i + lane / kVecs
@@ -232,8 +233,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             const T *wb = w;
             if (EXT && g >= 2 * NP) {
                 k = (g - 2 * NP) * U;
-                K = k < P * W && nseg > 0 ? p.r : 0;
-                k = narrow_k<T>(k, W);
+                K = nseg > 0 ? p.r : 0;
                 wb = static_cast<const T *>(p.v) + (int64_t)(nseg > 0 ? s_seg_g[seg] : 0) * p.r * p.N;
             }
             have[i] = K - k;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                     for (int q = 0; q < Q; ++q)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) b[q][e] = in_seg ? h[s][q][e] : 0u;
-                    product(NP + s, b);
+                    product(NP + s % XE, b);
                 }
                 if (++seg >= nseg) break;
                 __syncthreads();
