@@ -48,18 +48,32 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     const int wr = wave % WR, wc = wave / WR;
     const int r0 = wr * (BM / WR), c0w = wc * (BN / WC);
 
-    // waves 0 and 1 stage a, waves 2 and 3 b: lanes first .. first + CW - 1, k-group kg
-    constexpr int kHalf = kThreads / 2;
+    // waves 0 and 1 stage a, waves 2 and 3 b: lanes first .. first + CW - 1 of k-group kg, of b of one of its parts.
+    // b's parts are spread over the threads (narrow tiles leave most without work in one part alone).
+    constexpr int kHalf = kThreads / 2, kPart = KG * (BN / CW), NL = (P * kPart + kHalf - 1) / kHalf;
+    static_assert(KG * (BM / CW) <= kHalf, "a: one task a thread");
     const bool of_b = wave >= 2;
-    const int task = tid % kHalf, lanes = of_b ? BN : BM, kg = task / (lanes / CW);
-    const bool has = kg < KG;  // else nothing: a narrow tile
-    const int first = CW * (task % (lanes / CW)), col = (of_b ? b0 : a0) + first;
     const int width = !of_b ? q.A : NARROW ? W : B;
-    const T *const from = static_cast<const T *>(!of_b ? q.a : NARROW ? q.h : q.b) +
-                          (WIDE && col + CW > width ? width - CW : col);
-    const int early = WIDE && col < width && col + CW > width ? col + CW - width : 0;
-    uint4_t l[P][8];
-    unsigned in;  // bit u: row u of the k-group exists
+    struct Task {
+        bool has;
+        int part, kg, first, early;
+        const T *from;
+    } tasks[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        const int all = tid % kHalf + kHalf * i, lanes = of_b ? BN : BM, task = of_b ? all % kPart : all;
+        Task &k = tasks[i];
+        k.part = of_b ? all / kPart : 0;
+        k.kg = task / (lanes / CW);
+        k.first = CW * (task % (lanes / CW));
+        k.has = k.kg < KG && k.part < P && (of_b || i == 0);
+        const int col = (of_b ? b0 : a0) + k.first;
+        k.early = WIDE && col < width && col + CW > width ? col + CW - width : 0;
+        k.from = static_cast<const T *>(!of_b ? q.a : NARROW ? q.h : q.b) +
+                 ((k.has ? k.part : 0) * (NARROW ? W : 0) + (WIDE && col + CW > width ? width - CW : col));
+    }
+    uint4_t l[NL][8];
+    unsigned in[NL];  // bit u: row u of the k-group exists
     float sign = 1.f;  // of the step's a
     const int steps = (int)((t.p1 - t.p0 + BK - 1) / BK);
     // ids of the rows of step s, -1 past the chunk; loads without a condition, as the operands'
@@ -81,40 +95,38 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         }
     };
     auto fetch = [&](int s) {
-        if (!has) return;
-        const int64_t *const at = s_at[of_b][s & 1] + kg * kU;
-        in = s_rows_in[s & 1][kg / 4] >> 8 * (kg % 4) & 0xffu;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (WIDE) l[0][u] = *reinterpret_cast<const uint4_any *>(from + at[u]);
-            else l[0][u] = load_16<T, false>(from + at[u], width - col);
-            if (of_b)
+        for (int i = 0; i < NL; ++i) {
+            const Task &k = tasks[i];
+            if (!k.has) continue;
+            const int64_t *const at = s_at[of_b][s & 1] + k.kg * kU;
+            in[i] = s_rows_in[s & 1][k.kg / 4] >> 8 * (k.kg % 4) & 0xffu;
 #pragma unroll
-                for (int e = 1; e < P; ++e) {
-                    if (WIDE) l[e][u] = *reinterpret_cast<const uint4_any *>(from + at[u] + e * W);
-                    else l[e][u] = load_16<T, false>(from + at[u] + e * W, width - col);
-                }
+            for (int u = 0; u < 8; ++u) {
+                if (WIDE) l[i][u] = *reinterpret_cast<const uint4_any *>(k.from + at[u]);
+                else l[i][u] = load_16<T, false>(k.from + at[u], width - ((of_b ? b0 : a0) + k.first));
+            }
         }
     };
     auto stage = [&]() {
-        if (!has) return;
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            if (e > 0 && !of_b) break;
-            if (early > 0) {
+        for (int i = 0; i < NL; ++i) {
+            const Task &k = tasks[i];
+            if (!k.has) continue;
+            if (k.early > 0) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) settle<T>(l[e][r], early);
+                for (int r = 0; r < 8; ++r) settle<T>(l[i][r], k.early);
             }
-            if (in != 0xffu) {
+            if (in[i] != 0xffu) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) l[e][r] = in >> r & 1 ? l[e][r] : uint4_t{0, 0, 0, 0};
+                for (int r = 0; r < 8; ++r) l[i][r] = in[i] >> r & 1 ? l[i][r] : uint4_t{0, 0, 0, 0};
             }
             uint4_t u[CW][Q];
-            to_units(l[e], u, of_b ? 1.f : sign);
+            to_units(l[i], u, of_b ? 1.f : sign);
 #pragma unroll
             for (int j = 0; j < CW; ++j) {
-                if (of_b) put<T, BN>(s_cols[e], KG, kg, place_full<T>(first + j), u[j]);
-                else put<T, BM>(s_rows, KG, kg, place_full<T>(first + j), u[j]);
+                if (of_b) put<T, BN>(s_cols[k.part], KG, k.kg, place_full<T>(k.first + j), u[j]);
+                else put<T, BM>(s_rows, KG, k.kg, place_full<T>(k.first + j), u[j]);
             }
         }
     };
@@ -310,8 +322,9 @@ hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, bool bi
     const bool wide = q.A >= kFull<T> && (q.r > 0 || B >= kFull<T>);  // 16 bytes of a row and more
     const int64_t chunks = ((big ? o.n / kFewRows : o.n / sh.rows + o.G) + 7) / 8 * 8;
     if (chunks * sh.tiles > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    auto *kernel = q.r > 0 ? (wide ? k_row_outer<T, BM, BN, WR, true, true> : k_row_outer<T, BM, BN, WR, false, true>)
-                           : (wide ? k_row_outer<T, BM, BN, WR, true, false> : k_row_outer<T, BM, BN, WR, false, false>);
+    auto *kernel = wide ? k_row_outer<T, BM, BN, WR, true, false> : k_row_outer<T, BM, BN, WR, false, false>;
+    if constexpr (BN <= CGTP_MAX_ADAPTER_RANK)
+        if (q.r > 0) kernel = wide ? k_row_outer<T, BM, BN, WR, true, true> : k_row_outer<T, BM, BN, WR, false, true>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks * sh.tiles)), dim3(kThreads), 0, s, o, q, ChunkRows(sh.rows), big,
                        slots);
     return hipGetLastError();
