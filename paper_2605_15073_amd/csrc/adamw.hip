@@ -7,9 +7,10 @@
 // depend on nothing but the formulas, and a program that forms them in single fp32 operations
 // gets the same ones.
 //
-// Measured: 5 million parameters in 200 tensors, 32-bit states, 24 us (5.9 TB/s, partly from the caches); 64
-// million, 8-bit states, bf16 gradients and copies, the step 232 us (4.4 TB/s; 80 more with the codes from
-// rounded divisions and roots throughout, bound by the vector ALU) and the decoding 128 us (5.0 TB/s).
+// Measured, calls in a row: 5 million parameters in 200 tensors, 32-bit states, 23 us (6.1 TB/s, partly from the
+// caches); 64 million, 8-bit states, bf16 gradients and copies, the step 243 us (4.2 TB/s; 80 more with the codes from
+// rounded divisions and roots throughout, bound by the vector ALU), the decoding 94 us (6.8 TB/s, partly from the
+// caches), step and decoding in turn 331.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -252,8 +253,8 @@ __global__ __launch_bounds__(kThreads) void k_adamw_states(const Tensor *__restr
 }
 
 // Whether a call over that many items moves more bytes than the memory-side cache holds. Then its stores go past
-// the caches: 64 million parameters, 8-bit states, step and decoding 340 us, 360 without; 5 million in 32 bits
-// 23.9 and 23.3.
+// the caches: 64 million parameters, 8-bit states, us past and through them: the step 243 and 244, the decoding
+// 94 and 143, both in turn 331 and 356; 5 million in 32 bits 24 and 23.
 bool past_caches(int64_t items, int bytes) { return items * kItem * bytes > (int64_t)256 << 20; }
 
 template <bool PAST> auto *pick(int grad_dtype, int bits)

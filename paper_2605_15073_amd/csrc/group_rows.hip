@@ -9,7 +9,7 @@
 //
 // Up to kRound rows one workgroup does all of it in one launch. Bound by latency: the chains of three
 // launches, and in each of memory, LDS and barriers. Measured: 525,308 rows of 4,005 groups 26 us (counting
-// 6.3, scan 4.5, placing 15; 1.5 of it for stores to scattered places), of 5 groups 18, 64 rows 9 us (the kernel 5.5).
+// 6.3, scan 4.5, placing 15.7; 1.5 of it for stores to scattered places), of 5 groups 17, 64 rows 9 us (the kernel 4.9).
 // 512 threads of eight ids took 27 us; ranks from atomic adds, with ballots only where keys meet, 27.
 #include "internal.h"
 #include "rows.h"

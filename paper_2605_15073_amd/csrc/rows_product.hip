@@ -9,9 +9,9 @@
 // early, one without values points to some that exist, and both are put right when they are staged. Only
 // widths below a vector (WIDE false) load value by value.
 //
-// Measured: row gradients of 261,766 rows, 1344 -> 128 bf16, 203 us (3.8 TB/s; bound by the reads and the
-// latency of a step's loads); 60,000 rows, 896 x 896: 184 us in bf16 (520 TFLOP/s), 708 us in fp32
-// (136 TFLOP/s, six instructions a product: bound by the matrix cores and the splitting of the operands).
+// Measured: row gradients of 261,766 rows, 1344 -> 128 bf16, 197 us (3.9 TB/s; bound by the reads and the
+// latency of a step's loads); 60,000 rows, 896 x 896: 174 us in bf16 (550 TFLOP/s), 658 us in fp32
+// (146 TFLOP/s, six instructions a product: bound by the matrix cores and the splitting of the operands).
 //
 // Adapters: after the steps over the shared W, a tile's sums go on over the adapters of its rows, one
 // segment of rows at a time, with the narrow product's result as input rows (zero outside the
@@ -20,8 +20,9 @@
 //
 // FUSED: tiles of one adapter each, whose narrow product is formed here too. Its matrix, [r][K] like the
 // shared weights, gives 32 more columns of the tile (so the input is read once for both); the result goes
-// through LDS as the input rows of one more step, over the adapter's second matrix: 131,327 rows of 8
-// adapters, 896 -> 128, rank 16, fp32 344 us where the two products apart took 323 and 138.
+// through LDS as the input rows of one more step (bf16 ranks above 16: two, as its parts fill them), over the
+// adapter's second matrix: 131,327 rows of 8 adapters, 896 -> 128, rank 16, fp32 290 us, bf16 86; 100,000 rows of 100,
+// fp32 265 where the two products apart take 298, bf16 71 and 105.
 #include "internal.h"
 #include "rows_tile.h"
 

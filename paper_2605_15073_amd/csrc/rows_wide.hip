@@ -17,11 +17,11 @@
 // leave line by line: a line is stored once the columns that it takes are there, the ends of a row in vectors that
 // overlap. WHOLE: columns come in aligned fours.
 // 525,308 rows from 64, us now, and with pieces stored where their columns start, through and past the caches:
-// bf16 452 195, 252, 473; 480 148, 201, 148; 900 345, 485, 896; fp32 452 377, 433, 812; 900 667, 815, 1,540; 912
-// 541, 659, 544. Rows on lines, past and through the caches: bf16 896 200, 243, fp32 440, 505; with a reader right
+// bf16 452 191, 252, 473; 480 146, 201, 148; 900 341, 485, 896; fp32 452 368, 433, 812; 900 644, 815, 1,540; 912
+// 544, 659, 544. Rows on lines, past and through the caches: bf16 896 200, 243, fp32 440, 505; with a reader right
 // behind, results of 4 to 900 MB, between 9% more (4 MB) and 13% less.
 //
-// Measured: 525,308 rows, 64 -> 896: 440 to 470 us in fp32 (4.3 to 4.6 TB/s) and 199 us in bf16 (5.1 TB/s), 93% of
+// Measured: 525,308 rows, 64 -> 896: 447 to 477 us in fp32 (4.2 to 4.5 TB/s) and 198 us in bf16 (5.1 TB/s), 93% of
 // it stores; bound by memory, a large copy reaches 4.8 TB/s. Rows apart from lines: 2.3 to 3.4 TB/s, bound by the
 // two broken lines of each row, whose other parts other workgroups write.
 //
@@ -30,8 +30,8 @@
 // adapters takes them one after the other, with the rows of the others zero. Where adapters have rows enough
 // for tiles of their own (FUSED) the narrow product is formed here too: from the inputs in registers and the
 // adapter's first matrix through LDS, turned in the wave's piece, and held from then on: 525,308 rows of 32
-// adapters, 64 -> 896, rank 16, bf16 201 us (5.0 TB/s); before its stores went past the caches 240, and 305 with a
-// narrow product of its own.
+// adapters, 64 -> 896, bf16, rank 16 212 us (4.8 TB/s), rank 32 250: three and six pairs of k-groups for its parts
+// beside the inputs' four; fp32, rank 16, 606.
 #include "internal.h"
 #include "rows_tile.h"
 
