@@ -203,13 +203,18 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             const int64_t at = q.transposed ? (int64_t)c * q.A + i : (int64_t)i * B + c;
             if (__builtin_isfinite(whole ? stored(out + at) : stored(part + at))) continue;
             float sum = 0.f;
-            for (int64_t pos = t.p0; pos < t.p1; ++pos) {
-                const int row = row_at(o, pos);
-                if (row < 0) continue;
+            auto add = [&](int64_t pos) {  // no load waits for a branch
+                const int row = row_at(o, pos), any = row < 0 ? 0 : row;
                 const float y = NARROW ? narrow_at<T>(q.h, pos, W, c)
-                                       : (float)static_cast<const T *>(q.b)[row * q.b_stride + c];
-                sum += (float)static_cast<const T *>(q.a)[row * q.a_stride + i] * y;
-            }
+                                       : (float)static_cast<const T *>(q.b)[any * q.b_stride + c];
+                const float x = (float)static_cast<const T *>(q.a)[any * q.a_stride + i];
+                sum = row < 0 ? sum : fmaf(x, y, sum);
+            };
+            int64_t pos = t.p0;
+            for (; pos + 8 <= t.p1 && sum == sum; pos += 8)  // NaN stays
+#pragma unroll
+                for (int u = 0; u < 8; ++u) add(pos + u);
+            for (; pos < t.p1 && sum == sum; ++pos) add(pos);
             if (whole) out[at] = (T)sum;
             else part[at] = sum;
         }

@@ -12,8 +12,9 @@
 // step, so that the parts hold every x up to 2^112 whole, however small, beside whatever others. Sums beyond
 // 2^96, larger inputs, infinities and NaN leave results that are not finite, and so do an adapter's weights that
 // are not, which rows of other adapters in a tile meet as zeros. Those results, and no others, are formed again in
-// plain fp32, one result a thread at a time. 131,072 rows, 64 -> 896, 8 groups: y 121 us, with one infinite input
-// 370, with one in every 128 rows 778; all gradients 382, 2,990 and 5,580 us (a cell of dw runs over its chunk's rows).
+// plain fp32, one result a thread at a time, up to the term that makes it NaN. 131,072 rows, 64 -> 896, 8 groups: y
+// 122 us, with one infinite input 339, with one in every 128 rows 650; all gradients 361, 2,700 and 3,800 us (a cell of
+// dw runs over its chunk's rows); 896 -> 128, dy all NaN, 2,060 us where numbers take 579.
 //
 // Operands whose k is contiguous in memory are staged eight k a load. The others (weights of the
 // forward product, both operands of a weight gradient) are loaded 8 or 16 bytes wide (kWide, kFull lanes), 8
@@ -656,7 +657,12 @@ __device__ void row_plain_sums(const RowOrder &o, const RowProduct &p, int group
         if (__builtin_isfinite(narrow ? stored(narrow_out) : stored(out))) continue;
         const T *const in = static_cast<const T *>(p.in) + s_row[r] * p.in_stride;
         float sum = 0.f;
-        for (int k = 0; k < p.K; ++k) sum += (float)in[k] * (float)w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c];
+        auto term = [&](int k) { return (float)in[k] * (float)w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c]; };
+        int k0 = 0;
+        for (; k0 + 8 <= p.K && sum == sum; k0 += 8)  // NaN stays
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += term(k0 + u);
+        for (; k0 < p.K && sum == sum; ++k0) sum += term(k0);
         if ((p.h || h) && s_g[r] < o.G) {
             const T *const v = static_cast<const T *>(p.v) + (int64_t)s_g[r] * p.r * p.N;
             for (int k = 0; k < p.r; ++k)
