@@ -385,10 +385,10 @@ int cgtp_plan_set_receiver_order(cgtp_plan plan, int64_t n_nodes, const int32_t 
  *  - dtype is CGTP_F32 or CGTP_BF16 for every tensor of values, unless noted. Sums are held in fp32
  *    and rounded once, to the output's type; bf16 sums are those of the matrix instruction, which
  *    rounds each addition of 16 terms down (1.6e-7 of 20,000 terms of one sign, less of others).
- *    Products of fp32 operands leave out less than 2^-24 of
- *    a term; infinities, NaN and values of any magnitude are treated as fp32 arithmetic does. What is
- *    not finite in one group reaches no row of another. Results that are not finite, and fp32 ones
- *    whose sums pass 2^96, are formed a second time, one by one: correct, but slow.
+ *    Products of fp32 operands leave out less than 2^-24 of a term; infinities, NaN and values of any
+ *    magnitude are treated as fp32 arithmetic does. What is not finite in one group reaches no row of
+ *    another. Results that are not finite, of fp32 and of adapters, and fp32 ones whose sums pass
+ *    2^96, are formed a second time, one by one: correct, but slow.
  *  - x, y, dx, dy are rows: element (i, c) at [i * stride + c], stride >= width. Other tensors are
  *    contiguous. Any width, stride and alignment of the element works; widths and strides that
  *    are multiples of 64 bytes with pointers on 64-byte boundaries are the fastest, of 16 the next.
