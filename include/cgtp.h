@@ -464,6 +464,98 @@ int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups, int n_in, 
                              int64_t dy_stride, void *dx, int64_t dx_stride, void *da, void *db,
                              void *workspace, size_t ws_bytes, void *stream);
 
+/* Routing of rows to experts: which top_k of n_experts a row has, and with what weights. The ids of all rows,
+ * read as [n_rows top_k], are those that cgtp_group_rows orders; the layers below then run over these pairs, and
+ * cgtp_mix_rows joins the results of each row.
+ *   logits  [n_rows][n_experts]. An expert whose logit is -inf or NaN is not available to the row.
+ *   score   CGTP_SCORE_SOFTMAX: s = softmax of the row's available logits; CGTP_SCORE_SIGMOID: s = 1 / (1 + exp(-l)).
+ *   bias    [n_experts] fp32 or NULL (0): key = s + bias decides the choice, and nothing else. Keys that are not
+ *           above -inf are not available.
+ *   n_blocks  blocks of n_experts / n_blocks consecutive experts, of which the keep_blocks with the largest sum of
+ *           their two largest keys (of one, where there is one) are left; 1 <= keep_blocks <= n_blocks <=
+ *           CGTP_MAX_ROUTE_BLOCKS. keep_blocks = n_blocks: all are left.
+ *   ids     [n_rows][top_k] int32: the experts of the largest keys, largest first, the lowest expert among equals;
+ *           -1 where no expert is left. Keys are compared as the formula gives them in 64 bits; without a bias
+ *           and blocks they are the logits.
+ *   weights [n_rows][top_k] fp32: scale s, or scale s / (sum of the row's chosen s) where renormalize is 1; 0 beside
+ *           -1. Softmax scores of a row that holds NaN or +inf are NaN.
+ * 1 <= top_k <= CGTP_MAX_TOP_K, and no more than the experts left; n_rows top_k < 2^31; n_experts <= CGTP_MAX_GROUPS.
+ * Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
+#define CGTP_MAX_TOP_K 64
+#define CGTP_MAX_ROUTE_BLOCKS 64
+#define CGTP_SCORE_SOFTMAX 0
+#define CGTP_SCORE_SIGMOID 1
+int cgtp_route_rows(int dtype, int64_t n_rows, int n_experts, int top_k, const void *logits,
+                    int64_t logits_stride, const float *bias, int score, int n_blocks,
+                    int keep_blocks, int renormalize, float scale, int32_t *ids, float *weights,
+                    void *stream);
+
+/* Its gradient, the choice held: dlogits [n_rows][n_experts] from dweights [n_rows][top_k] fp32 and the ids of the
+ * forward call, with the same logits, score, renormalize and scale. With u = dweights and sums over the chosen:
+ *   softmax:               dl_e = scale s_e (u_e - sum_i u_i s_i), u_e = 0 for those not chosen;
+ *   softmax, renormalised: dl_e = scale p_e (u_e - sum_i u_i p_i), p = s / sum of the chosen s; 0 if not chosen;
+ *   sigmoid:               dl_e = scale s_e (1 - s_e) u_e;
+ *   sigmoid, renormalised: dl_e = scale p_e (1 - s_e) (u_e - sum_i u_i p_i).
+ * An id outside [0, n_experts), or of an expert that is not available, has no part in it. Errors: CGTP_ERR_ARG,
+ * CGTP_ERR_HIP. */
+int cgtp_route_rows_grad(int dtype, int64_t n_rows, int n_experts, int top_k, const void *logits,
+                         int64_t logits_stride, const int32_t *ids, const float *dweights,
+                         int score, int renormalize, float scale, void *dlogits,
+                         int64_t dlogits_stride, void *stream);
+
+/* A layer of grouped rows: z_i = w[g]^T x_t + bias[g], y_i = act(z_i) + residual_i, with g = g(i), t = i / per_row
+ * (integer division): per_row consecutive rows share a row of x, as the experts of a routed row do. For a row of
+ * no group z_i = 0 and y_i = residual_i (0 without one).
+ *   x [n_rows / per_row][n_in], w [n_groups][n_in][n_out], bias [n_groups][n_out] or NULL (0),
+ *   residual [n_rows][n_out] or NULL (0), y [n_rows][n_out], z [n_rows][n_out] or NULL (not kept).
+ *   activation  CGTP_ACT_NONE: z; CGTP_ACT_SILU: z / (1 + exp(-z)); CGTP_ACT_GELU: z P(z), P the normal
+ *           distribution function; CGTP_ACT_RELU: max(z, 0), NaN where z is.
+ * Everything after the product is fp32 and rounded once: the activation takes z before it is rounded. n_rows is a
+ * multiple of per_row, 1 <= per_row <= CGTP_MAX_PER_ROW. Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
+#define CGTP_MAX_PER_ROW 64
+#define CGTP_ACT_NONE 0
+#define CGTP_ACT_SILU 1
+#define CGTP_ACT_GELU 2
+#define CGTP_ACT_RELU 3
+int cgtp_grouped_layer(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out, int per_row,
+                       const int32_t *offsets, const int32_t *order, const void *x,
+                       int64_t x_stride, const void *w, const void *bias, int activation,
+                       const void *residual, int64_t residual_stride, void *y, int64_t y_stride,
+                       void *z, int64_t z_stride, void *stream);
+
+/* Its gradients, from dy [n_rows][n_out] and the z of the forward call (that of the residual is dy itself). With
+ * dz_i = dy_i act'(z_i), for CGTP_BF16 rounded to bf16 as the products' operand:
+ *   dx_t     = sum over the rows i of t of w[g(i)] dz_i  [n_rows / per_row][n_in], summed in fp32;
+ *   dw[g]    = sum over the rows of g of x_t dz_i^T      [n_groups][n_in][n_out];
+ *   dbias[g] = sum over the rows of g of dz_i            [n_groups][n_out].
+ * Any of the three may be NULL (not all); x is needed for dw alone, w for dx alone, z unless the activation is
+ * CGTP_ACT_NONE. Rows of no group have no part, and groups without rows get 0. Where per_row is above 1, order has
+ * to hold every row, as cgtp_group_rows makes it, for dx to be defined. Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE,
+ * CGTP_ERR_HIP. */
+int cgtp_grouped_layer_grad_bytes(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                                  int per_row, int activation, size_t *bytes);
+int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
+                            int per_row, const int32_t *offsets, const int32_t *order,
+                            const void *x, int64_t x_stride, const void *w, const void *z,
+                            int64_t z_stride, int activation, const void *dy, int64_t dy_stride,
+                            void *dx, int64_t dx_stride, void *dw, void *dbias, void *workspace,
+                            size_t ws_bytes, void *stream);
+
+/* Rows joined: out_t = residual_t + sum over j < per_row of weights[t][j] y_(t per_row + j).
+ *   y [n_rows per_row][width], weights [n_rows][per_row] fp32 or NULL (1), residual [n_rows][width] or NULL (0),
+ *   out [n_rows][width]. n_rows per_row < 2^31, 1 <= per_row <= CGTP_MAX_PER_ROW.
+ * Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
+int cgtp_mix_rows(int dtype, int64_t n_rows, int per_row, int width, const void *y,
+                  int64_t y_stride, const float *weights, const void *residual,
+                  int64_t residual_stride, void *out, int64_t out_stride, void *stream);
+
+/* Its gradients, from dout [n_rows][width] (that of the residual is dout itself):
+ *   dy_(t per_row + j) = weights[t][j] dout_t, dweights[t][j] = y_(t per_row + j) . dout_t (fp32).
+ * dy or dweights may be NULL (not both); y is needed for dweights alone. Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
+int cgtp_mix_rows_grad(int dtype, int64_t n_rows, int per_row, int width, const void *dout,
+                       int64_t dout_stride, const float *weights, const void *y, int64_t y_stride,
+                       void *dy, int64_t dy_stride, float *dweights, void *stream);
+
 /* AdamW over many tensors in one launch. For every element, in fp32 with each operation rounded
  * (no fused multiply-add), g = grad * grad_scale[0]:
  *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2,
@@ -505,6 +597,15 @@ int cgtp_adamw_step(cgtp_adamw handle, double lr, double beta1, double beta2, do
  * are HOST arrays of one device pointer per tensor, [n] fp32 each.
  * Errors: CGTP_ERR_ARG (also for 32-bit states), CGTP_ERR_HIP. */
 int cgtp_adamw_states(cgtp_adamw handle, float *const *m_out, float *const *v_out, void *stream);
+/* The norm of the gradients of all tensors, read where they lie, and the factor that clips it:
+ *   norm  = |grad_scale[0]| sqrt(sum of squares), in 64 bits, rounded once to fp32;
+ *   scale = grad_scale[0] min(1, max_norm / norm): the grad_scale of the cgtp_adamw_step that follows; grad_scale[0]
+ *           where the norm is NaN.
+ * norm, scale: device floats, either may be NULL (not both). grad_scale: device float, or NULL (1); it may be scale
+ * itself. max_norm > 0. Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
+int cgtp_adamw_grad_norm_bytes(cgtp_adamw handle, size_t *bytes);
+int cgtp_adamw_grad_norm(cgtp_adamw handle, double max_norm, const float *grad_scale, float *norm,
+                         float *scale, void *workspace, size_t ws_bytes, void *stream);
 /* Synchronises the device; NULL is a no-op. */
 int cgtp_adamw_destroy(cgtp_adamw handle);
 

@@ -42,6 +42,15 @@ CGTP_MAX_GROUPS = 4096
 CGTP_MAX_WIDTH = 65536
 CGTP_MAX_ADAPTER_RANK = 64
 CGTP_ADAMW_BLOCK = 256
+CGTP_MAX_TOP_K = 64
+CGTP_MAX_ROUTE_BLOCKS = 64
+CGTP_SCORE_SOFTMAX = 0
+CGTP_SCORE_SIGMOID = 1
+CGTP_MAX_PER_ROW = 64
+CGTP_ACT_NONE = 0
+CGTP_ACT_SILU = 1
+CGTP_ACT_GELU = 2
+CGTP_ACT_RELU = 3
 
 EXPORTED = ("cgtp_plan_create", "cgtp_plan_grid", "cgtp_workspace_bytes", "cgtp_onsite",
             "cgtp_message_pass", "cgtp_message_pass_two_slot", "cgtp_workspace_bytes_general",
@@ -53,7 +62,10 @@ EXPORTED = ("cgtp_plan_create", "cgtp_plan_grid", "cgtp_workspace_bytes", "cgtp_
             "cgtp_grouped_linear", "cgtp_grouped_linear_grad_bytes", "cgtp_grouped_linear_grad",
             "cgtp_adapter_linear_bytes", "cgtp_adapter_linear", "cgtp_adapter_linear_grad_bytes",
             "cgtp_adapter_linear_grad", "cgtp_adamw_create", "cgtp_adamw_step",
-            "cgtp_adamw_states", "cgtp_adamw_destroy")
+            "cgtp_adamw_states", "cgtp_adamw_destroy", "cgtp_route_rows", "cgtp_route_rows_grad",
+            "cgtp_grouped_layer", "cgtp_grouped_layer_grad_bytes", "cgtp_grouped_layer_grad",
+            "cgtp_mix_rows", "cgtp_mix_rows_grad", "cgtp_adamw_grad_norm_bytes",
+            "cgtp_adamw_grad_norm")
 CGTP_NOALLOC_SCRATCH_BYTES = 64 << 20
 ONSITE_STAGES = ("contract_operands", "grid_product_curl_analysis", "project")
 ONSITE_GENERAL_STAGES = ("contract_a", "contract_b", "grid_product_curl_analysis",
@@ -139,12 +151,25 @@ def load_library(path: str = LIB_PATH):
     lib.cgtp_adamw_step.argtypes = [vp] + [f64] * 5 + [i64, vp, vp]
     lib.cgtp_adamw_states.argtypes = [vp] * 4
     lib.cgtp_adamw_destroy.argtypes = [vp]
+    lib.cgtp_adamw_grad_norm_bytes.argtypes = [vp, szp]
+    lib.cgtp_adamw_grad_norm.argtypes = [vp, f64, vp, vp, vp, vp, sz, vp]
+    f32, routed = ctypes.c_float, [i32, i64, i32, i32]   # dtype, n_rows, n_experts, top_k
+    lib.cgtp_route_rows.argtypes = routed + [vp, i64, vp, i32, i32, i32, i32, f32, vp, vp, vp]
+    lib.cgtp_route_rows_grad.argtypes = routed + [vp, i64, vp, vp, i32, i32, f32, vp, i64, vp]
+    layer = rows + [i32]                          # per_row
+    lib.cgtp_grouped_layer.argtypes = layer + [vp] * 3 + [i64, vp, vp, i32, vp, i64, vp, i64, vp, i64, vp]
+    lib.cgtp_grouped_layer_grad_bytes.argtypes = layer + [i32, szp]
+    lib.cgtp_grouped_layer_grad.argtypes = (layer + [vp] * 3 + [i64, vp, vp, i64, i32, vp, i64, vp, i64]
+                                            + [vp] * 3 + [sz, vp])
+    mixed = [i32, i64, i32, i32, vp, i64]         # dtype, n_rows, per_row, width, y or dout
+    lib.cgtp_mix_rows.argtypes = mixed + [vp, vp, i64, vp, i64, vp]
+    lib.cgtp_mix_rows_grad.argtypes = mixed + [vp, vp, i64, vp, i64, vp, vp]
     for name in ("cgtp_plan_create", "cgtp_plan_grid", "cgtp_workspace_bytes", "cgtp_onsite",
                  "cgtp_onsite_noalloc", "cgtp_gather_probe",
                  "cgtp_message_pass", "cgtp_message_pass_two_slot", "cgtp_stage_times",
                  "cgtp_destroy", "cgtp_host_tables", "cgtp_receiver_order",
                  "cgtp_plan_set_receiver_order", *(n for n in EXPORTED if n.startswith(
-                     ("cgtp_group", "cgtp_adapter", "cgtp_adamw")))):
+                     ("cgtp_group", "cgtp_adapter", "cgtp_adamw", "cgtp_route", "cgtp_mix")))):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -818,6 +843,182 @@ def adapter_linear_grad(x, w, a, b, dy, offsets, order=None, scale=None, dx=None
     return dx, da, db
 
 
+_SCORES = {"softmax": CGTP_SCORE_SOFTMAX, "sigmoid": CGTP_SCORE_SIGMOID}
+_ACTIVATIONS = {None: CGTP_ACT_NONE, "silu": CGTP_ACT_SILU, "gelu": CGTP_ACT_GELU, "relu": CGTP_ACT_RELU}
+
+
+def _choice(name, value, known):
+    try:
+        return known[value]
+    except (KeyError, TypeError):
+        raise ValueError(f"{name}: expected one of {list(known)}, got {value!r}") from None
+
+
+def _route_head(logits, top_k, score):
+    if logits.dim() != 2:
+        raise ValueError(f"logits: expected two dimensions, got {tuple(logits.shape)}")
+    load_library()
+    n, E = logits.shape
+    return (_row_dtype("logits", logits), n, E, top_k, _want_rows("logits", logits, n, E, logits),
+            _choice("score", score, _SCORES))
+
+
+def route_rows(logits, top_k: int, bias=None, score: str = "softmax", n_blocks: int = 1, keep_blocks=None,
+               renormalize: bool = True, scale: float = 1.0, ids=None, weights=None, stream=None):
+    """cgtp_route_rows: (ids [n, top_k] int32, weights [n, top_k] float32) of the experts that the rows of
+    logits [n, E] are routed to: by "softmax" or "sigmoid" scores, with bias [E] float32 added for the choice
+    alone, among the best keep_blocks (None: all) of n_blocks blocks of experts. ids.view(-1) is what group_rows
+    orders."""
+    torch = _torch()
+    dt, n, E, k, ls, code = _route_head(logits, top_k, score)
+    handle, side = _row_call(logits, stream)
+    if bias is not None:
+        _want_dev("bias", bias, (E,), torch.float32, logits)
+    shape = (n, max(k, 0))
+    if ids is None:
+        ids = _new(shape, torch.int32, logits)
+    if weights is None:
+        weights = _new(shape, torch.float32, logits)
+    _want_dev("ids", ids, shape, torch.int32, logits)
+    _want_dev("weights", weights, shape, torch.float32, logits)
+    _run("cgtp_route_rows", logits, side, (logits, bias, ids, weights), dt, n, E, k, _addr(logits), ls, _addr(bias), code,
+         n_blocks, n_blocks if keep_blocks is None else keep_blocks, int(bool(renormalize)), scale, _addr(ids),
+         _addr(weights), handle)
+    return ids, weights
+
+
+def route_rows_grad(logits, ids, dweights, score: str = "softmax", renormalize: bool = True, scale: float = 1.0,
+                    dlogits=None, stream=None):
+    """cgtp_route_rows_grad: dlogits [n, E] from dweights [n, top_k] float32, with the ids, logits and options of
+    the forward call."""
+    torch = _torch()
+    if ids.dim() != 2:
+        raise ValueError(f"ids: expected two dimensions, got {tuple(ids.shape)}")
+    dt, n, E, k, ls, code = _route_head(logits, ids.shape[1], score)
+    handle, side = _row_call(logits, stream)
+    _want_dev("ids", ids, (n, k), torch.int32, logits)
+    _want_dev("dweights", dweights, (n, k), torch.float32, logits)
+    if dlogits is None:
+        dlogits = _new((n, E), logits.dtype, logits)
+    ds = _want_rows("dlogits", dlogits, n, E, logits)
+    _run("cgtp_route_rows_grad", logits, side, (logits, ids, dweights, dlogits), dt, n, E, k, _addr(logits), ls, _addr(ids),
+         _addr(dweights), code, int(bool(renormalize)), scale, _addr(dlogits), ds, handle)
+    return dlogits
+
+
+def _layer_head(x, w, offsets, order, per_row):
+    if x.dim() != 2 or w.dim() != 3:
+        raise ValueError(f"x, w: expected 2 and 3 dimensions, got {tuple(x.shape)} and {tuple(w.shape)}")
+    load_library()
+    t, (n_in, n_out) = x.shape[0], w.shape[-2:]
+    n, G = t * per_row, offsets.shape[0] - 1
+    _want_order(offsets, order, n, G, x)
+    _want_dev("w", w, (G, n_in, n_out), x.dtype, x)
+    return _row_dtype("x", x), t, n, G, n_in, n_out, _want_rows("x", x, t, n_in, x)
+
+
+def grouped_layer(x, w, offsets, order=None, bias=None, activation=None, residual=None, per_row: int = 1, y=None,
+                  z=False, stream=None):
+    """cgtp_grouped_layer: y_i = act(w[g]^T x_t + bias[g]) + residual_i, g = g(i), t = i // per_row. x [t, n_in];
+    residual and y [t * per_row, n_out] rows, w [G, n_in, n_out], bias [G, n_out]; activation None, "silu", "gelu"
+    or "relu". offsets, order from group_rows over the t * per_row rows. With z None or a tensor, what the
+    activation took is kept and (y, z) returned."""
+    dt, t, n, G, n_in, n_out, xs = _layer_head(x, w, offsets, order, per_row)
+    act = _choice("activation", activation, _ACTIVATIONS)
+    handle, side = _row_call(x, stream)
+    if bias is not None:
+        _want_dev("bias", bias, (G, n_out), x.dtype, x)
+    rs = 0 if residual is None else _want_rows("residual", residual, n, n_out, x)
+    if y is None:
+        y = _new((n, n_out), x.dtype, x)
+    ys = _want_rows("y", y, n, n_out, x)
+    kept, zs = _grad_out("z", z, (n, n_out), x, True)
+    _run("cgtp_grouped_layer", x, side, (x, w, offsets, order, bias, residual, y, kept), dt, n, G, n_in, n_out, per_row,
+         _addr(offsets), _addr(order), _addr(x), xs, _addr(w), _addr(bias), act, _addr(residual), rs, _addr(y), ys,
+         _addr(kept), zs, handle)
+    return y if kept is None else (y, kept)
+
+
+def grouped_layer_grad(x, w, dy, offsets, order=None, z=None, activation=None, per_row: int = 1, dx=None, dw=None,
+                       dbias=None, workspace=None, stream=None):
+    """cgtp_grouped_layer_grad: (dx [t, n_in], dw [G, n_in, n_out], dbias [G, n_out]) from dy [t * per_row, n_out]
+    and the z that the forward call kept (not needed without an activation); an output given as False is skipped
+    (None in its place)."""
+    dt, t, n, G, n_in, n_out, xs = _layer_head(x, w, offsets, order, per_row)
+    act = _choice("activation", activation, _ACTIVATIONS)
+    dys = _want_rows("dy", dy, n, n_out, x)
+    if act == CGTP_ACT_NONE:
+        z, zs = None, 0
+    elif z is None:
+        raise ValueError("z: needed where there is an activation")
+    else:
+        zs = _want_rows("z", z, n, n_out, x)
+    handle, side = _row_call(x, stream)
+    dx, dxs = _grad_out("dx", dx, (t, n_in), x, True)
+    dw, _ = _grad_out("dw", dw, (G, n_in, n_out), x, False)
+    dbias, _ = _grad_out("dbias", dbias, (G, n_out), x, False)
+    need = _bytes("cgtp_grouped_layer_grad_bytes", dt, n, G, n_in, n_out, per_row, act)
+    ws_ptr, ws_len, ws = _row_workspace(workspace, need, x)
+    _run("cgtp_grouped_layer_grad", x, side, (x, w, dy, z, offsets, order, dx, dw, dbias, ws), dt, n, G, n_in, n_out, per_row,
+         _addr(offsets), _addr(order), _addr(x), xs, _addr(w), _addr(z), zs, act, _addr(dy), dys, _addr(dx), dxs,
+         _addr(dw), _addr(dbias), ws_ptr, ws_len, handle)
+    return dx, dw, dbias
+
+
+def _mix_rows_of(name, y, per_row):
+    if y.dim() != 2:
+        raise ValueError(f"{name}: expected two dimensions, got {tuple(y.shape)}")
+    if per_row < 1 or y.shape[0] % per_row != 0:
+        raise ValueError(f"{name}: {y.shape[0]} rows are no multiple of per_row {per_row}")
+    return y.shape[0] // per_row, y.shape[1]
+
+
+def mix_rows(y, per_row: int, weights=None, residual=None, out=None, stream=None):
+    """cgtp_mix_rows: out_t = residual_t + sum_j weights[t][j] y_(t per_row + j). y [t * per_row, width] rows,
+    weights [t, per_row] float32 or None (1), residual and out [t, width] rows."""
+    load_library()
+    n, width = _mix_rows_of("y", y, per_row)
+    dt, ys = _row_dtype("y", y), _want_rows("y", y, n * per_row, width, y)
+    handle, side = _row_call(y, stream)
+    if weights is not None:
+        _want_dev("weights", weights, (n, per_row), _torch().float32, y)
+    rs = 0 if residual is None else _want_rows("residual", residual, n, width, y)
+    if out is None:
+        out = _new((n, width), y.dtype, y)
+    outs = _want_rows("out", out, n, width, y)
+    _run("cgtp_mix_rows", y, side, (y, weights, residual, out), dt, n, per_row, width, _addr(y), ys, _addr(weights),
+         _addr(residual), rs, _addr(out), outs, handle)
+    return out
+
+
+def mix_rows_grad(dout, per_row: int, weights=None, y=None, dy=None, dweights=None, stream=None):
+    """cgtp_mix_rows_grad: (dy [t * per_row, width], dweights [t, per_row] float32) from dout [t, width]; an output
+    given as False is skipped (None in its place). dweights needs y."""
+    torch = _torch()
+    load_library()
+    if dout.dim() != 2:
+        raise ValueError(f"dout: expected two dimensions, got {tuple(dout.shape)}")
+    n, width = dout.shape
+    dt, ds = _row_dtype("dout", dout), _want_rows("dout", dout, n, width, dout)
+    handle, side = _row_call(dout, stream)
+    if weights is not None:
+        _want_dev("weights", weights, (n, per_row), torch.float32, dout)
+    dy, dys = _grad_out("dy", dy, (n * per_row, width), dout, True)
+    ys = 0
+    if dweights is False:
+        dweights = None
+    else:
+        if y is None:
+            raise ValueError("y: needed for dweights")
+        ys = _want_rows("y", y, n * per_row, width, dout)
+        if dweights is None:
+            dweights = _new((n, per_row), torch.float32, dout)
+        _want_dev("dweights", dweights, (n, per_row), torch.float32, dout)
+    _run("cgtp_mix_rows_grad", dout, side, (dout, weights, y, dy, dweights), dt, n, per_row, width, _addr(dout), ds,
+         _addr(weights), _addr(y) if dweights is not None else None, ys, _addr(dy), dys, _addr(dweights), handle)
+    return dy, dweights
+
+
 class AdamWTensors:
     """Owns a cgtp_adamw handle over lists of device tensors, which it keeps alive: params (float32),
     grads (all float32 or all bfloat16), the moments m and v (float32; or int8 and uint8 with the
@@ -866,6 +1067,9 @@ class AdamWTensors:
             _check(load_library().cgtp_adamw_create(n, table, code, bits, ctypes.byref(h)),
                    "cgtp_adamw_create")
         self.handle = h
+        need = ctypes.c_size_t()
+        _check(load_library().cgtp_adamw_grad_norm_bytes(h, ctypes.byref(need)), "cgtp_adamw_grad_norm_bytes")
+        self.norm_bytes = need.value
 
     def close(self):
         if getattr(self, "handle", None):
@@ -910,3 +1114,26 @@ def adamw_states(tensors: AdamWTensors, m_out=None, v_out=None, stream=None):
     arrays = [(ctypes.c_void_p * len(o))(*[t.data_ptr() for t in o]) for o in outs]
     _run("cgtp_adamw_states", first, side, (*outs[0], *outs[1]), tensors.handle, arrays[0], arrays[1], handle)
     return outs[0], outs[1]
+
+
+def adamw_grad_norm(tensors: AdamWTensors, max_norm: float, grad_scale=None, norm=None, scale=None, workspace=None,
+                    stream=None):
+    """cgtp_adamw_grad_norm: (norm, scale), device float32 tensors of one element: the norm of all gradients of the
+    handle times |grad_scale|, and grad_scale min(1, max_norm / norm), the grad_scale of the adamw call that
+    follows. An output given as False is skipped (None in its place)."""
+    torch = _torch()
+    first = tensors._keep[0][0]
+    handle, side = _row_call(first, stream)
+    if grad_scale is not None:
+        _want_dev("grad_scale", grad_scale, (1,), torch.float32, first)
+    outs = []
+    for name, out in (("norm", norm), ("scale", scale)):
+        if out is None:
+            out = _new((1,), torch.float32, first)
+        if out is not False:
+            _want_dev(name, out, (1,), torch.float32, first)
+        outs.append(None if out is False else out)
+    ws_ptr, ws_len, ws = _row_workspace(workspace, tensors.norm_bytes, first)
+    _run("cgtp_adamw_grad_norm", first, side, (grad_scale, *outs, ws), tensors.handle, max_norm, _addr(grad_scale),
+         _addr(outs[0]), _addr(outs[1]), ws_ptr, ws_len, handle)
+    return tuple(outs)

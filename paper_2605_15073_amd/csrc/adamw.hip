@@ -217,6 +217,54 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const Tensor *__restrict__ t
     }
 }
 
+// The norm of all gradients: sums of squares in 64 bits (the square of an fp32 number is one of them, and none
+// passes their range), of each work item to its place in the workspace, then of those in their order.
+template <typename G>
+__global__ __launch_bounds__(kThreads) void k_grad_squares(const Tensor *__restrict__ tensors, const Item *__restrict__ items,
+                                                           double *__restrict__ sums)
+{
+    typedef G g4_t __attribute__((ext_vector_type(4)));
+    __shared__ double s_sum[kThreads / 64];
+    const Item item = items[blockIdx.x];
+    const Tensor &tn = tensors[item.tensor];
+    const G *const grad = (const G *)tn.t.grad;
+    const int64_t n = tn.t.n, start = (int64_t)item.start * CGTP_ADAMW_BLOCK;
+    double sum = 0;
+#pragma unroll
+    for (int it = 0; it < kItem / 1024; ++it) {
+        const int64_t i = start + it * 1024 + threadIdx.x * 4;
+        const g4_t g = load4<g4_t>(grad, i, n, tn.vec);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum = fma((double)(float)g[k], (double)(float)g[k], sum);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) sums[blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+}
+
+constexpr int kNormThreads = 1024;
+
+__global__ __launch_bounds__(kNormThreads) void k_grad_norm(const double *__restrict__ sums, int64_t n, double max_norm,
+                                                            const float *__restrict__ grad_scale, float *__restrict__ norm,
+                                                            float *__restrict__ scale)
+{
+    __shared__ double s_sum[kNormThreads / 64];
+    double sum = 0;
+    for (int64_t i = threadIdx.x; i < n; i += kNormThreads) sum += sums[i];
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    sum = 0;
+    for (int w = 0; w < kNormThreads / 64; ++w) sum += s_sum[w];
+    const double by = grad_scale ? grad_scale[0] : 1.f, all = sqrt(sum) * fabs(by);
+    if (norm) norm[0] = (float)all;
+    if (scale) scale[0] = (float)(all > max_norm ? by * (max_norm / all) : by);
+}
+
 struct Outs {
     float *m[kStatesMax], *v[kStatesMax];
 };
@@ -468,6 +516,49 @@ extern "C" int cgtp_adamw_states(cgtp_adamw a, float *const *m_out, float *const
         if (e != hipSuccess) return hip_fail(e, "adamw states");
     }
     return CGTP_OK;
+}
+
+namespace {
+
+size_t norm_bytes(const cgtp_adamw_s *a) { return sizeof(double) * (size_t)a->n_items; }
+
+}  // namespace
+
+extern "C" int cgtp_adamw_grad_norm_bytes(cgtp_adamw a, size_t *bytes)
+{
+    cgtp::clear_error();
+    if (!a) return report(CGTP_ERR_ARG, "handle is NULL");
+    if (!bytes) return report(CGTP_ERR_ARG, "bytes is NULL");
+    *bytes = norm_bytes(a);
+    return CGTP_OK;
+}
+
+extern "C" int cgtp_adamw_grad_norm(cgtp_adamw a, double max_norm, const float *grad_scale, float *norm, float *scale,
+                                    void *workspace, size_t ws_bytes, void *stream)
+{
+    cgtp::clear_error();
+    const int st = check_handle(a);
+    if (st != CGTP_OK) return st;
+    if (!(max_norm > 0)) return report(CGTP_ERR_ARG, "max_norm %g", max_norm);
+    if (!norm && !scale) return report(CGTP_ERR_ARG, "norm and scale are both NULL");
+    if (!aligned(norm, 4) || !aligned(scale, 4) || !aligned(grad_scale, 4))
+        return report(CGTP_ERR_ARG, "norm, scale or grad_scale is not 4-byte aligned");
+    const size_t need = norm_bytes(a);
+    if (need > 0 && !workspace) return report(CGTP_ERR_WORKSPACE, "no workspace, %zu bytes needed", need);
+    if (!aligned(workspace, 256)) return report(CGTP_ERR_ARG, "workspace %p is not 256-byte aligned", workspace);
+    if (ws_bytes < need) return report(CGTP_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, need);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    double *const sums = static_cast<double *>(workspace);
+    if (a->n_items > 0) {
+        auto *kernel = a->grad_dtype == CGTP_BF16 ? k_grad_squares<bf16_t> : k_grad_squares<float>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)a->n_items), dim3(kThreads), 0, s,
+                           static_cast<const Tensor *>(a->table), a->items, sums);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hip_fail(e, "gradient squares");
+    }
+    hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(kNormThreads), 0, s, sums, a->n_items, max_norm, grad_scale, norm, scale);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? CGTP_OK : hip_fail(e, "gradient norm");
 }
 
 extern "C" int cgtp_adamw_destroy(cgtp_adamw a)

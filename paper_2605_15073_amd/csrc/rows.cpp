@@ -418,3 +418,327 @@ extern "C" int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups,
     }
     return CGTP_OK;
 }
+
+// ---------------------------------------------------------------- layers, routing, joining
+
+namespace {
+
+int check_per_row(int64_t n_rows, int per_row)
+{
+    if (per_row < 1 || per_row > CGTP_MAX_PER_ROW)
+        return report(CGTP_ERR_ARG, "per_row %d outside [1, %d]", per_row, CGTP_MAX_PER_ROW);
+    if (n_rows % per_row != 0)
+        return report(CGTP_ERR_ARG, "n_rows %lld is no multiple of per_row %d", (long long)n_rows, per_row);
+    return CGTP_OK;
+}
+
+int check_activation(int activation)
+{
+    if (activation < CGTP_ACT_NONE || activation > CGTP_ACT_RELU)
+        return report(CGTP_ERR_ARG, "activation %d is not known", activation);
+    return CGTP_OK;
+}
+
+// dz where there is an activation, the row gradients in fp32 where rows share their input, and sums of the weight
+// gradients.
+struct LayerGradBytes {
+    size_t dz, rows, sums;
+    size_t all() const { return dz + rows + sums; }
+};
+
+LayerGradBytes layer_grad_bytes(int dtype, int64_t n, int G, int n_in, int n_out, int per_row, int activation)
+{
+    const size_t sums = cgtp::row_outer_bytes(dtype, n, G, n_in, n_out, true);
+    const size_t bare = cgtp::row_outer_bytes(dtype, n, G, 1, n_out, true);
+    return {activation == CGTP_ACT_NONE ? 0 : align256((size_t)n * n_out * elem(dtype)),
+            per_row == 1 ? 0 : align256((size_t)n * n_in * 4), sums > bare ? sums : bare};
+}
+
+int check_score(int score, int renormalize, float scale)
+{
+    if (score != CGTP_SCORE_SOFTMAX && score != CGTP_SCORE_SIGMOID)
+        return report(CGTP_ERR_ARG, "score %d is neither CGTP_SCORE_SOFTMAX nor CGTP_SCORE_SIGMOID", score);
+    if (renormalize != 0 && renormalize != 1) return report(CGTP_ERR_ARG, "renormalize %d is neither 0 nor 1", renormalize);
+    if (!__builtin_isfinite(scale)) return report(CGTP_ERR_ARG, "scale %g is not finite", scale);
+    return CGTP_OK;
+}
+
+int check_route(int dtype, int64_t n_rows, int n_experts, int top_k)
+{
+    CGTP_TRY(check_sizes(dtype, n_rows, n_experts, 1, 1));
+    if (top_k < 1 || top_k > CGTP_MAX_TOP_K || top_k > n_experts)
+        return report(CGTP_ERR_ARG, "top_k %d outside [1, %d] or above %d experts", top_k, CGTP_MAX_TOP_K, n_experts);
+    if (n_rows * top_k > 0x7fffffffLL)
+        return report(CGTP_ERR_ARG, "%lld rows of %d experts: 2^31 pairs or more", (long long)n_rows, top_k);
+    return CGTP_OK;
+}
+
+}  // namespace
+
+extern "C" int cgtp_route_rows(int dtype, int64_t n_rows, int n_experts, int top_k, const void *logits,
+                               int64_t logits_stride, const float *bias, int score, int n_blocks, int keep_blocks,
+                               int renormalize, float scale, int32_t *ids, float *weights, void *stream)
+{
+    cgtp::clear_error();
+    CGTP_TRY(check_route(dtype, n_rows, n_experts, top_k));
+    CGTP_TRY(check_score(score, renormalize, scale));
+    if (n_blocks < 1 || n_blocks > CGTP_MAX_ROUTE_BLOCKS || n_experts % n_blocks != 0)
+        return report(CGTP_ERR_ARG, "n_blocks %d outside [1, %d] or no divisor of %d experts", n_blocks,
+                      CGTP_MAX_ROUTE_BLOCKS, n_experts);
+    if (keep_blocks < 1 || keep_blocks > n_blocks)
+        return report(CGTP_ERR_ARG, "keep_blocks %d outside [1, %d]", keep_blocks, n_blocks);
+    if (top_k > n_experts / n_blocks * keep_blocks)
+        return report(CGTP_ERR_ARG, "top_k %d above the %d experts of the blocks kept", top_k,
+                      n_experts / n_blocks * keep_blocks);
+    if (n_rows == 0) return CGTP_OK;
+    CGTP_TRY(check_rows(logits, "logits", logits_stride, n_experts, n_rows, elem(dtype)));
+    if (bias) CGTP_TRY(check_ptr(bias, "bias", 4));
+    CGTP_TRY(check_ptr(ids, "ids", 4));
+    CGTP_TRY(check_ptr(weights, "weights", 4));
+    cgtp::RowRoute p{};
+    p.n = n_rows;
+    p.E = n_experts;
+    p.k = top_k;
+    p.logits = logits;
+    p.stride = logits_stride;
+    p.bias = bias;
+    p.score = score;
+    p.blocks = keep_blocks == n_blocks ? 1 : n_blocks;  // all are kept
+    p.keep = keep_blocks;
+    p.renorm = renormalize != 0;
+    p.scale = scale;
+    p.ids = ids;
+    p.weights = weights;
+    const hipError_t e = cgtp::launch_route_rows(dtype, p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? CGTP_OK : hip_fail(e, "route");
+}
+
+extern "C" int cgtp_route_rows_grad(int dtype, int64_t n_rows, int n_experts, int top_k, const void *logits,
+                                    int64_t logits_stride, const int32_t *ids, const float *dweights, int score,
+                                    int renormalize, float scale, void *dlogits, int64_t dlogits_stride, void *stream)
+{
+    cgtp::clear_error();
+    CGTP_TRY(check_route(dtype, n_rows, n_experts, top_k));
+    CGTP_TRY(check_score(score, renormalize, scale));
+    if (n_rows == 0) return CGTP_OK;
+    const size_t es = elem(dtype);
+    CGTP_TRY(check_rows(logits, "logits", logits_stride, n_experts, n_rows, es));
+    CGTP_TRY(check_ptr(ids, "ids", 4));
+    CGTP_TRY(check_ptr(dweights, "dweights", 4));
+    CGTP_TRY(check_rows(dlogits, "dlogits", dlogits_stride, n_experts, n_rows, es));
+    cgtp::RowRoute p{};
+    p.n = n_rows;
+    p.E = n_experts;
+    p.k = top_k;
+    p.logits = logits;
+    p.stride = logits_stride;
+    p.score = score;
+    p.renorm = renormalize != 0;
+    p.scale = scale;
+    p.ids = const_cast<int32_t *>(ids);
+    p.dweights = dweights;
+    p.dlogits = dlogits;
+    p.dstride = dlogits_stride;
+    const hipError_t e = cgtp::launch_route_rows_grad(dtype, p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? CGTP_OK : hip_fail(e, "route gradient");
+}
+
+extern "C" int cgtp_grouped_layer(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out, int per_row,
+                                  const int32_t *offsets, const int32_t *order, const void *x, int64_t x_stride,
+                                  const void *w, const void *bias, int activation, const void *residual,
+                                  int64_t residual_stride, void *y, int64_t y_stride, void *z, int64_t z_stride,
+                                  void *stream)
+{
+    cgtp::clear_error();
+    CGTP_TRY(check_sizes(dtype, n_rows, n_groups, n_in, n_out));
+    CGTP_TRY(check_per_row(n_rows, per_row));
+    CGTP_TRY(check_activation(activation));
+    if (n_rows == 0) return CGTP_OK;
+    const size_t es = elem(dtype);
+    CGTP_TRY(check_order(offsets, order));
+    CGTP_TRY(check_rows(x, "x", x_stride, n_in, n_rows, es));
+    CGTP_TRY(check_ptr(w, "w", es));
+    if (bias) CGTP_TRY(check_ptr(bias, "bias", es));
+    if (residual) CGTP_TRY(check_rows(residual, "residual", residual_stride, n_out, n_rows, es));
+    CGTP_TRY(check_rows(y, "y", y_stride, n_out, n_rows, es));
+    if (z) CGTP_TRY(check_rows(z, "z", z_stride, n_out, n_rows, es));
+    cgtp::RowProduct p{};
+    p.in = x;
+    p.in_stride = x_stride;
+    p.K = n_in;
+    p.w = w;
+    p.w_group = (int64_t)n_in * n_out;
+    p.N = n_out;
+    p.out = y;
+    p.out_stride = y_stride;
+    p.per = per_row;
+    p.bias = bias;
+    p.act = activation;
+    p.residual = residual;
+    p.residual_stride = residual_stride;
+    p.z = z;
+    p.z_stride = z_stride;
+    const hipError_t e = cgtp::launch_row_product(dtype, {n_rows, n_groups, offsets, order}, p,
+                                                  static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? CGTP_OK : hip_fail(e, "grouped layer");
+}
+
+extern "C" int cgtp_grouped_layer_grad_bytes(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out, int per_row,
+                                             int activation, size_t *bytes)
+{
+    cgtp::clear_error();
+    CGTP_TRY(check_sizes(dtype, n_rows, n_groups, n_in, n_out));
+    CGTP_TRY(check_per_row(n_rows, per_row));
+    CGTP_TRY(check_activation(activation));
+    if (!bytes) return report(CGTP_ERR_ARG, "bytes is NULL");
+    *bytes = layer_grad_bytes(dtype, n_rows, n_groups, n_in, n_out, per_row, activation).all();
+    return CGTP_OK;
+}
+
+extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out, int per_row,
+                                       const int32_t *offsets, const int32_t *order, const void *x, int64_t x_stride,
+                                       const void *w, const void *z, int64_t z_stride, int activation, const void *dy,
+                                       int64_t dy_stride, void *dx, int64_t dx_stride, void *dw, void *dbias,
+                                       void *workspace, size_t ws_bytes, void *stream)
+{
+    cgtp::clear_error();
+    CGTP_TRY(check_sizes(dtype, n_rows, n_groups, n_in, n_out));
+    CGTP_TRY(check_per_row(n_rows, per_row));
+    CGTP_TRY(check_activation(activation));
+    if (!dw && !dbias && n_rows == 0) return CGTP_OK;
+    if (!dx && !dw && !dbias) return report(CGTP_ERR_ARG, "dx, dw and dbias are all NULL");
+    const size_t es = elem(dtype);
+    CGTP_TRY(check_order(offsets, order));
+    CGTP_TRY(check_rows(dy, "dy", dy_stride, n_out, n_rows, es));
+    if (activation != CGTP_ACT_NONE) CGTP_TRY(check_rows(z, "z", z_stride, n_out, n_rows, es));
+    if (dx) {
+        CGTP_TRY(check_ptr(w, "w", es));
+        CGTP_TRY(check_rows(dx, "dx", dx_stride, n_in, n_rows, es));
+    }
+    if (dw) {
+        CGTP_TRY(check_rows(x, "x", x_stride, n_in, n_rows, es));
+        CGTP_TRY(check_ptr(dw, "dw", es));
+    }
+    if (dbias) CGTP_TRY(check_ptr(dbias, "dbias", es));
+    const LayerGradBytes need = layer_grad_bytes(dtype, n_rows, n_groups, n_in, n_out, per_row, activation);
+    CGTP_TRY(check_ws(workspace, ws_bytes, need.all()));
+    const cgtp::RowOrder o{n_rows, n_groups, offsets, order};
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    char *const dz = static_cast<char *>(workspace), *const rows = dz + need.dz, *const sums = rows + need.rows;
+    hipError_t e;
+    const void *b = dy;
+    int64_t b_stride = dy_stride;
+    if (activation != CGTP_ACT_NONE && n_rows > 0) {
+        e = cgtp::launch_layer_dz(dtype, n_rows, n_out, activation, dy, dy_stride, z, z_stride, dz, s);
+        if (e != hipSuccess) return hip_fail(e, "activation's gradient");
+        b = dz;
+        b_stride = n_out;
+    }
+    if (dx && n_rows > 0) {
+        cgtp::RowProduct p{};
+        p.in = b;
+        p.in_stride = b_stride;
+        p.K = n_out;
+        p.w = w;
+        p.w_group = (int64_t)n_in * n_out;
+        p.w_nk = true;
+        p.N = n_in;
+        p.out = per_row > 1 ? rows : dx;
+        p.out_stride = per_row > 1 ? n_in : dx_stride;
+        p.out_f32 = per_row > 1 && dtype == CGTP_BF16;
+        e = cgtp::launch_row_product(dtype, o, p, s);
+        if (e != hipSuccess) return hip_fail(e, "row gradient");
+        if (per_row > 1) {
+            cgtp::RowMix m{};
+            m.n = n_rows / per_row;
+            m.k = per_row;
+            m.N = n_in;
+            m.y = rows;
+            m.y_stride = n_in;
+            m.out = dx;
+            m.out_stride = dx_stride;
+            e = cgtp::launch_mix_rows(dtype, m, true, s);
+            if (e != hipSuccess) return hip_fail(e, "row gradient's sum");
+        }
+    }
+    if (dw || dbias) {
+        cgtp::RowOuter q{};
+        q.a = dw ? x : b;
+        q.a_stride = dw ? x_stride : b_stride;
+        q.A = dw ? n_in : 1;  // no products are asked for: those with b's first column, which are not stored
+        q.b = b;
+        q.b_stride = b_stride;
+        q.B = n_out;
+        q.out = dw;
+        q.per = dw ? per_row : 1;
+        q.sums = dbias;
+        e = cgtp::launch_row_outer(dtype, o, q, sums, s);
+        if (e != hipSuccess) return hip_fail(e, "weight gradient");
+    }
+    return CGTP_OK;
+}
+
+extern "C" int cgtp_mix_rows(int dtype, int64_t n_rows, int per_row, int width, const void *y, int64_t y_stride,
+                             const float *weights, const void *residual, int64_t residual_stride, void *out,
+                             int64_t out_stride, void *stream)
+{
+    cgtp::clear_error();
+    CGTP_TRY(check_sizes(dtype, n_rows, 1, width, width));
+    CGTP_TRY(check_per_row(0, per_row));
+    if (n_rows * per_row > 0x7fffffffLL)
+        return report(CGTP_ERR_ARG, "%lld times %d rows: 2^31 or more", (long long)n_rows, per_row);
+    if (n_rows == 0) return CGTP_OK;
+    const size_t es = elem(dtype);
+    CGTP_TRY(check_rows(y, "y", y_stride, width, n_rows, es));
+    if (weights) CGTP_TRY(check_ptr(weights, "weights", 4));
+    if (residual) CGTP_TRY(check_rows(residual, "residual", residual_stride, width, n_rows, es));
+    CGTP_TRY(check_rows(out, "out", out_stride, width, n_rows, es));
+    cgtp::RowMix p{};
+    p.n = n_rows;
+    p.k = per_row;
+    p.N = width;
+    p.y = y;
+    p.y_stride = y_stride;
+    p.weights = weights;
+    p.residual = residual;
+    p.residual_stride = residual_stride;
+    p.out = out;
+    p.out_stride = out_stride;
+    const hipError_t e = cgtp::launch_mix_rows(dtype, p, false, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? CGTP_OK : hip_fail(e, "mix");
+}
+
+extern "C" int cgtp_mix_rows_grad(int dtype, int64_t n_rows, int per_row, int width, const void *dout,
+                                  int64_t dout_stride, const float *weights, const void *y, int64_t y_stride, void *dy,
+                                  int64_t dy_stride, float *dweights, void *stream)
+{
+    cgtp::clear_error();
+    CGTP_TRY(check_sizes(dtype, n_rows, 1, width, width));
+    CGTP_TRY(check_per_row(0, per_row));
+    if (n_rows * per_row > 0x7fffffffLL)
+        return report(CGTP_ERR_ARG, "%lld times %d rows: 2^31 or more", (long long)n_rows, per_row);
+    if (n_rows == 0) return CGTP_OK;
+    if (!dy && !dweights) return report(CGTP_ERR_ARG, "dy and dweights are both NULL");
+    const size_t es = elem(dtype);
+    CGTP_TRY(check_rows(dout, "dout", dout_stride, width, n_rows, es));
+    if (weights) CGTP_TRY(check_ptr(weights, "weights", 4));
+    if (dweights) {
+        CGTP_TRY(check_rows(y, "y", y_stride, width, n_rows, es));
+        CGTP_TRY(check_ptr(dweights, "dweights", 4));
+    }
+    if (dy) CGTP_TRY(check_rows(dy, "dy", dy_stride, width, n_rows, es));
+    cgtp::RowMixGrad p{};
+    p.n = n_rows;
+    p.k = per_row;
+    p.N = width;
+    p.dout = dout;
+    p.dout_stride = dout_stride;
+    p.weights = weights;
+    p.y = y;
+    p.y_stride = y_stride;
+    p.dy = dy;
+    p.dy_stride = dy_stride;
+    p.dweights = dweights;
+    const hipError_t e = cgtp::launch_mix_rows_grad(dtype, p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? CGTP_OK : hip_fail(e, "mix gradient");
+}

@@ -44,6 +44,16 @@ struct RowProduct {
     int r;
     bool narrow;       // out is a narrow product: in sequence order, fp32 [n][N]
     const float *narrow_scale;  // its factor per group, or NULL
+    // layers (rows_layer.h): row i is of input row i / per, out_i = act(in W_g + bias_g) + residual_i, and z_i,
+    // if not NULL, what the activation took. 0: a plain product.
+    int per;
+    const void *bias;  // [G][N], or NULL
+    int act;           // CGTP_ACT_*
+    const void *residual;  // or NULL
+    int64_t residual_stride;
+    void *z;
+    int64_t z_stride;
+    bool out_f32;      // row gradients of rows that share their input: out is fp32 whatever the type
 };
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
 // The form for short inputs and wide outputs (rows_wide.hip), and whether it covers a product.
@@ -74,8 +84,10 @@ struct RowOuter {
     int r;
     bool transposed;
     void *out;
+    int per;     // row i of the order is row i / per of a; 0: row i
+    void *sums;  // if not NULL: the sum over the rows of group g of b_i, [G][B], beside out
 };
-size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B);
+size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B, bool sums = false);
 hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &p, void *ws,
                             hipStream_t s);
 // The forms for groups of few rows (rows_few.hip), up to kFewMean on the mean, and whether that of products
@@ -85,6 +97,56 @@ bool row_few_takes(int dtype, const RowOrder &o, const RowProduct &p);
 hipError_t launch_row_few(const RowOrder &o, const RowProduct &p, hipStream_t s);
 hipError_t launch_row_outer_few(int dtype, const RowOrder &o, const RowOuter &q, hipStream_t s);
 size_t narrow_bytes(int dtype, int64_t n_rows, int N);
+
+// dz_i = dy_i act'(z_i), rows of N values at a stride of N.
+hipError_t launch_layer_dz(int dtype, int64_t n, int N, int act, const void *dy, int64_t dy_stride, const void *z,
+                           int64_t z_stride, void *dz, hipStream_t s);
+
+// Row t of out (n rows) from rows t k .. t k + k - 1 of y, with a weight each.
+struct RowMix {
+    int64_t n;
+    int k, N;
+    const void *y;          // [n k][N]
+    int64_t y_stride;
+    const float *weights;   // [n][k], or NULL: 1
+    const void *residual;   // [n][N], or NULL
+    int64_t residual_stride;
+    void *out;
+    int64_t out_stride;
+};
+// y_f32: y is fp32 whatever the type of out.
+hipError_t launch_mix_rows(int dtype, const RowMix &p, bool y_f32, hipStream_t s);
+struct RowMixGrad {
+    int64_t n;
+    int k, N;
+    const void *dout;
+    int64_t dout_stride;
+    const float *weights;  // or NULL
+    const void *y;         // for dweights
+    int64_t y_stride;
+    void *dy;              // or NULL
+    int64_t dy_stride;
+    float *dweights;       // or NULL
+};
+hipError_t launch_mix_rows_grad(int dtype, const RowMixGrad &p, hipStream_t s);
+
+struct RowRoute {
+    int64_t n;
+    int E, k;
+    const void *logits;
+    int64_t stride;
+    const float *bias;
+    int score, blocks, keep;
+    bool renorm;
+    float scale;
+    int32_t *ids;      // written by the choice, read by the gradient
+    float *weights;    // the choice's
+    const float *dweights;
+    void *dlogits;
+    int64_t dstride;
+};
+hipError_t launch_route_rows(int dtype, const RowRoute &p, hipStream_t s);
+hipError_t launch_route_rows_grad(int dtype, const RowRoute &p, hipStream_t s);
 
 }  // namespace cgtp
 

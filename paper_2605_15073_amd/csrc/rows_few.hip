@@ -219,13 +219,15 @@ __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter
     float acc[kOuterA];
 #pragma unroll
     for (int i = 0; i < kOuterA; ++i) acc[i] = 0.f;
+    float column = 0.f;  // b's own sum
     for (int64_t p0 = start; p0 < end; p0 += kOuterRows) {
         const int rows = end - p0 < kOuterRows ? (int)(end - p0) : kOuterRows;
         if (p0 > start) __syncthreads();
         if (tid < kOuterRows) s_row[tid] = tid < rows ? row_at(o, p0 + tid) : -1;
         __syncthreads();
         for (int i = tid; i < rows * kA; i += kThreads) {
-            const int r = i / kA, a = i % kA, row = s_row[r];
+            const int r = i / kA, a = i % kA, own = s_row[r];
+            const int row = q.per > 1 && own >= 0 ? (int)((unsigned)own / (unsigned)q.per) : own;
             reinterpret_cast<float *>(&s_a[r])[a] =
                 row >= 0 && a0 + a < q.A ? (float)static_cast<const T *>(q.a)[row * q.a_stride + a0 + a] : 0.f;
         }
@@ -243,6 +245,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 if (r0 + u >= rows) break;
+                column += f[u];
 #pragma unroll
                 for (int i = 0; i < kOuterA; i += 4) {
                     const float4_t a = s_a[r0 + u][(ai + i) / 4];
@@ -253,6 +256,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter
         }
     }
     if (b >= B) return;
+    if (q.sums && a0 + ai == 0) static_cast<T *>(q.sums)[(int64_t)g * B + b] = (T)column;
+    if (!q.out) return;
     T *const out = static_cast<T *>(q.out) + (int64_t)g * q.A * B;
 #pragma unroll
     for (int i = 0; i < kOuterA; ++i) {

@@ -1,0 +1,122 @@
+// The activations of layers (cgtp_grouped_layer) and what a product's tile does with them.
+#ifndef CGTP_ROWS_LAYER_H
+#define CGTP_ROWS_LAYER_H
+
+#include "rows_tile.h"
+
+namespace cgtp {
+namespace rows {
+
+// silu: z s(z), s the logistic function; gelu: z P(z), P the normal distribution function; relu: max(z, 0).
+// An infinite z gives what the formula's products do: -inf s(-inf) is NaN.
+__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + __expf(-z)); }
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(z * -0.70710678f); }
+
+__device__ __forceinline__ float activate(float z, int act)
+{
+    if (act == CGTP_ACT_SILU) return z * logistic(z);
+    if (act == CGTP_ACT_GELU) return z * normal_cdf(z);
+    if (act == CGTP_ACT_RELU) return z <= 0.f ? 0.f : z;
+    return z;
+}
+
+// The derivative.
+__device__ __forceinline__ float activate_slope(float z, int act)
+{
+    if (act == CGTP_ACT_SILU) {
+        const float f = logistic(z);
+        return f * (1.f + z * (1.f - f));
+    }
+    if (act == CGTP_ACT_GELU) return normal_cdf(z) + z * 0.39894228f * __expf(-0.5f * z * z);
+    if (act == CGTP_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+    return 1.f;
+}
+
+// Four values from p on, zero past the `left` that exist.
+__device__ __forceinline__ float4_t load_four(const float *p, int64_t left)
+{
+    if (left >= 4) return *reinterpret_cast<const float4_any *>(p);
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (left > e) v[e] = p[e];
+    return v;
+}
+__device__ __forceinline__ float4_t load_four(const bf16_t *p, int64_t left)
+{
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
+    if (left >= 4) {
+        const bf4_t h = *reinterpret_cast<const bf4_any *>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)h[e];
+        return v;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (left > e) v[e] = (float)p[e];
+    return v;
+}
+
+// Columns col .. col + 3 of row `row` of group g of a layer, from the product's sums (not grouped: of no group, whose
+// z is zero). MARK: a sum that is not finite leaves NaN in y whatever the activation makes of it, for
+// layer_plain_sums to find.
+template <typename T, bool MARK>
+__device__ __forceinline__ void store_layer(const RowProduct &p, int g, bool grouped, int64_t row, int col, float4_t sum)
+{
+    const int left = p.N - col;
+    if (left <= 0) return;
+    float4_t x = sum;
+    if (p.bias && grouped) x += load_four(static_cast<const T *>(p.bias) + (int64_t)g * p.N + col, left);
+    if (p.z) store_four<false>(static_cast<T *>(p.z) + row * p.z_stride + col, x, left);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = activate(x[e], p.act);
+        if (MARK) x[e] = fmaf(sum[e], 0.f, x[e]);
+    }
+    if (p.residual) x += load_four(static_cast<const T *>(p.residual) + row * p.residual_stride + col, left);
+    store_four<false>(static_cast<T *>(p.out) + row * p.out_stride + col, x, left);
+}
+
+// Columns [c0, c1) of a tile's rows of no group.
+template <typename T>
+__device__ __forceinline__ void store_bare(const RowProduct &p, const int *row, int rows, int c0, int c1)
+{
+    const int quads = (c1 - c0 + 3) / 4;
+    for (int i = threadIdx.x; i < rows * quads; i += kThreads) {
+        const int r = row[i / quads], col = c0 + 4 * (i % quads);
+        if (r < 0) continue;
+        if (p.out_f32)
+            store_four<false>(static_cast<float *>(p.out) + r * p.out_stride + col, float4_t{0.f, 0.f, 0.f, 0.f}, p.N - col);
+        else store_layer<T, false>(p, 0, false, r, col, float4_t{0.f, 0.f, 0.f, 0.f});
+    }
+}
+
+// The results of a workgroup's rows that are not finite, in the columns [c0, c1), in plain fp32.
+template <typename T, bool WNK>
+__device__ void layer_plain_sums(const RowProduct &p, int group, int rows, const int *s_row, int c0, int c1)
+{
+    stores_done();
+    const int width = c1 - c0;
+    const T *const w = static_cast<const T *>(p.w) + (int64_t)group * p.w_group;
+    for (int i = threadIdx.x; i < rows * width; i += kThreads) {
+        const int64_t row = s_row[i / width];
+        const int c = c0 + i % width;
+        if (row < 0) continue;
+        T *const out = static_cast<T *>(p.out) + row * p.out_stride + c;
+        if (__builtin_isfinite(stored(out))) continue;
+        const T *const in = static_cast<const T *>(p.in) + (int64_t)((unsigned)row / (unsigned)p.per) * p.in_stride;
+        float x = 0.f;
+        for (int k = 0; k < p.K && x == x; ++k)  // NaN stays
+            x += (float)in[k] * (float)w[WNK ? (int64_t)c * p.K + k : (int64_t)k * p.N + c];
+        if (p.bias) x += (float)static_cast<const T *>(p.bias)[(int64_t)group * p.N + c];
+        if (p.z) static_cast<T *>(p.z)[row * p.z_stride + c] = (T)x;
+        x = activate(x, p.act);
+        if (p.residual) x += (float)static_cast<const T *>(p.residual)[row * p.residual_stride + c];
+        *out = (T)x;
+    }
+}
+
+}  // namespace rows
+}  // namespace cgtp
+
+#endif

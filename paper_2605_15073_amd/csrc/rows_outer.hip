@@ -25,7 +25,27 @@ namespace {
 
 using namespace rows;
 
-template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW>
+// Sums of b's columns, from the loads of its values: of the tiles that hold the first columns of a.
+__device__ __forceinline__ void add_columns(float (&sum)[8], const uint4_t (&in)[8], bf16_t)
+{
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sum[2 * e] += __builtin_bit_cast(float, in[r][e] << 16);
+            sum[2 * e + 1] += __builtin_bit_cast(float, in[r][e] & 0xffff0000u);
+        }
+}
+__device__ __forceinline__ void add_columns(float (&sum)[4], const uint4_t (&in)[8], float)
+{
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += __builtin_bit_cast(float, (unsigned)in[r][e]);
+}
+
+// LAYER: rows of a are shared (per), and the columns of b are summed beside the products (sums).
+template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW, bool LAYER>
 __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, ChunkRows R, bool big,
                                                         float *slots)
 {
@@ -89,7 +109,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         const int row = o.order ? id : (int)pos;
         const bool in = pos < t.p1 && (unsigned)row < (unsigned)o.n;
         if (tid < BK) {
-            s_at[0][s & 1][tid] = in ? row * q.a_stride : 0;  // row 0 in place of none: zeroed when staged
+            const int of_a = LAYER && q.per > 1 ? (int)((unsigned)row / (unsigned)q.per) : row;
+            s_at[0][s & 1][tid] = in ? of_a * q.a_stride : 0;  // row 0 in place of none: zeroed when staged
             s_at[1][s & 1][tid] = !in ? 0 : NARROW ? pos * (P * W) : row * q.b_stride;
             const unsigned long long m = __ballot(in);
             if (tid % 32 == 0) s_rows_in[s & 1][tid / 32] = (unsigned)(m >> (tid & 32));
@@ -109,6 +130,10 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             }
         }
     };
+    const bool sums = LAYER && q.sums && of_b && a0 == 0;
+    float column[LAYER ? CW : 1];
+#pragma unroll
+    for (int j = 0; j < (LAYER ? CW : 1); ++j) column[j] = 0.f;
     auto stage = [&]() {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
@@ -122,6 +147,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 #pragma unroll
                 for (int r = 0; r < 8; ++r) l[i][r] = in[i] >> r & 1 ? l[i][r] : uint4_t{0, 0, 0, 0};
             }
+            if constexpr (LAYER)
+                if (sums) add_columns(column, l[i], T());
             uint4_t u[CW][Q];
             to_units(l[i], u, of_b ? 1.f : sign);
 #pragma unroll
@@ -159,10 +186,29 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         }
     }
     const bool whole = t.end - t.start <= R.rows;
-    const int64_t cells = (int64_t)q.A * B;
+    const int64_t cells = (int64_t)q.A * B, slot_cells = cells + (LAYER && q.sums ? B : 0);
     const int64_t slot = 2 * (int64_t)R.of((int)t.start) + R.of((int)(t.p0 - t.start));
     T *const out = static_cast<T *>(q.out) + t.g * cells;
-    float *const part = slots + (whole ? 0 : slot * cells);
+    float *const part = slots + (whole ? 0 : slot * slot_cells);
+    if constexpr (LAYER) {
+        static_assert(NL == 1, "one task a thread");
+        if (q.sums && a0 == 0) {
+            float *const of_kg = reinterpret_cast<float *>(s_rows);  // [KG][BN]
+            __syncthreads();
+            if (of_b && tasks[0].has)
+#pragma unroll
+                for (int j = 0; j < CW; ++j) of_kg[tasks[0].kg * BN + tasks[0].first + j] = column[j];
+            __syncthreads();
+            if (tid < BN && b0 + tid < B) {
+                float sum = 0.f;
+#pragma unroll
+                for (int g = 0; g < KG; ++g) sum += of_kg[g * BN + tid];
+                if (whole) static_cast<T *>(q.sums)[(int64_t)t.g * B + b0 + tid] = (T)sum;
+                else part[cells + b0 + tid] = sum;
+            }
+        }
+    }
+    if (LAYER && !q.out) return;  // the sums alone
 #pragma unroll
     for (int r = 0; r < TR; ++r) {
         const int i = a0 + lane_of_full<T>(r0 + 32 * r + (lane & 31));
@@ -207,7 +253,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                 const int row = row_at(o, pos), any = row < 0 ? 0 : row;
                 const float y = NARROW ? narrow_at<T>(q.h, pos, W, c)
                                        : (float)static_cast<const T *>(q.b)[any * q.b_stride + c];
-                const float x = (float)static_cast<const T *>(q.a)[any * q.a_stride + i];
+                const int of_a = LAYER && q.per > 1 ? (int)((unsigned)any / (unsigned)q.per) : any;
+                const float x = (float)static_cast<const T *>(q.a)[of_a * q.a_stride + i];
                 sum = row < 0 ? sum : fmaf(x, y, sum);
             };
             int64_t pos = t.p0;
@@ -227,9 +274,11 @@ constexpr int kJoinCells = 128, kJoinLanes = 8;
 // four of them of every eighth slot, and the eight sums are then added in order. Where there are fewer
 // groups than chunk sizes in the sequence, block x is for group x; else for the group whose first multiple
 // of the chunk size beyond its start is x + 1 (each such group has one).
+// Cells from `split` on are those of a second output.
 template <typename T, bool VEC>
-__global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, ChunkRows R, bool by_group, int64_t cells,
-                                                       const float *__restrict__ slots, T *__restrict__ out)
+__global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, ChunkRows R, bool by_group, int64_t cells, int64_t split,
+                                                       const float *__restrict__ slots, T *__restrict__ out,
+                                                       T *__restrict__ rest)
 {
     __shared__ float4_t s_sum[kJoinLanes][kJoinCells / 4];
     const int64_t pos = ((int64_t)blockIdx.x + 1) * R.rows;
@@ -274,7 +323,16 @@ __global__ __launch_bounds__(kThreads) void k_row_join(RowOrder o, ChunkRows R, 
             for (int j = 1; j < kJoinLanes; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[e] += s_sum[j][quad][e];
-            store_four<VEC>(out + lo * cells + i, sum, left);
+            if (!out) {
+                for (int e = 0; e < 4 && e < left; ++e)
+                    if (i + e >= split) rest[lo * (cells - split) + (i + e - split)] = (T)sum[e];
+            } else if (i + 4 <= split || split == cells) store_four<VEC>(out + lo * split + i, sum, split - i);
+            else if (i >= split) store_four<VEC>(rest + lo * (cells - split) + (i - split), sum, left);
+            else
+                for (int e = 0; e < 4 && e < left; ++e) {
+                    if (i + e < split) out[lo * split + i + e] = (T)sum[e];
+                    else rest[lo * (cells - split) + (i + e - split)] = (T)sum[e];
+                }
         }
     }
 }
@@ -328,9 +386,10 @@ hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, bool bi
     const bool wide = q.A >= kFull<T> && (q.r > 0 || B >= kFull<T>);  // 16 bytes of a row and more
     const int64_t chunks = ((big ? o.n / kFewRows : o.n / sh.rows + o.G) + 7) / 8 * 8;
     if (chunks * sh.tiles > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    auto *kernel = wide ? k_row_outer<T, BM, BN, WR, true, false> : k_row_outer<T, BM, BN, WR, false, false>;
+    auto *kernel = wide ? k_row_outer<T, BM, BN, WR, true, false, false> : k_row_outer<T, BM, BN, WR, false, false, false>;
+    if (q.per > 0) kernel = wide ? k_row_outer<T, BM, BN, WR, true, false, true> : k_row_outer<T, BM, BN, WR, false, false, true>;
     if constexpr (BN <= CGTP_MAX_ADAPTER_RANK)
-        if (q.r > 0) kernel = wide ? k_row_outer<T, BM, BN, WR, true, true> : k_row_outer<T, BM, BN, WR, false, true>;
+        if (q.r > 0) kernel = wide ? k_row_outer<T, BM, BN, WR, true, true, false> : k_row_outer<T, BM, BN, WR, false, true, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks * sh.tiles)), dim3(kThreads), 0, s, o, q, ChunkRows(sh.rows), big,
                        slots);
     return hipGetLastError();
@@ -351,22 +410,23 @@ template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float
     else if (sh.bn == 64) e = launch<T, 128, 64, 4>(o, q, sh, big, slots, s);
     else e = launch<T, 128, 128, kWaveRows<T>>(o, q, sh, big, slots, s);
     if (e != hipSuccess || o.n <= sh.rows) return e;
-    const int64_t cells = (int64_t)q.A * B, by = (cells + kJoinCells - 1) / kJoinCells;
+    const int64_t split = (int64_t)q.A * B, cells = split + (q.sums ? B : 0), by = (cells + kJoinCells - 1) / kJoinCells;
     const int64_t spans = o.n / sh.rows, bx = o.G < spans ? o.G : spans;
     const int64_t y = 8192 / bx < 1 ? 1 : 8192 / bx;
-    const bool vec = cells % 4 == 0 && aligned_rows<T>(q.out, 0);
+    const bool vec = split % 4 == 0 && aligned_rows<T>(q.out, 0) &&
+                     (!q.sums || (B % 4 == 0 && aligned_rows<T>(q.sums, 0)));
     auto *kernel = vec ? k_row_join<T, true> : k_row_join<T, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)bx, (unsigned)(by < y ? by : y)), dim3(kThreads), 0, s, o, ChunkRows(sh.rows),
-                       o.G < spans, cells, slots, static_cast<T *>(q.out));
+                       o.G < spans, cells, split, slots, static_cast<T *>(q.out), static_cast<T *>(q.sums));
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t row_outer_bytes(int dtype, int64_t n, int G, int A, int B)
+size_t row_outer_bytes(int dtype, int64_t n, int G, int A, int B, bool sums)
 {
     const Shape sh = shape(dtype == CGTP_BF16 ? 2 : 4, n, G, A, B);
-    return n <= sh.rows ? 0 : ((size_t)2 * (n / sh.rows) + 2) * A * B * sizeof(float);
+    return n <= sh.rows ? 0 : ((size_t)2 * (n / sh.rows) + 2) * (A + sums) * B * sizeof(float);
 }
 
 hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &q, void *ws, hipStream_t s)

@@ -24,7 +24,7 @@
 // adapter's second matrix: 131,327 rows of 8 adapters, 896 -> 128, rank 16, fp32 290 us, bf16 86; 100,000 rows of 100,
 // fp32 265 where the two products apart take 298, bf16 71 and 105.
 #include "internal.h"
-#include "rows_tile.h"
+#include "rows_layer.h"
 
 namespace cgtp {
 
@@ -32,12 +32,16 @@ namespace {
 
 using namespace rows;
 
-template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED>
+// What a launch does beside the product: nothing, a layer's bias, activation and residual, or rows of sums in fp32.
+enum Extra { kBare, kLayer, kSums };
+
+template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED, Extra EX>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_product(RowOrder o, RowProduct p, int splits)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
     constexpr int BX = BN + (FUSED ? 32 : 0), TX = TC + (FUSED ? 1 : 0);  // with the narrow product's columns
+    static_assert(EX == kBare || !FUSED, "layers have no adapters");
     static_assert(!FUSED || (WNK && WR == 4 && WIDE), "fused: a wave has whole rows, weights are [N][K]");
     static_assert(TR >= 1 && TC >= 1, "tile");
     constexpr int kLanes = kThreads / KG;              // rows staged at once
@@ -75,7 +79,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     if (!FUSED && !shared_w && t.g == o.G) {  // rows of no group
         if (p.narrow) return;
         __syncthreads();
-        store_zeros<T>(p, s_row, rows, ct0 * BN, col_end);
+        if constexpr (EX != kBare) store_bare<T>(p, s_row, rows, ct0 * BN, col_end);
+        else store_zeros<T>(p, s_row, rows, ct0 * BN, col_end);
         return;
     }
     const bool grouped = t.g < o.G;
@@ -92,7 +97,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const int r = rr + kLanes * i, row = r < BM ? s_row[r] : -1;
-        in[i] = static_cast<const T *>(p.in) + (row < 0 ? s_any : row) * p.in_stride;  // any: never stored
+        const int any = row < 0 ? s_any : row;  // never stored
+        in[i] = static_cast<const T *>(p.in) +
+                (EX == kLayer && p.per > 1 ? (int)((unsigned)any / (unsigned)p.per) : any) * p.in_stride;
     }
     const T *const w = static_cast<const T *>(p.w) + (FUSED ? 0 : (int64_t)t.g * p.w_group);
     const T *const narrow_w = FUSED && grouped ? static_cast<const T *>(p.a) + (int64_t)t.g * p.r * p.K : w;
@@ -246,14 +253,26 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
             for (int r = 0; r < TR; ++r) {
                 const int row = s_row[r0 + 32 * r + (lane & 31)];
                 if (row < 0) continue;
-                T *const q = static_cast<T *>(p.out) + row * p.out_stride;
+                if constexpr (EX == kBare) {
+                    T *const q = static_cast<T *>(p.out) + row * p.out_stride;
 #pragma unroll
-                for (int c = 0; c < TC; ++c)
+                    for (int c = 0; c < TC; ++c)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
-                        store_four<false>(q + col, vec_val<T, !WNK>(acc[c][r], v), p.N - col);
-                    }
+                        for (int v = 0; v < 4; ++v) {
+                            const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
+                            store_four<false>(q + col, vec_val<T, !WNK>(acc[c][r], v), p.N - col);
+                        }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < TC; ++c)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
+                            const float4_t x = vec_val<T, !WNK>(acc[c][r], v);
+                            if (EX == kLayer) store_layer<T, (Q > 1)>(p, t.g, true, row, col, x);
+                            else store_four<false>(static_cast<float *>(p.out) + row * p.out_stride + col, x, p.N - col);
+                        }
+                }
             }
         }
     };
@@ -313,7 +332,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     clear();
     fetch();
     while (now.ct < ct1) step();
-    if ((Q > 1 || FUSED || nseg > 0) && __syncthreads_or(odd != odd)) {
+    if constexpr (EX == kLayer) {
+        if (Q > 1 && __syncthreads_or(odd != odd)) layer_plain_sums<T, WNK>(p, t.g, rows, s_row, ct0 * BN, col_end);
+    } else if ((Q > 1 || FUSED || nseg > 0) && __syncthreads_or(odd != odd)) {
         float *const h = FUSED ? reinterpret_cast<float *>(s_tiles) : nullptr;
         if constexpr (FUSED) {
             stores_done();
@@ -338,7 +359,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     }
 }
 
-template <typename T, bool WNK, int BM, int BN, int WR, bool FUSED = false>
+template <typename T, bool WNK, int BM, int BN, int WR, bool FUSED = false, Extra EX = kBare>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     // rows of eight values or more, of columns or k as they are loaded
@@ -349,17 +370,32 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     // workgroups 119, 113 and 113 us; 60,000 rows, 300 -> 1344 443, 439 and 455, bf16 160, 155 and 156)
     int splits = (int)(2048 / tiles);
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
-    auto *kernel = FUSED || wide ? k_row_product<T, WNK, BM, BN, WR, true, FUSED>
-                                 : k_row_product<T, WNK, BM, BN, WR, FUSED, FUSED>;
+    auto *kernel = FUSED || wide ? k_row_product<T, WNK, BM, BN, WR, true, FUSED, EX>
+                                 : k_row_product<T, WNK, BM, BN, WR, FUSED, FUSED, EX>;
     const TileGrid grid = tile_grid(tiles);
     hipLaunchKernelGGL(kernel, dim3(grid.x, (unsigned)splits, grid.z), dim3(kThreads), 0, s, o, p, splits);
     return hipGetLastError();
+}
+
+// Tiles as pick() takes them.
+template <typename T, bool WNK, Extra EX>
+hipError_t pick_extra(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    const bool few = o.n < 40 * (int64_t)o.G;
+    if (p.N <= 32) return launch<T, WNK, 128, 32, 4, false, EX>(o, p, s);
+    if (few && p.N > 64) return launch<T, WNK, 32, 128, 1, false, EX>(o, p, s);
+    if (few || p.N <= 64) return launch<T, WNK, 64, 64, 2, false, EX>(o, p, s);
+    return launch<T, WNK, 128, 128, kWaveRows<T>, false, EX>(o, p, s);
 }
 
 template <typename T, bool WNK>
 hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
+    if constexpr (WNK && sizeof(T) == 2)
+        if (p.out_f32) return pick_extra<T, true, kSums>(o, p, s);
+    if constexpr (!WNK)
+        if (p.per > 0) return pick_extra<T, false, kLayer>(o, p, s);
     if constexpr (WNK)
         // 100,000 rows, 896 -> 64, us with tiles of 64 and 128 columns: bf16 51 and 62, fp32 169 and 234
         if (p.a) return p.N <= 64 ? launch<T, true, 128, 64, 4, true>(o, p, s) : launch<T, true, 128, 128, 4, true>(o, p, s);
