@@ -57,6 +57,23 @@ __device__ __forceinline__ float4_t load_four(const bf16_t *p, int64_t left)
     return v;
 }
 
+// V values to p on, of which `left` exist.
+template <typename T, int V> __device__ __forceinline__ void store_values(T *p, const float (&v)[V], int left)
+{
+    if (left >= V) {
+        typedef T vec_t __attribute__((ext_vector_type(V)));
+        typedef vec_t any_t __attribute__((aligned(sizeof(T))));
+        vec_t h;
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[e] = (T)v[e];
+        *reinterpret_cast<any_t *>(p) = h;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (e < left) p[e] = (T)v[e];
+}
+
 // Columns col .. col + 3 of row `row` of group g of a layer, from the product's sums (not grouped: of no group, whose
 // z is zero). MARK: a sum that is not finite leaves NaN in y whatever the activation makes of it, for
 // layer_plain_sums to find.

@@ -27,22 +27,6 @@ template <typename T> __device__ __forceinline__ Vals<T> load_vals(const T *p, i
     return r;
 }
 
-template <typename T, int V> __device__ __forceinline__ void store_vals(T *p, const float (&v)[V], int left)
-{
-    if (left >= V) {
-        typedef T vec_t __attribute__((ext_vector_type(V)));
-        typedef vec_t any_t __attribute__((aligned(sizeof(T))));
-        vec_t h;
-#pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = (T)v[e];
-        *reinterpret_cast<any_t *>(p) = h;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-        if (e < left) p[e] = (T)v[e];
-}
-
 // Where vector i of a row of N starts.
 template <int V> __device__ __forceinline__ int vec_at(int i, int N) { return i * V + V <= N || N < V ? i * V : N - V; }
 
@@ -77,7 +61,7 @@ __global__ __launch_bounds__(kThreads) void k_mix_rows(RowMix p, int rows)
             for (int e = 0; e < V; ++e)
                 if (e < left) sum[e] += (float)q[e];
         }
-        store_vals(static_cast<T *>(p.out) + t * p.out_stride + c, sum, left);
+        store_values(static_cast<T *>(p.out) + t * p.out_stride + c, sum, left);
     }
 }
 
@@ -106,7 +90,7 @@ __global__ __launch_bounds__(kThreads) void k_mix_rows_grad(RowMixGrad p)
                 float out[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) out[e] = w * g.v[e];
-                store_vals(static_cast<T *>(p.dy) + row * p.dy_stride + c, out, left);
+                store_values(static_cast<T *>(p.dy) + row * p.dy_stride + c, out, left);
             }
         }
         if (p.dweights) {
@@ -133,16 +117,20 @@ __global__ __launch_bounds__(kThreads) void k_layer_dz(int64_t n, int N, int act
         float out[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) out[e] = g.v[e] * activate_slope(a.v[e], act);
-        store_vals(dz + t * N + c, out, left);
+        store_values(dz + t * N + c, out, left);
     }
 }
 
-// Rows of a workgroup, where each has nv vectors.
-int rows_of(int nv) { return nv >= kRowsTasks ? 1 : kRowsTasks / nv; }
+// Rows of a workgroup, of n with nv vectors each: four vectors a thread, one where that leaves too few workgroups.
+int rows_of(int64_t n, int nv)
+{
+    const int tasks = n * nv < (int64_t)2048 * kRowsTasks ? kThreads : kRowsTasks;
+    return nv >= tasks ? 1 : tasks / nv;
+}
 
 template <typename T, typename Y> hipError_t mix(const RowMix &p, hipStream_t s)
 {
-    const int rows = rows_of((p.N + kVec<Y> - 1) / kVec<Y>);
+    const int rows = rows_of(p.n, (p.N + kVec<Y> - 1) / kVec<Y>);
     const TileGrid grid = tile_grid((p.n + rows - 1) / rows);
     hipLaunchKernelGGL((k_mix_rows<T, Y>), dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p, rows);
     return hipGetLastError();
@@ -168,7 +156,7 @@ template <typename T>
 hipError_t layer_dz(int64_t n, int N, int act, const void *dy, int64_t dy_stride, const void *z, int64_t z_stride,
                     void *dz, hipStream_t s)
 {
-    const int rows = rows_of((N + kVec<T> - 1) / kVec<T>);
+    const int rows = rows_of(n, (N + kVec<T> - 1) / kVec<T>);
     const TileGrid grid = tile_grid((n + rows - 1) / rows);
     hipLaunchKernelGGL(k_layer_dz<T>, dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, n, N, act,
                        static_cast<const T *>(dy), dy_stride, static_cast<const T *>(z), z_stride, static_cast<T *>(dz),
