@@ -81,113 +81,236 @@ template <int L, typename F, int D = 1> __device__ __forceinline__ F row_sum(F v
     else return v;
 }
 
-__device__ __forceinline__ float exponential(float x) { return __expf(x); }
-__device__ __forceinline__ double exponential(double x) { return exp(x); }
-__device__ __forceinline__ float inverse(float x) { return __builtin_amdgcn_rcpf(x); }
-__device__ __forceinline__ double inverse(double x) { return 1.0 / x; }
+// Keys whose order is that of ints: of fp32 values above -inf, all of them above kGone. Low bits say where a key is, so
+// that the largest tells: kPlace, PER - 1 - j, which tells a lane's keys apart; kExpert, 16 bits, 65535 - e, the order of
+// equals too.
+enum Embed { kNothing, kPlace, kExpert };
+constexpr int kGone = -0x7fffffff - 1;
+__device__ __forceinline__ int ordered(float f)
+{
+    const int b = __builtin_bit_cast(int, f);
+    return b ^ (b >> 31 & 0x7fffffff);
+}
+__device__ __forceinline__ float value_of(int k) { return __builtin_bit_cast(float, k ^ (k >> 31 & 0x7fffffff)); }
+
+template <int L, int D = 1> __device__ __forceinline__ int row_max(int v)
+{
+    if constexpr (D < L) {
+        int o;
+        if constexpr (D < 16) o = other_lane<D>(v);
+        else o = __shfl_xor(v, D);
+        return row_max<L, 2 * D>(o > v ? o : v);
+    } else return v;
+}
+
+// The lowest lane of a row, counted from its first, for which it holds (one does).
+template <int L> __device__ __forceinline__ int lowest(bool it)
+{
+    const unsigned long long m = __ballot(it);
+    if constexpr (L == 1) return 0;
+    else if constexpr (L == 64) return __ffsll(m) - 1;
+    else return __ffs((int)(m >> ((threadIdx.x & 63) / L * L))) - 1;  // other rows' bits lie above
+}
+
+// Experts of the k largest keys to ids. With `off`, false where a chosen key is within that (off[0],
+// and off[1] of their magnitudes) of the next.
+template <int L, int PER, Embed EMBED>
+__device__ __forceinline__ bool take(int (&key)[PER], int k, int l, const float *off, int *ids)
+{
+    bool sure = true;
+    float before = 0.f;
+    for (int i = 0;; ++i) {
+        if (i == k && !off) break;
+        int own = key[0];
+#pragma unroll
+        for (int j = 1; j < PER; ++j) own = key[j] > own ? key[j] : own;
+        const int best = row_max<L>(own);
+        if (off) {
+            const float now = value_of(best);
+            const float near = off[0] + off[1] * (fabsf(now) + fabsf(before));
+            if (i > 0 && best != kGone && !(now < before - near)) sure = false;
+            before = now;
+            if (i == k) break;
+        }
+        if constexpr (EMBED == kExpert) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) key[j] = key[j] == best ? kGone : key[j];
+            if (l == 0) ids[i] = best == kGone ? -1 : 65535 - (best & 65535);
+            continue;
+        }
+        const int winner = lowest<L>(own == best);
+        if constexpr (EMBED == kPlace) {
+            const int gone = l == winner ? best : kGone;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) key[j] = key[j] == gone ? kGone : key[j];
+            if (l == winner) ids[i] = best == kGone ? -1 : l * PER + (PER - 1 - (best & (PER - 1)));
+        } else if (l == winner) {
+            int at = 0;
+#pragma unroll
+            for (int j = PER - 1; j >= 0; --j) at = key[j] == best ? j : at;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) key[j] = j == at ? kGone : key[j];
+            ids[i] = best == kGone ? -1 : l * PER + at;
+        }
+    }
+    return sure;
+}
 
 // How far a key in fp32 may be off. s = 1 / (1 + e), and s times a share of at most one: their exponentials are off by
 // 2^-24 (2 + 2.5 |a|) of themselves, a the argument: a score by 2.9 2^-24 of the largest from its own, where s |a| is
 // below 0.37 of that; by 23 from a sum of 512, where the mean of |a| is below log 512 + 2; by 14 more from its
-// additions, 8 of a lane and 6 over lanes, and by 3 from reciprocal and product. The bias adds the rounding of the key.
-constexpr float kOffScore = 48 * 0x1p-24f, kOffKey = 0x1p-23f;
+// additions, 8 of a lane and 6 over lanes, and by 3 from reciprocal and product. The bias adds the rounding of the
+// key, embedding the lane's place 7 steps.
+constexpr float kOffScore = 48 * 0x1p-24f, kOffKey = 9 * 0x1p-23f;
 
-// The choice, experts in s_ids. Key float: false where keys in fp32 do not settle it (the caller then takes 64 bits).
-template <int L, int PER, bool KEYS, typename Key>
-__device__ __forceinline__ bool choose(const RowRoute &p, const float (&x)[PER], float top, int l, Key *row_keys, int *ids)
+// The two largest keys of a block, added (one where there is one).
+template <typename Key> struct Two {
+    Key first = -(Key)__builtin_inff(), second = first;
+    __device__ __forceinline__ void add(Key v)
+    {
+        const Key low = v > first ? first : v;
+        first = v > first ? v : first;
+        second = low > second ? low : second;
+    }
+    __device__ __forceinline__ Key sum() const { return second > -(Key)__builtin_inff() ? first + second : first; }
+};
+
+// The choice by keys in fp32. False where it does not settle it.
+template <int L, int PER>
+__device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[PER], float top, int l, float *row_keys,
+                                            int *ids)
 {
-    constexpr Key kNone = -(Key)__builtin_inff();
-    constexpr bool kExact = sizeof(Key) == 8 || !KEYS;
-    Key key[PER];
-    Key most = 1;  // the largest score
-    if constexpr (KEYS) {
-        if (p.score == CGTP_SCORE_SOFTMAX) {
-            Key sum = 0;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                key[j] = there(x[j]) ? exponential((Key)x[j] - (Key)top) : (Key)0;
-                sum += key[j];
-            }
-            most = inverse(row_sum<L>(sum));
-#pragma unroll
-            for (int j = 0; j < PER; ++j) key[j] *= most;
-        } else {
-#pragma unroll
-            for (int j = 0; j < PER; ++j) key[j] = inverse((Key)1 + exponential(-(Key)x[j]));
-        }
+    constexpr float kNone = -__builtin_inff();
+    float f[PER], bias[PER], most = 1.f;  // the largest score
+    if (p.bias) load_logits(bias, p.bias, l * PER, p.E);
+    if (p.score == CGTP_SCORE_SOFTMAX) {
+        float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            const int e = l * PER + j;
-            if (p.bias) key[j] += (Key)p.bias[e < p.E ? e : 0];
-            if (!there(x[j]) || !(key[j] > kNone)) key[j] = kNone;
+            f[j] = there(x[j]) ? __expf(x[j] - top) : 0.f;
+            sum += f[j];
         }
+        most = __builtin_amdgcn_rcpf(row_sum<L>(sum));
+#pragma unroll
+        for (int j = 0; j < PER; ++j) f[j] *= most;
     } else {
 #pragma unroll
-        for (int j = 0; j < PER; ++j) key[j] = there(x[j]) ? x[j] : kNone;
+        for (int j = 0; j < PER; ++j) f[j] = __builtin_amdgcn_rcpf(1.f + __expf(-x[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (p.bias) f[j] += bias[j];
+        f[j] = there(x[j]) && f[j] > kNone ? f[j] : kNone;
     }
     bool sure = true;
-    if (KEYS && p.blocks > 1) {
+    if (p.blocks > 1) {
+        const int size = p.E / p.blocks;
+        float *const scores = row_keys + L * PER;
+        // whether block b is left, by the scores
+        auto left = [&](int b) {
+            const float own = scores[b], off = 4 * kOffScore * most + 9 * kOffKey * fabsf(own);
+            int ahead = 0, perhaps = 0;
+            for (int i = 0; i < p.blocks; ++i) {
+                const float v = scores[i];
+                ahead += v > own + off;
+                perhaps += v >= own - off;  // itself among them
+            }
+            // infinite ones are for 64 bits
+            if (own > kNone && (!(own < -kNone) || (ahead < p.keep && perhaps > p.keep))) sure = false;
+            return ahead < p.keep;
+        };
+        if (size == PER && p.blocks <= L) {  // a block is a lane's
+            Two<float> two;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) two.add(f[j]);
+            if (l < p.blocks) scores[l] = two.sum();
+            wave_sync();
+            if (l < p.blocks && !left(l))
+#pragma unroll
+                for (int j = 0; j < PER; ++j) f[j] = kNone;
+        } else {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) row_keys[l * PER + j] = f[j];
+            wave_sync();
+            for (int b = l; b < p.blocks; b += L) {
+                Two<float> two;
+                for (int i = 0; i < size; ++i) two.add(row_keys[b * size + i]);
+                scores[b] = two.sum();
+            }
+            wave_sync();
+            for (int b = l; b < p.blocks; b += L)
+                if (!left(b))
+                    for (int i = 0; i < size; ++i) row_keys[b * size + i] = kNone;
+            wave_sync();
+#pragma unroll
+            for (int j = 0; j < PER; ++j) f[j] = row_keys[l * PER + j];
+        }
+    }
+    int key[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) key[j] = f[j] > kNone ? (ordered(f[j]) & -PER) | (PER - 1 - j) : kGone;
+    const float off[2] = {2 * kOffScore * most, 2 * kOffKey};
+    return take<L, PER, kPlace>(key, p.k, l, off, ids) && sure;
+}
+
+// The same in 64 bits.
+template <int L, int PER>
+__device__ __forceinline__ void choose_exact(const RowRoute &p, const float (&x)[PER], float top, int l, double *row_keys,
+                                             int *ids)
+{
+    constexpr double kNone = -(double)__builtin_inff();
+    double key[PER];
+    if (p.score == CGTP_SCORE_SOFTMAX) {
+        double sum = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            key[j] = there(x[j]) ? exp((double)x[j] - (double)top) : 0.0;
+            sum += key[j];
+        }
+        sum = row_sum<L>(sum);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] /= sum;
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = 1.0 / (1.0 + exp(-(double)x[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int e = l * PER + j;
+        if (p.bias) key[j] += (double)p.bias[e < p.E ? e : 0];
+        if (!there(x[j]) || !(key[j] > kNone)) key[j] = kNone;
+    }
+    if (p.blocks > 1) {
         // keys of the row, then scores of its blocks; those left out lose their keys
         const int size = p.E / p.blocks;
-        Key *const scores = row_keys + L * PER;
+        double *const scores = row_keys + L * PER;
 #pragma unroll
         for (int j = 0; j < PER; ++j) row_keys[l * PER + j] = key[j];
         wave_sync();
         for (int b = l; b < p.blocks; b += L) {
-            Key first = kNone, second = kNone;
-            for (int i = 0; i < size; ++i) {
-                const Key v = row_keys[b * size + i];
-                const Key low = v > first ? first : v;
-                first = v > first ? v : first;
-                second = low > second ? low : second;
-            }
-            scores[b] = second > kNone ? first + second : first;
+            Two<double> two;
+            for (int i = 0; i < size; ++i) two.add(row_keys[b * size + i]);
+            scores[b] = two.sum();
         }
         wave_sync();
         for (int b = l; b < p.blocks; b += L) {
-            const Key own = scores[b];
-            int ahead = 0, perhaps = 0;
-            for (int i = 0; i < p.blocks; ++i) {
-                const Key v = scores[i];
-                if constexpr (kExact) {
-                    ahead += v > own || (v == own && i < b);
-                } else {
-                    const Key off = 4 * (kOffScore * most + kOffKey * (fabsf(own) + fabsf(v)));
-                    ahead += v > own + off;
-                    perhaps += i != b && v > own - off;
-                    if (v == own && i != b && own > kNone) ++perhaps;  // infinite ones
-                }
-            }
-            const bool out = ahead >= p.keep;
-            if (!kExact && !out && perhaps >= p.keep && own > kNone) sure = false;
-            if (out)
+            int ahead = 0;
+            for (int i = 0; i < p.blocks; ++i) ahead += scores[i] > scores[b] || (scores[i] == scores[b] && i < b);
+            if (ahead >= p.keep)
                 for (int i = 0; i < size; ++i) row_keys[b * size + i] = kNone;
         }
         wave_sync();
 #pragma unroll
         for (int j = 0; j < PER; ++j) key[j] = row_keys[l * PER + j];
     }
-    Key before = -kNone;
-    const int lane = threadIdx.x & 63, first = lane / L * L;
-    // one more round where the last chosen has to be told from the next
-    for (int i = 0; i < p.k + !kExact; ++i) {
-        Key own = key[0];
+    for (int i = 0; i < p.k; ++i) {
+        double own = key[0];
 #pragma unroll
         for (int j = 1; j < PER; ++j) own = key[j] > own ? key[j] : own;
-        const Key best = row_max<L>(own);
-        if constexpr (!kExact) {
-            const Key off = 2 * (kOffScore * most + kOffKey * (fabsf(best) + fabsf(before)));
-            if (best > kNone && !(best < before - off) && i > 0) sure = false;
-            before = best;
-            if (i == p.k) break;
-        }
-        int winner = l;
-        if constexpr (L > 1) {
-            const unsigned long long same = __ballot(own == best) >> first;
-            winner = __ffsll((unsigned long long)same) - 1;  // the lowest of the row: others' bits lie above
-        }
+        const double best = row_max<L>(own);
+        const int winner = lowest<L>(own == best);
         if (l == winner) {
-            int at = -1;
+            int at = 0;
 #pragma unroll
             for (int j = PER - 1; j >= 0; --j) at = key[j] == best ? j : at;
 #pragma unroll
@@ -195,7 +318,6 @@ __device__ __forceinline__ bool choose(const RowRoute &p, const float (&x)[PER],
             ids[i] = best > kNone ? l * PER + at : -1;
         }
     }
-    return sure;
 }
 
 // KEYS: keys are scores with a bias or of blocks; else the logits.
@@ -224,54 +346,69 @@ __global__ __launch_bounds__(kThreads) void k_route(RowRoute p)
     int *const ids = s_ids[wave][r];
     char *const mine = sh + wave * wave_bytes(R, L * PER, p.blocks);
     double *const keys = reinterpret_cast<double *>(mine) + r * (L * PER + p.blocks);
-    if constexpr (!KEYS) choose<L, PER, false, float>(p, x, top, l, nullptr, ids);
-    else if constexpr (PER > 8) choose<L, PER, true, double>(p, x, top, l, keys, ids);
-    else {
+    if constexpr (!KEYS) {
+        constexpr Embed kEmbed = sizeof(T) == 2 ? kExpert : kNothing;  // bf16's lower half is free
+        int key[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int k = ordered(x[j] + 0.f);  // one zero
+            key[j] = there(x[j]) ? (kEmbed == kExpert ? (k & -65536) | (65535 - (l * PER + j)) : k) : kGone;
+        }
+        take<L, PER, kEmbed>(key, p.k, l, nullptr, ids);
+    } else if constexpr (PER > 8) {
+        choose_exact<L, PER>(p, x, top, l, keys, ids);
+    } else {
         float *const near = reinterpret_cast<float *>(mine) + r * (L * PER + p.blocks + 4);
-        const bool sure = choose<L, PER, true, float>(p, x, top, l, near, ids);
+        const bool sure = choose_near<L, PER>(p, x, top, l, near, ids);
         if (__any(!sure)) {
             wave_sync();
-            choose<L, PER, true, double>(p, x, top, l, keys, ids);
+            choose_exact<L, PER>(p, x, top, l, keys, ids);
         }
     }
     wave_sync();
-    // weights. Renormalised ones are formed relative to the largest of the chosen.
-    float sum = 0.f, shift = top;
+    // weights, rank l + L i. Renormalised ones are formed relative to the largest of the chosen.
+    constexpr int NI = (kMost<L * PER> + L - 1) / L;
     const bool soft = p.score == CGTP_SCORE_SOFTMAX;
+    float w[NI], sum = 0.f, shift = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        if (l + L * i >= p.k) break;
+        const int e = ids[l + L * i];
+        w[i] = e >= 0 ? (float)from[e] : kNone;
+    }
     if (p.renorm) {
         shift = kNone;
-        for (int i = l; i < p.k; i += L) {
-            const int e = ids[i];
-            if (e >= 0) shift = fmaxf(shift, soft ? (float)from[e] : fminf((float)from[e], 0.f));
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            if (l + L * i >= p.k) break;
+            shift = fmaxf(shift, soft ? w[i] : fminf(w[i], 0.f));
         }
         shift = row_max<L>(shift);
     } else if (soft) {
+        shift = top;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) sum += there(x[j]) ? expf(x[j] - top) : 0.f;
+        for (int j = 0; j < PER; ++j) sum += there(x[j]) ? __expf(x[j] - top) : 0.f;
         sum = row_sum<L>(sum);
-    } else {
-        shift = 0.f;
     }
-    auto part = [&](int e) {
-        const float v = (float)from[e];
-        return soft ? expf(v - shift) : expf(fminf(v, 0.f) - shift) / (1.f + expf(-fabsf(v)));
-    };
-    if (p.renorm) {
-        for (int i = l; i < p.k; i += L)
-            if (ids[i] >= 0) sum += part(ids[i]);
-        sum = row_sum<L>(sum);
-    } else if (!soft) {
-        sum = 1.f;
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        if (l + L * i >= p.k) break;
+        const float v = w[i];
+        w[i] = !there(v) ? 0.f : soft ? __expf(v - shift) : __expf(fminf(v, 0.f) - shift) / (1.f + __expf(-fabsf(v)));
+        total += w[i];
     }
-    unsigned long long any = __ballot(odd);
+    if (p.renorm) sum = row_sum<L>(total);
+    else if (!soft) sum = 1.f;
+    unsigned long long any = soft ? __ballot(odd) : 0;
     if (L < 64) any = any >> (lane / L * L) & ((1ull << (L % 64)) - 1);
     if (!stores) return;
-    for (int i = l; i < p.k; i += L) {
-        const int e = ids[i];
-        p.ids[row * p.k + i] = e;
-        float w = e >= 0 ? part(e) / sum * p.scale : 0.f;
-        if (soft && any) w = __builtin_nanf("");
-        p.weights[row * p.k + i] = w;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int c = l + L * i;
+        if (c >= p.k) break;
+        p.ids[row * p.k + c] = ids[c];
+        p.weights[row * p.k + c] = any ? __builtin_nanf("") : w[i] == 0.f ? 0.f : w[i] / sum * p.scale;
     }
 }
 
