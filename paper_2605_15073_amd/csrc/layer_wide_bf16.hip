@@ -1,0 +1,43 @@
+// Launches of layers with short inputs and wide outputs (rows_wide.h), in bf16.
+#include "rows_wide.h"
+
+namespace cgtp {
+
+namespace {
+
+using namespace rows;
+
+template <typename T, int NP, bool WHOLE, bool LINES, bool Z, bool RES>
+hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    const WideGrid g = wide_grid(o.n / kRows + o.G + 1, p.N);
+    hipLaunchKernelGGL((k_row_wide<T, false, NP, 0, false, WHOLE, LINES, kLayer, Z, RES>), g.grid, dim3(kThreads), 0, s, o, p,
+                       g.splits);
+    return hipGetLastError();
+}
+
+template <typename T, bool WHOLE, bool LINES, bool Z, bool RES>
+hipError_t with_rows(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    constexpr int M = kPairs<T>;
+    if (p.K <= M / 4 * 2 * kU) return launch<T, M / 4, WHOLE, LINES, Z, RES>(o, p, s);
+    if (p.K <= M / 2 * 2 * kU) return launch<T, M / 2, WHOLE, LINES, Z, RES>(o, p, s);
+    return launch<T, M, WHOLE, LINES, Z, RES>(o, p, s);
+}
+
+template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    if (by_lines<T>(p.out, p.out_stride, p.N)) {
+        if (p.z) return p.residual ? with_rows<T, true, true, true, true>(o, p, s) : with_rows<T, true, true, true, false>(o, p, s);
+        return p.residual ? with_rows<T, true, true, false, true>(o, p, s) : with_rows<T, true, true, false, false>(o, p, s);
+    }
+    if (by_fours<T>(p.out, p.out_stride, p.N))
+        return p.residual ? with_rows<T, true, false, false, true>(o, p, s) : with_rows<T, true, false, false, false>(o, p, s);
+    return p.residual ? with_rows<T, false, false, false, true>(o, p, s) : with_rows<T, false, false, false, false>(o, p, s);
+}
+
+}  // namespace
+
+hipError_t launch_layer_wide_bf16(const RowOrder &o, const RowProduct &p, hipStream_t s) { return pick<bf16_t>(o, p, s); }
+
+}  // namespace cgtp

@@ -59,6 +59,11 @@ hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p,
 // The form for short inputs and wide outputs (rows_wide.hip), and whether it covers a product.
 bool row_wide_takes(int dtype, const RowProduct &p);
 hipError_t launch_row_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
+// Layers (RowProduct::per) in that form.
+bool layer_wide_takes(int dtype, const RowProduct &p);
+hipError_t launch_layer_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
+hipError_t launch_layer_wide_bf16(const RowOrder &o, const RowProduct &p, hipStream_t s);
+hipError_t launch_layer_wide_f32(const RowOrder &o, const RowProduct &p, hipStream_t s);
 // Whether adapters get tiles of 128 rows of their own, in which the product forms the narrow rows itself: where they
 // have 64 rows on the mean, or all tiles run at once anyway. Us in one launch, and with a narrow product of its own
 // and tiles that adapters share: 300 adapters of 1, 8 and 48 rows, bf16, y 64 -> 896, rank 16 23 and 94, 28 and 33,

@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void k_layer_dz(int64_t n, int N, int act
         const Vals<T> g = load_vals(dy + t * dy_stride + c, left), a = load_vals(z + t * z_stride + c, left);
         float out[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[e] = g.v[e] * activate_slope(a.v[e], act);
+        for (int e = 0; e < V; ++e) out[e] = g.v[e] * activate_slope<T>(a.v[e], act);
         store_values(dz + t * N + c, out, left);
     }
 }

@@ -32,9 +32,6 @@ namespace {
 
 using namespace rows;
 
-// What a launch does beside the product: nothing, a layer's bias, activation and residual, or rows of sums in fp32.
-enum Extra { kBare, kLayer, kSums };
-
 template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED, Extra EX>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_product(RowOrder o, RowProduct p, int splits)
 {
@@ -382,6 +379,8 @@ template <typename T, bool WNK, Extra EX>
 hipError_t pick_extra(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const bool few = o.n < 40 * (int64_t)o.G;
+    if (EX == kLayer && !few && layer_wide_takes(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, p))
+        return launch_layer_wide(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4, false, EX>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1, false, EX>(o, p, s);
     if (few || p.N <= 64) return launch<T, WNK, 64, 64, 2, false, EX>(o, p, s);

@@ -1,8 +1,12 @@
 """The reference of layers, joining and routing against differences of its own forward forms, on the CPU."""
 from __future__ import annotations
 
+import os
+import re
+
 import numpy as np
 import pytest
+from scipy.special import erfcx
 
 from tests import layers_ref as ref
 
@@ -55,3 +59,16 @@ def test_mix():
     loss = lambda: (ref.mix(y, w, None, 3, "f32")[0] * d).sum()
     for got, a in zip(ref.mix_grad(d, w, y, 3, "f32"), (y, w)):
         assert np.abs(got[0] - differences(loss, a)).max() < 1e-7
+
+
+def test_tail_of_bf16_gelu():
+    """The polynomial of the sources, from 0 to where only its first coefficient counts: error below 2^-15.6."""
+    path = os.path.join(os.path.dirname(os.path.dirname(__file__)), "paper_2605_15073_amd", "csrc", "rows_layer.h")
+    body = re.search(r"float normal_cdf\(.*?\n}", open(path).read(), re.S).group()
+    by = float(re.search(r"fmaf\(([\d.]+)f, fabsf\(z\), 1.f\)", body).group(1))
+    first = re.search(r"q = fmaf\((-?[\d.]+)f, t, (-?[\d.]+)f\)", body)
+    c = [float(first.group(1)), float(first.group(2))] + [float(v) for v in re.findall(r"fmaf\(q, t, (-?[\d.]+)f\)", body)]
+    assert len(c) == 6
+    z = np.concatenate([np.linspace(0, 20, 400001), np.geomspace(20, 1e8, 2001)])
+    t = 1 / (1 + by * z)
+    assert np.abs(t * np.polyval(c, t) / (0.5 * erfcx(z / np.sqrt(2))) - 1).max() < ref.TAIL
