@@ -300,13 +300,17 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     fetch(ct0, 0);
     for (int ct = ct0; ct < ct1; ++ct) {
         float16_t acc[2];
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
         __syncthreads();
         stage();
         __syncthreads();
+        // a layer's bf16 sums start at the bias; fp32's, of scaled parts, get it behind
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                if (EX == kLayer && Q == 1) set_vec<T, !WNK>(acc[c], v, s_bias[(32 * c + vec_col<T, !WNK>(v, half)) / 4]);
+                else set_vec<T, !WNK>(acc[c], v, float4_t{0.f, 0.f, 0.f, 0.f});
+            }
         fetch(nseg > 1 || ct + 1 == ct1 ? ct : ct + 1, nseg > 1 ? 1 : 0);
         auto product = [&](int pair, const uint4_t (&b)[Q]) {
             uint4_t c0[Q], c1[Q];
@@ -355,9 +359,11 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const float4_t b = s_bias[(32 * c + vec_col<T, !WNK>(v, half)) / 4];
-                    const float4_t f = kOut * vec_val<T, !WNK>(acc[c], v) + b;
-                    set_vec<T, !WNK>(acc[c], v, f);
+                    float4_t f = vec_val<T, !WNK>(acc[c], v);
+                    if (Q > 1) {
+                        f = kOut * f + s_bias[(32 * c + vec_col<T, !WNK>(v, half)) / 4];
+                        set_vec<T, !WNK>(acc[c], v, f);
+                    }
                     if (Z) convert(f, z_turn[((lane & 31) * ZTURN + 32 * c + vec_col<T, !WNK>(v, half)) / 4]);
                 }
             // fp32: NaN where z is not finite, for layer_plain_sums to find

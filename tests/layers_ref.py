@@ -34,14 +34,14 @@ def density(z):
     return np.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
 
 
-# What the normal distribution's tail P(-|z|) of bf16 results may be off by, relative to itself: the largest error of its
-# polynomial over all z is 1.91e-5 < 2^-15.6 (test_layers_ref.py evaluates it), beside fp32's roundings, 16 U and 2 z^2 U.
-# gelu takes it times |z|, its slope once.
-TAIL = 2.0 ** -15.6
-
-
+# What the normal distribution's tail P(-|z|) of bf16 results may be off by: it is 2^q, q a polynomial in |z|, whose
+# relative error up to 8 is at most 2^-14.9 and which stays below 2^-50 past it (test_layers_ref.py evaluates it); fp32
+# rounds q, below 53 up to there, in seven steps of at most 53 U each: times log 2, 260 U, 2^-15.9. gelu takes the tail
+# times |z|, its slope once.
 def tail(z, dtype):
-    return TAIL * cdf(-np.abs(z)) if dtype == "bf16" else 0.0
+    if dtype != "bf16":
+        return 0.0
+    return np.where(np.abs(z) > 8, 2.0 ** -49, (2.0 ** -14.9 + 260 * U) * cdf(-np.abs(z)))
 
 
 def act(z, name, dtype="f32"):

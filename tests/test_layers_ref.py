@@ -6,7 +6,7 @@ import re
 
 import numpy as np
 import pytest
-from scipy.special import erfcx
+from scipy.special import log_ndtr
 
 from tests import layers_ref as ref
 
@@ -62,13 +62,14 @@ def test_mix():
 
 
 def test_tail_of_bf16_gelu():
-    """The polynomial of the sources, from 0 to where only its first coefficient counts: error below 2^-15.6."""
+    """The polynomial of the sources: its error up to 8, and that it falls past it."""
     path = os.path.join(os.path.dirname(os.path.dirname(__file__)), "paper_2605_15073_amd", "csrc", "rows_layer.h")
     body = re.search(r"float normal_cdf\(.*?\n}", open(path).read(), re.S).group()
-    by = float(re.search(r"fmaf\(([\d.]+)f, fabsf\(z\), 1.f\)", body).group(1))
-    first = re.search(r"q = fmaf\((-?[\d.]+)f, t, (-?[\d.]+)f\)", body)
-    c = [float(first.group(1)), float(first.group(2))] + [float(v) for v in re.findall(r"fmaf\(q, t, (-?[\d.]+)f\)", body)]
-    assert len(c) == 6
-    z = np.concatenate([np.linspace(0, 20, 400001), np.geomspace(20, 1e8, 2001)])
-    t = 1 / (1 + by * z)
-    assert np.abs(t * np.polyval(c, t) / (0.5 * erfcx(z / np.sqrt(2))) - 1).max() < ref.TAIL
+    number = r"(-?[\d.]+(?:e-?\d+)?)f"
+    c = [float(v) for v in re.search(rf"q = fmaf\({number}, a, {number}\)", body).groups()]
+    c += [float(v) for v in re.findall(rf"q = fmaf\(q, a, {number}\)", body)]
+    assert len(c) == 8
+    z = np.linspace(0, 8, 400001)
+    assert np.abs(np.exp2(np.polyval(c, z) - log_ndtr(-z) / np.log(2)) - 1).max() < 2.0 ** -14.9
+    far = np.polyval(c, np.concatenate([np.linspace(8, 100, 100001), np.geomspace(101, 1e30, 1001)]))
+    assert far[0] < -50 and (np.diff(far) < 0).all()
