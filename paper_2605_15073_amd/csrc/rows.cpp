@@ -448,10 +448,14 @@ struct LayerGradBytes {
 
 LayerGradBytes layer_grad_bytes(int dtype, int64_t n, int G, int n_in, int n_out, int per_row, int activation)
 {
-    const size_t sums = cgtp::row_outer_bytes(dtype, n, G, n_in, n_out, true);
-    const size_t bare = cgtp::row_outer_bytes(dtype, n, G, 1, n_out, true);
+    const size_t of[3] = {cgtp::row_outer_bytes(dtype, n, G, n_in, n_out, true),
+                          cgtp::row_outer_bytes(dtype, n, G, 1, n_out, true),  // dbias alone
+                          cgtp::layer_grad_takes(dtype, n, G, n_in, n_out)
+                              ? cgtp::layer_grad_slots(dtype, n, G, n_in, n_out) : 0};
+    size_t sums = of[0];
+    for (const size_t b : of) sums = b > sums ? b : sums;
     return {activation == CGTP_ACT_NONE ? 0 : align256((size_t)n * n_out * elem(dtype)),
-            per_row == 1 ? 0 : align256((size_t)n * n_in * 4), sums > bare ? sums : bare};
+            per_row == 1 ? 0 : align256((size_t)n * n_in * 4), sums};
 }
 
 int check_score(int score, int renormalize, float scale)
@@ -626,6 +630,40 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
     const hipStream_t s = static_cast<hipStream_t>(stream);
     char *const dz = static_cast<char *>(workspace), *const rows = dz + need.dz, *const sums = rows + need.rows;
     hipError_t e;
+    auto add_shared = [&]() {  // dx from the rows that share an input
+        cgtp::RowMix m{};
+        m.n = n_rows / per_row;
+        m.k = per_row;
+        m.N = n_in;
+        m.y = rows;
+        m.y_stride = n_in;
+        m.out = dx;
+        m.out_stride = dx_stride;
+        return cgtp::launch_mix_rows(dtype, m, true, s);
+    };
+    if (dw && cgtp::layer_grad_takes(dtype, n_rows, n_groups, n_in, n_out)) {
+        cgtp::LayerGrad q{};
+        q.x = x;
+        q.x_stride = x_stride;
+        q.K = n_in;
+        q.per = per_row;
+        q.w = w;
+        q.z = z;
+        q.z_stride = z_stride;
+        q.act = activation;
+        q.dy = dy;
+        q.dy_stride = dy_stride;
+        q.N = n_out;
+        q.dx = dx && per_row > 1 ? rows : dx;
+        q.dx_stride = per_row > 1 ? n_in : dx_stride;
+        q.dx_f32 = per_row > 1;
+        q.dw = dw;
+        q.dbias = dbias;
+        e = cgtp::launch_layer_grad(dtype, o, q, sums, s);
+        if (e != hipSuccess) return hip_fail(e, "layer gradient");
+        if (dx && per_row > 1) e = add_shared();
+        return e == hipSuccess ? CGTP_OK : hip_fail(e, "row gradient's sum");
+    }
     const void *b = dy;
     int64_t b_stride = dy_stride;
     if (activation != CGTP_ACT_NONE && n_rows > 0) {
@@ -649,15 +687,7 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
         e = cgtp::launch_row_product(dtype, o, p, s);
         if (e != hipSuccess) return hip_fail(e, "row gradient");
         if (per_row > 1) {
-            cgtp::RowMix m{};
-            m.n = n_rows / per_row;
-            m.k = per_row;
-            m.N = n_in;
-            m.y = rows;
-            m.y_stride = n_in;
-            m.out = dx;
-            m.out_stride = dx_stride;
-            e = cgtp::launch_mix_rows(dtype, m, true, s);
+            e = add_shared();
             if (e != hipSuccess) return hip_fail(e, "row gradient's sum");
         }
     }

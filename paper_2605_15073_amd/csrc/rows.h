@@ -107,6 +107,29 @@ size_t narrow_bytes(int dtype, int64_t n_rows, int N);
 hipError_t launch_layer_dz(int dtype, int64_t n, int N, int act, const void *dy, int64_t dy_stride, const void *z,
                            int64_t z_stride, void *dz, hipStream_t s);
 
+// Both products of a narrow layer's gradient in one pass (layer_grad.hip), dw always, dx and dbias where not NULL.
+struct LayerGrad {
+    const void *x;
+    int64_t x_stride;
+    int K, per;
+    const void *w, *z;
+    int64_t z_stride;
+    int act;
+    const void *dy;
+    int64_t dy_stride;
+    int N;
+    void *dx;
+    int64_t dx_stride;
+    bool dx_f32;  // dx is fp32 whatever the type
+    void *dw, *dbias;
+};
+bool layer_grad_takes(int dtype, int64_t n, int G, int K, int N);
+size_t layer_grad_slots(int dtype, int64_t n, int G, int K, int N);
+hipError_t launch_layer_grad(int dtype, const RowOrder &o, const LayerGrad &q, void *slots, hipStream_t s);
+// out [G][A][B], and sums [G][B] where not NULL, of the groups of more than one chunk, from their slots.
+hipError_t launch_row_join(int dtype, const RowOrder &o, int chunk_rows, int A, int B, const float *slots, void *out,
+                           void *sums, hipStream_t s);
+
 // Row t of out (n rows) from rows t k .. t k + k - 1 of y, with a weight each.
 struct RowMix {
     int64_t n;

@@ -395,6 +395,19 @@ hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, bool bi
     return hipGetLastError();
 }
 
+template <typename T>
+hipError_t join(const RowOrder &o, int chunk, int A, int B, const float *slots, void *out, void *sums, hipStream_t s)
+{
+    const int64_t split = (int64_t)A * B, cells = split + (sums ? B : 0), by = (cells + kJoinCells - 1) / kJoinCells;
+    const int64_t spans = o.n / chunk, bx = o.G < spans ? o.G : spans;
+    const int64_t y = 8192 / bx < 1 ? 1 : 8192 / bx;
+    const bool vec = split % 4 == 0 && aligned_rows<T>(out, 0) && (!sums || (B % 4 == 0 && aligned_rows<T>(sums, 0)));
+    auto *kernel = vec ? k_row_join<T, true> : k_row_join<T, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)bx, (unsigned)(by < y ? by : y)), dim3(kThreads), 0, s, o, ChunkRows(chunk),
+                       o.G < spans, cells, split, slots, static_cast<T *>(out), static_cast<T *>(sums));
+    return hipGetLastError();
+}
+
 template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float *slots, hipStream_t s)
 {
     const int B = q.r > 0 ? q.r : q.B;
@@ -410,15 +423,7 @@ template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float
     else if (sh.bn == 64) e = launch<T, 128, 64, 4>(o, q, sh, big, slots, s);
     else e = launch<T, 128, 128, kWaveRows<T>>(o, q, sh, big, slots, s);
     if (e != hipSuccess || o.n <= sh.rows) return e;
-    const int64_t split = (int64_t)q.A * B, cells = split + (q.sums ? B : 0), by = (cells + kJoinCells - 1) / kJoinCells;
-    const int64_t spans = o.n / sh.rows, bx = o.G < spans ? o.G : spans;
-    const int64_t y = 8192 / bx < 1 ? 1 : 8192 / bx;
-    const bool vec = split % 4 == 0 && aligned_rows<T>(q.out, 0) &&
-                     (!q.sums || (B % 4 == 0 && aligned_rows<T>(q.sums, 0)));
-    auto *kernel = vec ? k_row_join<T, true> : k_row_join<T, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)bx, (unsigned)(by < y ? by : y)), dim3(kThreads), 0, s, o, ChunkRows(sh.rows),
-                       o.G < spans, cells, split, slots, static_cast<T *>(q.out), static_cast<T *>(q.sums));
-    return hipGetLastError();
+    return join<T>(o, sh.rows, q.A, B, slots, q.out, q.sums, s);
 }
 
 }  // namespace
@@ -427,6 +432,13 @@ size_t row_outer_bytes(int dtype, int64_t n, int G, int A, int B, bool sums)
 {
     const Shape sh = shape(dtype == CGTP_BF16 ? 2 : 4, n, G, A, B);
     return n <= sh.rows ? 0 : ((size_t)2 * (n / sh.rows) + 2) * (A + sums) * B * sizeof(float);
+}
+
+hipError_t launch_row_join(int dtype, const RowOrder &o, int chunk_rows, int A, int B, const float *slots, void *out,
+                           void *sums, hipStream_t s)
+{
+    return dtype == CGTP_BF16 ? join<bf16_t>(o, chunk_rows, A, B, slots, out, sums, s)
+                              : join<float>(o, chunk_rows, A, B, slots, out, sums, s);
 }
 
 hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &q, void *ws, hipStream_t s)

@@ -369,17 +369,32 @@ def test_layer_of_large_sums(cg, act):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_layer_grad_keeps_values_that_are_not_finite_apart(cg, dtype):
+@pytest.mark.parametrize("N", [72, 56])
+def test_layer_grad_keeps_values_that_are_not_finite_apart(cg, dtype, N):
     import torch
 
     rng = np.random.default_rng(17)
-    t, per, G, K, N = 300, 2, 4, 40, 72
+    t, per, G, K = 300, 2, 4, 40
     x, w, b, ids = draw_layer(rng, t, per, G, K, N, "even", dtype)
     z, dy = (rounded(rng.standard_normal((t * per, N)), dtype) for _ in range(2))
     o = cg.group_rows(dev(ids), G)
     run = lambda dy: cg.grouped_layer_grad(dev(x, dtype), dev(w, dtype), dev(dy, dtype), *o, z=dev(z, dtype), activation="silu",
                                            per_row=per)
     base = run(dy)
+    w0 = w.copy()
+    w[1, 6, 9] = math.inf                                        # a weight: dx of its group's rows, input 6
+    own = np.repeat(np.arange(t), per)[ids == 1]
+    got = run(dy)
+    hit = torch.zeros(t, K, dtype=torch.bool, device="cuda")
+    hit[torch.from_numpy(own).cuda(), 6] = True
+    assert torch.equal(got[0][~hit], base[0][~hit]) and not torch.isfinite(got[0][hit]).any()
+    assert torch.equal(got[1], base[1]) and torch.equal(got[2], base[2])
+    sign = np.sign(dy * ref.slope(z, "silu")[0])[:, 9]           # infinite by the sign of dz alone, where no two meet
+    for i in own[:20]:
+        s = {sign[r] for r in range(i * per, i * per + per) if ids[r] == 1}
+        if len(s) == 1:
+            assert got[0][i, 6].item() == s.pop() * math.inf
+    w = w0
     for bad in (math.inf, math.nan):
         d1 = dy.copy()
         d1[31, 8] = bad
