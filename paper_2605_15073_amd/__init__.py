@@ -1069,7 +1069,8 @@ class AdamWTensors:
         self.handle = h
         need = ctypes.c_size_t()
         _check(load_library().cgtp_adamw_grad_norm_bytes(h, ctypes.byref(need)), "cgtp_adamw_grad_norm_bytes")
-        self.norm_bytes = need.value
+        # for adamw_grad_norm: like the tensors it serves one stream at a time, and lives until close() has waited
+        self._norm_workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -1133,7 +1134,7 @@ def adamw_grad_norm(tensors: AdamWTensors, max_norm: float, grad_scale=None, nor
         if out is not False:
             _want_dev(name, out, (1,), torch.float32, first)
         outs.append(None if out is False else out)
-    ws_ptr, ws_len, ws = _row_workspace(workspace, tensors.norm_bytes, first)
+    ws_ptr, ws_len, ws = _row_workspace(tensors._norm_workspace if workspace is None else workspace, 0, first)
     _run("cgtp_adamw_grad_norm", first, side, (grad_scale, *outs, ws), tensors.handle, max_norm, _addr(grad_scale),
          _addr(outs[0]), _addr(outs[1]), ws_ptr, ws_len, handle)
     return tuple(outs)

@@ -15,9 +15,11 @@ template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
 // so many values at all; else the missing ones are zero.
 template <typename T> struct Vals { float v[kVec<T>]; };
 
-template <typename T> __device__ __forceinline__ Vals<T> load_vals(const T *p, int left)
+// PAST: past the caches, for what is too large to be found there again.
+template <bool PAST, typename T> __device__ __forceinline__ Vals<T> load_vals(const T *p, int left)
 {
-    const uint4_t u = load_16<T, false>(p, left);
+    const uint4_t u = PAST && left >= kVec<T> ? __builtin_nontemporal_load(reinterpret_cast<const uint4_any *>(p))
+                                              : load_16<T, false>(p, left);
     Vals<T> r;
 #pragma unroll
     for (int e = 0; e < kVec<T>; ++e) {
@@ -27,16 +29,33 @@ template <typename T> __device__ __forceinline__ Vals<T> load_vals(const T *p, i
     return r;
 }
 
+template <bool PAST, typename T, int V> __device__ __forceinline__ void store_vals(T *p, const float (&v)[V], int left)
+{
+    if (PAST && left >= V) {
+        typedef T vec_t __attribute__((ext_vector_type(V)));
+        typedef vec_t any_t __attribute__((aligned(sizeof(T))));
+        vec_t h;
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[e] = (T)v[e];
+        __builtin_nontemporal_store(h, reinterpret_cast<any_t *>(p));
+        return;
+    }
+    store_values(p, v, left);
+}
+
+// Whether a call moves more than the memory-side cache holds.
+bool past_caches(double bytes) { return bytes > (double)((int64_t)256 << 20); }
+
 // Where vector i of a row of N starts.
 template <int V> __device__ __forceinline__ int vec_at(int i, int N) { return i * V + V <= N || N < V ? i * V : N - V; }
 
 constexpr int kRowsTasks = 1024;  // vectors of a workgroup, about
 
 // out_t = residual_t + sum_j weights_tj y_(t k + j), in fp32, j ascending. Y: the type of y.
-template <typename T, typename Y>
+template <typename T, typename Y, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_mix_rows(RowMix p, int rows)
 {
-    constexpr int V = kVec<Y>;
+    constexpr int V = kVec<Y>, kAhead = 4;
     const int nv = (p.N + V - 1) / V;
     const int64_t t0 = tile_at(blockIdx.x, blockIdx.z, gridDim.x) * rows;
     if (t0 >= p.n) return;
@@ -49,54 +68,113 @@ __global__ __launch_bounds__(kThreads) void k_mix_rows(RowMix p, int rows)
         for (int e = 0; e < V; ++e) sum[e] = 0.f;
         const Y *y = static_cast<const Y *>(p.y) + t * p.k * p.y_stride + c;
         const float *const w = p.weights ? p.weights + t * p.k : nullptr;
-        for (int j = 0; j < p.k; ++j) {
-            const Vals<Y> v = load_vals(y + j * p.y_stride, left);
+        int j = 0;
+        for (; j + kAhead <= p.k; j += kAhead) {
+            Vals<Y> v[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) v[a] = load_vals<PAST>(y + (j + a) * p.y_stride, left);
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const float f = w ? w[j + a] : 1.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] = fmaf(f, v[a].v[e], sum[e]);
+            }
+        }
+        for (; j < p.k; ++j) {
+            const Vals<Y> v = load_vals<PAST>(y + j * p.y_stride, left);
             const float f = w ? w[j] : 1.f;
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[e] = fmaf(f, v.v[e], sum[e]);
         }
         if (p.residual) {
             const T *const q = static_cast<const T *>(p.residual) + t * p.residual_stride + c;
+            if constexpr (sizeof(T) == sizeof(Y)) {
+                const Vals<T> v = load_vals<PAST>(q, left);
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (e < left) sum[e] += (float)q[e];
+                for (int e = 0; e < V; ++e) sum[e] += v.v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (e < left) sum[e] += (float)q[e];
+            }
         }
-        store_values(static_cast<T *>(p.out) + t * p.out_stride + c, sum, left);
+        store_vals<PAST>(static_cast<T *>(p.out) + t * p.out_stride + c, sum, left);
     }
 }
 
-// dy_(t k + j) = weights_tj dout_t, dweights_tj = y_(t k + j) . dout_t. L lanes of a wave to a row t.
-template <typename T, int L>
+// dy_(t k + j) = weights_tj dout_t, dweights_tj = y_(t k + j) . dout_t. L lanes of a wave to a row t, whose dout they
+// hold, NI vectors each (0: read again for each j).
+template <typename T, int L, int NI, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_mix_rows_grad(RowMixGrad p)
 {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, kHeld = NI > 0 ? NI : 1, kAhead = NI > 0 ? (NI <= 2 ? 4 / NI : 1) : 1;
     const int nv = (p.N + V - 1) / V, lane = threadIdx.x % L;
     const int64_t t = tile_at(blockIdx.x, blockIdx.z, gridDim.x) * (kThreads / L) + threadIdx.x / L;
     if (t >= p.n) return;
     const T *const d = static_cast<const T *>(p.dout) + t * p.dout_stride;
-    for (int j = 0; j < p.k; ++j) {
-        const int64_t row = t * p.k + j;
-        const float w = p.weights ? p.weights[row] : 1.f;
-        float dot = 0.f;
-        for (int i = lane; i < nv; i += L) {
-            const int c = vec_at<V>(i, p.N), left = p.N - c, again = i * V - c;  // values that the vector before has too
-            const Vals<T> g = load_vals(d + c, left);
-            if (p.dweights) {
-                const Vals<T> y = load_vals(static_cast<const T *>(p.y) + row * p.y_stride + c, left);
+    const T *const y = static_cast<const T *>(p.y) + t * p.k * p.y_stride;
+    T *const dy = static_cast<T *>(p.dy) + t * p.k * p.dy_stride;
+    auto at = [&](int i) { return vec_at<V>(i < nv ? i : nv - 1, p.N); };
+    Vals<T> g[kHeld];
 #pragma unroll
-                for (int e = 0; e < V; ++e) dot = e >= again ? fmaf(y.v[e], g.v[e], dot) : dot;
+    for (int h = 0; h < NI; ++h) {
+        const int i = lane + L * h, c = at(i);
+        g[h] = load_vals<PAST>(d + c, p.N - c);
+    }
+    auto add = [&](float dot, const Vals<T> &v, const Vals<T> &o, int i) {
+        const int again = i < nv ? i * V - at(i) : V;  // values that the vector before has too; past the row all
+#pragma unroll
+        for (int e = 0; e < V; ++e) dot = e >= again ? fmaf(v.v[e], o.v[e], dot) : dot;
+        return dot;
+    };
+    auto scaled = [&](int j, float w, const Vals<T> &v, int i) {
+        const int c = at(i);
+        float out[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = w * v.v[e];
+        if (i < nv) store_vals<PAST>(dy + j * p.dy_stride + c, out, p.N - c);
+    };
+    auto finish = [&](int j, float dot) {
+#pragma unroll
+        for (int s = L / 2; s > 0; s /= 2) dot += __shfl_xor(dot, s);
+        if (lane == 0) p.dweights[t * p.k + j] = dot;
+    };
+    for (int j0 = 0; j0 < p.k; j0 += kAhead) {
+        float w[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) w[a] = p.weights ? p.weights[t * p.k + (j0 + a < p.k ? j0 + a : 0)] : 1.f;
+        if constexpr (NI > 0) {
+            Vals<T> v[kAhead][NI];
+            if (p.dweights)
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+                    for (int h = 0; h < NI; ++h) {
+                        const int c = at(lane + L * h);
+                        v[a][h] = load_vals<PAST>(y + (j0 + a < p.k ? j0 + a : j0) * p.y_stride + c, p.N - c);
+                    }
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                if (j0 + a >= p.k) break;
+                if (p.dy)
+#pragma unroll
+                    for (int h = 0; h < NI; ++h) scaled(j0 + a, w[a], g[h], lane + L * h);
+                if (p.dweights) {
+                    float dot = 0.f;
+#pragma unroll
+                    for (int h = 0; h < NI; ++h) dot = add(dot, v[a][h], g[h], lane + L * h);
+                    finish(j0 + a, dot);
+                }
             }
-            if (p.dy) {
-                float out[V];
-#pragma unroll
-                for (int e = 0; e < V; ++e) out[e] = w * g.v[e];
-                store_values(static_cast<T *>(p.dy) + row * p.dy_stride + c, out, left);
+        } else {
+            float dot = 0.f;
+            for (int i = lane; i < nv; i += L) {
+                const int c = at(i);
+                const Vals<T> o = load_vals<false>(d + c, p.N - c);
+                if (p.dweights) dot = add(dot, load_vals<PAST>(y + j0 * p.y_stride + c, p.N - c), o, i);
+                if (p.dy) scaled(j0, w[0], o, i);
             }
-        }
-        if (p.dweights) {
-#pragma unroll
-            for (int s = L / 2; s > 0; s /= 2) dot += __shfl_xor(dot, s);
-            if (lane == 0) p.dweights[row] = dot;
+            if (p.dweights) finish(j0, dot);
         }
     }
 }
@@ -113,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void k_layer_dz(int64_t n, int N, int act
     for (int i = threadIdx.x; i < mine * nv; i += kThreads) {
         const int64_t t = t0 + i / nv;
         const int c = vec_at<V>(i % nv, N), left = N - c;
-        const Vals<T> g = load_vals(dy + t * dy_stride + c, left), a = load_vals(z + t * z_stride + c, left);
+        const Vals<T> g = load_vals<false>(dy + t * dy_stride + c, left), a = load_vals<false>(z + t * z_stride + c, left);
         float out[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) out[e] = g.v[e] * activate_slope<T>(a.v[e], act);
@@ -132,24 +210,31 @@ template <typename T, typename Y> hipError_t mix(const RowMix &p, hipStream_t s)
 {
     const int rows = rows_of(p.n, (p.N + kVec<Y> - 1) / kVec<Y>);
     const TileGrid grid = tile_grid((p.n + rows - 1) / rows);
-    hipLaunchKernelGGL((k_mix_rows<T, Y>), dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p, rows);
+    const bool past = past_caches((double)p.n * p.N * (p.k * sizeof(Y) + sizeof(T)));
+    auto *kernel = past ? k_mix_rows<T, Y, true> : k_mix_rows<T, Y, false>;
+    hipLaunchKernelGGL(kernel, dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p, rows);
     return hipGetLastError();
 }
 
-template <typename T, int L> hipError_t grad(const RowMixGrad &p, hipStream_t s)
+template <typename T, int L, int NI> hipError_t grad(const RowMixGrad &p, hipStream_t s)
 {
     constexpr int rows = kThreads / L;
     const TileGrid grid = tile_grid((p.n + rows - 1) / rows);
-    hipLaunchKernelGGL((k_mix_rows_grad<T, L>), dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p);
+    const bool past = past_caches((double)p.n * p.N * p.k * sizeof(T) * 2);
+    auto *kernel = past ? k_mix_rows_grad<T, L, NI, true> : k_mix_rows_grad<T, L, NI, false>;
+    hipLaunchKernelGGL(kernel, dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
 
 template <typename T> hipError_t grad(const RowMixGrad &p, hipStream_t s)
 {
     const int nv = (p.N + kVec<T> - 1) / kVec<T>;
-    if (nv <= 4) return grad<T, 4>(p, s);
-    if (nv <= 16) return grad<T, 16>(p, s);
-    return grad<T, 64>(p, s);
+    if (nv <= 4) return grad<T, 4, 1>(p, s);
+    if (nv <= 16) return grad<T, 16, 1>(p, s);
+    if (nv <= 64) return grad<T, 64, 1>(p, s);
+    if (nv <= 128) return grad<T, 64, 2>(p, s);
+    if (nv <= 256) return grad<T, 64, 4>(p, s);
+    return grad<T, 64, 0>(p, s);
 }
 
 template <typename T>
