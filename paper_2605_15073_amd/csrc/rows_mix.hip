@@ -15,10 +15,12 @@ template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
 // so many values at all; else the missing ones are zero.
 template <typename T> struct Vals { float v[kVec<T>]; };
 
-// PAST: past the caches, for what is too large to be found there again.
-template <bool PAST, typename T> __device__ __forceinline__ Vals<T> load_vals(const T *p, int left)
+// Past the caches, where a call is too large to be found there again: nothing, loads alone, or all. Stores go there
+// where rows begin on half a line; else a row's two broken lines would leave in parts.
+enum Past { kThrough, kLoads, kAll };
+template <Past PAST, typename T> __device__ __forceinline__ Vals<T> load_vals(const T *p, int left)
 {
-    const uint4_t u = PAST && left >= kVec<T> ? __builtin_nontemporal_load(reinterpret_cast<const uint4_any *>(p))
+    const uint4_t u = PAST != kThrough && left >= kVec<T> ? __builtin_nontemporal_load(reinterpret_cast<const uint4_any *>(p))
                                               : load_16<T, false>(p, left);
     Vals<T> r;
 #pragma unroll
@@ -29,9 +31,9 @@ template <bool PAST, typename T> __device__ __forceinline__ Vals<T> load_vals(co
     return r;
 }
 
-template <bool PAST, typename T, int V> __device__ __forceinline__ void store_vals(T *p, const float (&v)[V], int left)
+template <Past PAST, typename T, int V> __device__ __forceinline__ void store_vals(T *p, const float (&v)[V], int left)
 {
-    if (PAST && left >= V) {
+    if (PAST == kAll && left >= V) {
         typedef T vec_t __attribute__((ext_vector_type(V)));
         typedef vec_t any_t __attribute__((aligned(sizeof(T))));
         vec_t h;
@@ -43,8 +45,12 @@ template <bool PAST, typename T, int V> __device__ __forceinline__ void store_va
     store_values(p, v, left);
 }
 
-// Whether a call moves more than the memory-side cache holds.
-bool past_caches(double bytes) { return bytes > (double)((int64_t)256 << 20); }
+// By what a call moves (the memory-side cache holds 256 MB) and where its output's rows lie.
+Past past_caches(double bytes, const void *out, int64_t stride, size_t es)
+{
+    if (bytes <= (double)((int64_t)256 << 20)) return kThrough;
+    return reinterpret_cast<uintptr_t>(out) % 64 == 0 && stride * es % 64 == 0 ? kAll : kLoads;
+}
 
 // Where vector i of a row of N starts.
 template <int V> __device__ __forceinline__ int vec_at(int i, int N) { return i * V + V <= N || N < V ? i * V : N - V; }
@@ -52,7 +58,7 @@ template <int V> __device__ __forceinline__ int vec_at(int i, int N) { return i 
 constexpr int kRowsTasks = 1024;  // vectors of a workgroup, about
 
 // out_t = residual_t + sum_j weights_tj y_(t k + j), in fp32, j ascending. Y: the type of y.
-template <typename T, typename Y, bool PAST>
+template <typename T, typename Y, Past PAST>
 __global__ __launch_bounds__(kThreads) void k_mix_rows(RowMix p, int rows)
 {
     constexpr int V = kVec<Y>, kAhead = 4;
@@ -104,7 +110,7 @@ __global__ __launch_bounds__(kThreads) void k_mix_rows(RowMix p, int rows)
 
 // dy_(t k + j) = weights_tj dout_t, dweights_tj = y_(t k + j) . dout_t. L lanes of a wave to a row t, whose dout they
 // hold, NI vectors each (0: read again for each j).
-template <typename T, int L, int NI, bool PAST>
+template <typename T, int L, int NI, Past PAST>
 __global__ __launch_bounds__(kThreads) void k_mix_rows_grad(RowMixGrad p)
 {
     constexpr int V = kVec<T>, kHeld = NI > 0 ? NI : 1, kAhead = NI > 0 ? (NI <= 2 ? 4 / NI : 1) : 1;
@@ -170,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void k_mix_rows_grad(RowMixGrad p)
             float dot = 0.f;
             for (int i = lane; i < nv; i += L) {
                 const int c = at(i);
-                const Vals<T> o = load_vals<false>(d + c, p.N - c);
+                const Vals<T> o = load_vals<kThrough>(d + c, p.N - c);
                 if (p.dweights) dot = add(dot, load_vals<PAST>(y + j0 * p.y_stride + c, p.N - c), o, i);
                 if (p.dy) scaled(j0, w[0], o, i);
             }
@@ -191,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void k_layer_dz(int64_t n, int N, int act
     for (int i = threadIdx.x; i < mine * nv; i += kThreads) {
         const int64_t t = t0 + i / nv;
         const int c = vec_at<V>(i % nv, N), left = N - c;
-        const Vals<T> g = load_vals<false>(dy + t * dy_stride + c, left), a = load_vals<false>(z + t * z_stride + c, left);
+        const Vals<T> g = load_vals<kThrough>(dy + t * dy_stride + c, left), a = load_vals<kThrough>(z + t * z_stride + c, left);
         float out[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) out[e] = g.v[e] * activate_slope<T>(a.v[e], act);
@@ -210,8 +216,8 @@ template <typename T, typename Y> hipError_t mix(const RowMix &p, hipStream_t s)
 {
     const int rows = rows_of(p.n, (p.N + kVec<Y> - 1) / kVec<Y>);
     const TileGrid grid = tile_grid((p.n + rows - 1) / rows);
-    const bool past = past_caches((double)p.n * p.N * (p.k * sizeof(Y) + sizeof(T)));
-    auto *kernel = past ? k_mix_rows<T, Y, true> : k_mix_rows<T, Y, false>;
+    const Past past = past_caches((double)p.n * p.N * (p.k * sizeof(Y) + sizeof(T)), p.out, p.out_stride, sizeof(T));
+    auto *kernel = past == kAll ? k_mix_rows<T, Y, kAll> : past == kLoads ? k_mix_rows<T, Y, kLoads> : k_mix_rows<T, Y, kThrough>;
     hipLaunchKernelGGL(kernel, dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p, rows);
     return hipGetLastError();
 }
@@ -220,8 +226,9 @@ template <typename T, int L, int NI> hipError_t grad(const RowMixGrad &p, hipStr
 {
     constexpr int rows = kThreads / L;
     const TileGrid grid = tile_grid((p.n + rows - 1) / rows);
-    const bool past = past_caches((double)p.n * p.N * p.k * sizeof(T) * 2);
-    auto *kernel = past ? k_mix_rows_grad<T, L, NI, true> : k_mix_rows_grad<T, L, NI, false>;
+    const Past past = past_caches((double)p.n * p.N * p.k * sizeof(T) * 2, p.dy, p.dy_stride, sizeof(T));
+    auto *kernel = past == kAll ? k_mix_rows_grad<T, L, NI, kAll>
+                                : past == kLoads ? k_mix_rows_grad<T, L, NI, kLoads> : k_mix_rows_grad<T, L, NI, kThrough>;
     hipLaunchKernelGGL(kernel, dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
