@@ -10,8 +10,11 @@ using namespace rows;
 template <typename T, int NP, bool WHOLE, bool LINES, bool Z, bool RES>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    const WideGrid g = wide_grid(o.n / kRows + o.G + 1, p.N);
-    hipLaunchKernelGGL((k_row_wide<T, false, NP, 0, false, WHOLE, LINES, kLayer, Z, RES>), g.grid, dim3(kThreads), 0, s, o, p,
+    const int64_t per = tiles_per_xcd(o.n / kRows + o.G + 1);
+    const WideGrid g = wide_grid(p.xcd_tiles > 0 ? kTileXcds * per : o.n / kRows + o.G + 1, p.N);
+    RowProduct by_xcd = p;
+    if (p.xcd_tiles > 0) by_xcd.xcd_tiles = per;
+    hipLaunchKernelGGL((k_row_wide<T, false, NP, 0, false, WHOLE, LINES, kLayer, Z, RES>), g.grid, dim3(kThreads), 0, s, o, by_xcd,
                        g.splits);
     return hipGetLastError();
 }

@@ -582,6 +582,7 @@ extern "C" int cgtp_grouped_layer(int dtype, int64_t n_rows, int n_groups, int n
     p.residual_stride = residual_stride;
     p.z = z;
     p.z_stride = z_stride;
+    p.xcd_tiles = 1;
     const hipError_t e = cgtp::launch_row_product(dtype, {n_rows, n_groups, offsets, order}, p,
                                                   static_cast<hipStream_t>(stream));
     return e == hipSuccess ? CGTP_OK : hip_fail(e, "grouped layer");

@@ -53,6 +53,7 @@ struct RowProduct {
     int64_t residual_stride;
     void *z;
     int64_t z_stride;
+    int64_t xcd_tiles; // 0, or tiles of an XCD, which follow each other there (rows_index.h)
     bool out_f32;      // row gradients of rows that share their input: out is fp32 whatever the type
 };
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);

@@ -49,7 +49,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg, s_any;
 
     const bool shared_w = !FUSED && p.w_group == 0;
-    const int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
+    int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
+    if (EX == kLayer) {
+        if (p.xcd_tiles > 0) index = xcd_tile(index, p.xcd_tiles);
+        if (index < 0) return;
+    }
     Tile t;
     if (shared_w) {
         t.p0 = index * BM;
@@ -369,8 +373,10 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     splits = splits < 1 ? 1 : splits > ctiles ? ctiles : splits;
     auto *kernel = FUSED || wide ? k_row_product<T, WNK, BM, BN, WR, true, FUSED, EX>
                                  : k_row_product<T, WNK, BM, BN, WR, FUSED, FUSED, EX>;
-    const TileGrid grid = tile_grid(tiles);
-    hipLaunchKernelGGL(kernel, dim3(grid.x, (unsigned)splits, grid.z), dim3(kThreads), 0, s, o, p, splits);
+    RowProduct by_xcd = p;
+    if (p.xcd_tiles > 0) by_xcd.xcd_tiles = tiles_per_xcd(tiles);
+    const TileGrid grid = tile_grid(by_xcd.xcd_tiles > 0 ? kTileXcds * by_xcd.xcd_tiles : tiles);
+    hipLaunchKernelGGL(kernel, dim3(grid.x, (unsigned)splits, grid.z), dim3(kThreads), 0, s, o, by_xcd, splits);
     return hipGetLastError();
 }
 

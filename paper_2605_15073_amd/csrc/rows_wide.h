@@ -99,7 +99,11 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     __shared__ int s_row[kRows], s_place[kRows], s_any;
     __shared__ int s_g[EXT ? kRows : 1], s_seg_g[EXT ? kRows : 1], s_seg_at[EXT ? kRows + 1 : 1], s_nseg;
 
-    const int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
+    int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
+    if (EX != kBare) {
+        if (p.xcd_tiles > 0) index = xcd_tile(index, p.xcd_tiles);
+        if (index < 0) return;
+    }
     Tile t;
     if (EXT && !FUSED) {
         t.p0 = index * kRows;

@@ -170,7 +170,8 @@ LAYERS = [(1, 1, 1, 1, 1), (1, 1, 3, 64, 64), (2, 1, 5, 7, 3), (64, 1, 5, 64, 64
           (129, 1, 3, 128, 130), (300, 1, 7, 37, 129), (1000, 1, 400, 24, 40), (257, 1, 2, 896, 72), (2050, 1, 5, 16, 448),
           (515, 1, 2, 1, 300), (515, 1, 2, 300, 1), (90, 1, 80, 200, 130), (1, 8, 8, 64, 64), (33, 3, 5, 31, 67),
           (500, 4, 32, 128, 448), (700, 2, 3, 64, 64), (129, 64, 40, 9, 20), (600, 2, 4, 8, 64), (400, 4, 1000, 16, 24),
-          (3000, 1, 2, 64, 64), (2500, 2, 6, 40, 56)]
+          (3000, 1, 2, 64, 64), (2500, 2, 6, 40, 56), (1000, 4, 5, 128, 448), (900, 1, 3, 100, 130), (700, 2, 2, 128, 250),
+          (3000, 1, 4, 40, 128), (1200, 1, 3, 33, 447), (800, 1, 2, 128, 100), (600, 1, 2, 4, 5), (600, 1, 2, 129, 90)]
 ACTS = ["silu", "gelu", "relu", "none"]
 
 
@@ -259,7 +260,8 @@ def test_layer_grad(cg, t, per, G, K, N, dtype, act, pad, kind):
 def test_layer_grad_of_long_groups(cg, dtype, act):
     """Groups of several chunks, whose sums are joined; odd widths, so that a cell's quad holds both outputs."""
     rng = np.random.default_rng(11)
-    for t, per, G, K, N in ((40000, 1, 2, 15, 17), (9000, 4, 3, 33, 64), (50000, 1, 1, 64, 64), (30000, 1, 3, 16, 130)):
+    for t, per, G, K, N in ((40000, 1, 2, 15, 17), (9000, 4, 3, 33, 64), (50000, 1, 1, 64, 64), (30000, 1, 3, 16, 130),
+                           (9000, 2, 3, 128, 448), (20000, 1, 2, 127, 255), (9000, 1, 2, 130, 64)):
         x, w, b, ids = draw_layer(rng, t, per, G, K, N, "holes", dtype)
         z, dy = (rounded(rng.standard_normal((t * per, N)), dtype) for _ in range(2))
         o = cg.group_rows(dev(ids), G)
@@ -369,7 +371,7 @@ def test_layer_of_large_sums(cg, act):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("N", [72, 56])
+@pytest.mark.parametrize("N", [72, 56, 300, 500])
 def test_layer_grad_keeps_values_that_are_not_finite_apart(cg, dtype, N):
     import torch
 
