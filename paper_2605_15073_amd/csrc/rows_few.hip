@@ -2,7 +2,7 @@
 // group's weights are read, or its gradient written, for a handful of rows: memory and latency bound, too
 // little for the matrix cores' tiles. Sums are plain fp32.
 #include "internal.h"
-#include "rows_tile.h"
+#include "rows_layer.h"
 
 #include <type_traits>
 
@@ -30,7 +30,7 @@ constexpr int kColumns = 64;       // of a product's workgroup
 // and the tiles, 2.5 rows a group: 4,005 groups, 37 -> 129 45 and 66 us, 129 -> 37 as the row gradient 30 and 50
 // (2.5 TB/s of weights); 4,000 groups, 64 -> 64 19 and 36; 500 groups, 256 -> 256 30 and 40. bf16: 44 and 33, 24
 // and 26, 17 and 19, 21 and 17. At 8 rows a group the tiles are ahead (1,000 groups, 128 -> 128 29 and 25).
-template <bool WNK>
+template <bool WNK, bool LAYER>
 __global__ __launch_bounds__(kThreads) void k_row_product_few(RowOrder o, RowProduct p)
 {
     constexpr int kC = WNK ? 2 : 4;
@@ -57,7 +57,11 @@ __global__ __launch_bounds__(kThreads) void k_row_product_few(RowOrder o, RowPro
     const int sr = tid / 32, sc = tid % 32;
     const int row = sr < rows ? row_at(o, p0 + sr) : -1;
     if (g == o.G) {
-        if (row >= 0)
+        if (LAYER) {
+            if (row >= 0)
+                for (int c = c0 + 4 * sc; c < c0 + kColumns && c < p.N; c += 128)
+                    store_layer<float, false>(p, 0, false, row, c, float4_t{0.f, 0.f, 0.f, 0.f});
+        } else if (row >= 0)
             for (int c = c0 + sc; c < c0 + kColumns && c < p.N; c += 32)
                 static_cast<float *>(p.out)[row * p.out_stride + c] = 0.f;
         return;
@@ -100,7 +104,8 @@ __global__ __launch_bounds__(kThreads) void k_row_product_few(RowOrder o, RowPro
     for (int j = 0; j < kC; ++j)
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) acc[j][r] = 0.f;
-    const float *const in = static_cast<const float *>(p.in) + (row < 0 ? 0 : row) * p.in_stride;
+    const int from = row < 0 ? 0 : LAYER && p.per > 1 ? (int)((unsigned)row / (unsigned)p.per) : row;
+    const float *const in = static_cast<const float *>(p.in) + from * p.in_stride;
     for (int kc = 0; kc < p.K; kc += kChunk) {
         const int width = p.K - kc < kChunk ? (p.K - kc + 63) / 64 * 64 : kChunk;
         if (kc > 0) __syncthreads();
@@ -165,7 +170,10 @@ __global__ __launch_bounds__(kThreads) void k_row_product_few(RowOrder o, RowPro
         if (to < 0) return;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            if (col[j] < p.N) static_cast<float *>(p.out)[to * p.out_stride + col[j]] = mine[j];
+            if (col[j] < p.N) {
+                if (LAYER) store_layer_one<float>(p, g, to, col[j], mine[j]);
+                else static_cast<float *>(p.out)[to * p.out_stride + col[j]] = mine[j];
+            }
     } else {
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) {
@@ -185,7 +193,8 @@ __global__ __launch_bounds__(kThreads) void k_row_product_few(RowOrder o, RowPro
             const int c = (own + 4 <= p.N ? own : p.N - 4) + i % 4;
             if (own >= p.N || c < own) continue;  // of the quad before
             const float v = s_part[0][sr][i] + s_part[1][sr][i] + (s_part[2][sr][i] + s_part[3][sr][i]);
-            static_cast<float *>(p.out)[row * p.out_stride + c] = v;
+            if (LAYER) store_layer_one<float>(p, g, row, c, v);
+            else static_cast<float *>(p.out)[row * p.out_stride + c] = v;
         }
     }
 }
@@ -305,7 +314,7 @@ bool row_few_takes(int dtype, const RowOrder &o, const RowProduct &p)
 hipError_t launch_row_few(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const dim3 grid((unsigned)(o.G + 1 + o.n / kHeld), (unsigned)((p.N + kColumns - 1) / kColumns));
-    auto *kernel = p.w_nk ? k_row_product_few<true> : k_row_product_few<false>;
+    auto *kernel = p.w_nk ? k_row_product_few<true, false> : p.per > 0 ? k_row_product_few<false, true> : k_row_product_few<false, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, o, p);
     return hipGetLastError();
 }

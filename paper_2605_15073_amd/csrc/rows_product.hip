@@ -380,16 +380,20 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     return hipGetLastError();
 }
 
+// Whether tiles of 128 by 128 would leave compute units without one.
+bool idle(const RowOrder &o, const RowProduct &p) { return (o.n / 128 + o.G) * ((p.N + 127) / 128) < 256; }
+
 // Tiles as pick() takes them.
 template <typename T, bool WNK, Extra EX>
 hipError_t pick_extra(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
+    if (EX == kLayer && row_few_takes(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, p)) return launch_row_few(o, p, s);
     const bool few = o.n < 40 * (int64_t)o.G;
     if (EX == kLayer && !few && layer_wide_takes(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, p))
         return launch_layer_wide(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4, false, EX>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1, false, EX>(o, p, s);
-    if (few || p.N <= 64) return launch<T, WNK, 64, 64, 2, false, EX>(o, p, s);
+    if (few || p.N <= 64 || idle(o, p)) return launch<T, WNK, 64, 64, 2, false, EX>(o, p, s);
     return launch<T, WNK, 128, 128, kWaveRows<T>, false, EX>(o, p, s);
 }
 
@@ -416,7 +420,7 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
     if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1>(o, p, s);
-    if (few || p.N <= 64) return launch<T, WNK, 64, 64, 2>(o, p, s);
+    if (few || p.N <= 64 || (groups > 1 && idle(o, p))) return launch<T, WNK, 64, 64, 2>(o, p, s);
     return launch<T, WNK, 128, 128, kWaveRows<T>>(o, p, s);
 }
 

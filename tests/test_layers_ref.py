@@ -6,7 +6,7 @@ import re
 
 import numpy as np
 import pytest
-from scipy.special import log_ndtr
+from scipy.special import erfcx, log_ndtr
 
 from tests import layers_ref as ref
 
@@ -61,15 +61,32 @@ def test_mix():
         assert np.abs(got[0] - differences(loss, a)).max() < 1e-7
 
 
-def test_tail_of_bf16_gelu():
-    """The polynomial of the sources: its error up to 8, and that it falls past it."""
-    path = os.path.join(os.path.dirname(os.path.dirname(__file__)), "paper_2605_15073_amd", "csrc", "rows_layer.h")
-    body = re.search(r"float normal_cdf\(.*?\n}", open(path).read(), re.S).group()
+def _coefficients(part, first):
     number = r"(-?[\d.]+(?:e-?\d+)?)f"
-    c = [float(v) for v in re.search(rf"q = fmaf\({number}, a, {number}\)", body).groups()]
-    c += [float(v) for v in re.findall(rf"q = fmaf\(q, a, {number}\)", body)]
+    c = [float(v) for v in re.search(rf"q = fmaf\({number}, {first}, {number}\)", part).groups()]
+    return c + [float(v) for v in re.findall(rf"q = fmaf\(q, {first}, {number}\)", part)]
+
+
+def test_tail_of_gelu():
+    """The polynomials of the sources: bf16's up to 8, and that it falls past it; fp32's for all z, and as fp32 evaluates
+    it, where the reference allows 16 U for it, the exponential's 2 U, the reciprocal's and three products."""
+    path = os.path.join(os.path.dirname(os.path.dirname(__file__)), "paper_2605_15073_amd", "csrc", "rows_layer.h")
+    low, high = re.search(r"float normal_cdf\(.*?\n}", open(path).read(), re.S).group().split("} else {")
+    c = _coefficients(low, "a")
     assert len(c) == 8
     z = np.linspace(0, 8, 400001)
     assert np.abs(np.exp2(np.polyval(c, z) - log_ndtr(-z) / np.log(2)) - 1).max() < 2.0 ** -14.9
     far = np.polyval(c, np.concatenate([np.linspace(8, 100, 100001), np.geomspace(101, 1e30, 1001)]))
     assert far[0] < -50 and (np.diff(far) < 0).all()
+    c = _coefficients(high, "t")
+    assert len(c) == 10 and "fmaf(0.25f, a, 1.f)" in high
+    z = np.concatenate([np.linspace(0, 20, 400001), np.geomspace(20, 1e8, 2001)])
+    t = 1 / (1 + 0.25 * z)
+    assert np.abs(t * np.polyval(c, t) / (0.5 * erfcx(z / np.sqrt(2))) - 1).max() < 2.0 ** -24
+    f = np.float32
+    z = z.astype(f)
+    t = f(1) / (f(1) + f(0.25) * z)
+    q = np.full_like(z, f(c[0]))
+    for k in c[1:]:
+        q = q * t + f(k)
+    assert np.abs((q * t).astype(float) / (0.5 * erfcx(z.astype(float) / np.sqrt(2))) - 1).max() < 8 * ref.U
