@@ -43,9 +43,12 @@ template <typename T, int PER> __device__ __forceinline__ void load_logits(float
         for (int e = 0; e < V; ++e) {
             const float f = sizeof(T) == 4 ? __builtin_bit_cast(float, (unsigned)u[e % 4])
                                            : __builtin_bit_cast(float, e % 2 ? u[e / 2 % 4] & 0xffff0000u : u[e / 2 % 4] << 16);
-            x[v + e] = first + v + e < E ? f : -__builtin_inff();
+            x[v + e] = f;
         }
     }
+    if (first + PER > E)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) x[j] = first + j < E ? x[j] : -__builtin_inff();
 }
 
 // The value of the lane that differs in the bits of D, D < 16: no trip through LDS.
@@ -112,24 +115,33 @@ template <int L> __device__ __forceinline__ int lowest(bool it)
     else return __ffs((int)(m >> ((threadIdx.x & 63) / L * L))) - 1;  // other rows' bits lie above
 }
 
+// Whether a key is within off[0], and off[1] of their magnitudes, of the one before.
+__device__ __forceinline__ bool near(int before, int key, const float *off)
+{
+    const float a = value_of(before), b = value_of(key);
+    return key != kGone && !(b < a - (off[0] + off[1] * (fabsf(a) + fabsf(b))));
+}
+
 // Experts of the k largest keys to ids. With `off`, false where a chosen key is within that (off[0],
-// and off[1] of their magnitudes) of the next.
+// and off[1] of their magnitudes) of the next; the lanes of a row say it for a part of them each.
 template <int L, int PER, Embed EMBED>
 __device__ __forceinline__ bool take(int (&key)[PER], int k, int l, const float *off, int *ids)
 {
     bool sure = true;
-    float before = 0.f;
-    for (int i = 0;; ++i) {
-        if (i == k && !off) break;
+    int mine = kGone, before = kGone;  // the key of rank l, the one before
+    const int rounds = off ? k + 1 : k;
+    for (int i = 0; i < rounds; ++i) {
         int own = key[0];
 #pragma unroll
         for (int j = 1; j < PER; ++j) own = key[j] > own ? key[j] : own;
         const int best = row_max<L>(own);
         if (off) {
-            const float now = value_of(best);
-            const float near = off[0] + off[1] * (fabsf(now) + fabsf(before));
-            if (i > 0 && best != kGone && !(now < before - near)) sure = false;
-            before = now;
+            if (rounds <= L) {
+                mine = l == i ? best : mine;
+            } else {
+                if (i > 0 && near(before, best, off)) sure = false;
+                before = best;
+            }
             if (i == k) break;
         }
         if constexpr (EMBED == kExpert) {
@@ -152,6 +164,10 @@ __device__ __forceinline__ bool take(int (&key)[PER], int k, int l, const float 
             for (int j = 0; j < PER; ++j) key[j] = j == at ? kGone : key[j];
             ids[i] = best == kGone ? -1 : l * PER + at;
         }
+    }
+    if (off && rounds <= L) {
+        before = __shfl_up(mine, 1);
+        sure = !(l > 0 && near(before, mine, off));
     }
     return sure;
 }
@@ -200,7 +216,7 @@ __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         if (p.bias) f[j] += bias[j];
-        f[j] = there(x[j]) && f[j] > kNone ? f[j] : kNone;
+        f[j] = (there(x[j]) & (f[j] > kNone)) ? f[j] : kNone;
     }
     bool sure = true;
     if (p.blocks > 1) {
@@ -335,14 +351,17 @@ __global__ __launch_bounds__(kThreads) void k_route(RowRoute p)
     const T *const from = static_cast<const T *>(p.logits) + row * p.stride;
     float x[PER];
     load_logits(x, from, l * PER, p.E);
+    const bool soft = p.score == CGTP_SCORE_SOFTMAX;
     float top = kNone;
     bool odd = false;  // NaN or +inf among the logits
+    if (soft) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        top = fmaxf(top, there(x[j]) ? x[j] : kNone);
-        odd |= !(x[j] < __builtin_inff());
+        for (int j = 0; j < PER; ++j) {
+            top = fmaxf(top, there(x[j]) ? x[j] : kNone);
+            odd |= !(x[j] < __builtin_inff());
+        }
+        top = row_max<L>(top);
     }
-    top = row_max<L>(top);
     int *const ids = s_ids[wave][r];
     char *const mine = sh + wave * wave_bytes(R, L * PER, p.blocks);
     double *const keys = reinterpret_cast<double *>(mine) + r * (L * PER + p.blocks);
@@ -358,8 +377,8 @@ __global__ __launch_bounds__(kThreads) void k_route(RowRoute p)
     } else if constexpr (PER > 8) {
         choose_exact<L, PER>(p, x, top, l, keys, ids);
     } else {
-        float *const near = reinterpret_cast<float *>(mine) + r * (L * PER + p.blocks + 4);
-        const bool sure = choose_near<L, PER>(p, x, top, l, near, ids);
+        float *const keys32 = reinterpret_cast<float *>(mine) + r * (L * PER + p.blocks + 4);
+        const bool sure = choose_near<L, PER>(p, x, top, l, keys32, ids);
         if (__any(!sure)) {
             wave_sync();
             choose_exact<L, PER>(p, x, top, l, keys, ids);
@@ -368,7 +387,6 @@ __global__ __launch_bounds__(kThreads) void k_route(RowRoute p)
     wave_sync();
     // weights, rank l + L i. Renormalised ones are formed relative to the largest of the chosen.
     constexpr int NI = (kMost<L * PER> + L - 1) / L;
-    const bool soft = p.score == CGTP_SCORE_SOFTMAX;
     float w[NI], sum = 0.f, shift = 0.f;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
