@@ -28,15 +28,17 @@ hipError_t with_rows(const RowOrder &o, const RowProduct &p, hipStream_t s)
     return launch<T, M, WHOLE, LINES, Z, RES>(o, p, s);
 }
 
+template <typename T, bool WHOLE, bool LINES> hipError_t with_extras(const RowOrder &o, const RowProduct &p, hipStream_t s)
+{
+    if (p.z) return p.residual ? with_rows<T, WHOLE, LINES, true, true>(o, p, s) : with_rows<T, WHOLE, LINES, true, false>(o, p, s);
+    return p.residual ? with_rows<T, WHOLE, LINES, false, true>(o, p, s) : with_rows<T, WHOLE, LINES, false, false>(o, p, s);
+}
+
 template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
-    if (by_lines<T>(p.out, p.out_stride, p.N)) {
-        if (p.z) return p.residual ? with_rows<T, true, true, true, true>(o, p, s) : with_rows<T, true, true, true, false>(o, p, s);
-        return p.residual ? with_rows<T, true, true, false, true>(o, p, s) : with_rows<T, true, true, false, false>(o, p, s);
-    }
-    if (by_fours<T>(p.out, p.out_stride, p.N))
-        return p.residual ? with_rows<T, true, false, false, true>(o, p, s) : with_rows<T, true, false, false, false>(o, p, s);
-    return p.residual ? with_rows<T, false, false, false, true>(o, p, s) : with_rows<T, false, false, false, false>(o, p, s);
+    if (by_lines<T>(p.out, p.out_stride, p.N) && (!p.z || by_lines<T>(p.z, p.z_stride, p.N))) return with_extras<T, true, true>(o, p, s);
+    if (by_fours<T>(p.out, p.out_stride, p.N)) return with_extras<T, true, false>(o, p, s);
+    return with_extras<T, false, false>(o, p, s);
 }
 
 }  // namespace

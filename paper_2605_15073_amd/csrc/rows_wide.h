@@ -87,13 +87,12 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     constexpr float kOut = Q > 1 ? kSign * kDown : kSign;
     static_assert(NP <= kPairs<T> && !(EXT && WNK), "adapters: [K][N] weights");
     static_assert(EX == kBare || (EX == kLayer && !EXT && !WNK), "layers: [K][N] weights, no adapters");
-    static_assert(LINES || !Z, "z leaves by whole lines");
     typedef typename Out4<T>::t O;
     typedef typename Out4<T>::any O_any;
     __shared__ uint4_t s_w[Q * KG * LD];
     constexpr int TURN = kTurn<T, LINES, FUSED ? XP : 0>, RING = 2 * kPiece<T>;
     __shared__ O s_turn[4 * 32 * TURN / 4];
-    constexpr int ZTURN = kCols + 4;
+    constexpr int ZTURN = LINES ? kCols + 4 : TURN;  // z of all columns at once, or a ring like that of the results
     __shared__ O s_z_turn[Z ? 4 * 32 * ZTURN / 4 : 1];
     __shared__ float4_t s_bias[EX == kLayer ? kCols / 4 : 1];
     __shared__ int s_row[kRows], s_place[kRows], s_any;
@@ -355,7 +354,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
             }
         }
-        if (Q > 1 || EXT)
+        if (EX == kBare && (Q > 1 || EXT))
 #pragma unroll
             for (int c = 0; c < 2; ++c) probe(odd, acc[c]);
         if constexpr (EX == kLayer) {
@@ -368,17 +367,37 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                         f = kOut * f + s_bias[(32 * c + vec_col<T, !WNK>(v, half)) / 4];
                         set_vec<T, !WNK>(acc[c], v, f);
                     }
-                    if (Z) convert(f, z_turn[((lane & 31) * ZTURN + 32 * c + vec_col<T, !WNK>(v, half)) / 4]);
+                    if (Z && LINES) convert(f, z_turn[((lane & 31) * ZTURN + 32 * c + vec_col<T, !WNK>(v, half)) / 4]);
                 }
-            // fp32: NaN where z is not finite, for layer_plain_sums to find
+            // fp32: NaN where z, an infinite bias with it, is not finite, for layer_plain_sums to find
+            if (Q > 1)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) activate_all<T, (Q > 1)>(acc[c], p.act);
+                for (int c = 0; c < 2; ++c) probe(odd, acc[c]);
+            if (!Z || LINES)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) activate_all<T, (Q > 1)>(acc[c], p.act);
         }
         constexpr float kLast = EX == kLayer ? 1.f : kOut;
         // rows of 128 bytes, several a store
 #pragma unroll
         for (int piece = 0; piece < kCols; piece += kPiece<T>) {
             const int first = first_col(ct) + piece, end = first + kPiece<T>;
+            if constexpr (Z && !LINES) {  // z of the piece to its ring, whose lines are where the results' are
+#pragma unroll
+                for (int c = 0; c < kPiece<T> / 32; ++c) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float4_t f = vec_val<T, !WNK>(acc[piece / 32 + c], v);
+                        const int at = my_at + first + 32 * c + vec_col<T, !WNK>(v, half);
+                        if (WHOLE) convert(f, z_turn[((lane & 31) * TURN + at % RING) / 4]);
+                        else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) reinterpret_cast<T *>(z_turn)[(lane & 31) * TURN + (at + e) % RING] = (T)f[e];
+                        }
+                    }
+                    activate_all<T, (Q > 1)>(acc[piece / 32 + c], p.act);
+                }
+            }
 #pragma unroll
             for (int c = 0; c < kPiece<T> / 32; ++c)
 #pragma unroll
@@ -417,14 +436,18 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                         const int at = (int)(reinterpret_cast<uintptr_t>(out[i]) % 128 / sizeof(T));
                         int c = line * kPiece<T> - at + in_piece;
                         c = c < from_col ? from_col : c > end - 4 ? end - 4 : c;
-                        const T *const from = reinterpret_cast<const T *>(turn) + ((64 / kVecs) * i + lane / kVecs) * TURN;
-                        O v;
-                        if (WHOLE) v = *reinterpret_cast<const O *>(from + (at + c) % RING);
-                        else {
+                        auto store = [&](const O *ring, T *to) {
+                            const T *const from = reinterpret_cast<const T *>(ring) + ((64 / kVecs) * i + lane / kVecs) * TURN;
+                            O v;
+                            if (WHOLE) v = *reinterpret_cast<const O *>(from + (at + c) % RING);
+                            else {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] = from[(at + c + e) % RING];
-                        }
-                        *reinterpret_cast<O_any *>(out[i] + c) = v;
+                                for (int e = 0; e < 4; ++e) v[e] = from[(at + c + e) % RING];
+                            }
+                            *reinterpret_cast<O_any *>(to + c) = v;
+                        };
+                        store(turn, out[i]);
+                        if constexpr (Z) store(z_turn, z_out[i]);
                     }
                 };
                 // a line more for each piece; at the end all that is left

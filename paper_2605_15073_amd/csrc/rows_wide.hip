@@ -57,10 +57,12 @@ template <typename T> bool takes(const RowProduct &p)
 
 }  // namespace
 
-// z leaves by whole lines alone.
+// z, where it is kept, lies on lines as the results do, or both on whole ones.
 template <typename T> bool layer_takes(const RowProduct &p)
 {
-    return p.N >= kCols && p.K <= 2 * kPairs<T> * kU && !p.w_nk && (!p.z || (by_lines<T>(p.out, p.out_stride, p.N) && by_lines<T>(p.z, p.z_stride, p.N)));
+    const bool z_fits = !p.z || (p.z_stride == p.out_stride && (reinterpret_cast<uintptr_t>(p.z) - reinterpret_cast<uintptr_t>(p.out)) % 128 == 0) ||
+                        (by_lines<T>(p.out, p.out_stride, p.N) && by_lines<T>(p.z, p.z_stride, p.N));
+    return p.N >= kCols && p.K <= 2 * kPairs<T> * kU && !p.w_nk && z_fits;
 }
 
 bool layer_wide_takes(int dtype, const RowProduct &p) { return dtype == CGTP_BF16 ? layer_takes<bf16_t>(p) : layer_takes<float>(p); }
