@@ -389,7 +389,12 @@ hipError_t pick_extra(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     if (EX == kLayer && row_few_takes(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, p)) return launch_row_few(o, p, s);
     const bool few = o.n < 40 * (int64_t)o.G;
-    if (EX == kLayer && !few && layer_wide_takes(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, p))
+    // Groups of few rows take the wide form too where all of its tiles run at once. Us of 32- or 64-row tiles and it, with
+    // its tiles: bf16 500 rows of 60 groups, 64 -> 64 6.9 and 5.0 (63), 500 of 100, 48 -> 128 7.6 and 5.5 (206), 1,200 of
+    // 32, 128 -> 448 8.8 and 6.6 (287), 2,000 of 150, 64 -> 896 12.2 and 19.9 (2,310); fp32 8.6 and 6.7, 9.0 and 7.4, -,
+    // 21 and 38.
+    const bool at_once = (o.n / 128 + o.G) * ((p.N + 63) / 64) < 512;
+    if (EX == kLayer && (!few || at_once) && layer_wide_takes(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, p))
         return launch_layer_wide(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4, false, EX>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1, false, EX>(o, p, s);
