@@ -212,7 +212,8 @@ constexpr int kOuterRows = 16;   // rows in LDS at once
 // Measured as this form came in, with it and with the tiled one for all: 10,007 rows in 4,005 groups,
 // 37 x 129 fp32, the whole gradient call 73 and 119 us; 1,000 rows in 500 groups, 256 x 256 63 and 78 us;
 // 4,000 rows 138 and 134. The kernel alone takes 38 us of the first (2.2 TB/s, 76 MB of it written).
-template <typename T, int COLS, bool NARROW>
+// LAYER: rows of a are shared (per), and b's columns are summed beside the products (sums).
+template <typename T, int COLS, bool NARROW, bool LAYER>
 __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter q)
 {
     constexpr int kA = kOuterA * kThreads / COLS;
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter
         __syncthreads();
         for (int i = tid; i < rows * kA; i += kThreads) {
             const int r = i / kA, a = i % kA, own = s_row[r];
-            const int row = q.per > 1 && own >= 0 ? (int)((unsigned)own / (unsigned)q.per) : own;
+            const int row = LAYER && q.per > 1 && own >= 0 ? (int)((unsigned)own / (unsigned)q.per) : own;
             reinterpret_cast<float *>(&s_a[r])[a] =
                 row >= 0 && a0 + a < q.A ? (float)static_cast<const T *>(q.a)[row * q.a_stride + a0 + a] : 0.f;
         }
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 if (r0 + u >= rows) break;
-                column += f[u];
+                if (LAYER) column += f[u];
 #pragma unroll
                 for (int i = 0; i < kOuterA; i += 4) {
                     const float4_t a = s_a[r0 + u][(ai + i) / 4];
@@ -265,8 +266,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter
         }
     }
     if (b >= B) return;
-    if (q.sums && a0 + ai == 0) static_cast<T *>(q.sums)[(int64_t)g * B + b] = (T)column;
-    if (!q.out) return;
+    if (LAYER && q.sums && a0 + ai == 0) static_cast<T *>(q.sums)[(int64_t)g * B + b] = (T)column;
+    if (LAYER && !q.out) return;
     T *const out = static_cast<T *>(q.out) + (int64_t)g * q.A * B;
 #pragma unroll
     for (int i = 0; i < kOuterA; ++i) {
@@ -281,7 +282,8 @@ template <typename T, int COLS> hipError_t outer(const RowOrder &o, const RowOut
     const int B = q.r > 0 ? q.r : q.B;
     const int64_t blocks = (int64_t)o.G * ((q.A + kA - 1) / kA) * ((B + COLS - 1) / COLS);
     if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    auto *kernel = q.r > 0 ? k_row_outer_few<T, COLS, true> : k_row_outer_few<T, COLS, false>;
+    auto *kernel = q.r > 0 ? k_row_outer_few<T, COLS, true, false>
+                           : q.per > 0 ? k_row_outer_few<T, COLS, false, true> : k_row_outer_few<T, COLS, false, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, o, q);
     return hipGetLastError();
 }

@@ -303,17 +303,18 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     fetch(ct0, 0);
     for (int ct = ct0; ct < ct1; ++ct) {
         float16_t acc[2];
-        __syncthreads();
-        stage();
-        __syncthreads();
-        // a layer's bf16 sums start at the bias; fp32's, of scaled parts, get it behind
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                if (EX == kLayer && Q == 1) set_vec<T, !WNK>(acc[c], v, s_bias[(32 * c + vec_col<T, !WNK>(v, half)) / 4]);
-                else set_vec<T, !WNK>(acc[c], v, float4_t{0.f, 0.f, 0.f, 0.f});
-            }
+            for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
+        __syncthreads();
+        stage();
+        __syncthreads();
+        if (EX == kLayer && Q == 1)  // bf16 sums start at the bias; fp32's, of scaled parts, get it behind
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) set_vec<T, !WNK>(acc[c], v, s_bias[(32 * c + vec_col<T, !WNK>(v, half)) / 4]);
         fetch(nseg > 1 || ct + 1 == ct1 ? ct : ct + 1, nseg > 1 ? 1 : 0);
         auto product = [&](int pair, const uint4_t (&b)[Q]) {
             uint4_t c0[Q], c1[Q];
