@@ -222,6 +222,11 @@ __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[
     if (p.blocks > 1) {
         const int size = p.E / p.blocks;
         float *const scores = row_keys + L * PER;
+        // A sum's magnitude stands for those of its keys (below) but where they cancel: those are for 64 bits.
+        auto sum_of = [&](const Two<float> &two) {
+            if (two.second > kNone && two.second < -16.f * most) sure = false;
+            return two.sum();
+        };
         // whether block b is left, by the scores
         auto left = [&](int b) {
             const float own = scores[b], off = 4 * kOffScore * most + 9 * kOffKey * fabsf(own);
@@ -239,7 +244,7 @@ __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[
             Two<float> two;
 #pragma unroll
             for (int j = 0; j < PER; ++j) two.add(f[j]);
-            if (l < p.blocks) scores[l] = two.sum();
+            if (l < p.blocks) scores[l] = sum_of(two);
             wave_sync();
             if (l < p.blocks && !left(l))
 #pragma unroll
@@ -251,7 +256,7 @@ __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[
             for (int b = l; b < p.blocks; b += L) {
                 Two<float> two;
                 for (int i = 0; i < size; ++i) two.add(row_keys[b * size + i]);
-                scores[b] = two.sum();
+                scores[b] = sum_of(two);
             }
             wave_sync();
             for (int b = l; b < p.blocks; b += L)

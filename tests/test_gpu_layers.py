@@ -74,6 +74,18 @@ def test_route_near_ties_are_told_apart(cg):
             assert np.array_equal(ids.cpu().numpy(), ref.route(logits, 6, b, score, blocks, keep, True, 1.0)[0])
 
 
+@pytest.mark.parametrize("size", [8, 5])
+def test_route_blocks_whose_keys_cancel(cg, size):
+    """Biases of both signs, far larger than the scores: the sums of a block's keys keep what the scores say."""
+    rng = np.random.default_rng(5)
+    for by in (1.0, 30.0, 1e4):
+        b = rounded(by * (1 + 1e-6 * rng.standard_normal(6 * size)) * np.where(np.arange(6 * size) % size == 0, 1, -1), F32)
+        logits = rounded(0.01 * rng.standard_normal((2000, 6 * size)), F32)
+        for score in ("softmax", "sigmoid"):
+            ids, _ = cg.route_rows(dev(logits), 4, bias=dev(b), score=score, n_blocks=6, keep_blocks=2)
+            assert np.array_equal(ids.cpu().numpy(), ref.route(logits, 4, b, score, 6, 2, True, 1.0)[0]), (by, score)
+
+
 def test_route_values_that_are_not_finite(cg):
     import torch
 
