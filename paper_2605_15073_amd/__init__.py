@@ -770,7 +770,7 @@ def _grad_out(name, out, shape, like, rows):
     if out is False:
         return None, 0
     if out is None:
-        out = _new(shape, like.dtype, like)
+        return _new(shape, like.dtype, like), shape[-1] if rows else 0
     if rows:
         return out, _want_rows(name, out, *shape, like)
     _want_dev(name, out, shape, like.dtype, like)
@@ -843,6 +843,11 @@ def adapter_linear_grad(x, w, a, b, dy, offsets, order=None, scale=None, dx=None
     return dx, da, db
 
 
+def _out_rows(name, out, n, width, like):
+    """Rows that a call writes, allocated if None; (tensor, row stride)."""
+    return (_new((n, width), like.dtype, like), width) if out is None else (out, _want_rows(name, out, n, width, like))
+
+
 _SCORES = {"softmax": CGTP_SCORE_SOFTMAX, "sigmoid": CGTP_SCORE_SIGMOID}
 _ACTIVATIONS = {None: CGTP_ACT_NONE, "silu": CGTP_ACT_SILU, "gelu": CGTP_ACT_GELU, "relu": CGTP_ACT_RELU}
 
@@ -877,10 +882,12 @@ def route_rows(logits, top_k: int, bias=None, score: str = "softmax", n_blocks: 
     shape = (n, max(k, 0))
     if ids is None:
         ids = _new(shape, torch.int32, logits)
+    else:
+        _want_dev("ids", ids, shape, torch.int32, logits)
     if weights is None:
         weights = _new(shape, torch.float32, logits)
-    _want_dev("ids", ids, shape, torch.int32, logits)
-    _want_dev("weights", weights, shape, torch.float32, logits)
+    else:
+        _want_dev("weights", weights, shape, torch.float32, logits)
     _run("cgtp_route_rows", logits, side, (logits, bias, ids, weights), dt, n, E, k, _addr(logits), ls, _addr(bias), code,
          n_blocks, n_blocks if keep_blocks is None else keep_blocks, int(bool(renormalize)), scale, _addr(ids),
          _addr(weights), handle)
@@ -898,9 +905,7 @@ def route_rows_grad(logits, ids, dweights, score: str = "softmax", renormalize: 
     handle, side = _row_call(logits, stream)
     _want_dev("ids", ids, (n, k), torch.int32, logits)
     _want_dev("dweights", dweights, (n, k), torch.float32, logits)
-    if dlogits is None:
-        dlogits = _new((n, E), logits.dtype, logits)
-    ds = _want_rows("dlogits", dlogits, n, E, logits)
+    dlogits, ds = _out_rows("dlogits", dlogits, n, E, logits)
     _run("cgtp_route_rows_grad", logits, side, (logits, ids, dweights, dlogits), dt, n, E, k, _addr(logits), ls, _addr(ids),
          _addr(dweights), code, int(bool(renormalize)), scale, _addr(dlogits), ds, handle)
     return dlogits
@@ -929,9 +934,7 @@ def grouped_layer(x, w, offsets, order=None, bias=None, activation=None, residua
     if bias is not None:
         _want_dev("bias", bias, (G, n_out), x.dtype, x)
     rs = 0 if residual is None else _want_rows("residual", residual, n, n_out, x)
-    if y is None:
-        y = _new((n, n_out), x.dtype, x)
-    ys = _want_rows("y", y, n, n_out, x)
+    y, ys = _out_rows("y", y, n, n_out, x)
     kept, zs = _grad_out("z", z, (n, n_out), x, True)
     _run("cgtp_grouped_layer", x, side, (x, w, offsets, order, bias, residual, y, kept), dt, n, G, n_in, n_out, per_row,
          _addr(offsets), _addr(order), _addr(x), xs, _addr(w), _addr(bias), act, _addr(residual), rs, _addr(y), ys,
@@ -983,9 +986,7 @@ def mix_rows(y, per_row: int, weights=None, residual=None, out=None, stream=None
     if weights is not None:
         _want_dev("weights", weights, (n, per_row), _torch().float32, y)
     rs = 0 if residual is None else _want_rows("residual", residual, n, width, y)
-    if out is None:
-        out = _new((n, width), y.dtype, y)
-    outs = _want_rows("out", out, n, width, y)
+    out, outs = _out_rows("out", out, n, width, y)
     _run("cgtp_mix_rows", y, side, (y, weights, residual, out), dt, n, per_row, width, _addr(y), ys, _addr(weights),
          _addr(residual), rs, _addr(out), outs, handle)
     return out
@@ -1013,7 +1014,8 @@ def mix_rows_grad(dout, per_row: int, weights=None, y=None, dy=None, dweights=No
         ys = _want_rows("y", y, n * per_row, width, dout)
         if dweights is None:
             dweights = _new((n, per_row), torch.float32, dout)
-        _want_dev("dweights", dweights, (n, per_row), torch.float32, dout)
+        else:
+            _want_dev("dweights", dweights, (n, per_row), torch.float32, dout)
     _run("cgtp_mix_rows_grad", dout, side, (dout, weights, y, dy, dweights), dt, n, per_row, width, _addr(dout), ds,
          _addr(weights), _addr(y) if dweights is not None else None, ys, _addr(dy), dys, _addr(dweights), handle)
     return dy, dweights
@@ -1131,7 +1133,7 @@ def adamw_grad_norm(tensors: AdamWTensors, max_norm: float, grad_scale=None, nor
     for name, out in (("norm", norm), ("scale", scale)):
         if out is None:
             out = _new((1,), torch.float32, first)
-        if out is not False:
+        elif out is not False:
             _want_dev(name, out, (1,), torch.float32, first)
         outs.append(None if out is False else out)
     ws_ptr, ws_len, ws = _row_workspace(tensors._norm_workspace if workspace is None else workspace, 0, first)

@@ -529,13 +529,14 @@ def _adam(cg, grads, dtype):
     return cg.AdamWTensors(like(), [dev(g, dtype) for g in grads], like(), like())
 
 
-@pytest.mark.parametrize("sizes", [(1,), (0, 3), (256, 4096, 4097), (5,) * 300, (1000003, 7, 0, 64)])
+@pytest.mark.parametrize("sizes", [(1,), (0, 3), (0,), (256, 4096, 4097), (5,) * 31, (5,) * 32, (5,) * 33, (5,) * 300,
+                                   (1000003, 7, 0, 64), (2048 * 4096,), (2049 * 4096 + 1, 3)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_grad_norm(cg, sizes, dtype):
     rng = np.random.default_rng(len(sizes))
     grads = [rounded(rng.standard_normal(s) * 10.0 ** -(i % 4), dtype) for i, s in enumerate(sizes)]
     a = _adam(cg, grads, dtype)
-    want = math.sqrt(math.fsum(float(v) ** 2 for g in grads for v in g))
+    want = math.sqrt(math.fsum(float((g ** 2).sum()) for g in grads))       # sums of up to 2^23 in 64 bits: 2^-30 at most
     for gs in (None, 0.5, -2.0):
         g = None if gs is None else dev(np.array([gs]))
         f = 1.0 if gs is None else gs
@@ -581,7 +582,7 @@ def test_grad_norm_refusals(cg):
     with pytest.raises(cg.CgtpError):
         cg.adamw_grad_norm(a, 1.0, norm=False, scale=False)
     with pytest.raises(cg.CgtpError):
-        cg.adamw_grad_norm(a, 1.0, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+        cg.adamw_grad_norm(_adam(cg, [np.ones(10), np.ones(10)], F32), 1.0, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         cg.adamw_grad_norm(a, 1.0, norm=torch.zeros(2, device="cuda"))
     with pytest.raises(ValueError):
