@@ -476,7 +476,7 @@ int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups, int n_in, 
  *           CGTP_MAX_ROUTE_BLOCKS. keep_blocks = n_blocks: all are left.
  *   ids     [n_rows][top_k] int32: the experts of the largest keys, largest first, the lowest expert among equals;
  *           -1 where no expert is left. Keys are compared as the formula gives them in 64 bits; without a bias
- *           and blocks they are the logits.
+ *           by the logits, whose order theirs is.
  *   weights [n_rows][top_k] fp32: scale s, or scale s / (sum of the row's chosen s) where renormalize is 1; 0 beside
  *           -1. Softmax scores of a row that holds NaN or +inf are NaN.
  * 1 <= top_k <= CGTP_MAX_TOP_K, and no more than the experts left; n_rows top_k < 2^31; n_experts <= CGTP_MAX_GROUPS.

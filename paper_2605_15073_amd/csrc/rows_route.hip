@@ -96,6 +96,15 @@ __device__ __forceinline__ int ordered(float f)
 }
 __device__ __forceinline__ float value_of(int k) { return __builtin_bit_cast(float, k ^ (k >> 31 & 0x7fffffff)); }
 
+// A logit of expert e: bf16's lower half is free.
+template <typename T> constexpr Embed kByLogit = sizeof(T) == 2 ? kExpert : kNothing;
+template <typename T> __device__ __forceinline__ int logit_key(float x, int e)
+{
+    const int k = ordered(x + 0.f);  // one zero
+    if (!there(x)) return kGone;
+    return sizeof(T) == 2 ? (k & -65536) | (65535 - e) : k;
+}
+
 template <int L, int D = 1> __device__ __forceinline__ int row_max(int v)
 {
     if constexpr (D < L) {
@@ -172,12 +181,13 @@ __device__ __forceinline__ bool take(int (&key)[PER], int k, int l, const float 
     return sure;
 }
 
-// How far a key in fp32 may be off. s = 1 / (1 + e), and s times a share of at most one: their exponentials are off by
-// 2^-24 (2 + 2.5 |a|) of themselves, a the argument: a score by 2.9 2^-24 of the largest from its own, where s |a| is
-// below 0.37 of that; by 23 from a sum of 512, where the mean of |a| is below log 512 + 2; by 14 more from its
-// additions, 8 of a lane and 6 over lanes, and by 3 from reciprocal and product. The bias adds the rounding of the
-// key, embedding the lane's place 7 steps.
-constexpr float kOffScore = 48 * 0x1p-24f, kOffKey = 9 * 0x1p-23f;
+// How far a score in fp32 may be off, in 2^-24 of the largest. Exponentials of an argument a are off by 2 + 2.5 |a| of
+// 2^-24 of themselves. s = 1 / (1 + e): s (1 - s) of that is below 1.1; the sum and the reciprocal add 1 and 2. A share
+// of a sum: 2.9 from its own, where s |a| is below 0.37 of the largest; 23 from a sum of 512, where the mean of |a| is
+// below log 512 + 2; 14 from its additions, of a lane and over lanes; 3 from reciprocal and product. A bias adds the
+// rounding of the key, kStep of it; the lane's place PER - 1 steps.
+constexpr float kStep = 0x1p-23f;
+__device__ __forceinline__ float off_score(int score) { return (score == CGTP_SCORE_SOFTMAX ? 48.f : 6.f) * 0x1p-24f; }
 
 // The two largest keys of a block, added (one where there is one).
 template <typename Key> struct Two {
@@ -192,7 +202,7 @@ template <typename Key> struct Two {
 };
 
 // The choice by keys in fp32. False where it does not settle it.
-template <int L, int PER>
+template <typename T, int L, int PER>
 __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[PER], float top, int l, float *row_keys,
                                             int *ids)
 {
@@ -222,14 +232,14 @@ __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[
     if (p.blocks > 1) {
         const int size = p.E / p.blocks;
         float *const scores = row_keys + L * PER;
-        // A sum's magnitude stands for those of its keys (below) but where they cancel: those are for 64 bits.
+        // Keys of a sum add up to its magnitude and twice the largest score at most, or they are for 64 bits.
         auto sum_of = [&](const Two<float> &two) {
-            if (two.second > kNone && two.second < -16.f * most) sure = false;
+            if (two.second > kNone && two.second < -most) sure = false;
             return two.sum();
         };
         // whether block b is left, by the scores
         auto left = [&](int b) {
-            const float own = scores[b], off = 4 * kOffScore * most + 9 * kOffKey * fabsf(own);
+            const float own = scores[b], off = 4 * off_score(p.score) * most + 4 * kStep * (fabsf(own) + most);
             int ahead = 0, perhaps = 0;
             for (int i = 0; i < p.blocks; ++i) {
                 const float v = scores[i];
@@ -268,9 +278,14 @@ __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[
         }
     }
     int key[PER];
+    if (!p.bias) {  // the scores' order is the logits'
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = f[j] > kNone ? logit_key<T>(x[j], l * PER + j) : kGone;
+        return take<L, PER, kByLogit<T>>(key, p.k, l, nullptr, ids) && sure;
+    }
 #pragma unroll
     for (int j = 0; j < PER; ++j) key[j] = f[j] > kNone ? (ordered(f[j]) & -PER) | (PER - 1 - j) : kGone;
-    const float off[2] = {2 * kOffScore * most, 2 * kOffKey};
+    const float off[2] = {2 * off_score(p.score) * most, (PER + 1) * kStep};
     return take<L, PER, kPlace>(key, p.k, l, off, ids) && sure;
 }
 
@@ -324,6 +339,9 @@ __device__ __forceinline__ void choose_exact(const RowRoute &p, const float (&x)
 #pragma unroll
         for (int j = 0; j < PER; ++j) key[j] = row_keys[l * PER + j];
     }
+    if (!p.bias)  // the scores' order is the logits'
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = key[j] > kNone ? (double)x[j] : kNone;
     for (int i = 0; i < p.k; ++i) {
         double own = key[0];
 #pragma unroll
@@ -371,19 +389,15 @@ __global__ __launch_bounds__(kThreads) void k_route(RowRoute p)
     char *const mine = sh + wave * wave_bytes(R, L * PER, p.blocks);
     double *const keys = reinterpret_cast<double *>(mine) + r * (L * PER + p.blocks);
     if constexpr (!KEYS) {
-        constexpr Embed kEmbed = sizeof(T) == 2 ? kExpert : kNothing;  // bf16's lower half is free
         int key[PER];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int k = ordered(x[j] + 0.f);  // one zero
-            key[j] = there(x[j]) ? (kEmbed == kExpert ? (k & -65536) | (65535 - (l * PER + j)) : k) : kGone;
-        }
-        take<L, PER, kEmbed>(key, p.k, l, nullptr, ids);
+        for (int j = 0; j < PER; ++j) key[j] = logit_key<T>(x[j], l * PER + j);
+        take<L, PER, kByLogit<T>>(key, p.k, l, nullptr, ids);
     } else if constexpr (PER > 8) {
         choose_exact<L, PER>(p, x, top, l, keys, ids);
     } else {
         float *const keys32 = reinterpret_cast<float *>(mine) + r * (L * PER + p.blocks + 4);
-        const bool sure = choose_near<L, PER>(p, x, top, l, keys32, ids);
+        const bool sure = choose_near<T, L, PER>(p, x, top, l, keys32, ids);
         if (__any(!sure)) {
             wave_sync();
             choose_exact<L, PER>(p, x, top, l, keys, ids);
@@ -535,44 +549,66 @@ __global__ __launch_bounds__(kThreads) void k_route_grad(RowRoute p)
     }
 }
 
-template <typename T, int L, int PER> hipError_t launch(const RowRoute &p, bool gradient, hipStream_t s)
+template <typename T, int L, int PER, bool KEYS> hipError_t route(const RowRoute &p, hipStream_t s)
 {
     constexpr int rows = kWaves * (64 / L);
     const TileGrid grid = tile_grid((p.n + rows - 1) / rows);
-    const dim3 blocks(grid.x, 1, grid.z);
-    if (gradient) {
-        hipLaunchKernelGGL((k_route_grad<T, L, PER>), blocks, dim3(kThreads), 0, s, p);
-        return hipGetLastError();
-    }
-    const bool keys = p.bias || p.blocks > 1;
     const size_t lds = p.blocks > 1 ? (size_t)kWaves * wave_bytes(64 / L, L * PER, p.blocks) : 0;
-    auto *kernel = keys ? k_route<T, L, PER, true> : k_route<T, L, PER, false>;
-    hipLaunchKernelGGL(kernel, blocks, dim3(kThreads), lds, s, p);
+    hipLaunchKernelGGL((k_route<T, L, PER, KEYS>), dim3(grid.x, 1, grid.z), dim3(kThreads), lds, s, p);
     return hipGetLastError();
 }
 
-template <typename T> hipError_t pick(const RowRoute &p, bool gradient, hipStream_t s)
+// Sixteen logits a lane, eight keys: us with eight and sixteen, bf16, 525,308 rows of 64, 4 of them, by the logits 32
+// and 27, by a bias 51 and 54, in blocks 71 and 112 (more rows of a wave share the 64-bit choice of one).
+template <typename T, int L> hipError_t route(const RowRoute &p, hipStream_t s)
 {
-    if (p.E <= 8) return launch<T, 1, 8>(p, gradient, s);
-    if (p.E <= 16) return launch<T, 2, 8>(p, gradient, s);
-    if (p.E <= 32) return launch<T, 4, 8>(p, gradient, s);
-    if (p.E <= 64) return launch<T, 8, 8>(p, gradient, s);
-    if (p.E <= 128) return launch<T, 16, 8>(p, gradient, s);
-    if (p.E <= 256) return launch<T, 32, 8>(p, gradient, s);
-    if (p.E <= 512) return launch<T, 64, 8>(p, gradient, s);
-    return launch<T, 64, 64>(p, gradient, s);
+    if (p.bias || p.blocks > 1) return route<T, L, 8, true>(p, s);
+    return route<T, L / 2, 16, false>(p, s);
+}
+
+template <typename T, int L, int PER> hipError_t gradient(const RowRoute &p, hipStream_t s)
+{
+    constexpr int rows = kWaves * (64 / L);
+    const TileGrid grid = tile_grid((p.n + rows - 1) / rows);
+    hipLaunchKernelGGL((k_route_grad<T, L, PER>), dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t pick(const RowRoute &p, hipStream_t s)
+{
+    const bool keys = p.bias || p.blocks > 1;
+    if (p.E <= 8) return keys ? route<T, 1, 8, true>(p, s) : route<T, 1, 8, false>(p, s);
+    if (p.E <= 16) return route<T, 2>(p, s);
+    if (p.E <= 32) return route<T, 4>(p, s);
+    if (p.E <= 64) return route<T, 8>(p, s);
+    if (p.E <= 128) return route<T, 16>(p, s);
+    if (p.E <= 256) return route<T, 32>(p, s);
+    if (p.E <= 512) return route<T, 64>(p, s);
+    return keys ? route<T, 64, 64, true>(p, s) : route<T, 64, 64, false>(p, s);
+}
+
+template <typename T> hipError_t pick_gradient(const RowRoute &p, hipStream_t s)
+{
+    if (p.E <= 8) return gradient<T, 1, 8>(p, s);
+    if (p.E <= 16) return gradient<T, 2, 8>(p, s);
+    if (p.E <= 32) return gradient<T, 4, 8>(p, s);
+    if (p.E <= 64) return gradient<T, 8, 8>(p, s);
+    if (p.E <= 128) return gradient<T, 16, 8>(p, s);
+    if (p.E <= 256) return gradient<T, 32, 8>(p, s);
+    if (p.E <= 512) return gradient<T, 64, 8>(p, s);
+    return gradient<T, 64, 64>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_route_rows(int dtype, const RowRoute &p, hipStream_t s)
 {
-    return dtype == CGTP_BF16 ? pick<bf16_t>(p, false, s) : pick<float>(p, false, s);
+    return dtype == CGTP_BF16 ? pick<bf16_t>(p, s) : pick<float>(p, s);
 }
 
 hipError_t launch_route_rows_grad(int dtype, const RowRoute &p, hipStream_t s)
 {
-    return dtype == CGTP_BF16 ? pick<bf16_t>(p, true, s) : pick<float>(p, true, s);
+    return dtype == CGTP_BF16 ? pick_gradient<bf16_t>(p, s) : pick_gradient<float>(p, s);
 }
 
 }  // namespace cgtp
