@@ -250,13 +250,20 @@ __device__ __forceinline__ bool choose_near(const RowRoute &p, const float (&x)[
             if (own > kNone && (!(own < -kNone) || (ahead < p.keep && perhaps > p.keep))) sure = false;
             return ahead < p.keep;
         };
-        if (size == PER && p.blocks <= L) {  // a block is a lane's
+        const int lanes = size / PER;
+        if (size % PER == 0 && (lanes & (lanes - 1)) == 0) {  // a block is one lane's, or 2, 4, 8, ... lanes'
             Two<float> two;
 #pragma unroll
             for (int j = 0; j < PER; ++j) two.add(f[j]);
-            if (l < p.blocks) scores[l] = sum_of(two);
+            for (int d = 1; d < lanes; d *= 2) {
+                const float first = __shfl_xor(two.first, d), second = __shfl_xor(two.second, d);
+                two.add(first);
+                two.add(second);
+            }
+            const int b = l / lanes;
+            if (b < p.blocks && l % lanes == 0) scores[b] = sum_of(two);
             wave_sync();
-            if (l < p.blocks && !left(l))
+            if (b < p.blocks && !left(b))
 #pragma unroll
                 for (int j = 0; j < PER; ++j) f[j] = kNone;
         } else {
