@@ -13,7 +13,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libcgtp.so")
 SOURCES = ["plan.cpp", "tables.cpp", "order.cpp", "rows.cpp", "contract.hip", "contract_rows.hip", "kernels.hip", "onsite.hip", "receiver_mfma.hip",
            "receiver_values.hip", "folded.hip",
-           "fourier_mfma.hip", "noalloc.hip", "group_rows.hip", "rows_product.hip", "rows_outer.hip", "rows_wide.hip", "layer_wide_bf16.hip", "layer_wide_f32.hip", "rows_few.hip", "layer_grad.hip", "rows_route.hip", "rows_mix.hip", "adamw.hip"]
+           "fourier_mfma.hip", "noalloc.hip", "group_rows.hip", "rows_product.hip", "rows_outer.hip", "rows_wide.hip", "layer_wide_bf16.hip", "layer_wide_f32.hip", "rows_few.hip", "rows_thin.hip", "layer_grad.hip", "rows_route.hip", "rows_mix.hip", "adamw.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Per-source flags. The receivers' matrix-core results feed vector ALU products at once, those of
 # the row products the conversion of a store: accumulating them in VGPRs (not AccVGPRs) saves a
@@ -21,7 +21,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
                 for src in ("receiver_mfma.hip", "receiver_values.hip", "rows_product.hip",
                             "rows_outer.hip", "rows_wide.hip", "layer_wide_bf16.hip", "layer_wide_f32.hip",
-                            "layer_grad.hip")}
+                            "rows_thin.hip", "layer_grad.hip")}
 
 # Packed fp32 VALU ops are disabled for all device code.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

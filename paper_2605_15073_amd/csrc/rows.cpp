@@ -685,6 +685,7 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
         p.out = per_row > 1 ? rows : dx;
         p.out_stride = per_row > 1 ? n_in : dx_stride;
         p.out_f32 = per_row > 1 && dtype == CGTP_BF16;
+        p.split_k = true;
         e = cgtp::launch_row_product(dtype, o, p, s);
         if (e != hipSuccess) return hip_fail(e, "row gradient");
         if (per_row > 1) {

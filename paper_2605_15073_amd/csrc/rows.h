@@ -54,6 +54,7 @@ struct RowProduct {
     void *z;
     int64_t z_stride;
     int64_t xcd_tiles; // 0, or tiles of an XCD, which follow each other there (rows_index.h)
+    bool split_k;      // sums may be split over k (rows_thin.hip); layers' may
     bool out_f32;      // row gradients of rows that share their input: out is fp32 whatever the type
 };
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
@@ -65,6 +66,9 @@ bool layer_wide_takes(int dtype, const RowProduct &p);
 hipError_t launch_layer_wide(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
 hipError_t launch_layer_wide_bf16(const RowOrder &o, const RowProduct &p, hipStream_t s);
 hipError_t launch_layer_wide_f32(const RowOrder &o, const RowProduct &p, hipStream_t s);
+// The form for long inputs and few tiles (rows_thin.hip), and whether it covers a product.
+bool row_thin_takes(int dtype, const RowOrder &o, const RowProduct &p);
+hipError_t launch_row_thin(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
 // Whether adapters get tiles of 128 rows of their own, in which the product forms the narrow rows itself: where they
 // have 64 rows on the mean, or all tiles run at once anyway. Us in one launch, and with a narrow product of its own
 // and tiles that adapters share: 300 adapters of 1, 8 and 48 rows, bf16, y 64 -> 896, rank 16 23 and 94, 28 and 33,

@@ -406,6 +406,7 @@ template <typename T, bool WNK>
 hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
+    if ((p.per > 0 || p.split_k) && !row_few_takes(dtype, o, p) && row_thin_takes(dtype, o, p)) return launch_row_thin(dtype, o, p, s);
     if constexpr (WNK && sizeof(T) == 2)
         if (p.out_f32) return pick_extra<T, true, kSums>(o, p, s);
     if constexpr (!WNK)

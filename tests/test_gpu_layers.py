@@ -183,7 +183,8 @@ LAYERS = [(1, 1, 1, 1, 1), (1, 1, 3, 64, 64), (2, 1, 5, 7, 3), (64, 1, 5, 64, 64
           (515, 1, 2, 1, 300), (515, 1, 2, 300, 1), (90, 1, 80, 200, 130), (1, 8, 8, 64, 64), (33, 3, 5, 31, 67),
           (500, 4, 32, 128, 448), (700, 2, 3, 64, 64), (129, 64, 40, 9, 20), (600, 2, 4, 8, 64), (400, 4, 1000, 16, 24),
           (3000, 1, 2, 64, 64), (2500, 2, 6, 40, 56), (1000, 4, 5, 128, 448), (900, 1, 3, 100, 130), (700, 2, 2, 128, 250),
-          (3000, 1, 4, 40, 128), (1200, 1, 3, 33, 447), (800, 1, 2, 128, 100), (600, 1, 2, 4, 5), (600, 1, 2, 129, 90)]
+          (3000, 1, 4, 40, 128), (1200, 1, 3, 33, 447), (800, 1, 2, 128, 100), (600, 1, 2, 4, 5), (600, 1, 2, 129, 90),
+          (70, 1, 3, 1344, 33), (31, 2, 40, 647, 8), (200, 3, 2, 8, 1345), (6000, 1, 3, 450, 96)]
 ACTS = ["silu", "gelu", "relu", "none"]
 
 
@@ -332,13 +333,14 @@ def test_layer_grad_against_differences(cg, act):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ACTS)
-@pytest.mark.parametrize("N,keep", [(72, True), (96, True), (96, False), (73, False), (61, True)])
-def test_layer_keeps_values_that_are_not_finite_apart(cg, dtype, act, N, keep):
+@pytest.mark.parametrize("N,keep,K", [(72, True, 40), (96, True, 40), (96, False, 40), (73, False, 40), (61, True, 40),
+                                      (70, True, 333), (65, False, 256)])
+def test_layer_keeps_values_that_are_not_finite_apart(cg, dtype, act, N, keep, K):
     """An infinite or NaN input, weight or residual reaches its own rows' results and no others."""
     import torch
 
     rng = np.random.default_rng(15)
-    t, per, G, K = 400, 2, 4, 40
+    t, per, G = 400, 2, 4
     x, w, b, ids = draw_layer(rng, t, per, G, K, N, "even", dtype)
     o = cg.group_rows(dev(ids), G)
 
