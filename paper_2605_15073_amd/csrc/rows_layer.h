@@ -9,8 +9,9 @@
 namespace cgtp {
 namespace rows {
 
-// What a launch does beside the product: nothing, a layer's bias, activation and residual, or rows of sums in fp32.
-enum Extra { kBare, kLayer, kSums };
+// What a launch does beside the product: nothing, a layer's bias, activation and residual, or rows of sums in fp32; kGrad:
+// nothing, for a layer's row gradient.
+enum Extra { kBare, kLayer, kSums, kGrad };
 
 // silu: z s(z), s the logistic function; gelu: z P(z), P the normal distribution function; relu: max(z, 0).
 // An infinite z gives what the formula's products do: -inf s(-inf) is NaN.

@@ -23,6 +23,14 @@
 // through LDS as the input rows of one more step (bf16 ranks above 16: two, as its parts fill them), over the
 // adapter's second matrix: 131,327 rows of 8 adapters, 896 -> 128, rank 16, fp32 290 us, bf16 86; 100,000 rows of 100,
 // fp32 265 where the two products apart take 298, bf16 71 and 105.
+//
+// Layers and their row gradients (EX) have no adapters: a step all of whose k exist loads from pointers that move along and
+// stages without a condition, and the workgroups of a tile's columns follow each other on one XCD, so that its rows come
+// from one L2. Us without both and now: 60,000 rows of 32 groups, 1344 -> 448, bf16 y 152 and 125, dx 161 and 115; fp32
+// 631 and 541, 599 and 512; 6,000 of 20, bf16 43 and 36, 36 and 30; 262,144, 448 -> 128, y 92 and 89, dx 83 and 82. Steps
+// two ahead in flight, bf16, gave nothing (36; 110 of 262,144 rows), nor did steps without any branch where widths are
+// whole vectors (37; 90): with two waves a SIMD the matrix cores are busy a quarter of the time, as are LDS and the
+// vector ALU, each waiting for the others between two barriers a step.
 #include "internal.h"
 #include "rows_layer.h"
 
@@ -32,8 +40,12 @@ namespace {
 
 using namespace rows;
 
+// Waves of a SIMD that bf16 registers have to leave room for: a gradient from 448 columns, 262,144 rows, 83 us with three
+// and 87 with two.
+template <Extra EX> constexpr int kLeanWaves = EX == kBare ? 1 : 3;
+
 template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED, Extra EX>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_product(RowOrder o, RowProduct p, int splits)
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void k_row_product(RowOrder o, RowProduct p, int splits)
 {
     constexpr int KG = kGroups<T>, BK = kStep<T>, P = kNarrow<T>, Q = kSplit<T>, CW = kWide<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
@@ -44,15 +56,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     constexpr int kLanes = kThreads / KG;              // rows staged at once
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
     constexpr int NC = (BX + kLanes - 1) / kLanes;
+    constexpr bool kLean = EX != kBare && WIDE;  // no adapters: whole steps load and stage without a condition
     __shared__ uint4_t s_tiles[kTile<T, BX> + kTile<T, BM>];
     uint4_t *const s_cols = s_tiles, *const s_rows = s_tiles + kTile<T, BX>;
     __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg, s_any;
 
     const bool shared_w = !FUSED && p.w_group == 0;
     int64_t index = tile_at(blockIdx.x, blockIdx.z, gridDim.x);
-    if (EX == kLayer) {
+    int share = blockIdx.y;
+    if (EX != kBare) {
         if (p.xcd_tiles > 0) index = xcd_tile(index, p.xcd_tiles);
         if (index < 0) return;
+        if (splits > 1) {  // the shares of a tile's columns follow each other
+            share = (int)(index % splits);
+            index /= splits;
+        }
     }
     Tile t;
     if (shared_w) {
@@ -69,8 +87,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     const int rows = (int)(t.p1 - t.p0);
     // this workgroup's column tiles
     const int ctiles = (p.N + BN - 1) / BN;
-    const int ct0 = (int)((int64_t)ctiles * blockIdx.y / splits);
-    const int ct1 = (int)((int64_t)ctiles * (blockIdx.y + 1) / splits);
+    const int ct0 = (int)((int64_t)ctiles * share / splits);
+    const int ct1 = (int)((int64_t)ctiles * (share + 1) / splits);
     if (ct0 >= ct1) return;
     const int col_end = ct1 * BN < p.N ? ct1 * BN : p.N;
 
@@ -80,7 +98,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     if (!FUSED && !shared_w && t.g == o.G) {  // rows of no group
         if (p.narrow) return;
         __syncthreads();
-        if constexpr (EX != kBare) store_bare<T>(p, s_row, rows, ct0 * BN, col_end);
+        if constexpr (EX == kLayer || EX == kSums) store_bare<T>(p, s_row, rows, ct0 * BN, col_end);
         else store_zeros<T>(p, s_row, rows, ct0 * BN, col_end);
         return;
     }
@@ -128,11 +146,46 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
         int xk, wk;  // values that exist of this thread's k-group of rows and weights
         int xe, we;  // what their loads started early
         unsigned rows;  // bit i: x[i] is of a row that takes part
+        bool whole;     // kLean: all k of the step exist
     } l;
+    // kLean: where this thread's weights of the column tile start
+    const T *col[kLean ? (WNK ? NC : 1) : 1];
+    auto to_columns = [&](int ct) {
+        const int c0 = ct * BN;
+        if constexpr (WNK) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const int c = c0 + rr + kLanes * i;
+                col[i] = w + (int64_t)(c < p.N ? c : p.N - 1) * p.K + kg * kU;
+            }
+        } else {
+            const int c = c0 + CW * tc;
+            col[0] = w + (int64_t)(tg * kU) * p.N + (c + CW <= p.N ? c : p.N - CW);
+            l.we = c + CW <= p.N || c >= p.N ? 0 : c + CW - p.N;
+        }
+    };
     float odd = 0.f;  // NaN once a result is not finite
     float sign = 1.f;  // of the step's rows
     auto fetch = [&]() {
         if (!WIDE && next.ct >= ct1) return;  // else past the last step the last tile's first loads again
+        if constexpr (kLean) {
+            l.whole = next.k + BK <= p.K && next.ct < ct1;
+            if (l.whole) {
+                if (next.k == 0) to_columns(next.ct);
+#pragma unroll
+                for (int i = 0; i < NR; ++i) l.x[i] = load_any8(in[i] + next.k + kg * kU);
+                if constexpr (WNK) {
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) l.wn[i] = load_any8(col[i] + next.k);
+                } else {
+                    const T *const q = col[0] + (int64_t)next.k * p.N;
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) l.wt[u] = *reinterpret_cast<const uint2_any *>(q + (int64_t)u * p.N);
+                }
+                advance(next);
+                return;
+            }
+        }
         const bool ext = next.seg >= 0;
         const int seg = ext ? next.seg : 0, c0 = (next.ct < ct1 ? next.ct : ct1 - 1) * BN, k = next.k;
         const int K = ext ? P * W : p.K;   // of the rows
@@ -186,6 +239,32 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
     };
     auto stage = [&]() {
         uint4_t u[Q];
+        if (kLean && l.whole) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                if (BM < kLanes && rr >= BM) break;
+                to_units(l.x[i], u, sign);
+                put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
+            }
+            if constexpr (WNK) {
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    if (BX % kLanes != 0 && rr + kLanes * i >= BX) break;
+                    to_units(l.wn[i], u);
+                    put<T, BX>(s_cols, KG, kg, rr + kLanes * i, u);
+                }
+            } else if (has_w) {
+                if (p.N % CW != 0 && l.we > 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) settle<T>(l.wt[e], l.we);
+                }
+                uint4_t c[CW][Q];
+                to_units(l.wt, c);
+#pragma unroll
+                for (int j = 0; j < CW; ++j) put<T, BX>(s_cols, KG, tg, place<T>(CW * tc + j), c[j]);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             if (BM < kLanes && rr >= BM) break;
@@ -254,7 +333,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 1) void k_row_produc
             for (int r = 0; r < TR; ++r) {
                 const int row = s_row[r0 + 32 * r + (lane & 31)];
                 if (row < 0) continue;
-                if constexpr (EX == kBare) {
+                if constexpr (EX == kBare || EX == kGrad) {
                     T *const q = static_cast<T *>(p.out) + row * p.out_stride;
 #pragma unroll
                     for (int c = 0; c < TC; ++c)
@@ -374,9 +453,9 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
     auto *kernel = FUSED || wide ? k_row_product<T, WNK, BM, BN, WR, true, FUSED, EX>
                                  : k_row_product<T, WNK, BM, BN, WR, FUSED, FUSED, EX>;
     RowProduct by_xcd = p;
-    if (p.xcd_tiles > 0) by_xcd.xcd_tiles = tiles_per_xcd(tiles);
-    const TileGrid grid = tile_grid(by_xcd.xcd_tiles > 0 ? kTileXcds * by_xcd.xcd_tiles : tiles);
-    hipLaunchKernelGGL(kernel, dim3(grid.x, (unsigned)splits, grid.z), dim3(kThreads), 0, s, o, by_xcd, splits);
+    by_xcd.xcd_tiles = EX != kBare && (p.xcd_tiles > 0 || splits > 1) ? tiles_per_xcd(tiles * splits) : 0;
+    const TileGrid grid = tile_grid(EX == kBare ? tiles : by_xcd.xcd_tiles > 0 ? kTileXcds * by_xcd.xcd_tiles : tiles * splits);
+    hipLaunchKernelGGL(kernel, dim3(grid.x, EX == kBare ? (unsigned)splits : 1, grid.z), dim3(kThreads), 0, s, o, by_xcd, splits);
     return hipGetLastError();
 }
 
@@ -409,6 +488,9 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
     if ((p.per > 0 || p.split_k) && !row_few_takes(dtype, o, p) && row_thin_takes(dtype, o, p)) return launch_row_thin(dtype, o, p, s);
     if constexpr (WNK && sizeof(T) == 2)
         if (p.out_f32) return pick_extra<T, true, kSums>(o, p, s);
+    if constexpr (WNK)
+        if (p.split_k && !row_few_takes(dtype, o, p) && (o.n < 40 * (int64_t)o.G || !row_wide_takes(dtype, p)))
+            return pick_extra<T, true, kGrad>(o, p, s);
     if constexpr (!WNK)
         if (p.per > 0) return pick_extra<T, false, kLayer>(o, p, s);
     if constexpr (WNK)
