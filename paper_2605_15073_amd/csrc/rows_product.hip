@@ -27,7 +27,7 @@
 // Layers and their row gradients (EX) have no adapters: a step all of whose k exist loads from pointers that move along and
 // stages without a condition, and the workgroups of a tile's columns follow each other on one XCD, so that its rows come
 // from one L2. Us without both and now: 60,000 rows of 32 groups, 1344 -> 448, bf16 y 152 and 125, dx 161 and 115; fp32
-// 631 and 541, 599 and 512; 6,000 of 20, bf16 43 and 36, 36 and 30; 262,144, 448 -> 128, y 92 and 89, dx 83 and 82. Steps
+// 631 and 541, 599 and 512; 6,000 of 20, in tiles of 128, bf16 43 and 36, 36 and 30; 262,144, 448 -> 128, y 92 and 89, dx 83 and 82. Steps
 // two ahead in flight, bf16, gave nothing (36; 110 of 262,144 rows), nor did steps without any branch where widths are
 // whole vectors (37; 90): with two waves a SIMD the matrix cores are busy a quarter of the time, as are LDS and the
 // vector ALU, each waiting for the others between two barriers a step.
@@ -462,6 +462,17 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 // Whether tiles of 128 by 128 would leave compute units without one.
 bool idle(const RowOrder &o, const RowProduct &p) { return (o.n / 128 + o.G) * ((p.N + 127) / 128) < 256; }
 
+// Whether tiles of 64 by 64, of which 1,024 run at once, end before those of 128 by 128, of which 512 do. Us of 128 and 64,
+// with the tiles of each: fp32 y of 6,000 rows of 20 groups, 1344 -> 448, 117 and 93 (264, 791), 12,500 of 3, 126 and 156
+// (400, 1,386), 24,000 of 10, 1344 -> 258, 222 and 196 (591, 1,925), 12,500 of 3, 300 -> 897, 78 and 103 (800, 2,970); dx
+// 104 and 80, 114 and 128, 218 and 167, 70 and 84; bf16 dx 31 and 25, 33 and 36, 43 and 43, 33 and 36. bf16 y, 37 and 37,
+// 38 and 52, 53 and 72, 38 and 57: only where compute units would be idle.
+bool small_sooner(const RowOrder &o, const RowProduct &p)
+{
+    const int64_t big = (o.n / 128 + o.G) * ((p.N + 127) / 128), small = (o.n / 64 + o.G) * ((p.N + 63) / 64);
+    return small <= 1024 * ((big + 511) / 512);
+}
+
 // Tiles as pick() takes them.
 template <typename T, bool WNK, Extra EX>
 hipError_t pick_extra(const RowOrder &o, const RowProduct &p, hipStream_t s)
@@ -477,7 +488,8 @@ hipError_t pick_extra(const RowOrder &o, const RowProduct &p, hipStream_t s)
         return launch_layer_wide(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4, false, EX>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1, false, EX>(o, p, s);
-    if (few || p.N <= 64 || idle(o, p)) return launch<T, WNK, 64, 64, 2, false, EX>(o, p, s);
+    const bool small = WNK || sizeof(T) == 4 ? small_sooner(o, p) : idle(o, p);
+    if (few || p.N <= 64 || small) return launch<T, WNK, 64, 64, 2, false, EX>(o, p, s);
     return launch<T, WNK, 128, 128, kWaveRows<T>, false, EX>(o, p, s);
 }
 
