@@ -289,6 +289,46 @@ def test_layer_grad_of_long_groups(cg, dtype, act):
         check(only, ref.layer_grad(x, w, z, dy, ids, act, per, dtype)[2], "dbias alone")
 
 
+@pytest.mark.parametrize("t,per,G,K,N,act,kind,pad", [
+    (66001, 1, 3, 100, 72, "silu", "holes", 3), (16700, 4, 33, 128, 168, "gelu", "holes", 8), (70000, 1, 7, 33, 200, "relu", "one", 1),
+    (33000, 2, 2, 16, 136, "none", "holes", 0), (65600, 1, 1, 90, 8, "silu", "even", 0), (66000, 1, 4, 128, 448, "silu", "even", 0),
+    (65537, 1, 128, 65, 16, "gelu", "even", 0), (70000, 1, 3, 40, 24, "silu", "none", 0)])
+def test_layer_grad_of_many_rows(cg, t, per, G, K, N, act, kind, pad):
+    """Rows in order and not, and rows that the order does not hold."""
+    import torch
+
+    rng = np.random.default_rng(17)
+    x, w, b, ids = draw_layer(rng, t, per, G, K, N, kind, "bf16")
+    z, dy = (rounded(rng.standard_normal((t * per, N)), "bf16") for _ in range(2))
+    kw = dict(z=None if act == "none" else strided(dev(z, "bf16"), pad), activation=named(act), per_row=per)
+    a = (strided(dev(x, "bf16"), pad), dev(w, "bf16"), strided(dev(dy, "bf16"), pad))
+    o = cg.group_rows(dev(ids), G)
+    want = ref.layer_grad(x, w, z, dy, ids, act, per, "bf16")
+    got = cg.grouped_layer_grad(*a, *o, **kw)
+    again = cg.grouped_layer_grad(*a, *o, **kw)
+    for g, h, v, name in zip(got, again, want, ("dx", "dw", "dbias")):
+        check(g, v, name)
+        assert torch.equal(g, h), name
+    check(cg.grouped_layer_grad(*a, *o, dw=False, dbias=False, **kw)[0], want[0], "dx alone")
+    if per > 1:
+        return
+    by = o[1].long()
+    sorted_kw = {**kw, "z": None if act == "none" else kw["z"][by]}
+    for g, h, name in zip(cg.grouped_layer_grad(a[0][by], a[1], a[2][by], o[0], **sorted_kw), got, ("dx", "dw", "dbias")):
+        assert torch.equal(g, h[by] if name == "dx" else h), name
+    # every 97th position without a row
+    order = o[1].clone()
+    order[::97] = -1
+    gone = torch.zeros(t, dtype=torch.bool, device="cuda")
+    gone[o[1][::97].long()] = True
+    dx = torch.full((t, K), 7.0, dtype=a[0].dtype, device="cuda")
+    got = cg.grouped_layer_grad(*a, o[0], order, dx=dx, **kw)
+    assert (dx[gone] == 7).all() and torch.equal(dx[~gone], again[0][~gone])
+    rest = ref.layer_grad(x, w, z, dy, np.where(gone.cpu().numpy(), -1, ids), act, per, "bf16")
+    for g, v, name in zip(got[1:], rest[1:], ("dw", "dbias")):
+        check(g, v, name)
+
+
 def test_layer_grad_of_no_rows(cg):
     import torch
 
