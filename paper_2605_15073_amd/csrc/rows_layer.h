@@ -163,6 +163,36 @@ __device__ __forceinline__ void store_layer(const RowProduct &p, int g, bool gro
     store_four<false>(static_cast<T *>(p.out) + row * p.out_stride + col, x, left);
 }
 
+// Columns col .. col + 7 of it in bf16, in vectors of 16 bytes: 131,327 rows of four, 448 -> 128, with z 282 us by fours, 231
+// by eights; 20,000 of 10 groups, 300 -> 897, 81 and 66; 262,144, 448 -> 128, 102 and 95.
+__device__ __forceinline__ void store_layer8(const RowProduct &p, int g, int64_t row, int col, float4_t lo, float4_t hi)
+{
+    typedef bf8_t any_t __attribute__((aligned(2)));
+    const int left = p.N - col;
+    if (left < 8) {
+        store_layer<bf16_t, false>(p, g, true, row, col, lo);
+        store_layer<bf16_t, false>(p, g, true, row, col + 4, hi);
+        return;
+    }
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = lo[e];
+        x[4 + e] = hi[e];
+    }
+    auto add = [&](const void *from, int64_t at) {
+        const bf8_t b = *reinterpret_cast<const any_t *>(static_cast<const bf16_t *>(from) + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += (float)b[e];
+    };
+    if (p.bias) add(p.bias, (int64_t)g * p.N + col);
+    if (p.z) store_values(static_cast<bf16_t *>(p.z) + row * p.z_stride + col, x, 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = activate<bf16_t>(x[e], p.act);
+    if (p.residual) add(p.residual, row * p.residual_stride + col);
+    store_values(static_cast<bf16_t *>(p.out) + row * p.out_stride + col, x, 8);
+}
+
 // One value of it, from its sum.
 template <typename T> __device__ __forceinline__ void store_layer_one(const RowProduct &p, int g, int64_t row, int c, float x)
 {

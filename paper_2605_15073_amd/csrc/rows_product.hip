@@ -27,10 +27,10 @@
 // Layers and their row gradients (EX) have no adapters: a step all of whose k exist loads from pointers that move along and
 // stages without a condition, and the workgroups of a tile's columns follow each other on one XCD, so that its rows come
 // from one L2. Us without both and now: 60,000 rows of 32 groups, 1344 -> 448, bf16 y 152 and 125, dx 161 and 115; fp32
-// 631 and 541, 599 and 512; 6,000 of 20, in tiles of 128, bf16 43 and 36, 36 and 30; 262,144, 448 -> 128, y 92 and 89, dx 83 and 82. Steps
-// two ahead in flight, bf16, gave nothing (36; 110 of 262,144 rows), nor did steps without any branch where widths are
-// whole vectors (37; 90): with two waves a SIMD the matrix cores are busy a quarter of the time, as are LDS and the
-// vector ALU, each waiting for the others between two barriers a step.
+// 631 and 541, 599 and 512; 6,000 of 20, in tiles of 128, bf16 43 and 36, 36 and 30; 262,144, 448 -> 128, y 92 and 89, dx
+// 83 and 82. Two steps ahead in flight, bf16, gave nothing (36; 110 of 262,144 rows), nor did steps without any branch
+// where widths are whole vectors (37; 90): with two waves a SIMD the matrix cores are busy a quarter of the time, as are
+// LDS and the vector ALU, each waiting for the others between two barriers a step.
 #include "internal.h"
 #include "rows_layer.h"
 
@@ -349,6 +349,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
                         for (int v = 0; v < 4; ++v) {
                             const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
                             const float4_t x = vec_val<T, !WNK>(acc[c][r], v);
+                            if constexpr (EX == kLayer && sizeof(T) == 2) {  // vectors v and v + 1 follow each other
+                                if (v % 2 == 0) store_layer8(p, t.g, row, col, x, vec_val<T, !WNK>(acc[c][r], v + 1));
+                                continue;
+                            }
                             if (EX == kLayer) store_layer<T, (Q > 1)>(p, t.g, true, row, col, x);
                             else store_four<false>(static_cast<float *>(p.out) + row * p.out_stride + col, x, p.N - col);
                         }
