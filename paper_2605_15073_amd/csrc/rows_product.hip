@@ -40,6 +40,26 @@ namespace {
 
 using namespace rows;
 
+// Eight columns from col on, of which N exist. A lane below 32 holds the first four of a in its row and the lane 32 above
+// the other four, and so with b, eight columns on: each gets the eight of one. Row gradients, us with eight bytes a store
+// and sixteen: 262,144 rows, 448 -> 128, 87 and 78; 896 -> 128 158 and 146; 60,000, 256 -> 896, 78 and 62.
+__device__ __forceinline__ void store_traded(bf16_t *row, int col, int N, float4_t a, float4_t b)
+{
+    const bf4_t ha = {(bf16_t)a[0], (bf16_t)a[1], (bf16_t)a[2], (bf16_t)a[3]}, hb = {(bf16_t)b[0], (bf16_t)b[1], (bf16_t)b[2], (bf16_t)b[3]};
+    const uint2_t ua = __builtin_bit_cast(uint2_t, ha), ub = __builtin_bit_cast(uint2_t, hb);
+    uint4_t both;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {  // a's upper lanes for b's lower ones
+        const auto t = __builtin_amdgcn_permlane32_swap(ua[i], ub[i], false, false);
+        both[i] = t[0];
+        both[2 + i] = t[1];
+    }
+    if (col + 8 <= N) *reinterpret_cast<uint4_any *>(row + col) = both;
+    else
+        for (int e = 0; e < 8; ++e)
+            if (col + e < N) row[col + e] = __builtin_bit_cast(bf8_t, both)[e];
+}
+
 // Waves of a SIMD that bf16 registers have to leave room for: a gradient from 448 columns, 262,144 rows, 83 us with three
 // and 87 with two.
 template <Extra EX> constexpr int kLeanWaves = EX == kBare ? 1 : 3;
@@ -339,6 +359,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
                     for (int c = 0; c < TC; ++c)
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
+                            if constexpr (EX == kGrad && sizeof(T) == 2) {
+                                // the wave's halves trade, so that each has eight columns that follow each other
+                                if (v % 2 == 0)
+                                    store_traded(q, c0 + 32 * c + 8 * (v + half), p.N, vec_val<T, !WNK>(acc[c][r], v),
+                                                 vec_val<T, !WNK>(acc[c][r], v + 1));
+                                continue;
+                            }
                             const int col = c0 + 32 * c + vec_col<T, !WNK>(v, half);
                             store_four<false>(q + col, vec_val<T, !WNK>(acc[c][r], v), p.N - col);
                         }
