@@ -1,5 +1,5 @@
-// All gradients of a narrow layer (up to kWidth inputs and outputs) in one pass over its rows: dz is formed once, from
-// dy and z as they are read, and serves both products.
+// The gradients of a narrow layer (up to kWidth inputs and outputs) in one pass over its rows: dz is formed once, from
+// dy and z as they are read, and serves both products. Whichever of them are asked for, each has the same bits.
 //
 // A workgroup owns a chunk of a group's rows and takes them kTileRows at a time. Half of the waves load x, half dy and z,
 // 8 rows by 4 columns a thread, a tile ahead; both are staged transposed, units of 8 rows, for dw = x^T dz, whose sums
@@ -79,7 +79,8 @@ __device__ __forceinline__ float one_dz(const LayerGrad &q, int64_t row, int n)
     return HAS_Z ? g * activate_slope<T>((float)static_cast<const T *>(q.z)[row * q.z_stride + n], q.act) : g;
 }
 
-template <typename T, bool HAS_Z>
+// DW: dw is asked for; else nothing of x is read.
+template <typename T, bool HAS_Z, bool DW>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad(RowOrder o, LayerGrad q, ChunkRows R,
                                                                                float *slots)
 {
@@ -149,6 +150,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
     Raw l[8], lz[HAS_Z ? 8 : 1];
     unsigned in = 0;  // bit u: row u of the block exists
     auto fetch = [&](int s) {
+        if (!DW && !of_z) return;
         const T *const from = static_cast<const T *>(of_z ? q.dy : q.x) + start;
         in = 0;
 #pragma unroll
@@ -163,6 +165,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
     };
     float column[kCW] = {0.f, 0.f, 0.f, 0.f};
     auto stage = [&]() {
+        if (!DW && !of_z) return;
         const int sub = kg / KG, g = kg % KG;
         float4_t f[8];
 #pragma unroll
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
             fetch(s + 1);
             if (q.dx) product_dx(s);
 #pragma unroll
-            for (int i = 0; i < SUB; ++i)
+            for (int i = 0; i < (DW ? SUB : 0); ++i)
                 if constexpr (Q > 1) {
                     step_products<T, kWidth, kWidth, 1, 1>(dw, s_zt[i][0], s_xt[i][0], 32 * wc, 32 * wr, i % 2 ? -1.f : 1.f);
                 } else {
@@ -268,7 +271,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
         }
     }
     const bool whole = t.end - t.start <= R.rows;
-    const int64_t cells = (int64_t)q.K * q.N, slot_cells = cells + (q.dbias ? q.N : 0);
+    const int64_t of_w = (int64_t)q.K * q.N, cells = DW ? of_w : 0, slot_cells = cells + (q.dbias ? q.N : 0);
     const int64_t slot = 2 * (int64_t)R.of((int)t.start) + R.of((int)(t.p0 - t.start));
     T *const out = static_cast<T *>(q.dw) + t.g * cells;
     float *const part = slots + (whole ? 0 : slot * slot_cells);
@@ -288,7 +291,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
         }
     }
     const int i = lane_of_full<float>(32 * wr + (lane & 31));
-    if (i < q.K)
+    if (DW && i < q.K)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int col = vec_col_full<float>(32 * wc, v, half);
@@ -298,11 +301,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
             else store_four<false>(part + at, x, q.N - col);
         }
     if (Q == 1 && P == 1) return;
-    probe(odd, dw[0][0]);
+    if (DW) probe(odd, dw[0][0]);
     if (!__syncthreads_or(odd != odd)) return;
     // the results that are not finite, in plain fp32
     stores_done();
-    const T *const wg = static_cast<const T *>(q.w) + (int64_t)t.g * cells;
+    const T *const wg = static_cast<const T *>(q.w) + (int64_t)t.g * of_w;
     if (q.dx)
         for (int64_t e = tid; e < (t.p1 - t.p0) * q.K; e += kThreads) {
             const int row = row_at(o, t.p0 + e / q.K), k = (int)(e % q.K);
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
             if (q.dx_f32) *wide = sum;
             else *to = (T)sum;
         }
-    for (int e = tid; e < q.K * q.N; e += kThreads) {
+    for (int e = tid; e < (int)cells; e += kThreads) {
         if (__builtin_isfinite(whole ? stored(out + e) : stored(part + e))) continue;
         const int k = e / q.N, n = e % q.N;
         float sum = 0.f;
@@ -353,11 +356,12 @@ template <typename T> hipError_t launch(const RowOrder &o, const LayerGrad &q, f
 {
     const int rows = chunk_rows(sizeof(T), o.n, o.G, q.K, q.N);
     const TileGrid grid = tile_grid(o.n / rows + o.G + 1);
-    auto *kernel = q.act == CGTP_ACT_NONE ? k_layer_grad<T, false> : k_layer_grad<T, true>;
+    auto *kernel = q.act == CGTP_ACT_NONE ? (q.dw ? k_layer_grad<T, false, true> : k_layer_grad<T, false, false>)
+                                          : (q.dw ? k_layer_grad<T, true, true> : k_layer_grad<T, true, false>);
     hipLaunchKernelGGL(kernel, dim3(grid.x, 1, grid.z), dim3(kThreads), 0, s, o, q, ChunkRows(rows), slots);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || o.n <= rows) return e;
-    return launch_row_join(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, rows, q.K, q.N, slots, q.dw, q.dbias, s);
+    if (e != hipSuccess || o.n <= rows || (!q.dw && !q.dbias)) return e;
+    return launch_row_join(sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32, o, rows, q.dw ? q.K : 0, q.N, slots, q.dw, q.dbias, s);
 }
 
 }  // namespace

@@ -642,7 +642,7 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
         m.out_stride = dx_stride;
         return cgtp::launch_mix_rows(dtype, m, true, s);
     };
-    if (dw && cgtp::layer_grad_takes(dtype, n_rows, n_groups, n_in, n_out)) {
+    if (cgtp::layer_grad_takes(dtype, n_rows, n_groups, n_in, n_out)) {
         cgtp::LayerGrad q{};
         q.x = x;
         q.x_stride = x_stride;

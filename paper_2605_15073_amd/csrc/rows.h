@@ -112,7 +112,8 @@ size_t narrow_bytes(int dtype, int64_t n_rows, int N);
 hipError_t launch_layer_dz(int dtype, int64_t n, int N, int act, const void *dy, int64_t dy_stride, const void *z,
                            int64_t z_stride, void *dz, hipStream_t s);
 
-// Both products of a narrow layer's gradient in one pass (layer_grad.hip), dw always, dx and dbias where not NULL.
+// Both products of a narrow layer's gradient in one pass (layer_grad.hip): dx, dw and dbias where not NULL; x for dw
+// alone, w for dx alone.
 struct LayerGrad {
     const void *x;
     int64_t x_stride;
