@@ -524,7 +524,8 @@ int cgtp_grouped_layer(int dtype, int64_t n_rows, int n_groups, int n_in, int n_
                        void *z, int64_t z_stride, void *stream);
 
 /* Its gradients, from dy [n_rows][n_out] and the z of the forward call (that of the residual is dy itself). With
- * dz_i = dy_i act'(z_i), for CGTP_BF16 rounded to bf16 as the products' operand:
+ * dz_i = dy_i act'(z_i), formed in fp32, for CGTP_BF16 held in two bf16 parts as the products' operand (16 bits of
+ * significand, where there is an activation):
  *   dx_t     = sum over the rows i of t of w[g(i)] dz_i  [n_rows / per_row][n_in], summed in fp32;
  *   dw[g]    = sum over the rows of g of x_t dz_i^T      [n_groups][n_in][n_out];
  *   dbias[g] = sum over the rows of g of dz_i            [n_groups][n_out].

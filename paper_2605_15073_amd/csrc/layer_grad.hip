@@ -36,12 +36,6 @@ __device__ __forceinline__ float4_t unpack(uint2_t v)
                     __builtin_bit_cast(float, v[1] << 16), __builtin_bit_cast(float, v[1] & 0xffff0000u)};
 }
 
-__device__ __forceinline__ unsigned pack(float a, float b)
-{
-    const bf2_t h = {(bf16_t)a, (bf16_t)b};
-    return __builtin_bit_cast(unsigned, h);
-}
-
 // The transposed units of a block in fp32, of columns j: P parts of eight rows; fp32's of 2^16 times sign.
 template <typename T, int P>
 __device__ __forceinline__ void parts_of(const float4_t (&in)[8], uint4_t (&u)[kCW][P], float sign)
@@ -61,12 +55,12 @@ __device__ __forceinline__ void parts_of(const float4_t (&in)[8], uint4_t (&u)[k
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float a = in[2 * k][j], b = in[2 * k + 1][j];
-                u[j][0][k] = pack(a, b);
                 if constexpr (P > 1) {
-                    const float ra = a - __builtin_bit_cast(float, u[j][0][k] << 16);
-                    const float rb = b - __builtin_bit_cast(float, u[j][0][k] & 0xffff0000u);
-                    u[j][1][k] = pack(__builtin_isfinite(a) ? ra : 0.f, __builtin_isfinite(b) ? rb : 0.f);
-                }
+                    unsigned high, low;
+                    split_pair(a, b, high, low);
+                    u[j][0][k] = high;
+                    u[j][1][k] = low;
+                } else u[j][0][k] = pack_pair(a, b);
             }
     }
 }

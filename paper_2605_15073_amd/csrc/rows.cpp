@@ -439,7 +439,16 @@ int check_activation(int activation)
     return CGTP_OK;
 }
 
-// dz where there is an activation, the row gradients in fp32 where rows share their input, and sums of the weight
+// Whether dz is formed in a pass of its own, 4 bytes a value: fp32, or two bf16 parts. In bf16 the products form it themselves
+// where each of them does so once, up to 128 inputs: they read dy and z in place of the parts. Us of all gradients with the
+// pass and without, silu: 261,764 rows, 128 -> 448, 492 and 428, 525,308, 64 -> 128, 247 and 168, 262,144, 128 -> 128, 155 and
+// 133; 100,000, 136 -> 64, 66 and 77, 192 -> 192 126 and 139, 60,000, 1344 -> 448, 503 and 759.
+bool dz_apart(int dtype, int n_in, int activation)
+{
+    return activation != CGTP_ACT_NONE && (dtype == CGTP_F32 || n_in > 128);
+}
+
+// dz where it has a pass of its own, the row gradients in fp32 where rows share their input, and sums of the weight
 // gradients.
 struct LayerGradBytes {
     size_t dz, rows, sums;
@@ -454,7 +463,7 @@ LayerGradBytes layer_grad_bytes(int dtype, int64_t n, int G, int n_in, int n_out
                               ? cgtp::layer_grad_slots(dtype, n, G, n_in, n_out) : 0};
     size_t sums = of[0];
     for (const size_t b : of) sums = b > sums ? b : sums;
-    return {activation == CGTP_ACT_NONE ? 0 : align256((size_t)n * n_out * elem(dtype)),
+    return {dz_apart(dtype, n_in, activation) ? align256((size_t)n * n_out * 4) : 0,
             per_row == 1 ? 0 : align256((size_t)n * n_in * 4), sums};
 }
 
@@ -665,13 +674,23 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
         if (dx && per_row > 1) e = add_shared();
         return e == hipSuccess ? CGTP_OK : hip_fail(e, "row gradient's sum");
     }
-    const void *b = dy;
-    int64_t b_stride = dy_stride;
-    if (activation != CGTP_ACT_NONE && n_rows > 0) {
+    // dz, one of the products' operands: dy itself, in a pass of its own, or in bf16 from dy and z within the products
+    const void *b = dy, *slope_z = nullptr;
+    int64_t b_stride = dy_stride, slope_stride = 0;
+    int act = activation;
+    if (need.dz > 0 && n_rows > 0) {
         e = cgtp::launch_layer_dz(dtype, n_rows, n_out, activation, dy, dy_stride, z, z_stride, dz, s);
         if (e != hipSuccess) return hip_fail(e, "activation's gradient");
         b = dz;
         b_stride = n_out;
+        if (dtype == CGTP_BF16) {
+            slope_z = dz + (size_t)n_out * es;
+            b_stride = slope_stride = 2 * (int64_t)n_out;
+            act = cgtp::kDzHeld;
+        }
+    } else if (activation != CGTP_ACT_NONE) {
+        slope_z = z;
+        slope_stride = z_stride;
     }
     if (dx && n_rows > 0) {
         cgtp::RowProduct p{};
@@ -686,6 +705,9 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
         p.out_stride = per_row > 1 ? n_in : dx_stride;
         p.out_f32 = per_row > 1 && dtype == CGTP_BF16;
         p.split_k = true;
+        p.act = act;
+        p.slope_z = slope_z;
+        p.slope_stride = slope_stride;
         e = cgtp::launch_row_product(dtype, o, p, s);
         if (e != hipSuccess) return hip_fail(e, "row gradient");
         if (per_row > 1) {
@@ -704,6 +726,9 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
         q.out = dw;
         q.per = dw ? per_row : 1;
         q.sums = dbias;
+        q.act = act;
+        q.slope_z = slope_z;
+        q.slope_stride = slope_stride;
         e = cgtp::launch_row_outer(dtype, o, q, sums, s);
         if (e != hipSuccess) return hip_fail(e, "weight gradient");
     }

@@ -56,7 +56,12 @@ struct RowProduct {
     int64_t xcd_tiles; // 0, or tiles of an XCD, which follow each other there (rows_index.h)
     bool split_k;      // sums may be split over k (rows_thin.hip); layers' may
     bool out_f32;      // row gradients of rows that share their input: out is fp32 whatever the type
+    // row gradients of layers in bf16: row i of the input is in_i act'(slope_z_i), or in_i + slope_z_i where act is
+    // kDzHeld, or in_i where NULL
+    const void *slope_z;
+    int64_t slope_stride;
 };
+constexpr int kDzHeld = -1;
 hipError_t launch_row_product(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s);
 // The form for short inputs and wide outputs (rows_wide.hip), and whether it covers a product.
 bool row_wide_takes(int dtype, const RowProduct &p);
@@ -96,6 +101,11 @@ struct RowOuter {
     void *out;
     int per;     // row i of the order is row i / per of a; 0: row i
     void *sums;  // if not NULL: the sum over the rows of group g of b_i, [G][B], beside out
+    // weight gradients of layers in bf16: row i of b is b_i act'(slope_z_i), or b_i + slope_z_i where act is kDzHeld, or
+    // b_i where NULL
+    const void *slope_z;
+    int64_t slope_stride;
+    int act;
 };
 size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B, bool sums = false);
 hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &p, void *ws,
@@ -108,7 +118,7 @@ hipError_t launch_row_few(const RowOrder &o, const RowProduct &p, hipStream_t s)
 hipError_t launch_row_outer_few(int dtype, const RowOrder &o, const RowOuter &q, hipStream_t s);
 size_t narrow_bytes(int dtype, int64_t n_rows, int N);
 
-// dz_i = dy_i act'(z_i), rows of N values at a stride of N.
+// dz_i = dy_i act'(z_i), rows of N fp32 values at a stride of N, or in bf16 two parts of N values, one behind the other.
 hipError_t launch_layer_dz(int dtype, int64_t n, int N, int act, const void *dy, int64_t dy_stride, const void *z,
                            int64_t z_stride, void *dz, hipStream_t s);
 

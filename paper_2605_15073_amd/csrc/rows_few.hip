@@ -212,7 +212,8 @@ constexpr int kOuterRows = 16;   // rows in LDS at once
 // Measured as this form came in, with it and with the tiled one for all: 10,007 rows in 4,005 groups,
 // 37 x 129 fp32, the whole gradient call 73 and 119 us; 1,000 rows in 500 groups, 256 x 256 63 and 78 us;
 // 4,000 rows 138 and 134. The kernel alone takes 38 us of the first (2.2 TB/s, 76 MB of it written).
-// LAYER: rows of a are shared (per), and b's columns are summed beside the products (sums).
+// LAYER: rows of a are shared (per), b's columns are summed beside the products (sums), and its rows may be formed as
+// b act'(slope_z).
 template <typename T, int COLS, bool NARROW, bool LAYER>
 __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter q)
 {
@@ -251,6 +252,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer_few(RowOrder o, RowOuter
                 if (row >= 0 && b < B)
                     f[u] = NARROW ? narrow_at<T>(q.h, p0 + r0 + u, W, b)
                                   : (float)static_cast<const T *>(q.b)[row * q.b_stride + b];
+                if (LAYER && q.slope_z && row >= 0 && b < B)
+                    f[u] = dz_value(f[u], (float)static_cast<const T *>(q.slope_z)[row * q.slope_stride + b], q.act);
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {

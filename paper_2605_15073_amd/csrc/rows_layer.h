@@ -10,8 +10,10 @@ namespace cgtp {
 namespace rows {
 
 // What a launch does beside the product: nothing, a layer's bias, activation and residual, or rows of sums in fp32; kGrad:
-// nothing, for a layer's row gradient.
-enum Extra { kBare, kLayer, kSums, kGrad };
+// nothing, for a layer's row gradient. Z: that forms its rows dz = dy act'(z) in bf16 from both.
+enum Extra { kBare, kLayer, kSums, kGrad, kSumsZ, kGradZ };
+template <Extra EX> constexpr bool kForms = EX == kSumsZ || EX == kGradZ;
+template <Extra EX> constexpr int kRowParts = kForms<EX> ? 2 : 1;  // bf16 operands that a row of the input is
 
 // silu: z s(z), s the logistic function; gelu: z P(z), P the normal distribution function; relu: max(z, 0).
 // An infinite z gives what the formula's products do: -inf s(-inf) is NaN.
@@ -72,6 +74,63 @@ template <typename T> __device__ __forceinline__ float activate_slope(float z, i
     if (act == CGTP_ACT_GELU) return normal_cdf<T>(z) + z * 0.39894228f * bell(z);
     if (act == CGTP_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
     return 1.f;
+}
+
+// dz = dy act'(z) of bf16 rows is an operand of two products. It is held in two bf16 parts, 16 bits of significand: off by
+// 2^-17, a five-hundredth of what the rounding of the results may be. In one, gradients were 2.4e-3 off (relative norm)
+// where that rounding alone gives 1.7e-3. The products form it where they load dy and z, or load the parts (kDzHeld).
+// One that is not finite makes results that are not, which are formed again.
+__device__ __forceinline__ unsigned pack_pair(float a, float b)
+{
+    const bf2_t h = {(bf16_t)a, (bf16_t)b};
+    return __builtin_bit_cast(unsigned, h);
+}
+__device__ __forceinline__ void split_pair(float a, float b, unsigned &high, unsigned &low)
+{
+    high = pack_pair(a, b);
+    const float ra = a - __builtin_bit_cast(float, high << 16), rb = b - __builtin_bit_cast(float, high & 0xffff0000u);
+    low = pack_pair(ra, rb);
+}
+
+// Calls f with the activation, or kDzHeld, as a constant.
+template <typename F> __device__ __forceinline__ void with_act(int act, F f)
+{
+    if (act == CGTP_ACT_SILU) f(std::integral_constant<int, CGTP_ACT_SILU>());
+    else if (act == CGTP_ACT_GELU) f(std::integral_constant<int, CGTP_ACT_GELU>());
+    else if (act == CGTP_ACT_RELU) f(std::integral_constant<int, CGTP_ACT_RELU>());
+    else f(std::integral_constant<int, kDzHeld>());
+}
+
+// The parts of two values of dz, from a pair of dy and of z.
+template <int ACT> __device__ __forceinline__ void dz_pair(unsigned dy, unsigned z, unsigned &high, unsigned &low)
+{
+    if constexpr (ACT == kDzHeld) {
+        high = dy;
+        low = z;
+    } else {
+        const float a = __builtin_bit_cast(float, dy << 16) * activate_slope<bf16_t>(__builtin_bit_cast(float, z << 16), ACT);
+        const float b = __builtin_bit_cast(float, dy & 0xffff0000u) *
+                        activate_slope<bf16_t>(__builtin_bit_cast(float, z & 0xffff0000u), ACT);
+        split_pair(a, b, high, low);
+    }
+}
+
+// The parts of eight.
+template <int ACT> __device__ __forceinline__ void dz_parts(uint4_t dy, uint4_t z, uint4_t (&part)[2])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        unsigned high, low;
+        dz_pair<ACT>(dy[k], z[k], high, low);
+        part[0][k] = high;
+        part[1][k] = low;
+    }
+}
+
+// One value of it.
+__device__ __forceinline__ float dz_value(float dy, float z, int act)
+{
+    return act == kDzHeld ? (__builtin_isfinite(dy) ? dy + z : dy) : dy * activate_slope<bf16_t>(z, act);
 }
 
 // All sums of a lane in place. MARK: NaN where z is not finite.
@@ -214,6 +273,27 @@ __device__ __forceinline__ void store_bare(const RowProduct &p, const int *row, 
         if (p.out_f32)
             store_four<false>(static_cast<float *>(p.out) + r * p.out_stride + col, float4_t{0.f, 0.f, 0.f, 0.f}, p.N - col);
         else store_layer<T, false>(p, 0, false, r, col, float4_t{0.f, 0.f, 0.f, 0.f});
+    }
+}
+
+// The same of row gradients whose rows are formed in parts: an infinite weight times a part of the other sign, or times
+// none, is NaN.
+template <typename Out> __device__ void grad_plain_sums(const RowProduct &p, int group, int rows, const int *s_row, int c0, int c1)
+{
+    stores_done();
+    const int width = c1 - c0;
+    const bf16_t *const w = static_cast<const bf16_t *>(p.w) + (int64_t)group * p.w_group;
+    for (int i = threadIdx.x; i < rows * width; i += kThreads) {
+        const int64_t row = s_row[i / width];
+        const int c = c0 + i % width;
+        if (row < 0) continue;
+        Out *const out = static_cast<Out *>(p.out) + row * p.out_stride + c;
+        if (__builtin_isfinite(stored(out))) continue;
+        const bf16_t *const dy = static_cast<const bf16_t *>(p.in) + row * p.in_stride;
+        const bf16_t *const z = static_cast<const bf16_t *>(p.slope_z) + row * p.slope_stride;
+        float x = 0.f;
+        for (int k = 0; k < p.K && x == x; ++k) x = fmaf(dz_value((float)dy[k], (float)z[k], p.act), (float)w[(int64_t)c * p.K + k], x);  // NaN stays
+        *out = (Out)x;
     }
 }
 

@@ -185,11 +185,12 @@ __global__ __launch_bounds__(kThreads) void k_mix_rows_grad(RowMixGrad p)
     }
 }
 
+// dz = dy act'(z); of bf16 the two parts of rows_layer.h, one behind the other: an infinity or NaN has one.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_layer_dz(int64_t n, int N, int act, const T *dy, int64_t dy_stride,
                                                        const T *z, int64_t z_stride, T *dz, int rows)
 {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, P = sizeof(T) == 2 ? 2 : 1;
     const int nv = (N + V - 1) / V;
     const int64_t t0 = tile_at(blockIdx.x, blockIdx.z, gridDim.x) * rows;
     if (t0 >= n) return;
@@ -201,7 +202,16 @@ __global__ __launch_bounds__(kThreads) void k_layer_dz(int64_t n, int N, int act
         float out[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) out[e] = g.v[e] * activate_slope<T>(a.v[e], act);
-        store_values(dz + t * N + c, out, left);
+        T *const to = dz + t * N * P + c;
+        store_values(to, out, left);
+        if constexpr (P == 2) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float high = (float)(T)out[e];
+                out[e] = __builtin_isfinite(high) ? out[e] - high : 0.f;
+            }
+            store_values(to + N, out, left);
+        }
     }
 }
 

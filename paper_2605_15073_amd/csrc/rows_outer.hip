@@ -15,7 +15,7 @@
 // more. Bound by the latency of the loads of a step, of which three workgroups on a compute unit hide a part. dA of
 // 131,327 rows, 128 x 16 bf16, with the narrow product 78 us.
 #include "internal.h"
-#include "rows_tile.h"
+#include "rows_layer.h"
 
 #include <cmath>
 
@@ -44,15 +44,23 @@ __device__ __forceinline__ void add_columns(float (&sum)[4], const uint4_t (&in)
         for (int e = 0; e < 4; ++e) sum[e] += __builtin_bit_cast(float, (unsigned)in[r][e]);
 }
 
-// LAYER: rows of a are shared (per), and the columns of b are summed beside the products (sums).
-template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW, bool LAYER>
-__global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, ChunkRows R, bool big,
+enum Dz { kNoDz, kFormDz, kHeldDz };
+
+// LAYER: rows of a are shared (per), and the columns of b are summed beside the products (sums). b's rows may be layers' dz
+// in two bf16 parts (rows_layer.h), which meet the same a: kHeldDz, as they lie, like a narrow product's; kFormDz, from dy
+// and z as they are loaded. That takes registers for both and for their parts, so that there all waves stage both
+// operands, 8 bytes of eight rows a thread, a row's slopes at a time.
+template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW, bool LAYER, Dz DZ_>
+__global__ __launch_bounds__(kThreads, DZ_ != kNoDz ? 3 : 1) void k_row_outer(RowOrder o, RowOuter q, ChunkRows R, bool big,
                                                         float *slots)
 {
-    constexpr int KG = kGroups<T>, BK = kStep<T>, P = NARROW ? kNarrow<T> : 1, Q = kSplit<T>, CW = kFull<T>;
+    constexpr bool DZ = DZ_ == kFormDz, HELD = DZ_ == kHeldDz;
+    constexpr int KG = kGroups<T>, BK = kStep<T>, P = NARROW ? kNarrow<T> : DZ || HELD ? 2 : 1, Q = kSplit<T>, CW = DZ ? 4 : kFull<T>;
     constexpr int WC = 4 / WR, TR = BM / WR / 32, TC = BN / WC / 32;
+    static_assert(DZ_ == kNoDz || (LAYER && !NARROW && sizeof(T) == 2), "dz in parts: layers in bf16");
+    typedef typename std::conditional<DZ, float, T>::type Places;  // of loads of CW lanes: fp32's for four
     __shared__ uint4_t s_cols[P][kTile<T, BN>], s_rows[kTile<T, BM>];
-    __shared__ int64_t s_at[2][2][BK];  // where the rows of a and b of a step start
+    __shared__ int64_t s_at[DZ ? 3 : 2][2][BK];  // where the rows of a, b and slope_z of a step start
     __shared__ unsigned s_rows_in[2][BK / 32];  // bit per row of a step: it exists
 
     // Block b runs on XCD b % 8: the tiles of a chunk, which share its rows, follow each other on one.
@@ -71,8 +79,8 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 
     // waves 0 and 1 stage a, waves 2 and 3 b: lanes first .. first + CW - 1 of k-group kg, of b of one of its parts.
     // b's parts are spread over the threads (narrow tiles leave most without work in one part alone).
-    constexpr int kHalf = kThreads / 2, kPart = KG * (BN / CW), NL = (P * kPart + kHalf - 1) / kHalf;
-    static_assert(KG * (BM / CW) <= kHalf, "a: one task a thread");
+    constexpr int kHalf = kThreads / 2, kPart = KG * (BN / CW), NL = DZ ? 1 : (P * kPart + kHalf - 1) / kHalf;
+    static_assert(KG * (BM / CW) <= (DZ ? kThreads : kHalf) && (!DZ || kPart <= kThreads), "a, and b of DZ: one task a thread");
     const bool of_b = wave >= 2;
     const int width = !of_b ? q.A : NARROW ? W : B;
     struct Task {
@@ -91,8 +99,17 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
         const int col = (of_b ? b0 : a0) + k.first;
         k.early = WIDE && col < width && col + CW > width ? col + CW - width : 0;
         k.from = static_cast<const T *>(!of_b ? q.a : NARROW ? q.h : q.b) +
-                 ((k.has ? k.part : 0) * (NARROW ? W : 0) + (WIDE && col + CW > width ? width - CW : col));
+                 ((k.has ? k.part : 0) * (NARROW ? W : HELD ? B : 0) + (WIDE && col + CW > width ? width - CW : col));
     }
+    // DZ: a task of a for the first threads, one of b for the last, without a branch inside a wave
+    const int task_a = tid, task_b = tid - (kThreads - kPart);
+    const bool has_a = DZ && task_a < KG * (BM / CW), has_b = DZ && task_b >= 0;
+    const int kg_a = task_a / (BM / CW) % KG, first_a = CW * (task_a % (BM / CW));
+    const int kg_b = has_b ? task_b / (BN / CW) : 0, first_b = has_b ? CW * (task_b % (BN / CW)) : 0;
+    auto start4 = [&](int col, int width) { return WIDE && col + CW > width ? width - CW : col; };
+    auto early4 = [&](int col, int width) { return WIDE && col < width && col + CW > width ? col + CW - width : 0; };
+    uint2_t la[DZ ? 8 : 1], lb[DZ ? 8 : 1], lz[DZ ? 8 : 1];
+    unsigned in_a = 0, in_b = 0;
     uint4_t l[NL][8];
     unsigned in[NL];  // bit u: row u of the k-group exists
     float sign = 1.f;  // of the step's a
@@ -112,11 +129,32 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             const int of_a = LAYER && q.per > 1 ? (int)((unsigned)row / (unsigned)q.per) : row;
             s_at[0][s & 1][tid] = in ? of_a * q.a_stride : 0;  // row 0 in place of none: zeroed when staged
             s_at[1][s & 1][tid] = !in ? 0 : NARROW ? pos * (P * W) : row * q.b_stride;
+            if constexpr (DZ) s_at[2][s & 1][tid] = in ? row * q.slope_stride : 0;
             const unsigned long long m = __ballot(in);
             if (tid % 32 == 0) s_rows_in[s & 1][tid / 32] = (unsigned)(m >> (tid & 32));
         }
     };
+    auto load4 = [&](uint2_t (&to)[DZ ? 8 : 1], const void *from, const int64_t *at, int col, int width) __attribute__((always_inline)) {
+        const T *const p = static_cast<const T *>(from) + start4(col, width);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (WIDE) to[u] = *reinterpret_cast<const uint2_any *>(p + at[u]);
+            else to[u] = load_8<T, false>(p + at[u], width - col);
+        }
+    };
     auto fetch = [&](int s) {
+        if constexpr (DZ) {
+            if (has_a) {
+                in_a = s_rows_in[s & 1][kg_a / 4] >> 8 * (kg_a % 4) & 0xffu;
+                load4(la, q.a, s_at[0][s & 1] + kg_a * kU, a0 + first_a, q.A);
+            }
+            if (has_b) {
+                in_b = s_rows_in[s & 1][kg_b / 4] >> 8 * (kg_b % 4) & 0xffu;
+                load4(lb, q.b, s_at[1][s & 1] + kg_b * kU, b0 + first_b, B);
+                load4(lz, q.slope_z, s_at[2][s & 1] + kg_b * kU, b0 + first_b, B);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const Task &k = tasks[i];
@@ -130,11 +168,77 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             }
         }
     };
-    const bool sums = LAYER && q.sums && of_b && a0 == 0;
+    const bool sums = LAYER && q.sums && (DZ || of_b) && a0 == 0;
     float column[LAYER ? CW : 1];
 #pragma unroll
     for (int j = 0; j < (LAYER ? CW : 1); ++j) column[j] = 0.f;
     auto stage = [&]() {
+        if constexpr (DZ) {
+            uint4_t u[CW][Q];
+            if (has_a) {
+                const int early = early4(a0 + first_a, q.A);
+                if (early > 0) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) settle<T>(la[r], early);
+                }
+                if (in_a != 0xffu) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) la[r] = in_a >> r & 1 ? la[r] : uint2_t{0, 0};
+                }
+                to_units(la, u);
+#pragma unroll
+                for (int j = 0; j < CW; ++j) put<T, BM>(s_rows, KG, kg_a, place_full<Places>(first_a + j), u[j]);
+            }
+            if (has_b) {
+                const int early = early4(b0 + first_b, B);
+                if (early > 0) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        settle<T>(lb[r], early);
+                        settle<T>(lz[r], early);
+                    }
+                }
+                if (in_b != 0xffu) {  // 0 act'(0)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        lb[r] = in_b >> r & 1 ? lb[r] : uint2_t{0, 0};
+                        lz[r] = in_b >> r & 1 ? lz[r] : uint2_t{0, 0};
+                    }
+                }
+                // the parts in place of what they are formed from, a row at a time: its registers are free for the next
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    with_act(q.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            unsigned high, low;
+                            dz_pair<decltype(act)::value>(lb[r][k], lz[r][k], high, low);
+                            lb[r][k] = high;
+                            lz[r][k] = low;
+                        }
+                    });
+                if (sums) {  // of the parts; an infinity or NaN is the first alone
+                    auto add = [&](float &sum, unsigned high, unsigned low) {
+                        const float h = __builtin_bit_cast(float, high);
+                        sum += __builtin_isfinite(h) ? h + __builtin_bit_cast(float, low) : h;
+                    };
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            add(column[2 * k], lb[r][k] << 16, lz[r][k] << 16);
+                            add(column[2 * k + 1], lb[r][k] & 0xffff0000u, lz[r][k] & 0xffff0000u);
+                        }
+                }
+                to_units(lb, u);
+#pragma unroll
+                for (int j = 0; j < CW; ++j) put<T, BN>(s_cols[0], KG, kg_b, place_full<Places>(first_b + j), u[j]);
+                to_units(lz, u);
+#pragma unroll
+                for (int j = 0; j < CW; ++j) put<T, BN>(s_cols[P - 1], KG, kg_b, place_full<Places>(first_b + j), u[j]);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const Task &k = tasks[i];
@@ -147,10 +251,10 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
 #pragma unroll
                 for (int r = 0; r < 8; ++r) l[i][r] = in[i] >> r & 1 ? l[i][r] : uint4_t{0, 0, 0, 0};
             }
-            if constexpr (LAYER)
+            if constexpr (LAYER && !DZ)
                 if (sums) add_columns(column, l[i], T());
             uint4_t u[CW][Q];
-            to_units(l[i], u, of_b ? 1.f : sign);
+            if constexpr (!DZ) to_units(l[i], u, of_b ? 1.f : sign);  // DZ is staged above
 #pragma unroll
             for (int j = 0; j < CW; ++j) {
                 if (of_b) put<T, BN>(s_cols[k.part], KG, k.kg, place_full<T>(k.first + j), u[j]);
@@ -191,18 +295,20 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     T *const out = static_cast<T *>(q.out) + t.g * cells;
     float *const part = slots + (whole ? 0 : slot * slot_cells);
     if constexpr (LAYER) {
-        static_assert(NL == 1, "one task a thread");
+        // parts of b that threads of their own load, each with sums of its own
+        constexpr int SP = NL == 1 ? P : 1, sp = DZ ? 1 : SP;
+        static_assert(NL <= 2 && sizeof(s_rows) >= sizeof(float) * sp * KG * BN, "one task a thread, or both parts of it");
         if (q.sums && a0 == 0) {
-            float *const of_kg = reinterpret_cast<float *>(s_rows);  // [KG][BN]
+            float *const of_kg = reinterpret_cast<float *>(s_rows);  // [sp][KG][BN]
             __syncthreads();
-            if (of_b && tasks[0].has)
+            if (DZ ? has_b : of_b && tasks[0].has)
 #pragma unroll
-                for (int j = 0; j < CW; ++j) of_kg[tasks[0].kg * BN + tasks[0].first + j] = column[j];
+                for (int j = 0; j < CW; ++j) of_kg[DZ ? kg_b * BN + first_b + j : (tasks[0].part * KG + tasks[0].kg) * BN + tasks[0].first + j] = column[j];
             __syncthreads();
             if (tid < BN && b0 + tid < B) {
                 float sum = 0.f;
 #pragma unroll
-                for (int g = 0; g < KG; ++g) sum += of_kg[g * BN + tid];
+                for (int g = 0; g < sp * KG; ++g) sum += of_kg[g * BN + tid];
                 if (whole) static_cast<T *>(q.sums)[(int64_t)t.g * B + b0 + tid] = (T)sum;
                 else part[cells + b0 + tid] = sum;
             }
@@ -211,13 +317,13 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
     if (LAYER && !q.out) return;  // the sums alone
 #pragma unroll
     for (int r = 0; r < TR; ++r) {
-        const int i = a0 + lane_of_full<T>(r0 + 32 * r + (lane & 31));
+        const int i = a0 + lane_of_full<Places>(r0 + 32 * r + (lane & 31));
         if (i >= q.A) continue;
 #pragma unroll
         for (int c = 0; c < TC; ++c)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const int col = b0 + vec_col_full<T>(c0w + 32 * c, v, half);
+                const int col = b0 + vec_col_full<Places>(c0w + 32 * c, v, half);
                 const float4_t x = {acc[c][r][v], acc[c][r][4 + v], acc[c][r][8 + v], acc[c][r][12 + v]};
                 if (q.transposed) {
 #pragma unroll
@@ -234,7 +340,7 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
                 }
             }
     }
-    if constexpr (Q > 1 || NARROW) {
+    if constexpr (Q > 1 || NARROW || DZ_ != kNoDz) {
         float odd = 0.f;
 #pragma unroll
         for (int c = 0; c < TC; ++c)
@@ -251,8 +357,11 @@ __global__ __launch_bounds__(kThreads) void k_row_outer(RowOrder o, RowOuter q, 
             float sum = 0.f;
             auto add = [&](int64_t pos) {  // no load waits for a branch
                 const int row = row_at(o, pos), any = row < 0 ? 0 : row;
-                const float y = NARROW ? narrow_at<T>(q.h, pos, W, c)
-                                       : (float)static_cast<const T *>(q.b)[any * q.b_stride + c];
+                float y;
+                if constexpr (NARROW) y = narrow_at<T>(q.h, pos, W, c);
+                else y = (float)static_cast<const T *>(q.b)[any * q.b_stride + c];
+                if constexpr (DZ_ != kNoDz)
+                    y = dz_value(y, (float)static_cast<const T *>(q.slope_z)[any * q.slope_stride + c], q.act);
                 const int of_a = LAYER && q.per > 1 ? (int)((unsigned)any / (unsigned)q.per) : any;
                 const float x = (float)static_cast<const T *>(q.a)[of_a * q.a_stride + i];
                 sum = row < 0 ? sum : fmaf(x, y, sum);
@@ -386,10 +495,18 @@ hipError_t launch(const RowOrder &o, const RowOuter &q, const Shape &sh, bool bi
     const bool wide = q.A >= kFull<T> && (q.r > 0 || B >= kFull<T>);  // 16 bytes of a row and more
     const int64_t chunks = ((big ? o.n / kFewRows : o.n / sh.rows + o.G) + 7) / 8 * 8;
     if (chunks * sh.tiles > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    auto *kernel = wide ? k_row_outer<T, BM, BN, WR, true, false, false> : k_row_outer<T, BM, BN, WR, false, false, false>;
-    if (q.per > 0) kernel = wide ? k_row_outer<T, BM, BN, WR, true, false, true> : k_row_outer<T, BM, BN, WR, false, false, true>;
+    auto *kernel = wide ? k_row_outer<T, BM, BN, WR, true, false, false, kNoDz>
+                        : k_row_outer<T, BM, BN, WR, false, false, false, kNoDz>;
+    if (q.per > 0)
+        kernel = wide ? k_row_outer<T, BM, BN, WR, true, false, true, kNoDz> : k_row_outer<T, BM, BN, WR, false, false, true, kNoDz>;
+    if constexpr (sizeof(T) == 2 && BN <= 64)
+        if (q.slope_z)
+            kernel = q.act == kDzHeld
+                         ? (wide ? k_row_outer<T, BM, BN, WR, true, false, true, kHeldDz> : k_row_outer<T, BM, BN, WR, false, false, true, kHeldDz>)
+                         : (wide ? k_row_outer<T, BM, BN, WR, true, false, true, kFormDz> : k_row_outer<T, BM, BN, WR, false, false, true, kFormDz>);
     if constexpr (BN <= CGTP_MAX_ADAPTER_RANK)
-        if (q.r > 0) kernel = wide ? k_row_outer<T, BM, BN, WR, true, true, false> : k_row_outer<T, BM, BN, WR, false, true, false>;
+        if (q.r > 0)
+            kernel = wide ? k_row_outer<T, BM, BN, WR, true, true, false, kNoDz> : k_row_outer<T, BM, BN, WR, false, true, false, kNoDz>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks * sh.tiles)), dim3(kThreads), 0, s, o, q, ChunkRows(sh.rows), big,
                        slots);
     return hipGetLastError();
@@ -411,7 +528,14 @@ hipError_t join(const RowOrder &o, int chunk, int A, int B, const float *slots, 
 template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float *slots, hipStream_t s)
 {
     const int B = q.r > 0 ? q.r : q.B;
-    const Shape sh = shape(sizeof(T), o.n, o.G, q.A, B);
+    Shape sh = shape(sizeof(T), o.n, o.G, q.A, B);
+    // dz in parts: 64 columns, whose sums leave registers for both. Us with 128 of them and 64: formed, 261,764 rows, 128 x
+    // 448, 230 (two workgroups on a compute unit) and 229; held, 60,000 rows, 1344 x 448, 304 and 302, 20,000 of 100
+    // groups, 128 x 128, 25 and 22, 6,000 of 20, 1344 x 448, 64 and 56.
+    if (q.slope_z && sh.bn == 128) {
+        sh.bn = 64;
+        sh.tiles = (int64_t)((q.A + 127) / 128) * ((B + 63) / 64);
+    }
     const bool big = o.n <= kFewMean * (int64_t)o.G;  // the groups of few rows go their own way
     hipError_t e;
     if (big) {

@@ -62,7 +62,7 @@ __device__ __forceinline__ void store_traded(bf16_t *row, int col, int N, float4
 
 // Waves of a SIMD that bf16 registers have to leave room for: a gradient from 448 columns, 262,144 rows, 83 us with three
 // and 87 with two.
-template <Extra EX> constexpr int kLeanWaves = EX == kBare ? 1 : 3;
+template <Extra EX> constexpr int kLeanWaves = EX == kBare ? 1 : kForms<EX> ? 2 : 3;
 
 template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED, Extra EX>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void k_row_product(RowOrder o, RowProduct p, int splits)
@@ -77,7 +77,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
     constexpr int NR = BM / kLanes > 0 ? BM / kLanes : 1;
     constexpr int NC = (BX + kLanes - 1) / kLanes;
     constexpr bool kLean = EX != kBare && WIDE;  // no adapters: whole steps load and stage without a condition
-    __shared__ uint4_t s_tiles[kTile<T, BX> + kTile<T, BM>];
+    constexpr bool kDz = kForms<EX>;
+    constexpr int kParts = kRowParts<EX>;
+    static_assert(!kDz || (sizeof(T) == 2 && WNK), "dz in parts: row gradients in bf16");
+    __shared__ uint4_t s_tiles[kTile<T, BX> + kParts * kTile<T, BM>];
     uint4_t *const s_cols = s_tiles, *const s_rows = s_tiles + kTile<T, BX>;
     __shared__ int s_row[BM], s_g[BM], s_seg_g[BM], s_seg_at[BM + 1], s_nseg, s_any;
 
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
     if (!FUSED && !shared_w && t.g == o.G) {  // rows of no group
         if (p.narrow) return;
         __syncthreads();
-        if constexpr (EX == kLayer || EX == kSums) store_bare<T>(p, s_row, rows, ct0 * BN, col_end);
+        if constexpr (EX == kLayer || EX == kSums || EX == kSumsZ) store_bare<T>(p, s_row, rows, ct0 * BN, col_end);
         else store_zeros<T>(p, s_row, rows, ct0 * BN, col_end);
         return;
     }
@@ -132,11 +135,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
 
     // rows of the input, and of [N][K] weights: k-group tid % KG of lanes tid / KG + kLanes i
     const int kg = tid % KG, rr = tid / KG;
-    const T *in[NR];
+    const T *in[NR], *in_z[kDz ? NR : 1];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const int r = rr + kLanes * i, row = r < BM ? s_row[r] : -1;
         const int any = row < 0 ? s_any : row;  // never stored
+        if constexpr (kDz) in_z[i] = static_cast<const T *>(p.slope_z) + any * p.slope_stride;
         in[i] = static_cast<const T *>(p.in) +
                 (EX == kLayer && p.per > 1 ? (int)((unsigned)any / (unsigned)p.per) : any) * p.in_stride;
     }
@@ -161,7 +165,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
         }
     };
     struct {
-        Raw8<T> x[NR], wn[WNK ? NC : 1];
+        Raw8<T> x[NR], z[kDz ? NR : 1], wn[WNK ? NC : 1];
         uint2_t wt[WNK ? 1 : 8];
         int xk, wk;  // values that exist of this thread's k-group of rows and weights
         int xe, we;  // what their loads started early
@@ -194,6 +198,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
                 if (next.k == 0) to_columns(next.ct);
 #pragma unroll
                 for (int i = 0; i < NR; ++i) l.x[i] = load_any8(in[i] + next.k + kg * kU);
+                if constexpr (kDz) {
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) l.z[i] = load_any8(in_z[i] + next.k + kg * kU);
+                }
                 if constexpr (WNK) {
 #pragma unroll
                     for (int i = 0; i < NC; ++i) l.wn[i] = load_any8(col[i] + next.k);
@@ -229,6 +237,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
             const T *q = ext ? static_cast<const T *>(p.h) + (t.p0 + (r < rows ? r : 0)) * K : in[i];
             if constexpr (WIDE) l.x[i] = load_any8(q + xs);
             else l.x[i] = load_row8<T, false>(q + kx, l.xk);
+            if constexpr (kDz) {
+                if constexpr (WIDE) l.z[i] = load_any8(in_z[i] + xs);
+                else l.z[i] = load_row8<T, false>(in_z[i] + kx, l.xk);
+            }
         }
         int kw = WNK ? kx : k + tg * kU;
         const bool in_k = kw < K;
@@ -257,14 +269,38 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
         }
         if (next.ct < ct1) advance(next);
     };
+    auto stage_dz = [&]() __attribute__((always_inline)) {  // both parts of the rows
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            if (BM < kLanes && rr >= BM) break;
+            with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+                uint4_t part[2];
+                dz_parts<decltype(act)::value>(l.x[i].v[0], l.z[i].v[0], part);
+                s_rows[kg * (BM + 1) + rr + kLanes * i] = part[0];
+                s_rows[kTile<T, BM> + kg * (BM + 1) + rr + kLanes * i] = part[1];
+            });
+        }
+    };
     auto stage = [&]() {
         uint4_t u[Q];
-        if (kLean && l.whole) {
+        if constexpr (kDz) {  // past the k that exist 0 act'(0)
+            if (!(kLean && l.whole) && l.xk < kU) {
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                if (BM < kLanes && rr >= BM) break;
-                to_units(l.x[i], u, sign);
-                put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
+                for (int i = 0; i < NR; ++i) {
+                    settle(l.x[i], WIDE ? l.xe : 0, l.xk);
+                    settle(l.z[i], WIDE ? l.xe : 0, l.xk);
+                }
+            }
+            stage_dz();
+        }
+        if (kLean && l.whole) {
+            if constexpr (!kDz) {
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    if (BM < kLanes && rr >= BM) break;
+                    to_units(l.x[i], u, sign);
+                    put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
+                }
             }
             if constexpr (WNK) {
 #pragma unroll
@@ -285,12 +321,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
             }
             return;
         }
+        if constexpr (!kDz) {
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            if (BM < kLanes && rr >= BM) break;
-            if (l.xk < kU || !(l.rows >> i & 1)) settle(l.x[i], WIDE ? l.xe : 0, l.rows >> i & 1 ? l.xk : 0);
-            to_units(l.x[i], u, sign);
-            put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
+            for (int i = 0; i < NR; ++i) {
+                if (BM < kLanes && rr >= BM) break;
+                if (l.xk < kU || !(l.rows >> i & 1)) settle(l.x[i], WIDE ? l.xe : 0, l.rows >> i & 1 ? l.xk : 0);
+                to_units(l.x[i], u, sign);
+                put<T, BM>(s_rows, KG, kg, rr + kLanes * i, u);
+            }
         }
         if constexpr (WNK) {
 #pragma unroll
@@ -353,13 +391,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
             for (int r = 0; r < TR; ++r) {
                 const int row = s_row[r0 + 32 * r + (lane & 31)];
                 if (row < 0) continue;
-                if constexpr (EX == kBare || EX == kGrad) {
+                if constexpr (EX == kBare || EX == kGrad || EX == kGradZ) {
                     T *const q = static_cast<T *>(p.out) + row * p.out_stride;
 #pragma unroll
                     for (int c = 0; c < TC; ++c)
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
-                            if constexpr (EX == kGrad && sizeof(T) == 2) {
+                            if constexpr ((EX == kGrad || EX == kGradZ) && sizeof(T) == 2) {
                                 // the wave's halves trade, so that each has eight columns that follow each other
                                 if (v % 2 == 0)
                                     store_traded(q, c0 + 32 * c + 8 * (v + half), p.N, vec_val<T, !WNK>(acc[c][r], v),
@@ -425,14 +463,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
         stage();
         __syncthreads();
         fetch();
-        step_products<T, BX, BM, TX, TR>(acc, s_cols, s_rows, c0w, r0, sign);
+        step_products<T, BX, BM, TX, TR, kParts>(acc, s_cols, s_rows, c0w, r0, sign);
         sign = -sign;
         const int ct = now.ct;
         advance(now);
         if (now.ct != ct) {
             if constexpr (FUSED) narrow_step();
             store(ct);
-            if (Q > 1 || FUSED || nseg > 0)
+            if (Q > 1 || FUSED || kDz || nseg > 0)
 #pragma unroll
                 for (int c = 0; c < TC; ++c)
 #pragma unroll
@@ -445,6 +483,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kLeanWaves<EX>) void
     while (now.ct < ct1) step();
     if constexpr (EX == kLayer) {
         if (Q > 1 && __syncthreads_or(odd != odd)) layer_plain_sums<T, WNK>(p, t.g, rows, s_row, ct0 * BN, col_end);
+    } else if constexpr (kDz) {
+        if (!__syncthreads_or(odd != odd)) return;
+        if constexpr (EX == kSumsZ) grad_plain_sums<float>(p, t.g, rows, s_row, ct0 * BN, col_end);
+        else grad_plain_sums<T>(p, t.g, rows, s_row, ct0 * BN, col_end);
     } else if ((Q > 1 || FUSED || nseg > 0) && __syncthreads_or(odd != odd)) {
         float *const h = FUSED ? reinterpret_cast<float *>(s_tiles) : nullptr;
         if constexpr (FUSED) {
@@ -530,10 +572,13 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
     const int dtype = sizeof(T) == 2 ? CGTP_BF16 : CGTP_F32;
     if ((p.per > 0 || p.split_k) && !row_few_takes(dtype, o, p) && row_thin_takes(dtype, o, p)) return launch_row_thin(dtype, o, p, s);
     if constexpr (WNK && sizeof(T) == 2)
-        if (p.out_f32) return pick_extra<T, true, kSums>(o, p, s);
+        if (p.out_f32) return p.slope_z ? pick_extra<T, true, kSumsZ>(o, p, s) : pick_extra<T, true, kSums>(o, p, s);
     if constexpr (WNK)
-        if (p.split_k && !row_few_takes(dtype, o, p) && (o.n < 40 * (int64_t)o.G || !row_wide_takes(dtype, p)))
+        if (p.split_k && !row_few_takes(dtype, o, p) && (o.n < 40 * (int64_t)o.G || !row_wide_takes(dtype, p))) {
+            if constexpr (sizeof(T) == 2)
+                if (p.slope_z) return pick_extra<T, true, kGradZ>(o, p, s);
             return pick_extra<T, true, kGrad>(o, p, s);
+        }
     if constexpr (!WNK)
         if (p.per > 0) return pick_extra<T, false, kLayer>(o, p, s);
     if constexpr (WNK)

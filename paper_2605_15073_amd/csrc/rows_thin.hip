@@ -57,6 +57,8 @@ template <typename T, bool WNK, Extra EX>
 __global__ __launch_bounds__(kThreads) void k_row_thin(RowOrder o, RowProduct p)
 {
     constexpr int Q = kSplit<T>, S = kGroups<T> / 2, KS = kStep<T>, LD = kThin + 4;
+    constexpr bool kDz = kForms<EX>;
+    static_assert(!kDz || (sizeof(T) == 2 && WNK), "dz in parts: row gradients in bf16");
     __shared__ float4_t s_sum[kWaves][kThin][LD / 4];
     __shared__ int s_row[kThin];
     const Tile t = find_tile(o, TileRows<kThin>{}, tile_at(blockIdx.x, blockIdx.z, gridDim.x));
@@ -67,21 +69,23 @@ __global__ __launch_bounds__(kThreads) void k_row_thin(RowOrder o, RowProduct p)
     if (tid < kThin) s_row[tid] = tid < rows ? row_at(o, t.p0 + tid) : -1;
     __syncthreads();
     if (t.g == o.G) {
-        if (EX == kBare) store_zeros<T>(p, s_row, rows, c0, c1);
+        if (EX == kBare || EX == kGradZ) store_zeros<T>(p, s_row, rows, c0, c1);
         else store_bare<T>(p, s_row, rows, c0, c1);
         return;
     }
     const int own = s_row[n32], any = own < 0 ? 0 : own;  // row 0 in place of none: never stored
     const T *const in = static_cast<const T *>(p.in) + (EX == kLayer && p.per > 1 ? (int)((unsigned)any / (unsigned)p.per) : any) * p.in_stride;
+    const T *const in_z = kDz ? static_cast<const T *>(p.slope_z) + any * p.slope_stride : nullptr;
     const T *const w = static_cast<const T *>(p.w) + (int64_t)t.g * p.w_group;
     const int col = c0 + n32 < p.N ? c0 + n32 : p.N - 1;  // the last one's in place of none
-    struct Step { Raw8<T> x[S], w[S]; };
+    struct Step { Raw8<T> x[S], z[kDz ? S : 1], w[S]; };
     auto load = [&](int s) {
         Step l;
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             const int k = s * KS + (2 * i + half) * kU;
             l.x[i] = load_row8<T, false>(in + k, p.K - k);
+            if constexpr (kDz) l.z[i] = load_row8<T, false>(in_z + k, p.K - k);  // past the k that exist 0 act'(0)
             if constexpr (WNK) l.w[i] = load_row8<T, false>(w + (int64_t)col * p.K + k, p.K - k);
             else l.w[i] = load_column8(w, col, k, p.K, p.N);
         }
@@ -111,6 +115,16 @@ __global__ __launch_bounds__(kThreads) void k_row_thin(RowOrder o, RowProduct p)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[i] = fmaf(sign * kDown, sum[i], acc[i]);
                 sign = -sign;
+            } else if constexpr (kDz) {
+#pragma unroll
+                for (int i = 0; i < S; ++i) {
+                    uint4_t part[2];
+                    with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+                        dz_parts<decltype(act)::value>(now.x[i].v[0], now.z[i].v[0], part);
+                    });
+                    mfma(acc, now.w[i].v[0], part[1]);
+                    mfma(acc, now.w[i].v[0], part[0]);
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < S; ++i) mfma(acc, now.w[i].v[0], now.x[i].v[0]);
@@ -129,8 +143,13 @@ __global__ __launch_bounds__(kThreads) void k_row_thin(RowOrder o, RowProduct p)
 #pragma unroll
         for (int e = 0; e < 4; ++e) odd |= c + e < p.N && !__builtin_isfinite(x[e]);
         if (EX == kLayer) store_layer<T, (Q > 1)>(p, t.g, true, row, c, x);
-        else if (EX == kSums) store_four<false>(static_cast<float *>(p.out) + row * p.out_stride + c, x, p.N - c);
+        else if (EX == kSums || EX == kSumsZ) store_four<false>(static_cast<float *>(p.out) + row * p.out_stride + c, x, p.N - c);
         else store_four<false>(static_cast<T *>(p.out) + row * p.out_stride + c, x, p.N - c);
+    }
+    if constexpr (kDz) {
+        if (!__syncthreads_or(odd)) return;
+        if constexpr (EX == kSumsZ) grad_plain_sums<float>(p, t.g, rows, s_row, c0, c1);
+        else grad_plain_sums<T>(p, t.g, rows, s_row, c0, c1);
     }
     if constexpr (Q > 1) {
         if (!__syncthreads_or(odd)) return;
@@ -150,8 +169,10 @@ template <typename T, bool WNK, Extra EX> hipError_t launch(const RowOrder &o, c
 template <typename T> hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     if (p.per > 0) return launch<T, false, kLayer>(o, p, s);
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2) {
+        if (p.slope_z) return p.out_f32 ? launch<T, true, kSumsZ>(o, p, s) : launch<T, true, kGradZ>(o, p, s);
         if (p.out_f32) return launch<T, true, kSums>(o, p, s);
+    }
     return launch<T, true, kBare>(o, p, s);
 }
 

@@ -452,7 +452,9 @@ __device__ __forceinline__ void mma(float16_t &acc, const uint4_t (&a)[3], const
 // products keep it: against sums in 64 bits rounded to bf16, results are low by 1e-8 of their magnitude on the mean
 // for up to 1,344 terms and for chunks of 16,384 rows, by 1.6e-7 for 20,000 terms of one sign, and 5e-6 to 6e-4 of
 // them are another bf16 number (of fp32 sums in another order 1e-3).
-template <typename T, int BN, int BM, int TC, int TR, int TX>
+//
+// PARTS: tiles of rows, behind each other, that meet the same columns; of bf16 alone, the smallest last.
+template <typename T, int BN, int BM, int TC, int TR, int PARTS = 1, int TX>
 __device__ __forceinline__ void step_products(float16_t (&acc)[TX][TR], const uint4_t *cols,
                                               const uint4_t *rws, int c0, int r0, float sign)
 {
@@ -465,11 +467,14 @@ __device__ __forceinline__ void step_products(float16_t (&acc)[TX][TR], const ui
 #pragma unroll
             for (int c = 0; c < TC; ++c) a[c][0] = cols[(2 * s + half) * (BN + 1) + c0 + 32 * c + n];
 #pragma unroll
-            for (int r = 0; r < TR; ++r) b[r][0] = rws[(2 * s + half) * (BM + 1) + r0 + 32 * r + n];
+            for (int part = PARTS - 1; part >= 0; --part) {
 #pragma unroll
-            for (int c = 0; c < TC; ++c)
+                for (int r = 0; r < TR; ++r) b[r][0] = rws[part * kTile<T, BM> + (2 * s + half) * (BM + 1) + r0 + 32 * r + n];
 #pragma unroll
-                for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r]);
+                for (int c = 0; c < TC; ++c)
+#pragma unroll
+                    for (int r = 0; r < TR; ++r) mma(acc[c][r], a[c], b[r]);
+            }
         }
     } else {
 #pragma unroll

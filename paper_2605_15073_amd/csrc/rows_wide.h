@@ -86,7 +86,10 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     constexpr float kSign = kPlus < NP ? -1.f : 1.f;  // of the adapters' products and of the result
     constexpr float kOut = Q > 1 ? kSign * kDown : kSign;
     static_assert(NP <= kPairs<T> && !(EXT && WNK), "adapters: [K][N] weights");
-    static_assert(EX == kBare || (EX == kLayer && !EXT && !WNK), "layers: [K][N] weights, no adapters");
+    constexpr bool kDz = kForms<EX>;
+    constexpr int kParts = kDz ? 2 : Q;  // operands of a row's k
+    static_assert(EX == kBare || (EX == kLayer && !EXT && !WNK) || (EX == kGradZ && !EXT && WNK && sizeof(T) == 2),
+                  "layers: [K][N] weights, no adapters; their row gradients from dz in parts: bf16");
     typedef typename Out4<T>::t O;
     typedef typename Out4<T>::any O_any;
     __shared__ uint4_t s_w[Q * KG * LD];
@@ -155,12 +158,28 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
     const T *const in = static_cast<const T *>(p.in) +
                         (EX == kLayer && p.per > 1 ? (int)((unsigned)s_row[pl] / (unsigned)p.per) : s_row[pl]) * p.in_stride;
     const int W = EXT ? narrow_width(p.r) : 0;
-    uint4_t x[NP][Q], h[EXT ? XP : 1][Q];
+    uint4_t x[NP][kParts], h[EXT ? XP : 1][Q];
     float odd = 0.f;  // NaN once a result is not finite
+    if constexpr (kDz) {
+        const T *const in_z = static_cast<const T *>(p.slope_z) + s_row[pl] * p.slope_stride;
+        Raw8<T> dy[NP], z[NP];
 #pragma unroll
-    for (int s = 0; s < NP; ++s) {
-        const int k = (2 * s + half) * U;
-        to_units(load_row8<T, false>(in + k, p.K - k), x[s], s < kPlus ? 1.f : -1.f);
+        for (int s = 0; s < NP; ++s) {
+            const int k = (2 * s + half) * U;
+            dy[s] = load_row8<T, false>(in + k, p.K - k);
+            z[s] = load_row8<T, false>(in_z + k, p.K - k);  // past the k that exist 0 act'(0)
+        }
+#pragma unroll
+        for (int s = 0; s < NP; ++s)
+            with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+                dz_parts<decltype(act)::value>(dy[s].v[0], z[s].v[0], x[s]);
+            });
+    } else {
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+            const int k = (2 * s + half) * U;
+            to_units(load_row8<T, false>(in + k, p.K - k), x[s], s < kPlus ? 1.f : -1.f);
+        }
     }
     O *const turn = s_turn + wave * (32 * TURN / 4), *const z_turn = s_z_turn + (Z ? wave * (32 * ZTURN / 4) : 0);
     if constexpr (FUSED) {
@@ -316,15 +335,23 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
 #pragma unroll
                 for (int v = 0; v < 4; ++v) set_vec<T, !WNK>(acc[c], v, s_bias[(32 * c + vec_col<T, !WNK>(v, half)) / 4]);
         fetch(nseg > 1 || ct + 1 == ct1 ? ct : ct + 1, nseg > 1 ? 1 : 0);
-        auto product = [&](int pair, const uint4_t (&b)[Q]) {
+        auto product = [&](int pair, const uint4_t (&b)[kParts]) {
             uint4_t c0[Q], c1[Q];
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 c0[q] = a[(q * KG + 2 * pair) * LD];
                 c1[q] = a[(q * KG + 2 * pair) * LD + 32];
             }
-            mma(acc[0], c0, b);
-            mma(acc[1], c1, b);
+            if constexpr (kDz) {
+#pragma unroll
+                for (int e = kParts - 1; e >= 0; --e) {
+                    mfma(acc[0], c0[0], b[e]);
+                    mfma(acc[1], c1[0], b[e]);
+                }
+            } else {
+                mma(acc[0], c0, b);
+                mma(acc[1], c1, b);
+            }
         };
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
@@ -340,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 const bool in_seg = nseg > 0 && pl >= s_seg_at[seg] && pl < s_seg_at[seg + 1];
 #pragma unroll
                 for (int s = 0; s < XP; ++s) {
-                    uint4_t b[Q];
+                    uint4_t b[kParts];
 #pragma unroll
                     for (int q = 0; q < Q; ++q)
 #pragma unroll
@@ -355,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
                 else fetch(ct + 1 < ct1 ? ct + 1 : ct, 0);
             }
         }
-        if (EX == kBare && (Q > 1 || EXT))
+        if (kDz || (EX == kBare && (Q > 1 || EXT)))
 #pragma unroll
             for (int c = 0; c < 2; ++c) probe(odd, acc[c]);
         if constexpr (EX == kLayer) {
@@ -462,6 +489,9 @@ __global__ __launch_bounds__(kThreads) void k_row_wide(RowOrder o, RowProduct p,
             }
             wave_sync();
         }
+    }
+    if constexpr (kDz) {
+        if (__syncthreads_or(odd != odd)) grad_plain_sums<T>(p, t.g, rows, s_row, ct0 * kCols, ct1 * kCols < p.N ? ct1 * kCols : p.N);
     }
     if constexpr (Q > 1 || EXT) {
         const int end = ct1 * kCols < p.N ? ct1 * kCols : p.N;

@@ -7,12 +7,12 @@ namespace {
 
 using namespace rows;
 
-template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool LINES>
+template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool LINES, Extra EX = kBare>
 hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
     const int64_t tiles = XP > 0 && !FUSED ? (o.n + kRows - 1) / kRows : o.n / kRows + o.G + 1;
     const WideGrid g = wide_grid(tiles, p.N);
-    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, LINES, kBare, false, false>), g.grid, dim3(kThreads), 0, s, o, p,
+    hipLaunchKernelGGL((k_row_wide<T, WNK, NP, XP, FUSED, WHOLE, LINES, EX, false, false>), g.grid, dim3(kThreads), 0, s, o, p,
                        g.splits);
     return hipGetLastError();
 }
@@ -20,6 +20,8 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 template <typename T, int NP, bool WHOLE, bool LINES>
 hipError_t with_pairs(const RowOrder &o, const RowProduct &p, hipStream_t s)
 {
+    if constexpr (sizeof(T) == 2)
+        if (p.slope_z) return launch<T, true, NP, 0, false, WHOLE, LINES, kGradZ>(o, p, s);
     if (!p.h && !p.a)
         return p.w_nk ? launch<T, true, NP, 0, false, WHOLE, LINES>(o, p, s)
                       : launch<T, false, NP, 0, false, WHOLE, LINES>(o, p, s);

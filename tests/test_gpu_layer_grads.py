@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 from tests import layers_ref as ref
-from tests.test_gpu_layers import draw_layer, named
+from tests.test_gpu_layers import LAYERS, draw_layer, named
 from tests.test_gpu_rows import cg, check, dev, host, rounded, strided  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +43,88 @@ def test_narrow_outputs_do_not_depend_on_each_other(cg, t, per, G, K, N, pad, ki
                                     **{n: None if a else False for n, a in zip(NAMES, asked)}, **kw)
         for g, h, a, name in zip(got, whole, asked, NAMES):
             assert torch.equal(g, h) if a else g is None, (name, asked)
+
+
+def grad_of_parts(x, w, z, dy, ids, name, per):
+    """(dx, dw, dbias), each (value, bound), of bf16 layers whose dz is held in two bf16 parts between its forming and the
+    products: dz in [1, 2) leaves at most 2^-8 to the second part, which rounds that by 2^-17. Sums have two terms for each
+    product; dbias adds dz itself or its parts. Without an activation dz is dy."""
+    G, K, N = w.shape
+    s, sb = ref.slope(z, name, "bf16")
+    dz = dy * s
+    formed = np.abs(dy) * sb + ref.U * np.abs(dz)
+    held = formed + (2.0 ** -17 * (np.abs(dz) + formed) if name != "none" else 0.0)
+    n, u_sum, half = ids.size, 2.0 ** -23, ref.out("bf16")
+    dx, dxb = np.zeros((n, K)), np.zeros((n, K))
+    dw, dwb, db, dbb = np.zeros(w.shape), np.zeros(w.shape), np.zeros((G, N)), np.zeros((G, N))
+    for g in range(G):
+        rows = np.flatnonzero(ids == g)
+        d, xs = dz[rows], x[rows // per]
+        dx[rows] = d @ w[g].T
+        dxb[rows] = (held[rows] + u_sum * (2 * N + 4) * np.abs(d)) @ np.abs(w[g]).T
+        dw[g] = xs.T @ d
+        dwb[g] = np.abs(xs).T @ (held[rows] + u_sum * (2 * len(rows) + 4) * np.abs(d)) + half * np.abs(dw[g])
+        db[g] = d.sum(0)
+        dbb[g] = (held[rows] + u_sum * (len(rows) + 4) * np.abs(d)).sum(0) + half * np.abs(db[g])
+    of = lambda a: a.reshape(n // per, per, K).sum(1)
+    v = of(dx)
+    return ((v, of(dxb + u_sum * per * np.abs(dx)) + half * np.abs(v) + ref.TINY), (dw, dwb + ref.TINY), (db, dbb + ref.TINY))
+
+
+# rows of x, rows that share one, groups, widths: each form of the two products, with whole steps and remainders
+HELD = LAYERS + [(20000, 1, 3, 128, 448), (9000, 4, 7, 128, 448), (20000, 1, 3, 448, 128), (6000, 3, 3, 900, 130),
+                 (30000, 1, 4, 72, 100), (12000, 2, 5, 300, 333), (40000, 1, 3, 333, 200), (5000, 1, 100, 70, 450),
+                 (2000, 1, 900, 100, 70), (300, 2, 300, 200, 90), (30000, 1, 2, 66, 5), (30000, 1, 2, 5, 66)]
+
+
+@pytest.mark.parametrize("t,per,G,K,N", HELD)
+@pytest.mark.parametrize("act,pad,kind", [("silu", 0, "even"), ("gelu", 3, "holes"), ("relu", 8, "holes"), ("none", 1, "even")])
+def test_bf16_gradients_hold_dz_in_two_parts(cg, t, per, G, K, N, act, pad, kind):
+    import torch
+
+    rng = np.random.default_rng(t + 5 * G + N)
+    x, w, ids, z, dy = draw_grad(rng, t, per, G, K, N, kind, "bf16")
+    o = cg.group_rows(dev(ids), G)
+    a = (strided(dev(x, "bf16"), pad), dev(w, "bf16"), strided(dev(dy, "bf16"), pad), *o)
+    kw = dict(z=None if act == "none" else strided(dev(z, "bf16"), pad + pad % 2), activation=named(act), per_row=per)
+    dx = strided(torch.zeros(t, K, dtype=torch.bfloat16, device="cuda"), pad) if pad else None
+    got = cg.grouped_layer_grad(*a, dx=dx, **kw)
+    for g, v, name in zip(got, grad_of_parts(x, w, z, dy, ids, act, per), NAMES):
+        check(g, v, name)
+    if pad:                                                     # what lies between the rows is left as it was
+        assert torch.isnan(got[0]._base[:, K:]).all()
+    # dx and dw are those of a call for them alone
+    assert torch.equal(cg.grouped_layer_grad(*a, dw=False, dbias=False, **kw)[0], got[0])
+    assert torch.equal(cg.grouped_layer_grad(*a, dx=False, dbias=False, **kw)[1], got[1])
+
+
+@pytest.mark.parametrize("t,per,G,K,N", [(300, 2, 4, 40, 500), (300, 1, 4, 40, 72), (400, 1, 2, 100, 96), (6000, 1, 3, 200, 200),
+                                         (600, 3, 3, 150, 130), (900, 1, 2, 300, 8), (500, 1, 400, 90, 70)])
+@pytest.mark.parametrize("act", ["silu", "relu"])
+def test_bf16_gradients_beside_what_is_not_finite(cg, t, per, G, K, N, act):
+    """Infinite weights and rows, and an infinite dy: dx and dw hold the infinities and NaN of the formula, and what they do
+    not reach keeps its bits."""
+    import torch
+
+    rng = np.random.default_rng(t + N)
+    x, w, ids, z, dy = draw_grad(rng, t, per, G, K, N, "even", "bf16")
+    o = cg.group_rows(dev(ids), G)
+    run = lambda x, w, dy: cg.grouped_layer_grad(dev(x, "bf16"), dev(w, "bf16"), dev(dy, "bf16"), *o, z=dev(z, "bf16"),
+                                                 activation=act, per_row=per)
+    base = run(x, w, dy)
+    x1, w1, dy1 = x.copy(), w.copy(), dy.copy()
+    g = ids[5]
+    w1[g, 3, 2] = np.inf
+    x1[1, 4] = -np.inf
+    dy1[7, 1] = np.inf
+    z[7, 1] = 1.0                                                # whose slope is no zero
+    base, got = run(x, w, dy), run(x1, w1, dy1)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = [v for v, _ in grad_of_parts(x1, w1, z, dy1, ids, act, per)]
+        plain = [v for v, _ in grad_of_parts(x, w, z, dy, ids, act, per)]
+    for h, b, v, p, name in zip(got, base, want, plain, NAMES):
+        fine = np.isfinite(v)
+        assert np.array_equal(np.isfinite(host(h)), fine), name
+        assert np.array_equal(host(h)[np.isinf(v)], v[np.isinf(v)]), name
+        same = torch.from_numpy(fine & (v == p)).cuda()
+        assert torch.equal(h[same], b[same]), name
