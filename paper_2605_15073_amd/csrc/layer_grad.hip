@@ -181,9 +181,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void k_layer_grad
                 if (!(in >> u & 1) || first >= width) f[u] = float4_t{0.f, 0.f, 0.f, 0.f};
         if (of_z) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-#pragma unroll
-                for (int e = 0; e < kCW; ++e) column[e] += f[u][e];
+            for (int e = 0; e < kCW; ++e) column[e] += sum_of_eight([&](int u) { return f[u][e]; });
             uint4_t u[kCW][P];
             parts_of<T, P>(f, u, 1.f);
 #pragma unroll

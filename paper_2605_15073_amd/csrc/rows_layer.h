@@ -92,6 +92,11 @@ __device__ __forceinline__ void split_pair(float a, float b, unsigned &high, uns
     low = pack_pair(ra, rb);
 }
 
+template <typename F> __device__ __forceinline__ float sum_of_eight(F f)
+{
+    return ((f(0) + f(1)) + (f(2) + f(3))) + ((f(4) + f(5)) + (f(6) + f(7)));
+}
+
 // Calls f with the activation, or kDzHeld, as a constant.
 template <typename F> __device__ __forceinline__ void with_act(int act, F f)
 {

@@ -25,23 +25,20 @@ namespace {
 
 using namespace rows;
 
-// Sums of b's columns, from the loads of its values: of the tiles that hold the first columns of a.
+// Sums of b's columns, from the loads of its values: of the tiles that hold the first columns of a. The eight rows of a
+// load are added first, so that a long sum takes an eighth of the additions.
 __device__ __forceinline__ void add_columns(float (&sum)[8], const uint4_t (&in)[8], bf16_t)
 {
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sum[2 * e] += __builtin_bit_cast(float, in[r][e] << 16);
-            sum[2 * e + 1] += __builtin_bit_cast(float, in[r][e] & 0xffff0000u);
-        }
+    for (int e = 0; e < 4; ++e) {
+        sum[2 * e] += sum_of_eight([&](int r) { return __builtin_bit_cast(float, in[r][e] << 16); });
+        sum[2 * e + 1] += sum_of_eight([&](int r) { return __builtin_bit_cast(float, in[r][e] & 0xffff0000u); });
+    }
 }
 __device__ __forceinline__ void add_columns(float (&sum)[4], const uint4_t (&in)[8], float)
 {
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += __builtin_bit_cast(float, (unsigned)in[r][e]);
+    for (int e = 0; e < 4; ++e) sum[e] += sum_of_eight([&](int r) { return __builtin_bit_cast(float, (unsigned)in[r][e]); });
 }
 
 enum Dz { kNoDz, kFormDz, kHeldDz };
@@ -218,17 +215,16 @@ __global__ __launch_bounds__(kThreads, DZ_ != kNoDz ? 3 : 1) void k_row_outer(Ro
                         }
                     });
                 if (sums) {  // of the parts; an infinity or NaN is the first alone
-                    auto add = [&](float &sum, unsigned high, unsigned low) {
+                    auto value = [](unsigned high, unsigned low) {
                         const float h = __builtin_bit_cast(float, high);
-                        sum += __builtin_isfinite(h) ? h + __builtin_bit_cast(float, low) : h;
+                        return __builtin_isfinite(h) ? h + __builtin_bit_cast(float, low) : h;
                     };
 #pragma unroll
-                    for (int r = 0; r < 8; ++r)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            add(column[2 * k], lb[r][k] << 16, lz[r][k] << 16);
-                            add(column[2 * k + 1], lb[r][k] & 0xffff0000u, lz[r][k] & 0xffff0000u);
-                        }
+                    for (int k = 0; k < 2; ++k) {
+                        column[2 * k] += sum_of_eight([&](int r) { return value(lb[r][k] << 16, lz[r][k] << 16); });
+                        column[2 * k + 1] +=
+                            sum_of_eight([&](int r) { return value(lb[r][k] & 0xffff0000u, lz[r][k] & 0xffff0000u); });
+                    }
                 }
                 to_units(lb, u);
 #pragma unroll

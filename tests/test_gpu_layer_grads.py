@@ -128,3 +128,20 @@ def test_bf16_gradients_beside_what_is_not_finite(cg, t, per, G, K, N, act):
         assert np.array_equal(host(h)[np.isinf(v)], v[np.isinf(v)]), name
         same = torch.from_numpy(fine & (v == p)).cuda()
         assert torch.equal(h[same], b[same]), name
+
+
+@pytest.mark.parametrize("G,K,N", [(512, 8, 60), (376, 8, 72)])
+def test_bias_gradient_of_many_small_terms(cg, G, K, N):
+    """Groups of 4,096 rows, the first 1 and the others 2^-25, which are lost where they are added to it one by one. Eight
+    rows of 32 or 64 are added first, so that a sum takes 128 additions of those, 3 within them and 16 of lanes, each off by
+    U of it."""
+    import torch
+
+    n = 4096
+    dy = torch.full((G * n, N), 2.0 ** -25, device="cuda")
+    dy[::n] = 1.0
+    x, w = torch.zeros(G * n, K, device="cuda"), torch.zeros(G, K, N, device="cuda")
+    offsets = torch.arange(0, G * n + 1, n, dtype=torch.int32, device="cuda")
+    got = cg.grouped_layer_grad(x, w, dy, offsets, dx=False)[2].double()
+    want = 1 + (n - 1) * 2.0 ** -25
+    assert (got - want).abs().max().item() <= (128 + 3 + 16) * ref.U * want
