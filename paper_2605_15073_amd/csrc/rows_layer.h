@@ -15,9 +15,24 @@ enum Extra { kBare, kLayer, kSums, kGrad, kSumsZ, kGradZ };
 template <Extra EX> constexpr bool kForms = EX == kSumsZ || EX == kGradZ;
 template <Extra EX> constexpr int kRowParts = kForms<EX> ? 2 : 1;  // bf16 operands that a row of the input is
 
+// exp(a), 4 2^-24 of it off whatever a is: the rounding of a / log 2, which alone would be off by that times |a|, is put
+// back behind the exponential. Arguments are held where the results are 0 or infinite already. Layers in fp32, silu, us with
+// the plain exponential and with it: 525,308 rows, 64 -> 64, z, 84 and 88, 262,144, 64 -> 448, 140 and 152, gradients 116 and 120.
+__device__ __forceinline__ float exp_far(float a)
+{
+    constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f;  // 1 / log 2 in two parts
+    a = __builtin_amdgcn_fmed3f(a, -150.f, 150.f);
+    const float t = a * kLog2e, off = fmaf(a, kRest, fmaf(a, kLog2e, -t));
+    return __builtin_amdgcn_exp2f(t) * fmaf(0.693147182f, off, 1.f);
+}
+
 // silu: z s(z), s the logistic function; gelu: z P(z), P the normal distribution function; relu: max(z, 0).
-// An infinite z gives what the formula's products do: -inf s(-inf) is NaN.
-__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+// An infinite z gives what the formula's products do: -inf s(-inf) is NaN. The exponential of bf16 results is the plain
+// one, off by 2.5 |z| 2^-24.
+template <typename T> __device__ __forceinline__ float logistic(float z)
+{
+    return __builtin_amdgcn_rcpf(1.f + (sizeof(T) == 2 ? __expf(-z) : exp_far(-z)));
+}
 
 __device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(-0.72134752f * z * z); }  // exp(-z^2 / 2)
 
@@ -58,7 +73,7 @@ template <typename T> __device__ __forceinline__ float normal_cdf(float z)
 // T: the type that the result is rounded to.
 template <typename T> __device__ __forceinline__ float activate(float z, int act)
 {
-    if (act == CGTP_ACT_SILU) return z * logistic(z);
+    if (act == CGTP_ACT_SILU) return z * logistic<T>(z);
     if (act == CGTP_ACT_GELU) return z * normal_cdf<T>(z);
     if (act == CGTP_ACT_RELU) return z <= 0.f ? 0.f : z;
     return z;
@@ -68,7 +83,7 @@ template <typename T> __device__ __forceinline__ float activate(float z, int act
 template <typename T> __device__ __forceinline__ float activate_slope(float z, int act)
 {
     if (act == CGTP_ACT_SILU) {
-        const float f = logistic(z);
+        const float f = logistic<T>(z);
         return f * (1.f + z * (1.f - f));
     }
     if (act == CGTP_ACT_GELU) return normal_cdf<T>(z) + z * 0.39894228f * bell(z);
