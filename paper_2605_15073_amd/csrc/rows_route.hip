@@ -431,7 +431,7 @@ __global__ __launch_bounds__(kThreads) void k_route(RowRoute p)
     } else if (soft) {
         shift = top;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) sum += there(x[j]) ? __expf(x[j] - top) : 0.f;
+        for (int j = 0; j < PER; ++j) sum += there(x[j]) ? exp_far(x[j] - top) : 0.f;
         sum = row_sum<L>(sum);
     }
     float total = 0.f;
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void k_route(RowRoute p)
     for (int i = 0; i < NI; ++i) {
         if (l + L * i >= p.k) break;
         const float v = w[i];
-        w[i] = !there(v) ? 0.f : soft ? __expf(v - shift) : __expf(fminf(v, 0.f) - shift) / (1.f + __expf(-fabsf(v)));
+        w[i] = !there(v) ? 0.f : soft ? exp_far(v - shift) : exp_far(fminf(v, 0.f) - shift) / (1.f + exp_far(-fabsf(v)));
         total += w[i];
     }
     if (p.renorm) sum = row_sum<L>(total);

@@ -34,3 +34,19 @@ def test_slope_of_silu_below_zero_in_fp32(cg):
     dx, _, _ = cg.grouped_layer_grad(dev(z), one, torch.ones(len(z), 1, device="cuda"), *o, z=dev(z), activation="silu")
     f = ref.logistic(z)
     assert np.all(np.abs(host(dx) - f * (1 + z * (1 - f))) <= 16 * ref.U * (f + np.abs(z) * f * (1 - f)) + ref.TINY)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("E,k", [(8, 8), (48, 24), (130, 40)])
+def test_routing_weights_of_far_logits(cg, dtype, score, renorm, E, k):
+    """Logits that are multiples of 1/4 up to 60, whose differences fp32 holds. A share is an exponential, 4 U, over one plus
+    another, 3 U, a quotient's U: 8 U. Their sum, of k or E, has the same and U of each addition; quotient and scale U each."""
+    rng = np.random.default_rng(E)
+    logits = rng.integers(-120, 121, (700, E)) * 0.25
+    scale = 3.0 if score == "softmax" else 2.0
+    ids, w = cg.route_rows(dev(logits, dtype), k, score=score, renormalize=renorm, scale=scale)
+    want, (value, _) = ref.route(logits, k, None, score, 1, 1, renorm, scale)
+    assert np.array_equal(ids.cpu().numpy(), want)
+    assert np.all(np.abs(host(w) - value) <= (20 + E) * ref.U * np.abs(value) + ref.TINY)
