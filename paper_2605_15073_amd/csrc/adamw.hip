@@ -245,10 +245,11 @@ __device__ __forceinline__ double block_sum(double sum, double *s_sum)
     return (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
 }
 
+// grad_scale may be scale (or norm): it is read first.
 template <typename G>
 __global__ __launch_bounds__(kThreads) void k_grad_norm(const Tensor *__restrict__ tensors, const Item *__restrict__ items,
                                                         int64_t n_items, double *sums, unsigned *counters, double max_norm,
-                                                        const float *__restrict__ grad_scale, float *norm, float *scale)
+                                                        const float *grad_scale, float *norm, float *scale)
 {
     typedef G g4_t __attribute__((ext_vector_type(4)));
     __shared__ double s_sum[kThreads / 64];
