@@ -531,8 +531,8 @@ int cgtp_grouped_layer(int dtype, int64_t n_rows, int n_groups, int n_in, int n_
  *   dbias[g] = sum over the rows of g of dz_i            [n_groups][n_out].
  * Any of the three may be NULL (not all); x is needed for dw alone, w for dx alone, z unless the activation is
  * CGTP_ACT_NONE. Rows of no group have no part, and groups without rows get 0. Where per_row is above 1, order has
- * to hold every row, as cgtp_group_rows makes it, for dx to be defined. Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE,
- * CGTP_ERR_HIP. */
+ * to hold every row, as cgtp_group_rows makes it, for dx to be defined. A call whose dx is NULL needs the workspace of
+ * per_row 1. Errors: CGTP_ERR_ARG, CGTP_ERR_WORKSPACE, CGTP_ERR_HIP. */
 int cgtp_grouped_layer_grad_bytes(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,
                                   int per_row, int activation, size_t *bytes);
 int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, int n_in, int n_out,

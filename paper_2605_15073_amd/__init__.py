@@ -960,7 +960,7 @@ def grouped_layer_grad(x, w, dy, offsets, order=None, z=None, activation=None, p
     dx, dxs = _grad_out("dx", dx, (t, n_in), x, True)
     dw, _ = _grad_out("dw", dw, (G, n_in, n_out), x, False)
     dbias, _ = _grad_out("dbias", dbias, (G, n_out), x, False)
-    need = _bytes("cgtp_grouped_layer_grad_bytes", dt, n, G, n_in, n_out, per_row, act)
+    need = _bytes("cgtp_grouped_layer_grad_bytes", dt, n, G, n_in, n_out, 1 if dx is None else per_row, act)
     ws_ptr, ws_len, ws = _row_workspace(workspace, need, x)
     _run("cgtp_grouped_layer_grad", x, side, (x, w, dy, z, offsets, order, dx, dw, dbias, ws), dt, n, G, n_in, n_out, per_row,
          _addr(offsets), _addr(order), _addr(x), xs, _addr(w), _addr(z), zs, act, _addr(dy), dys, _addr(dx), dxs,

@@ -448,8 +448,8 @@ bool dz_apart(int dtype, int n_in, int activation)
     return activation != CGTP_ACT_NONE && (dtype == CGTP_F32 || n_in > 128);
 }
 
-// dz where it has a pass of its own, the row gradients in fp32 where rows share their input, and sums of the weight
-// gradients.
+// dz where it has a pass of its own, the row gradients (per_row 1 where they are not asked for) in fp32 where rows share
+// their input, and sums of the weight gradients. The form of narrow layers has no dz, whatever it is asked for.
 struct LayerGradBytes {
     size_t dz, rows, sums;
     size_t all() const { return dz + rows + sums; }
@@ -457,14 +457,11 @@ struct LayerGradBytes {
 
 LayerGradBytes layer_grad_bytes(int dtype, int64_t n, int G, int n_in, int n_out, int per_row, int activation)
 {
-    const size_t of[3] = {cgtp::row_outer_bytes(dtype, n, G, n_in, n_out, true),
-                          cgtp::row_outer_bytes(dtype, n, G, 1, n_out, true),  // dbias alone
-                          cgtp::layer_grad_takes(dtype, n, G, n_in, n_out)
-                              ? cgtp::layer_grad_slots(dtype, n, G, n_in, n_out) : 0};
-    size_t sums = of[0];
-    for (const size_t b : of) sums = b > sums ? b : sums;
-    return {dz_apart(dtype, n_in, activation) ? align256((size_t)n * n_out * 4) : 0,
-            per_row == 1 ? 0 : align256((size_t)n * n_in * 4), sums};
+    const size_t rows = per_row == 1 ? 0 : align256((size_t)n * n_in * 4);
+    if (cgtp::layer_grad_takes(dtype, n, G, n_in, n_out)) return {0, rows, cgtp::layer_grad_slots(dtype, n, G, n_in, n_out)};
+    const size_t all = cgtp::row_outer_bytes(dtype, n, G, n_in, n_out, true);
+    const size_t alone = cgtp::row_outer_bytes(dtype, n, G, 1, n_out, true);  // dbias
+    return {dz_apart(dtype, n_in, activation) ? align256((size_t)n * n_out * 4) : 0, rows, all > alone ? all : alone};
 }
 
 int check_score(int score, int renormalize, float scale)
@@ -634,7 +631,7 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
         CGTP_TRY(check_ptr(dw, "dw", es));
     }
     if (dbias) CGTP_TRY(check_ptr(dbias, "dbias", es));
-    const LayerGradBytes need = layer_grad_bytes(dtype, n_rows, n_groups, n_in, n_out, per_row, activation);
+    const LayerGradBytes need = layer_grad_bytes(dtype, n_rows, n_groups, n_in, n_out, dx ? per_row : 1, activation);
     CGTP_TRY(check_ws(workspace, ws_bytes, need.all()));
     const cgtp::RowOrder o{n_rows, n_groups, offsets, order};
     const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -145,3 +145,27 @@ def test_bias_gradient_of_many_small_terms(cg, G, K, N):
     got = cg.grouped_layer_grad(x, w, dy, offsets, dx=False)[2].double()
     want = 1 + (n - 1) * 2.0 ** -25
     assert (got - want).abs().max().item() <= (128 + 3 + 16) * ref.U * want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t,per,G,K,N", [(3000, 4, 3, 64, 64), (3000, 4, 3, 200, 72), (500, 3, 900, 64, 64)])
+def test_workspace_without_row_gradients(cg, dtype, t, per, G, K, N):
+    """dw and dbias alone take the workspace that the query gives for rows of their own, and no less."""
+    import torch
+
+    rng = np.random.default_rng(t)
+    x, w, ids, z, dy = draw_grad(rng, t, per, G, K, N, "even", dtype)
+    o = cg.group_rows(dev(ids), G)
+    run = lambda **kw: cg.grouped_layer_grad(dev(x, dtype), dev(w, dtype), dev(dy, dtype), *o, z=dev(z, dtype), activation="silu",
+                                             per_row=per, **kw)
+    need = cg._bytes("cgtp_grouped_layer_grad_bytes", cg.CGTP_BF16 if dtype == "bf16" else cg.CGTP_F32, t * per, G, K, N, 1,
+                     cg.CGTP_ACT_SILU)
+    space = torch.empty(need, dtype=torch.uint8, device="cuda")
+    whole = run()
+    _, dw, db = run(dx=False, workspace=space)
+    assert torch.equal(dw, whole[1]) and torch.equal(db, whole[2])
+    with pytest.raises(cg.CgtpError):
+        run(workspace=space)
+    if need > 0:
+        with pytest.raises(cg.CgtpError):
+            run(dx=False, workspace=space[:need - 1])
