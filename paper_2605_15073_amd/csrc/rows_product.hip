@@ -535,6 +535,19 @@ hipError_t launch(const RowOrder &o, const RowProduct &p, hipStream_t s)
 // Whether tiles of 128 by 128 would leave compute units without one.
 bool idle(const RowOrder &o, const RowProduct &p) { return (o.n / 128 + o.G) * ((p.N + 127) / 128) < 256; }
 
+// The same of plain products, whose k is not one of lean steps: they are ahead up to three tiles of 64 by 64 a compute unit,
+// bf16 with [K][N] weights up to two. Us of 64 and 128, with the tiles of 64: y in fp32, 2,000 rows of 20 groups, 1344 -> 128,
+// 57 and 97 (102), 14,000 of 2, 896 -> 128, 47 and 68 (440), 22,000 59 and 69 (690), 26,000 86 and 70 (816), 24,000 of 10
+// 60 and 70 (770), 28,000 of 2, 256 -> 72, 29 and 25 (878); bf16 26 and 32, 21 and 24, 25 and 26, 29 and 27, 28 and 27, 12 and
+// 11, 18,000 of 100, 300 -> 96, 14.4 and 13.1 (762); dx fp32 46 and 94, 35 and 66, 49 and 66, 60 and 67, 58 and 67, 21 and
+// 23; bf16 20 and 28, 17 and 21, 19 and 23, 21 and 25, 21 and 25, 9.4 and 10, 26,000 of 2, 256 -> 72, 10.1 and 9.9 (816).
+// One group's tiles, and those that adapters share, have not been compared and stay at 128.
+template <typename T, bool WNK> bool plain_small(const RowOrder &o, const RowProduct &p)
+{
+    return p.w_group != 0 && o.G > 1 && idle(o, p) &&
+           (o.n / 64 + o.G) * ((p.N + 63) / 64) <= (sizeof(T) == 2 && !WNK ? 512 : 768);
+}
+
 // Whether tiles of 64 by 64, of which 1,024 run at once, end before those of 128 by 128, of which 512 do. Us of 128 and 64,
 // with the tiles of each: fp32 y of 6,000 rows of 20 groups, 1344 -> 448, 117 and 93 (264, 791), 12,500 of 3, 126 and 156
 // (400, 1,386), 24,000 of 10, 1344 -> 258, 222 and 196 (591, 1,925), 12,500 of 3, 300 -> 897, 78 and 103 (800, 2,970); dx
@@ -596,7 +609,7 @@ hipError_t pick(const RowOrder &o, const RowProduct &p, hipStream_t s)
     if (!few && row_wide_takes(dtype, p)) return launch_row_wide(dtype, o, p, s);
     if (p.N <= 32) return launch<T, WNK, 128, 32, 4>(o, p, s);
     if (few && p.N > 64) return launch<T, WNK, 32, 128, 1>(o, p, s);
-    if (few || p.N <= 64 || (groups > 1 && idle(o, p))) return launch<T, WNK, 64, 64, 2>(o, p, s);
+    if (few || p.N <= 64 || plain_small<T, WNK>(o, p)) return launch<T, WNK, 64, 64, 2>(o, p, s);
     return launch<T, WNK, 128, 128, kWaveRows<T>>(o, p, s);
 }
 
