@@ -20,14 +20,6 @@ template <int E> constexpr int kMost = E < CGTP_MAX_TOP_K ? E : CGTP_MAX_TOP_K; 
 // LDS of a wave's rows: keys and blocks' scores, in 64 bits or (the row 4 longer) in 32.
 __host__ __device__ constexpr int wave_bytes(int rows, int keys, int blocks) { return rows * (8 * (keys + blocks) + 16); }
 
-// Orders a wave's LDS writes before its other lanes' reads.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // A logit of -inf, or NaN, is of an expert that the row may not have.
 __device__ __forceinline__ bool there(float l) { return l > -__builtin_inff(); }
 

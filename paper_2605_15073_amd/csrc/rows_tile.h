@@ -48,6 +48,14 @@ template <typename T> constexpr int kStep = kGroups<T> * kU;           // k of a
 template <typename T> constexpr int kWide = 8 / (int)sizeof(T);        // lanes of a transposed load
 template <typename T, int R> constexpr int kTile = kSplit<T> * kGroups<T> * (R + 1);  // units of a tile
 
+// Orders a wave's LDS writes before its other lanes' reads.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ __forceinline__ int clamp_offset(int v, int64_t n)
 {
     return v < 0 ? 0 : (int64_t)v > n ? (int)n : v;

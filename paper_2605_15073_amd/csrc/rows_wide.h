@@ -66,14 +66,6 @@ __device__ __forceinline__ void convert(float4_t v, bf4_t &o)
     o = bf4_t{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
 }
 
-// Orders a wave's LDS writes before its other lanes' reads.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // NP, XP: pairs of k-groups of the inputs and of the narrow product's rows (0: no adapters). All parts of those
 // rows, XP / P pairs each, meet the same weights, which lie in LDS once.
 template <typename T, bool WNK, int NP, int XP, bool FUSED, bool WHOLE, bool LINES, Extra EX, bool Z, bool RES>
