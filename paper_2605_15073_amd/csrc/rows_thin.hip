@@ -3,21 +3,32 @@
 // A tile of the general product takes its k in steps that wait for memory one after the other, 1.5 to 2 us each; where
 // tiles are too few to fill the GPU, that is the call's time. Here a workgroup has 32 rows by 32 columns, and its waves
 // share the k: wave w takes the steps w, w + 4, ... with the operands straight from memory, a step ahead, and the four
-// sums are added in LDS. Us, general product and this form, of a layer and of its x gradient (n rows in G groups):
+// sums are added in LDS. Us, in a graph, general product and this form, of a layer (silu) and of the row gradient whose
+// product has the same K and N (n rows in G groups):
 //
-//     n, G          K, N         bf16                      fp32
-//     64, 5         256, 64      8.3 4.5     5.7 3.4       15 5.8      11 5.3
-//     64, 5         896, 16      20 7.5      14 5.1        48 13       39 10
-//     64, 5         1344, 448    21 10       16 6.8        56 18       52 14
-//     3000, 20      896, 128     17 15       15 13         41 23       33 22
-//     1000, 10      1344, 448    24 23       20 21         60 38       47 38
-//     2000, 300     256, 64      9.4 5.8     6.7 4.8       18 9.1      13 9.0
-//     12000, 10     896, 16      22 11       17 9.0        50 21       41 17
-//     6000, 20      896, 128     18 19       16 19         42 32       33 35
-//     3000, 20      1344, 448    29 50       23 43         72 78       52 83
+//     n, G          K, N         tiles     bf16                      fp32
+//     64, 5         896, 16      7         16 8.0     9.9 5.3        45 13      34 10
+//     64, 5         256, 64      14        7.8 4.9    5.1 3.6        16 6.2     11 5.4
+//     64, 5         1344, 448    98        18 11      13 7.0         52 19      49 15
+//     12000, 10     896, 16      385       17 11      12 9.1         46 22      35 17
+//     3000, 20      896, 128     452       15 16      9.3 13         40 23      29 22
+//     500, 100      448, 128     460       10 7.6     6.7 5.4        22 13      19 11
+//     8000, 20      256, 64      540       8.3 6.8    5.5 5.9        17 11      11 11
+//     1000, 10      1344, 448    574       20 23      12 21          58 38      41 38
+//     4000, 200     300, 64      650       10 8.5     7.5 6.2        21 12      15 11
+//     2000, 300     256, 64      724       9.0 7.2    6.2 5.1        19 9.8     13 9.0
+//     6000, 20      896, 128     828       15 19      10 19          41 34      29 35
+//     500, 200      448, 128     860       10 8.6     7.4 7.2        16 16      14 14
+//     1500, 20      256, 448     924       8.9 10     6.1 6.8        19 15      13 13
+//     1500, 300     256, 96      1038      8.6 9.1    6.7 6.0        18 12      15 11
+//     16000, 20     256, 64      1040      9.1 11     6.2 8.3        19 18      13 16
+//     1000, 500     256, 64      1062      11 9.2     6.8 6.3        9.7 9.9    8.1 8.3
+//     3000, 20      1344, 448    1582      24 49      17 44          68 79      49 82
 //
-// The rows are in the order of the tiles that a call may have here, 14 to 1,582: every one reads its operands from L2
-// anew, so that from 512 (bf16) and 1,024 tiles (fp32) on the general product is the faster one.
+// Tiles are those that a call may have, (n / 32 + G) ceil(N / 32). Every one reads its operands from L2 anew, so that of
+// groups that fill tiles the general product is ahead from 512 of them or 370,000 tiles times k on in bf16, from 1,024 in
+// fp32, row gradients from 640. Groups of fewer rows than a tile leave the general product's larger ones emptier still: there
+// bf16 rows of up to 64 columns are ahead at any number.
 //
 // Sums are split over k: they are other fp32 sums than the general product's, so that only layers and their row
 // gradients take this form.
@@ -182,7 +193,10 @@ bool row_thin_takes(int dtype, const RowOrder &o, const RowProduct &p)
 {
     const int es = dtype == CGTP_BF16 ? 2 : 4;
     if (!(p.per > 0 || p.split_k) || p.h || p.a || p.narrow || p.K <= 128 * 2 / es) return false;
-    return (o.n / kThin + o.G) * ((p.N + kThin - 1) / kThin) <= (es == 2 ? 512 : 1024);
+    const int64_t tiles = (o.n / kThin + o.G) * ((p.N + kThin - 1) / kThin);
+    const bool part_tiles = o.n < (int64_t)kThin * o.G;
+    if (es == 4) return tiles <= (part_tiles || !p.w_nk ? 1024 : 640);
+    return part_tiles ? tiles <= 512 || p.N <= 64 : tiles <= 512 && tiles * p.K <= 370000;
 }
 
 hipError_t launch_row_thin(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)
