@@ -28,7 +28,8 @@
 // Tiles are those that a call may have, (n / 32 + G) ceil(N / 32). Every one reads its operands from L2 anew, so that of
 // groups that fill tiles the general product is ahead from 512 of them or 370,000 tiles times k on in bf16, from 1,024 in
 // fp32, row gradients from 640. Groups of fewer rows than a tile leave the general product's larger ones emptier still: there
-// bf16 rows of up to 64 columns are ahead at any number.
+// bf16 rows of up to 64 columns are ahead to 1,100 tiles, of 32 at any number (4,000 rows of 4,000 groups, 256 -> 32, 36 and
+// 22; but the row gradient of 10,007 of 4,005, 37 -> 129, from dz in parts takes 54 and 64).
 //
 // Sums are split over k: they are other fp32 sums than the general product's, so that only layers and their row
 // gradients take this form.
@@ -196,7 +197,8 @@ bool row_thin_takes(int dtype, const RowOrder &o, const RowProduct &p)
     const int64_t tiles = (o.n / kThin + o.G) * ((p.N + kThin - 1) / kThin);
     const bool part_tiles = o.n < (int64_t)kThin * o.G;
     if (es == 4) return tiles <= (part_tiles || !p.w_nk ? 1024 : 640);
-    return part_tiles ? tiles <= 512 || p.N <= 64 : tiles <= 512 && tiles * p.K <= 370000;
+    if (part_tiles) return tiles <= (p.N <= kThin ? INT64_MAX : p.N <= 2 * kThin ? 1100 : 512);
+    return tiles <= 512 && tiles * p.K <= 370000;
 }
 
 hipError_t launch_row_thin(int dtype, const RowOrder &o, const RowProduct &p, hipStream_t s)
