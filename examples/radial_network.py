@@ -3,10 +3,10 @@
 Message passing takes the radial features `edge_radial` [E, C, L] as given. Here a small network makes
 them from the 8 Gaussians of each edge's distance:
 
-    hidden = silu(w1[pair of elements]^T g)                                    (grouped_linear)
+    hidden = silu(w1[pair of elements]^T g)                                    (grouped_layer)
     edge_radial = w2^T hidden + scale[request] b[request]^T (a[request]^T hidden)  (adapter_linear)
 
-1. w1 and w2 learn given radial features (grouped_linear_grad, adamw with states in 8 bits).
+1. w1 and w2 learn given radial features (grouped_linear_grad, grouped_layer_grad, adamw with states in 8 bits).
 2. w1 and w2 stay; every request learns its own change of them by its adapter
    (adapter_linear_grad, adamw with states in 32 bits).
 3. One message pass serves all requests at once, and the atoms of none, which keep the base model.
@@ -67,9 +67,9 @@ class Model:
         dist = inputs.periodic_neighbours(pos, box, r_cut)[3]
         return inputs.gaussian_radial(dist, r_cut).astype(np.float32)
 
-    def hidden(self):
-        z = cg.grouped_linear(self.g, self.w1, *self.by_pair)
-        return z, z * torch.sigmoid(z)
+    def hidden(self, z=False):
+        """The hidden features; with z None (features, what the activation took)."""
+        return cg.grouped_layer(self.g, self.w1, *self.by_pair, activation="silu", z=z)
 
     def radial(self, h):
         return cg.adapter_linear(h, self.w2, self.a, self.b, *self.by_request, scale=self.scale)
@@ -84,14 +84,13 @@ class Model:
         opt = cg.AdamWTensors(weights, grads, codes(torch.int8), codes(torch.uint8), scales(), scales())
         losses = []
         for step in range(1, steps + 1):
-            z, h = self.hidden()
+            h, z = self.hidden(z=None)
             err = self.radial(h) - self.target
             losses.append(err.square().mean())
             dy = err * (2.0 / err.numel())
             dh, _ = cg.grouped_linear_grad(h, self.w2[None], dy, *self.all_rows, dw=grads[1][None])
-            s = torch.sigmoid(z)
-            dz = dh * (s * (1 + z * (1 - s)))
-            cg.grouped_linear_grad(self.g, self.w1, dz, *self.by_pair, dx=False, dw=grads[0])
+            cg.grouped_layer_grad(self.g, self.w1, dh, *self.by_pair, z=z, activation="silu", dx=False,
+                                  dw=grads[0], dbias=False)
             cg.adamw(opt, step=step, lr=lr, weight_decay=0.0)
         return torch.stack(losses).tolist()
 
@@ -101,7 +100,7 @@ class Model:
         grads = [torch.empty_like(w) for w in weights]
         zeros = lambda: [torch.zeros_like(w) for w in weights]
         opt = cg.AdamWTensors(weights, grads, zeros(), zeros())
-        _, h = self.hidden()
+        h = self.hidden()
         losses = []
         for step in range(1, steps + 1):
             err = self.radial(h) - target
@@ -114,7 +113,7 @@ class Model:
 
     def serve(self):
         """One message pass over the whole batch: (radial features, out_even, out_odd)."""
-        y = self.radial(self.hidden()[1])
+        y = self.radial(self.hidden())
         t = dict(self.call, edge_radial=y.view_as(self.call["edge_radial"]))
         return y, *cg.message_pass(self.plan, *t.values())
 
