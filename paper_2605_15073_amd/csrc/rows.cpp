@@ -459,8 +459,9 @@ LayerGradBytes layer_grad_bytes(int dtype, int64_t n, int G, int n_in, int n_out
 {
     const size_t rows = per_row == 1 ? 0 : align256((size_t)n * n_in * 4);
     if (cgtp::layer_grad_takes(dtype, n, G, n_in, n_out)) return {0, rows, cgtp::layer_grad_slots(dtype, n, G, n_in, n_out)};
-    const size_t all = cgtp::row_outer_bytes(dtype, n, G, n_in, n_out, true);
-    const size_t alone = cgtp::row_outer_bytes(dtype, n, G, 1, n_out, true);  // dbias
+    const bool parts = dtype == CGTP_BF16 && activation != CGTP_ACT_NONE;
+    const size_t all = cgtp::row_outer_bytes(dtype, n, G, n_in, n_out, true, parts);
+    const size_t alone = cgtp::row_outer_bytes(dtype, n, G, 1, n_out, true, parts);  // dbias
     return {dz_apart(dtype, n_in, activation) ? align256((size_t)n * n_out * 4) : 0, rows, all > alone ? all : alone};
 }
 
@@ -685,7 +686,7 @@ extern "C" int cgtp_grouped_layer_grad(int dtype, int64_t n_rows, int n_groups, 
             b_stride = slope_stride = 2 * (int64_t)n_out;
             act = cgtp::kDzHeld;
         }
-    } else if (activation != CGTP_ACT_NONE) {
+    } else if (activation != CGTP_ACT_NONE && dtype == CGTP_BF16) {
         slope_z = z;
         slope_stride = z_stride;
     }

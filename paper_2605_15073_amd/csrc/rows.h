@@ -107,7 +107,8 @@ struct RowOuter {
     int64_t slope_stride;
     int act;
 };
-size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B, bool sums = false);
+// parts: b is formed from slope_z.
+size_t row_outer_bytes(int dtype, int64_t n_rows, int G, int A, int B, bool sums = false, bool parts = false);
 hipError_t launch_row_outer(int dtype, const RowOrder &o, const RowOuter &p, void *ws,
                             hipStream_t s);
 // The forms for groups of few rows (rows_few.hip), up to kFewMean on the mean, and whether that of products

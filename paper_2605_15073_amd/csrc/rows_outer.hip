@@ -446,6 +446,7 @@ constexpr int kMinRows = 256, kMaxRows = 16384;  // of a chunk
 
 struct Shape {
     int bm, bn, rows;  // of a chunk
+    int per_cu;        // workgroups on a compute unit
     int64_t tiles;
 };
 
@@ -456,8 +457,7 @@ struct Shape {
 // mean, 14% at worst; powers of two that leave two rounds were 13% off, 25% at worst.
 int chunk_rows(size_t es, int64_t n, int G, const Shape &s)
 {
-    const int per_cu = es == 4 ? (s.bm == 128 && s.bn >= 64 ? 2 : 3) : s.bn == 128 ? 3 : 4;
-    const double at_once = 256 * per_cu, groups = (double)(n < G ? n : G), mean = n / groups;
+    const double at_once = 256 * s.per_cu, groups = (double)(n < G ? n : G), mean = n / groups;
     int best = kMinRows;
     double least = 0;
     for (int r = kMinRows; r <= kMaxRows; r += r / 1024 * 64 + 64) {
@@ -473,12 +473,17 @@ int chunk_rows(size_t es, int64_t n, int G, const Shape &s)
     return best >= mean && wide > best ? wide : best;
 }
 
-Shape shape(size_t es, int64_t n, int G, int A, int B)
+// dz in parts: 64 columns, whose sums leave registers for both. Us with 128 of them and 64: formed, 261,764 rows, 128 x 448,
+// 230 (two workgroups on a compute unit) and 229; held, 60,000 rows, 1344 x 448, 304 and 302, 20,000 of 100 groups, 128 x
+// 128, 25 and 22, 6,000 of 20, 1344 x 448, 64 and 56.
+Shape shape(size_t es, int64_t n, int G, int A, int B, bool parts)
 {
     Shape s;
     s.bm = A > 64 ? 128 : 64;
-    s.bn = B > 64 ? 128 : B > 32 ? 64 : 32;
+    s.bn = B > 64 ? (parts ? 64 : 128) : B > 32 ? 64 : 32;
     if (s.bm == 64) s.bn = 64;
+    const bool large = s.bm == 128 && s.bn >= 64;
+    s.per_cu = es == 4 ? (large ? 2 : 3) : large && (parts || s.bn == 128) ? 3 : 4;
     s.tiles = (int64_t)((A + s.bm - 1) / s.bm) * ((B + s.bn - 1) / s.bn);
     s.rows = n > 0 ? chunk_rows(es, n, G, s) : kMinRows;
     return s;
@@ -524,14 +529,7 @@ hipError_t join(const RowOrder &o, int chunk, int A, int B, const float *slots, 
 template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float *slots, hipStream_t s)
 {
     const int B = q.r > 0 ? q.r : q.B;
-    Shape sh = shape(sizeof(T), o.n, o.G, q.A, B);
-    // dz in parts: 64 columns, whose sums leave registers for both. Us with 128 of them and 64: formed, 261,764 rows, 128 x
-    // 448, 230 (two workgroups on a compute unit) and 229; held, 60,000 rows, 1344 x 448, 304 and 302, 20,000 of 100
-    // groups, 128 x 128, 25 and 22, 6,000 of 20, 1344 x 448, 64 and 56.
-    if (q.slope_z && sh.bn == 128) {
-        sh.bn = 64;
-        sh.tiles = (int64_t)((q.A + 127) / 128) * ((B + 63) / 64);
-    }
+    const Shape sh = shape(sizeof(T), o.n, o.G, q.A, B, q.slope_z != nullptr);
     const bool big = o.n <= kFewMean * (int64_t)o.G;  // the groups of few rows go their own way
     hipError_t e;
     if (big) {
@@ -548,9 +546,9 @@ template <typename T> hipError_t run(const RowOrder &o, const RowOuter &q, float
 
 }  // namespace
 
-size_t row_outer_bytes(int dtype, int64_t n, int G, int A, int B, bool sums)
+size_t row_outer_bytes(int dtype, int64_t n, int G, int A, int B, bool sums, bool parts)
 {
-    const Shape sh = shape(dtype == CGTP_BF16 ? 2 : 4, n, G, A, B);
+    const Shape sh = shape(dtype == CGTP_BF16 ? 2 : 4, n, G, A, B, parts);
     return n <= sh.rows ? 0 : ((size_t)2 * (n / sh.rows) + 2) * (A + sums) * B * sizeof(float);
 }
 

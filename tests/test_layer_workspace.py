@@ -27,10 +27,12 @@ def test_narrow_layers_have_no_dz(dtype, n, G, n_in, n_out):
 
 
 def test_wide_layers_in_bf16_form_dz_in_the_products():
-    assert need(BF16, 261764, 32, 128, 448, 1, SILU) == need(BF16, 261764, 32, 128, 448, 1, NONE)
-    dz = 60000 * 448 * 4
-    assert need(BF16, 60000, 32, 1344, 448, 1, SILU) == need(BF16, 60000, 32, 1344, 448, 1, NONE) + dz
-    assert need(F32, 60000, 32, 128, 448, 1, SILU) == need(F32, 60000, 32, 128, 448, 1, NONE) + dz
+    """Up to 128 inputs: sums of chunks are all that is kept then."""
+    dz = lambda n, n_out: n * n_out * 4
+    assert need(BF16, 261764, 32, 128, 448, 1, SILU) < dz(261764, 448) / 4
+    slots = (2 * (60000 // 256) + 2) * (1344 + 1) * 448 * 4      # of chunks of 256 rows, the shortest
+    assert dz(60000, 448) <= need(BF16, 60000, 32, 1344, 448, 1, SILU) <= dz(60000, 448) + slots
+    assert dz(60000, 448) <= need(F32, 60000, 32, 128, 448, 1, SILU) <= dz(60000, 448) + slots
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
