@@ -189,3 +189,19 @@ def test_join_gradients(cg, n, k, N, pad, dtype):
     rows = slice(0, n, max(1, n // 500))
     terms = y.reshape(n, k, N)[rows].double() * d[rows].double()[:, None, :]
     assert ((dw[rows].double() - terms.sum(2)).abs() <= 2.0 ** -23 * (N + 2) * terms.abs().sum(2) + ref.TINY).all()
+
+
+@pytest.mark.parametrize("t,per,G,K,N", [(20000, 1, 3, 200, 24), (9000, 3, 2, 150, 32), (30000, 1, 3, 300, 8), (20000, 1, 2, 400, 5),
+                                         (40000, 1, 4, 72, 30), (30000, 1, 3, 200, 60)])
+@pytest.mark.parametrize("act,pad,kind", [("silu", 0, "even"), ("gelu", 3, "holes")])
+def test_bf16_gradients_of_narrow_outputs(cg, t, per, G, K, N, act, pad, kind):
+    """Column tiles of 32 and 64 of the weights' gradients, from dz that is held in parts and that is formed."""
+    import torch
+
+    rng = np.random.default_rng(t + K)
+    x, w, ids, z, dy = draw_grad(rng, t, per, G, K, N, kind, "bf16")
+    o = cg.group_rows(dev(ids), G)
+    a = (strided(dev(x, "bf16"), pad), dev(w, "bf16"), strided(dev(dy, "bf16"), pad), *o)
+    got = cg.grouped_layer_grad(*a, z=strided(dev(z, "bf16"), pad), activation=act, per_row=per)
+    for g, v, name in zip(got, grad_of_parts(x, w, z, dy, ids, act, per), NAMES):
+        check(g, v, name)
