@@ -48,7 +48,7 @@ enum Dz { kNoDz, kFormDz, kHeldDz };
 // and z as they are loaded. That takes registers for both and for their parts, so that there all waves stage both
 // operands, 8 bytes of eight rows a thread, a row's slopes at a time.
 template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW, bool LAYER, Dz DZ_>
-__global__ __launch_bounds__(kThreads, DZ_ != kNoDz ? 3 : 1) void k_row_outer(RowOrder o, RowOuter q, ChunkRows R, bool big,
+__global__ __launch_bounds__(kThreads, DZ_ == kNoDz ? 1 : DZ_ == kFormDz ? 3 : 4) void k_row_outer(RowOrder o, RowOuter q, ChunkRows R, bool big,
                                                         float *slots)
 {
     constexpr bool DZ = DZ_ == kFormDz, HELD = DZ_ == kHeldDz;
@@ -474,8 +474,9 @@ int chunk_rows(size_t es, int64_t n, int G, const Shape &s)
 }
 
 // dz in parts: 64 columns, whose sums leave registers for both. Us with 128 of them and 64: formed, 261,764 rows, 128 x 448,
-// 230 (two workgroups on a compute unit) and 229; held, 60,000 rows, 1344 x 448, 304 and 302, 20,000 of 100 groups, 128 x
-// 128, 25 and 22, 6,000 of 20, 1344 x 448, 64 and 56.
+// 230 (two workgroups on a compute unit) and 229, 20,000 of 100 groups, 128 x 128, 25 and 22; held, 60,000, 1344 x 448, 304
+// and 302, 6,000 of 20 groups 64 and 56. With three and four workgroups on a compute unit: the first 217 and 247, the third
+// 300 and 286.
 Shape shape(size_t es, int64_t n, int G, int A, int B, bool parts)
 {
     Shape s;
@@ -483,7 +484,7 @@ Shape shape(size_t es, int64_t n, int G, int A, int B, bool parts)
     s.bn = B > 64 ? (parts ? 64 : 128) : B > 32 ? 64 : 32;
     if (s.bm == 64) s.bn = 64;
     const bool large = s.bm == 128 && s.bn >= 64;
-    s.per_cu = es == 4 ? (large ? 2 : 3) : large && (parts || s.bn == 128) ? 3 : 4;
+    s.per_cu = es == 4 ? (large ? 2 : 3) : large && (s.bn == 128 || (parts && A <= 128)) ? 3 : 4;  // formed up to 128
     s.tiles = (int64_t)((A + s.bm - 1) / s.bm) * ((B + s.bn - 1) / s.bn);
     s.rows = n > 0 ? chunk_rows(es, n, G, s) : kMinRows;
     return s;
