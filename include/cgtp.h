@@ -387,8 +387,9 @@ int cgtp_plan_set_receiver_order(cgtp_plan plan, int64_t n_nodes, const int32_t 
  *    rounds each addition of 16 terms down (1.6e-7 of 20,000 terms of one sign, less of others).
  *    Products of fp32 operands leave out less than 2^-24 of a term; infinities, NaN and values of any
  *    magnitude are treated as fp32 arithmetic does. What is not finite in one group reaches no row of
- *    another. Results that are not finite, of fp32 and of adapters, and fp32 ones whose sums pass
- *    2^96, are formed a second time, one by one: correct, but slow.
+ *    another. Results that are not finite, of fp32, of adapters and of the gradients of bf16 layers with
+ *    an activation, and fp32 ones whose sums pass 2^96, are formed a second time, one by one: correct,
+ *    but slow.
  *  - x, y, dx, dy are rows: element (i, c) at [i * stride + c], stride >= width. Other tensors are
  *    contiguous. Any width, stride and alignment of the element works; widths and strides that
  *    are multiples of 64 bytes with pointers on 64-byte boundaries are the fastest, of 16 the next.
@@ -478,7 +479,8 @@ int cgtp_adapter_linear_grad(int dtype, int64_t n_rows, int n_groups, int n_in, 
  *           -1 where no expert is left. Keys are compared as the formula gives them in 64 bits; without a bias
  *           by the logits, whose order theirs is.
  *   weights [n_rows][top_k] fp32: scale s, or scale s / (sum of the row's chosen s) where renormalize is 1; 0 beside
- *           -1. Softmax scores of a row that holds NaN or +inf are NaN.
+ *           -1. A softmax row that holds NaN or +inf has NaN for all its weights, and with +inf, where the keys are
+ *           scores, no expert; NaN alone leaves its choice among the others as it is.
  * 1 <= top_k <= CGTP_MAX_TOP_K, and no more than the experts left; n_rows top_k < 2^31; n_experts <= CGTP_MAX_GROUPS.
  * Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
 #define CGTP_MAX_TOP_K 64
@@ -496,8 +498,8 @@ int cgtp_route_rows(int dtype, int64_t n_rows, int n_experts, int top_k, const v
  *   softmax, renormalised: dl_e = scale p_e (u_e - sum_i u_i p_i), p = s / sum of the chosen s; 0 if not chosen;
  *   sigmoid:               dl_e = scale s_e (1 - s_e) u_e;
  *   sigmoid, renormalised: dl_e = scale p_e (1 - s_e) (u_e - sum_i u_i p_i).
- * An id outside [0, n_experts), or of an expert that is not available, has no part in it. Errors: CGTP_ERR_ARG,
- * CGTP_ERR_HIP. */
+ * An id outside [0, n_experts), or of an expert that is not available, has no part in it, and renormalised gradients
+ * read the logits of the chosen alone. Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
 int cgtp_route_rows_grad(int dtype, int64_t n_rows, int n_experts, int top_k, const void *logits,
                          int64_t logits_stride, const int32_t *ids, const float *dweights,
                          int score, int renormalize, float scale, void *dlogits,
@@ -510,7 +512,8 @@ int cgtp_route_rows_grad(int dtype, int64_t n_rows, int n_experts, int top_k, co
  *   residual [n_rows][n_out] or NULL (0), y [n_rows][n_out], z [n_rows][n_out] or NULL (not kept).
  *   activation  CGTP_ACT_NONE: z; CGTP_ACT_SILU: z / (1 + exp(-z)); CGTP_ACT_GELU: z P(z), P the normal
  *           distribution function; CGTP_ACT_RELU: max(z, 0), NaN where z is.
- * Everything after the product is fp32 and rounded once: the activation takes z before it is rounded. n_rows is a
+ * Everything after the product is fp32 and rounded once: the activation takes z before it is rounded. gelu of CGTP_BF16
+ * takes P from a polynomial, off by 2^-14.9 of its tail, under a hundredth of what the result's rounding may be. n_rows is a
  * multiple of per_row, 1 <= per_row <= CGTP_MAX_PER_ROW. Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
 #define CGTP_MAX_PER_ROW 64
 #define CGTP_ACT_NONE 0

@@ -40,7 +40,7 @@ __device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(-
 // |z| = 8 is 2^-15, under a fiftieth of bf16's rounding; past it the tail is below 2^-50, and falls on to zero. Of fp32
 // ones it is exp(-z^2 / 2) t times a polynomial in t = 1 / (1 + |z| / 4): 2^-25 for all z, 8 2^-24 as fp32 evaluates it.
 // Linear programs chose the coefficients for the smallest relative error. Seven products and one exponential, or eleven,
-// one and a reciprocal: 525,308 rows, 64 to 64, fp32, 118 us with erfc where silu takes 79.
+// one and a reciprocal: 525,308 rows, 64 to 64, z, fp32, 90 us where erfc takes 118.
 template <typename T> __device__ __forceinline__ float normal_cdf(float z)
 {
     const float a = fabsf(z);

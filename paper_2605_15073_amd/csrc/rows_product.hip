@@ -24,6 +24,9 @@
 // adapter's second matrix: 131,327 rows of 8 adapters, 896 -> 128, rank 16, fp32 290 us, bf16 86; 100,000 rows of 100,
 // fp32 265 where the two products apart take 298, bf16 71 and 105.
 //
+// Row gradients of bf16 layers with an activation (Z) have two parts of each row in LDS, which meet the same columns: 261,764
+// rows, 128 -> 448, dx in fp32, dz formed in here, 160 us; bound by memory (470 MB read, 134 written, partly in the caches).
+//
 // Layers and their row gradients (EX) have no adapters: a step all of whose k exist loads from pointers that move along and
 // stages without a condition, and the workgroups of a tile's columns follow each other on one XCD, so that its rows come
 // from one L2. Us without both and now: 60,000 rows of 32 groups, 1344 -> 448, bf16 y 152 and 125, dx 161 and 115; fp32
@@ -61,7 +64,7 @@ __device__ __forceinline__ void store_traded(bf16_t *row, int col, int N, float4
 }
 
 // Waves of a SIMD that bf16 registers have to leave room for: a gradient from 448 columns, 262,144 rows, 83 us with three
-// and 87 with two.
+// and 87 with two. With dz in parts two: three spill (60,000 rows, 1344 -> 448, 240 and 369).
 template <Extra EX> constexpr int kLeanWaves = EX == kBare ? 1 : kForms<EX> ? 2 : 3;
 
 template <typename T, bool WNK, int BM, int BN, int WR, bool WIDE, bool FUSED, Extra EX>

@@ -558,7 +558,8 @@ template <typename T, int L, int PER, bool KEYS> hipError_t route(const RowRoute
 }
 
 // Sixteen logits a lane, eight keys: us with eight and sixteen, bf16, 525,308 rows of 64, 4 of them, by the logits 32
-// and 27, by a bias 51 and 54, in blocks 71 and 112 (more rows of a wave share the 64-bit choice of one).
+// and 27, by a bias 51 and 54, in blocks 71 and 112 (more rows of a wave share the 64-bit choice of one); with eight these two
+// take 49 and 66 by now.
 template <typename T, int L> hipError_t route(const RowRoute &p, hipStream_t s)
 {
     if (p.bias || p.blocks > 1) return route<T, L, 8, true>(p, s);
