@@ -512,9 +512,9 @@ int cgtp_route_rows_grad(int dtype, int64_t n_rows, int n_experts, int top_k, co
  *   residual [n_rows][n_out] or NULL (0), y [n_rows][n_out], z [n_rows][n_out] or NULL (not kept).
  *   activation  CGTP_ACT_NONE: z; CGTP_ACT_SILU: z / (1 + exp(-z)); CGTP_ACT_GELU: z P(z), P the normal
  *           distribution function; CGTP_ACT_RELU: max(z, 0), NaN where z is.
- * Everything after the product is fp32 and rounded once: the activation takes z before it is rounded. gelu of CGTP_BF16
- * takes P from a polynomial, off by 2^-14.9 of its tail, under a hundredth of what the result's rounding may be. n_rows is a
- * multiple of per_row, 1 <= per_row <= CGTP_MAX_PER_ROW. Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
+ * Everything after the product is fp32 and rounded once: the activation takes z before it is rounded. gelu of
+ * CGTP_BF16 takes P from a polynomial, off by 2^-14.9 of its tail, under a fiftieth of the result's rounding. n_rows
+ * is a multiple of per_row, 1 <= per_row <= CGTP_MAX_PER_ROW. Errors: CGTP_ERR_ARG, CGTP_ERR_HIP. */
 #define CGTP_MAX_PER_ROW 64
 #define CGTP_ACT_NONE 0
 #define CGTP_ACT_SILU 1
