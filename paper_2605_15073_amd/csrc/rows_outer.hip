@@ -47,8 +47,8 @@ enum Dz { kNoDz, kFormDz, kHeldDz };
 // in two bf16 parts (rows_layer.h), which meet the same a: kHeldDz, as they lie, like a narrow product's; kFormDz, from dy
 // and z as they are loaded. That takes registers for both and for their parts, so that there all waves stage both
 // operands, 8 bytes of eight rows a thread, a row's slopes at a time: 261,764 rows, 128 x 448, 200 us and the join's 17. Waves
-// wait three fifths of their time: for loads (470 MB of dy and z) and each other, vector ALU and matrix cores are busy a
-// third of it. Columns summed from the parts behind the slopes, not between them: 262,144 rows, 64 x 448, 145 and 200.
+// wait three fifths of their time: for loads (470 MB of dy and z) and each other; the vector ALU is busy for half of it, the
+// matrix cores for a seventh. Columns summed from the parts behind the slopes, not between them: 262,144 rows, 64 x 448, 145 and 200.
 template <typename T, int BM, int BN, int WR, bool WIDE, bool NARROW, bool LAYER, Dz DZ_>
 __global__ __launch_bounds__(kThreads, DZ_ == kNoDz ? 1 : DZ_ == kFormDz ? 3 : 4) void k_row_outer(RowOrder o, RowOuter q, ChunkRows R, bool big,
                                                         float *slots)
